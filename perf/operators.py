@@ -168,7 +168,7 @@ def prepare(case, seed):
         elif c["kind"] == "rec":
             s["bufs"] = wm.LinrecBuffers(c["T"], c["B"], c["H"], dt, grad=c["grad"])
         else:
-            s["bufs"] = wm.ClipBuffers(s["x"]["grads"])
+            s["bufs"] = wm.ClipPlan(s["x"]["grads"], s["views"])
     return s
 
 
@@ -201,7 +201,7 @@ def run(s):
             wm.linrec_grad(x["x"], x["gate"], x["dy"], dh_T=x["dh_T"], resets=x["resets"], lengths=x["lengths"], bufs=b)
             r.update(dx=b.dx, dgate=b.dgate, dh0=b.dh0)
         return r
-    wm.clip_grads(x["grads"], x["max_norm"], outs=s["views"], bufs=b)
+    wm.clip_grads(b, x["max_norm"])
     return dict(norm=b.norm, fp32=s["flats"][torch.float32], bf16=s["flats"][torch.bfloat16])
 
 
