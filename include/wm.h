@@ -346,12 +346,154 @@ wm_status wm_adam_step(int64_t n, float *params, const float *grads, float *m, f
 float wm_poly_lr(int32_t epoch, float lr0, float lr_end, int32_t epochs);
 
 /*
+ * Sequence-core operators.  A recurrent core whose steps depend on each other
+ * only through a linear recurrence trains in parallel over logged sequences;
+ * besides its matrix products it consists of the operators below, and its
+ * training step ends in wm_clip_grads and wm_adam_step.  They take what the
+ * library logs: int32 actions with the codes -1 and -2 for "no action" (as a
+ * zero one-hot), time-major arrays, and per-row lengths with zero padding as
+ * in section 3.3.1.
+ *   - `dtype` (wm_dtype) is the type of the activations: WM_FP32 floats, or
+ *     WM_BF16 values, computed on in fp32 and rounded once, to nearest even.
+ *     Parameters' gradients, statistics and states are float32.
+ *   - Arrays are aligned to their element (float32 to 4 bytes, bf16 to 2).
+ *     A leading dimension (`_ld`) is the distance between rows in elements,
+ *     at least the row's width; output rows must not overlap.
+ *   - Every sum has a fixed order: a call's result does not depend on
+ *     scheduling.
+ *   - A workspace is 256-byte aligned; its size comes from the function named
+ *     ..._workspace_bytes with the call's sizes, 0 on sizes that the call
+ *     refuses.
+ */
+
+/*
+ * Rows of a table for n actions, scaled: out[i] = scale * table[tokens[i]],
+ * and 0 where tokens[i] is outside [0, V).
+ *   tokens [n] int32; table [V, H] and out [n, H] in dtype.
+ * H at most 65536.  n = 0 is a no-op.
+ */
+wm_status wm_embed(int32_t dtype, int64_t n, int32_t V, int32_t H, const int32_t *tokens,
+                   const void *table, float scale, void *out, int64_t out_ld, wm_stream_t stream);
+
+/*
+ * Gradient of wm_embed with respect to the table, written whole (rows that no
+ * token names become 0):
+ *   grad_table[v] = scale * sum over the i with tokens[i] = v of grad_out[i].
+ *   grad_out [n, H] in dtype; grad_table [V, H] float32.
+ * n at most 2^30.  n = 0 writes zeros.
+ */
+size_t wm_embed_grad_workspace_bytes(int64_t n, int32_t V, int32_t H);
+wm_status wm_embed_grad(int32_t dtype, int64_t n, int32_t V, int32_t H, const int32_t *tokens,
+                        const void *grad_out, int64_t grad_out_ld, float scale, float *grad_table,
+                        void *workspace, size_t workspace_bytes, wm_stream_t stream);
+
+/*
+ * Layer norm of each row x of width H (1 .. 8192):
+ *   mean = sum x / H, rstd = (sum (x - mean)^2 / H + eps)^(-1/2),
+ *   y = (x - mean) rstd gamma + beta.
+ *   x, y [rows, H] in dtype; gamma, beta [H] float32, nullable (1 and 0);
+ *   mean, rstd [rows] float32, both or neither (what the gradient reads).
+ * eps >= 0 and finite.  rows = 0 is a no-op.
+ */
+wm_status wm_layer_norm(int32_t dtype, int64_t rows, int32_t H, const void *x, int64_t x_ld,
+                        const float *gamma, const float *beta, float eps, void *y, int64_t y_ld,
+                        float *mean, float *rstd, wm_stream_t stream);
+
+/*
+ * Gradient of wm_layer_norm from its input and statistics.  With
+ * xh = (x - mean) rstd and q = grad_y gamma:
+ *   grad_x = rstd (q - sum q / H - xh sum(q xh) / H);
+ *   grad_gamma = sum over rows of grad_y xh; grad_beta = sum of grad_y
+ *   ([H] float32, nullable, written whole; rows = 0 writes zeros).
+ */
+size_t wm_layer_norm_grad_workspace_bytes(int64_t rows, int32_t H);
+wm_status wm_layer_norm_grad(int32_t dtype, int64_t rows, int32_t H, const void *x, int64_t x_ld,
+                             const void *grad_y, int64_t grad_y_ld, const float *gamma,
+                             const float *mean, const float *rstd, void *grad_x,
+                             int64_t grad_x_ld, float *grad_gamma, float *grad_beta,
+                             void *workspace, size_t workspace_bytes, wm_stream_t stream);
+
+/*
+ * Gated linear recurrence over B sequences of T steps, every one of the H
+ * channels for itself:
+ *   a_t = sigmoid(gate_t);  h_t = a_t h_{t-1} + (1 - a_t) x_t;  y_t = h_t.
+ * A step with resets[t, b] != 0 starts a new trajectory: it takes
+ * h_{t-1} = 0, whatever the state holds (NaN and infinities too).  A step
+ * t >= lengths[b] is padding: y_t = 0, the state stays, and neither x, gate
+ * nor resets of it enter any result.
+ *   x, gate [T, B, H] in dtype, unit stride along H, element strides x_t and
+ *   x_b (gate_t, gate_b) of steps and rows: the halves of one projection's
+ *   rows, for example.
+ *   h0 [B, H] float32, nullable (0); resets [T, B] uint8, nullable (none);
+ *   lengths [B] int32, nullable (T; values outside [0, T] act as clamped).
+ *   y [T, B, H] in dtype; h_T [B, H] float32, nullable, may be h0: the state
+ *   after the last step (T = 1 with h0 and h_T is the form for acting).
+ *   states               nullable: a 256-byte aligned buffer of
+ *                        wm_linrec_states_bytes that receives what
+ *                        wm_linrec_grad needs.
+ *   workspace            of wm_linrec_workspace_bytes, also for the gradient.
+ * T B at most 2^31 - 1, B H at most 2^31 - 1.  B = 0 is a no-op; T = 0 gives
+ * h_T = h0.
+ */
+size_t wm_linrec_states_bytes(int32_t T, int32_t B, int32_t H);
+size_t wm_linrec_workspace_bytes(int32_t T, int32_t B, int32_t H);
+wm_status wm_linrec(int32_t dtype, int32_t T, int32_t B, int32_t H, const void *x, int64_t x_t,
+                    int64_t x_b, const void *gate, int64_t gate_t, int64_t gate_b,
+                    const float *h0, const uint8_t *resets, const int32_t *lengths, void *y,
+                    float *h_T, void *states, size_t states_bytes, void *workspace,
+                    size_t workspace_bytes, wm_stream_t stream);
+
+/*
+ * Gradient of wm_linrec by the reverse recurrence, from its inputs and the
+ * states that it saved.  With R_T-1 = grad_h_T and, for a step inside its
+ * sequence, D_t = grad_y_t + R_t:
+ *   grad_x_t = (1 - a_t) D_t,  grad_gate_t = a_t (1 - a_t) (h_{t-1} - x_t) D_t,
+ *   R_{t-1} = a_t D_t, or 0 at a reset;  grad_h0 = R_{-1}.
+ * Padded steps get grad_x = grad_gate = 0 and pass R on.
+ *   grad_y, grad_x, grad_gate as x (dtype, strides); grad_h_T [B, H] float32,
+ *   nullable (0); grad_h0 [B, H] float32, nullable, may be grad_h_T.
+ */
+wm_status wm_linrec_grad(int32_t dtype, int32_t T, int32_t B, int32_t H, const void *x,
+                         int64_t x_t, int64_t x_b, const void *gate, int64_t gate_t,
+                         int64_t gate_b, const uint8_t *resets, const int32_t *lengths,
+                         const void *grad_y, int64_t grad_y_t, int64_t grad_y_b,
+                         const float *grad_h_T, const void *states, size_t states_bytes,
+                         void *grad_x, int64_t grad_x_t, int64_t grad_x_b, void *grad_gate,
+                         int64_t grad_gate_t, int64_t grad_gate_b, float *grad_h0,
+                         void *workspace, size_t workspace_bytes, wm_stream_t stream);
+
+/*
+ * The global norm of n gradient tensors (one list, types may differ) and the
+ * tensors clipped to it:
+ *   norm = sqrt(sum over all tensors of sum g^2), summed in 64 bits;
+ *   out = g * (max_norm / norm) where norm > max_norm, else out = g.
+ * Where the norm is NaN or infinite (a gradient holds one), out = g: the
+ * caller sees it in `norm`.
+ *   tensors [n]          HOST array, read before the call returns: contiguous
+ *                        device arrays of `n` values each; `out` in the same
+ *                        type, may be `grad` itself, and overlaps no other.
+ *   norm [1]             float32.
+ * max_norm >= 0 and finite.
+ */
+typedef struct {
+  const void *grad;
+  void *out;
+  int64_t n;
+  int32_t dtype; /* wm_dtype */
+} wm_grad_tensor;
+
+size_t wm_clip_grads_workspace_bytes(int32_t n, const wm_grad_tensor *tensors);
+wm_status wm_clip_grads(int32_t n, const wm_grad_tensor *tensors, float max_norm, float *norm,
+                        void *workspace, size_t workspace_bytes, wm_stream_t stream);
+
+/*
  * Measurement aid (no counterpart in the paper).  While a prefix is set, every
  * kernel launch of the library whose name starts with it is bracketed by HIP
  * events on its stream.  Kernel names: "ctrl", "gates", "mdn" (each followed by
  * "/" and the tile that the call's sizes picked, as "gates/64x32"), "lh", "init",
- * "finish", "nll_init", "nll_reduce", "nll_means", "pack", "returns", "adam", and the
- * "grad_" kernels of wm_nll_grad; "" selects all,
+ * "finish", "nll_init", "nll_reduce", "nll_means", "pack", "returns", "adam", the
+ * "grad_" kernels of wm_nll_grad, and "embed", "norm", "linrec" and "clip" with
+ * what follows these words in the sequence-core operators; "" selects all,
  * NULL turns timing off.  wm_profile_read waits for the recorded events and
  * returns the summed duration (ms) and count of the launches whose name
  * starts with `prefix` (NULL = all); wm_profile_reset forgets them.  Timing

@@ -28,6 +28,10 @@ _DTYPES = {"fp32": WM_FP32, "bf16": WM_BF16}
 # Every symbol the C header declares.
 EXPORTS = ("wm_packed_weights_bytes", "wm_pack_weights", "wm_workspace_bytes", "wm_controller_step",
            "wm_rollout", "wm_rollout_noalloc", "wm_nll", "wm_nll_grad", "wm_returns", "wm_adam_step", "wm_poly_lr",
+           "wm_embed", "wm_embed_grad_workspace_bytes", "wm_embed_grad", "wm_layer_norm",
+           "wm_layer_norm_grad_workspace_bytes", "wm_layer_norm_grad", "wm_linrec_states_bytes",
+           "wm_linrec_workspace_bytes", "wm_linrec", "wm_linrec_grad", "wm_clip_grads_workspace_bytes",
+           "wm_clip_grads",
            "wm_profile_enable", "wm_profile_read", "wm_profile_reset", "wm_profile_phases",
            "wm_profile_phases_read", "wm_workspace_status",
            "wm_last_error", "wm_version")
@@ -48,6 +52,11 @@ class CDims(ctypes.Structure):
 class CWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("W_g", "b_g", "W_m", "b_m", "w_r", "b_r", "w_d", "b_d", "W_c", "b_c")]
+
+
+class CGradTensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -89,6 +98,30 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.wm_adam_step.restype = I32
     lib.wm_poly_lr.argtypes = [I32, F32, F32, I32]
     lib.wm_poly_lr.restype = F32
+    I64, pg = ctypes.c_int64, ctypes.POINTER(CGradTensor)
+    lib.wm_embed.argtypes = [I32, I64, I32, I32, P, P, F32, P, I64, P]
+    lib.wm_embed.restype = I32
+    lib.wm_embed_grad_workspace_bytes.argtypes = [I64, I32, I32]
+    lib.wm_embed_grad_workspace_bytes.restype = SZ
+    lib.wm_embed_grad.argtypes = [I32, I64, I32, I32, P, P, I64, F32, P, P, SZ, P]
+    lib.wm_embed_grad.restype = I32
+    lib.wm_layer_norm.argtypes = [I32, I64, I32, P, I64, P, P, F32, P, I64, P, P, P]
+    lib.wm_layer_norm.restype = I32
+    lib.wm_layer_norm_grad_workspace_bytes.argtypes = [I64, I32]
+    lib.wm_layer_norm_grad_workspace_bytes.restype = SZ
+    lib.wm_layer_norm_grad.argtypes = [I32, I64, I32, P, I64, P, I64, P, P, P, P, I64, P, P, P, SZ, P]
+    lib.wm_layer_norm_grad.restype = I32
+    for f in (lib.wm_linrec_states_bytes, lib.wm_linrec_workspace_bytes):
+        f.argtypes, f.restype = [I32, I32, I32], SZ
+    lib.wm_linrec.argtypes = [I32, I32, I32, I32, P, I64, I64, P, I64, I64, P, P, P, P, P, P, SZ, P, SZ, P]
+    lib.wm_linrec.restype = I32
+    lib.wm_linrec_grad.argtypes = [I32, I32, I32, I32, P, I64, I64, P, I64, I64, P, P, P, I64, I64, P, P, SZ,
+                                   P, I64, I64, P, I64, I64, P, P, SZ, P]
+    lib.wm_linrec_grad.restype = I32
+    lib.wm_clip_grads_workspace_bytes.argtypes = [I32, pg]
+    lib.wm_clip_grads_workspace_bytes.restype = SZ
+    lib.wm_clip_grads.argtypes = [I32, pg, F32, P, P, SZ, P]
+    lib.wm_clip_grads.restype = I32
     lib.wm_profile_enable.argtypes = [ctypes.c_char_p]
     lib.wm_profile_enable.restype = I32
     lib.wm_profile_read.argtypes = [ctypes.c_char_p, ctypes.POINTER(ctypes.c_double),
@@ -456,6 +489,270 @@ def adam_step(params, grads, m, v, step: int, lr: float, beta1: float = 0.9, bet
 
 def poly_lr(epoch: int, lr0: float, lr_end: float, epochs: int = 5000) -> float:
     return float(load().wm_poly_lr(epoch, lr0, lr_end, epochs))
+
+
+# ---------------------------------------------------------------------------
+# sequence-core operators (activations in float32 or bfloat16)
+# ---------------------------------------------------------------------------
+
+_ACT = {torch.float32: WM_FP32, torch.bfloat16: WM_BF16}
+
+
+def _act(name, t, dtype=None):
+    """The wm_dtype of an activation tensor; ``dtype`` (a torch type) must match."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype not in _ACT or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype or 'float32 or bfloat16'}")
+    return _ACT[t.dtype]
+
+
+def _rows(name, t, H, dtype, device):
+    """(rows, distance between rows) of a [..., H] tensor with unit stride
+    along H whose leading dimensions step evenly."""
+    _act(name, t, dtype)
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.dim() < 1 or t.shape[-1] != H:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [..., {H}]")
+    if t.dim() != 2:
+        if t.numel() == 0:
+            return t.numel() // max(H, 1), H
+        try:
+            t = t.view(-1, H)
+        except RuntimeError:
+            raise ValueError(f"{name}'s rows are not evenly spaced (strides {t.stride()})") from None
+    n = t.shape[0]
+    if H > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have unit stride along its last dimension")
+    ld = t.stride(0) if n > 1 else H
+    if n > 1 and ld < H:
+        raise ValueError(f"{name}'s rows overlap (stride {ld}, width {H})")
+    return n, ld
+
+
+def embed(table, tokens, scale: float = 1.0, out=None):
+    """Launch wm_embed on the current stream: rows of ``table`` [V, H] for
+    int32 ``tokens`` of any shape, times ``scale`` (zero rows for tokens
+    outside [0, V)).  Returns ``out``, tokens.shape + (H,) in the table's type."""
+    dt = _act("table", table)
+    dev = table.device
+    V, H = table.shape
+    _need("table", table, table.dtype, (V, H))
+    _need("tokens", tokens, torch.int32, tokens.shape, dev)
+    n = tokens.numel()
+    if out is None:
+        out = torch.empty((*tokens.shape, H), dtype=table.dtype, device=dev)
+    rows, ld = _rows("out", out, H, table.dtype, dev)
+    if rows != n:
+        raise ValueError(f"out has {rows} rows for {n} tokens")
+    _check(load().wm_embed(dt, n, V, H, tokens.data_ptr(), table.data_ptr(), scale, out.data_ptr(), ld, _stream()))
+    return out
+
+
+class EmbedGradBuffers:
+    """The table's gradient [V, H] float32 and the workspace of wm_embed_grad
+    for up to n tokens."""
+
+    def __init__(self, n: int, V: int, H: int, device="cuda"):
+        self.n, self.V, self.H = n, V, H
+        self.grad = torch.empty((V, H), dtype=torch.float32, device=device)
+        self.ws_bytes = load().wm_embed_grad_workspace_bytes(n, V, H)
+        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=device)
+
+
+def embed_grad(tokens, dout, V: int, scale: float = 1.0, bufs: EmbedGradBuffers | None = None) -> EmbedGradBuffers:
+    """Launch wm_embed_grad on the current stream: the gradient of embed with
+    respect to its table, from ``dout`` (tokens.shape + (H,))."""
+    dt = _act("dout", dout)
+    dev, H, n = dout.device, dout.shape[-1], tokens.numel()
+    _need("tokens", tokens, torch.int32, tokens.shape, dev)
+    rows, ld = _rows("dout", dout, H, dout.dtype, dev)
+    if rows != n:
+        raise ValueError(f"dout has {rows} rows for {n} tokens")
+    if bufs is None:
+        bufs = EmbedGradBuffers(n, V, H, dev)
+    if (bufs.V, bufs.H) != (V, H) or bufs.grad.device != dev:
+        raise ValueError(f"buffers for V={bufs.V} H={bufs.H} on {bufs.grad.device}; the call has V={V} H={H} on {dev}")
+    _check(load().wm_embed_grad(dt, n, V, H, tokens.data_ptr(), dout.data_ptr(), ld, scale, bufs.grad.data_ptr(),
+                                bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
+    return bufs
+
+
+class LayerNormBuffers:
+    """Output and statistics of layer norm over ``rows`` rows of width H, and
+    with ``grad`` its gradients and workspace."""
+
+    def __init__(self, rows: int, H: int, dtype=torch.float32, device="cuda", grad: bool = True):
+        self.rows, self.H, self.dtype = rows, H, dtype
+        self.y = torch.empty((rows, H), dtype=dtype, device=device)
+        self.mean = torch.empty(rows, dtype=torch.float32, device=device) if grad else None
+        self.rstd = torch.empty(rows, dtype=torch.float32, device=device) if grad else None
+        self.dx = torch.empty((rows, H), dtype=dtype, device=device) if grad else None
+        self.dgamma = torch.empty(H, dtype=torch.float32, device=device) if grad else None
+        self.dbeta = torch.empty(H, dtype=torch.float32, device=device) if grad else None
+        self.ws_bytes = load().wm_layer_norm_grad_workspace_bytes(rows, H) if grad else 0
+        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=device) if grad else None
+
+
+def _norm_bufs(x, bufs, rows, H):
+    if (bufs.rows, bufs.H, bufs.dtype) != (rows, H, x.dtype) or bufs.y.device != x.device:
+        raise ValueError(f"buffers for rows={bufs.rows} H={bufs.H} {bufs.dtype} on {bufs.y.device}; the call has "
+                         f"rows={rows} H={H} {x.dtype} on {x.device}")
+
+
+def layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, bufs: LayerNormBuffers | None = None) -> LayerNormBuffers:
+    """Launch wm_layer_norm on the current stream over the rows of ``x``
+    [..., H] (gamma, beta [H] float32 or None); returns the filled buffers."""
+    dt = _act("x", x)
+    dev, H = x.device, x.shape[-1]
+    rows, ld = _rows("x", x, H, x.dtype, dev)
+    _need("gamma", gamma, torch.float32, (H,), dev, optional=True)
+    _need("beta", beta, torch.float32, (H,), dev, optional=True)
+    if bufs is None:
+        bufs = LayerNormBuffers(rows, H, x.dtype, dev)
+    _norm_bufs(x, bufs, rows, H)
+    _check(load().wm_layer_norm(dt, rows, H, x.data_ptr(), ld, _ptr(gamma), _ptr(beta), eps, bufs.y.data_ptr(), H,
+                                _ptr(bufs.mean), _ptr(bufs.rstd), _stream()))
+    return bufs
+
+
+def layer_norm_grad(x, dy, gamma=None, bufs: LayerNormBuffers | None = None) -> LayerNormBuffers:
+    """Launch wm_layer_norm_grad on the current stream: dx, dgamma and dbeta
+    from the forward call's input and the statistics in its ``bufs``."""
+    dt = _act("x", x)
+    dev, H = x.device, x.shape[-1]
+    rows, ld = _rows("x", x, H, x.dtype, dev)
+    nd, dld = _rows("dy", dy, H, x.dtype, dev)
+    _need("gamma", gamma, torch.float32, (H,), dev, optional=True)
+    if bufs is None or bufs.dx is None:
+        raise ValueError("layer_norm_grad needs the forward call's buffers, made with grad=True")
+    _norm_bufs(x, bufs, rows, H)
+    if nd != rows:
+        raise ValueError(f"dy has {nd} rows, x has {rows}")
+    _check(load().wm_layer_norm_grad(dt, rows, H, x.data_ptr(), ld, dy.data_ptr(), dld, _ptr(gamma),
+                                     bufs.mean.data_ptr(), bufs.rstd.data_ptr(), bufs.dx.data_ptr(), H,
+                                     bufs.dgamma.data_ptr(), bufs.dbeta.data_ptr(), bufs.workspace.data_ptr(),
+                                     bufs.ws_bytes, _stream()))
+    return bufs
+
+
+class LinrecBuffers:
+    """Output, final state and workspace of the gated linear recurrence over
+    [T, B, H]; with ``grad`` the saved states and the gradients (dx and dgate
+    are the halves of one [T, B, 2H] tensor, ``dxg``)."""
+
+    def __init__(self, T: int, B: int, H: int, dtype=torch.float32, device="cuda", grad: bool = True):
+        self.T, self.B, self.H, self.dtype = T, B, H, dtype
+        lib = load()
+        self.y = torch.empty((T, B, H), dtype=dtype, device=device)
+        self.h_T = torch.empty((B, H), dtype=torch.float32, device=device)
+        self.ws_bytes = lib.wm_linrec_workspace_bytes(T, B, H)
+        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=device)
+        self.states_bytes = lib.wm_linrec_states_bytes(T, B, H) if grad else 0
+        self.states = torch.empty(max(self.states_bytes, 1), dtype=torch.uint8, device=device) if grad else None
+        self.dxg = torch.empty((T, B, 2 * H), dtype=dtype, device=device) if grad else None
+        self.dx = self.dxg[..., :H] if grad else None
+        self.dgate = self.dxg[..., H:] if grad else None
+        self.dh0 = torch.empty((B, H), dtype=torch.float32, device=device) if grad else None
+
+
+def _seq(name, t, shape, dtype, device):
+    """Checks a [T, B, H] tensor with unit stride along H; its strides."""
+    _act(name, t, dtype)
+    if tuple(t.shape) != shape or t.device != device:
+        raise ValueError(f"{name} is {tuple(t.shape)} on {t.device}, expected {shape} on {device}")
+    st = t.stride()
+    if shape[2] > 1 and st[2] != 1:
+        raise ValueError(f"{name} must have unit stride along its last dimension")
+    return st
+
+
+def _linrec_args(x, gate, resets, lengths, bufs):
+    dt = _act("x", x)
+    if x.dim() != 3:
+        raise ValueError(f"x has shape {tuple(x.shape)}, expected [T, B, H]")
+    dev, shape = x.device, tuple(x.shape)
+    sx, sg = _seq("x", x, shape, x.dtype, dev), _seq("gate", gate, shape, x.dtype, dev)
+    _need("resets", resets, _mask_dtype(resets), shape[:2], dev, optional=True)
+    _need("lengths", lengths, torch.int32, shape[1:2], dev, optional=True)
+    if bufs is not None and ((bufs.T, bufs.B, bufs.H) != shape or bufs.dtype != x.dtype or bufs.y.device != dev):
+        raise ValueError(f"buffers for T={bufs.T} B={bufs.B} H={bufs.H} {bufs.dtype} on {bufs.y.device}; the call has "
+                         f"{shape} {x.dtype} on {dev}")
+    return dt, dev, shape, sx, sg
+
+
+def linrec(x, gate, h0=None, resets=None, lengths=None, bufs: LinrecBuffers | None = None) -> LinrecBuffers:
+    """Launch wm_linrec on the current stream: h_t = a_t h_{t-1} + (1 - a_t)
+    x_t with a = sigmoid(gate) over ``x``, ``gate`` [T, B, H] (resets [T, B]
+    uint8: the step starts a new trajectory; lengths [B] int32); returns the
+    filled buffers (y, h_T, and the states that linrec_grad reads)."""
+    dt, dev, (T, B, H), sx, sg = _linrec_args(x, gate, resets, lengths, bufs)
+    _need("h0", h0, torch.float32, (B, H), dev, optional=True)
+    if bufs is None:
+        bufs = LinrecBuffers(T, B, H, x.dtype, dev)
+    _check(load().wm_linrec(dt, T, B, H, x.data_ptr(), sx[0], sx[1], gate.data_ptr(), sg[0], sg[1], _ptr(h0),
+                            _ptr(resets), _ptr(lengths), bufs.y.data_ptr(), bufs.h_T.data_ptr(), _ptr(bufs.states),
+                            bufs.states_bytes, bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
+    return bufs
+
+
+def linrec_grad(x, gate, dy, dh_T=None, resets=None, lengths=None, bufs: LinrecBuffers | None = None) -> LinrecBuffers:
+    """Launch wm_linrec_grad on the current stream: dx, dgate and dh0 from
+    the forward call's inputs and the states in its ``bufs``."""
+    dt, dev, (T, B, H), sx, sg = _linrec_args(x, gate, resets, lengths, bufs)
+    if bufs is None or bufs.states is None:
+        raise ValueError("linrec_grad needs the forward call's buffers, made with grad=True")
+    sd = _seq("dy", dy, (T, B, H), x.dtype, dev)
+    _need("dh_T", dh_T, torch.float32, (B, H), dev, optional=True)
+    o = bufs.dx.stride()
+    _check(load().wm_linrec_grad(dt, T, B, H, x.data_ptr(), sx[0], sx[1], gate.data_ptr(), sg[0], sg[1], _ptr(resets),
+                                 _ptr(lengths), dy.data_ptr(), sd[0], sd[1], _ptr(dh_T), bufs.states.data_ptr(),
+                                 bufs.states_bytes, bufs.dx.data_ptr(), o[0], o[1], bufs.dgate.data_ptr(), o[0], o[1],
+                                 bufs.dh0.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
+    return bufs
+
+
+class ClipPlan:
+    """The gradient tensors of a training program (contiguous, float32 or
+    bfloat16), where their clipped values go (``outs``; None = in place), the
+    norm and the workspace of wm_clip_grads."""
+
+    def __init__(self, grads, outs=None):
+        self.grads = list(grads)
+        self.outs = self.grads if outs is None else list(outs)
+        if not self.grads:
+            raise ValueError("no gradient tensors")
+        if len(self.outs) != len(self.grads):
+            raise ValueError(f"{len(self.outs)} outputs for {len(self.grads)} tensors")
+        self._fill()
+        dev = self.grads[0].device
+        self.norm = torch.empty(1, dtype=torch.float32, device=dev)
+        self.ws_bytes = load().wm_clip_grads_workspace_bytes(len(self.grads), self.table)
+        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=dev)
+
+    def _fill(self):
+        dev = self.grads[0].device
+        self.ptrs = [t.data_ptr() for t in self.grads] + [t.data_ptr() for t in self.outs]
+        self.table = (CGradTensor * len(self.grads))()
+        for i, (g, o) in enumerate(zip(self.grads, self.outs)):
+            dt = _act(f"grads[{i}]", g)
+            _need(f"grads[{i}]", g, g.dtype, g.shape, dev)
+            _need(f"outs[{i}]", o, g.dtype, g.shape, dev)
+            self.table[i] = CGradTensor(g.data_ptr(), o.data_ptr(), g.numel(), dt)
+
+
+def clip_grads(plan: ClipPlan, max_norm: float):
+    """Launch wm_clip_grads on the current stream over the plan's tensors:
+    plan.norm becomes their global norm, plan.outs their values scaled to
+    max_norm where the norm is above it.  Returns plan.norm (a device tensor:
+    nothing waits)."""
+    # a tensor may have been given other memory since (its sizes stay the plan's)
+    if [t.data_ptr() for t in plan.grads] + [t.data_ptr() for t in plan.outs] != plan.ptrs:
+        plan._fill()
+    _check(load().wm_clip_grads(len(plan.table), plan.table, max_norm, plan.norm.data_ptr(), plan.workspace.data_ptr(),
+                                plan.ws_bytes, _stream()))
+    return plan.norm
 
 
 def profile_enable(prefix: str | None):

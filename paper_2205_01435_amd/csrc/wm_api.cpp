@@ -11,6 +11,7 @@
 
 #include "../../include/wm.h"
 #include "wm_kernels.h"
+#include "wm_seq.h"
 
 namespace {
 
@@ -169,6 +170,88 @@ wm_status rollout_call(const wm_dims* dims, const void* packed, int32_t B, int32
   if (e != hipSuccess) return hip_fail(e, "wm_rollout");
   if (flags & WM_FLAG_CHECK) return (st = read_status(workspace, s)) == WM_OK ? ok() : st;
   return ok();
+}
+
+
+// ---- sequence-core operators ----------------------------------------------
+
+bool aligned_el(const void* p, int32_t dtype) {
+  return (reinterpret_cast<uintptr_t>(p) & (dtype == WM_FP32 ? 3u : 1u)) == 0;
+}
+
+wm_status check_dtype(int32_t dtype) {
+  return dtype == WM_FP32 || dtype == WM_BF16 ? WM_OK : fail(WM_ERR_INVALID_ARG, "unknown dtype %d", dtype);
+}
+
+// Leading dimension of rows of width H; the array's extent stays addressable.
+wm_status check_ld(const char* name, int64_t rows, int64_t H, int64_t ld) {
+  if (ld < H) return fail(WM_ERR_INVALID_ARG, "%s_ld=%lld is below the row's width %lld", name, (long long)ld, (long long)H);
+  if (rows > 0 && ld > ((int64_t)1 << 48) / rows) return fail(WM_ERR_UNSUPPORTED, "%s: rows too far apart", name);
+  return WM_OK;
+}
+
+wm_status check_workspace(const char* what, const void* ws, size_t bytes, size_t need) {
+  if (need > 0 && (!ws || bytes < need))
+    return fail(WM_ERR_WORKSPACE, "%s needs %zu bytes, got %zu", what, need, ws ? bytes : (size_t)0);
+  if (reinterpret_cast<uintptr_t>(ws) & 255u) return fail(WM_ERR_INVALID_ARG, "%s must be 256-byte aligned", what);
+  return WM_OK;
+}
+
+wm_status check_embed(int64_t n, int32_t V, int32_t H) {
+  if (n < 0 || V <= 0 || H <= 0)
+    return fail(WM_ERR_INVALID_ARG, "n=%lld must not be negative, V=%d and H=%d must be positive", (long long)n, V, H);
+  if (n > (int64_t)1 << 30) return fail(WM_ERR_UNSUPPORTED, "n=%lld: at most 2^30 tokens", (long long)n);
+  if (H > 65536) return fail(WM_ERR_UNSUPPORTED, "H=%d: at most 65536", H);
+  return WM_OK;
+}
+
+wm_status check_norm(int64_t rows, int32_t H) {
+  if (rows < 0 || H <= 0) return fail(WM_ERR_INVALID_ARG, "rows=%lld must not be negative, H=%d must be positive", (long long)rows, H);
+  if (H > wm::kNormMaxH) return fail(WM_ERR_UNSUPPORTED, "H=%d: at most %d", H, wm::kNormMaxH);
+  if (rows > (int64_t)1 << 32) return fail(WM_ERR_UNSUPPORTED, "rows=%lld: at most 2^32", (long long)rows);
+  return WM_OK;
+}
+
+wm_status check_linrec(int32_t T, int32_t B, int32_t H) {
+  if (T < 0 || B < 0 || H <= 0)
+    return fail(WM_ERR_INVALID_ARG, "T=%d and B=%d must not be negative, H=%d must be positive", T, B, H);
+  if ((int64_t)T * B > INT32_MAX || (int64_t)B * H > INT32_MAX)
+    return fail(WM_ERR_UNSUPPORTED, "T*B and B*H must stay below 2^31 (T=%d B=%d H=%d)", T, B, H);
+  return WM_OK;
+}
+
+// A [T, B, H] array with element strides t, b and unit stride along H.  An
+// output's rows must not overlap: one of the two dimensions lies whole inside
+// the other's stride.
+wm_status check_view(const char* name, int32_t dtype, const void* p, int64_t t, int64_t b, int32_t T, int32_t B,
+                     int32_t H, bool output) {
+  if (T == 0 || B == 0) return WM_OK;
+  if (!p) return fail(WM_ERR_INVALID_ARG, "%s is required", name);
+  if (!aligned_el(p, dtype)) return fail(WM_ERR_INVALID_ARG, "%s is not aligned to its element", name);
+  const int64_t lim = (int64_t)1 << 48;
+  if (t < 0 || b < 0) return fail(WM_ERR_INVALID_ARG, "%s: strides must not be negative", name);
+  if ((T > 1 && t > lim / T) || (B > 1 && b > lim / B))
+    return fail(WM_ERR_UNSUPPORTED, "%s: rows too far apart", name);
+  if (output) {
+    const bool rows_inside = (B == 1 || b >= H) && (T == 1 || t >= (B - 1) * (B > 1 ? b : 0) + H);
+    const bool steps_inside = (T == 1 || t >= H) && (B == 1 || b >= (T - 1) * (T > 1 ? t : 0) + H);
+    if (!rows_inside && !steps_inside) return fail(WM_ERR_INVALID_ARG, "%s: output rows overlap", name);
+  }
+  return WM_OK;
+}
+
+wm_status check_grads(int32_t n, const wm_grad_tensor* t) {
+  if (n < 0) return fail(WM_ERR_INVALID_ARG, "n=%d must not be negative", n);
+  if (n > 0 && !t) return fail(WM_ERR_INVALID_ARG, "tensors is NULL");
+  int64_t total = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    if (t[i].n < 0) return fail(WM_ERR_INVALID_ARG, "tensor %d: n=%lld must not be negative", i, (long long)t[i].n);
+    if (t[i].dtype != WM_FP32 && t[i].dtype != WM_BF16)
+      return fail(WM_ERR_INVALID_ARG, "tensor %d: unknown dtype %d", i, t[i].dtype);
+    if (t[i].n > ((int64_t)1 << 42) - total) return fail(WM_ERR_UNSUPPORTED, "more than 2^42 values");
+    total += t[i].n;
+  }
+  return WM_OK;
 }
 
 }  // namespace
@@ -400,6 +483,176 @@ float wm_poly_lr(int32_t epoch, float lr0, float lr_end, int32_t epochs) {
   const double e = epoch < 0 ? 0.0 : (epoch > epochs ? (double)epochs : (double)epoch);
   const double f = 1.0 - e / epochs;
   return (float)(((double)lr0 - lr_end) * f * f + lr_end);
+}
+
+wm_status wm_embed(int32_t dtype, int64_t n, int32_t V, int32_t H, const int32_t* tokens, const void* table, float scale,
+                   void* out, int64_t out_ld, wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_embed(n, V, H)) != WM_OK || (st = check_ld("out", n, H, out_ld)) != WM_OK) return st;
+  if (n == 0) return ok();
+  if (!tokens || !table || !out) return fail(WM_ERR_INVALID_ARG, "tokens, table and out are required");
+  if (!aligned4(tokens) || !aligned_el(table, dtype) || !aligned_el(out, dtype))
+    return fail(WM_ERR_INVALID_ARG, "tokens, table and out must be aligned to their elements");
+  const wm::EmbedArgs a{(long)n, V, H, tokens, table, scale, out, (long)out_ld};
+  const hipError_t e = wm::launch_embed(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_embed");
+  return ok();
+}
+
+size_t wm_embed_grad_workspace_bytes(int64_t n, int32_t V, int32_t H) {
+  return check_embed(n, V, H) == WM_OK ? wm::embed_grad_workspace((long)n, V, H) : 0;
+}
+
+wm_status wm_embed_grad(int32_t dtype, int64_t n, int32_t V, int32_t H, const int32_t* tokens, const void* grad_out,
+                        int64_t grad_out_ld, float scale, float* grad_table, void* workspace, size_t workspace_bytes,
+                        wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_embed(n, V, H)) != WM_OK || (st = check_ld("grad_out", n, H, grad_out_ld)) != WM_OK)
+    return st;
+  if (!grad_table || (n > 0 && (!tokens || !grad_out)))
+    return fail(WM_ERR_INVALID_ARG, "tokens, grad_out and grad_table are required");
+  if (!aligned4(tokens) || !aligned_el(grad_out, dtype) || !aligned4(grad_table))
+    return fail(WM_ERR_INVALID_ARG, "tokens, grad_out and grad_table must be aligned to their elements");
+  if ((st = check_workspace("the workspace of wm_embed_grad", workspace, workspace_bytes,
+                            wm::embed_grad_workspace((long)n, V, H))) != WM_OK)
+    return st;
+  const wm::EmbedGradArgs a{(long)n, V, H, tokens, grad_out, (long)grad_out_ld, scale, grad_table, workspace};
+  const hipError_t e = wm::launch_embed_grad(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_embed_grad");
+  return ok();
+}
+
+wm_status wm_layer_norm(int32_t dtype, int64_t rows, int32_t H, const void* x, int64_t x_ld, const float* gamma,
+                        const float* beta, float eps, void* y, int64_t y_ld, float* mean, float* rstd,
+                        wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_norm(rows, H)) != WM_OK || (st = check_ld("x", rows, H, x_ld)) != WM_OK ||
+      (st = check_ld("y", rows, H, y_ld)) != WM_OK)
+    return st;
+  if (!(eps >= 0.0f) || !isfinite(eps)) return fail(WM_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (!mean != !rstd) return fail(WM_ERR_INVALID_ARG, "mean and rstd come together");
+  if (rows == 0) return ok();
+  if (!x || !y) return fail(WM_ERR_INVALID_ARG, "x and y are required");
+  if (!aligned_el(x, dtype) || !aligned_el(y, dtype) || !aligned4(gamma) || !aligned4(beta) || !aligned4(mean) ||
+      !aligned4(rstd))
+    return fail(WM_ERR_INVALID_ARG, "arrays must be aligned to their elements");
+  const wm::NormArgs a{(long)rows, H, x, (long)x_ld, gamma, beta, eps, y, (long)y_ld, mean, rstd};
+  const hipError_t e = wm::launch_layer_norm(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_layer_norm");
+  return ok();
+}
+
+size_t wm_layer_norm_grad_workspace_bytes(int64_t rows, int32_t H) {
+  return check_norm(rows, H) == WM_OK ? wm::layer_norm_grad_workspace((long)rows, H) : 0;
+}
+
+wm_status wm_layer_norm_grad(int32_t dtype, int64_t rows, int32_t H, const void* x, int64_t x_ld, const void* grad_y,
+                             int64_t grad_y_ld, const float* gamma, const float* mean, const float* rstd, void* grad_x,
+                             int64_t grad_x_ld, float* grad_gamma, float* grad_beta, void* workspace,
+                             size_t workspace_bytes, wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_norm(rows, H)) != WM_OK || (st = check_ld("x", rows, H, x_ld)) != WM_OK ||
+      (st = check_ld("grad_y", rows, H, grad_y_ld)) != WM_OK || (st = check_ld("grad_x", rows, H, grad_x_ld)) != WM_OK)
+    return st;
+  if (rows > 0 && (!x || !grad_y || !mean || !rstd || !grad_x))
+    return fail(WM_ERR_INVALID_ARG, "x, grad_y, mean, rstd and grad_x are required");
+  if (!aligned_el(x, dtype) || !aligned_el(grad_y, dtype) || !aligned_el(grad_x, dtype) || !aligned4(gamma) ||
+      !aligned4(mean) || !aligned4(rstd) || !aligned4(grad_gamma) || !aligned4(grad_beta))
+    return fail(WM_ERR_INVALID_ARG, "arrays must be aligned to their elements");
+  if ((st = check_workspace("the workspace of wm_layer_norm_grad", workspace, workspace_bytes,
+                            wm::layer_norm_grad_workspace((long)rows, H))) != WM_OK)
+    return st;
+  const wm::NormGradArgs a{(long)rows, H, x, (long)x_ld, grad_y, (long)grad_y_ld, gamma, mean, rstd, grad_x,
+                           (long)grad_x_ld, grad_gamma, grad_beta, reinterpret_cast<float*>(workspace)};
+  const hipError_t e = wm::launch_layer_norm_grad(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_layer_norm_grad");
+  return ok();
+}
+
+size_t wm_linrec_states_bytes(int32_t T, int32_t B, int32_t H) {
+  return check_linrec(T, B, H) == WM_OK ? wm::linrec_states(T, B, H) : 0;
+}
+
+size_t wm_linrec_workspace_bytes(int32_t T, int32_t B, int32_t H) {
+  return check_linrec(T, B, H) == WM_OK ? wm::linrec_workspace(T, B, H) : 0;
+}
+
+wm_status wm_linrec(int32_t dtype, int32_t T, int32_t B, int32_t H, const void* x, int64_t x_t, int64_t x_b,
+                    const void* gate, int64_t gate_t, int64_t gate_b, const float* h0, const uint8_t* resets,
+                    const int32_t* lengths, void* y, float* h_T, void* states, size_t states_bytes, void* workspace,
+                    size_t workspace_bytes, wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_linrec(T, B, H)) != WM_OK ||
+      (st = check_view("x", dtype, x, x_t, x_b, T, B, H, false)) != WM_OK ||
+      (st = check_view("gate", dtype, gate, gate_t, gate_b, T, B, H, false)) != WM_OK ||
+      (st = check_view("y", dtype, y, (int64_t)B * H, H, T, B, H, true)) != WM_OK)
+    return st;
+  if (!aligned4(h0) || !aligned4(lengths) || !aligned4(h_T))
+    return fail(WM_ERR_INVALID_ARG, "h0, lengths and h_T must be 4-byte aligned");
+  if (B == 0) return ok();
+  if (states && (st = check_workspace("states", states, states_bytes, wm::linrec_states(T, B, H))) != WM_OK) return st;
+  if ((st = check_workspace("the workspace of wm_linrec", workspace, workspace_bytes, wm::linrec_workspace(T, B, H))) !=
+      WM_OK)
+    return st;
+  const wm::LinrecArgs a{T, B, H, {x, (long)x_t, (long)x_b}, {gate, (long)gate_t, (long)gate_b}, h0, resets, lengths, y,
+                         h_T, reinterpret_cast<float*>(states), workspace};
+  const hipError_t e = wm::launch_linrec(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_linrec");
+  return ok();
+}
+
+wm_status wm_linrec_grad(int32_t dtype, int32_t T, int32_t B, int32_t H, const void* x, int64_t x_t, int64_t x_b,
+                         const void* gate, int64_t gate_t, int64_t gate_b, const uint8_t* resets,
+                         const int32_t* lengths, const void* grad_y, int64_t grad_y_t, int64_t grad_y_b,
+                         const float* grad_h_T, const void* states, size_t states_bytes, void* grad_x,
+                         int64_t grad_x_t, int64_t grad_x_b, void* grad_gate, int64_t grad_gate_t, int64_t grad_gate_b,
+                         float* grad_h0, void* workspace, size_t workspace_bytes, wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_linrec(T, B, H)) != WM_OK ||
+      (st = check_view("x", dtype, x, x_t, x_b, T, B, H, false)) != WM_OK ||
+      (st = check_view("gate", dtype, gate, gate_t, gate_b, T, B, H, false)) != WM_OK ||
+      (st = check_view("grad_y", dtype, grad_y, grad_y_t, grad_y_b, T, B, H, false)) != WM_OK ||
+      (st = check_view("grad_x", dtype, grad_x, grad_x_t, grad_x_b, T, B, H, true)) != WM_OK ||
+      (st = check_view("grad_gate", dtype, grad_gate, grad_gate_t, grad_gate_b, T, B, H, true)) != WM_OK)
+    return st;
+  if (!aligned4(grad_h_T) || !aligned4(lengths) || !aligned4(grad_h0))
+    return fail(WM_ERR_INVALID_ARG, "grad_h_T, lengths and grad_h0 must be 4-byte aligned");
+  if (B == 0) return ok();
+  if ((st = check_workspace("states", states, states_bytes, wm::linrec_states(T, B, H))) != WM_OK ||
+      (st = check_workspace("the workspace of wm_linrec_grad", workspace, workspace_bytes,
+                            wm::linrec_workspace(T, B, H))) != WM_OK)
+    return st;
+  const wm::LinrecGradArgs a{T, B, H, {x, (long)x_t, (long)x_b}, {gate, (long)gate_t, (long)gate_b},
+                             {grad_y, (long)grad_y_t, (long)grad_y_b}, {grad_x, (long)grad_x_t, (long)grad_x_b},
+                             {grad_gate, (long)grad_gate_t, (long)grad_gate_b}, resets, lengths, grad_h_T,
+                             reinterpret_cast<const float*>(states), grad_h0, workspace};
+  const hipError_t e = wm::launch_linrec_grad(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_linrec_grad");
+  return ok();
+}
+
+size_t wm_clip_grads_workspace_bytes(int32_t n, const wm_grad_tensor* tensors) {
+  return check_grads(n, tensors) == WM_OK ? wm::clip_workspace(n, tensors) : 0;
+}
+
+wm_status wm_clip_grads(int32_t n, const wm_grad_tensor* tensors, float max_norm, float* norm, void* workspace,
+                        size_t workspace_bytes, wm_stream_t stream) {
+  wm_status st = check_grads(n, tensors);
+  if (st != WM_OK) return st;
+  if (!(max_norm >= 0.0f) || !isfinite(max_norm)) return fail(WM_ERR_INVALID_ARG, "max_norm must be finite and >= 0");
+  if (!norm || !aligned4(norm)) return fail(WM_ERR_INVALID_ARG, "norm is required, 4-byte aligned");
+  for (int32_t i = 0; i < n; ++i) {
+    if (tensors[i].n == 0) continue;
+    if (!tensors[i].grad || !tensors[i].out) return fail(WM_ERR_INVALID_ARG, "tensor %d: grad and out are required", i);
+    if (!aligned_el(tensors[i].grad, tensors[i].dtype) || !aligned_el(tensors[i].out, tensors[i].dtype))
+      return fail(WM_ERR_INVALID_ARG, "tensor %d is not aligned to its element", i);
+  }
+  if ((st = check_workspace("the workspace of wm_clip_grads", workspace, workspace_bytes,
+                            wm::clip_workspace(n, tensors))) != WM_OK)
+    return st;
+  const hipError_t e = wm::launch_clip(n, tensors, max_norm, norm, workspace, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_clip_grads");
+  return ok();
 }
 
 wm_status wm_workspace_status(const void* workspace, wm_stream_t stream) {

@@ -1,0 +1,108 @@
+// Shared by the sequence-core operators (wm_embed.hip, wm_norm.hip,
+// wm_linrec.hip, wm_clip.hip): launch arguments and device helpers.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "wm_device.h"
+
+namespace wm {
+
+struct EmbedArgs {
+  long n;
+  int V, H;
+  const int32_t* tokens;
+  const void* table;
+  float scale;
+  void* out;
+  long out_ld;
+};
+hipError_t launch_embed(int dtype, const EmbedArgs& a, hipStream_t s);
+
+struct EmbedGradArgs {
+  long n;
+  int V, H;
+  const int32_t* tokens;
+  const void* dout;
+  long dout_ld;
+  float scale;
+  float* dtable;
+  void* ws;
+};
+size_t embed_grad_workspace(long n, int V, int H);
+hipError_t launch_embed_grad(int dtype, const EmbedGradArgs& a, hipStream_t s);
+
+constexpr int kNormMaxH = 8192;
+struct NormArgs {
+  long rows;
+  int H;
+  const void* x;
+  long x_ld;
+  const float *gamma, *beta;
+  float eps;
+  void* y;
+  long y_ld;
+  float *mean, *rstd;
+};
+hipError_t launch_layer_norm(int dtype, const NormArgs& a, hipStream_t s);
+
+struct NormGradArgs {
+  long rows;
+  int H;
+  const void* x;
+  long x_ld;
+  const void* dy;
+  long dy_ld;
+  const float *gamma, *mean, *rstd;
+  void* dx;
+  long dx_ld;
+  float *dgamma, *dbeta;
+  float* part;  // workspace
+};
+size_t layer_norm_grad_workspace(long rows, int H);
+hipError_t launch_layer_norm_grad(int dtype, const NormGradArgs& a, hipStream_t s);
+
+// A [T, B, H] array: element strides of the steps and the rows, unit stride
+// along H.
+struct SeqView {
+  const void* p;
+  long t, b;
+};
+struct LinrecArgs {
+  int T, B, H;
+  SeqView x, gate;
+  const float* h0;        // [B, H] or null (0)
+  const uint8_t* resets;  // [T, B] or null
+  const int32_t* lengths; // [B] or null (T)
+  void* y;                // [T, B, H]
+  float* h_T;             // [B, H] or null
+  float* states;          // linrec_states floats or null
+  void* ws;
+};
+struct LinrecGradArgs {
+  int T, B, H;
+  SeqView x, gate, dy, dx, dgate;  // dx, dgate are written
+  const uint8_t* resets;
+  const int32_t* lengths;
+  const float* dh_T;      // [B, H] or null (0)
+  const float* states;
+  float* dh0;             // [B, H] or null
+  void* ws;
+};
+size_t linrec_states(int T, int B, int H);     // bytes
+size_t linrec_workspace(int T, int B, int H);  // bytes
+hipError_t launch_linrec(int dtype, const LinrecArgs& a, hipStream_t s);
+hipError_t launch_linrec_grad(int dtype, const LinrecGradArgs& a, hipStream_t s);
+
+size_t clip_workspace(int n, const wm_grad_tensor* t);
+hipError_t launch_clip(int n, const wm_grad_tensor* t, float max_norm, float* norm, void* ws, hipStream_t s);
+
+// (1 / (1 + e^-g), 1 / (1 + e^g)), each to full relative precision.
+__device__ __forceinline__ float2 gate_pair(float g) {
+  const float e = expf(-fabsf(g));
+  const float r = 1.0f / (1.0f + e), q = e * r;
+  return g >= 0.0f ? make_float2(r, q) : make_float2(q, r);
+}
+
+}  // namespace wm
