@@ -432,8 +432,9 @@ wm_status wm_layer_norm_grad(int32_t dtype, int64_t rows, int32_t H, const void 
  *                        wm_linrec_states_bytes that receives what
  *                        wm_linrec_grad needs.
  *   workspace            of wm_linrec_workspace_bytes, also for the gradient.
- * T B at most 2^31 - 1, B H at most 2^31 - 1.  B = 0 is a no-op; T = 0 gives
- * h_T = h0.
+ * T B at most 2^31 - 1, B H at most 2^31 - 1, and the rows that hold 128
+ * neighbouring channels within 2 GiB of each other.  B = 0 is a no-op; T = 0
+ * gives h_T = h0.
  */
 size_t wm_linrec_states_bytes(int32_t T, int32_t B, int32_t H);
 size_t wm_linrec_workspace_bytes(int32_t T, int32_t B, int32_t H);

@@ -51,22 +51,25 @@ constexpr unsigned long long kEmpty = ~0ull;  // a map not yet published (A's bi
 template <typename DT, int V> struct Chan;
 template <> struct Chan<float, 1> {
   typedef float raw;
-  __device__ static raw load(const float* p) { return *p; }
+  __device__ static raw load(const char* p) { return *reinterpret_cast<const float*>(p); }
   __device__ static float get(raw r, int) { return r; }
-  __device__ static void put(float* p, const float* v) { *p = v[0]; }
+  __device__ static void put(char* p, const float* v) { *reinterpret_cast<float*>(p) = v[0]; }
+  __device__ static uint32_t size(raw r) { return __float_as_uint(r) & 0x7fffffffu; }
 };
 template <> struct Chan<bf16_t, 1> {
   typedef bf16_t raw;
-  __device__ static raw load(const bf16_t* p) { return *p; }
+  __device__ static raw load(const char* p) { return *reinterpret_cast<const bf16_t*>(p); }
   __device__ static float get(raw r, int) { return bf16_bits_to_f32(r); }
-  __device__ static void put(bf16_t* p, const float* v) { *p = (bf16_t)f32_to_bf16_bits(v[0]); }
+  __device__ static void put(char* p, const float* v) { *reinterpret_cast<bf16_t*>(p) = (bf16_t)f32_to_bf16_bits(v[0]); }
+  __device__ static uint32_t size(raw r) { return (uint32_t)r << 16 & 0x7fffffffu; }
 };
 template <> struct Chan<bf16_t, 2> {
   typedef uint32_t raw;
   typedef uint32_t __attribute__((aligned(2))) mem;
-  __device__ static raw load(const bf16_t* p) { return *reinterpret_cast<const mem*>(p); }
+  __device__ static raw load(const char* p) { return *reinterpret_cast<const mem*>(p); }
   __device__ static float get(raw r, int j) { return __uint_as_float(j ? r & 0xffff0000u : r << 16); }
-  __device__ static void put(bf16_t* p, const float* v) { *reinterpret_cast<mem*>(p) = pack2_bf16(v[0], v[1]); }
+  __device__ static void put(char* p, const float* v) { *reinterpret_cast<mem*>(p) = pack2_bf16(v[0], v[1]); }
+  __device__ static uint32_t size(raw r) { return max(r & 0x7fffffffu, r << 16 & 0x7fffffffu); }
 };
 
 struct Map {
@@ -79,11 +82,14 @@ __device__ __forceinline__ Map then(Map m, Map n) {
 }
 __device__ __forceinline__ float apply(Map m, float h) { return m.A < 0.0f ? m.U : fmaf(m.A, h, m.U); }
 
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // What a wave knows of its tile: the lane's channels and the masks of its steps.
 template <int TT, int V>
 struct Tile {
   long c;        // first channel of the lane (row b, column h)
-  int b, h, t0, nt;
+  int b, h, b0;  // b0: the wave's first row
+  int t0, nt;
   bool on;       // the channels exist
   int live;      // steps of the tile inside the row's length
   uint32_t rs;   // bit i: step i starts anew
@@ -93,9 +99,10 @@ struct Tile {
     const long C = (long)B * H;
     c = (group * 64 + lane) * V;
     on = c < C;
-    const long cc = on ? c : C - V;
-    b = (int)(cc / H);
-    h = (int)(cc - (long)b * H);
+    const uint32_t cc = (uint32_t)(on ? c : C - V);  // B H is below 2^31
+    b = (int)(cc / (uint32_t)H);
+    h = (int)(cc - (uint32_t)b * (uint32_t)H);
+    b0 = uniform(b);
     nt = min(max(T - t0, 0), TT);
     live = on ? nt : 0;
     if (lengths) live = min(live, max(lengths[b] - t0, 0));
@@ -103,8 +110,7 @@ struct Tile {
     if (resets) {
       // 64 / TT rows by TT steps at a time: one byte per lane, handed round as a ballot
       constexpr int kRows = 64 / TT;
-      const int b0 = __builtin_amdgcn_readfirstlane(b), b1 = __builtin_amdgcn_readlane(b, 63);
-      const int ti = lane % TT;
+      const int b1 = __builtin_amdgcn_readlane(b, 63), ti = lane % TT;
       for (int r = b0; r <= b1; r += kRows) {
         const int br = r + lane / TT;
         const bool hit = ti < nt && br <= b1 && resets[(long)(t0 + ti) * B + br] != 0;
@@ -116,17 +122,35 @@ struct Tile {
     }
   }
   __device__ bool reset(int i) const { return (rs >> i) & 1u; }
+  // whether every step of every lane counts and none starts anew
+  __device__ bool whole() const { return __all(live == TT && rs == 0); }
+};
+
+// A [T, B, H] array at a wave's tile: the step's row of the wave's first lane
+// in scalar registers, the lane's place from there as a 32-bit offset (the
+// launch checks that the rows that a wave can reach lie within 2 GiB).
+template <typename DT, int TT, int V>
+struct At {
+  char* p;
+  long step;     // bytes
+  uint32_t off;
+  __device__ At(const void* base, long st, long sb, const Tile<TT, V>& k) {
+    p = reinterpret_cast<char*>(const_cast<void*>(base)) + ((long)k.t0 * st + (long)k.b0 * sb) * (long)sizeof(DT);
+    step = st * (long)sizeof(DT);
+    off = (uint32_t)(((long)(k.b - k.b0) * sb + k.h) * (long)sizeof(DT));
+  }
+  __device__ char* at(int i) const { return p + i * step + off; }
 };
 
 template <typename DT, int V, int TT>
 __device__ __forceinline__ void load_tile(typename Chan<DT, V>::raw (&r)[TT], const SeqView& v, const Tile<TT, V>& k) {
-  const DT* p = reinterpret_cast<const DT*>(v.p) + (long)k.t0 * v.t + (long)k.b * v.b + k.h;
+  At<DT, TT, V> q(v.p, v.t, v.b, k);
   if (k.nt == TT) {
 #pragma unroll
-    for (int i = 0; i < TT; ++i) r[i] = Chan<DT, V>::load(p + i * v.t);
+    for (int i = 0; i < TT; ++i, q.p += q.step) r[i] = Chan<DT, V>::load(q.p + q.off);
   } else {
 #pragma unroll
-    for (int i = 0; i < TT; ++i) r[i] = i < k.nt ? Chan<DT, V>::load(p + i * v.t) : typename Chan<DT, V>::raw(0);
+    for (int i = 0; i < TT; ++i, q.p += q.step) r[i] = i < k.nt ? Chan<DT, V>::load(q.p + q.off) : typename Chan<DT, V>::raw(0);
   }
 }
 
@@ -197,7 +221,7 @@ template <int V> struct Shared {
 template <int V>
 __device__ __forceinline__ void before(Map (&m)[V], Shared<V>& sh, const Chain& ch, int order, long group, int waves,
                                        bool forward) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
   const long stride = ch.groups * 64 * V, at = (group * 64 + lane) * V;
   if (w == waves - 1) {  // the segment's map
     Map s[V];
@@ -243,13 +267,50 @@ __device__ __forceinline__ void place(unsigned* order, const Chain& ch, long& gr
   if (ch.segs > 1) {
     if (threadIdx.x == 0) *order = atomicAdd(ch.head, 1u);
     __syncthreads();
-    const unsigned k = *order;
-    seg = (int)(k / ch.groups);
-    group = k - (long)seg * ch.groups;
+    const uint32_t k = (uint32_t)uniform((int)*order), n = (uint32_t)ch.groups;
+    seg = (int)(k / n);
+    group = k - (uint32_t)seg * n;
   } else {
     seg = 0;
     group = blockIdx.x;
   }
+}
+
+// The tile's steps of a wave, in registers: a, u = (1 - a) x (forward) and
+// their map.  MASKED: some step is padding or starts anew, or some gate is
+// beyond kGateMost.
+template <bool MASKED, typename DT, int V, int TT>
+__device__ __forceinline__ void fold(float (&A)[TT][V], float (&U)[TT][V], Map (&m)[V],
+                                     const typename Chan<DT, V>::raw (&xr)[TT], const typename Chan<DT, V>::raw (&gr)[TT],
+                                     const Tile<TT, V>& k) {
+#pragma unroll
+  for (int i = 0; i < TT; ++i) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float g = Chan<DT, V>::get(gr[i], v), x = Chan<DT, V>::get(xr[i], v);
+      if constexpr (MASKED) {
+        const float2 p = gate_pair(g);
+        const bool live = i < k.live;
+        A[i][v] = live ? (k.reset(i) ? -1.0f : p.x) : 1.0f;
+        U[i][v] = live ? p.y * x : 0.0f;
+        m[v] = then(m[v], {A[i][v], U[i][v]});
+      } else {
+        const float2 p = gate_pair_small(g);
+        A[i][v] = p.x;
+        U[i][v] = p.y * x;
+        m[v].A *= p.x;
+        m[v].U = fmaf(p.x, m[v].U, U[i][v]);
+      }
+    }
+  }
+}
+
+template <typename DT, int V, int TT>
+__device__ __forceinline__ bool small_gates(const typename Chan<DT, V>::raw (&gr)[TT]) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int i = 0; i < TT; ++i) most = max(most, Chan<DT, V>::size(gr[i]));
+  return __all(most <= __float_as_uint(kGateMost));  // NaN and infinity lie above
 }
 
 // waves: tiles of a segment; with one wave per segment the work-group holds
@@ -259,14 +320,14 @@ __global__ void __launch_bounds__(64 * kWaves) k_linrec(const LinrecArgs a, cons
   __shared__ Shared<V> sh;
   typedef Chan<DT, V> Ch;
   const int lane = threadIdx.x & 63;
-  int w = threadIdx.x >> 6, seg;
+  int w = uniform(threadIdx.x >> 6), seg;
   long group;
   place(&sh.order, ch, group, seg);
   if (waves == 1) group = group * (blockDim.x >> 6) + w, w = 0;
   const Tile<TT, V> k(group, (ch.seg0 + seg) * waves * TT + w * TT, a.T, a.B, a.H, a.resets, a.lengths);
   typename Ch::raw xr[TT], gr[TT];
-  load_tile<DT, V, TT>(xr, a.x, k);
   load_tile<DT, V, TT>(gr, a.gate, k);
+  load_tile<DT, V, TT>(xr, a.x, k);
   float h[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) h[v] = w == 0 && ch.enter && k.on ? ch.enter[k.c + v] : 0.0f;
@@ -274,17 +335,11 @@ __global__ void __launch_bounds__(64 * kWaves) k_linrec(const LinrecArgs a, cons
   Map m[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) m[v] = {1.0f, 0.0f};
-#pragma unroll
-  for (int i = 0; i < TT; ++i) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float2 p = gate_pair(Ch::get(gr[i], v));
-      const bool live = i < k.live;
-      A[i][v] = live ? (k.reset(i) ? -1.0f : p.x) : 1.0f;
-      U[i][v] = live ? p.y * Ch::get(xr[i], v) : 0.0f;
-      m[v] = then(m[v], {A[i][v], U[i][v]});
-    }
-  }
+  const bool whole = k.whole() && small_gates<DT, V, TT>(gr);
+  if (whole)
+    fold<false, DT, V, TT>(A, U, m, xr, gr, k);
+  else
+    fold<true, DT, V, TT>(A, U, m, xr, gr, k);
   if (waves > 1) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -310,20 +365,105 @@ __global__ void __launch_bounds__(64 * kWaves) k_linrec(const LinrecArgs a, cons
 #pragma unroll
     for (int v = 0; v < V; ++v) a.states[k.c + v] = h[v];
   }
-  DT* y = reinterpret_cast<DT*>(a.y) + (long)k.t0 * a.B * a.H + k.c;
+  At<DT, TT, V> y(a.y, (long)a.B * a.H, a.H, k);
+  if (whole) {
 #pragma unroll
-  for (int i = 0; i < TT; ++i) {
-    float o[V];
+    for (int i = 0; i < TT; ++i, y.p += y.step) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      h[v] = apply({A[i][v], U[i][v]}, h[v]);
-      o[v] = i < k.live ? h[v] : 0.0f;
+      for (int v = 0; v < V; ++v) h[v] = fmaf(A[i][v], h[v], U[i][v]);
+      Ch::put(y.p + y.off, h);
     }
-    if (i < k.nt && k.on) Ch::put(y + (long)i * a.B * a.H, o);
+  } else {
+#pragma unroll
+    for (int i = 0; i < TT; ++i, y.p += y.step) {
+      float o[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        h[v] = apply({A[i][v], U[i][v]}, h[v]);
+        o[v] = i < k.live ? h[v] : 0.0f;
+      }
+      if (i < k.nt && k.on) Ch::put(y.p + y.off, o);
+    }
   }
   if (ch.leave && k.on && k.t0 + TT >= ch.t1 && k.t0 < max(ch.t1, 1))
 #pragma unroll
     for (int v = 0; v < V; ++v) ch.leave[k.c + v] = h[v];
+}
+
+// The gradient's tile: a and 1 - a of its steps, the map of h and that of R,
+//   R_out = sum_i (prod_{j <= i} a_j) dy_i + (prod a) R_in.
+template <bool MASKED, typename DT, int V, int TT>
+__device__ __forceinline__ void fold_grad(float (&A)[TT][V], float (&M)[TT][V], Map (&m)[V], Map (&r)[V],
+                                          const typename Chan<DT, V>::raw (&xr)[TT],
+                                          const typename Chan<DT, V>::raw (&gr)[TT],
+                                          const typename Chan<DT, V>::raw (&dr)[TT], const Tile<TT, V>& k) {
+#pragma unroll
+  for (int i = 0; i < TT; ++i) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float g = Chan<DT, V>::get(gr[i], v), x = Chan<DT, V>::get(xr[i], v), d = Chan<DT, V>::get(dr[i], v);
+      const float2 p = MASKED ? gate_pair(g) : gate_pair_small(g);
+      A[i][v] = p.x;
+      M[i][v] = p.y;
+      if constexpr (MASKED) {
+        if (i < k.live) {
+          const bool cut = k.reset(i);
+          m[v] = then(m[v], {cut ? -1.0f : p.x, p.y * x});
+          if (cut) r[v].A = -1.0f;
+          if (!(r[v].A < 0.0f)) {
+            r[v].A *= p.x;
+            r[v].U = fmaf(r[v].A, d, r[v].U);
+          }
+        }
+      } else {
+        m[v].A *= p.x;
+        m[v].U = fmaf(p.x, m[v].U, p.y * x);
+        r[v].U = fmaf(m[v].A, d, r[v].U);
+      }
+    }
+  }
+  if constexpr (!MASKED)
+#pragma unroll
+    for (int v = 0; v < V; ++v) r[v].A = m[v].A;
+}
+
+template <bool MASKED, typename DT, int V, int TT>
+__device__ __forceinline__ void emit_grad(float (&A)[TT][V], float (&M)[TT][V], float (&h)[V], float (&R)[V],
+                                          const typename Chan<DT, V>::raw (&xr)[TT],
+                                          const typename Chan<DT, V>::raw (&dr)[TT], const Tile<TT, V>& k,
+                                          const LinrecGradArgs& a) {
+  typedef Chan<DT, V> Ch;
+  // forward: what h_{t-1} puts into dgate
+  float G[TT][V];
+#pragma unroll
+  for (int i = 0; i < TT; ++i) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float x = Ch::get(xr[i], v);
+      if (MASKED && k.reset(i)) h[v] = 0.0f;
+      G[i][v] = A[i][v] * M[i][v] * (h[v] - x);
+      if (!MASKED || i < k.live) h[v] = fmaf(A[i][v], h[v], M[i][v] * x);
+    }
+  }
+  At<DT, TT, V> dx(a.dx.p, a.dx.t, a.dx.b, k), dg(a.dgate.p, a.dgate.t, a.dgate.b, k);
+  dx.p += (TT - 1) * dx.step;
+  dg.p += (TT - 1) * dg.step;
+#pragma unroll
+  for (int i = TT - 1; i >= 0; --i, dx.p -= dx.step, dg.p -= dg.step) {
+    float ox[V], og[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const bool live = !MASKED || i < k.live;
+      const float D = R[v] + Ch::get(dr[i], v);
+      ox[v] = live ? M[i][v] * D : 0.0f;
+      og[v] = live ? G[i][v] * D : 0.0f;
+      R[v] = live ? (MASKED && k.reset(i) ? 0.0f : A[i][v] * D) : R[v];
+    }
+    if (!MASKED || (i < k.nt && k.on)) {
+      Ch::put(dx.p + dx.off, ox);
+      Ch::put(dg.p + dg.off, og);
+    }
+  }
 }
 
 template <typename DT, int V, int TT>
@@ -332,15 +472,15 @@ __global__ void __launch_bounds__(64 * kWaves) k_linrec_grad(const LinrecGradArg
   __shared__ Map fwd[kWaves][64][V];
   typedef Chan<DT, V> Ch;
   const int lane = threadIdx.x & 63;
-  int w = threadIdx.x >> 6, order;
+  int w = uniform(threadIdx.x >> 6), order;
   long group;
   place(&sh.order, ch, group, order);
   const int seg = ch.seg0 + ch.segs - 1 - order;  // the chain runs from the last segment to the first
   if (waves == 1) group = group * (blockDim.x >> 6) + w, w = 0;
   const Tile<TT, V> k(group, seg * waves * TT + w * TT, a.T, a.B, a.H, a.resets, a.lengths);
   typename Ch::raw xr[TT], gr[TT], dr[TT];
-  load_tile<DT, V, TT>(xr, a.x, k);
   load_tile<DT, V, TT>(gr, a.gate, k);
+  load_tile<DT, V, TT>(xr, a.x, k);
   load_tile<DT, V, TT>(dr, a.dy, k);
   float h[V], R[V];
 #pragma unroll
@@ -348,30 +488,15 @@ __global__ void __launch_bounds__(64 * kWaves) k_linrec_grad(const LinrecGradArg
     h[v] = k.on ? a.states[(long)seg * a.B * a.H + k.c + v] : 0.0f;
     R[v] = w == waves - 1 && ch.enter && k.on ? ch.enter[k.c + v] : 0.0f;
   }
-  // the tile's map of h, and that of R: R_out = sum_i (prod_{j <= i} a_j) dy_i + (prod a) R_in
   float A[TT][V], M[TT][V];  // a, 1 - a
   Map m[V], r[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) m[v] = r[v] = {1.0f, 0.0f};
-#pragma unroll
-  for (int i = 0; i < TT; ++i) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float2 p = gate_pair(Ch::get(gr[i], v));
-      const bool live = i < k.live;
-      A[i][v] = p.x;
-      M[i][v] = p.y;
-      if (live) {
-        const bool cut = k.reset(i);
-        m[v] = then(m[v], {cut ? -1.0f : p.x, p.y * Ch::get(xr[i], v)});
-        if (cut) r[v].A = -1.0f;
-        if (r[v].A >= 0.0f || __isnanf(r[v].A)) {
-          r[v].A *= p.x;
-          r[v].U = fmaf(r[v].A, Ch::get(dr[i], v), r[v].U);
-        }
-      }
-    }
-  }
+  const bool whole = k.whole() && small_gates<DT, V, TT>(gr);
+  if (whole)
+    fold_grad<false, DT, V, TT>(A, M, m, r, xr, gr, dr, k);
+  else
+    fold_grad<true, DT, V, TT>(A, M, m, r, xr, gr, dr, k);
   if (waves > 1) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -395,36 +520,10 @@ __global__ void __launch_bounds__(64 * kWaves) k_linrec_grad(const LinrecGradArg
 #pragma unroll
       for (int v = 0; v < V; ++v) R[v] = apply(sh.tile[i][lane][v], R[v]);
   }
-  // forward: what h_{t-1} puts into dgate
-  float G[TT][V];
-#pragma unroll
-  for (int i = 0; i < TT; ++i) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float x = Ch::get(xr[i], v);
-      if (k.reset(i)) h[v] = 0.0f;
-      G[i][v] = A[i][v] * M[i][v] * (h[v] - x);
-      if (i < k.live) h[v] = fmaf(A[i][v], h[v], M[i][v] * x);
-    }
-  }
-  DT* dx = reinterpret_cast<DT*>(const_cast<void*>(a.dx.p)) + (long)k.t0 * a.dx.t + (long)k.b * a.dx.b + k.h;
-  DT* dg = reinterpret_cast<DT*>(const_cast<void*>(a.dgate.p)) + (long)k.t0 * a.dgate.t + (long)k.b * a.dgate.b + k.h;
-#pragma unroll
-  for (int i = TT - 1; i >= 0; --i) {
-    float ox[V], og[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const bool live = i < k.live;
-      const float D = R[v] + Ch::get(dr[i], v);
-      ox[v] = live ? M[i][v] * D : 0.0f;
-      og[v] = live ? G[i][v] * D : 0.0f;
-      R[v] = live ? (k.reset(i) ? 0.0f : A[i][v] * D) : R[v];
-    }
-    if (i < k.nt && k.on) {
-      Ch::put(dx + (long)i * a.dx.t, ox);
-      Ch::put(dg + (long)i * a.dgate.t, og);
-    }
-  }
+  if (whole)
+    emit_grad<false, DT, V, TT>(A, M, h, R, xr, dr, k, a);
+  else
+    emit_grad<true, DT, V, TT>(A, M, h, R, xr, dr, k, a);
   if (ch.leave && k.on && k.t0 == ch.t0)
 #pragma unroll
     for (int v = 0; v < V; ++v) ch.leave[k.c + v] = R[v];
@@ -532,8 +631,6 @@ hipError_t launch_linrec(int dtype, const LinrecArgs& a, hipStream_t s) {
 hipError_t launch_linrec_grad(int dtype, const LinrecGradArgs& a, hipStream_t s) {
   if (dtype == WM_FP32)
     return run<1>("linrec_grad", k_linrec_grad<float, 1, kTT>, k_linrec_grad<float, 1, 1>, a, a.dh_T, a.dh0, true, s);
-  if (a.H % 2 == 0)
-    return run<2>("linrec_grad", k_linrec_grad<bf16_t, 2, kTT>, k_linrec_grad<bf16_t, 2, 1>, a, a.dh_T, a.dh0, true, s);
   return run<1>("linrec_grad", k_linrec_grad<bf16_t, 1, kTT>, k_linrec_grad<bf16_t, 1, 1>, a, a.dh_T, a.dh0, true, s);
 }
 
