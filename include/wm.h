@@ -432,7 +432,7 @@ wm_status wm_layer_norm_grad(int32_t dtype, int64_t rows, int32_t H, const void 
  *                        wm_linrec_states_bytes that receives what
  *                        wm_linrec_grad needs.
  *   workspace            of wm_linrec_workspace_bytes, also for the gradient.
- * T B at most 2^31 - 1, B H at most 2^31 - 1, and the rows that hold 128
+ * T B at most 2^31 - 1, B H at most 2^31 - 1, and the rows that hold 64
  * neighbouring channels within 2 GiB of each other.  B = 0 is a no-op; T = 0
  * gives h_T = h0.
  */

@@ -5,30 +5,34 @@
 //   D = dy_t + R_t, dx_t = (1 - a_t) D, dgate_t = a_t (1 - a_t) (h_{t-1} - x_t) D,
 //   R_{t-1} = a_t D, or 0 at a reset.
 //
-// A run of steps is an affine map of the state that enters it, h -> U + A h,
-// and maps compose: that is what splits the time axis.
-//   - A wave owns a tile of TT steps of 64 lanes (a lane: one fp32 channel or
-//     two bf16 ones), loads it whole, and folds it into the tile's map.
+// With enough channels to fill the device a wave walks its 64 channels through
+// all steps, the state in a register (k_linrec_walk).  With fewer, the time
+// axis is split (k_linrec_split): a run of steps is an affine map of the state
+// that enters it, h -> U + A h, and maps compose.
+//   - A wave owns a tile of kTT steps of 64 channels, loads it whole, and folds
+//     it into the tile's map.
 //   - The waves of a work-group own the tiles of one segment of up to kWaves
-//     TT steps; their maps meet in LDS.
+//     tiles; their maps meet in LDS.
 //   - Longer sequences take several segments, each a work-group of the same
 //     launch.  A work-group publishes its segment's map, then composes the
 //     maps of the segments before it, and only then runs its steps from the
-//     state that enters each tile.  Inputs are read once and outputs written
-//     once, whatever T is.
+//     state that enters each tile.
+// Either way inputs are read once and outputs written once, whatever T is.
 // A segment waits only for maps, and a map is published before its segment
 // waits for anything; segments take their numbers from a counter in the order
 // in which they start, so every map that is waited for belongs to a work-group
 // that already runs: no wait depends on what else occupies the device.  (The
 // waits are bounded all the same; one that reached its bound would set the
 // workspace's error word.)
+//
 // The gradient recomputes h_{t-1} from the inputs and the fp32 state that
-// entered the segment (saved by the forward call: 1 / (kWaves TT) of the
-// input), in fp32 and without reading y.
+// entered each tile of kTT steps, which the forward call saves (4 / kTT bytes
+// a value): in fp32, and without reading y.
 //
 // A map whose run holds a reset does not depend on the state at all: A = -1
 // says so (a true A is never negative), because 0 * inf would not.
 #include <algorithm>
+#include <cstdlib>
 
 #include "../../include/wm.h"
 #include "wm_kernels.h"
@@ -43,114 +47,340 @@ constexpr int kTT = 16;        // steps of a tile
 constexpr int kSeg = kWaves * kTT;
 constexpr int kFan = 16;       // segments whose maps are composed into one for the segments after them
 constexpr int kMaxSegs = 1024; // segments of a launch; longer sequences take several
+constexpr long kWalk = 2048;   // channel groups from which a wave walks all steps
 constexpr unsigned kSpinLimit = 1u << 22;
 constexpr unsigned long long kEmpty = ~0ull;  // a map not yet published (A's bits would be a NaN of this sign)
 
-// V channels of one lane at one step, as loaded.  Rows are aligned to their
-// element only; the hardware takes such addresses for wide loads too.
-template <typename DT, int V> struct Chan;
-template <> struct Chan<float, 1> {
+// One value at one step, as loaded; from a row's address, the same in every
+// lane, and the lane's offset in it.
+#define WM_GLOBAL __attribute__((address_space(1)))
+template <typename DT> struct Chan;
+template <> struct Chan<float> {
   typedef float raw;
-  __device__ static raw load(const char* p) { return *reinterpret_cast<const float*>(p); }
-  __device__ static float get(raw r, int) { return r; }
-  __device__ static void put(char* p, const float* v) { *reinterpret_cast<float*>(p) = v[0]; }
-  __device__ static uint32_t size(raw r) { return __float_as_uint(r) & 0x7fffffffu; }
+  __device__ static raw load(uint64_t row, uint32_t off) { return *reinterpret_cast<const WM_GLOBAL float*>(row + off); }
+  __device__ static float get(raw r) { return r; }
+  __device__ static void put(uint64_t row, uint32_t off, float v) { *reinterpret_cast<WM_GLOBAL float*>(row + off) = v; }
 };
-template <> struct Chan<bf16_t, 1> {
-  typedef bf16_t raw;
-  __device__ static raw load(const char* p) { return *reinterpret_cast<const bf16_t*>(p); }
-  __device__ static float get(raw r, int) { return bf16_bits_to_f32(r); }
-  __device__ static void put(char* p, const float* v) { *reinterpret_cast<bf16_t*>(p) = (bf16_t)f32_to_bf16_bits(v[0]); }
-  __device__ static uint32_t size(raw r) { return (uint32_t)r << 16 & 0x7fffffffu; }
+template <> struct Chan<bf16_t> {
+  typedef uint32_t raw;  // a register of its own: halves would make one load wait for another
+  __device__ static raw load(uint64_t row, uint32_t off) { return *reinterpret_cast<const WM_GLOBAL bf16_t*>(row + off); }
+  __device__ static float get(raw r) { return bf16_bits_to_f32(r); }
+  __device__ static void put(uint64_t row, uint32_t off, float v) {
+    *reinterpret_cast<WM_GLOBAL bf16_t*>(row + off) = (bf16_t)f32_to_bf16_bits(v);
+  }
 };
-template <> struct Chan<bf16_t, 2> {
-  typedef uint32_t raw;
-  typedef uint32_t __attribute__((aligned(2))) mem;
-  __device__ static raw load(const char* p) { return *reinterpret_cast<const mem*>(p); }
-  __device__ static float get(raw r, int j) { return __uint_as_float(j ? r & 0xffff0000u : r << 16); }
-  __device__ static void put(char* p, const float* v) { *reinterpret_cast<mem*>(p) = pack2_bf16(v[0], v[1]); }
-  __device__ static uint32_t size(raw r) { return max(r & 0x7fffffffu, r << 16 & 0x7fffffffu); }
-};
+#undef WM_GLOBAL
 
 struct Map {
   float A, U;
 };
+__device__ __forceinline__ float apply(Map m, float h) {
+  const float u = fmaf(m.A, h, m.U);
+  return m.A < 0.0f ? m.U : u;
+}
 // first m, then n
 __device__ __forceinline__ Map then(Map m, Map n) {
-  if (n.A < 0.0f) return n;
-  return {m.A < 0.0f ? -1.0f : n.A * m.A, fmaf(n.A, m.U, n.U)};
+  const float a = n.A * m.A;
+  return {n.A < 0.0f || m.A < 0.0f ? -1.0f : a, apply(n, m.U)};
 }
-__device__ __forceinline__ float apply(Map m, float h) { return m.A < 0.0f ? m.U : fmaf(m.A, h, m.U); }
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// What a wave knows of its tile: the lane's channels and the masks of its steps.
-template <int TT, int V>
-struct Tile {
-  long c;        // first channel of the lane (row b, column h)
-  int b, h, b0;  // b0: the wave's first row
-  int t0, nt;
-  bool on;       // the channels exist
-  int live;      // steps of the tile inside the row's length
-  uint32_t rs;   // bit i: step i starts anew
+// e^-|g|, on the short way where the whole wave allows it (NaN and infinity
+// lie beyond the bound).
+__device__ __forceinline__ float gate_exp(float g) {
+  if (__builtin_expect(__any(!(fabsf(g) <= kGateMost)), 0)) return expf(-fabsf(g));
+  return gate_exp_small(g);
+}
 
-  __device__ Tile(long group, int t0_, int T, int B, int H, const uint8_t* resets, const int32_t* lengths) : t0(t0_) {
-    const int lane = threadIdx.x & 63;
+// What a wave knows of its 64 channels.
+struct Lanes {
+  long c;        // the lane's channel (row b, column h)
+  int b, h;
+  int b0, b1;    // the wave's first and last row
+  bool on;       // the channel exists
+  int n;         // the row's length
+  int most;      // the most of the wave's rows
+
+  __device__ Lanes(long group, int T, int B, int H, const int32_t* lengths) {
     const long C = (long)B * H;
-    c = (group * 64 + lane) * V;
+    c = group * 64 + (threadIdx.x & 63);
     on = c < C;
-    const uint32_t cc = (uint32_t)(on ? c : C - V);  // B H is below 2^31
+    const uint32_t cc = (uint32_t)(on ? c : C - 1);  // B H is below 2^31
     b = (int)(cc / (uint32_t)H);
     h = (int)(cc - (uint32_t)b * (uint32_t)H);
     b0 = uniform(b);
-    nt = min(max(T - t0, 0), TT);
-    live = on ? nt : 0;
-    if (lengths) live = min(live, max(lengths[b] - t0, 0));
-    rs = 0;
-    if (resets) {
-      // 64 / TT rows by TT steps at a time: one byte per lane, handed round as a ballot
-      constexpr int kRows = 64 / TT;
-      const int b1 = __builtin_amdgcn_readlane(b, 63), ti = lane % TT;
-      for (int r = b0; r <= b1; r += kRows) {
-        const int br = r + lane / TT;
-        const bool hit = ti < nt && br <= b1 && resets[(long)(t0 + ti) * B + br] != 0;
-        const unsigned long long m = __ballot(hit);
-        const int k = b - r;
-        if (k >= 0 && k < kRows) rs = (uint32_t)(m >> (TT * k)) & ((1u << TT) - 1u);
-      }
-      rs &= (1u << live) - 1u;
+    b1 = __builtin_amdgcn_readlane(b, 63);
+    n = most = T;
+    if (lengths) {
+      n = min(max(lengths[b], 0), T);
+      most = 0;
+      for (int r = b0; r <= b1; ++r) most = max(most, __builtin_amdgcn_readlane(n, uniform(lane_of(r, group, H))));
     }
+    if (!on) n = 0;
+  }
+  // a lane of the wave that holds row r
+  __device__ int lane_of(int r, long group, int H) const {
+    return max((int)((long)r * H - group * 64), 0);
+  }
+};
+
+// A [T, B, H] array as a wave goes through it: the present step's row of the
+// wave's first lane as an address in scalar registers, the lane's place from
+// there as a 32-bit offset (the call checks that the rows that a wave can reach
+// lie within 2 GiB).
+template <typename DT>
+struct Rows {
+  uint64_t base, row;
+  long st, b;    // bytes
+  uint32_t off;
+  __device__ Rows(const SeqView& v, const Lanes& l, int t) {
+    constexpr long es = sizeof(DT);
+    base = reinterpret_cast<uint64_t>(v.p) + (uint64_t)((long)l.b0 * v.b * es);
+    st = v.t * es;
+    off = (uint32_t)(((long)(l.b - l.b0) * v.b + l.h) * es);
+    to(t);
+  }
+  __device__ void to(int t) { row = base + (uint64_t)((long)t * st); }
+  // The empty asm keeps the rows' addresses from being computed all at once
+  // (they would not fit the scalar registers), and the offset 32 bits wide.
+  __device__ void move(long bytes) {
+    row += (uint64_t)bytes;
+    asm volatile("" : "+s"(row));
+    asm volatile("" : "+v"(off));
+  }
+  __device__ typename Chan<DT>::raw load() const { return Chan<DT>::load(row, off); }
+  __device__ void put(float v) const { Chan<DT>::put(row, off, v); }
+};
+
+// The resets of TT steps from t0 on: one byte a lane holds 64 / TT rows by TT
+// steps, handed round as ballots.
+template <int TT>
+struct Resets {
+  static constexpr int kRows = 64 / TT;
+  uint32_t byte;  // of the wave's first rows, requested ahead of its use
+  __device__ static uint32_t flag(const uint8_t* resets, const Lanes& l, int r, int t0, int T, int B) {
+    const int lane = threadIdx.x & 63, t = t0 + lane % TT, br = r + lane / TT;
+    return t < T && br <= l.b1 ? resets[(long)t * B + br] : 0;
+  }
+  __device__ void ask(const uint8_t* resets, const Lanes& l, int t0, int T, int B) {
+    byte = resets ? flag(resets, l, l.b0, t0, T, B) : 0;
+  }
+  // bit i: step t0 + i of the lane's row starts anew
+  __device__ uint32_t bits(const uint8_t* resets, const Lanes& l, int t0, int T, int B) const {
+    uint32_t rs = 0, f = byte;
+    if (!resets) return 0;
+    for (int r = l.b0; r <= l.b1; r += kRows) {
+      if (r > l.b0) f = flag(resets, l, r, t0, T, B);
+      const unsigned long long m = __ballot(f != 0);
+      const int k = l.b - r;
+      if (k >= 0 && k < kRows) rs = (uint32_t)(m >> (TT * k)) & (uint32_t)((1ull << TT) - 1);
+    }
+    return rs;
+  }
+};
+
+// ---------------------------------------------------------------------------
+// All steps in one wave
+// ---------------------------------------------------------------------------
+
+// One tile; LOAD: the next tile's value of each step is requested as soon as
+// the present one's is used.  MASKED: some step is padding or starts anew.
+template <bool LOAD, bool MASKED, typename DT, int TT>
+__device__ __forceinline__ float walk_tile(float h, typename Chan<DT>::raw (&gr)[TT], typename Chan<DT>::raw (&xr)[TT],
+                                           Rows<DT>& g, Rows<DT>& x, Rows<DT>& y, int steps, int ahead, int live,
+                                           uint32_t rs, bool on) {
+#pragma unroll
+  for (int i = 0; i < TT; ++i) {
+    if (MASKED && i >= steps) continue;
+    const float gv = Chan<DT>::get(gr[i]), xv = Chan<DT>::get(xr[i]);
+    if (LOAD) {  // (past the last step: that one's place again)
+      gr[i] = g.load();
+      xr[i] = x.load();
+      g.move(i + 1 < ahead ? g.st : 0);
+      x.move(i + 1 < ahead ? x.st : 0);
+    }
+    const float2 p = gate_pair_of(gv, gate_exp(gv));
+    if (MASKED) {
+      const float from = (rs >> i) & 1u ? 0.0f : h;
+      const float to = fmaf(p.x, from, p.y * xv);
+      h = i < live ? to : h;
+      if (on) y.put(i < live ? h : 0.0f);
+    } else {
+      h = fmaf(p.x, h, p.y * xv);
+      y.put(h);
+    }
+    y.move(y.st);
+  }
+  return h;
+}
+
+template <typename DT, int TT>
+__global__ void __launch_bounds__(256) k_linrec_walk(const LinrecArgs a) {
+  const long C = (long)a.B * a.H, group = (long)blockIdx.x * (blockDim.x >> 6) + uniform(threadIdx.x >> 6);
+  if (group * 64 >= C) return;
+  const Lanes l(group, a.T, a.B, a.H, a.lengths);
+  Resets<TT> rb;
+  rb.ask(a.resets, l, 0, l.most, a.B);
+  Rows<DT> g(a.gate, l, 0), x(a.x, l, 0), y(SeqView{a.y, C, a.H}, l, 0);
+  typename Chan<DT>::raw gr[TT], xr[TT];
+  if (l.most > 0)
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      gr[i] = g.load();
+      xr[i] = x.load();
+      g.move(i + 1 < l.most ? g.st : 0);
+      x.move(i + 1 < l.most ? x.st : 0);
+    }
+  float h = a.h0 && l.on ? a.h0[l.c] : 0.0f;
+  for (int t0 = 0; t0 < l.most; t0 += TT) {
+    const uint32_t rs = rb.bits(a.resets, l, t0, l.most, a.B);
+    const int steps = min(l.most - t0, TT), live = min(max(l.n - t0, 0), TT), ahead = l.most - t0 - TT;
+    const bool masked = !__all(live == TT && rs == 0);
+    if (ahead > 0) rb.ask(a.resets, l, t0 + TT, l.most, a.B);
+    if (a.states && l.on) a.states[(long)(t0 / kTT) * C + l.c] = h;
+    if (ahead > 0)
+      h = masked ? walk_tile<true, true, DT, TT>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on)
+                 : walk_tile<true, false, DT, TT>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on);
+    else
+      h = masked ? walk_tile<false, true, DT, TT>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on)
+                 : walk_tile<false, false, DT, TT>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on);
+  }
+  // padding of every row of the wave
+  y.to(l.most);
+  for (int t = l.most; t < a.T; ++t, y.move(y.st))
+    if (l.on) y.put(0.0f);
+  if (a.h_T && l.on) a.h_T[l.c] = h;
+}
+
+// From the last tile to the first; in each forward from the saved state, then
+// backward.  Of each step e^-|gate| with the gate's sign and h_{t-1} - x stay in
+// registers; the gates come from them again on the way back, which costs less
+// than to keep them (half the waves).  Masks are looked at step by step: with a second loop for tiles
+// without them the compiler loads both ways' next values ahead of the branch, 48
+// registers too many, and selections in every step keep as many conditions in
+// scalar registers.
+template <typename DT, int TT>
+__global__ void __launch_bounds__(256, 4) k_linrec_grad_walk(const LinrecGradArgs a) {
+  const long C = (long)a.B * a.H, group = (long)blockIdx.x * (blockDim.x >> 6) + uniform(threadIdx.x >> 6);
+  if (group * 64 >= C) return;
+  const Lanes l(group, a.T, a.B, a.H, a.lengths);
+  Rows<DT> dx(a.dx, l, l.most), dg(a.dgate, l, l.most);
+  for (int t = l.most; t < a.T; ++t, dx.move(dx.st), dg.move(dg.st))
+    if (l.on) {
+      dx.put(0.0f);
+      dg.put(0.0f);
+    }
+  float R = a.dh_T && l.on ? a.dh_T[l.c] : 0.0f;
+  if (l.most > 0) {
+    int t0 = (l.most - 1) / TT * TT;
+    Resets<TT> rb;
+    rb.ask(a.resets, l, t0, l.most, a.B);
+    Rows<DT> g(a.gate, l, t0), x(a.x, l, t0), d(a.dy, l, t0);
+    typename Chan<DT>::raw gr[TT], xr[TT], dr[TT];
+    // the last tile, which may be short: a step past the end reads the last one's place
+#pragma unroll
+    for (int i = 0; i < TT; ++i) {
+      gr[i] = g.load();
+      xr[i] = x.load();
+      dr[i] = d.load();
+      const bool more = t0 + i + 1 < l.most;
+      g.move(more ? g.st : 0);
+      x.move(more ? x.st : 0);
+      d.move(more ? d.st : 0);
+    }
+    float s = l.on ? a.states[(long)(t0 / kTT) * C + l.c] : 0.0f;
+    for (; t0 >= 0; t0 -= TT) {
+      uint32_t rs = rb.bits(a.resets, l, t0, l.most, a.B);
+      int live = min(max(l.n - t0, 0), TT), lim = l.on ? min(l.most - t0, TT) : 0;
+      const bool masked = !__all(live == TT && rs == 0);
+      // the tile before it (the first one reads its first step again, for nothing), dy from its end
+      const int tb = max(t0 - TT, 0);
+      rb.ask(a.resets, l, tb, l.most, a.B);
+      const bool more = t0 > 0;
+      g.to(tb);
+      x.to(tb);
+      d.to(max(t0 - 1, 0));
+      const float before = l.on ? a.states[(long)(tb / kTT) * C + l.c] : 0.0f;
+      float E[TT], K[TT];
+#pragma unroll
+      for (int i = 0; i < TT; ++i) {
+        const float gv = Chan<DT>::get(gr[i]), xv = Chan<DT>::get(xr[i]);
+        gr[i] = g.load();
+        g.move(more ? g.st : 0);
+        E[i] = copysignf(gate_exp(gv), gv);
+        const float2 p = gate_pair_of(gv, fabsf(E[i]));
+        if (masked) s = (rs >> i) & 1u ? 0.0f : s;
+        K[i] = s - xv;
+        float to = fmaf(p.x, s, p.y * xv);
+        if (masked) to = i < live ? to : s;
+        s = to;
+        // the step ends here: drawn out over the tile, its parts would not fit the registers
+        asm volatile("" : "+v"(s), "+v"(E[i]), "+v"(K[i]));
+      }
+      dx.to(t0 + TT - 1);
+      dg.to(t0 + TT - 1);
+      // the steps' conditions anew: kept from above they would fill the scalar registers
+      asm volatile("" : "+v"(rs), "+v"(live), "+v"(lim));
+#pragma unroll
+      for (int i = TT - 1; i >= 0; --i) {
+        const float2 p = gate_pair_of(E[i], fabsf(E[i]));
+        const float D = R + Chan<DT>::get(dr[i]);
+        dr[i] = d.load();
+        d.move(more ? -d.st : 0);
+        xr[TT - 1 - i] = x.load();  // (into what the steps done leave free)
+        x.move(more ? x.st : 0);
+        const float ox = p.y * D, og = p.x * K[i] * ox;
+        if (masked) {
+          const bool in = i < live;
+          if (i < lim) {
+            dx.put(in ? ox : 0.0f);
+            dg.put(in ? og : 0.0f);
+          }
+          R = in ? ((rs >> i) & 1u ? 0.0f : p.x * D) : R;
+        } else {
+          dx.put(ox);
+          dg.put(og);
+          R = p.x * D;
+        }
+        dx.move(-dx.st);
+        dg.move(-dg.st);
+      }
+      s = before;
+    }
+  }
+  if (a.dh0 && l.on) a.dh0[l.c] = R;
+}
+
+// ---------------------------------------------------------------------------
+// The time axis split
+// ---------------------------------------------------------------------------
+
+// A wave's tile: the masks of its steps.
+struct Tile : Lanes {
+  int t0, nt, some; // the tile's steps; those inside some row's length
+  int live;         // those inside the lane's row
+  uint32_t rs;      // bit i: step i starts anew
+  __device__ Tile(long group, int t0_, int T, int B, int H, const int32_t* lengths)
+      : Lanes(group, T, B, H, lengths), t0(t0_), rs(0) {
+    nt = min(max(T - t0, 0), kTT);
+    some = min(max(most - t0, 0), kTT);
+    live = min(max(n - t0, 0), kTT);
   }
   __device__ bool reset(int i) const { return (rs >> i) & 1u; }
   // whether every step of every lane counts and none starts anew
-  __device__ bool whole() const { return __all(live == TT && rs == 0); }
+  __device__ bool whole() const { return __all(live == kTT && rs == 0); }
 };
 
-// A [T, B, H] array at a wave's tile: the step's row of the wave's first lane
-// in scalar registers, the lane's place from there as a 32-bit offset (the
-// launch checks that the rows that a wave can reach lie within 2 GiB).
-template <typename DT, int TT, int V>
-struct At {
-  char* p;
-  long step;     // bytes
-  uint32_t off;
-  __device__ At(const void* base, long st, long sb, const Tile<TT, V>& k) {
-    p = reinterpret_cast<char*>(const_cast<void*>(base)) + ((long)k.t0 * st + (long)k.b0 * sb) * (long)sizeof(DT);
-    step = st * (long)sizeof(DT);
-    off = (uint32_t)(((long)(k.b - k.b0) * sb + k.h) * (long)sizeof(DT));
-  }
-  __device__ char* at(int i) const { return p + i * step + off; }
-};
-
-template <typename DT, int V, int TT>
-__device__ __forceinline__ void load_tile(typename Chan<DT, V>::raw (&r)[TT], const SeqView& v, const Tile<TT, V>& k) {
-  At<DT, TT, V> q(v.p, v.t, v.b, k);
-  if (k.nt == TT) {
+template <typename DT>
+__device__ __forceinline__ void load_tile(typename Chan<DT>::raw (&r)[kTT], const SeqView& v, const Tile& k) {
+  Rows<DT> q(v, k, k.t0);
+  if (k.some == kTT) {
 #pragma unroll
-    for (int i = 0; i < TT; ++i, q.p += q.step) r[i] = Chan<DT, V>::load(q.p + q.off);
+    for (int i = 0; i < kTT; ++i, q.move(q.st)) r[i] = q.load();
   } else {
 #pragma unroll
-    for (int i = 0; i < TT; ++i, q.p += q.step) r[i] = i < k.nt ? Chan<DT, V>::load(q.p + q.off) : typename Chan<DT, V>::raw(0);
+    for (int i = 0; i < kTT; ++i, q.move(q.st)) r[i] = i < k.some ? q.load() : typename Chan<DT>::raw(0);
   }
 }
 
@@ -164,7 +394,7 @@ struct Chain {
   float* leave;       // [channels] state that leaves it, or null
   int seg0, segs;     // first segment and segments of this launch
   int t0, t1;         // its steps
-  long groups;        // channel groups of 64 V
+  long groups;        // channel groups of 64
 };
 
 __device__ __forceinline__ void publish(unsigned long long* p, Map m) {
@@ -188,81 +418,62 @@ __device__ __forceinline__ Map await(const unsigned long long* p, unsigned long 
 }
 
 // Composes n maps, `stride` words apart, in order; four loads in flight.
-template <int V>
-__device__ __forceinline__ void compose(Map (&m)[V], const unsigned long long* p, int n, long stride, unsigned* head) {
+__device__ __forceinline__ Map compose(Map m, const unsigned long long* p, int n, long stride, unsigned* head) {
   for (int i = 0; i < n; i += 4) {
-    unsigned long long w[4][V];
+    unsigned long long v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = i + k < n ? peek(p + (i + k) * stride) : 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-      if (i + k < n)
-#pragma unroll
-        for (int v = 0; v < V; ++v) w[k][v] = peek(p + (i + k) * stride + v);
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (i + k < n)
-#pragma unroll
-        for (int v = 0; v < V; ++v) m[v] = then(m[v], await(p + (i + k) * stride + v, w[k][v], head));
+      if (i + k < n) m = then(m, await(p + (i + k) * stride, v[k], head));
   }
+  return m;
 }
 
-// What the work-group's waves share: the tiles' maps, and the parts of the
-// composition over earlier segments.
-template <int V> struct Shared {
-  Map tile[kWaves][64][V];
-  Map part[kWaves][64][V];
-  float enter[64][V];
+// What the work-group's waves share: the tiles' maps, the parts of the
+// composition over earlier segments, the state that enters the launch.
+struct Shared {
+  Map tile[kWaves][64];
+  Map part[kWaves][64];
+  float enter[64];
   unsigned order;
 };
 
 // The map of everything before the segment that is `order`th in the chain
 // (identity for the first), composed by all waves of the work-group; publishes
-// the segment's own map first.  Every wave of the work-group calls it, after
-// the barrier that completes sh.tile.
-template <int V>
-__device__ __forceinline__ void before(Map (&m)[V], Shared<V>& sh, const Chain& ch, int order, long group, int waves,
-                                       bool forward) {
+// the segment's own map first.  All kWaves waves of the work-group call it,
+// after the barrier that completes sh.tile.
+__device__ __forceinline__ Map before(Shared& sh, const Chain& ch, int order, long group, bool forward) {
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
-  const long stride = ch.groups * 64 * V, at = (group * 64 + lane) * V;
-  if (w == waves - 1) {  // the segment's map
-    Map s[V];
+  const long stride = ch.groups * 64, at = group * 64 + lane;
+  const Map none{1.0f, 0.0f};
+  if (w == kWaves - 1) {  // the segment's map
+    Map s = none;
 #pragma unroll
-    for (int v = 0; v < V; ++v) s[v] = {1.0f, 0.0f};
-    for (int i = 0; i < waves; ++i)
-#pragma unroll
-      for (int v = 0; v < V; ++v) s[v] = then(s[v], sh.tile[forward ? i : waves - 1 - i][lane][v]);
-#pragma unroll
-    for (int v = 0; v < V; ++v) publish(ch.seg + order * stride + at + v, s[v]);
-    if (order % kFan == kFan - 1) {  // ... and that of its fan
-      Map f[V];
-#pragma unroll
-      for (int v = 0; v < V; ++v) f[v] = {1.0f, 0.0f};
-      compose<V>(f, ch.seg + (order - (kFan - 1)) * stride + at, kFan - 1, stride, ch.head);
-#pragma unroll
-      for (int v = 0; v < V; ++v) publish(ch.fan + order / kFan * stride + at + v, then(f[v], s[v]));
-    }
+    for (int i = 0; i < kWaves; ++i) s = then(s, sh.tile[forward ? i : kWaves - 1 - i][lane]);
+    publish(ch.seg + order * stride + at, s);
+    if (order % kFan == kFan - 1)  // ... and that of its fan
+      publish(ch.fan + order / kFan * stride + at,
+              then(compose(none, ch.seg + (order - (kFan - 1)) * stride + at, kFan - 1, stride, ch.head), s));
   }
   // whole fans before it, then the segments of its own fan: dealt to the waves in runs
   const int fans = order / kFan, n = fans + order % kFan;
-  const int i0 = n * w / waves, i1 = n * (w + 1) / waves;
-  Map p[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) p[v] = {1.0f, 0.0f};
-  if (i0 < fans) compose<V>(p, ch.fan + i0 * stride + at, min(i1, fans) - i0, stride, ch.head);
+  const int i0 = n * w / kWaves, i1 = n * (w + 1) / kWaves;
+  Map p = none;
+  if (i0 < fans) p = compose(p, ch.fan + i0 * stride + at, min(i1, fans) - i0, stride, ch.head);
   if (i1 > fans) {
     const int j = max(i0, fans);
-    compose<V>(p, ch.seg + ((long)fans * kFan + j - fans) * stride + at, i1 - j, stride, ch.head);
+    p = compose(p, ch.seg + ((long)fans * kFan + j - fans) * stride + at, i1 - j, stride, ch.head);
   }
-#pragma unroll
-  for (int v = 0; v < V; ++v) sh.part[w][lane][v] = p[v];
+  sh.part[w][lane] = p;
   __syncthreads();
+  Map m = none;
 #pragma unroll
-  for (int v = 0; v < V; ++v) m[v] = {1.0f, 0.0f};
-  for (int i = 0; i < waves; ++i)
-#pragma unroll
-    for (int v = 0; v < V; ++v) m[v] = then(m[v], sh.part[i][lane][v]);
+  for (int i = 0; i < kWaves; ++i) m = then(m, sh.part[i][lane]);
+  return m;
 }
 
-// The work-group's place: which channels, which segment.
+// The work-group's place: which channels, which segment in the chain's order.
 __device__ __forceinline__ void place(unsigned* order, const Chain& ch, long& group, int& seg) {
   if (ch.segs > 1) {
     if (threadIdx.x == 0) *order = atomicAdd(ch.head, 1u);
@@ -276,257 +487,176 @@ __device__ __forceinline__ void place(unsigned* order, const Chain& ch, long& gr
   }
 }
 
-// The tile's steps of a wave, in registers: a, u = (1 - a) x (forward) and
-// their map.  MASKED: some step is padding or starts anew, or some gate is
-// beyond kGateMost.
-template <bool MASKED, typename DT, int V, int TT>
-__device__ __forceinline__ void fold(float (&A)[TT][V], float (&U)[TT][V], Map (&m)[V],
-                                     const typename Chan<DT, V>::raw (&xr)[TT], const typename Chan<DT, V>::raw (&gr)[TT],
-                                     const Tile<TT, V>& k) {
-#pragma unroll
-  for (int i = 0; i < TT; ++i) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float g = Chan<DT, V>::get(gr[i], v), x = Chan<DT, V>::get(xr[i], v);
-      if constexpr (MASKED) {
-        const float2 p = gate_pair(g);
-        const bool live = i < k.live;
-        A[i][v] = live ? (k.reset(i) ? -1.0f : p.x) : 1.0f;
-        U[i][v] = live ? p.y * x : 0.0f;
-        m[v] = then(m[v], {A[i][v], U[i][v]});
-      } else {
-        const float2 p = gate_pair_small(g);
-        A[i][v] = p.x;
-        U[i][v] = p.y * x;
-        m[v].A *= p.x;
-        m[v].U = fmaf(p.x, m[v].U, U[i][v]);
-      }
-    }
-  }
-}
-
-template <typename DT, int V, int TT>
-__device__ __forceinline__ bool small_gates(const typename Chan<DT, V>::raw (&gr)[TT]) {
+template <typename DT>
+__device__ __forceinline__ bool small_gates(const typename Chan<DT>::raw (&gr)[kTT]) {
   uint32_t most = 0;
 #pragma unroll
-  for (int i = 0; i < TT; ++i) most = max(most, Chan<DT, V>::size(gr[i]));
+  for (int i = 0; i < kTT; ++i) most = max(most, __float_as_uint(Chan<DT>::get(gr[i])) & 0x7fffffffu);
   return __all(most <= __float_as_uint(kGateMost));  // NaN and infinity lie above
 }
 
-// waves: tiles of a segment; with one wave per segment the work-group holds
-// blockDim / 64 channel groups instead.
-template <typename DT, int V, int TT>
-__global__ void __launch_bounds__(64 * kWaves) k_linrec(const LinrecArgs a, const Chain ch, int waves) {
-  __shared__ Shared<V> sh;
-  typedef Chan<DT, V> Ch;
-  const int lane = threadIdx.x & 63;
-  int w = uniform(threadIdx.x >> 6), seg;
+// Folds the tile's steps into its map; keeps a and u = (1 - a) x of each.
+// MASKED: some step is padding or starts anew, or some gate is beyond
+// kGateMost.
+template <bool MASKED, typename DT>
+__device__ __forceinline__ Map fold(float (&A)[kTT], float (&U)[kTT], const typename Chan<DT>::raw (&xr)[kTT],
+                                    const typename Chan<DT>::raw (&gr)[kTT], const Tile& k) {
+  Map m{1.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < kTT; ++i) {
+    if (MASKED && i >= k.some) continue;
+    const float g = Chan<DT>::get(gr[i]), x = Chan<DT>::get(xr[i]);
+    if constexpr (MASKED) {
+      const float2 p = gate_pair(g);
+      const bool live = i < k.live;
+      A[i] = live ? (k.reset(i) ? -1.0f : p.x) : 1.0f;
+      U[i] = live ? p.y * x : 0.0f;
+      m = then(m, {A[i], U[i]});
+    } else {
+      const float2 p = gate_pair_small(g);
+      A[i] = p.x;
+      U[i] = p.y * x;
+      m.A *= p.x;
+      m.U = fmaf(p.x, m.U, U[i]);
+    }
+  }
+  return m;
+}
+
+template <typename DT>
+__global__ void __launch_bounds__(64 * kWaves) k_linrec_split(const LinrecArgs a, const Chain ch, int waves) {
+  __shared__ Shared sh;
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
+  const long C = (long)a.B * a.H;
+  int seg;
   long group;
   place(&sh.order, ch, group, seg);
-  if (waves == 1) group = group * (blockDim.x >> 6) + w, w = 0;
-  const Tile<TT, V> k(group, (ch.seg0 + seg) * waves * TT + w * TT, a.T, a.B, a.H, a.resets, a.lengths);
-  typename Ch::raw xr[TT], gr[TT];
-  load_tile<DT, V, TT>(gr, a.gate, k);
-  load_tile<DT, V, TT>(xr, a.x, k);
-  float h[V];
+  Tile k(group, ((ch.seg0 + seg) * waves + w) * kTT, a.T, a.B, a.H, a.lengths);
+  Resets<kTT> rb;
+  rb.ask(a.resets, k, k.t0, a.T, a.B);
+  typename Chan<DT>::raw xr[kTT], gr[kTT];
+  load_tile<DT>(gr, a.gate, k);
+  load_tile<DT>(xr, a.x, k);
+  k.rs = rb.bits(a.resets, k, k.t0, a.T, a.B);
+  float h = w == 0 && ch.enter && k.on ? ch.enter[k.c] : 0.0f;
+  float A[kTT], U[kTT];
+  const bool whole = k.whole() && small_gates<DT>(gr);
+  sh.tile[w][lane] = whole ? fold<false, DT>(A, U, xr, gr, k) : fold<true, DT>(A, U, xr, gr, k);
+  if (w == 0) sh.enter[lane] = h;  // read once, before anything of this row may be written
+  __syncthreads();
+  h = sh.enter[lane];
+  if (ch.segs > 1) h = apply(before(sh, ch, seg, group, true), h);
 #pragma unroll
-  for (int v = 0; v < V; ++v) h[v] = w == 0 && ch.enter && k.on ? ch.enter[k.c + v] : 0.0f;
-  float A[TT][V], U[TT][V];
-  Map m[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) m[v] = {1.0f, 0.0f};
-  const bool whole = k.whole() && small_gates<DT, V, TT>(gr);
-  if (whole)
-    fold<false, DT, V, TT>(A, U, m, xr, gr, k);
-  else
-    fold<true, DT, V, TT>(A, U, m, xr, gr, k);
-  if (waves > 1) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      sh.tile[w][lane][v] = m[v];
-      if (w == 0) sh.enter[lane][v] = h[v];  // read once, before anything of this row may be written
-    }
-    __syncthreads();
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = sh.enter[lane][v];
-    if (ch.segs > 1) {
-      Map e[V];
-      before<V>(e, sh, ch, seg, group, waves, true);
-#pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = apply(e[v], h[v]);
-    }
-    if (a.states && w == 0 && k.on)
-#pragma unroll
-      for (int v = 0; v < V; ++v) a.states[(long)(ch.seg0 + seg) * a.B * a.H + k.c + v] = h[v];
-    for (int i = 0; i < w; ++i)
-#pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = apply(sh.tile[i][lane][v], h[v]);
-  } else if (a.states && k.on) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) a.states[k.c + v] = h[v];
-  }
-  At<DT, TT, V> y(a.y, (long)a.B * a.H, a.H, k);
+  for (int i = 0; i < kWaves - 1; ++i)
+    if (i < w) h = apply(sh.tile[i][lane], h);
+  if (a.states && k.on && k.nt > 0) a.states[(long)(k.t0 / kTT) * C + k.c] = h;
+  Rows<DT> y(SeqView{a.y, C, a.H}, k, k.t0);
   if (whole) {
 #pragma unroll
-    for (int i = 0; i < TT; ++i, y.p += y.step) {
-#pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = fmaf(A[i][v], h[v], U[i][v]);
-      Ch::put(y.p + y.off, h);
+    for (int i = 0; i < kTT; ++i, y.move(y.st)) {
+      h = fmaf(A[i], h, U[i]);
+      y.put(h);
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < TT; ++i, y.p += y.step) {
-      float o[V];
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        h[v] = apply({A[i][v], U[i][v]}, h[v]);
-        o[v] = i < k.live ? h[v] : 0.0f;
-      }
-      if (i < k.nt && k.on) Ch::put(y.p + y.off, o);
+    for (int i = 0; i < kTT; ++i, y.move(y.st)) {
+      if (i < k.some) h = apply({A[i], U[i]}, h);
+      if (i < k.nt && k.on) y.put(i < k.live ? h : 0.0f);
     }
   }
-  if (ch.leave && k.on && k.t0 + TT >= ch.t1 && k.t0 < max(ch.t1, 1))
-#pragma unroll
-    for (int v = 0; v < V; ++v) ch.leave[k.c + v] = h[v];
+  if (ch.leave && k.on && k.t0 + kTT >= ch.t1 && k.t0 < ch.t1) ch.leave[k.c] = h;
 }
 
-// The gradient's tile: a and 1 - a of its steps, the map of h and that of R,
+// The gradient's tile: a and 1 - a of its steps, what h_{t-1} puts into dgate,
+// and the map of R:
 //   R_out = sum_i (prod_{j <= i} a_j) dy_i + (prod a) R_in.
-template <bool MASKED, typename DT, int V, int TT>
-__device__ __forceinline__ void fold_grad(float (&A)[TT][V], float (&M)[TT][V], Map (&m)[V], Map (&r)[V],
-                                          const typename Chan<DT, V>::raw (&xr)[TT],
-                                          const typename Chan<DT, V>::raw (&gr)[TT],
-                                          const typename Chan<DT, V>::raw (&dr)[TT], const Tile<TT, V>& k) {
+template <bool MASKED, typename DT>
+__device__ __forceinline__ Map fold_grad(float (&A)[kTT], float (&M)[kTT], float (&G)[kTT], float h,
+                                         const typename Chan<DT>::raw (&xr)[kTT],
+                                         const typename Chan<DT>::raw (&gr)[kTT],
+                                         const typename Chan<DT>::raw (&dr)[kTT], const Tile& k) {
+  Map r{1.0f, 0.0f};
 #pragma unroll
-  for (int i = 0; i < TT; ++i) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float g = Chan<DT, V>::get(gr[i], v), x = Chan<DT, V>::get(xr[i], v), d = Chan<DT, V>::get(dr[i], v);
-      const float2 p = MASKED ? gate_pair(g) : gate_pair_small(g);
-      A[i][v] = p.x;
-      M[i][v] = p.y;
-      if constexpr (MASKED) {
-        if (i < k.live) {
-          const bool cut = k.reset(i);
-          m[v] = then(m[v], {cut ? -1.0f : p.x, p.y * x});
-          if (cut) r[v].A = -1.0f;
-          if (!(r[v].A < 0.0f)) {
-            r[v].A *= p.x;
-            r[v].U = fmaf(r[v].A, d, r[v].U);
-          }
+  for (int i = 0; i < kTT; ++i) {
+    if (MASKED && i >= k.some) continue;
+    const float g = Chan<DT>::get(gr[i]), x = Chan<DT>::get(xr[i]), d = Chan<DT>::get(dr[i]);
+    const float2 p = MASKED ? gate_pair(g) : gate_pair_small(g);
+    A[i] = p.x;
+    M[i] = p.y;
+    if (MASKED && k.reset(i)) h = 0.0f;
+    G[i] = p.x * p.y * (h - x);
+    const float to = fmaf(p.x, h, p.y * x);
+    if constexpr (MASKED) {
+      if (i < k.live) {
+        h = to;
+        if (k.reset(i)) r.A = -1.0f;
+        if (!(r.A < 0.0f)) {
+          r.A *= p.x;
+          r.U = fmaf(r.A, d, r.U);
         }
-      } else {
-        m[v].A *= p.x;
-        m[v].U = fmaf(p.x, m[v].U, p.y * x);
-        r[v].U = fmaf(m[v].A, d, r[v].U);
       }
+    } else {
+      h = to;
+      r.A *= p.x;
+      r.U = fmaf(r.A, d, r.U);
     }
   }
-  if constexpr (!MASKED)
-#pragma unroll
-    for (int v = 0; v < V; ++v) r[v].A = m[v].A;
+  return r;
 }
 
-template <bool MASKED, typename DT, int V, int TT>
-__device__ __forceinline__ void emit_grad(float (&A)[TT][V], float (&M)[TT][V], float (&h)[V], float (&R)[V],
-                                          const typename Chan<DT, V>::raw (&xr)[TT],
-                                          const typename Chan<DT, V>::raw (&dr)[TT], const Tile<TT, V>& k,
-                                          const LinrecGradArgs& a) {
-  typedef Chan<DT, V> Ch;
-  // forward: what h_{t-1} puts into dgate
-  float G[TT][V];
+template <bool MASKED, typename DT>
+__device__ __forceinline__ float emit_grad(const float (&A)[kTT], const float (&M)[kTT], const float (&G)[kTT], float R,
+                                           const typename Chan<DT>::raw (&dr)[kTT], const Tile& k,
+                                           const LinrecGradArgs& a) {
+  Rows<DT> dx(a.dx, k, k.t0 + kTT - 1), dg(a.dgate, k, k.t0 + kTT - 1);
 #pragma unroll
-  for (int i = 0; i < TT; ++i) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float x = Ch::get(xr[i], v);
-      if (MASKED && k.reset(i)) h[v] = 0.0f;
-      G[i][v] = A[i][v] * M[i][v] * (h[v] - x);
-      if (!MASKED || i < k.live) h[v] = fmaf(A[i][v], h[v], M[i][v] * x);
-    }
-  }
-  At<DT, TT, V> dx(a.dx.p, a.dx.t, a.dx.b, k), dg(a.dgate.p, a.dgate.t, a.dgate.b, k);
-  dx.p += (TT - 1) * dx.step;
-  dg.p += (TT - 1) * dg.step;
-#pragma unroll
-  for (int i = TT - 1; i >= 0; --i, dx.p -= dx.step, dg.p -= dg.step) {
-    float ox[V], og[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
+  for (int i = kTT - 1; i >= 0; --i, dx.move(-dx.st), dg.move(-dg.st)) {
+    float ox = 0.0f, og = 0.0f;
+    if (!MASKED || i < k.some) {
       const bool live = !MASKED || i < k.live;
-      const float D = R[v] + Ch::get(dr[i], v);
-      ox[v] = live ? M[i][v] * D : 0.0f;
-      og[v] = live ? G[i][v] * D : 0.0f;
-      R[v] = live ? (MASKED && k.reset(i) ? 0.0f : A[i][v] * D) : R[v];
+      const float D = R + Chan<DT>::get(dr[i]);
+      ox = live ? M[i] * D : 0.0f;
+      og = live ? G[i] * D : 0.0f;
+      R = live ? (MASKED && k.reset(i) ? 0.0f : A[i] * D) : R;
     }
     if (!MASKED || (i < k.nt && k.on)) {
-      Ch::put(dx.p + dx.off, ox);
-      Ch::put(dg.p + dg.off, og);
+      dx.put(ox);
+      dg.put(og);
     }
   }
+  return R;
 }
 
-template <typename DT, int V, int TT>
-__global__ void __launch_bounds__(64 * kWaves) k_linrec_grad(const LinrecGradArgs a, const Chain ch, int waves) {
-  __shared__ Shared<V> sh;
-  __shared__ Map fwd[kWaves][64][V];
-  typedef Chan<DT, V> Ch;
-  const int lane = threadIdx.x & 63;
-  int w = uniform(threadIdx.x >> 6), order;
+template <typename DT>
+__global__ void __launch_bounds__(64 * kWaves) k_linrec_grad_split(const LinrecGradArgs a, const Chain ch, int waves) {
+  __shared__ Shared sh;
+  const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
+  int order;
   long group;
   place(&sh.order, ch, group, order);
   const int seg = ch.seg0 + ch.segs - 1 - order;  // the chain runs from the last segment to the first
-  if (waves == 1) group = group * (blockDim.x >> 6) + w, w = 0;
-  const Tile<TT, V> k(group, seg * waves * TT + w * TT, a.T, a.B, a.H, a.resets, a.lengths);
-  typename Ch::raw xr[TT], gr[TT], dr[TT];
-  load_tile<DT, V, TT>(gr, a.gate, k);
-  load_tile<DT, V, TT>(xr, a.x, k);
-  load_tile<DT, V, TT>(dr, a.dy, k);
-  float h[V], R[V];
+  Tile k(group, (seg * waves + w) * kTT, a.T, a.B, a.H, a.lengths);
+  Resets<kTT> rb;
+  rb.ask(a.resets, k, k.t0, a.T, a.B);
+  typename Chan<DT>::raw xr[kTT], gr[kTT], dr[kTT];
+  load_tile<DT>(gr, a.gate, k);
+  load_tile<DT>(xr, a.x, k);
+  load_tile<DT>(dr, a.dy, k);
+  const float h = k.on && k.nt > 0 ? a.states[(long)(k.t0 / kTT) * a.B * a.H + k.c] : 0.0f;
+  k.rs = rb.bits(a.resets, k, k.t0, a.T, a.B);
+  float R = w == waves - 1 && ch.enter && k.on ? ch.enter[k.c] : 0.0f;
+  float A[kTT], M[kTT], G[kTT];
+  const bool whole = k.whole() && small_gates<DT>(gr);
+  sh.tile[w][lane] = whole ? fold_grad<false, DT>(A, M, G, h, xr, gr, dr, k) : fold_grad<true, DT>(A, M, G, h, xr, gr, dr, k);
+  if (w == waves - 1) sh.enter[lane] = R;  // read once, before anything of this row may be written
+  __syncthreads();
+  R = sh.enter[lane];
+  if (ch.segs > 1) R = apply(before(sh, ch, order, group, false), R);
 #pragma unroll
-  for (int v = 0; v < V; ++v) {
-    h[v] = k.on ? a.states[(long)seg * a.B * a.H + k.c + v] : 0.0f;
-    R[v] = w == waves - 1 && ch.enter && k.on ? ch.enter[k.c + v] : 0.0f;
-  }
-  float A[TT][V], M[TT][V];  // a, 1 - a
-  Map m[V], r[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) m[v] = r[v] = {1.0f, 0.0f};
-  const bool whole = k.whole() && small_gates<DT, V, TT>(gr);
-  if (whole)
-    fold_grad<false, DT, V, TT>(A, M, m, r, xr, gr, dr, k);
-  else
-    fold_grad<true, DT, V, TT>(A, M, m, r, xr, gr, dr, k);
-  if (waves > 1) {
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      fwd[w][lane][v] = m[v];
-      sh.tile[w][lane][v] = r[v];
-      if (w == waves - 1) sh.enter[lane][v] = R[v];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int v = 0; v < V; ++v) R[v] = sh.enter[lane][v];
-    if (ch.segs > 1) {
-      Map e[V];
-      before<V>(e, sh, ch, order, group, waves, false);
-#pragma unroll
-      for (int v = 0; v < V; ++v) R[v] = apply(e[v], R[v]);
-    }
-    for (int i = 0; i < w; ++i)
-#pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = apply(fwd[i][lane][v], h[v]);
-    for (int i = waves - 1; i > w; --i)
-#pragma unroll
-      for (int v = 0; v < V; ++v) R[v] = apply(sh.tile[i][lane][v], R[v]);
-  }
-  if (whole)
-    emit_grad<false, DT, V, TT>(A, M, h, R, xr, dr, k, a);
-  else
-    emit_grad<true, DT, V, TT>(A, M, h, R, xr, dr, k, a);
-  if (ch.leave && k.on && k.t0 == ch.t0)
-#pragma unroll
-    for (int v = 0; v < V; ++v) ch.leave[k.c + v] = R[v];
+  for (int i = kWaves - 1; i > 0; --i)
+    if (i > w && i < waves) R = apply(sh.tile[i][lane], R);
+  R = whole ? emit_grad<false, DT>(A, M, G, R, dr, k, a) : emit_grad<true, DT>(A, M, G, R, dr, k, a);
+  if (ch.leave && k.on && k.t0 == ch.t0) ch.leave[k.c] = R;
 }
 
 // Empties the maps of a launch, and copies the state that enters it (which the
@@ -540,31 +670,31 @@ __global__ void __launch_bounds__(256) k_linrec_init(const Chain ch, long words,
     for (long j = i; j < C; j += step) const_cast<float*>(ch.enter)[j] = from[j];
 }
 
-// How a call of T steps is split: steps of a tile, tiles of a segment, segments.
+// How a call is split.  waves = 0: not at all.
 struct Plan {
-  int tt, waves;
+  int waves;  // tiles of a segment
   long segs;
 };
-Plan plan(int T) {
-  if (T <= 1) return {1, 1, 1};
-  const int tiles = (int)(((long)T + kTT - 1) / kTT);
-  if (tiles <= kWaves) return {kTT, tiles, 1};
-  return {kTT, kWaves, (tiles + kWaves - 1) / kWaves};
+Plan plan(int T, int B, int H) {
+  const long groups = ((long)B * H + 63) / 64, tiles = ((long)T + kTT - 1) / kTT;
+  if (tiles <= 1 || groups >= kWalk) return {0, 0};
+  if (tiles <= kWaves) return {(int)tiles, 1};
+  return {kWaves, (tiles + kWaves - 1) / kWaves};
 }
 
 // The workspace of a call with several segments.
 constexpr size_t kHeadBytes = kSyncWords * sizeof(unsigned);
-long pad_channels(int B, int H) { return ((long)B * H + 127) / 128 * 128; }  // whole groups, of one or two channels a lane
+long pad_channels(int B, int H) { return ((long)B * H + 63) / 64 * 64; }  // whole groups
 long map_words(long segs, long channels) { return (segs + segs / kFan) * channels; }
 
 // Runs go(Chain, first launch, last launch) for every launch of a call, in
 // order; `from` is the state that enters the call, `to` the one that leaves it.
 template <typename F>
-hipError_t run_chain(int T, int B, int H, int V, const Plan& p, void* ws, const float* from, float* to, bool reverse,
+hipError_t run_chain(int T, int B, int H, const Plan& p, void* ws, const float* from, float* to, bool reverse,
                      hipStream_t s, F go) {
-  const long C = (long)B * H, groups = (C + 64 * V - 1) / (64 * V);
+  const long C = (long)B * H, pad = pad_channels(B, H);
   Chain ch{};
-  ch.groups = groups;
+  ch.groups = pad / 64;
   if (p.segs == 1) {
     ch.enter = from;
     ch.leave = to;
@@ -572,7 +702,7 @@ hipError_t run_chain(int T, int B, int H, int V, const Plan& p, void* ws, const 
     ch.t1 = T;
     return go(ch);
   }
-  const long most = std::min<long>(p.segs, kMaxSegs), pad = pad_channels(B, H);
+  const long most = std::min<long>(p.segs, kMaxSegs);
   char* base = reinterpret_cast<char*>(ws);
   ch.head = reinterpret_cast<unsigned*>(base);
   ch.seg = reinterpret_cast<unsigned long long*>(base + kHeadBytes);
@@ -585,11 +715,11 @@ hipError_t run_chain(int T, int B, int H, int V, const Plan& p, void* ws, const 
     ch.segs = (int)std::min<long>(kMaxSegs, p.segs - s0);
     ch.t0 = (int)(s0 * kSeg);
     ch.t1 = (int)std::min<long>(T, (s0 + ch.segs) * kSeg);
-    ch.fan = ch.seg + ch.segs * groups * 64 * V;
+    ch.fan = ch.seg + ch.segs * pad;
     const float* f = n == 0 ? from : carry;
     ch.enter = f ? enter : nullptr;
     ch.leave = n == launches - 1 ? to : carry;
-    const long words = map_words(ch.segs, groups * 64 * V);
+    const long words = map_words(ch.segs, pad);
     const unsigned grid = (unsigned)std::min<long>(1024, (std::max(words, C) + 255) / 256);
     hipError_t e = launch("linrec_init", k_linrec_init, dim3(grid), dim3(256), 0, s, ch, words, f, C, n == 0);
     if (e == hipSuccess) e = go(ch);
@@ -598,40 +728,42 @@ hipError_t run_chain(int T, int B, int H, int V, const Plan& p, void* ws, const 
   return hipSuccess;
 }
 
-template <int V, typename K, typename A>
-hipError_t run(const char* name, K tile, K step, const A& a, const float* from, float* to, bool reverse, hipStream_t s) {
-  const Plan p = plan(a.T);
-  return run_chain(a.T, a.B, a.H, V, p, a.ws, from, to, reverse, s, [&](const Chain& ch) {
-    // a work-group of one tile per segment holds four channel groups
-    const int per = p.waves == 1 ? 4 : 1;
-    const long grid = (ch.groups + per - 1) / per * ch.segs;
-    return launch(name, p.tt == 1 ? step : tile, dim3((unsigned)grid), dim3(64u * (p.waves == 1 ? per : p.waves)), 0, s, a,
-                  ch, p.waves);
+template <typename W, typename S, typename A>
+hipError_t run(const char* name, W walk, W step, S split, const A& a, const float* from, float* to, bool reverse,
+               hipStream_t s) {
+  const Plan p = plan(a.T, a.B, a.H);
+  if (p.waves == 0) {
+    const long groups = ((long)a.B * a.H + 63) / 64;
+    return launch(name, a.T <= 1 ? step : walk, dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, s, a);
+  }
+  return run_chain(a.T, a.B, a.H, p, a.ws, from, to, reverse, s, [&](const Chain& ch) {
+    return launch(name, split, dim3((unsigned)(ch.groups * ch.segs)), dim3(64u * p.waves), 0, s, a, ch, p.waves);
   });
 }
 
 }  // namespace
 
-size_t linrec_states(int T, int B, int H) { return (size_t)plan(T).segs * B * H * sizeof(float); }
+size_t linrec_states(int T, int B, int H) { return ((size_t)T + kTT - 1) / kTT * B * H * sizeof(float); }
 
 size_t linrec_workspace(int T, int B, int H) {
-  const Plan p = plan(T);
-  if (p.segs == 1) return 0;
+  const Plan p = plan(T, B, H);
+  if (p.segs <= 1) return 0;
   const long pad = pad_channels(B, H);
   return kHeadBytes + (size_t)map_words(std::min<long>(p.segs, kMaxSegs), pad) * 8 + (size_t)pad * 2 * sizeof(float);
 }
 
 hipError_t launch_linrec(int dtype, const LinrecArgs& a, hipStream_t s) {
-  if (dtype == WM_FP32) return run<1>("linrec", k_linrec<float, 1, kTT>, k_linrec<float, 1, 1>, a, a.h0, a.h_T, false, s);
-  if (a.H % 2 == 0)
-    return run<2>("linrec", k_linrec<bf16_t, 2, kTT>, k_linrec<bf16_t, 2, 1>, a, a.h0, a.h_T, false, s);
-  return run<1>("linrec", k_linrec<bf16_t, 1, kTT>, k_linrec<bf16_t, 1, 1>, a, a.h0, a.h_T, false, s);
+  return dtype == WM_FP32 ? run("linrec", k_linrec_walk<float, kTT>, k_linrec_walk<float, 1>, k_linrec_split<float>, a,
+                                a.h0, a.h_T, false, s)
+                          : run("linrec", k_linrec_walk<bf16_t, kTT>, k_linrec_walk<bf16_t, 1>, k_linrec_split<bf16_t>, a,
+                                a.h0, a.h_T, false, s);
 }
 
 hipError_t launch_linrec_grad(int dtype, const LinrecGradArgs& a, hipStream_t s) {
-  if (dtype == WM_FP32)
-    return run<1>("linrec_grad", k_linrec_grad<float, 1, kTT>, k_linrec_grad<float, 1, 1>, a, a.dh_T, a.dh0, true, s);
-  return run<1>("linrec_grad", k_linrec_grad<bf16_t, 1, kTT>, k_linrec_grad<bf16_t, 1, 1>, a, a.dh_T, a.dh0, true, s);
+  return dtype == WM_FP32 ? run("linrec_grad", k_linrec_grad_walk<float, kTT>, k_linrec_grad_walk<float, 1>,
+                                k_linrec_grad_split<float>, a, a.dh_T, a.dh0, true, s)
+                          : run("linrec_grad", k_linrec_grad_walk<bf16_t, kTT>, k_linrec_grad_walk<bf16_t, 1>,
+                                k_linrec_grad_split<bf16_t>, a, a.dh_T, a.dh0, true, s);
 }
 
 }  // namespace wm

@@ -98,27 +98,28 @@ hipError_t launch_linrec_grad(int dtype, const LinrecGradArgs& a, hipStream_t s)
 size_t clip_workspace(int n, const wm_grad_tensor* t);
 hipError_t launch_clip(int n, const wm_grad_tensor* t, float max_norm, float* norm, void* ws, hipStream_t s);
 
-// (sigmoid(g), sigmoid(-g)), each to full relative precision, any g.
-__device__ __forceinline__ float2 gate_pair(float g) {
-  const float e = expf(-fabsf(g));
-  const float r = 1.0f / (1.0f + e), q = e * r;
-  return g >= 0.0f ? make_float2(r, q) : make_float2(q, r);
-}
-
-// The same for |g| <= kGateMost, in half the instructions.  e^-n = 2^p (1 + d)
-// with p = -n log2(e) rounded and d = -n - p ln 2 what the rounding left over;
-// 1 / (1 + e) by one Newton step from the hardware's reciprocal.
-constexpr float kGateMost = 87.0f;  // e^-87 is still a normal number
-__device__ __forceinline__ float2 gate_pair_small(float g) {
-  const float n = fabsf(g);
-  const float p = n * -1.44269504088896341f;
-  const float d = fmaf(p, -0.693147180559945309f, -n);
-  const float t = __builtin_amdgcn_exp2f(p);
-  const float e = fmaf(t, d, t), w = 1.0f + e;
+// (sigmoid(g), sigmoid(-g)), each to full relative precision, from e^-|g|:
+// 1 / (1 + e) by one Newton step from the hardware's reciprocal, and e times it.
+__device__ __forceinline__ float2 gate_pair_of(float g, float e) {
+  const float w = 1.0f + e;
   float r = __builtin_amdgcn_rcpf(w);
   r = fmaf(fmaf(-w, r, 1.0f), r, r);
   const float q = e * r;
   return g >= 0.0f ? make_float2(r, q) : make_float2(q, r);
 }
+__device__ __forceinline__ float2 gate_pair(float g) { return gate_pair_of(g, expf(-fabsf(g))); }
+
+// e^-|g| for |g| <= kGateMost, in half of expf's instructions: with p =
+// -|g| log2(e) rounded and d = -|g| - p ln 2 what the rounding left over it is
+// 2^p (1 + d).
+constexpr float kGateMost = 87.0f;  // e^-87 is still a normal number
+__device__ __forceinline__ float gate_exp_small(float g) {
+  const float n = fabsf(g);
+  const float p = n * -1.44269504088896341f;
+  const float d = fmaf(p, -0.693147180559945309f, -n);
+  const float t = __builtin_amdgcn_exp2f(p);
+  return fmaf(t, d, t);
+}
+__device__ __forceinline__ float2 gate_pair_small(float g) { return gate_pair_of(g, gate_exp_small(g)); }
 
 }  // namespace wm
