@@ -4,12 +4,14 @@
 //
 // A row is read once, in pieces of 16 bytes, and stays in registers: the mean,
 // then the sum of squares about it (not the difference of two large sums), then
-// the output.  kLanes lanes share a row: 16 for narrow ones, a wave up to 1024
-// values, and four waves, which add their parts in LDS, beyond (up to 32 values
-// a lane).  A group of lanes goes over rows in strides with gamma and beta in
+// the output.  L lanes share a row, with at most 16 values each: sixteen for
+// narrow ones, a wave up to 1024 values, and beyond four or eight waves, which
+// add their parts in LDS.  A group of lanes goes over rows in strides with gamma and beta in
 // registers, and requests the next row before it works on the present one.
 // Rows are aligned to their element only: the hardware takes 16-byte accesses
-// at such addresses, and only a row's last, partial piece goes value by value.
+// at such addresses.  A row's last, partial piece is read and written as the
+// last 16 bytes of the row, over the end of the piece before it: the values
+// that two lanes then hold count in one of them, and both write the same.
 //
 // The gradient keeps the sums of dy xh and dy for its lanes' columns in
 // registers as well; every work-group leaves one row of partial sums, which a
@@ -23,11 +25,11 @@
 namespace wm {
 namespace {
 
-constexpr int kThreads = 256;
+// threads of a work-group whose rows take L lanes each
+constexpr int threads(int L) { return L > 256 ? L : 256; }
 constexpr int kGroups = 2048;  // work-groups at most: eight a CU
-constexpr int kParts = 512;    // ... of the gradient: two a CU
 
-// Sixteen bytes of a row; piece p of lane t holds columns (kLanes p + t) VEC on.
+// Sixteen bytes of a row; piece p of lane t holds the columns from (L p + t) VEC on.
 template <typename DT> struct Piece;
 template <> struct Piece<float> {
   static constexpr int VEC = 4;
@@ -64,55 +66,96 @@ template <typename DT> struct Memory;
 template <> struct Memory<float> { typedef u32x4_4 type; };
 template <> struct Memory<bf16_t> { typedef u32x4_2 type; };
 
-// The piece at column c of a row of width H; 0 past its end.
-template <typename DT>
-__device__ __forceinline__ uint4 load_piece(const DT* row, int c, int H) {
-  if (c + Piece<DT>::VEC <= H) {
-    const u32x4 v = *reinterpret_cast<const typename Memory<DT>::type*>(row + c);
-    return make_uint4(v.x, v.y, v.z, v.w);
-  }
-  float v[Piece<DT>::VEC];
-#pragma unroll
-  for (int j = 0; j < Piece<DT>::VEC; ++j) v[j] = c + j < H ? DType<DT>::load(row, c + j) : 0.0f;
-  return Piece<DT>::put(v);
-}
-template <typename DT>
-__device__ __forceinline__ void store_piece(DT* row, int c, int H, const float* v) {
-  if (c + Piece<DT>::VEC <= H) {
-    const uint4 r = Piece<DT>::put(v);
-    *reinterpret_cast<typename Memory<DT>::type*>(row + c) = u32x4{r.x, r.y, r.z, r.w};
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < Piece<DT>::VEC; ++j)
-    if (c + j < H) DType<DT>::store(row, c + j, v[j]);
-}
+// The places of a lane's pieces in a row of width H: piece p holds the columns
+// from col[p] on, of which [lo[p], hi) are the lane's own (none where lo = VEC).
 template <typename DT, int P, int L>
-__device__ __forceinline__ void load_row(uint4 (&r)[P], const void* base, long row, long ld, int t, int H) {
-  const DT* p = reinterpret_cast<const DT*>(base) + row * ld;
+struct Place {
+  static constexpr int V = Piece<DT>::VEC;
+  int col[P], lo[P], hi;
+  __device__ Place(int t, int H) {
+    hi = min(V, H);
 #pragma unroll
-  for (int i = 0; i < P; ++i) r[i] = load_piece(p, (L * i + t) * Piece<DT>::VEC, H);
-}
-// The lane's values of a per-column array, `none` where there is none and past the row's end.
-template <typename DT, int P, int L>
-__device__ __forceinline__ void load_columns(float (&g)[P][Piece<DT>::VEC], const float* a, float none, int t, int H) {
-#pragma unroll
-  for (int p = 0; p < P; ++p)
-#pragma unroll
-    for (int j = 0; j < Piece<DT>::VEC; ++j) {
-      const int c = (L * p + t) * Piece<DT>::VEC + j;
-      g[p][j] = a && c < H ? a[c] : none;
+    for (int p = 0; p < P; ++p) {
+      const int c = (L * p + t) * V;
+      col[p] = max(min(c, H - V), 0);
+      lo[p] = min(c - col[p], V);
     }
+  }
+  __device__ bool own(int p, int j) const { return j >= lo[p] && j < hi; }
+  __device__ void load(uint4 (&r)[P], const void* base, long row, long ld) const {
+    const DT* x = reinterpret_cast<const DT*>(base) + row * ld;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      if (hi == V) {
+        const u32x4 v = *reinterpret_cast<const typename Memory<DT>::type*>(x + col[p]);
+        r[p] = make_uint4(v.x, v.y, v.z, v.w);
+      } else {  // a row narrower than a piece
+        float v[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) v[j] = j < hi ? DType<DT>::load(x, j) : 0.0f;
+        r[p] = Piece<DT>::put(v);
+      }
+    }
+  }
+  __device__ void store(DT* x, int p, const float* v) const {
+    if (lo[p] >= hi) return;
+    if (hi == V) {
+      const uint4 r = Piece<DT>::put(v);
+      *reinterpret_cast<typename Memory<DT>::type*>(x + col[p]) = u32x4{r.x, r.y, r.z, r.w};
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j < hi) DType<DT>::store(x, j, v[j]);
+    }
+  }
+  // The lane's values of a per-column array, `none` where there is none.
+  __device__ void columns(float (&g)[P][V], const float* a, float none) const {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) g[p][j] = none;
+      if (!a) continue;
+      if (hi == V) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+          const u32x4 v = *reinterpret_cast<const u32x4_4*>(a + col[p] + j);
+          Piece<float>::get(make_uint4(v.x, v.y, v.z, v.w), &g[p][j]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+          if (j < hi) g[p][j] = a[j];
+      }
+    }
+  }
+};
+
+// v plus the value of another lane of the same sixteen.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane));
+}
+// Sum over sixteen lanes, or all of the wave (L >= 64), in every one of them:
+// the neighbour, the other pair, the other four, the other eight, then the four
+// sixteens.  No step goes through LDS.
+template <int L>
+__device__ __forceinline__ float lanes_sum(float v) {
+  v = dpp_add<0xB1>(v);   // quad_perm 1 0 3 2
+  v = dpp_add<0x4E>(v);   // quad_perm 2 3 0 1
+  v = dpp_add<0x141>(v);  // row_half_mirror
+  v = dpp_add<0x140>(v);  // row_mirror
+  if constexpr (L >= 64) v = (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+  return v;
 }
 
 // Sums over the lanes of a row; two at a time.
 template <int L>
-__device__ __forceinline__ float2 row_sum(float2 v, float2 (*sh)[4], int& turn) {
-#pragma unroll
-  for (int k = (L < 64 ? L : 64) / 2; k; k >>= 1) {
-    v.x += __shfl_xor(v.x, k);
-    v.y += __shfl_xor(v.y, k);
-  }
+__device__ __forceinline__ float2 row_sum(float2 v, float2 (*sh)[8], int& turn) {
+  v.x = lanes_sum<L>(v.x);
+  v.y = lanes_sum<L>(v.y);
   if constexpr (L > 64) {
     // two places in turn: a wave may be one sum ahead of another
     if ((threadIdx.x & 63) == 0) sh[turn][threadIdx.x >> 6] = v;
@@ -129,19 +172,20 @@ __device__ __forceinline__ float2 row_sum(float2 v, float2 (*sh)[4], int& turn) 
 }
 
 template <typename DT, int P, int L>
-__global__ void __launch_bounds__(kThreads) k_norm(const NormArgs a) {
-  constexpr int V = Piece<DT>::VEC, kRows = kThreads / L;
-  __shared__ float2 sh[2][4];
+__global__ void __launch_bounds__(threads(L)) k_norm(const NormArgs a) {
+  constexpr int V = Piece<DT>::VEC, kThreads = threads(L), kRows = kThreads / L;
+  __shared__ float2 sh[2][8];
   int turn = 0;
   const int t = threadIdx.x % L;
+  const Place<DT, P, L> at(t, a.H);
   const long step = (long)gridDim.x * kRows;
   long row = (long)blockIdx.x * kRows + threadIdx.x / L;
   if (row >= a.rows) return;
   uint4 next[P];
-  load_row<DT, P, L>(next, a.x, row, a.x_ld, t, a.H);
+  at.load(next, a.x, row, a.x_ld);
   float g[P][V], b[P][V];
-  load_columns<DT, P, L>(g, a.gamma, 1.0f, t, a.H);
-  load_columns<DT, P, L>(b, a.beta, 0.0f, t, a.H);
+  at.columns(g, a.gamma, 1.0f);
+  at.columns(b, a.beta, 0.0f);
   const float inv = 1.0f / (float)a.H;
   for (; row < a.rows; row += step) {
     float v[P][V];
@@ -150,26 +194,26 @@ __global__ void __launch_bounds__(kThreads) k_norm(const NormArgs a) {
     for (int p = 0; p < P; ++p) {
       Piece<DT>::get(next[p], v[p]);
 #pragma unroll
-      for (int j = 0; j < V; ++j) s.x += v[p][j];
+      for (int j = 0; j < V; ++j) s.x += at.own(p, j) ? v[p][j] : 0.0f;
     }
-    if (row + step < a.rows) load_row<DT, P, L>(next, a.x, row + step, a.x_ld, t, a.H);
+    if (row + step < a.rows) at.load(next, a.x, row + step, a.x_ld);
     const float mu = row_sum<L>(s, sh, turn).x * inv;
     s = {0.0f, 0.0f};
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        v[p][j] = (L * p + t) * V + j < a.H ? v[p][j] - mu : 0.0f;
-        s.x = fmaf(v[p][j], v[p][j], s.x);
+        v[p][j] -= mu;
+        const float d = at.own(p, j) ? v[p][j] : 0.0f;
+        s.x = fmaf(d, d, s.x);
       }
     const float rs = 1.0f / sqrtf(row_sum<L>(s, sh, turn).x * inv + a.eps);
     DT* y = reinterpret_cast<DT*>(a.y) + row * a.y_ld;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int c = (L * p + t) * V;
 #pragma unroll
       for (int j = 0; j < V; ++j) v[p][j] = fmaf(v[p][j] * rs, g[p][j], b[p][j]);
-      if (c < a.H) store_piece(y, c, a.H, v[p]);
+      at.store(y, p, v[p]);
     }
     if (t == 0 && a.mean) {
       a.mean[row] = mu;
@@ -180,34 +224,32 @@ __global__ void __launch_bounds__(kThreads) k_norm(const NormArgs a) {
 
 // part [gridDim.x][2][H]: this work-group's sums of dy xh, then of dy.
 template <typename DT, int P, int L>
-__global__ void __launch_bounds__(kThreads) k_norm_grad(const NormGradArgs a) {
-  constexpr int V = Piece<DT>::VEC, kRows = kThreads / L;
-  constexpr bool kAhead = P * V <= 16;  // registers for the next row
-  __shared__ float2 sh[2][4];
+__global__ void __launch_bounds__(threads(L)) k_norm_grad(const NormGradArgs a) {
+  constexpr int V = Piece<DT>::VEC, kThreads = threads(L), kRows = kThreads / L;
+  __shared__ float2 sh[2][8];
   __shared__ float add[L < kThreads ? kThreads * P * V : 1];
   int turn = 0;
   const int t = threadIdx.x % L;
+  const Place<DT, P, L> at(t, a.H);
   const float inv = 1.0f / (float)a.H;
   const long step = (long)gridDim.x * kRows;
   long row = (long)blockIdx.x * kRows + threadIdx.x / L;
   uint4 xr[P], dr[P];
   float mu = 0.0f, rs = 0.0f;
   auto load = [&](long i) {
-    load_row<DT, P, L>(xr, a.x, i, a.x_ld, t, a.H);
-    load_row<DT, P, L>(dr, a.dy, i, a.dy_ld, t, a.H);
+    at.load(xr, a.x, i, a.x_ld);
+    at.load(dr, a.dy, i, a.dy_ld);
     mu = a.mean[i];
     rs = a.rstd[i];
   };
   if (row < a.rows) load(row);
   float g[P][V], dg[P][V], db[P][V];
-  load_columns<DT, P, L>(g, a.gamma, 1.0f, t, a.H);
+  at.columns(g, a.gamma, 1.0f);
 #pragma unroll
   for (int p = 0; p < P; ++p)
 #pragma unroll
     for (int j = 0; j < V; ++j) dg[p][j] = db[p][j] = 0.0f;
   for (; row < a.rows; row += step) {
-    if (!kAhead && row >= step) load(row);
-    // (past the row's end dy is 0, and so is all that counts there)
     const float m0 = mu, r0 = rs;
     uint4 x0[P], d0[P];
     float2 s = {0.0f, 0.0f};
@@ -220,20 +262,19 @@ __global__ void __launch_bounds__(kThreads) k_norm_grad(const NormGradArgs a) {
       Piece<DT>::get(d0[p], d);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float xh = (v[j] - m0) * r0, q = d[j] * g[p][j];
+        const float xh = (v[j] - m0) * r0, e = at.own(p, j) ? d[j] : 0.0f, q = e * g[p][j];
         s.x += q;
         s.y = fmaf(q, xh, s.y);
-        dg[p][j] = fmaf(d[j], xh, dg[p][j]);
-        db[p][j] += d[j];
+        dg[p][j] = fmaf(e, xh, dg[p][j]);
+        db[p][j] += e;
       }
     }
-    if (kAhead && row + step < a.rows) load(row + step);
+    if (row + step < a.rows) load(row + step);
     s = row_sum<L>(s, sh, turn);
     const float m = s.x * inv, mx = s.y * inv;
     DT* dx = reinterpret_cast<DT*>(a.dx) + row * a.dx_ld;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      const int c = (L * p + t) * V;
       float v[V], d[V];
       Piece<DT>::get(x0[p], v);
       Piece<DT>::get(d0[p], d);
@@ -242,7 +283,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_grad(const NormGradArgs a) {
         const float xh = (v[j] - m0) * r0;
         v[j] = r0 * (d[j] * g[p][j] - m - xh * mx);
       }
-      if (c < a.H) store_piece(dx, c, a.H, v);
+      at.store(dx, p, v);
     }
   }
   // the groups' sums in order: a thread adds one column at a time
@@ -256,19 +297,19 @@ __global__ void __launch_bounds__(kThreads) k_norm_grad(const NormGradArgs a) {
         for (int j = 0; j < V; ++j) add[(p * V + j) * kThreads + threadIdx.x] = which ? db[p][j] : dg[p][j];
       __syncthreads();
       for (int i = threadIdx.x; i < P * V * L; i += kThreads) {  // value i / L of lane i % L
-        const int c = (L * (i / L / V) + i % L) * V + i / L % V;
+        const int p = i / L / V, j = i / L % V;
+        const int first = (L * p + i % L) * V, col = max(min(first, a.H - V), 0), c = col + j;
         float v = 0.0f;
 #pragma unroll
         for (int k = 0; k < kRows; ++k) v += add[i / L * kThreads + k * L + i % L];
-        if (c < a.H) part[c] = v;
+        if (c >= first && c < a.H) part[c] = v;
       }
     } else {
 #pragma unroll
       for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const int c = (L * p + t) * V + j;
-          if (c < a.H) part[c] = which ? db[p][j] : dg[p][j];
+          if (at.own(p, j)) part[at.col[p] + j] = which ? db[p][j] : dg[p][j];
         }
     }
   }
@@ -276,7 +317,7 @@ __global__ void __launch_bounds__(kThreads) k_norm_grad(const NormGradArgs a) {
 
 // Adds the n rows of partial sums: 16 columns a work-group, 16 rows at a time,
 // each of the 16 in its own order, then these.
-__global__ void __launch_bounds__(kThreads) k_norm_sum(const NormGradArgs a, int n) {
+__global__ void __launch_bounds__(256) k_norm_sum(const NormGradArgs a, int n) {
   __shared__ float sh[16][17];
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4, j = blockIdx.x * 16 + c;
   float s = 0.0f;
@@ -297,13 +338,14 @@ __global__ void __launch_bounds__(kThreads) k_norm_sum(const NormGradArgs a, int
 // Lanes of a row, by its width.
 int lanes(int dtype, int H) {
   const int v = dtype == WM_FP32 ? 4 : 8;
-  return H <= 16 * v ? 16 : H <= 1024 ? 64 : 256;
+  return H <= 16 * v ? 16 : H <= 1024 ? 64 : H <= 4096 ? 256 : 512;
 }
-// Work-groups of the gradient: enough to fill the device, few rows of partial
-// sums.  (The narrowest rows of the type that packs more of them.)
+// Work-groups of the gradient, each with a row of partial sums: as many as the
+// registers let run at once.
 int parts(long rows, int H) {
-  const long per = kThreads / lanes(WM_FP32, H);
-  return (int)std::max<long>(1, std::min<long>((rows + per - 1) / per, kParts));
+  const long per = std::max(1, 256 / lanes(WM_FP32, H));  // (bf16 rows just above 64 values lie two or four times as dense)
+  const long most = H <= 256 ? 1024 : H <= 4096 ? 512 : 256;
+  return (int)std::max<long>(1, std::min<long>((rows + per - 1) / per, most));
 }
 
 // Runs f with the pieces of a lane and the lanes of a row as constants.
@@ -317,7 +359,7 @@ hipError_t by_width(int H, F f) {
   if (H <= 1024) return f(Const<4 / k>(), Const<64>());
   if (H <= 2048) return f(Const<2 / k>(), Const<256>());
   if (H <= 4096) return f(Const<4 / k>(), Const<256>());
-  return f(Const<8 / k>(), Const<256>());
+  return f(Const<4 / k>(), Const<512>());
 }
 
 }  // namespace
@@ -326,8 +368,8 @@ hipError_t launch_layer_norm(int dtype, const NormArgs& a, hipStream_t s) {
   auto run = [&](auto dt) {
     typedef decltype(dt) DT;
     return by_width<DT>(a.H, [&](auto p, auto l) {
-      const long per = kThreads / l, groups = std::min<long>((a.rows + per - 1) / per, kGroups);
-      return launch("norm", k_norm<DT, p, l>, dim3((unsigned)groups), dim3(kThreads), 0, s, a);
+      const long per = threads(l) / l, groups = std::min<long>((a.rows + per - 1) / per, kGroups);
+      return launch("norm", k_norm<DT, p, l>, dim3((unsigned)groups), dim3(threads(l)), 0, s, a);
     });
   };
   return dtype == WM_FP32 ? run(0.0f) : run(bf16_t());
@@ -340,12 +382,12 @@ hipError_t launch_layer_norm_grad(int dtype, const NormGradArgs& a, hipStream_t 
   auto run = [&](auto dt) {
     typedef decltype(dt) DT;
     return by_width<DT>(a.H, [&](auto p, auto l) {
-      return launch("norm_grad", k_norm_grad<DT, p, l>, dim3(n), dim3(kThreads), 0, s, a);
+      return launch("norm_grad", k_norm_grad<DT, p, l>, dim3(n), dim3(threads(l)), 0, s, a);
     });
   };
   const hipError_t e = dtype == WM_FP32 ? run(0.0f) : run(bf16_t());
   if (e != hipSuccess) return e;
-  return launch("norm_sum", k_norm_sum, dim3((unsigned)((2 * a.H + 15) / 16)), dim3(kThreads), 0, s, a, n);
+  return launch("norm_sum", k_norm_sum, dim3((unsigned)((2 * a.H + 15) / 16)), dim3(256), 0, s, a, n);
 }
 
 }  // namespace wm
