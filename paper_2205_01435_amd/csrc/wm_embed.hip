@@ -2,6 +2,19 @@
 // gradient (the one-hot product of the world model's input as a gather, and
 // its transpose).
 //   y_i = s E[a_i], 0 where a_i is outside [0, V);  dE_v = s sum_{a_i = v} dy_i.
+//
+// The gradient sorts the positions by token (stably, by 8-bit digits, least
+// first; codes outside the table sort behind it), so that a row's positions lie
+// together, and cuts the sorted list into equal chunks whatever the tokens are:
+// a row that every token names costs as much as one row each.  A wave sums the
+// runs of equal tokens of its chunk, 16 bytes a lane, and writes the rows that
+// lie inside the chunk; the first and the last run, which may go on in the
+// neighbouring chunks, become partial sums.  The last launch adds a row's
+// partial sums in order and clears the rows that no token names: every row of
+// the gradient is written once, and the order of each sum is fixed.
+// All of it is bound by memory: dy is read once, the gradient written once.
+#include <algorithm>
+
 #include "../../include/wm.h"
 #include "wm_seq.h"
 #include "wm_profile.h"
@@ -9,66 +22,483 @@
 namespace wm {
 namespace {
 
+typedef uint32_t __attribute__((ext_vector_type(4))) u32x4;
+typedef u32x4 __attribute__((aligned(2))) u32x4_2;
+typedef u32x4 __attribute__((aligned(4))) u32x4_4;
+
+// Sixteen bytes of a row as fp32 values.  Rows are aligned to their element
+// only: the hardware takes 16-byte accesses at such addresses.
+template <typename DT> struct Piece;
+template <> struct Piece<float> {
+  static constexpr int V = 4;
+  __device__ static void load(const float* p, float* v) {
+    const u32x4 r = *reinterpret_cast<const u32x4_4*>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(r[j]);
+  }
+  __device__ static void store(float* p, const float* v) {
+    *reinterpret_cast<u32x4_4*>(p) =
+        u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  }
+};
+template <> struct Piece<bf16_t> {
+  static constexpr int V = 8;
+  __device__ static void load(const bf16_t* p, float* v) {
+    const u32x4 r = *reinterpret_cast<const u32x4_2*>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[2 * j] = __uint_as_float(r[j] << 16);
+      v[2 * j + 1] = __uint_as_float(r[j] & 0xffff0000u);
+    }
+  }
+  __device__ static void store(bf16_t* p, const float* v) {
+    *reinterpret_cast<u32x4_2*>(p) =
+        u32x4{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+  }
+};
+
+// A row's last, partial piece is read and written as the last 16 bytes of the
+// row, over the end of the piece before it: both hold the same values.  A row
+// narrower than a piece goes value by value.
 template <typename DT>
+__device__ __forceinline__ void load_piece(const DT* row, int col, int H, float* v) {
+  if (H >= Piece<DT>::V) {
+    Piece<DT>::load(row + col, v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < Piece<DT>::V; ++j) v[j] = j < H ? DType<DT>::load(row, j) : 0.0f;
+  }
+}
+// N values to a row of type DT.
+template <typename DT, int N>
+__device__ __forceinline__ void store_values(DT* row, int col, int H, const float* v) {
+  if (H >= N) {
+#pragma unroll
+    for (int j = 0; j < N; j += Piece<DT>::V) Piece<DT>::store(row + col + j, v + j);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (j < H) DType<DT>::store(row, j, v[j]);
+  }
+}
+template <typename DT>
+__device__ __forceinline__ int column(int piece, int H) {
+  return max(min(piece * Piece<DT>::V, H - Piece<DT>::V), 0);
+}
+
+// L lanes a row.
+template <typename DT, int L>
 __global__ void __launch_bounds__(256) k_embed(const EmbedArgs a) {
+  constexpr int V = Piece<DT>::V;
   const DT* table = reinterpret_cast<const DT*>(a.table);
   DT* out = reinterpret_cast<DT*>(a.out);
-  for (long i = blockIdx.x; i < a.n; i += gridDim.x) {
+  const int t = threadIdx.x % L;
+  const long step = (long)gridDim.x * (256 / L);
+  for (long i = (long)blockIdx.x * (256 / L) + threadIdx.x / L; i < a.n; i += step) {
     const int tok = a.tokens[i];
     const bool ok = tok >= 0 && tok < a.V;
-    for (int h = threadIdx.x; h < a.H; h += 256)
-      DType<DT>::store(out, i * a.out_ld + h, ok ? a.scale * DType<DT>::load(table, (long)tok * a.H + h) : 0.0f);
+    const DT* from = table + (long)(ok ? tok : 0) * a.H;
+    DT* to = out + i * a.out_ld;
+    for (int p = t; p * V < a.H; p += L) {
+      const int c = column<DT>(p, a.H);
+      float v[V];
+      if (ok) load_piece(from, c, a.H, v);
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = ok ? a.scale * v[j] : 0.0f;
+      store_values<DT, V>(to, c, a.H, v);
+    }
   }
 }
 
-// One work-group per table row: its tokens' positions are collected 256 at a
-// time in order, and their rows summed.
-template <typename DT>
-__global__ void __launch_bounds__(256) k_embed_grad(const EmbedGradArgs a) {
-  __shared__ int pos[256];
-  __shared__ int cnt[4];
-  const DT* dout = reinterpret_cast<const DT*>(a.dout);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int v = blockIdx.x; v < a.V; v += gridDim.x) {
-    for (int h0 = 0; h0 < a.H; h0 += 256) {
-      const int h = h0 + threadIdx.x;
-      float acc = 0.0f;
-      for (long i0 = 0; i0 < a.n; i0 += 256) {
-        const long i = i0 + threadIdx.x;
-        const bool hit = i < a.n && a.tokens[i] == v;
-        const unsigned long long m = __ballot(hit);
-        if (lane == 0) cnt[wave] = __popcll(m);
-        __syncthreads();
-        int base = 0, total = 0;
-        for (int w = 0; w < 4; ++w) {
-          if (w < wave) base += cnt[w];
-          total += cnt[w];
-        }
-        if (hit) pos[base + __popcll(m & ((1ull << lane) - 1))] = (int)i;
-        __syncthreads();
-        for (int k = 0; k < total; ++k)
-          if (h < a.H) acc += DType<DT>::load(dout, (long)pos[k] * a.dout_ld + h);
-        __syncthreads();
+// ---------------------------------------------------------------------------
+// Sorting the positions by token
+// ---------------------------------------------------------------------------
+
+constexpr int kDigits = 256;
+constexpr int kOne = 2048;     // positions that one work-group sorts by itself
+constexpr int kMaxTiles = 256; // tiles of a longer list
+
+__device__ __forceinline__ uint32_t key_of(int tok, int V) { return tok >= 0 && tok < V ? (uint32_t)tok : (uint32_t)V; }
+
+// Lanes of the wave with the same digit as this one, among those in `in`.
+__device__ __forceinline__ unsigned long long same_digit(uint32_t d, unsigned long long in) {
+#pragma unroll
+  for (int b = 0; b < 8; ++b) {
+    const bool bit = (d >> b) & 1u;
+    const unsigned long long m = __ballot(bit);
+    in &= bit ? m : ~m;
+  }
+  return in;
+}
+
+// Places the entries [begin, end) of a wave, in order: `at[digit]` holds where
+// its next entry of that digit goes.  get(i) is entry i as (key, position).
+template <typename Get, typename Put>
+__device__ __forceinline__ void place_run(int begin, int end, int shift, uint32_t* at, Get get, Put put) {
+  const int lane = threadIdx.x & 63;
+  for (int i0 = begin; i0 < end; i0 += 64) {
+    const int i = i0 + lane;
+    const bool in = i < end;
+    uint2 e = make_uint2(0u, 0u);
+    if (in) e = get(i);
+    const uint32_t d = (e.x >> shift) & (kDigits - 1);
+    const unsigned long long peers = same_digit(d, __ballot(in));
+    const uint32_t rank = __popcll(peers & ((1ull << lane) - 1ull));
+    uint32_t to = 0;
+    if (in) to = at[d] + rank;
+    // (every lane has read before the last of each digit's lanes writes: they are one wave)
+    if (in && (peers >> lane) == 1ull) at[d] = to + 1u;
+    if (in) put(to, e);
+  }
+}
+
+// Exclusive sums of 256 counts, one a thread of the first 256.
+__device__ __forceinline__ uint32_t scan256(uint32_t v, uint32_t* sh) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  uint32_t s = v;
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) {
+    const uint32_t o = __shfl_up(s, k);
+    if (lane >= k) s += o;
+  }
+  if (w < 4 && lane == 63) sh[w] = s;
+  __syncthreads();
+  for (int i = 0; i < w && i < 3; ++i) s += sh[i];
+  __syncthreads();
+  return s - v;
+}
+
+// All passes of a short list in one work-group of 16 waves.
+__global__ void __launch_bounds__(1024) k_embed_sort(const int32_t* tokens, int n, int V, int passes, uint32_t* keys,
+                                                     uint32_t* pos) {
+  __shared__ uint2 list[2][kOne];
+  __shared__ uint32_t at[16][kDigits];
+  __shared__ uint32_t sh[4];
+  const int w = threadIdx.x >> 6, run = ((n + 15) / 16 + 63) / 64 * 64;
+  for (int i = threadIdx.x; i < n; i += 1024) list[0][i] = make_uint2(key_of(tokens[i], V), (uint32_t)i);
+  for (int p = 0; p < passes; ++p) {
+    for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) at[i / kDigits][i % kDigits] = 0;
+    __syncthreads();
+    const uint2* from = list[p & 1];
+    uint2* to = list[(p & 1) ^ 1];
+    const int begin = min(w * run, n), end = min(begin + run, n);
+    for (int i = begin + (threadIdx.x & 63); i < end; i += 64) atomicAdd(&at[w][(from[i].x >> 8 * p) & (kDigits - 1)], 1u);
+    __syncthreads();
+    uint32_t total = 0;
+    if (threadIdx.x < kDigits)
+      for (int k = 0; k < 16; ++k) total += at[k][threadIdx.x];
+    uint32_t base = scan256(total, sh);
+    if (threadIdx.x < kDigits)
+      for (int k = 0; k < 16; ++k) {
+        const uint32_t c = at[k][threadIdx.x];
+        at[k][threadIdx.x] = base;
+        base += c;
       }
-      if (h < a.H) a.dtable[(long)v * a.H + h] = a.scale * acc;
+    __syncthreads();
+    place_run(begin, end, 8 * p, at[w], [&](int i) { return from[i]; }, [&](uint32_t i, uint2 e) { to[i] = e; });
+    __syncthreads();
+  }
+  for (int i = threadIdx.x; i < n; i += 1024) {
+    const uint2 e = list[passes & 1][i];
+    keys[i] = e.x;
+    pos[i] = e.y;
+  }
+}
+
+struct SortArgs {
+  const int32_t* tokens;        // the first pass's entries: positions 0 .. n - 1
+  const uint32_t *keys, *pos;   // the others'
+  uint32_t *keys_to, *pos_to;
+  uint32_t* hist;               // [tiles][256]
+  int n, V, tile, tiles, pass;
+};
+__device__ __forceinline__ uint2 entry(const SortArgs& a, int i) {
+  return a.pass == 0 ? make_uint2(key_of(a.tokens[i], a.V), (uint32_t)i) : make_uint2(a.keys[i], a.pos[i]);
+}
+
+// How often each digit occurs in each tile.
+__global__ void __launch_bounds__(1024) k_embed_hist(const SortArgs a) {
+  __shared__ uint32_t cnt[kDigits];
+  if (threadIdx.x < kDigits) cnt[threadIdx.x] = 0;
+  __syncthreads();
+  const int begin = blockIdx.x * a.tile, end = min(begin + a.tile, a.n);
+  for (int i = begin + threadIdx.x; i < end; i += 1024) {
+    const uint32_t key = a.pass == 0 ? key_of(a.tokens[i], a.V) : a.keys[i];
+    atomicAdd(&cnt[(key >> 8 * a.pass) & (kDigits - 1)], 1u);
+  }
+  __syncthreads();
+  if (threadIdx.x < kDigits) a.hist[blockIdx.x * kDigits + threadIdx.x] = cnt[threadIdx.x];
+}
+
+// Places a tile's entries behind those of smaller digits and of earlier tiles.
+__global__ void __launch_bounds__(1024) k_embed_scatter(const SortArgs a) {
+  __shared__ uint32_t at[16][kDigits];
+  __shared__ uint32_t part[2][4][kDigits];
+  __shared__ uint32_t sh[4];
+  const int w = threadIdx.x >> 6, d = threadIdx.x % kDigits, q = threadIdx.x / kDigits;
+  const int begin0 = blockIdx.x * a.tile, run = a.tile / 16;
+  const int begin = min(begin0 + w * run, a.n), end = min(begin + run, a.n);
+  for (int i = threadIdx.x; i < 16 * kDigits; i += 1024) at[i / kDigits][i % kDigits] = 0;
+  uint32_t all = 0, before = 0;
+#pragma unroll 4
+  for (int t = q; t < a.tiles; t += 4) {
+    const uint32_t c = a.hist[t * kDigits + d];
+    all += c;
+    before += t < (int)blockIdx.x ? c : 0u;
+  }
+  part[0][q][d] = all;
+  part[1][q][d] = before;
+  __syncthreads();
+  for (int i = begin + (threadIdx.x & 63); i < end; i += 64) {
+    const uint32_t key = a.pass == 0 ? key_of(a.tokens[i], a.V) : a.keys[i];
+    atomicAdd(&at[w][(key >> 8 * a.pass) & (kDigits - 1)], 1u);
+  }
+  all = part[0][0][d] + part[0][1][d] + part[0][2][d] + part[0][3][d];
+  before = part[1][0][d] + part[1][1][d] + part[1][2][d] + part[1][3][d];
+  uint32_t base = scan256(all, sh) + before;  // (its barriers complete the counts)
+  if (threadIdx.x < kDigits)
+    for (int k = 0; k < 16; ++k) {
+      const uint32_t c = at[k][d];
+      at[k][d] = base;
+      base += c;
+    }
+  __syncthreads();
+  place_run(begin, end, 8 * a.pass, at[w], [&](int i) { return entry(a, i); },
+            [&](uint32_t i, uint2 e) {
+              a.keys_to[i] = e.x;
+              a.pos_to[i] = e.y;
+            });
+}
+
+// ---------------------------------------------------------------------------
+// Sums over runs of equal tokens
+// ---------------------------------------------------------------------------
+
+struct RowsArgs {
+  EmbedGradArgs g;
+  const uint32_t *keys, *pos;  // sorted
+  float* part;                 // [chunks][2][H]
+  int chunk, chunks;
+};
+
+// A wave's chunk of sorted positions, for 64 pieces of the columns.  The run at
+// the chunk's begin is a partial sum of slot 0 if it began before the chunk or
+// goes on after it; another run that goes on after it is one of slot 1.
+template <typename DT>
+__global__ void __launch_bounds__(256) k_embed_rows(const RowsArgs a) {
+  constexpr int V = Piece<DT>::V, kAhead = 8;
+  const int lane = threadIdx.x & 63;
+  const int chunk = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (chunk >= a.chunks) return;
+  const int H = a.g.H, piece = blockIdx.y * 64 + lane, col = column<DT>(piece, H);
+  const bool on = piece * V < H;
+  const DT* dy = reinterpret_cast<const DT*>(a.g.dout);
+  const int n = (int)a.g.n, begin = chunk * a.chunk, end = min(begin + a.chunk, n);
+  float* const part = a.part + (long)chunk * 2 * H;
+  const uint32_t before = begin > 0 ? a.keys[begin - 1] : ~0u, after = end < n ? a.keys[end] : ~0u;
+  float sum[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+  uint32_t run = a.keys[begin];  // the run's token
+  bool first = true;             // ... is the chunk's first
+  auto flush = [&](bool last) {
+    if (run >= (uint32_t)a.g.V) return;  // codes outside the table
+    const bool shared = (first && run == before) || (last && run == after);
+    if (!on) return;
+    if (shared) {
+      store_values<float, V>(part + (first ? 0 : H), col, H, sum);
+    } else {
+      float v[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) v[j] = a.g.scale * sum[j];
+      store_values<float, V>(a.g.dtable + (long)run * H, col, H, v);
+    }
+  };
+  for (int i0 = begin; i0 < end; i0 += 64) {
+    const int m = min(64, end - i0);
+    const uint32_t key = lane < m ? a.keys[i0 + lane] : 0u, pos = lane < m ? a.pos[i0 + lane] : 0u;
+    for (int k0 = 0; k0 < m; k0 += kAhead) {
+      if ((uint32_t)__builtin_amdgcn_readlane((int)key, k0) >= (uint32_t)a.g.V) break;  // only codes from here on
+      float v[kAhead][V];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int q = min(k0 + k, m - 1);
+        const long row = (uint32_t)__builtin_amdgcn_readlane((int)pos, q);
+        if (on) load_piece(dy + row * a.g.dout_ld, col, H, v[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (k0 + k >= m) break;
+        const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)key, k0 + k);
+        if (t != run) {
+          flush(false);
+          run = t;
+          first = false;
+#pragma unroll
+          for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += v[k][j];
+      }
+    }
+    const uint32_t t = (uint32_t)__builtin_amdgcn_readlane((int)key, m - 1);
+    if (t >= (uint32_t)a.g.V && run < (uint32_t)a.g.V) {  // the table's last run, before the codes
+      flush(false);
+      run = t;
+      first = false;
     }
   }
+  flush(true);
+}
+
+// First sorted position whose token is at least v.
+__device__ __forceinline__ int lower_bound(const uint32_t* keys, int n, uint32_t v) {
+  int lo = 0, hi = n;
+  while (lo < hi) {
+    const int mid = lo + (hi - lo) / 2;
+    if (keys[mid] < v)
+      lo = mid + 1;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+// Rows of the table, `rows` a work-group of 16 waves, 64 pieces of four columns:
+// clears those that no token names, and adds up those that lie in several
+// chunks, the waves in turn over the chunks and then their sums.
+constexpr int kJoinRows = 64;
+__device__ __forceinline__ void join_rows(const RowsArgs& a, int r0, int m, int (&start)[kJoinRows + 1],
+                                          float4 (&sums)[16][64]) {
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), H = a.g.H;
+  const int piece = blockIdx.y * 64 + lane, col = column<float>(piece, H);
+  const bool on = piece * 4 < H;
+  if ((int)threadIdx.x <= m) start[threadIdx.x] = lower_bound(a.keys, (int)a.g.n, (uint32_t)(r0 + threadIdx.x));
+  __syncthreads();
+  const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int r = w; r < m; r += 16)
+    if (start[r] == start[r + 1] && on) store_values<float, 4>(a.g.dtable + (long)(r0 + r) * H, col, H, zero);
+  for (int r = 0; r < m; ++r) {
+    const int s = start[r], e = start[r + 1];
+    if (s == e || s / a.chunk == (e - 1) / a.chunk) continue;
+    const int c0 = s / a.chunk, c1 = (e - 1) / a.chunk, count = c1 - c0 + 1;
+    const int i0 = (int)((long)count * w / 16), i1 = (int)((long)count * (w + 1) / 16);
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (on) {
+#pragma unroll 8
+      for (int i = i0; i < i1; ++i) {
+        // the first of them is its chunk's last run, and its first too if it begins there
+        const float* p = a.part + ((long)(c0 + i) * 2 + (i == 0 && s % a.chunk != 0)) * H;
+        float v[4];
+        load_piece(p, col, H, v);
+        sum.x += v[0];
+        sum.y += v[1];
+        sum.z += v[2];
+        sum.w += v[3];
+      }
+    }
+    sums[w][lane] = sum;
+    __syncthreads();
+    if (w == 0 && on) {
+      for (int k = 1; k < 16; ++k) {
+        const float4 v = sums[k][lane];
+        sum.x += v.x;
+        sum.y += v.y;
+        sum.z += v.z;
+        sum.w += v.w;
+      }
+      const float v[4] = {a.g.scale * sum.x, a.g.scale * sum.y, a.g.scale * sum.z, a.g.scale * sum.w};
+      store_values<float, 4>(a.g.dtable + (long)(r0 + r) * H, col, H, v);
+    }
+    __syncthreads();
+  }
+}
+
+__global__ void __launch_bounds__(1024) k_embed_join(const RowsArgs a, int rows) {
+  __shared__ int start[kJoinRows + 1];
+  __shared__ float4 sums[16][64];
+  for (long r0 = (long)blockIdx.x * rows; r0 < a.g.V; r0 += (long)gridDim.x * rows) {
+    join_rows(a, (int)r0, (int)min((long)rows, a.g.V - r0), start, sums);
+    __syncthreads();
+  }
+}
+
+// How a call is cut.
+struct Plan {
+  int passes, tile, tiles;  // of the sort (tiles 0: one work-group)
+  int chunk, chunks;
+  size_t hist, part, total;  // workspace, after the keys and positions twice: counts, partial sums
+};
+Plan plan(long n, int V, int H) {
+  Plan p{};
+  p.passes = 1;
+  while (p.passes < 4 && (uint64_t)V >> (8 * p.passes)) ++p.passes;  // the keys are 0 .. V
+  if (n > kOne) {
+    p.tile = (int)(((n + kMaxTiles - 1) / kMaxTiles + 1023) / 1024 * 1024);
+    p.tiles = (int)((n + p.tile - 1) / p.tile);
+  }
+  // about 16 waves for every CU, whole groups of loads
+  const long blocks = (H + 255) / 256;
+  p.chunk = (int)std::min<long>(128, std::max<long>(16, (n * blocks / 4096 + 7) / 8 * 8));
+  p.chunks = (int)((n + p.chunk - 1) / p.chunk);
+  // room for the chunks and tiles of this and every shorter list
+  const long most = std::min<long>((n + 15) / 16, std::max<long>(8192 / blocks + 1, (n + 127) / 128));
+  const auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+  const size_t list = up((size_t)n * 4);
+  p.hist = 4 * list;
+  p.part = p.hist + (n > kOne ? (size_t)kMaxTiles * kDigits * 4 : 0);
+  p.total = p.part + up((size_t)most * 2 * H * sizeof(float));
+  return p;
 }
 
 }  // namespace
 
 hipError_t launch_embed(int dtype, const EmbedArgs& a, hipStream_t s) {
-  const unsigned grid = (unsigned)(a.n < 65536 ? a.n : 65536);
-  return dtype == WM_FP32 ? launch("embed", k_embed<float>, dim3(grid), dim3(256), 0, s, a)
-                          : launch("embed", k_embed<bf16_t>, dim3(grid), dim3(256), 0, s, a);
+  auto run = [&](auto dt) {
+    typedef decltype(dt) DT;
+    const int pieces = (a.H + Piece<DT>::V - 1) / Piece<DT>::V;
+    auto go = [&](auto kernel, int L) {
+      const long per = 256 / L, grid = std::min<long>((a.n + per - 1) / per, 8192);
+      return launch("embed", kernel, dim3((unsigned)grid), dim3(256), 0, s, a);
+    };
+    return pieces <= 4 ? go(k_embed<DT, 4>, 4) : pieces <= 16 ? go(k_embed<DT, 16>, 16) : go(k_embed<DT, 64>, 64);
+  };
+  return dtype == WM_FP32 ? run(0.0f) : run(bf16_t());
 }
 
-size_t embed_grad_workspace(long n, int, int) { return 256 + (size_t)n * 8; }  // (token, position) pairs
+size_t embed_grad_workspace(long n, int V, int H) { return plan(n, V, H).total; }
 
 hipError_t launch_embed_grad(int dtype, const EmbedGradArgs& a, hipStream_t s) {
-  const unsigned grid = (unsigned)(a.V < 65536 ? a.V : 65536);
-  return dtype == WM_FP32 ? launch("embed_grad", k_embed_grad<float>, dim3(grid), dim3(256), 0, s, a)
-                          : launch("embed_grad", k_embed_grad<bf16_t>, dim3(grid), dim3(256), 0, s, a);
+  const Plan p = plan(a.n, a.V, a.H);
+  char* ws = reinterpret_cast<char*>(a.ws);
+  const size_t list = p.hist / 4;
+  uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws), reinterpret_cast<uint32_t*>(ws + list)};
+  uint32_t* pos[2] = {reinterpret_cast<uint32_t*>(ws + 2 * list), reinterpret_cast<uint32_t*>(ws + 3 * list)};
+  int at = 0;
+  hipError_t e = hipSuccess;
+  if (a.n > 0 && p.tiles == 0) {
+    e = launch("embed_sort", k_embed_sort, dim3(1), dim3(1024), 0, s, a.tokens, (int)a.n, a.V, p.passes, keys[0], pos[0]);
+  } else {
+    for (int k = 0; k < p.passes && a.n > 0 && e == hipSuccess; ++k) {
+      const SortArgs q{a.tokens, keys[at], pos[at], keys[at ^ 1], pos[at ^ 1], reinterpret_cast<uint32_t*>(ws + p.hist),
+                       (int)a.n, a.V, p.tile, p.tiles, k};
+      e = launch("embed_hist", k_embed_hist, dim3(p.tiles), dim3(1024), 0, s, q);
+      if (e == hipSuccess) e = launch("embed_scatter", k_embed_scatter, dim3(p.tiles), dim3(1024), 0, s, q);
+      at ^= 1;
+    }
+  }
+  if (e != hipSuccess) return e;
+  const RowsArgs r{a, keys[at], pos[at], reinterpret_cast<float*>(ws + p.part), p.chunk, p.chunks};
+  if (a.n > 0) {
+    const int v = dtype == WM_FP32 ? 4 : 8;
+    const dim3 grid((p.chunks + 3) / 4, ((a.H + v - 1) / v + 63) / 64);
+    e = dtype == WM_FP32 ? launch("embed_rows", k_embed_rows<float>, grid, dim3(256), 0, s, r)
+                         : launch("embed_rows", k_embed_rows<bf16_t>, grid, dim3(256), 0, s, r);
+    if (e != hipSuccess) return e;
+  }
+  const int rows = std::min(kJoinRows, std::max(1, a.V / 1024));
+  const unsigned groups = (unsigned)std::min<long>(((long)a.V + rows - 1) / rows, 16384);
+  return launch("embed_join", k_embed_join, dim3(groups, ((a.H + 3) / 4 + 63) / 64), dim3(1024), 0, s, r, rows);
 }
 
 }  // namespace wm
