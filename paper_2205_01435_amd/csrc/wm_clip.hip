@@ -1,10 +1,18 @@
 // The global norm of a list of gradient tensors, and the tensors scaled to it:
 //   N = sqrt(sum over all tensors of sum g^2),  out = g (N > max ? max / N : 1).
 // Squares are summed in 64 bits: fp32 squares overflow from |g| = 1.8e19 and
-// vanish below 1e-23, and the sum runs over up to billions of terms.  The
-// tensors are cut into chunks; every chunk's sum has its place in the
-// workspace and the second launch adds them in one order, so that the result
-// depends on the tensors alone.
+// vanish below 1e-23, and the sum runs over up to billions of terms (the 64-bit
+// multiply-add costs less than the bytes it works on).  The tensors are cut
+// into chunks of equal size; every chunk's sum has its place in the workspace,
+// and each work-group of the second launch adds them all in one order, so that
+// the result depends on the tensors alone.
+//
+// Bound by memory: the values are read twice (the second time from the
+// last-level cache where the list fits it: from its end, which was read last)
+// and written once.  Arrays are aligned to their element only; the hardware
+// takes 16-byte accesses at such addresses.
+#include <algorithm>
+
 #include "../../include/wm.h"
 #include "wm_seq.h"
 #include "wm_profile.h"
@@ -13,115 +21,190 @@ namespace wm {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 16384;  // elements
-constexpr int kPerLaunch = 64; // tensors whose table fits a launch's arguments
+constexpr int kPer = 8;                       // 16-byte pieces of a thread
+constexpr int kChunkBytes = kThreads * kPer * 16;
+constexpr int kPerLaunch = 128;               // tensors whose table fits a launch's arguments
+
+typedef uint32_t __attribute__((ext_vector_type(4))) u32x4;
+typedef u32x4 __attribute__((aligned(2))) u32x4_2;
 
 struct Table {
-  int n;                      // tensors of this launch
-  long part0;                 // place of its first chunk's sum
-  long first[kPerLaunch + 1]; // chunks before each tensor
+  int n;                        // tensors of this launch
+  uint32_t part0;               // place of its first chunk's sum
+  uint32_t first[kPerLaunch + 1]; // chunks before each tensor
   const void* in[kPerLaunch];
   void* out[kPerLaunch];
-  long len[kPerLaunch];
-  int32_t dtype[kPerLaunch];
+  int64_t bytes[kPerLaunch];    // < 0: bf16
 };
 
-__device__ __forceinline__ int find(const Table& t, long c) {
-  int i = 0;
-  while (c >= t.first[i + 1]) ++i;
-  return i;
+// The tensor of chunk c.
+__device__ __forceinline__ int find(const Table& t, uint32_t c) {
+  int lo = 0, hi = t.n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (t.first[mid] <= c)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
 }
 
-__device__ double block_sum(double v, double* sh) {
+struct Chunk {
+  const char* in;
+  char* out;
+  int bytes;   // of the chunk
+  bool bf16;
+  __device__ Chunk(const Table& t, uint32_t c) {
+    const int i = find(t, c);
+    const int64_t all = t.bytes[i], len = all < 0 ? -all : all, at = (int64_t)(c - t.first[i]) * kChunkBytes;
+    bf16 = all < 0;
+    bytes = (int)min((int64_t)kChunkBytes, len - at);
+    in = static_cast<const char*>(t.in[i]) + at;
+    out = static_cast<char*>(t.out[i]) + at;
+  }
+  __device__ u32x4 load(int at) const { return *reinterpret_cast<const u32x4_2*>(in + at); }
+};
+
+// The four waves' sums, in order.
+__device__ __forceinline__ double group_sum(double v, double* sh) {
   for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k);
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
   __syncthreads();
   return (sh[0] + sh[1]) + (sh[2] + sh[3]);
 }
 
+__device__ __forceinline__ double squares(u32x4 r, bool bf16, double s) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (bf16) {
+      const double a = __uint_as_float(r[j] << 16), b = __uint_as_float(r[j] & 0xffff0000u);
+      s = fma(a, a, s);
+      s = fma(b, b, s);
+    } else {
+      const double a = __uint_as_float(r[j]);
+      s = fma(a, a, s);
+    }
+  }
+  return s;
+}
+
 __global__ void __launch_bounds__(kThreads) k_clip_sum(const Table t, double* part) {
   __shared__ double sh[4];
-  const long c = blockIdx.x;
-  const int i = find(t, c);
-  const long at = (c - t.first[i]) * kChunk, end = min(at + (long)kChunk, t.len[i]);
+  const Chunk c(t, blockIdx.x);
   double s = 0.0;
-  for (long k = at + threadIdx.x; k < end; k += kThreads) {
-    const double g = t.dtype[i] == WM_FP32 ? DType<float>::load((const float*)t.in[i], k)
-                                           : DType<bf16_t>::load((const bf16_t*)t.in[i], k);
-    s += g * g;
+  if (c.bytes == kChunkBytes) {
+    u32x4 r[kPer];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) r[k] = c.load((k * kThreads + threadIdx.x) * 16);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) s = squares(r[k], c.bf16, s);
+  } else {
+    int at = threadIdx.x * 16;
+    for (; at + 16 <= c.bytes; at += kThreads * 16) s = squares(c.load(at), c.bf16, s);
+    const int es = c.bf16 ? 2 : 4;  // the values beyond the last whole piece: one lane's
+    for (; at < c.bytes; at += es) {
+      const double g = c.bf16 ? DType<bf16_t>::load(reinterpret_cast<const bf16_t*>(c.in + at), 0)
+                              : DType<float>::load(reinterpret_cast<const float*>(c.in + at), 0);
+      s = fma(g, g, s);
+    }
   }
-  s = block_sum(s, sh);
-  if (threadIdx.x == 0) part[t.part0 + c] = s;
+  s = group_sum(s, sh);
+  if (threadIdx.x == 0) part[t.part0 + blockIdx.x] = s;
 }
 
-__global__ void __launch_bounds__(kThreads) k_clip_scale(const Table t, const double* part, long nparts, float max_norm,
+__device__ __forceinline__ u32x4 scaled(u32x4 r, bool bf16, float f) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    r[j] = bf16 ? pack2_bf16(f * __uint_as_float(r[j] << 16), f * __uint_as_float(r[j] & 0xffff0000u))
+                : __float_as_uint(f * __uint_as_float(r[j]));
+  return r;
+}
+
+__global__ void __launch_bounds__(kThreads) k_clip_scale(const Table t, const double* part, uint32_t parts, float max_norm,
                                                          float* norm) {
   __shared__ double sh[4];
+  const Chunk c(t, gridDim.x - 1 - blockIdx.x);
+  const bool whole = c.bytes == kChunkBytes;
+  u32x4 r[kPer];
+  if (whole)
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) r[k] = c.load((k * kThreads + threadIdx.x) * 16);
   double s = 0.0;
-  for (long k = threadIdx.x; k < nparts; k += kThreads) s += part[k];
-  const double N = sqrt(block_sum(s, sh));
+#pragma unroll 8
+  for (uint32_t k = threadIdx.x; k < parts; k += kThreads) s += part[k];
+  const double N = sqrt(group_sum(s, sh));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)N;
   const float f = N > (double)max_norm && N < (double)INFINITY ? (float)((double)max_norm / N) : 1.0f;
-  const long c = blockIdx.x;
-  const int i = find(t, c);
-  const long at = (c - t.first[i]) * kChunk, end = min(at + (long)kChunk, t.len[i]);
-  if (t.in[i] == t.out[i] && f == 1.0f) return;
-  for (long k = at + threadIdx.x; k < end; k += kThreads) {
-    if (t.dtype[i] == WM_FP32)
-      ((float*)t.out[i])[k] = f * ((const float*)t.in[i])[k];
-    else
-      DType<bf16_t>::store((bf16_t*)t.out[i], k, f * DType<bf16_t>::load((const bf16_t*)t.in[i], k));
+  if (f == 1.0f && c.in == c.out) return;  // in place, and within the limit
+  const int es = c.bf16 ? 2 : 4;
+  if (whole) {
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+      *reinterpret_cast<u32x4_2*>(c.out + (k * kThreads + threadIdx.x) * 16) = scaled(r[k], c.bf16, f);
+  } else {
+    int at = threadIdx.x * 16;
+    for (; at + 16 <= c.bytes; at += kThreads * 16)
+      *reinterpret_cast<u32x4_2*>(c.out + at) = scaled(c.load(at), c.bf16, f);
+    for (; at < c.bytes; at += es) {
+      if (c.bf16)
+        DType<bf16_t>::store(reinterpret_cast<bf16_t*>(c.out + at), 0,
+                             f * DType<bf16_t>::load(reinterpret_cast<const bf16_t*>(c.in + at), 0));
+      else
+        *reinterpret_cast<float*>(c.out + at) = f * *reinterpret_cast<const float*>(c.in + at);
+    }
   }
 }
 
-long chunks(long n) { return (n + kChunk - 1) / kChunk; }
+__global__ void k_clip_none(float* norm) { *norm = 0.0f; }
+
+int64_t bytes_of(const wm_grad_tensor& t) { return t.n * (t.dtype == WM_FP32 ? 4 : 2); }
+int64_t chunks_of(const wm_grad_tensor& t) { return (bytes_of(t) + kChunkBytes - 1) / kChunkBytes; }
 
 // Runs f on the table of each launch.
 template <typename F>
 hipError_t tables(int n, const wm_grad_tensor* t, F f) {
-  long part0 = 0;
+  uint32_t part0 = 0;
   for (int i = 0; i < n;) {
-    Table tab{};
+    Table tab;
+    tab.n = 0;
     tab.part0 = part0;
+    tab.first[0] = 0;
     for (; i < n && tab.n < kPerLaunch; ++i) {
       if (t[i].n == 0) continue;
       const int k = tab.n++;
       tab.in[k] = t[i].grad;
       tab.out[k] = t[i].out;
-      tab.len[k] = t[i].n;
-      tab.dtype[k] = t[i].dtype;
-      tab.first[k + 1] = tab.first[k] + chunks(t[i].n);
+      tab.bytes[k] = t[i].dtype == WM_FP32 ? bytes_of(t[i]) : -bytes_of(t[i]);
+      tab.first[k + 1] = tab.first[k] + (uint32_t)chunks_of(t[i]);
     }
     if (tab.n == 0) break;
     part0 += tab.first[tab.n];
-    const hipError_t e = f(tab, (unsigned)tab.first[tab.n]);
+    const hipError_t e = f(tab, tab.first[tab.n]);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
-__global__ void k_clip_none(float* norm) { *norm = 0.0f; }
-
 }  // namespace
 
 size_t clip_workspace(int n, const wm_grad_tensor* t) {
-  long c = 0;
-  for (int i = 0; i < n; ++i) c += chunks(t[i].n);
-  return (size_t)(c > 0 ? c : 1) * sizeof(double);
+  int64_t c = 0;
+  for (int i = 0; i < n; ++i) c += chunks_of(t[i]);
+  return (size_t)c * sizeof(double);
 }
 
 hipError_t launch_clip(int n, const wm_grad_tensor* t, float max_norm, float* norm, void* ws, hipStream_t s) {
   double* part = reinterpret_cast<double*>(ws);
-  long total = 0;
-  for (int i = 0; i < n; ++i) total += chunks(t[i].n);
+  const uint32_t total = (uint32_t)(clip_workspace(n, t) / sizeof(double));
   if (total == 0) return launch("clip_none", k_clip_none, dim3(1), dim3(1), 0, s, norm);
   hipError_t e = tables(n, t, [&](const Table& tab, unsigned grid) {
     return launch("clip_sum", k_clip_sum, dim3(grid), dim3(kThreads), 0, s, tab, part);
   });
   if (e != hipSuccess) return e;
   return tables(n, t, [&](const Table& tab, unsigned grid) {
-    return launch("clip_scale", k_clip_scale, dim3(grid), dim3(kThreads), 0, s, tab, (const double*)part, total,
-                  max_norm, tab.part0 == 0 ? norm : nullptr);
+    return launch("clip_scale", k_clip_scale, dim3(grid), dim3(kThreads), 0, s, tab, (const double*)part, total, max_norm,
+                  tab.part0 == 0 ? norm : nullptr);
   });
 }
 
