@@ -3,9 +3,10 @@
 // Squares are summed in 64 bits: fp32 squares overflow from |g| = 1.8e19 and
 // vanish below 1e-23, and the sum runs over up to billions of terms (the 64-bit
 // multiply-add costs less than the bytes it works on).  The tensors are cut
-// into chunks of equal size; every chunk's sum has its place in the workspace,
-// and each work-group of the second launch adds them all in one order, so that
-// the result depends on the tensors alone.
+// into chunks of equal size, dealt to the work-groups in a fixed way; every
+// work-group's sum has its place in the workspace, and each work-group of the
+// second launch adds them all in one order, so that the result depends on the
+// tensors alone.
 //
 // Bound by memory: the values are read twice (the second time from the
 // last-level cache where the list fits it: from its end, which was read last)
@@ -24,9 +25,19 @@ constexpr int kThreads = 256;
 constexpr int kPer = 8;                       // 16-byte pieces of a thread
 constexpr int kChunkBytes = kThreads * kPer * 16;
 constexpr int kPerLaunch = 128;               // tensors whose table fits a launch's arguments
+constexpr int kGroups = 2048;                 // work-groups of a launch: eight a CU, each over chunks in strides
 
 typedef uint32_t __attribute__((ext_vector_type(4))) u32x4;
 typedef u32x4 __attribute__((aligned(2))) u32x4_2;
+
+// STREAM: past the caches.
+template <bool STREAM>
+__device__ __forceinline__ void put_piece(char* p, u32x4 v) {
+  if constexpr (STREAM)
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4_2*>(p));
+  else
+    *reinterpret_cast<u32x4_2*>(p) = v;
+}
 
 struct Table {
   int n;                        // tensors of this launch
@@ -37,35 +48,37 @@ struct Table {
   int64_t bytes[kPerLaunch];    // < 0: bf16
 };
 
-// The tensor of chunk c.
-__device__ __forceinline__ int find(const Table& t, uint32_t c) {
-  int lo = 0, hi = t.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (t.first[mid] <= c)
-      lo = mid;
-    else
-      hi = mid;
-  }
-  return lo;
-}
-
+// A chunk of a list: where, how many bytes.
 struct Chunk {
   const char* in;
   char* out;
-  int bytes;   // of the chunk
+  int bytes;
   bool bf16;
   __device__ Chunk(const Table& t, uint32_t c) {
-    const int i = find(t, c);
-    const int64_t all = t.bytes[i], len = all < 0 ? -all : all, at = (int64_t)(c - t.first[i]) * kChunkBytes;
+    int lo = 0, hi = t.n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (t.first[mid] <= c)
+        lo = mid;
+      else
+        hi = mid;
+    }
+    const int64_t all = t.bytes[lo], len = all < 0 ? -all : all;
+    const int64_t from = (int64_t)(c - t.first[lo]) * kChunkBytes;
     bf16 = all < 0;
-    bytes = (int)min((int64_t)kChunkBytes, len - at);
-    in = static_cast<const char*>(t.in[i]) + at;
-    out = static_cast<char*>(t.out[i]) + at;
+    bytes = (int)min((int64_t)kChunkBytes, len - from);
+    in = static_cast<const char*>(t.in[lo]) + from;
+    out = static_cast<char*>(t.out[lo]) + from;
   }
+  __device__ bool whole() const { return bytes == kChunkBytes; }
   __device__ u32x4 load(int at) const { return *reinterpret_cast<const u32x4_2*>(in + at); }
+  // the thread's pieces of a whole chunk
+  __device__ void load(u32x4 (&r)[kPer]) const {
+    if (whole())
+#pragma unroll
+      for (int k = 0; k < kPer; ++k) r[k] = load((k * kThreads + threadIdx.x) * 16);
+  }
 };
-
 // The four waves' sums, in order.
 __device__ __forceinline__ double group_sum(double v, double* sh) {
   for (int k = 32; k; k >>= 1) v += __shfl_xor(v, k);
@@ -91,22 +104,32 @@ __device__ __forceinline__ double squares(u32x4 r, bool bf16, double s) {
 
 __global__ void __launch_bounds__(kThreads) k_clip_sum(const Table t, double* part) {
   __shared__ double sh[4];
-  const Chunk c(t, blockIdx.x);
+  const uint32_t all = t.first[t.n];
   double s = 0.0;
-  if (c.bytes == kChunkBytes) {
+  Chunk next(t, blockIdx.x);
+  u32x4 ahead[kPer];
+  next.load(ahead);
+  for (uint32_t i = blockIdx.x; i < all; i += gridDim.x) {
+    const Chunk c = next;
     u32x4 r[kPer];
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) r[k] = c.load((k * kThreads + threadIdx.x) * 16);
+    for (int k = 0; k < kPer; ++k) r[k] = ahead[k];
+    if (i + gridDim.x < all) {
+      next = Chunk(t, i + gridDim.x);
+      next.load(ahead);
+    }
+    if (c.whole()) {
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) s = squares(r[k], c.bf16, s);
-  } else {
-    int at = threadIdx.x * 16;
-    for (; at + 16 <= c.bytes; at += kThreads * 16) s = squares(c.load(at), c.bf16, s);
-    const int es = c.bf16 ? 2 : 4;  // the values beyond the last whole piece: one lane's
-    for (; at < c.bytes; at += es) {
-      const double g = c.bf16 ? DType<bf16_t>::load(reinterpret_cast<const bf16_t*>(c.in + at), 0)
-                              : DType<float>::load(reinterpret_cast<const float*>(c.in + at), 0);
-      s = fma(g, g, s);
+      for (int k = 0; k < kPer; ++k) s = squares(r[k], c.bf16, s);
+    } else {
+      int at = threadIdx.x * 16;
+      for (; at + 16 <= c.bytes; at += kThreads * 16) s = squares(c.load(at), c.bf16, s);
+      const int es = c.bf16 ? 2 : 4;  // the values beyond the last whole piece: one lane's
+      for (; at < c.bytes; at += es) {
+        const double g = c.bf16 ? DType<bf16_t>::load(reinterpret_cast<const bf16_t*>(c.in + at), 0)
+                                : DType<float>::load(reinterpret_cast<const float*>(c.in + at), 0);
+        s = fma(g, g, s);
+      }
     }
   }
   s = group_sum(s, sh);
@@ -121,37 +144,46 @@ __device__ __forceinline__ u32x4 scaled(u32x4 r, bool bf16, float f) {
   return r;
 }
 
+template <bool STREAM>
 __global__ void __launch_bounds__(kThreads) k_clip_scale(const Table t, const double* part, uint32_t parts, float max_norm,
                                                          float* norm) {
   __shared__ double sh[4];
-  const Chunk c(t, gridDim.x - 1 - blockIdx.x);
-  const bool whole = c.bytes == kChunkBytes;
-  u32x4 r[kPer];
-  if (whole)
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) r[k] = c.load((k * kThreads + threadIdx.x) * 16);
+  const uint32_t all = t.first[t.n];
+  Chunk next(t, all - 1 - blockIdx.x);  // backwards: what was read last is read first
+  u32x4 ahead[kPer];
+  next.load(ahead);
   double s = 0.0;
 #pragma unroll 8
   for (uint32_t k = threadIdx.x; k < parts; k += kThreads) s += part[k];
   const double N = sqrt(group_sum(s, sh));
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)N;
   const float f = N > (double)max_norm && N < (double)INFINITY ? (float)((double)max_norm / N) : 1.0f;
-  if (f == 1.0f && c.in == c.out) return;  // in place, and within the limit
-  const int es = c.bf16 ? 2 : 4;
-  if (whole) {
+  for (uint32_t i = blockIdx.x; i < all; i += gridDim.x) {
+    const Chunk c = next;
+    u32x4 r[kPer];
 #pragma unroll
-    for (int k = 0; k < kPer; ++k)
-      *reinterpret_cast<u32x4_2*>(c.out + (k * kThreads + threadIdx.x) * 16) = scaled(r[k], c.bf16, f);
-  } else {
-    int at = threadIdx.x * 16;
-    for (; at + 16 <= c.bytes; at += kThreads * 16)
-      *reinterpret_cast<u32x4_2*>(c.out + at) = scaled(c.load(at), c.bf16, f);
-    for (; at < c.bytes; at += es) {
-      if (c.bf16)
-        DType<bf16_t>::store(reinterpret_cast<bf16_t*>(c.out + at), 0,
-                             f * DType<bf16_t>::load(reinterpret_cast<const bf16_t*>(c.in + at), 0));
-      else
-        *reinterpret_cast<float*>(c.out + at) = f * *reinterpret_cast<const float*>(c.in + at);
+    for (int k = 0; k < kPer; ++k) r[k] = ahead[k];
+    if (i + gridDim.x < all) {
+      next = Chunk(t, all - 1 - (i + gridDim.x));
+      if (f != 1.0f || next.in != next.out) next.load(ahead);
+    }
+    if (f == 1.0f && c.in == c.out) continue;  // in place, and within the limit
+    if (c.whole()) {
+#pragma unroll
+      for (int k = 0; k < kPer; ++k)
+        put_piece<STREAM>(c.out + (k * kThreads + threadIdx.x) * 16, scaled(r[k], c.bf16, f));
+    } else {
+      int at = threadIdx.x * 16;
+      for (; at + 16 <= c.bytes; at += kThreads * 16)
+        *reinterpret_cast<u32x4_2*>(c.out + at) = scaled(c.load(at), c.bf16, f);
+      const int es = c.bf16 ? 2 : 4;
+      for (; at < c.bytes; at += es) {
+        if (c.bf16)
+          DType<bf16_t>::store(reinterpret_cast<bf16_t*>(c.out + at), 0,
+                               f * DType<bf16_t>::load(reinterpret_cast<const bf16_t*>(c.in + at), 0));
+        else
+          *reinterpret_cast<float*>(c.out + at) = f * *reinterpret_cast<const float*>(c.in + at);
+      }
     }
   }
 }
@@ -161,10 +193,10 @@ __global__ void k_clip_none(float* norm) { *norm = 0.0f; }
 int64_t bytes_of(const wm_grad_tensor& t) { return t.n * (t.dtype == WM_FP32 ? 4 : 2); }
 int64_t chunks_of(const wm_grad_tensor& t) { return (bytes_of(t) + kChunkBytes - 1) / kChunkBytes; }
 
-// Runs f on the table of each launch.
+// Runs f on the table and the work-groups of each launch; the sums of them all.
 template <typename F>
-hipError_t tables(int n, const wm_grad_tensor* t, F f) {
-  uint32_t part0 = 0;
+hipError_t tables(int n, const wm_grad_tensor* t, uint32_t& part0, F f) {
+  part0 = 0;
   for (int i = 0; i < n;) {
     Table tab;
     tab.n = 0;
@@ -179,8 +211,9 @@ hipError_t tables(int n, const wm_grad_tensor* t, F f) {
       tab.first[k + 1] = tab.first[k] + (uint32_t)chunks_of(t[i]);
     }
     if (tab.n == 0) break;
-    part0 += tab.first[tab.n];
-    const hipError_t e = f(tab, tab.first[tab.n]);
+    const uint32_t groups = std::min<uint32_t>(tab.first[tab.n], kGroups);
+    part0 += groups;
+    const hipError_t e = f(tab, groups);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -189,22 +222,25 @@ hipError_t tables(int n, const wm_grad_tensor* t, F f) {
 }  // namespace
 
 size_t clip_workspace(int n, const wm_grad_tensor* t) {
-  int64_t c = 0;
-  for (int i = 0; i < n; ++i) c += chunks_of(t[i]);
-  return (size_t)c * sizeof(double);
+  uint32_t parts;
+  (void)tables(n, t, parts, [](const Table&, uint32_t) { return hipSuccess; });
+  return (size_t)parts * sizeof(double);
 }
 
 hipError_t launch_clip(int n, const wm_grad_tensor* t, float max_norm, float* norm, void* ws, hipStream_t s) {
   double* part = reinterpret_cast<double*>(ws);
-  const uint32_t total = (uint32_t)(clip_workspace(n, t) / sizeof(double));
-  if (total == 0) return launch("clip_none", k_clip_none, dim3(1), dim3(1), 0, s, norm);
-  hipError_t e = tables(n, t, [&](const Table& tab, unsigned grid) {
-    return launch("clip_sum", k_clip_sum, dim3(grid), dim3(kThreads), 0, s, tab, part);
+  uint32_t parts;
+  hipError_t e = tables(n, t, parts, [&](const Table& tab, uint32_t groups) {
+    return launch("clip_sum", k_clip_sum, dim3(groups), dim3(kThreads), 0, s, tab, part);
   });
   if (e != hipSuccess) return e;
-  return tables(n, t, [&](const Table& tab, unsigned grid) {
-    return launch("clip_scale", k_clip_scale, dim3(grid), dim3(kThreads), 0, s, tab, (const double*)part, total, max_norm,
-                  tab.part0 == 0 ? norm : nullptr);
+  if (parts == 0) return launch("clip_none", k_clip_none, dim3(1), dim3(1), 0, s, norm);
+  int64_t bytes = 0;
+  for (int i = 0; i < n; ++i) bytes += bytes_of(t[i]);
+  uint32_t again;
+  return tables(n, t, again, [&](const Table& tab, uint32_t groups) {
+    return launch("clip_scale", bytes >= kStreamBytes ? k_clip_scale<true> : k_clip_scale<false>, dim3(groups),
+                  dim3(kThreads), 0, s, tab, (const double*)part, parts, max_norm, tab.part0 == 0 ? norm : nullptr);
   });
 }
 

@@ -59,14 +59,25 @@ template <> struct Chan<float> {
   typedef float raw;
   __device__ static raw load(uint64_t row, uint32_t off) { return *reinterpret_cast<const WM_GLOBAL float*>(row + off); }
   __device__ static float get(raw r) { return r; }
-  __device__ static void put(uint64_t row, uint32_t off, float v) { *reinterpret_cast<WM_GLOBAL float*>(row + off) = v; }
+  template <bool STREAM>
+  __device__ static void put(uint64_t row, uint32_t off, float v) {
+    if constexpr (STREAM)  // past the caches
+      __builtin_nontemporal_store(v, reinterpret_cast<WM_GLOBAL float*>(row + off));
+    else
+      *reinterpret_cast<WM_GLOBAL float*>(row + off) = v;
+  }
 };
 template <> struct Chan<bf16_t> {
   typedef uint32_t raw;  // a register of its own: halves would make one load wait for another
   __device__ static raw load(uint64_t row, uint32_t off) { return *reinterpret_cast<const WM_GLOBAL bf16_t*>(row + off); }
   __device__ static float get(raw r) { return bf16_bits_to_f32(r); }
+  template <bool STREAM>
   __device__ static void put(uint64_t row, uint32_t off, float v) {
-    *reinterpret_cast<WM_GLOBAL bf16_t*>(row + off) = (bf16_t)f32_to_bf16_bits(v);
+    const bf16_t b = (bf16_t)f32_to_bf16_bits(v);
+    if constexpr (STREAM)
+      __builtin_nontemporal_store(b, reinterpret_cast<WM_GLOBAL bf16_t*>(row + off));
+    else
+      *reinterpret_cast<WM_GLOBAL bf16_t*>(row + off) = b;
   }
 };
 #undef WM_GLOBAL
@@ -129,7 +140,7 @@ struct Lanes {
 // wave's first lane as an address in scalar registers, the lane's place from
 // there as a 32-bit offset (the call checks that the rows that a wave can reach
 // lie within 2 GiB).
-template <typename DT>
+template <typename DT, bool STREAM = false>
 struct Rows {
   uint64_t base, row;
   long st, b;    // bytes
@@ -150,7 +161,7 @@ struct Rows {
     asm volatile("" : "+v"(off));
   }
   __device__ typename Chan<DT>::raw load() const { return Chan<DT>::load(row, off); }
-  __device__ void put(float v) const { Chan<DT>::put(row, off, v); }
+  __device__ void put(float v) const { Chan<DT>::template put<STREAM>(row, off, v); }
 };
 
 // The resets of TT steps from t0 on: one byte a lane holds 64 / TT rows by TT
@@ -186,9 +197,9 @@ struct Resets {
 
 // One tile; LOAD: the next tile's value of each step is requested as soon as
 // the present one's is used.  MASKED: some step is padding or starts anew.
-template <bool LOAD, bool MASKED, typename DT, int TT>
+template <bool LOAD, bool MASKED, typename DT, int TT, bool STREAM>
 __device__ __forceinline__ float walk_tile(float h, typename Chan<DT>::raw (&gr)[TT], typename Chan<DT>::raw (&xr)[TT],
-                                           Rows<DT>& g, Rows<DT>& x, Rows<DT>& y, int steps, int ahead, int live,
+                                           Rows<DT>& g, Rows<DT>& x, Rows<DT, STREAM>& y, int steps, int ahead, int live,
                                            uint32_t rs, bool on) {
 #pragma unroll
   for (int i = 0; i < TT; ++i) {
@@ -215,14 +226,15 @@ __device__ __forceinline__ float walk_tile(float h, typename Chan<DT>::raw (&gr)
   return h;
 }
 
-template <typename DT, int TT>
+template <typename DT, int TT, bool STREAM>
 __global__ void __launch_bounds__(256) k_linrec_walk(const LinrecArgs a) {
   const long C = (long)a.B * a.H, group = (long)blockIdx.x * (blockDim.x >> 6) + uniform(threadIdx.x >> 6);
   if (group * 64 >= C) return;
   const Lanes l(group, a.T, a.B, a.H, a.lengths);
   Resets<TT> rb;
   rb.ask(a.resets, l, 0, l.most, a.B);
-  Rows<DT> g(a.gate, l, 0), x(a.x, l, 0), y(SeqView{a.y, C, a.H}, l, 0);
+  Rows<DT> g(a.gate, l, 0), x(a.x, l, 0);
+  Rows<DT, STREAM> y(SeqView{a.y, C, a.H}, l, 0);
   typename Chan<DT>::raw gr[TT], xr[TT];
   if (l.most > 0)
 #pragma unroll
@@ -240,11 +252,11 @@ __global__ void __launch_bounds__(256) k_linrec_walk(const LinrecArgs a) {
     if (ahead > 0) rb.ask(a.resets, l, t0 + TT, l.most, a.B);
     if (a.states && l.on) a.states[(long)(t0 / kTT) * C + l.c] = h;
     if (ahead > 0)
-      h = masked ? walk_tile<true, true, DT, TT>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on)
-                 : walk_tile<true, false, DT, TT>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on);
+      h = masked ? walk_tile<true, true, DT, TT, STREAM>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on)
+                 : walk_tile<true, false, DT, TT, STREAM>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on);
     else
-      h = masked ? walk_tile<false, true, DT, TT>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on)
-                 : walk_tile<false, false, DT, TT>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on);
+      h = masked ? walk_tile<false, true, DT, TT, STREAM>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on)
+                 : walk_tile<false, false, DT, TT, STREAM>(h, gr, xr, g, x, y, steps, ahead, live, rs, l.on);
   }
   // padding of every row of the wave
   y.to(l.most);
@@ -260,12 +272,12 @@ __global__ void __launch_bounds__(256) k_linrec_walk(const LinrecArgs a) {
 // without them the compiler loads both ways' next values ahead of the branch, 48
 // registers too many, and selections in every step keep as many conditions in
 // scalar registers.
-template <typename DT, int TT>
+template <typename DT, int TT, bool STREAM>
 __global__ void __launch_bounds__(256, 4) k_linrec_grad_walk(const LinrecGradArgs a) {
   const long C = (long)a.B * a.H, group = (long)blockIdx.x * (blockDim.x >> 6) + uniform(threadIdx.x >> 6);
   if (group * 64 >= C) return;
   const Lanes l(group, a.T, a.B, a.H, a.lengths);
-  Rows<DT> dx(a.dx, l, l.most), dg(a.dgate, l, l.most);
+  Rows<DT, STREAM> dx(a.dx, l, l.most), dg(a.dgate, l, l.most);
   for (int t = l.most; t < a.T; ++t, dx.move(dx.st), dg.move(dg.st))
     if (l.on) {
       dx.put(0.0f);
@@ -523,7 +535,7 @@ __device__ __forceinline__ Map fold(float (&A)[kTT], float (&U)[kTT], const type
   return m;
 }
 
-template <typename DT>
+template <typename DT, bool STREAM>
 __global__ void __launch_bounds__(64 * kWaves) k_linrec_split(const LinrecArgs a, const Chain ch, int waves) {
   __shared__ Shared sh;
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
@@ -550,7 +562,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_linrec_split(const LinrecArgs a
   for (int i = 0; i < kWaves - 1; ++i)
     if (i < w) h = apply(sh.tile[i][lane], h);
   if (a.states && k.on && k.nt > 0) a.states[(long)(k.t0 / kTT) * C + k.c] = h;
-  Rows<DT> y(SeqView{a.y, C, a.H}, k, k.t0);
+  Rows<DT, STREAM> y(SeqView{a.y, C, a.H}, k, k.t0);
   if (whole) {
 #pragma unroll
     for (int i = 0; i < kTT; ++i, y.move(y.st)) {
@@ -604,11 +616,11 @@ __device__ __forceinline__ Map fold_grad(float (&A)[kTT], float (&M)[kTT], float
   return r;
 }
 
-template <bool MASKED, typename DT>
+template <bool MASKED, typename DT, bool STREAM>
 __device__ __forceinline__ float emit_grad(const float (&A)[kTT], const float (&M)[kTT], const float (&G)[kTT], float R,
                                            const typename Chan<DT>::raw (&dr)[kTT], const Tile& k,
                                            const LinrecGradArgs& a) {
-  Rows<DT> dx(a.dx, k, k.t0 + kTT - 1), dg(a.dgate, k, k.t0 + kTT - 1);
+  Rows<DT, STREAM> dx(a.dx, k, k.t0 + kTT - 1), dg(a.dgate, k, k.t0 + kTT - 1);
 #pragma unroll
   for (int i = kTT - 1; i >= 0; --i, dx.move(-dx.st), dg.move(-dg.st)) {
     float ox = 0.0f, og = 0.0f;
@@ -627,7 +639,7 @@ __device__ __forceinline__ float emit_grad(const float (&A)[kTT], const float (&
   return R;
 }
 
-template <typename DT>
+template <typename DT, bool STREAM>
 __global__ void __launch_bounds__(64 * kWaves) k_linrec_grad_split(const LinrecGradArgs a, const Chain ch, int waves) {
   __shared__ Shared sh;
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
@@ -655,7 +667,7 @@ __global__ void __launch_bounds__(64 * kWaves) k_linrec_grad_split(const LinrecG
 #pragma unroll
   for (int i = kWaves - 1; i > 0; --i)
     if (i > w && i < waves) R = apply(sh.tile[i][lane], R);
-  R = whole ? emit_grad<false, DT>(A, M, G, R, dr, k, a) : emit_grad<true, DT>(A, M, G, R, dr, k, a);
+  R = whole ? emit_grad<false, DT, STREAM>(A, M, G, R, dr, k, a) : emit_grad<true, DT, STREAM>(A, M, G, R, dr, k, a);
   if (ch.leave && k.on && k.t0 == ch.t0) ch.leave[k.c] = R;
 }
 
@@ -753,17 +765,24 @@ size_t linrec_workspace(int T, int B, int H) {
 }
 
 hipError_t launch_linrec(int dtype, const LinrecArgs& a, hipStream_t s) {
-  return dtype == WM_FP32 ? run("linrec", k_linrec_walk<float, kTT>, k_linrec_walk<float, 1>, k_linrec_split<float>, a,
-                                a.h0, a.h_T, false, s)
-                          : run("linrec", k_linrec_walk<bf16_t, kTT>, k_linrec_walk<bf16_t, 1>, k_linrec_split<bf16_t>, a,
-                                a.h0, a.h_T, false, s);
+  auto go = [&](auto dt) {
+    typedef decltype(dt) DT;
+    const bool stream = (long)a.T * a.B * a.H * (long)sizeof(DT) >= kStreamBytes;
+    return run("linrec", stream ? k_linrec_walk<DT, kTT, true> : k_linrec_walk<DT, kTT, false>, k_linrec_walk<DT, 1, false>,
+               stream ? k_linrec_split<DT, true> : k_linrec_split<DT, false>, a, a.h0, a.h_T, false, s);
+  };
+  return dtype == WM_FP32 ? go(0.0f) : go(bf16_t());
 }
 
 hipError_t launch_linrec_grad(int dtype, const LinrecGradArgs& a, hipStream_t s) {
-  return dtype == WM_FP32 ? run("linrec_grad", k_linrec_grad_walk<float, kTT>, k_linrec_grad_walk<float, 1>,
-                                k_linrec_grad_split<float>, a, a.dh_T, a.dh0, true, s)
-                          : run("linrec_grad", k_linrec_grad_walk<bf16_t, kTT>, k_linrec_grad_walk<bf16_t, 1>,
-                                k_linrec_grad_split<bf16_t>, a, a.dh_T, a.dh0, true, s);
+  auto go = [&](auto dt) {
+    typedef decltype(dt) DT;
+    const bool stream = 2L * a.T * a.B * a.H * (long)sizeof(DT) >= kStreamBytes;
+    return run("linrec_grad", stream ? k_linrec_grad_walk<DT, kTT, true> : k_linrec_grad_walk<DT, kTT, false>,
+               k_linrec_grad_walk<DT, 1, false>, stream ? k_linrec_grad_split<DT, true> : k_linrec_grad_split<DT, false>, a,
+               a.dh_T, a.dh0, true, s);
+  };
+  return dtype == WM_FP32 ? go(0.0f) : go(bf16_t());
 }
 
 }  // namespace wm

@@ -97,11 +97,17 @@ struct Place {
       }
     }
   }
+  template <bool STREAM>
   __device__ void store(DT* x, int p, const float* v) const {
     if (lo[p] >= hi) return;
     if (hi == V) {
       const uint4 r = Piece<DT>::put(v);
-      *reinterpret_cast<typename Memory<DT>::type*>(x + col[p]) = u32x4{r.x, r.y, r.z, r.w};
+      typename Memory<DT>::type* to = reinterpret_cast<typename Memory<DT>::type*>(x + col[p]);
+      const u32x4 w = {r.x, r.y, r.z, r.w};
+      if constexpr (STREAM)
+        __builtin_nontemporal_store(w, to);
+      else
+        *to = w;
     } else {
 #pragma unroll
       for (int j = 0; j < V; ++j)
@@ -171,7 +177,7 @@ __device__ __forceinline__ float2 row_sum(float2 v, float2 (*sh)[8], int& turn) 
   return v;
 }
 
-template <typename DT, int P, int L>
+template <typename DT, int P, int L, bool STREAM>
 __global__ void __launch_bounds__(threads(L)) k_norm(const NormArgs a) {
   constexpr int V = Piece<DT>::VEC, kThreads = threads(L), kRows = kThreads / L;
   __shared__ float2 sh[2][8];
@@ -213,7 +219,7 @@ __global__ void __launch_bounds__(threads(L)) k_norm(const NormArgs a) {
     for (int p = 0; p < P; ++p) {
 #pragma unroll
       for (int j = 0; j < V; ++j) v[p][j] = fmaf(v[p][j] * rs, g[p][j], b[p][j]);
-      at.store(y, p, v[p]);
+      at.template store<STREAM>(y, p, v[p]);
     }
     if (t == 0 && a.mean) {
       a.mean[row] = mu;
@@ -223,7 +229,7 @@ __global__ void __launch_bounds__(threads(L)) k_norm(const NormArgs a) {
 }
 
 // part [gridDim.x][2][H]: this work-group's sums of dy xh, then of dy.
-template <typename DT, int P, int L>
+template <typename DT, int P, int L, bool STREAM>
 __global__ void __launch_bounds__(threads(L)) k_norm_grad(const NormGradArgs a) {
   constexpr int V = Piece<DT>::VEC, kThreads = threads(L), kRows = kThreads / L;
   __shared__ float2 sh[2][8];
@@ -283,7 +289,7 @@ __global__ void __launch_bounds__(threads(L)) k_norm_grad(const NormGradArgs a) 
         const float xh = (v[j] - m0) * r0;
         v[j] = r0 * (d[j] * g[p][j] - m - xh * mx);
       }
-      at.store(dx, p, v);
+      at.template store<STREAM>(dx, p, v);
     }
   }
   // the groups' sums in order: a thread adds one column at a time
@@ -369,7 +375,9 @@ hipError_t launch_layer_norm(int dtype, const NormArgs& a, hipStream_t s) {
     typedef decltype(dt) DT;
     return by_width<DT>(a.H, [&](auto p, auto l) {
       const long per = threads(l) / l, groups = std::min<long>((a.rows + per - 1) / per, kGroups);
-      return launch("norm", k_norm<DT, p, l>, dim3((unsigned)groups), dim3(threads(l)), 0, s, a);
+      const bool stream = a.rows * a.H * (long)sizeof(DT) >= kStreamBytes;
+      return launch("norm", stream ? k_norm<DT, p, l, true> : k_norm<DT, p, l, false>, dim3((unsigned)groups),
+                    dim3(threads(l)), 0, s, a);
     });
   };
   return dtype == WM_FP32 ? run(0.0f) : run(bf16_t());
@@ -382,7 +390,9 @@ hipError_t launch_layer_norm_grad(int dtype, const NormGradArgs& a, hipStream_t 
   auto run = [&](auto dt) {
     typedef decltype(dt) DT;
     return by_width<DT>(a.H, [&](auto p, auto l) {
-      return launch("norm_grad", k_norm_grad<DT, p, l>, dim3(n), dim3(threads(l)), 0, s, a);
+      const bool stream = a.rows * a.H * (long)sizeof(DT) >= kStreamBytes;
+      return launch("norm_grad", stream ? k_norm_grad<DT, p, l, true> : k_norm_grad<DT, p, l, false>, dim3(n),
+                    dim3(threads(l)), 0, s, a);
     });
   };
   const hipError_t e = dtype == WM_FP32 ? run(0.0f) : run(bf16_t());

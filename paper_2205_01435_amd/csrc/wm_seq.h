@@ -9,6 +9,12 @@
 
 namespace wm {
 
+// An output of at least this size goes past the caches: it is half of the
+// last-level one, which it would empty of what is read again (the values of a
+// gradient list, the input of a norm for its gradient).  A smaller one is left
+// there for the next call.
+constexpr int64_t kStreamBytes = (int64_t)128 << 20;
+
 struct EmbedArgs {
   long n;
   int V, H;
