@@ -47,7 +47,11 @@ constexpr int kTT = 16;        // steps of a tile
 constexpr int kSeg = kWaves * kTT;
 constexpr int kFan = 16;       // segments whose maps are composed into one for the segments after them
 constexpr int kMaxSegs = 1024; // segments of a launch; longer sequences take several
-constexpr long kWalk = 2048;   // channel groups from which a wave walks all steps
+// Channel groups (of 64) from which a wave walks all steps.  Measured, forward
+// and gradient of 500 steps, split against walked: fp32 1024 groups 218 and 219
+// us, 1536 318 and 300; bf16 1024 groups 155 and 192 us, 1536 214 and 224, 4096
+// (128 steps) 141 and 105.
+constexpr long kWalk32 = 1280, kWalk16 = 2048;
 constexpr unsigned kSpinLimit = 1u << 22;
 constexpr unsigned long long kEmpty = ~0ull;  // a map not yet published (A's bits would be a NaN of this sign)
 
@@ -97,10 +101,14 @@ __device__ __forceinline__ Map then(Map m, Map n) {
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// e^-|g|, on the short way where the whole wave allows it (NaN and infinity
-// lie beyond the bound).
+// e^-|g|: the long way too where some lane of the wave needs it (NaN and
+// infinity lie beyond the bound), for that lane alone: a channel's bits do not
+// depend on its neighbours.
+__device__ __forceinline__ float gate_exp_any(float g) {
+  return fabsf(g) <= kGateMost ? gate_exp_small(g) : expf(-fabsf(g));
+}
 __device__ __forceinline__ float gate_exp(float g) {
-  if (__builtin_expect(__any(!(fabsf(g) <= kGateMost)), 0)) return expf(-fabsf(g));
+  if (__builtin_expect(__any(!(fabsf(g) <= kGateMost)), 0)) return gate_exp_any(g);
   return gate_exp_small(g);
 }
 
@@ -519,13 +527,13 @@ __device__ __forceinline__ Map fold(float (&A)[kTT], float (&U)[kTT], const type
     if (MASKED && i >= k.some) continue;
     const float g = Chan<DT>::get(gr[i]), x = Chan<DT>::get(xr[i]);
     if constexpr (MASKED) {
-      const float2 p = gate_pair(g);
+      const float2 p = gate_pair_of(g, gate_exp_any(g));
       const bool live = i < k.live;
       A[i] = live ? (k.reset(i) ? -1.0f : p.x) : 1.0f;
       U[i] = live ? p.y * x : 0.0f;
       m = then(m, {A[i], U[i]});
     } else {
-      const float2 p = gate_pair_small(g);
+      const float2 p = gate_pair_of(g, gate_exp_small(g));
       A[i] = p.x;
       U[i] = p.y * x;
       m.A *= p.x;
@@ -536,7 +544,7 @@ __device__ __forceinline__ Map fold(float (&A)[kTT], float (&U)[kTT], const type
 }
 
 template <typename DT, bool STREAM>
-__global__ void __launch_bounds__(64 * kWaves) k_linrec_split(const LinrecArgs a, const Chain ch, int waves) {
+__global__ void __launch_bounds__(64 * kWaves, 6) k_linrec_split(const LinrecArgs a, const Chain ch, int waves) {
   __shared__ Shared sh;
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
   const long C = (long)a.B * a.H;
@@ -592,7 +600,7 @@ __device__ __forceinline__ Map fold_grad(float (&A)[kTT], float (&M)[kTT], float
   for (int i = 0; i < kTT; ++i) {
     if (MASKED && i >= k.some) continue;
     const float g = Chan<DT>::get(gr[i]), x = Chan<DT>::get(xr[i]), d = Chan<DT>::get(dr[i]);
-    const float2 p = MASKED ? gate_pair(g) : gate_pair_small(g);
+    const float2 p = gate_pair_of(g, MASKED ? gate_exp_any(g) : gate_exp_small(g));
     A[i] = p.x;
     M[i] = p.y;
     if (MASKED && k.reset(i)) h = 0.0f;
@@ -687,9 +695,9 @@ struct Plan {
   int waves;  // tiles of a segment
   long segs;
 };
-Plan plan(int T, int B, int H) {
+Plan plan(int dtype, int T, int B, int H) {
   const long groups = ((long)B * H + 63) / 64, tiles = ((long)T + kTT - 1) / kTT;
-  if (tiles <= 1 || groups >= kWalk) return {0, 0};
+  if (tiles <= 1 || groups >= (dtype == WM_FP32 ? kWalk32 : kWalk16)) return {0, 0};
   if (tiles <= kWaves) return {(int)tiles, 1};
   return {kWaves, (tiles + kWaves - 1) / kWaves};
 }
@@ -741,9 +749,9 @@ hipError_t run_chain(int T, int B, int H, const Plan& p, void* ws, const float* 
 }
 
 template <typename W, typename S, typename A>
-hipError_t run(const char* name, W walk, W step, S split, const A& a, const float* from, float* to, bool reverse,
-               hipStream_t s) {
-  const Plan p = plan(a.T, a.B, a.H);
+hipError_t run(const char* name, int dtype, W walk, W step, S split, const A& a, const float* from, float* to,
+               bool reverse, hipStream_t s) {
+  const Plan p = plan(dtype, a.T, a.B, a.H);
   if (p.waves == 0) {
     const long groups = ((long)a.B * a.H + 63) / 64;
     return launch(name, a.T <= 1 ? step : walk, dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, s, a);
@@ -758,7 +766,7 @@ hipError_t run(const char* name, W walk, W step, S split, const A& a, const floa
 size_t linrec_states(int T, int B, int H) { return ((size_t)T + kTT - 1) / kTT * B * H * sizeof(float); }
 
 size_t linrec_workspace(int T, int B, int H) {
-  const Plan p = plan(T, B, H);
+  const Plan p = plan(WM_BF16, T, B, H);  // (split wherever fp32 is, and beyond)
   if (p.segs <= 1) return 0;
   const long pad = pad_channels(B, H);
   return kHeadBytes + (size_t)map_words(std::min<long>(p.segs, kMaxSegs), pad) * 8 + (size_t)pad * 2 * sizeof(float);
@@ -768,7 +776,7 @@ hipError_t launch_linrec(int dtype, const LinrecArgs& a, hipStream_t s) {
   auto go = [&](auto dt) {
     typedef decltype(dt) DT;
     const bool stream = (long)a.T * a.B * a.H * (long)sizeof(DT) >= kStreamBytes;
-    return run("linrec", stream ? k_linrec_walk<DT, kTT, true> : k_linrec_walk<DT, kTT, false>, k_linrec_walk<DT, 1, false>,
+    return run("linrec", dtype, stream ? k_linrec_walk<DT, kTT, true> : k_linrec_walk<DT, kTT, false>, k_linrec_walk<DT, 1, false>,
                stream ? k_linrec_split<DT, true> : k_linrec_split<DT, false>, a, a.h0, a.h_T, false, s);
   };
   return dtype == WM_FP32 ? go(0.0f) : go(bf16_t());
@@ -778,7 +786,7 @@ hipError_t launch_linrec_grad(int dtype, const LinrecGradArgs& a, hipStream_t s)
   auto go = [&](auto dt) {
     typedef decltype(dt) DT;
     const bool stream = 2L * a.T * a.B * a.H * (long)sizeof(DT) >= kStreamBytes;
-    return run("linrec_grad", stream ? k_linrec_grad_walk<DT, kTT, true> : k_linrec_grad_walk<DT, kTT, false>,
+    return run("linrec_grad", dtype, stream ? k_linrec_grad_walk<DT, kTT, true> : k_linrec_grad_walk<DT, kTT, false>,
                k_linrec_grad_walk<DT, 1, false>, stream ? k_linrec_grad_split<DT, true> : k_linrec_grad_split<DT, false>, a,
                a.dh_T, a.dh0, true, s);
   };

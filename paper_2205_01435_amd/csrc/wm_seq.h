@@ -106,14 +106,14 @@ hipError_t launch_clip(int n, const wm_grad_tensor* t, float max_norm, float* no
 
 // (sigmoid(g), sigmoid(-g)), each to full relative precision, from e^-|g|:
 // 1 / (1 + e) by one Newton step from the hardware's reciprocal, and e times it.
+// Only g's sign is looked at, that of a zero too (e itself may carry it).
 __device__ __forceinline__ float2 gate_pair_of(float g, float e) {
   const float w = 1.0f + e;
   float r = __builtin_amdgcn_rcpf(w);
   r = fmaf(fmaf(-w, r, 1.0f), r, r);
   const float q = e * r;
-  return g >= 0.0f ? make_float2(r, q) : make_float2(q, r);
+  return __float_as_int(g) >= 0 ? make_float2(r, q) : make_float2(q, r);
 }
-__device__ __forceinline__ float2 gate_pair(float g) { return gate_pair_of(g, expf(-fabsf(g))); }
 
 // e^-|g| for |g| <= kGateMost, in half of expf's instructions: with p =
 // -|g| log2(e) rounded and d = -|g| - p ln 2 what the rounding left over it is
@@ -126,6 +126,5 @@ __device__ __forceinline__ float gate_exp_small(float g) {
   const float t = __builtin_amdgcn_exp2f(p);
   return fmaf(t, d, t);
 }
-__device__ __forceinline__ float2 gate_pair_small(float g) { return gate_pair_of(g, gate_exp_small(g)); }
 
 }  // namespace wm

@@ -107,6 +107,26 @@ def test_non_finite_gradients_pass_and_show(bad):
     assert torch.equal(plan.outs[0], h) and torch.equal(plan.outs[1].nan_to_num(7.0), g.nan_to_num(7.0))
 
 
+@pytest.mark.parametrize("over", [True, False])
+def test_lists_larger_than_the_cache(over):
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    grads = [torch.randn(n, generator=gen, device="cuda").to(dt) for n, dt in
+             ((20000003, torch.float32), (5, torch.bfloat16), (40000001, torch.bfloat16), (1000, torch.float32))]
+    n = float(sum((g.double() ** 2).sum() for g in grads)) ** 0.5
+    plan = wm.ClipPlan(grads, [torch.empty_like(g) for g in grads])
+    limit = n / 4 if over else n * 2
+    norm = float(wm.clip_grads(plan, limit))
+    assert abs(norm - n) <= 2 * seq.U32 * n
+    for g, o in zip(grads, plan.outs):
+        if over:
+            f = limit / n
+            d = (o.double() - g.double() * f).abs()
+            lim = g.double().abs() * f * (3 * seq.U32 + (seq.U16 if g.dtype == torch.bfloat16 else 0.0)) + 2.0 ** -126
+            assert bool((d <= lim).all())
+        else:
+            assert torch.equal(o, g)
+
+
 def test_tensor_given_other_memory():
     p = torch.ones(100, device="cuda")
     plan = wm.ClipPlan([p], [torch.zeros(100, device="cuda")])

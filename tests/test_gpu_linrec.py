@@ -181,15 +181,75 @@ def test_a_nan_stays_to_the_end_of_its_trajectory():
     assert bool(nan[10:, 0, 5].all()) and int(nan.sum()) == T - 10
 
 
-@pytest.mark.parametrize("gate", [float("-inf"), float("inf"), -200.0, 200.0, -88.0, 0.0])
-def test_extreme_gates(gate):
-    T, B, H = 40, 2, 16
+@pytest.mark.parametrize("T", [12, 40])
+@pytest.mark.parametrize("gate", [float("-inf"), float("inf"), -200.0, 200.0, -88.0, -0.0, 0.0, -3.4028234e38])
+def test_extreme_gates(gate, T):
+    B, H = 2, 16
     d, t = _inputs(T, B, H, "fp32", False, 7)
     d["gate"] = np.full((T, B, H), gate)
     t["gate"] = torch.full((T, B, H), gate, device="cuda")
     bufs = wm.LinrecBuffers(T, B, H)
     _run(t, bufs)
     _compare(d, bufs, "fp32")
+
+
+@pytest.mark.parametrize("dtype,masks,packed", [("fp32", True, True), ("bf16", True, False), ("bf16", False, True)])
+def test_many_channels(dtype, masks, packed):
+    """Enough channels that a wave takes all steps of its own: rows that share
+    a wave (H 437), several tiles, a last one that is short."""
+    T, B, H = 50, 301, 437
+    d, t = _inputs(T, B, H, dtype, masks, 13, packed)
+    bufs, check = _bufs(T, B, H, dtype)
+    _run(t, bufs)
+    check()
+    _compare(d, bufs, dtype)
+
+
+def test_many_rows_of_one_channel():
+    T, B, H = 35, 131073, 1
+    d, t = _inputs(T, B, H, "fp32", True, 14)
+    bufs, check = _bufs(T, B, H, "fp32")
+    _run(t, bufs)
+    check()
+    _compare(d, bufs, "fp32")
+
+
+def test_masked_places_may_hold_anything_where_a_wave_takes_all_steps():
+    T, B, H = 40, 600, 256
+    _, t = _inputs(T, B, H, "fp32", True, 15)
+    clean, _ = _bufs(T, B, H, "fp32")
+    _run(t, clean)
+    pad = torch.arange(T, device="cuda")[:, None] >= t["lengths"][None, :]
+    dirty = {k: (t[k].masked_fill(pad[..., None], v) if k in ("x", "gate", "dy") else t[k])
+             for k, v in (("x", float("nan")), ("gate", float("inf")), ("dy", float("nan")), ("h0", 0), ("dh_T", 0),
+                          ("resets", 0), ("lengths", 0))}
+    first = (t["resets"][0] != 0) & (t["lengths"] > 0)
+    dirty["h0"] = t["h0"].masked_fill(first[:, None], float("nan"))
+    got, _ = _bufs(T, B, H, "fp32")
+    _run(dirty, got)
+    assert bool(first.any())
+    for k in ("y", "h_T", "dxg", "dh0"):
+        assert torch.equal(getattr(got, k), getattr(clean, k)), k
+
+
+@pytest.mark.parametrize("T,B,H,dtype", [(64, 600, 1024, "fp32"), (3000, 24, 1024, "bf16")])
+def test_outputs_larger_than_the_cache(T, B, H, dtype):
+    """The rows of a large call are those of two halves, bit for bit."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda", dtype=torch.float32).to(TORCH[dtype])  # noqa: E731
+    t = dict(x=r(T, B, H), gate=r(T, B, H) + 2, dy=r(T, B, H), h0=torch.randn(B, H, generator=g, device="cuda"),
+             dh_T=torch.randn(B, H, generator=g, device="cuda"),
+             resets=(torch.rand(T, B, generator=g, device="cuda") < 0.02).to(torch.uint8),
+             lengths=torch.randint(0, T + 1, (B,), generator=g, device="cuda", dtype=torch.int32))
+    whole = wm.LinrecBuffers(T, B, H, TORCH[dtype])
+    _run(t, whole)
+    for lo, hi in ((0, B // 2), (B // 2, B)):
+        cut = {k: v[:, lo:hi].contiguous() if v.dim() > 1 and v.shape[0] == T and v.shape[1] == B else v[lo:hi].contiguous()
+               for k, v in t.items()}
+        part = wm.LinrecBuffers(T, hi - lo, H, TORCH[dtype])
+        _run(cut, part)
+        assert torch.equal(whole.y[:, lo:hi], part.y) and torch.equal(whole.dxg[:, lo:hi], part.dxg)
+        assert torch.equal(whole.h_T[lo:hi], part.h_T) and torch.equal(whole.dh0[lo:hi], part.dh0)
 
 
 def test_steps_continue_a_sequence():

@@ -120,6 +120,21 @@ def test_gradient_against_differences():
     assert abs(slope - float((host(bufs.dx) * v).sum())) <= tol
 
 
+def test_outputs_larger_than_the_cache():
+    """The rows of a large call are those of its parts, bit for bit."""
+    rows, H = 140001, 512
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    x, dy = (torch.randn(rows, H, generator=gen, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    g, b = torch.randn(H, generator=gen, device="cuda"), torch.randn(H, generator=gen, device="cuda")
+    whole = wm.layer_norm(x, g, b)
+    wm.layer_norm_grad(x, dy, g, bufs=whole)
+    for lo, hi in ((0, 60000), (60000, rows)):
+        part = wm.layer_norm(x[lo:hi], g, b)
+        wm.layer_norm_grad(x[lo:hi], dy[lo:hi], g, bufs=part)
+        for k in ("y", "mean", "rstd", "dx"):
+            assert torch.equal(getattr(whole, k)[lo:hi], getattr(part, k)), k
+
+
 def test_no_rows():
     bufs = wm.LayerNormBuffers(0, 16)
     x = torch.empty(0, 16, device="cuda")
