@@ -507,26 +507,39 @@ def _act(name, t, dtype=None):
     return _ACT[t.dtype]
 
 
+def _arr(name, t, dtype, shape, device, optional=False):
+    """The address of a contiguous array argument (None if it is optional and
+    absent): _need's checks, spelled out only where one fails."""
+    if t is None and optional:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous()
+            and t.device == device):
+        _need(name, t, dtype, shape, device)
+    return t.data_ptr()
+
+
 def _rows(name, t, H, dtype, device):
     """(rows, distance between rows) of a [..., H] tensor with unit stride
     along H whose leading dimensions step evenly."""
-    _act(name, t, dtype)
-    if t.device != device:
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != device:
+        _act(name, t, dtype)
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if t.dim() < 1 or t.shape[-1] != H:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [..., {H}]")
-    if t.dim() != 2:
-        if t.numel() == 0:
-            return t.numel() // max(H, 1), H
+    shape = t.shape
+    if not shape or shape[-1] != H:
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected [..., {H}]")
+    if t.is_contiguous():
+        return t.numel() // H if H else 0, H
+    if len(shape) != 2:
         try:
             t = t.view(-1, H)
         except RuntimeError:
             raise ValueError(f"{name}'s rows are not evenly spaced (strides {t.stride()})") from None
-    n = t.shape[0]
-    if H > 1 and t.stride(1) != 1:
+    n, (ld, unit) = t.shape[0], t.stride()
+    if H > 1 and unit != 1:
         raise ValueError(f"{name} must have unit stride along its last dimension")
-    ld = t.stride(0) if n > 1 else H
-    if n > 1 and ld < H:
+    if n <= 1:
+        return n, H
+    if ld < H:
         raise ValueError(f"{name}'s rows overlap (stride {ld}, width {H})")
     return n, ld
 
@@ -536,17 +549,19 @@ def embed(table, tokens, scale: float = 1.0, out=None):
     int32 ``tokens`` of any shape, times ``scale`` (zero rows for tokens
     outside [0, V)).  Returns ``out``, tokens.shape + (H,) in the table's type."""
     dt = _act("table", table)
-    dev = table.device
+    dev, dtype = table.device, table.dtype
+    if table.dim() != 2:
+        raise ValueError(f"table has shape {tuple(table.shape)}, expected [V, H]")
     V, H = table.shape
-    _need("table", table, table.dtype, (V, H))
-    _need("tokens", tokens, torch.int32, tokens.shape, dev)
+    pt = _arr("table", table, dtype, table.shape, dev)
+    pk = _arr("tokens", tokens, torch.int32, getattr(tokens, "shape", ()), dev)
     n = tokens.numel()
     if out is None:
-        out = torch.empty((*tokens.shape, H), dtype=table.dtype, device=dev)
-    rows, ld = _rows("out", out, H, table.dtype, dev)
+        out = torch.empty((*tokens.shape, H), dtype=dtype, device=dev)
+    rows, ld = _rows("out", out, H, dtype, dev)
     if rows != n:
         raise ValueError(f"out has {rows} rows for {n} tokens")
-    _check(load().wm_embed(dt, n, V, H, tokens.data_ptr(), table.data_ptr(), scale, out.data_ptr(), ld, _stream()))
+    _check(load().wm_embed(dt, n, V, H, pk, pt, scale, out.data_ptr(), ld, _stream()))
     return out
 
 
@@ -565,8 +580,9 @@ def embed_grad(tokens, dout, V: int, scale: float = 1.0, bufs: EmbedGradBuffers 
     """Launch wm_embed_grad on the current stream: the gradient of embed with
     respect to its table, from ``dout`` (tokens.shape + (H,))."""
     dt = _act("dout", dout)
-    dev, H, n = dout.device, dout.shape[-1], tokens.numel()
-    _need("tokens", tokens, torch.int32, tokens.shape, dev)
+    dev, H = dout.device, dout.shape[-1]
+    pk = _arr("tokens", tokens, torch.int32, getattr(tokens, "shape", ()), dev)
+    n = tokens.numel()
     rows, ld = _rows("dout", dout, H, dout.dtype, dev)
     if rows != n:
         raise ValueError(f"dout has {rows} rows for {n} tokens")
@@ -574,7 +590,7 @@ def embed_grad(tokens, dout, V: int, scale: float = 1.0, bufs: EmbedGradBuffers 
         bufs = EmbedGradBuffers(n, V, H, dev)
     if (bufs.V, bufs.H) != (V, H) or bufs.grad.device != dev:
         raise ValueError(f"buffers for V={bufs.V} H={bufs.H} on {bufs.grad.device}; the call has V={V} H={H} on {dev}")
-    _check(load().wm_embed_grad(dt, n, V, H, tokens.data_ptr(), dout.data_ptr(), ld, scale, bufs.grad.data_ptr(),
+    _check(load().wm_embed_grad(dt, n, V, H, pk, dout.data_ptr(), ld, scale, bufs.grad.data_ptr(),
                                 bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
     return bufs
 
@@ -607,12 +623,12 @@ def layer_norm(x, gamma=None, beta=None, eps: float = 1e-5, bufs: LayerNormBuffe
     dt = _act("x", x)
     dev, H = x.device, x.shape[-1]
     rows, ld = _rows("x", x, H, x.dtype, dev)
-    _need("gamma", gamma, torch.float32, (H,), dev, optional=True)
-    _need("beta", beta, torch.float32, (H,), dev, optional=True)
+    pg = _arr("gamma", gamma, torch.float32, (H,), dev, optional=True)
+    pb = _arr("beta", beta, torch.float32, (H,), dev, optional=True)
     if bufs is None:
         bufs = LayerNormBuffers(rows, H, x.dtype, dev)
     _norm_bufs(x, bufs, rows, H)
-    _check(load().wm_layer_norm(dt, rows, H, x.data_ptr(), ld, _ptr(gamma), _ptr(beta), eps, bufs.y.data_ptr(), H,
+    _check(load().wm_layer_norm(dt, rows, H, x.data_ptr(), ld, pg, pb, eps, bufs.y.data_ptr(), H,
                                 _ptr(bufs.mean), _ptr(bufs.rstd), _stream()))
     return bufs
 
@@ -624,13 +640,13 @@ def layer_norm_grad(x, dy, gamma=None, bufs: LayerNormBuffers | None = None) -> 
     dev, H = x.device, x.shape[-1]
     rows, ld = _rows("x", x, H, x.dtype, dev)
     nd, dld = _rows("dy", dy, H, x.dtype, dev)
-    _need("gamma", gamma, torch.float32, (H,), dev, optional=True)
+    pg = _arr("gamma", gamma, torch.float32, (H,), dev, optional=True)
     if bufs is None or bufs.dx is None:
         raise ValueError("layer_norm_grad needs the forward call's buffers, made with grad=True")
     _norm_bufs(x, bufs, rows, H)
     if nd != rows:
         raise ValueError(f"dy has {nd} rows, x has {rows}")
-    _check(load().wm_layer_norm_grad(dt, rows, H, x.data_ptr(), ld, dy.data_ptr(), dld, _ptr(gamma),
+    _check(load().wm_layer_norm_grad(dt, rows, H, x.data_ptr(), ld, dy.data_ptr(), dld, pg,
                                      bufs.mean.data_ptr(), bufs.rstd.data_ptr(), bufs.dx.data_ptr(), H,
                                      bufs.dgamma.data_ptr(), bufs.dbeta.data_ptr(), bufs.workspace.data_ptr(),
                                      bufs.ws_bytes, _stream()))
@@ -659,11 +675,11 @@ class LinrecBuffers:
 
 def _seq(name, t, shape, dtype, device):
     """Checks a [T, B, H] tensor with unit stride along H; its strides."""
-    _act(name, t, dtype)
-    if tuple(t.shape) != shape or t.device != device:
-        raise ValueError(f"{name} is {tuple(t.shape)} on {t.device}, expected {shape} on {device}")
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.device != device:
+        _act(name, t, dtype)
+        raise ValueError(f"{name} is {tuple(t.shape)} on {t.device}, expected {tuple(shape)} on {device}")
     st = t.stride()
-    if shape[2] > 1 and st[2] != 1:
+    if st[2] != 1 and shape[2] > 1:
         raise ValueError(f"{name} must have unit stride along its last dimension")
     return st
 
@@ -672,14 +688,14 @@ def _linrec_args(x, gate, resets, lengths, bufs):
     dt = _act("x", x)
     if x.dim() != 3:
         raise ValueError(f"x has shape {tuple(x.shape)}, expected [T, B, H]")
-    dev, shape = x.device, tuple(x.shape)
+    dev, shape = x.device, x.shape
     sx, sg = _seq("x", x, shape, x.dtype, dev), _seq("gate", gate, shape, x.dtype, dev)
-    _need("resets", resets, _mask_dtype(resets), shape[:2], dev, optional=True)
-    _need("lengths", lengths, torch.int32, shape[1:2], dev, optional=True)
-    if bufs is not None and ((bufs.T, bufs.B, bufs.H) != shape or bufs.dtype != x.dtype or bufs.y.device != dev):
+    pr = _arr("resets", resets, _mask_dtype(resets), shape[:2], dev, optional=True)
+    pl = _arr("lengths", lengths, torch.int32, shape[1:2], dev, optional=True)
+    if bufs is not None and ((bufs.T, bufs.B, bufs.H) != shape or bufs.dtype is not x.dtype or bufs.y.device != dev):
         raise ValueError(f"buffers for T={bufs.T} B={bufs.B} H={bufs.H} {bufs.dtype} on {bufs.y.device}; the call has "
-                         f"{shape} {x.dtype} on {dev}")
-    return dt, dev, shape, sx, sg
+                         f"{tuple(shape)} {x.dtype} on {dev}")
+    return dt, dev, shape, sx, sg, pr, pl
 
 
 def linrec(x, gate, h0=None, resets=None, lengths=None, bufs: LinrecBuffers | None = None) -> LinrecBuffers:
@@ -687,28 +703,28 @@ def linrec(x, gate, h0=None, resets=None, lengths=None, bufs: LinrecBuffers | No
     x_t with a = sigmoid(gate) over ``x``, ``gate`` [T, B, H] (resets [T, B]
     uint8: the step starts a new trajectory; lengths [B] int32); returns the
     filled buffers (y, h_T, and the states that linrec_grad reads)."""
-    dt, dev, (T, B, H), sx, sg = _linrec_args(x, gate, resets, lengths, bufs)
-    _need("h0", h0, torch.float32, (B, H), dev, optional=True)
+    dt, dev, (T, B, H), sx, sg, pr, pl = _linrec_args(x, gate, resets, lengths, bufs)
+    ph = _arr("h0", h0, torch.float32, (B, H), dev, optional=True)
     if bufs is None:
         bufs = LinrecBuffers(T, B, H, x.dtype, dev)
-    _check(load().wm_linrec(dt, T, B, H, x.data_ptr(), sx[0], sx[1], gate.data_ptr(), sg[0], sg[1], _ptr(h0),
-                            _ptr(resets), _ptr(lengths), bufs.y.data_ptr(), bufs.h_T.data_ptr(), _ptr(bufs.states),
-                            bufs.states_bytes, bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
+    _check(load().wm_linrec(dt, T, B, H, x.data_ptr(), sx[0], sx[1], gate.data_ptr(), sg[0], sg[1], ph, pr, pl,
+                            bufs.y.data_ptr(), bufs.h_T.data_ptr(), _ptr(bufs.states), bufs.states_bytes,
+                            bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
     return bufs
 
 
 def linrec_grad(x, gate, dy, dh_T=None, resets=None, lengths=None, bufs: LinrecBuffers | None = None) -> LinrecBuffers:
     """Launch wm_linrec_grad on the current stream: dx, dgate and dh0 from
     the forward call's inputs and the states in its ``bufs``."""
-    dt, dev, (T, B, H), sx, sg = _linrec_args(x, gate, resets, lengths, bufs)
+    dt, dev, (T, B, H), sx, sg, pr, pl = _linrec_args(x, gate, resets, lengths, bufs)
     if bufs is None or bufs.states is None:
         raise ValueError("linrec_grad needs the forward call's buffers, made with grad=True")
-    sd = _seq("dy", dy, (T, B, H), x.dtype, dev)
-    _need("dh_T", dh_T, torch.float32, (B, H), dev, optional=True)
-    o = bufs.dx.stride()
-    _check(load().wm_linrec_grad(dt, T, B, H, x.data_ptr(), sx[0], sx[1], gate.data_ptr(), sg[0], sg[1], _ptr(resets),
-                                 _ptr(lengths), dy.data_ptr(), sd[0], sd[1], _ptr(dh_T), bufs.states.data_ptr(),
-                                 bufs.states_bytes, bufs.dx.data_ptr(), o[0], o[1], bufs.dgate.data_ptr(), o[0], o[1],
+    sd = _seq("dy", dy, x.shape, x.dtype, dev)
+    ph = _arr("dh_T", dh_T, torch.float32, (B, H), dev, optional=True)
+    ox, og = bufs.dx.stride(), bufs.dgate.stride()
+    _check(load().wm_linrec_grad(dt, T, B, H, x.data_ptr(), sx[0], sx[1], gate.data_ptr(), sg[0], sg[1], pr, pl,
+                                 dy.data_ptr(), sd[0], sd[1], ph, bufs.states.data_ptr(), bufs.states_bytes,
+                                 bufs.dx.data_ptr(), ox[0], ox[1], bufs.dgate.data_ptr(), og[0], og[1],
                                  bufs.dh0.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
     return bufs
 
