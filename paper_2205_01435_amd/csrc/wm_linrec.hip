@@ -19,11 +19,13 @@
 //     state that enters each tile.
 // Either way inputs are read once and outputs written once, whatever T is.
 // A segment waits only for maps, and a map is published before its segment
-// waits for anything; segments take their numbers from a counter in the order
-// in which they start, so every map that is waited for belongs to a work-group
-// that already runs: no wait depends on what else occupies the device.  (The
-// waits are bounded all the same; one that reached its bound would set the
-// workspace's error word.)
+// waits for anything; the segments of 64 channels take their numbers from these
+// channels' counter in the order in which they start, so every map that is
+// waited for belongs to a work-group that already runs: no wait depends on what
+// else occupies the device.  (The waits are bounded all the same; one that
+// reached its bound would set the workspace's error word.)  The device adds to
+// one address about every 4 ns: one counter for all channels held the 4096
+// work-groups of 32768 steps by 1024 channels back by 18 us.
 //
 // The gradient recomputes h_{t-1} from the inputs and the fp32 state that
 // entered each tile of kTT steps, which the forward call saves (4 / kTT bytes
@@ -52,6 +54,7 @@ constexpr int kMaxSegs = 1024; // segments of a launch; longer sequences take se
 // us, 1536 318 and 300; bf16 1024 groups 155 and 192 us, 1536 214 and 224, 4096
 // (128 steps) 141 and 105.
 constexpr long kWalk32 = 1280, kWalk16 = 2048;
+constexpr int kNextPitch = 32;  // words from one counter to the next: lines of their own
 constexpr unsigned kSpinLimit = 1u << 22;
 constexpr unsigned long long kEmpty = ~0ull;  // a map not yet published (A's bits would be a NaN of this sign)
 
@@ -404,11 +407,12 @@ __device__ __forceinline__ void load_tile(typename Chan<DT>::raw (&r)[kTT], cons
   }
 }
 
-// The segment maps of a launch, in the workspace: the counter and the status
-// words, then [segments][channels] maps, then those of kFan segments each, then
-// a copy of the state that enters the launch and the state between launches.
+// The segment maps of a launch, in the workspace: the status words, then the
+// counters, then [segments][channels] maps, then those of kFan segments each,
+// then a copy of the state that enters the launch and the state between launches.
 struct Chain {
-  unsigned* head;  // [0] next segment; [kSyncErr] the error word
+  unsigned* head;  // [kSyncErr] the error word
+  unsigned* next;  // [groups][kNextPitch] the segment that starts next
   unsigned long long *seg, *fan;
   const float* enter; // [channels] state that enters the launch, or null (0)
   float* leave;       // [channels] state that leaves it, or null
@@ -495,15 +499,13 @@ __device__ __forceinline__ Map before(Shared& sh, const Chain& ch, int order, lo
 
 // The work-group's place: which channels, which segment in the chain's order.
 __device__ __forceinline__ void place(unsigned* order, const Chain& ch, long& group, int& seg) {
+  seg = 0;
+  group = blockIdx.x;
   if (ch.segs > 1) {
-    if (threadIdx.x == 0) *order = atomicAdd(ch.head, 1u);
+    group = blockIdx.x % (uint32_t)ch.groups;
+    if (threadIdx.x == 0) *order = atomicAdd(ch.next + group * kNextPitch, 1u);
     __syncthreads();
-    const uint32_t k = (uint32_t)uniform((int)*order), n = (uint32_t)ch.groups;
-    seg = (int)(k / n);
-    group = k - (uint32_t)seg * n;
-  } else {
-    seg = 0;
-    group = blockIdx.x;
+    seg = uniform((int)*order);
   }
 }
 
@@ -679,12 +681,12 @@ __global__ void __launch_bounds__(64 * kWaves) k_linrec_grad_split(const LinrecG
   if (ch.leave && k.on && k.t0 == ch.t0) ch.leave[k.c] = R;
 }
 
-// Empties the maps of a launch, and copies the state that enters it (which the
+// Empties the maps of a launch, sets its counters to 0, and copies the state that enters it (which the
 // last segment's result may overwrite); the first one clears the status words.
 __global__ void __launch_bounds__(256) k_linrec_init(const Chain ch, long words, const float* from, long C, bool first) {
   const long i = (long)blockIdx.x * 256 + threadIdx.x, step = (long)gridDim.x * 256;
-  if (i == 0) ch.head[0] = 0;
   if (first && i < 2) ch.head[kSyncErr + i] = 0;
+  for (long j = i; j < ch.groups; j += step) ch.next[j * kNextPitch] = 0;
   for (long j = i; j < words; j += step) ch.seg[j] = kEmpty;
   if (from)
     for (long j = i; j < C; j += step) const_cast<float*>(ch.enter)[j] = from[j];
@@ -705,10 +707,10 @@ Plan plan(int dtype, int T, int B, int H) {
 // The workspace of a call with several segments.
 constexpr size_t kHeadBytes = kSyncWords * sizeof(unsigned);
 long pad_channels(int B, int H) { return ((long)B * H + 63) / 64 * 64; }  // whole groups
+constexpr size_t kNextBytes = kNextPitch * sizeof(unsigned);  // a group's
 long map_words(long segs, long channels) { return (segs + segs / kFan) * channels; }
 
-// Runs go(Chain, first launch, last launch) for every launch of a call, in
-// order; `from` is the state that enters the call, `to` the one that leaves it.
+// Runs go(Chain) for every launch of a call, in order; `from` is the state that enters the call, `to` the one that leaves it.
 template <typename F>
 hipError_t run_chain(int T, int B, int H, const Plan& p, void* ws, const float* from, float* to, bool reverse,
                      hipStream_t s, F go) {
@@ -725,7 +727,8 @@ hipError_t run_chain(int T, int B, int H, const Plan& p, void* ws, const float* 
   const long most = std::min<long>(p.segs, kMaxSegs);
   char* base = reinterpret_cast<char*>(ws);
   ch.head = reinterpret_cast<unsigned*>(base);
-  ch.seg = reinterpret_cast<unsigned long long*>(base + kHeadBytes);
+  ch.next = reinterpret_cast<unsigned*>(base + kHeadBytes);
+  ch.seg = reinterpret_cast<unsigned long long*>(base + kHeadBytes + ch.groups * kNextBytes);
   float* enter = reinterpret_cast<float*>(ch.seg + map_words(most, pad));
   float* carry = enter + pad;
   const long launches = (p.segs + kMaxSegs - 1) / kMaxSegs;
@@ -769,7 +772,8 @@ size_t linrec_workspace(int T, int B, int H) {
   const Plan p = plan(WM_BF16, T, B, H);  // (split wherever fp32 is, and beyond)
   if (p.segs <= 1) return 0;
   const long pad = pad_channels(B, H);
-  return kHeadBytes + (size_t)map_words(std::min<long>(p.segs, kMaxSegs), pad) * 8 + (size_t)pad * 2 * sizeof(float);
+  return kHeadBytes + (size_t)pad / 64 * kNextBytes + (size_t)map_words(std::min<long>(p.segs, kMaxSegs), pad) * 8 +
+         (size_t)pad * 2 * sizeof(float);
 }
 
 hipError_t launch_linrec(int dtype, const LinrecArgs& a, hipStream_t s) {
