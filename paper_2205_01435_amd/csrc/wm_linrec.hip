@@ -47,13 +47,15 @@ namespace {
 constexpr int kWaves = 8;      // tiles of a segment at most
 constexpr int kTT = 16;        // steps of a tile
 constexpr int kSeg = kWaves * kTT;
-constexpr int kFan = 16;       // segments whose maps are composed into one for the segments after them
+// Segments whose maps are composed into one for the segments after them.
+// Measured, 32768 steps of 1024 channels in bf16, both directions: 4 157 us, 8
+// 154, 16 162.
+constexpr int kFan = 8;
 constexpr int kMaxSegs = 1024; // segments of a launch; longer sequences take several
 // Channel groups (of 64) from which a wave walks all steps.  Measured, forward
-// and gradient of 500 steps, split against walked: fp32 1024 groups 218 and 219
-// us, 1536 318 and 300; bf16 1024 groups 155 and 192 us, 1536 214 and 224, 4096
-// (128 steps) 141 and 105.
-constexpr long kWalk32 = 1280, kWalk16 = 2048;
+// and gradient of 500 steps, split against walked: fp32 1280 groups 258 and 268
+// us, 1536 319 and 297; bf16 1536 groups 212 and 232 us, 2048 270 and 258.
+constexpr long kWalk32 = 1536, kWalk16 = 2048;
 constexpr int kNextPitch = 32;  // words from one counter to the next: lines of their own
 constexpr unsigned kSpinLimit = 1u << 22;
 constexpr unsigned long long kEmpty = ~0ull;  // a map not yet published (A's bits would be a NaN of this sign)
@@ -441,15 +443,33 @@ __device__ __forceinline__ Map await(const unsigned long long* p, unsigned long 
   return {__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
 }
 
-// Composes n maps, `stride` words apart, in order; four loads in flight.
-__device__ __forceinline__ Map compose(Map m, const unsigned long long* p, int n, long stride, unsigned* head) {
-  for (int i = 0; i < n; i += 4) {
-    unsigned long long v[4];
+// Composes the maps of segments [s, s1), in order; four loads in flight.  A
+// whole fan (s is one's first) comes from the fan's map if that is there; if
+// not, from its segments' maps, which are published earlier.
+__device__ __forceinline__ Map compose(const unsigned long long* seg, const unsigned long long* fan, int s, int s1,
+                                       long stride, unsigned* head) {
+  Map m{1.0f, 0.0f};
+#pragma unroll 1
+  while (s < s1) {
+    const int e = min(s + kFan, s1);
+    if (e - s == kFan) {
+      const unsigned long long f = peek(fan + s / kFan * stride);
+      if (__all(f != kEmpty)) {
+        m = then(m, await(fan, f, head));
+        s = e;
+        continue;
+      }
+    }
+#pragma unroll 1
+    for (; s < e; s += 4) {
+      unsigned long long v[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = i + k < n ? peek(p + (i + k) * stride) : 0;
+      for (int k = 0; k < 4; ++k) v[k] = s + k < e ? peek(seg + (s + k) * stride) : 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (i + k < n) m = then(m, await(p + (i + k) * stride, v[k], head));
+      for (int k = 0; k < 4; ++k)
+        if (s + k < e) m = then(m, await(seg + (s + k) * stride, v[k], head));
+    }
+    s = e;
   }
   return m;
 }
@@ -471,23 +491,23 @@ __device__ __forceinline__ Map before(Shared& sh, const Chain& ch, int order, lo
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
   const long stride = ch.groups * 64, at = group * 64 + lane;
   const Map none{1.0f, 0.0f};
-  if (w == kWaves - 1) {  // the segment's map
-    Map s = none;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) s = then(s, sh.tile[forward ? i : kWaves - 1 - i][lane]);
-    publish(ch.seg + order * stride + at, s);
-    if (order % kFan == kFan - 1)  // ... and that of its fan
-      publish(ch.fan + order / kFan * stride + at,
-              then(compose(none, ch.seg + (order - (kFan - 1)) * stride + at, kFan - 1, stride, ch.head), s));
-  }
   // whole fans before it, then the segments of its own fan: dealt to the waves in runs
   const int fans = order / kFan, n = fans + order % kFan;
   const int i0 = n * w / kWaves, i1 = n * (w + 1) / kWaves;
-  Map p = none;
-  if (i0 < fans) p = compose(p, ch.fan + i0 * stride + at, min(i1, fans) - i0, stride, ch.head);
-  if (i1 > fans) {
-    const int j = max(i0, fans);
-    p = compose(p, ch.seg + ((long)fans * kFan + j - fans) * stride + at, i1 - j, stride, ch.head);
+  auto first = [&](int i) { return i < fans ? i * kFan : fans * (kFan - 1) + i; };
+  Map own = none, p;
+  bool fan = false;
+  if (w == kWaves - 1) {  // the segment's map
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) own = then(own, sh.tile[forward ? i : kWaves - 1 - i][lane]);
+    publish(ch.seg + order * stride + at, own);
+    fan = order % kFan == kFan - 1;  // ... and that of its fan
+  }
+#pragma unroll 1
+  for (;; fan = false) {
+    p = compose(ch.seg + at, ch.fan + at, fan ? order - (kFan - 1) : first(i0), fan ? order : first(i1), stride, ch.head);
+    if (!fan) break;
+    publish(ch.fan + order / kFan * stride + at, then(p, own));
   }
   sh.part[w][lane] = p;
   __syncthreads();
