@@ -3,7 +3,9 @@
 // its transpose).
 //   y_i = s E[a_i], 0 where a_i is outside [0, V);  dE_v = s sum_{a_i = v} dy_i.
 //
-// The gradient sorts the positions by token (stably, by 8-bit digits, least
+// The gradient of a small table (k_embed_scan) looks for each row's positions in
+// the whole list, a part of it in every work-group, and adds the parts in order.
+// Otherwise it sorts the positions by token (stably, by 8-bit digits, least
 // first; codes outside the table sort behind it), so that a row's positions lie
 // together, and cuts the sorted list into equal chunks whatever the tokens are:
 // a row that every token names costs as much as one row each.  A wave sums the
@@ -460,14 +462,99 @@ __global__ void __launch_bounds__(1024) k_embed_join(const RowsArgs a, int joins
   }
 }
 
+// ---------------------------------------------------------------------------
+// Small tables: no sorting
+// ---------------------------------------------------------------------------
+
+constexpr int kScan = 512;  // positions that a work-group looks through
+
+struct ScanArgs {
+  EmbedGradArgs g;
+  float* part;  // [parts][V][H]; not used by a single one
+};
+
+// A row of the table, 64 pieces of its columns, kScan positions: every wave
+// looks through 64 of them and adds up the rows of dy that belong to it; the
+// waves' sums meet in LDS.  A row's parts are neighbouring work-groups: on
+// different XCDs, where one token has all positions.
+template <typename DT>
+__global__ void __launch_bounds__(kScan) k_embed_scan(const ScanArgs a, int parts) {
+  constexpr int V = Piece<DT>::V, kAhead = 8;
+  __shared__ float sums[kScan / 64][64 * V];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), H = a.g.H;
+  const int v = blockIdx.x / (unsigned)parts, part = blockIdx.x - v * parts, at = part * kScan + w * 64, n = (int)a.g.n;
+  const int col = column<DT>(blockIdx.y * 64 + lane, H);
+  const DT* dy = reinterpret_cast<const DT*>(a.g.dout);
+  float sum[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+  unsigned long long m = __ballot(at + lane < n && a.g.tokens[min(at + lane, n - 1)] == v);
+  while (m) {
+    u32x4 r[kAhead];
+    const int count = __popcll(m);
+    int q = 0;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      q = m ? __builtin_ctzll(m) : q;  // (past the last one: that one again)
+      m &= m - 1;
+      r[k] = load_piece(dy + (long)(at + q) * a.g.dout_ld, col, H);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (k >= count) break;
+      float x[V];
+      Piece<DT>::get(r[k], x);
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[j] += x[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) sums[w][lane * V + j] = sum[j];
+  __syncthreads();
+  const int piece = blockIdx.y * 64 + threadIdx.x / V, c = column<DT>(piece, H) + threadIdx.x % V;
+  if (threadIdx.x >= 64 * V || piece * V >= H || c >= H) return;
+  float total = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kScan / 64; ++i) total += sums[i][threadIdx.x];
+  const long to = (long)v * H + c;
+  if (parts == 1)
+    a.g.dtable[to] = a.g.scale * total;
+  else
+    a.part[(long)part * a.g.V * H + to] = total;
+}
+
+// Adds the parts in order.
+__global__ void __launch_bounds__(256) k_embed_parts(const ScanArgs a, int parts) {
+  const long i = (long)blockIdx.x * 256 + threadIdx.x, size = (long)a.g.V * a.g.H;
+  if (i >= size) return;
+  float total = 0.0f;
+#pragma unroll 8
+  for (int p = 0; p < parts; ++p) total += a.part[p * size + i];
+  a.g.dtable[i] = a.g.scale * total;
+}
+
+// The most work-groups (in columns of 256) of a gradient without sorting.
+// Measured against sorting, with tokens that name all rows alike and one row
+// only: 1024 rows of 64 from 500 positions (1024 work-groups) 3.8 and
+// 9.3 against 14.5 and 14.0 us, 50 of 367 from 7224 (1500) 11.1 and 14.4 against
+// 17.2 and 21.8, 128 of 64 from 16384 (4096) 13.8 and 14.0 against 17.4 and
+// 26.3, 128 of 367 from 16384 (8192) 24.0 and 21.1 against 18.8 and 29.4, 128 of
+// 64 from 40000 (10112) 28.5 and 19.7 against 19.4 and 45.2.
+constexpr long kScanGroups = 4096;
+constexpr long kScanParts = 64;  // ... and the most parts, which are added one after the other
+
 // How a call is cut.
 struct Plan {
+  int parts;                // without sorting; 0: with
   int passes, tile, tiles;  // of the sort (tiles 0: one work-group)
   int chunk, chunks;
   size_t hist, start, part, total;  // workspace, after the keys and positions twice: counts, rows' begins, partial sums
 };
 Plan plan(long n, int V, int H) {
   Plan p{};
+  const long columns = (H + 255) / 256;
+  const long parts = (n + kScan - 1) / kScan, most_parts = std::min(kScanParts, kScanGroups / ((long)V * columns));
+  if (n > 0 && parts <= most_parts) p.parts = (int)parts;
   p.passes = 1;
   while (p.passes < 4 && (uint64_t)V >> (8 * p.passes)) ++p.passes;  // the keys are 0 .. V
   if (n > kOne) {
@@ -485,7 +572,8 @@ Plan plan(long n, int V, int H) {
   p.hist = 4 * list;
   p.start = p.hist + (n > kOne ? (size_t)kMaxTiles * kDigits * 4 : 0);
   p.part = p.start + up(((size_t)V + 1) * 4);
-  p.total = p.part + up((size_t)most * 2 * H * sizeof(float));
+  p.total = std::max(p.part + up((size_t)most * 2 * H * sizeof(float)),
+                     (size_t)std::min(parts, most_parts) * V * H * sizeof(float));
   return p;
 }
 
@@ -509,6 +597,17 @@ size_t embed_grad_workspace(long n, int V, int H) { return plan(n, V, H).total; 
 hipError_t launch_embed_grad(int dtype, const EmbedGradArgs& a, hipStream_t s) {
   const Plan p = plan(a.n, a.V, a.H);
   char* ws = reinterpret_cast<char*>(a.ws);
+  const int piece = dtype == WM_FP32 ? 4 : 8;
+  const unsigned columns = (unsigned)(((a.H + piece - 1) / piece + 63) / 64);
+  if (p.parts > 0) {
+    const ScanArgs q{a, reinterpret_cast<float*>(ws)};
+    const dim3 grid((unsigned)a.V * p.parts, columns);
+    hipError_t e = dtype == WM_FP32 ? launch("embed_scan", k_embed_scan<float>, grid, dim3(kScan), 0, s, q, p.parts)
+                                    : launch("embed_scan", k_embed_scan<bf16_t>, grid, dim3(kScan), 0, s, q, p.parts);
+    if (e != hipSuccess || p.parts == 1) return e;
+    const long size = (long)a.V * a.H;
+    return launch("embed_parts", k_embed_parts, dim3((unsigned)((size + 255) / 256)), dim3(256), 0, s, q, p.parts);
+  }
   const size_t list = p.hist / 4;
   uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws), reinterpret_cast<uint32_t*>(ws + list)};
   uint32_t* pos[2] = {reinterpret_cast<uint32_t*>(ws + 2 * list), reinterpret_cast<uint32_t*>(ws + 3 * list)};
@@ -529,9 +628,8 @@ hipError_t launch_embed_grad(int dtype, const EmbedGradArgs& a, hipStream_t s) {
   const int groups = (p.chunks + 3) / 4, joins = (p.chunks + 15) / 16;
   const RowsArgs r{a, keys[at], pos[at], reinterpret_cast<float*>(ws + p.part), reinterpret_cast<int32_t*>(ws + p.start),
                    p.chunk, p.chunks, groups};
-  const int v = dtype == WM_FP32 ? 4 : 8;
   const unsigned look = (unsigned)std::min<long>((long)a.V / 256 + 1, 4096);
-  const dim3 grid(groups + look, ((a.H + v - 1) / v + 63) / 64);
+  const dim3 grid(groups + look, columns);
   e = dtype == WM_FP32 ? launch("embed_rows", k_embed_rows<float>, grid, dim3(256), 0, s, r)
                        : launch("embed_rows", k_embed_rows<bf16_t>, grid, dim3(256), 0, s, r);
   if (e != hipSuccess) return e;

@@ -77,6 +77,19 @@ def test_embed_grad(n, V, H, dtype, how):
     assert torch.equal(first, bufs.grad)  # the order of the sums is fixed
 
 
+@pytest.mark.parametrize("n,V,H,dtype,how", [
+    # one part, parts whose last is short or one position, the most parts; then one more, which sorts
+    (512, 40, 300, "bf16", "any"), (513, 40, 300, "fp32", "any"), (7224, 50, 367, "fp32", "one"),
+    (7224, 50, 700, "bf16", "any"), (32768, 3, 20, "fp32", "one"), (32768, 16, 1030, "bf16", "any"),
+    (32769, 3, 20, "fp32", "one"), (100, 4096, 64, "fp32", "any"), (100, 4097, 64, "fp32", "any"),
+    # short lists that are sorted: by one work-group, in one pass and in two
+    (4000, 200, 700, "bf16", "any"), (4000, 200, 700, "fp32", "one"), (3000, 900, 300, "fp32", "any"),
+    (3000, 900, 300, "bf16", "one"), (4096, 700, 520, "fp32", "rising"), (2500, 800, 600, "fp32", "none"),
+])
+def test_embed_grad_both_ways(n, V, H, dtype, how):
+    test_embed_grad(n, V, H, dtype, how)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_strided_rows_and_shapes(dtype):
     rng = np.random.default_rng(5)
