@@ -24,7 +24,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPer = 8;                       // 16-byte pieces of a thread
 constexpr int kChunkBytes = kThreads * kPer * 16;
-constexpr int kPerLaunch = 128;               // tensors whose table fits a launch's arguments
+constexpr int kPerLaunch = 176;               // tensors whose table fits a launch's arguments
 constexpr int kGroups = 2048;                 // work-groups of a launch: eight a CU, each over chunks in strides
 
 typedef uint32_t __attribute__((ext_vector_type(4))) u32x4;
@@ -45,8 +45,9 @@ struct Table {
   uint32_t first[kPerLaunch + 1]; // chunks before each tensor
   const void* in[kPerLaunch];
   void* out[kPerLaunch];
-  int64_t bytes[kPerLaunch];    // < 0: bf16
+  uint16_t last[kPerLaunch];    // bytes of its last chunk, less one; the top bit: bf16
 };
+static_assert(sizeof(Table) + 24 <= 4096, "a launch's arguments");
 
 // A chunk of a list: where, how many bytes.
 struct Chunk {
@@ -63,10 +64,9 @@ struct Chunk {
       else
         hi = mid;
     }
-    const int64_t all = t.bytes[lo], len = all < 0 ? -all : all;
     const int64_t from = (int64_t)(c - t.first[lo]) * kChunkBytes;
-    bf16 = all < 0;
-    bytes = (int)min((int64_t)kChunkBytes, len - from);
+    bf16 = t.last[lo] >> 15;
+    bytes = c + 1 < t.first[lo + 1] ? kChunkBytes : (t.last[lo] & 0x7fff) + 1;
     in = static_cast<const char*>(t.in[lo]) + from;
     out = static_cast<char*>(t.out[lo]) + from;
   }
@@ -207,7 +207,7 @@ hipError_t tables(int n, const wm_grad_tensor* t, uint32_t& part0, F f) {
       const int k = tab.n++;
       tab.in[k] = t[i].grad;
       tab.out[k] = t[i].out;
-      tab.bytes[k] = t[i].dtype == WM_FP32 ? bytes_of(t[i]) : -bytes_of(t[i]);
+      tab.last[k] = (uint16_t)((bytes_of(t[i]) - 1) % kChunkBytes | (t[i].dtype == WM_FP32 ? 0 : 0x8000));
       tab.first[k + 1] = tab.first[k] + (uint32_t)chunks_of(t[i]);
     }
     if (tab.n == 0) break;
