@@ -359,18 +359,18 @@ float wm_poly_lr(int32_t epoch, float lr0, float lr_end, int32_t epochs);
  *   - Arrays are aligned to their element (float32 to 4 bytes, bf16 to 2).
  *     A leading dimension (`_ld`) is the distance between rows in elements,
  *     at least the row's width; output rows must not overlap.
- *   - Every sum has a fixed order: a call's result does not depend on
- *     scheduling.
+ *   - Every sum has a fixed order, which depends on the call's sizes only: a
+ *     call's result does not depend on scheduling.
  *   - A workspace is 256-byte aligned; its size comes from the function named
  *     ..._workspace_bytes with the call's sizes, 0 on sizes that the call
- *     refuses.
+ *     refuses and where a call needs none (it may be NULL then).
  */
 
 /*
  * Rows of a table for n actions, scaled: out[i] = scale * table[tokens[i]],
  * and 0 where tokens[i] is outside [0, V).
  *   tokens [n] int32; table [V, H] and out [n, H] in dtype.
- * H at most 65536.  n = 0 is a no-op.
+ * H at most 65536, n at most 2^30.  n = 0 is a no-op.
  */
 wm_status wm_embed(int32_t dtype, int64_t n, int32_t V, int32_t H, const int32_t *tokens,
                    const void *table, float scale, void *out, int64_t out_ld, wm_stream_t stream);
@@ -431,7 +431,9 @@ wm_status wm_layer_norm_grad(int32_t dtype, int64_t rows, int32_t H, const void 
  *   states               nullable: a 256-byte aligned buffer of
  *                        wm_linrec_states_bytes that receives what
  *                        wm_linrec_grad needs.
- *   workspace            of wm_linrec_workspace_bytes, also for the gradient.
+ *   workspace            of wm_linrec_workspace_bytes, also for the gradient; 0
+ *                        bytes where the call splits no time axis over
+ *                        work-groups.
  * T B at most 2^31 - 1, B H at most 2^31 - 1, and the rows that hold 64
  * neighbouring channels within 2 GiB of each other.  B = 0 is a no-op; T = 0
  * gives h_T = h0.
@@ -538,12 +540,14 @@ wm_status wm_profile_phases_read(double *out, int32_t n);
 
 /*
  * Device-side status of the last call that used `workspace` (a workspace of
- * wm_rollout, wm_nll or wm_nll_grad), after waiting for `stream`.  The
- * persistent kernels wait for each other at barriers with a bounded spin; a
- * wait that times out (for example when other work on the device keeps some
- * of their work-groups from running) sets an error word in the workspace,
- * and every work-group then stops at its next wait, so the outputs of that
- * call are incomplete.  Returns WM_ERR_HIP if that word is set,
+ * wm_rollout, wm_nll or wm_nll_grad, or one of wm_linrec and wm_linrec_grad
+ * that is not empty), after waiting for `stream`.  The persistent kernels wait
+ * for each other at barriers with a bounded spin; a wait that times out (for
+ * example when other work on the device keeps some of their work-groups from
+ * running) sets an error word in the workspace, and every work-group then stops
+ * at its next wait, so the outputs of that call are incomplete.  The waits of
+ * the recurrence are bounded and reported the same way, though none depends on
+ * what else runs.  Returns WM_ERR_HIP if that word is set,
  * WM_ERR_INVALID_ARG if the call's WM_FLAG_CHECK pass counted violations,
  * WM_OK otherwise.  Host-side synchronisation; allocates nothing.
  */

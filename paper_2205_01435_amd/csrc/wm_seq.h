@@ -12,7 +12,10 @@ namespace wm {
 // An output of at least this size goes past the caches: it is half of the
 // last-level one, which it would empty of what is read again (the values of a
 // gradient list, the input of a norm for its gradient).  A smaller one is left
-// there for the next call.
+// there for the next call.  Measured, past the caches against through them: a
+// gradient list of 270 MB, summed and scaled, 138 and 164 us; a norm of 256 MB
+// and its gradient 231 and 246 us (forward alone 92 and 89); a recurrence of 128
+// MB and its gradient 157 and 181 us.
 constexpr int64_t kStreamBytes = (int64_t)128 << 20;
 
 struct EmbedArgs {

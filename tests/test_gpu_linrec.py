@@ -312,6 +312,22 @@ def test_gradient_against_differences():
     assert abs(slope - got) <= 60 * seq.U32 * size / eps + 20 * eps ** 2 * np.abs(d["dy"]).sum() / 6
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_status_of_the_workspace(dtype):
+    """Calls whose time axis is split over work-groups and not, in a workspace of any contents."""
+    for T, B, H in ((300, 2, 70), (200, 410, 256), (130, 520, 256)):
+        x, gate = torch.ones(T, B, H, device="cuda").to(TORCH[dtype]), torch.zeros(T, B, H, device="cuda").to(TORCH[dtype])
+        bufs = wm.LinrecBuffers(T, B, H, TORCH[dtype])
+        if not bufs.ws_bytes:  # enough channels for either type
+            continue
+        bufs.workspace.fill_(255)
+        wm.linrec(x, gate, bufs=bufs)
+        wm.status(bufs)
+        bufs.workspace.fill_(255)
+        wm.linrec_grad(x, gate, x, bufs=bufs)
+        wm.status(bufs)
+
+
 def test_under_a_graph():
     """Captured once, replayed with new inputs, eager work in between."""
     T, B, H = 700, 1, 64
