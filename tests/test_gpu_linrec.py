@@ -100,6 +100,10 @@ def test_linrec_and_gradient(T, B, H, dtype, masks, packed):
     assert all(torch.equal(p, q) for p, q in zip(got, (bufs.y, bufs.h_T, bufs.dxg, bufs.dh0)))
 
 
+def test_more_steps_than_one_launch_takes():
+    test_linrec_and_gradient(140001, 2, 1, "bf16", True, False)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_without_state_and_optional_arrays(dtype):
     d, t = _inputs(70, 3, 20, dtype, False, 1)
@@ -267,7 +271,7 @@ def test_steps_continue_a_sequence():
     within(host(h), f["h_T"], f["h_T_err"], "fp32", "h_T")
 
 
-@pytest.mark.parametrize("T", [5, 900])
+@pytest.mark.parametrize("T", [5, 900, 131500])
 def test_state_and_its_gradient_in_place(T):
     d, t = _inputs(T, 2, 40, "fp32", True, 9)
     bufs = wm.LinrecBuffers(T, 2, 40)
