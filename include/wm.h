@@ -359,6 +359,8 @@ float wm_poly_lr(int32_t epoch, float lr0, float lr_end, int32_t epochs);
  *   - Arrays are aligned to their element (float32 to 4 bytes, bf16 to 2).
  *     A leading dimension (`_ld`) is the distance between rows in elements,
  *     at least the row's width; output rows must not overlap.
+ *   - Outputs overlap neither inputs nor each other, except where a call says
+ *     that one may be the other.
  *   - Every sum has a fixed order, which depends on the call's sizes only: a
  *     call's result does not depend on scheduling.
  *   - A workspace is 256-byte aligned; its size comes from the function named

@@ -233,8 +233,8 @@ wm_status check_view(const char* name, int32_t dtype, const void* p, int64_t t, 
   if (t < 0 || b < 0) return fail(WM_ERR_INVALID_ARG, "%s: strides must not be negative", name);
   if ((T > 1 && t > lim / T) || (B > 1 && b > lim / B))
     return fail(WM_ERR_UNSUPPORTED, "%s: rows too far apart", name);
-  // a wave's 64 channels reach this many rows; it addresses them with 32-bit byte offsets
-  const int64_t reach = std::min<int64_t>(B - 1, 63 / H + 1), es = dtype == WM_FP32 ? 4 : 2;
+  // a wave's 64 channels reach this many rows beyond their first; it addresses them with 32-bit byte offsets
+  const int64_t reach = H % 64 == 0 ? 0 : std::min<int64_t>(B - 1, 63 / H + 1), es = dtype == WM_FP32 ? 4 : 2;
   if (H > INT32_MAX / es || (reach > 0 && b > (INT32_MAX / es - H) / reach))
     return fail(WM_ERR_UNSUPPORTED, "%s: the rows of 64 channels span over 2 GiB", name);
   if (output) {

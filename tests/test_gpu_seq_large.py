@@ -106,6 +106,27 @@ def test_linrec_walked():
     _windows(T, B, H, (0, at - 550, T - 600), slice(B - 3, B))
 
 
+@pytest.mark.parametrize("T", [20, 300])
+def test_linrec_rows_far_apart(T):
+    """Batch-major rows of a longer array, more than 2 GiB from one to the next."""
+    B, H, far = 3, 128, (1 << 30) + 640
+    say("linrec, rows far apart", T)
+    bufs = [torch.empty((B - 1) * far + T * H, dtype=BF, device="cuda") for _ in range(3)]
+    views = [b.as_strided((T, B, H), (H, far, 1)) for b in bufs]
+    for i, v in enumerate(views):
+        v.copy_(_normal((T, B, H), 8 + i))
+    near = [v.contiguous() for v in views]
+    a, b = wm.LinrecBuffers(T, B, H, BF), wm.LinrecBuffers(T, B, H, BF)
+    for q, (x, gate, dy) in ((a, near), (b, views)):
+        wm.linrec(x, gate, bufs=q)
+        wm.linrec_grad(x, gate, dy, bufs=q)
+    for k in ("y", "h_T", "dxg", "dh0"):
+        assert torch.equal(getattr(a, k), getattr(b, k)), k
+    with pytest.raises(wm.WmError) as e:  # 64 channels of several such rows
+        wm.linrec(views[0][..., :100], views[1][..., :100])
+    assert e.value.status == wm.WM_ERR_UNSUPPORTED
+
+
 def test_clip():
     n = 2200000003
     say("clip", n)
