@@ -11,12 +11,12 @@
 // that enters it, h -> U + A h, and maps compose.
 //   - A wave owns a tile of kTT steps of 64 channels, loads it whole, and folds
 //     it into the tile's map.
-//   - The waves of a work-group own the tiles of one segment of up to kWaves
-//     tiles; their maps meet in LDS.
-//   - Longer sequences take several segments, each a work-group of the same
-//     launch.  A work-group publishes its segment's map, then composes the
-//     maps of the segments before it, and only then runs its steps from the
-//     state that enters each tile.
+//   - The waves of a work-group own the tiles of one segment; their maps meet in
+//     LDS.
+//   - Sequences of more than kWide tiles take several segments of kWaves, each a
+//     work-group of the same launch.  A work-group publishes its segment's map,
+//     then composes the maps of the segments before it, and only then runs its
+//     steps from the state that enters each tile.
 // Either way inputs are read once and outputs written once, whatever T is.
 // A segment waits only for maps, and a map is published before its segment
 // waits for anything; the segments of 64 channels take their numbers from these
@@ -49,7 +49,12 @@
 namespace wm {
 namespace {
 
-constexpr int kWaves = 8;      // tiles of a segment at most
+// Tiles of a segment at most, where there are several, and of a single one: a
+// wide work-group leaves a CU fewer waves (16 of 24), but waits for no other and
+// needs no maps.  Measured, 200 steps, forward and gradient, two segments against
+// one: fp32 64 channels 22 and 14 us, 32768 59 and 51, 65536 103 and 97; bf16
+// 32768 47 and 35, 81920 90 and 82.
+constexpr int kWaves = 8, kWide = 16;
 constexpr int kTT = 16;        // steps of a tile
 constexpr int kSeg = kWaves * kTT;
 // Segments whose maps are composed into one for the segments after them.
@@ -488,9 +493,10 @@ __device__ __forceinline__ Map compose(const unsigned long long* seg, const unsi
 
 // What the work-group's waves share: the tiles' maps, the parts of the
 // composition over earlier segments, the state that enters the launch.
+template <int W>
 struct Shared {
-  Map tile[kWaves][64];
-  Map part[kWaves][64];
+  Map tile[W][64];
+  Map part[W == kWaves ? W : 1][64];  // (W = kWide: a single segment)
   float enter[64];
   unsigned order;
 };
@@ -499,7 +505,7 @@ struct Shared {
 // (identity for the first), composed by all waves of the work-group; publishes
 // the segment's own map first.  All kWaves waves of the work-group call it,
 // after the barrier that completes sh.tile.
-__device__ __forceinline__ Map before(Shared& sh, const Chain& ch, int order, long group, bool forward) {
+__device__ __forceinline__ Map before(Shared<kWaves>& sh, const Chain& ch, int order, long group, bool forward) {
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
   const long stride = ch.groups * 64, at = group * 64 + lane;
   const Map none{1.0f, 0.0f};
@@ -530,10 +536,11 @@ __device__ __forceinline__ Map before(Shared& sh, const Chain& ch, int order, lo
 }
 
 // The work-group's place: which channels, which segment in the chain's order.
+template <int W>
 __device__ __forceinline__ void place(unsigned* order, const Chain& ch, long& group, int& seg) {
   seg = 0;
   group = blockIdx.x;
-  if (ch.segs > 1) {
+  if (W == kWaves && ch.segs > 1) {
     group = blockIdx.x % (uint32_t)ch.groups;
     if (threadIdx.x == 0) *order = atomicAdd(ch.next + group * kNextPitch, 1u);
     __syncthreads();
@@ -577,14 +584,14 @@ __device__ __forceinline__ Map fold(float (&A)[kTT], float (&U)[kTT], const type
   return m;
 }
 
-template <typename DT, bool STREAM>
-__global__ void __launch_bounds__(64 * kWaves, 6) k_linrec_split(const LinrecArgs a, const Chain ch, int waves) {
-  __shared__ Shared sh;
+template <typename DT, bool STREAM, int W>
+__global__ void __launch_bounds__(64 * W, W == kWaves ? 6 : 4) k_linrec_split(const LinrecArgs a, const Chain ch, int waves) {
+  __shared__ Shared<W> sh;
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
   const long C = (long)a.B * a.H;
   int seg;
   long group;
-  place(&sh.order, ch, group, seg);
+  place<W>(&sh.order, ch, group, seg);
   Tile k(group, ((ch.seg0 + seg) * waves + w) * kTT, a.T, a.B, a.H, a.lengths);
   Resets<kTT> rb;
   rb.ask(a.resets, k, k.t0, a.T, a.B);
@@ -599,9 +606,10 @@ __global__ void __launch_bounds__(64 * kWaves, 6) k_linrec_split(const LinrecArg
   if (w == 0) sh.enter[lane] = h;  // read once, before anything of this row may be written
   __syncthreads();
   h = sh.enter[lane];
-  if (ch.segs > 1) h = apply(before(sh, ch, seg, group, true), h);
+  if constexpr (W == kWaves)
+    if (ch.segs > 1) h = apply(before(sh, ch, seg, group, true), h);
 #pragma unroll
-  for (int i = 0; i < kWaves - 1; ++i)
+  for (int i = 0; i < W - 1; ++i)
     if (i < w) h = apply(sh.tile[i][lane], h);
   if (a.states && k.on && k.nt > 0) a.states[(long)(k.t0 / kTT) * C + k.c] = h;
   Rows<DT, STREAM> y(SeqView{a.y, C, a.H}, k, k.t0);
@@ -681,13 +689,13 @@ __device__ __forceinline__ float emit_grad(const float (&A)[kTT], const float (&
   return R;
 }
 
-template <typename DT, bool STREAM>
-__global__ void __launch_bounds__(64 * kWaves) k_linrec_grad_split(const LinrecGradArgs a, const Chain ch, int waves) {
-  __shared__ Shared sh;
+template <typename DT, bool STREAM, int W>
+__global__ void __launch_bounds__(64 * W, 4) k_linrec_grad_split(const LinrecGradArgs a, const Chain ch, int waves) {
+  __shared__ Shared<W> sh;
   const int lane = threadIdx.x & 63, w = uniform(threadIdx.x >> 6);
   int order;
   long group;
-  place(&sh.order, ch, group, order);
+  place<W>(&sh.order, ch, group, order);
   const int seg = ch.seg0 + ch.segs - 1 - order;  // the chain runs from the last segment to the first
   Tile k(group, (seg * waves + w) * kTT, a.T, a.B, a.H, a.lengths);
   Resets<kTT> rb;
@@ -705,9 +713,10 @@ __global__ void __launch_bounds__(64 * kWaves) k_linrec_grad_split(const LinrecG
   if (w == waves - 1) sh.enter[lane] = R;  // read once, before anything of this row may be written
   __syncthreads();
   R = sh.enter[lane];
-  if (ch.segs > 1) R = apply(before(sh, ch, order, group, false), R);
+  if constexpr (W == kWaves)
+    if (ch.segs > 1) R = apply(before(sh, ch, order, group, false), R);
 #pragma unroll
-  for (int i = kWaves - 1; i > 0; --i)
+  for (int i = W - 1; i > 0; --i)
     if (i > w && i < waves) R = apply(sh.tile[i][lane], R);
   R = whole ? emit_grad<false, DT, STREAM>(A, M, G, R, dr, k, a) : emit_grad<true, DT, STREAM>(A, M, G, R, dr, k, a);
   if (ch.leave && k.on && k.t0 == ch.t0) ch.leave[k.c] = R;
@@ -732,7 +741,7 @@ struct Plan {
 Plan plan(int dtype, int T, int B, int H) {
   const long groups = ((long)B * H + 63) / 64, tiles = ((long)T + kTT - 1) / kTT;
   if (tiles <= 1 || groups >= (dtype == WM_FP32 ? kWalk32 : kWalk16)) return {0, 0};
-  if (tiles <= kWaves) return {(int)tiles, 1};
+  if (tiles <= kWide) return {(int)tiles, 1};
   return {kWaves, (tiles + kWaves - 1) / kWaves};
 }
 
@@ -784,7 +793,7 @@ hipError_t run_chain(int T, int B, int H, const Plan& p, void* ws, const float* 
 }
 
 template <typename W, typename S, typename A>
-hipError_t run(const char* name, int dtype, W walk, W step, S split, A a, const float* from, float* to,
+hipError_t run(const char* name, int dtype, W walk, W step, S split, S wide, A a, const float* from, float* to,
                bool reverse, hipStream_t s) {
   const Plan p = plan(dtype, a.T, a.B, a.H);
   if (linrec_workspace(a.T, a.B, a.H) == 0) a.ws = nullptr;
@@ -793,7 +802,7 @@ hipError_t run(const char* name, int dtype, W walk, W step, S split, A a, const 
     return launch(name, a.T <= 1 ? step : walk, dim3((unsigned)((groups + 3) / 4)), dim3(256), 0, s, a);
   }
   return run_chain(a.T, a.B, a.H, p, a.ws, from, to, reverse, s, [&](const Chain& ch) {
-    return launch(name, split, dim3((unsigned)(ch.groups * ch.segs)), dim3(64u * p.waves), 0, s, a, ch, p.waves);
+    return launch(name, p.waves > kWaves ? wide : split, dim3((unsigned)(ch.groups * ch.segs)), dim3(64u * p.waves), 0, s, a, ch, p.waves);
   });
 }
 
@@ -813,8 +822,10 @@ hipError_t launch_linrec(int dtype, const LinrecArgs& a, hipStream_t s) {
   auto go = [&](auto dt) {
     typedef decltype(dt) DT;
     const bool stream = (long)a.T * a.B * a.H * (long)sizeof(DT) >= kStreamBytes;
-    return run("linrec", dtype, stream ? k_linrec_walk<DT, kTT, true> : k_linrec_walk<DT, kTT, false>, k_linrec_walk<DT, 1, false>,
-               stream ? k_linrec_split<DT, true> : k_linrec_split<DT, false>, a, a.h0, a.h_T, false, s);
+    return run("linrec", dtype, stream ? k_linrec_walk<DT, kTT, true> : k_linrec_walk<DT, kTT, false>,
+               k_linrec_walk<DT, 1, false>,
+               stream ? k_linrec_split<DT, true, kWaves> : k_linrec_split<DT, false, kWaves>,
+               stream ? k_linrec_split<DT, true, kWide> : k_linrec_split<DT, false, kWide>, a, a.h0, a.h_T, false, s);
   };
   return dtype == WM_FP32 ? go(0.0f) : go(bf16_t());
 }
@@ -824,8 +835,10 @@ hipError_t launch_linrec_grad(int dtype, const LinrecGradArgs& a, hipStream_t s)
     typedef decltype(dt) DT;
     const bool stream = 2L * a.T * a.B * a.H * (long)sizeof(DT) >= kStreamBytes;
     return run("linrec_grad", dtype, stream ? k_linrec_grad_walk<DT, kTT, true> : k_linrec_grad_walk<DT, kTT, false>,
-               k_linrec_grad_walk<DT, 1, false>, stream ? k_linrec_grad_split<DT, true> : k_linrec_grad_split<DT, false>, a,
-               a.dh_T, a.dh0, true, s);
+               k_linrec_grad_walk<DT, 1, false>,
+               stream ? k_linrec_grad_split<DT, true, kWaves> : k_linrec_grad_split<DT, false, kWaves>,
+               stream ? k_linrec_grad_split<DT, true, kWide> : k_linrec_grad_split<DT, false, kWide>, a, a.dh_T, a.dh0, true,
+               s);
   };
   return dtype == WM_FP32 ? go(0.0f) : go(bf16_t());
 }

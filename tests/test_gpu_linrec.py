@@ -104,6 +104,14 @@ def test_more_steps_than_one_launch_takes():
     test_linrec_and_gradient(140001, 2, 1, "bf16", True, False)
 
 
+@pytest.mark.parametrize("T,B,H,dtype,masks,packed", [  # around the longest single segment
+    (129, 70, 3, "bf16", True, False), (144, 3, 66, "fp32", True, True), (145, 2, 64, "bf16", False, True),
+    (200, 5, 100, "fp32", True, False), (241, 1, 130, "bf16", True, True), (256, 3, 130, "bf16", True, False),
+    (256, 2, 64, "fp32", False, True), (257, 2, 64, "bf16", False, False), (272, 3, 70, "fp32", True, True)])
+def test_one_segment_or_several(T, B, H, dtype, masks, packed):
+    test_linrec_and_gradient(T, B, H, dtype, masks, packed)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_without_state_and_optional_arrays(dtype):
     d, t = _inputs(70, 3, 20, dtype, False, 1)
@@ -271,7 +279,7 @@ def test_steps_continue_a_sequence():
     within(host(h), f["h_T"], f["h_T_err"], "fp32", "h_T")
 
 
-@pytest.mark.parametrize("T", [5, 900, 131500])
+@pytest.mark.parametrize("T", [5, 200, 900, 131500])
 def test_state_and_its_gradient_in_place(T):
     d, t = _inputs(T, 2, 40, "fp32", True, 9)
     bufs = wm.LinrecBuffers(T, 2, 40)
@@ -319,7 +327,7 @@ def test_gradient_against_differences():
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_status_of_the_workspace(dtype):
     """Calls whose time axis is split over work-groups and not, in a workspace of any contents."""
-    for T, B, H in ((300, 2, 70), (200, 410, 256), (130, 520, 256)):
+    for T, B, H in ((300, 2, 70), (300, 410, 256), (300, 520, 256)):
         x, gate = torch.ones(T, B, H, device="cuda").to(TORCH[dtype]), torch.zeros(T, B, H, device="cuda").to(TORCH[dtype])
         bufs = wm.LinrecBuffers(T, B, H, TORCH[dtype])
         if not bufs.ws_bytes:  # enough channels for either type
