@@ -19,7 +19,7 @@
 //
 // Bound by memory.  Measured, 204800 rows of 1024 bf16 values: forward 153 to
 // 159 us (5.3 to 5.5 TB/s), gradient 218 us (5.8 TB/s) and 4 us for the sums;
-// 7224 rows of 367 fp32 values 7.6, 8.6 and 4.1 us, launches and first loads.
+// 7224 rows of 367 fp32 values 7, 8 and 4 us, launches and first loads.
 #include <algorithm>
 
 #include "../../include/wm.h"
@@ -357,8 +357,8 @@ __global__ void __launch_bounds__(256) k_norm_sum(const NormGradArgs a, int n) {
 }
 
 // Lanes of a row, by its width.  Measured, forward and gradient: rows of 64 fp32
-// values in 16 lanes 37 and 54 us, in 64 lanes 75 and 106; of 1024 in 64 lanes 92
-// and 138, in 256 102 and 143 (of 512 74 and 100, 97 and 170); of 4096 in
+// values in 16 lanes 37 and 54 us, in 64 lanes 74 and 106; of 1024 in 64 lanes 92
+// and 139, in 256 102 and 142 (of 512 74 and 101, 95 and 170); of 4096 in
 // 256 or 512 lanes the same; more than 16 values a lane, which 8192 in 256 lanes
 // would need, halve the waves.
 int lanes(int dtype, int H) {
@@ -371,9 +371,9 @@ int lanes(int dtype, int H) {
 // 4.7, 6.4 and 6.2.
 constexpr long kAlone = 2;
 // Work-groups of the gradient, each with a row of partial sums: as many as the
-// registers let run at once.  Half and twice as many took 228 and 240 us instead
-// of 218 at 1024 bf16 columns, 97 and 57 instead of 64 at 128 fp32 ones, 89 and 81
-// instead of 70 at 8192 bf16 ones.
+// registers let run at once.  Half and twice as many took 231 and 249 us instead
+// of 217 at 1024 bf16 columns, 97 and 56 instead of 64 at 128 fp32 ones, 83 and 71
+// instead of 65 at 8192 bf16 ones.
 int parts(long rows, int H) {
   const long per = std::max(1, 256 / lanes(WM_FP32, H));  // (bf16 rows just above 64 values lie two or four times as dense)
   const long most = H <= 256 ? 1024 : H <= 4096 ? 512 : 256;
