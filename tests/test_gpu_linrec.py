@@ -101,7 +101,7 @@ def test_linrec_and_gradient(T, B, H, dtype, masks, packed):
 
 
 def test_more_steps_than_one_launch_takes():
-    test_linrec_and_gradient(140001, 2, 1, "bf16", True, False)
+    test_linrec_and_gradient(140001, 3, 1, "bf16", True, False)
 
 
 @pytest.mark.parametrize("T,B,H,dtype,masks,packed", [  # around the longest single segment
@@ -338,6 +338,32 @@ def test_status_of_the_workspace(dtype):
         bufs.workspace.fill_(255)
         wm.linrec_grad(x, gate, x, bufs=bufs)
         wm.status(bufs)
+
+
+def test_two_streams_at_once():
+    """Calls whose work-groups wait for each other's maps share the device with each other and with
+    products that fill it: the same bits, and no wait at its bound."""
+    T, B, H = 5000, 1, 640
+    sets = [_inputs(T, B, H, "bf16", False, 30 + i)[1] for i in range(2)]
+    alone = [wm.LinrecBuffers(T, B, H, torch.bfloat16) for _ in sets]
+    for t, b in zip(sets, alone):
+        _run(t, b)
+    both = [wm.LinrecBuffers(T, B, H, torch.bfloat16) for _ in sets]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    m = torch.randn(4096, 4096, device="cuda").bfloat16()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(streams[2]):
+            for _ in range(3):
+                m @ m
+        for t, b, s in zip(sets, both, streams):
+            with torch.cuda.stream(s):
+                _run(t, b)
+    torch.cuda.synchronize()
+    for a, b in zip(alone, both):
+        wm.status(b)
+        for k in ("y", "h_T", "dxg", "dh0"):
+            assert torch.equal(getattr(a, k), getattr(b, k)), k
 
 
 def test_under_a_graph():
