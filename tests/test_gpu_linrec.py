@@ -100,6 +100,14 @@ def test_linrec_and_gradient(T, B, H, dtype, masks, packed):
     assert all(torch.equal(p, q) for p, q in zip(got, (bufs.y, bufs.h_T, bufs.dxg, bufs.dh0)))
 
 
+@pytest.mark.parametrize("T,B,H,dtype,packed", [  # (the masks take one row's steps and start another's anew at each)
+    (8, 4, 130, "fp32", False), (17, 4, 65, "fp32", True), (31, 5, 367, "bf16", False), (127, 6, 96, "fp32", True),
+    (513, 4, 31, "bf16", True), (1000, 4, 40, "fp32", True), (2049, 3, 70, "bf16", False), (4099, 5, 10, "fp32", False),
+    (20000, 3, 5, "bf16", True)])
+def test_masks_on_several_rows(T, B, H, dtype, packed):
+    test_linrec_and_gradient(T, B, H, dtype, True, packed)
+
+
 def test_more_steps_than_one_launch_takes():
     test_linrec_and_gradient(140001, 3, 1, "bf16", True, False)
 
