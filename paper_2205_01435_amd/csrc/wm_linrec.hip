@@ -626,7 +626,7 @@ __global__ void __launch_bounds__(64 * W, W == kWaves ? 6 : 4) k_linrec_split(co
       if (i < k.nt && k.on) y.put(i < k.live ? h : 0.0f);
     }
   }
-  if (ch.leave && k.on && k.t0 + kTT >= ch.t1 && k.t0 < ch.t1) ch.leave[k.c] = h;
+  if (ch.leave && k.on && k.t0 < ch.t1 && ch.t1 - k.t0 <= kTT) ch.leave[k.c] = h;
 }
 
 // The gradient's tile: a and 1 - a of its steps, what h_{t-1} puts into dgate,
@@ -733,14 +733,20 @@ __global__ void __launch_bounds__(256) k_linrec_init(const Chain ch, long words,
     for (long j = i; j < C; j += step) const_cast<float*>(ch.enter)[j] = from[j];
 }
 
-// How a call is split.  waves = 0: not at all.
+// How a call is split.  waves = 0: not at all.  A gradient of 2 to 16 steps is
+// one tile a work-group whatever the channels (the walk requests a whole tile's
+// values, the steps past the end too); the forward call walks these.  Measured,
+// walk against one tile, gradient of 4 steps: 64 fp32 channels 6.2 and 4.9 us,
+// 65536 7.9 and 5.6, 262144 bf16 ones 11.5 and 8.9; of 16 steps 5.8 and 4.1, 8.0
+// and 5.6, 12.8 and 10.5; forward of 4 steps 3.4 and 4.2, 4.0 and 4.8, 5.6 and 7.1.
 struct Plan {
   int waves;  // tiles of a segment
   long segs;
 };
-Plan plan(int dtype, int T, int B, int H) {
+Plan plan(int dtype, int T, int B, int H, bool grad) {
   const long groups = ((long)B * H + 63) / 64, tiles = ((long)T + kTT - 1) / kTT;
-  if (tiles <= 1 || groups >= (dtype == WM_FP32 ? kWalk32 : kWalk16)) return {0, 0};
+  if (T <= 1 || (tiles == 1 && !grad)) return {0, 0};
+  if (tiles > 1 && groups >= (dtype == WM_FP32 ? kWalk32 : kWalk16)) return {0, 0};
   if (tiles <= kWide) return {(int)tiles, 1};
   return {kWaves, (tiles + kWaves - 1) / kWaves};
 }
@@ -795,7 +801,7 @@ hipError_t run_chain(int T, int B, int H, const Plan& p, void* ws, const float* 
 template <typename W, typename S, typename A>
 hipError_t run(const char* name, int dtype, W walk, W step, S split, S wide, A a, const float* from, float* to,
                bool reverse, hipStream_t s) {
-  const Plan p = plan(dtype, a.T, a.B, a.H);
+  const Plan p = plan(dtype, a.T, a.B, a.H, reverse);
   if (linrec_workspace(a.T, a.B, a.H) == 0) a.ws = nullptr;
   if (p.waves == 0) {
     const long groups = ((long)a.B * a.H + 63) / 64;
@@ -811,7 +817,7 @@ hipError_t run(const char* name, int dtype, W walk, W step, S split, S wide, A a
 size_t linrec_states(int T, int B, int H) { return ((size_t)T + kTT - 1) / kTT * B * H * sizeof(float); }
 
 size_t linrec_workspace(int T, int B, int H) {
-  const Plan p = plan(WM_BF16, T, B, H);  // (split wherever fp32 is, and beyond)
+  const Plan p = plan(WM_BF16, T, B, H, false);  // (split wherever fp32 is, and beyond)
   if (p.segs <= 1) return 0;
   const long pad = pad_channels(B, H);
   return kHeadBytes + (size_t)pad / 64 * kNextBytes + (size_t)map_words(std::min<long>(p.segs, kMaxSegs), pad) * 8 +
