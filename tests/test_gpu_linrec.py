@@ -108,6 +108,13 @@ def test_masks_on_several_rows(T, B, H, dtype, packed):
     test_linrec_and_gradient(T, B, H, dtype, True, packed)
 
 
+@pytest.mark.parametrize("T,B,H,dtype,masks,packed", [  # one tile, few channels and many
+    (2, 1, 1, "fp32", False, False), (2, 1700, 64, "bf16", True, True), (3, 100, 1000, "fp32", True, False),
+    (15, 140, 1024, "bf16", False, True), (16, 2100, 65, "bf16", True, False), (16, 1600, 64, "fp32", False, False)])
+def test_a_single_tile(T, B, H, dtype, masks, packed):
+    test_linrec_and_gradient(T, B, H, dtype, masks, packed)
+
+
 def test_more_steps_than_one_launch_takes():
     test_linrec_and_gradient(140001, 3, 1, "bf16", True, False)
 
