@@ -71,6 +71,13 @@ def test_layer_norm_and_gradient(rows, H, dtype, affine):
         first = got
 
 
+@pytest.mark.parametrize("rows,H,dtype", [  # several wide rows a work-group, and around 64 rows of partial sums
+    (64, 2000, "fp32"), (65, 2000, "bf16"), (256, 4096, "fp32"), (259, 1025, "bf16"), (300, 8191, "bf16"),
+    (1100, 1500, "fp32"), (260, 1024, "fp32"), (261, 100, "bf16")])
+def test_column_sums(rows, H, dtype):
+    test_layer_norm_and_gradient(rows, H, dtype, True)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("H,at,wide", [(40, 3, 57), (512, 1, 515), (367, 0, 550), (1024, 8, 1040)])
 def test_strided_rows(dtype, H, at, wide):
