@@ -4,7 +4,8 @@
 //   y_i = s E[a_i], 0 where a_i is outside [0, V);  dE_v = s sum_{a_i = v} dy_i.
 //
 // The gradient of a small table (k_embed_scan) looks for each row's positions in
-// the whole list, a part of it in every work-group, and adds the parts in order.
+// the whole list, a part of it in every work-group, and adds the parts in order;
+// that of few positions (k_embed_few) does so for the tokens that occur.
 // Otherwise it sorts the positions by token (stably, by 8-bit digits, least
 // first; codes outside the table sort behind it), so that a row's positions lie
 // together, and cuts the sorted list into equal chunks whatever the tokens are:
@@ -480,22 +481,14 @@ struct ScanArgs {
   float* part;  // [parts][V][H]; not used by a single one
 };
 
-// A row of the table, 64 pieces of its columns, kScan positions: every wave
-// looks through 64 of them and adds up the rows of dy that belong to it; the
-// waves' sums meet in LDS.  A row's parts are neighbouring work-groups: on
-// different XCDs, where one token has all positions.
+// Adds to `sum` the rows of dy whose positions among the 64 from `at` on have
+// token v, a piece of each a lane.
 template <typename DT>
-__global__ void __launch_bounds__(kScan) k_embed_scan(const ScanArgs a, int parts) {
-  constexpr int V = Piece<DT>::V, kAhead = 8;
-  __shared__ float sums[kScan / 64][64 * V];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), H = a.g.H;
-  const int v = blockIdx.x / (unsigned)parts, part = blockIdx.x - v * parts, at = part * kScan + w * 64, n = (int)a.g.n;
-  const int col = column<DT>(blockIdx.y * 64 + lane, H);
-  const DT* dy = reinterpret_cast<const DT*>(a.g.dout);
-  float sum[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) sum[j] = 0.0f;
-  unsigned long long m = __ballot(at + lane < n && a.g.tokens[min(at + lane, n - 1)] == v);
+__device__ __forceinline__ void add_rows(float (&sum)[Piece<DT>::V], const EmbedGradArgs& g, int v, int at, int col) {
+  constexpr int kAhead = 8;
+  const int lane = threadIdx.x & 63, n = (int)g.n;
+  const DT* dy = reinterpret_cast<const DT*>(g.dout);
+  unsigned long long m = __ballot(at + lane < n && g.tokens[min(at + lane, n - 1)] == v);
   while (m) {
     u32x4 r[kAhead];
     const int count = __popcll(m);
@@ -504,25 +497,54 @@ __global__ void __launch_bounds__(kScan) k_embed_scan(const ScanArgs a, int part
     for (int k = 0; k < kAhead; ++k) {
       q = m ? __builtin_ctzll(m) : q;  // (past the last one: that one again)
       m &= m - 1;
-      r[k] = load_piece(dy + (long)(at + q) * a.g.dout_ld, col, H);
+      r[k] = load_piece(dy + (long)(at + q) * g.dout_ld, col, g.H);
     }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       if (k >= count) break;
-      float x[V];
+      float x[Piece<DT>::V];
       Piece<DT>::get(r[k], x);
 #pragma unroll
-      for (int j = 0; j < V; ++j) sum[j] += x[j];
+      for (int j = 0; j < Piece<DT>::V; ++j) sum[j] += x[j];
     }
   }
+}
+
+// The sums of the work-group's kScan / 64 waves, in order; the column and its
+// total of a thread that has one.
+template <int V>
+__device__ __forceinline__ bool add_waves(float (*sums)[64 * V], const float (&sum)[V], int H, int& c, float& total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
 #pragma unroll
   for (int j = 0; j < V; ++j) sums[w][lane * V + j] = sum[j];
   __syncthreads();
-  const int piece = blockIdx.y * 64 + threadIdx.x / V, c = column<DT>(piece, H) + threadIdx.x % V;
-  if (threadIdx.x >= 64 * V || piece * V >= H || c >= H) return;
-  float total = 0.0f;
+  const int piece = blockIdx.y * 64 + threadIdx.x / V;
+  c = max(min(piece * V, H - V), 0) + threadIdx.x % V;
+  if (threadIdx.x >= 64 * V || piece * V >= H || c >= H) return false;
+  total = 0.0f;
 #pragma unroll
   for (int i = 0; i < kScan / 64; ++i) total += sums[i][threadIdx.x];
+  return true;
+}
+
+// A row of the table, 64 pieces of its columns, kScan positions: every wave
+// looks through 64 of them and adds up the rows of dy that belong to it; the
+// waves' sums meet in LDS.  A row's parts are neighbouring work-groups: on
+// different XCDs, where one token has all positions.
+template <typename DT>
+__global__ void __launch_bounds__(kScan) k_embed_scan(const ScanArgs a, int parts) {
+  constexpr int V = Piece<DT>::V;
+  __shared__ float sums[kScan / 64][64 * V];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), H = a.g.H;
+  const int v = blockIdx.x / (unsigned)parts, part = blockIdx.x - v * parts, at = part * kScan + w * 64;
+  const int col = column<DT>(blockIdx.y * 64 + lane, H);
+  float sum[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+  add_rows<DT>(sum, a.g, v, at, col);
+  int c;
+  float total;
+  if (!add_waves<V>(sums, sum, H, c, total)) return;
   const long to = (long)v * H + c;
   if (parts == 1)
     a.g.dtable[to] = a.g.scale * total;
@@ -540,6 +562,49 @@ __global__ void __launch_bounds__(256) k_embed_parts(const ScanArgs a, int parts
   a.g.dtable[i] = a.g.scale * total;
 }
 
+// Few positions of a larger table, in one launch.  The first n work-groups: a
+// position each; if its token has not come earlier, all its positions' rows are
+// summed, the waves taking 64 positions in turn, and their sums meet in LDS.
+// The others: `rows` rows of the table each, cleared where no token names them.
+template <typename DT>
+__global__ void __launch_bounds__(kScan) k_embed_few(const EmbedGradArgs a, int rows) {
+  constexpr int V = Piece<DT>::V;
+  __shared__ float sums[kScan / 64][64 * V];
+  const int H = a.H, n = (int)a.n, i = blockIdx.x;
+  if (i >= n) {
+    if (blockIdx.y > 0) return;
+    uint32_t* named = reinterpret_cast<uint32_t*>(sums);
+    const int r0 = (i - n) * rows, count = min(rows, a.V - r0);
+    if ((int)threadIdx.x < count) named[threadIdx.x] = 0;
+    __syncthreads();
+    for (int j = threadIdx.x; j < n; j += kScan) {
+      const uint32_t r = (uint32_t)a.tokens[j] - (uint32_t)r0;
+      if (r < (uint32_t)count) named[r] = 1;
+    }
+    __syncthreads();
+    const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t pieces = (uint32_t)(H + 3) / 4, all = pieces * count;
+    for (uint32_t t = threadIdx.x; t < all; t += kScan) {
+      const uint32_t r = t / pieces;
+      if (!named[r])
+        store_values<float, 4>(a.dtable + (long)(r0 + (int)r) * H, column<float>((int)(t - r * pieces), H), H, zero);
+    }
+    return;
+  }
+  const int v = a.tokens[i], col = column<DT>(blockIdx.y * 64 + (threadIdx.x & 63), H);
+  if (v < 0 || v >= a.V) return;
+  int earlier = 0;
+  for (int j = threadIdx.x; j < i; j += kScan) earlier |= a.tokens[j] == v;
+  if (__syncthreads_or(earlier)) return;
+  float sum[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+  for (int at = threadIdx.x & ~63; at < n; at += kScan) add_rows<DT>(sum, a, v, __builtin_amdgcn_readfirstlane(at), col);
+  int c;
+  float total;
+  if (add_waves<V>(sums, sum, H, c, total)) a.dtable[(long)v * H + c] = a.scale * total;
+}
+
 // The most work-groups (in columns of 256) of a gradient without sorting.
 // Measured against sorting, with tokens that name all rows alike and one row
 // only: 1024 rows of 64 from 500 positions (1024 work-groups) 3.8 and
@@ -549,10 +614,17 @@ __global__ void __launch_bounds__(256) k_embed_parts(const ScanArgs a, int parts
 // 64 from 40000 (10112) 28.5 and 19.7 against 19.4 and 45.2.
 constexpr long kScanGroups = 4096;
 constexpr long kScanParts = 64;  // ... and the most parts, which are added one after the other
+// Positions up to which a larger table is done in one launch.  Measured against
+// sorting, tokens that name all rows alike and one row only: 1000 positions of
+// 4000 rows of 64 fp32 values 5.4 against 16.0 us, of 57600 of 512 bf16 ones 19.8
+// against 29.9; 1500 of 4000 of 64 7.0 and 22.6 against 17.1 and 19.2, 3000 11.5
+// and 42.2 against 19.6 and 25.1.
+constexpr int kFew = 1024;
 
 // How a call is cut.
 struct Plan {
   int parts;                // without sorting; 0: with
+  bool few;                 // one launch, no workspace
   int passes, tile, tiles;  // of the sort (tiles 0: one work-group)
   int chunk, chunks;
   size_t hist, start, part, total;  // workspace, after the keys and positions twice: counts, rows' begins, partial sums
@@ -562,6 +634,7 @@ Plan plan(long n, int V, int H) {
   const long columns = (H + 255) / 256;
   const long parts = (n + kScan - 1) / kScan, most_parts = std::min(kScanParts, kScanGroups / ((long)V * columns));
   if (n > 0 && parts <= most_parts) p.parts = (int)parts;
+  p.few = n > 0 && p.parts == 0 && n <= kFew && n * columns <= kScanGroups;
   p.passes = 1;
   while (p.passes < 4 && (uint64_t)V >> (8 * p.passes)) ++p.passes;  // the keys are 0 .. V
   if (n > kOne) {
@@ -617,6 +690,13 @@ hipError_t launch_embed_grad(int dtype, const EmbedGradArgs& a, hipStream_t s) {
     if (e != hipSuccess || p.parts == 1) return e;
     const long size = (long)a.V * a.H;
     return launch("embed_parts", k_embed_parts, dim3((unsigned)((size + 255) / 256)), dim3(256), 0, s, q, p.parts);
+  }
+  if (p.few) {
+    // 64 KB of the table a work-group, a flag for each row in LDS
+    const int rows = std::min(kScan, std::max(1, 16384 / a.H));
+    const dim3 grid((unsigned)(a.n + ((long)a.V + rows - 1) / rows), columns);
+    return dtype == WM_FP32 ? launch("embed_few", k_embed_few<float>, grid, dim3(kScan), 0, s, a, rows)
+                            : launch("embed_few", k_embed_few<bf16_t>, grid, dim3(kScan), 0, s, a, rows);
   }
   const size_t list = p.hist / 4;
   uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws), reinterpret_cast<uint32_t*>(ws + list)};

@@ -90,6 +90,16 @@ def test_embed_grad_both_ways(n, V, H, dtype, how):
     test_embed_grad(n, V, H, dtype, how)
 
 
+@pytest.mark.parametrize("n,V,H,dtype,how", [  # few positions of a large table, and one more than that way takes
+    (1, 5000, 64, "fp32", "one"), (2, 9001, 3, "bf16", "any"), (64, 5000, 257, "fp32", "one"),
+    (65, 5000, 8, "bf16", "rising"), (511, 4700, 100, "fp32", "any"), (513, 5000, 300, "bf16", "one"),
+    (1000, 5003, 367, "fp32", "any"), (1024, 2500, 1024, "bf16", "any"), (1024, 5000, 130, "fp32", "one"),
+    (1025, 5000, 130, "fp32", "one"), (700, 5000, 64, "bf16", "none"), (15, 40, 65536, "bf16", "any"),
+    (17, 40, 65536, "fp32", "any")])
+def test_embed_grad_of_few_positions(n, V, H, dtype, how):
+    test_embed_grad(n, V, H, dtype, how)
+
+
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 def test_strided_rows_and_shapes(dtype):
     rng = np.random.default_rng(5)
