@@ -127,6 +127,11 @@ __device__ __forceinline__ float gate_exp(float g) {
   return gate_exp_small(g);
 }
 
+// The gates of any g, in the same bits as gate_pair_small where that may be used.
+__device__ __forceinline__ float2 gate_pair_any(float g) {
+  return fabsf(g) <= kGateMost ? gate_pair_small(g) : gate_pair_of(g, expf(-fabsf(g)));
+}
+
 // What a wave knows of its 64 channels.
 struct Lanes {
   long c;        // the lane's channel (row b, column h)
@@ -568,13 +573,13 @@ __device__ __forceinline__ Map fold(float (&A)[kTT], float (&U)[kTT], const type
     if (MASKED && i >= k.some) continue;
     const float g = Chan<DT>::get(gr[i]), x = Chan<DT>::get(xr[i]);
     if constexpr (MASKED) {
-      const float2 p = gate_pair_of(g, gate_exp_any(g));
+      const float2 p = gate_pair_any(g);
       const bool live = i < k.live;
       A[i] = live ? (k.reset(i) ? -1.0f : p.x) : 1.0f;
       U[i] = live ? p.y * x : 0.0f;
       m = then(m, {A[i], U[i]});
     } else {
-      const float2 p = gate_pair_of(g, gate_exp_small(g));
+      const float2 p = gate_pair_small(g);
       A[i] = p.x;
       U[i] = p.y * x;
       m.A *= p.x;
@@ -642,7 +647,7 @@ __device__ __forceinline__ Map fold_grad(float (&A)[kTT], float (&M)[kTT], float
   for (int i = 0; i < kTT; ++i) {
     if (MASKED && i >= k.some) continue;
     const float g = Chan<DT>::get(gr[i]), x = Chan<DT>::get(xr[i]), d = Chan<DT>::get(dr[i]);
-    const float2 p = gate_pair_of(g, MASKED ? gate_exp_any(g) : gate_exp_small(g));
+    const float2 p = MASKED ? gate_pair_any(g) : gate_pair_small(g);
     A[i] = p.x;
     M[i] = p.y;
     if (MASKED && k.reset(i)) h = 0.0f;
