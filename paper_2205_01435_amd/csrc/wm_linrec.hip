@@ -36,12 +36,10 @@
 // bf16 channels 147 us in all, 2.7 TB/s, with 4 us each way for emptying the maps.
 // 17 us each way are the wait for earlier segments' maps, which begins anew with
 // each of the five to six rounds of work-groups that the registers admit.
-//
-// A map whose run holds a reset does not depend on the state at all: A = -1
-// says so (a true A is never negative), because 0 * inf would not.
 #include <algorithm>
 
 #include "../../include/wm.h"
+#include "wm_chain.h"
 #include "wm_kernels.h"
 #include "wm_seq.h"
 #include "wm_profile.h"
@@ -57,10 +55,6 @@ namespace {
 constexpr int kWaves = 8, kWide = 16;
 constexpr int kTT = 16;        // steps of a tile
 constexpr int kSeg = kWaves * kTT;
-// Segments whose maps are composed into one for the segments after them.
-// Measured, 32768 steps of 1024 channels in bf16, both directions: 4 157 us, 8
-// 154, 16 162.
-constexpr int kFan = 8;
 constexpr int kMaxSegs = 1024; // segments of a launch; longer sequences take several
 // Channel groups (of 64) from which a wave walks all steps.  Measured, forward
 // and gradient of 500 steps, split against walked: fp32 1280 groups 258 and 268
@@ -100,19 +94,6 @@ template <> struct Chan<bf16_t> {
   }
 };
 #undef WM_GLOBAL
-
-struct Map {
-  float A, U;
-};
-__device__ __forceinline__ float apply(Map m, float h) {
-  const float u = fmaf(m.A, h, m.U);
-  return m.A < 0.0f ? m.U : u;
-}
-// first m, then n
-__device__ __forceinline__ Map then(Map m, Map n) {
-  const float a = n.A * m.A;
-  return {n.A < 0.0f || m.A < 0.0f ? -1.0f : a, apply(n, m.U)};
-}
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
@@ -465,35 +446,28 @@ __device__ __forceinline__ Map await(const unsigned long long* p, unsigned long 
   return {__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
 }
 
-// Composes the maps of segments [s, s1), in order; four loads in flight.  A
-// whole fan (s is one's first) comes from the fan's map if that is there; if
-// not, from its segments' maps, which are published earlier.
-__device__ __forceinline__ Map compose(const unsigned long long* seg, const unsigned long long* fan, int s, int s1,
-                                       long stride, unsigned* head) {
-  Map m{1.0f, 0.0f};
+// compose() over the published maps of a lane's channel, four of a fan's members in flight.
+__device__ __forceinline__ Map published(const unsigned long long* seg, const unsigned long long* fan, int s, int s1,
+                                         long stride, unsigned* head) {
+  return compose(
+      s, s1,
+      [&](int i, Map& f) {
+        const unsigned long long v = peek(fan + i / kFan * stride);
+        if (!__all(v != kEmpty)) return false;
+        f = await(fan, v, head);
+        return true;
+      },
+      [&](int i, int e, auto take) {
 #pragma unroll 1
-  while (s < s1) {
-    const int e = min(s + kFan, s1);
-    if (e - s == kFan) {
-      const unsigned long long f = peek(fan + s / kFan * stride);
-      if (__all(f != kEmpty)) {
-        m = then(m, await(fan, f, head));
-        s = e;
-        continue;
-      }
-    }
-#pragma unroll 1
-    for (; s < e; s += 4) {
-      unsigned long long v[4];
+        for (; i < e; i += 4) {
+          unsigned long long v[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = s + k < e ? peek(seg + (s + k) * stride) : 0;
+          for (int k = 0; k < 4; ++k) v[k] = i + k < e ? peek(seg + (i + k) * stride) : 0;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (s + k < e) m = then(m, await(seg + (s + k) * stride, v[k], head));
-    }
-    s = e;
-  }
-  return m;
+          for (int k = 0; k < 4; ++k)
+            if (i + k < e) take(await(seg + (i + k) * stride, v[k], head));
+        }
+      });
 }
 
 // What the work-group's waves share: the tiles' maps, the parts of the
@@ -528,7 +502,7 @@ __device__ __forceinline__ Map before(Shared<kWaves>& sh, const Chain& ch, int o
   }
 #pragma unroll 1
   for (;; fan = false) {
-    p = compose(ch.seg + at, ch.fan + at, fan ? order - (kFan - 1) : first(i0), fan ? order : first(i1), stride, ch.head);
+    p = published(ch.seg + at, ch.fan + at, fan ? order - (kFan - 1) : first(i0), fan ? order : first(i1), stride, ch.head);
     if (!fan) break;
     publish(ch.fan + order / kFan * stride + at, then(p, own));
   }
