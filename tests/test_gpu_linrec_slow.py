@@ -47,3 +47,21 @@ def test_the_same_bits_again(T, mean, dtype):
         wm.status(again)
         for k in OUTS:
             assert torch.equal(getattr(first, k), getattr(again, k)), (k, i)
+
+
+@pytest.mark.parametrize("T,B,H,dtype,mean,masks", [  # segments, one fan, several, more than one launch takes
+    (1100, 2, 40, "fp32", 7.0, False), (1100, 5, 33, "bf16", 9.0, True), (1300, 3, 70, "fp32", 6.0, True),
+    (5000, 1, 130, "fp32", 8.0, False), (5100, 4, 10, "bf16", 6.0, True), (8191, 3, 22, "fp32", 9.0, True),
+    (20000, 1, 65, "bf16", 7.0, False), (20000, 2, 9, "fp32", 9.0, True), (140001, 1, 3, "fp32", 8.0, False),
+    (140001, 3, 1, "bf16", 9.0, True),
+    (100, 2, 64, "fp32", 8.0, False), (256, 3, 50, "bf16", 7.0, True),   # a single segment
+    (60, 301, 437, "fp32", 7.0, True)])                                  # a wave for all steps
+def test_slow_gates(T, B, H, dtype, mean, masks):
+    say("linrec slow", T, B, H, dtype, mean, masks)
+    d, t = _inputs(T, B, H, dtype, masks, T + B + H)
+    t["gate"] = dev(d["gate"] + (mean - 2.0), dtype)
+    d["gate"] = host(t["gate"])
+    bufs, check = _bufs(T, B, H, dtype)
+    _run(t, bufs)
+    check()
+    _compare(d, bufs, dtype)
