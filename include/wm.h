@@ -423,6 +423,9 @@ wm_status wm_layer_norm_grad(int32_t dtype, int64_t rows, int32_t H, const void 
  * h_{t-1} = 0, whatever the state holds (NaN and infinities too).  A step
  * t >= lengths[b] is padding: y_t = 0, the state stays, and neither x, gate
  * nor resets of it enter any result.
+ * An infinite state stays infinite to the end of its trajectory, however fast
+ * its steps forget; a gate of -inf (a = 0) makes it NaN, and so does an infinity
+ * of the other sign.  (The gradient's R likewise, backwards.)
  *   x, gate [T, B, H] in dtype, unit stride along H, element strides x_t and
  *   x_b (gate_t, gate_b) of steps and rows: the halves of one projection's
  *   rows, for example.

@@ -17,9 +17,24 @@ __host__ __device__ __forceinline__ float apply(Map m, float h) {
   const float u = fmaf(m.A, h, m.U);
   return m.A < 0.0f ? m.U : u;
 }
+// A product of two gates or of their products.  One that leaves fp32's range is
+// held at its least positive number, so that an infinite state stays infinite
+// however the steps are cut into maps (0 * inf is NaN); that moves a finite h by
+// at most 1.4e-45 |h|, the spacing of products there.  A gate that is 0 itself
+// (-inf) keeps its product 0.
+__host__ __device__ __forceinline__ float both(float a, float b) {
+  const int x = __builtin_bit_cast(int, a), y = __builtin_bit_cast(int, b), p = __builtin_bit_cast(int, a * b);
+  const int least = x < y ? (x < 1 ? x : 1) : (y < 1 ? y : 1);  // (positive floats lie in the order of their bits)
+  return __builtin_bit_cast(float, p > least ? p : least);
+}
+// ... where neither is 0.
+__host__ __device__ __forceinline__ float both_positive(float a, float b) {
+  const int p = __builtin_bit_cast(int, a * b);
+  return __builtin_bit_cast(float, p > 1 ? p : 1);
+}
 // first m, then n
 __host__ __device__ __forceinline__ Map then(Map m, Map n) {
-  const float a = n.A * m.A;
+  const float a = both(n.A, m.A);
   return {n.A < 0.0f || m.A < 0.0f ? -1.0f : a, apply(n, m.U)};
 }
 

@@ -97,11 +97,18 @@ template <> struct Chan<bf16_t> {
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// e^-|g| beyond kGateMost.  Where that of a finite g leaves fp32's range it is
+// held at the least positive number: only an infinite g makes a gate, or its
+// complement, 0, which an infinite state or input would turn to NaN.
+__device__ __forceinline__ float gate_exp_far(float g) {
+  const float e = expf(-fabsf(g));
+  return e == 0.0f && fabsf(g) < INFINITY ? __FLT_DENORM_MIN__ : e;
+}
 // e^-|g|: the long way too where some lane of the wave needs it (NaN and
 // infinity lie beyond the bound), for that lane alone: a channel's bits do not
 // depend on its neighbours.
 __device__ __forceinline__ float gate_exp_any(float g) {
-  return fabsf(g) <= kGateMost ? gate_exp_small(g) : expf(-fabsf(g));
+  return fabsf(g) <= kGateMost ? gate_exp_small(g) : gate_exp_far(g);
 }
 __device__ __forceinline__ float gate_exp(float g) {
   if (__builtin_expect(__any(!(fabsf(g) <= kGateMost)), 0)) return gate_exp_any(g);
@@ -110,7 +117,7 @@ __device__ __forceinline__ float gate_exp(float g) {
 
 // The gates of any g, in the same bits as gate_pair_small where that may be used.
 __device__ __forceinline__ float2 gate_pair_any(float g) {
-  return fabsf(g) <= kGateMost ? gate_pair_small(g) : gate_pair_of(g, expf(-fabsf(g)));
+  return fabsf(g) <= kGateMost ? gate_pair_small(g) : gate_pair_of(g, gate_exp_far(g));
 }
 
 // What a wave knows of its 64 channels.
@@ -560,6 +567,7 @@ __device__ __forceinline__ Map fold(float (&A)[kTT], float (&U)[kTT], const type
       m.U = fmaf(p.x, m.U, U[i]);
     }
   }
+  if constexpr (!MASKED) m.A = both_positive(m.A, 1.0f);  // (a gate within kGateMost is not 0)
   return m;
 }
 
@@ -632,13 +640,13 @@ __device__ __forceinline__ Map fold_grad(float (&A)[kTT], float (&M)[kTT], float
         h = to;
         if (k.reset(i)) r.A = -1.0f;
         if (!(r.A < 0.0f)) {
-          r.A *= p.x;
+          r.A = both(r.A, p.x);
           r.U = fmaf(r.A, d, r.U);
         }
       }
     } else {
       h = to;
-      r.A *= p.x;
+      r.A = both_positive(r.A, p.x);
       r.U = fmaf(r.A, d, r.U);
     }
   }
