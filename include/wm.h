@@ -475,8 +475,8 @@ wm_status wm_linrec_grad(int32_t dtype, int32_t T, int32_t B, int32_t H, const v
  * tensors clipped to it:
  *   norm = sqrt(sum over all tensors of sum g^2), summed in 64 bits;
  *   out = g * (max_norm / norm) where norm > max_norm, else out = g.
- * Where the norm is NaN or infinite (a gradient holds one), out = g: the
- * caller sees it in `norm`.
+ * Where `norm` is NaN or infinite (a gradient holds one, or float32 cannot hold
+ * the norm of finite ones), out = g: the caller sees it there.
  *   tensors [n]          HOST array, read before the call returns: contiguous
  *                        device arrays of `n` values each; `out` in the same
  *                        type, may be `grad` itself, and overlaps no other.

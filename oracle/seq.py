@@ -163,5 +163,7 @@ def linrec_grad(x, gate, dy, dh_T=None, h0=None, resets=None, lengths=None):
 def clip(grads, max_norm):
     """(norm, factor, outs)."""
     norm = float(np.sqrt(sum(float((g.astype(np.float64) ** 2).sum()) for g in grads)))
-    f = max_norm / norm if norm > max_norm and np.isfinite(norm) else 1.0
+    with np.errstate(over="ignore"):
+        seen = np.float32(norm)  # what the caller gets: infinite where fp32 cannot hold the norm
+    f = max_norm / norm if norm > max_norm and np.isfinite(seen) else 1.0
     return norm, f, [g.astype(np.float64) * f for g in grads]

@@ -159,8 +159,9 @@ __global__ void __launch_bounds__(kThreads) k_clip_scale(const Table t, const do
 #pragma unroll 8
   for (uint32_t k = threadIdx.x; k < parts; k += kThreads) s += part[k];
   const double N = sqrt(group_sum(s, sh));
-  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)N;
-  const float f = N > (double)max_norm && N < (double)INFINITY ? (float)((double)max_norm / N) : 1.0f;
+  const float seen = (float)N;  // what the caller sees decides: infinite where fp32 cannot hold it
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = seen;
+  const float f = N > (double)max_norm && seen < INFINITY ? (float)((double)max_norm / N) : 1.0f;
   for (uint32_t i = blockIdx.x; i < all; i += gridDim.x) {
     const Chunk c = next;
     u32x4 r[kPer];
