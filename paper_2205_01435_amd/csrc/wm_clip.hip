@@ -139,13 +139,25 @@ __global__ void __launch_bounds__(kThreads) k_clip_sum(const Table t, double* pa
   if (threadIdx.x == 0) part[t.part0 + blockIdx.x] = s;
 }
 
-__device__ __forceinline__ u32x4 scaled(u32x4 r, bool bf16, float f) {
+// The factor of every value.  Below fp32's normal numbers (values of 1e30 to a norm
+// of 1e-10) it has too few bits there: the product is then one of 64 bits.
+struct Factor {
+  float f;
+  double d;
+  bool small;
+  __device__ Factor(double v) : f((float)v), d(v), small(__any(v < 0x1p-126)) {}  // (the same in every lane)
+  __device__ float of(float g) const {
+    if (small) return (float)(d * (double)g);
+    return f * g;
+  }
+  __device__ u32x4 of(u32x4 r, bool bf16) const {
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    r[j] = bf16 ? pack2_bf16(f * __uint_as_float(r[j] << 16), f * __uint_as_float(r[j] & 0xffff0000u))
-                : __float_as_uint(f * __uint_as_float(r[j]));
-  return r;
-}
+    for (int j = 0; j < 4; ++j)
+      r[j] = bf16 ? pack2_bf16(of(__uint_as_float(r[j] << 16)), of(__uint_as_float(r[j] & 0xffff0000u)))
+                  : __float_as_uint(of(__uint_as_float(r[j])));
+    return r;
+  }
+};
 
 template <bool STREAM>
 __global__ void __launch_bounds__(kThreads) k_clip_scale(const Table t, const double* part, uint32_t parts, float max_norm,
@@ -161,7 +173,7 @@ __global__ void __launch_bounds__(kThreads) k_clip_scale(const Table t, const do
   const double N = sqrt(group_sum(s, sh));
   const float seen = (float)N;  // what the caller sees decides: infinite where fp32 cannot hold it
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = seen;
-  const float f = N > (double)max_norm && seen < INFINITY ? (float)((double)max_norm / N) : 1.0f;
+  const Factor by(N > (double)max_norm && seen < INFINITY ? (double)max_norm / N : 1.0);
   for (uint32_t i = blockIdx.x; i < all; i += gridDim.x) {
     const Chunk c = next;
     u32x4 r[kPer];
@@ -169,24 +181,24 @@ __global__ void __launch_bounds__(kThreads) k_clip_scale(const Table t, const do
     for (int k = 0; k < kPer; ++k) r[k] = ahead[k];
     if (i + gridDim.x < all) {
       next = Chunk(t, all - 1 - (i + gridDim.x));
-      if (f != 1.0f || next.in != next.out) next.load(ahead);
+      if (by.f != 1.0f || next.in != next.out) next.load(ahead);
     }
-    if (f == 1.0f && c.in == c.out) continue;  // in place, and within the limit
+    if (by.f == 1.0f && c.in == c.out) continue;  // in place, and within the limit
     if (c.whole()) {
 #pragma unroll
       for (int k = 0; k < kPer; ++k)
-        put_piece<STREAM>(c.out + (k * kThreads + threadIdx.x) * 16, scaled(r[k], c.bf16, f));
+        put_piece<STREAM>(c.out + (k * kThreads + threadIdx.x) * 16, by.of(r[k], c.bf16));
     } else {
       int at = threadIdx.x * 16;
       for (; at + 16 <= c.bytes; at += kThreads * 16)
-        *reinterpret_cast<u32x4_2*>(c.out + at) = scaled(c.load(at), c.bf16, f);
+        *reinterpret_cast<u32x4_2*>(c.out + at) = by.of(c.load(at), c.bf16);
       const int es = c.bf16 ? 2 : 4;
       for (; at < c.bytes; at += es) {
         if (c.bf16)
           DType<bf16_t>::store(reinterpret_cast<bf16_t*>(c.out + at), 0,
-                               f * DType<bf16_t>::load(reinterpret_cast<const bf16_t*>(c.in + at), 0));
+                               by.of(DType<bf16_t>::load(reinterpret_cast<const bf16_t*>(c.in + at), 0)));
         else
-          *reinterpret_cast<float*>(c.out + at) = f * *reinterpret_cast<const float*>(c.in + at);
+          *reinterpret_cast<float*>(c.out + at) = by.of(*reinterpret_cast<const float*>(c.in + at));
       }
     }
   }

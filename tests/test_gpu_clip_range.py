@@ -37,3 +37,22 @@ def test_the_largest_norm_that_fp32_holds_is_clipped():
     plan = wm.ClipPlan([g], [torch.zeros_like(g)])
     assert bool(torch.isfinite(wm.clip_grads(plan, 1.0)).all())
     within(host(plan.outs[0]), np.full(4, 0.5), np.full(4, 3 * seq.U32), "fp32", "out")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n", [5000, 40003])
+@pytest.mark.parametrize("size,limit", [  # factors from 8e-37 down to 0
+    (1e30, 1e-12), (1e36, 1e-3), (1e30, 1e-30), (1e36, 1e-40), (3e33, 0.1)])
+@pytest.mark.parametrize("place", ["out", "in"])
+def test_factors_far_below_one(size, limit, n, dtype, place):
+    say("clip factor", size, limit, n, dtype, place)
+    rng = np.random.default_rng(n)
+    a = host(dev(size * rng.uniform(-1, 1, n), dtype))
+    g = dev(a, dtype)
+    plan = wm.ClipPlan([g], None if place == "in" else [torch.zeros_like(g)])
+    limit = float(np.float32(limit))
+    norm = wm.clip_grads(plan, limit)
+    total, f, (ref,) = seq.clip([a], limit)
+    assert f < 2.0 ** -119 and abs(float(norm) - total) <= 2 * seq.U32 * total  # (below fp32's normal numbers, or near)
+    # the factor's rounding and the product's, and the spacing of the type's least numbers
+    within(host(plan.outs[0]), ref, 3 * seq.U32 * np.abs(ref) + 2.0 ** -149, dtype, "out")
