@@ -748,14 +748,15 @@ class ClipPlan:
         self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=dev)
 
     def _fill(self):
+        """The table of the tensors as they are, whole or not at all."""
         dev = self.grads[0].device
-        self.ptrs = [t.data_ptr() for t in self.grads] + [t.data_ptr() for t in self.outs]
-        self.table = (CGradTensor * len(self.grads))()
+        table = (CGradTensor * len(self.grads))()
         for i, (g, o) in enumerate(zip(self.grads, self.outs)):
             dt = _act(f"grads[{i}]", g)
             _need(f"grads[{i}]", g, g.dtype, g.shape, dev)
             _need(f"outs[{i}]", o, g.dtype, g.shape, dev)
-            self.table[i] = CGradTensor(g.data_ptr(), o.data_ptr(), g.numel(), dt)
+            table[i] = CGradTensor(g.data_ptr(), o.data_ptr(), g.numel(), dt)
+        self.table, self.ptrs = table, [t.data_ptr() for t in self.grads] + [t.data_ptr() for t in self.outs]
 
 
 def clip_grads(plan: ClipPlan, max_norm: float):
