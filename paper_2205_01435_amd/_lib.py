@@ -14,6 +14,7 @@ import os
 from dataclasses import dataclass
 
 import torch
+from torch._C._dynamo.guards import TensorGuards
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libwm.so")
@@ -729,18 +730,19 @@ def linrec_grad(x, gate, dy, dh_T=None, resets=None, lengths=None, bufs: LinrecB
     return bufs
 
 
+_address = torch.Tensor.data_ptr
+
+
 class ClipPlan:
     """The gradient tensors of a training program (contiguous, float32 or
     bfloat16), where their clipped values go (``outs``; None = in place), the
-    norm and the workspace of wm_clip_grads."""
+    norm and the workspace of wm_clip_grads.  The tensors may be given other
+    memory, sizes or types later, up to what the workspace serves."""
 
     def __init__(self, grads, outs=None):
         self.grads = list(grads)
         self.outs = self.grads if outs is None else list(outs)
-        if not self.grads:
-            raise ValueError("no gradient tensors")
-        if len(self.outs) != len(self.grads):
-            raise ValueError(f"{len(self.outs)} outputs for {len(self.grads)} tensors")
+        self.norm = None
         self._fill()
         dev = self.grads[0].device
         self.norm = torch.empty(1, dtype=torch.float32, device=dev)
@@ -749,14 +751,20 @@ class ClipPlan:
 
     def _fill(self):
         """The table of the tensors as they are, whole or not at all."""
-        dev = self.grads[0].device
+        if not self.grads:
+            raise ValueError("no gradient tensors")
+        if len(self.outs) != len(self.grads):
+            raise ValueError(f"{len(self.outs)} outputs for {len(self.grads)} tensors")
+        dev = self.grads[0].device if self.norm is None else self.norm.device
         table = (CGradTensor * len(self.grads))()
         for i, (g, o) in enumerate(zip(self.grads, self.outs)):
             dt = _act(f"grads[{i}]", g)
             _need(f"grads[{i}]", g, g.dtype, g.shape, dev)
             _need(f"outs[{i}]", o, g.dtype, g.shape, dev)
             table[i] = CGradTensor(g.data_ptr(), o.data_ptr(), g.numel(), dt)
-        self.table, self.ptrs = table, [t.data_ptr() for t in self.grads] + [t.data_ptr() for t in self.outs]
+        all_ = self.grads if self.outs is self.grads else [*self.grads, *self.outs]
+        self.table, self.ptrs = table, list(map(_address, all_))
+        self.same = TensorGuards(*all_, dynamic_dims_sizes=None, dynamic_dims_strides=None).check
 
 
 def clip_grads(plan: ClipPlan, max_norm: float):
@@ -764,8 +772,13 @@ def clip_grads(plan: ClipPlan, max_norm: float):
     plan.norm becomes their global norm, plan.outs their values scaled to
     max_norm where the norm is above it.  Returns plan.norm (a device tensor:
     nothing waits)."""
-    # a tensor may have been given other memory since (its sizes stay the plan's)
-    if [t.data_ptr() for t in plan.grads] + [t.data_ptr() for t in plan.outs] != plan.ptrs:
+    # The table is that of the tensors while their number, types, devices, sizes
+    # and strides (in one call for all of them: 15 tensors and 15 outputs 2.2 us,
+    # one by one 8) and addresses (1.8 us) are what they were.
+    grads, outs = plan.grads, plan.outs
+    all_ = grads if outs is grads else [*grads, *outs]
+    if not (len(grads) == len(plan.table) and len(all_) == len(plan.ptrs) and plan.same(*all_)
+            and list(map(_address, all_)) == plan.ptrs):
         plan._fill()
     _check(load().wm_clip_grads(len(plan.table), plan.table, max_norm, plan.norm.data_ptr(), plan.workspace.data_ptr(),
                                 plan.ws_bytes, _stream()))
