@@ -188,7 +188,14 @@ def _mask_dtype(t):
 def status(bufs) -> None:
     """Wait for the current stream and raise WmError if the last call that
     used ``bufs.workspace`` failed on the device (a timed-out barrier wait of
-    the persistent kernels, or WM_FLAG_CHECK violations)."""
+    the persistent kernels, or WM_FLAG_CHECK violations).  A recurrence that
+    needs no workspace has nothing that could; the buffers of the other
+    sequence-core operators hold no status and are refused."""
+    if isinstance(bufs, (EmbedGradBuffers, LayerNormBuffers, ClipPlan)):
+        raise ValueError(f"{type(bufs).__name__} holds no status")
+    if isinstance(bufs, LinrecBuffers) and bufs.ws_bytes == 0:
+        torch.cuda.current_stream().synchronize()
+        return
     _check(load().wm_workspace_status(_ptr(bufs.workspace), _stream()))
 
 
