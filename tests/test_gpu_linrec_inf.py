@@ -79,3 +79,20 @@ def test_a_gate_of_minus_infinity_forgets(T, B, H):
     assert np.isposinf(y[:T // 2, :, 0]).all() and np.isnan(y[T // 2:, :, 0]).all()
     np.testing.assert_array_equal(y[T // 2, :, 1:], d["x"][T // 2, :, 1:])
     assert np.isfinite(y[..., 1:]).all()
+
+
+@pytest.mark.parametrize("T,B,H", [(20, 4, 18), (600, 4, 18), (40, 600, 256)])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_masked_places_of_the_lowest_value(T, B, H, dtype):
+    """Padding that holds the type's lowest value, as masks are often filled."""
+    _, t = _inputs(T, B, H, dtype, True, 21)
+    clean, _ = _bufs(T, B, H, dtype)
+    _run(t, clean)
+    pad = (torch.arange(T, device="cuda")[:, None] >= t["lengths"][None, :])[..., None]
+    assert bool(pad.any())
+    low = torch.finfo(t["x"].dtype).min
+    dirty = dict(t, **{k: t[k].masked_fill(pad, low) for k in ("x", "gate", "dy")})
+    got, _ = _bufs(T, B, H, dtype)
+    _run(dirty, got)
+    for k in ("y", "h_T", "dxg", "dh0"):
+        assert torch.equal(getattr(got, k), getattr(clean, k)), k
