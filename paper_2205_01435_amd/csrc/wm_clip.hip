@@ -10,11 +10,11 @@
 //
 // Bound by memory: the values are read twice (the second time from the
 // last-level cache where the list fits it: from its end, which was read last)
-// and written once.  Measured, 153 tensors, 270 MB: sum 52 us (5.2 TB/s), scale
-// 86 us (6.3 TB/s).  Chunks in strides over the list keep the work-groups within
-// some MB of each other; a range of the list for each took the sum from 70 to 86
-// us.  Arrays are aligned to their element only; the hardware takes 16-byte
-// accesses at such addresses.
+// and written once.  Measured, 153 tensors, 270 MB: sum 45 us (6.0 TB/s, part of
+// it from the cache), scale 88 us (6.2 TB/s).  Chunks in strides over the list keep
+// the work-groups within some MB of each other; a range of the list for each took
+// the sum from 70 to 86 us.  Arrays are aligned to their element only; the hardware
+// takes 16-byte accesses at such addresses.
 #include <algorithm>
 
 #include "../../include/wm.h"

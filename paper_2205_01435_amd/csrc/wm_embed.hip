@@ -17,9 +17,9 @@
 // the gradient is written once, and the order of each sum is fixed.
 // All of it is bound by memory: dy is read once, the gradient written once.
 // Measured, 81920 positions of 57600 rows of 1024 bf16 values (690 MB both
-// ways): rows 53 us; gradient sort 21, sums 78 (168 MB read, 230 MB written or
-// cleared), join 22: 3.9 TB/s in all.  7224 positions of 50 rows of 367 fp32
-// values: rows 5 us, gradient 11, launches and first loads.
+// ways): rows 54 us; gradient sort 23, sums 79 (168 MB read, 230 MB written or
+// cleared), join 23: 3.9 TB/s in all.  7224 positions of 50 rows of 367 fp32
+// values: rows 5 us, gradient 12, launches and first loads.
 #include <algorithm>
 
 #include "../../include/wm.h"

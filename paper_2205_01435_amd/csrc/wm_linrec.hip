@@ -32,10 +32,11 @@
 // a value): in fp32, and without reading y.
 //
 // The walk is bound by memory: 128 steps of 262144 fp32 channels with padding
-// 62 us forward and 95 us back, 5.2 TB/s.  The split waits: 32768 steps of 1024
-// bf16 channels 147 us in all, 2.7 TB/s, with 4 us each way for emptying the maps.
-// 17 us each way are the wait for earlier segments' maps, which begins anew with
-// each of the five to six rounds of work-groups that the registers admit.
+// 53 us forward and 97 us back, 5.1 TB/s over both.  The split waits: 32768 steps
+// of 1024 bf16 channels 150 us in all, 2.7 TB/s; the kernels 54 and 82 us, and
+// 5 us each way for emptying the maps.  Of 4096 work-groups the registers admit
+// 768 at a time forward and 512 back, so that the wait for earlier segments' maps
+// begins anew five to six times forward and eight times back.
 #include <algorithm>
 
 #include "../../include/wm.h"
