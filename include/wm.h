@@ -495,13 +495,156 @@ wm_status wm_clip_grads(int32_t n, const wm_grad_tensor *tensors, float max_norm
                         void *workspace, size_t workspace_bytes, wm_stream_t stream);
 
 /*
+ * Attending core.  A core that mixes the steps of a sequence by linear attention
+ * in place of the channel-wise recurrence, with a feed-forward block between the
+ * mixings, needs the operators below besides embedding, norms, clipping and its
+ * plain products; the conventions are those of the sequence-core operators.
+ */
+
+/*
+ * Host function: the rotation's angles for `R` rotated values a head (even, 0 ..
+ * 512): table[i], i < R / 2, receives base^(-2 i / R) / (2 pi), the part of a
+ * turn that a step adds to pair i, as a 64-bit binary fraction (the integer
+ * nearest to it times 2^64).  base >= 1 and finite.  A caller with other
+ * frequencies fills its own table.
+ */
+wm_status wm_rotary_table(int32_t R, double base, uint64_t *table);
+
+/*
+ * Norm of every head's queries and keys and their rotation by position, in one
+ * pass.  With r = (sum x^2 / D + eps)^(-1/2) of a head's D values,
+ *   n = x r gamma,  out = n with pair i of its first R values turned by
+ *   positions[row] table[i] turns:
+ *   (n_a cos - n_b sin, n_a sin + n_b cos).
+ *   neighbours           0: pair i is (i, i + R / 2); 1: (2 i, 2 i + 1).
+ *   q [rows, Hq, D], k [rows, Hk, D] in dtype: the heads of a row one after the
+ *   other, rows q_ld and k_ld elements apart (parts of one projection's rows,
+ *   for example).  Hk = 0 takes queries alone (k and k_out are ignored).
+ *   gamma_q, gamma_k [D] float32, nullable (1): every head's.
+ *   positions [rows] int32 (of any sign; the angle is exact modulo a turn);
+ *   table [R / 2] DEVICE array (ignored with R = 0).
+ *   q_out, k_out as q and k, and each may be its input with the same ld.
+ * D in 1 .. 512, R even, 0 .. D; Hq in 1 .. 1024, Hk in 0 .. 1024; eps >= 0 and
+ * finite; rows (Hq + Hk) at most 2^31 - 1.  rows = 0 is a no-op.
+ */
+wm_status wm_qk_norm(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, int32_t D, int32_t R,
+                     int32_t neighbours, const void *q, int64_t q_ld, const void *k, int64_t k_ld,
+                     const float *gamma_q, const float *gamma_k, float eps,
+                     const int32_t *positions, const uint64_t *table, void *q_out,
+                     int64_t q_out_ld, void *k_out, int64_t k_out_ld, wm_stream_t stream);
+
+/*
+ * Gradient of wm_qk_norm from its inputs.  With d the output's gradient turned
+ * back, xh = x r and e = d gamma:
+ *   grad_x = r (e - xh sum(e xh) / D),  grad_gamma = sum of d xh over rows and heads
+ *   ([D] float32, nullable, written whole; rows = 0 writes zeros).
+ *   grad_q_out, grad_k_out, grad_q, grad_k as q and k; grad_q may be grad_q_out and
+ *   grad_k grad_k_out, with the same ld.
+ */
+size_t wm_qk_norm_grad_workspace_bytes(int64_t rows, int32_t Hq, int32_t Hk, int32_t D);
+wm_status wm_qk_norm_grad(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, int32_t D,
+                          int32_t R, int32_t neighbours, const void *q, int64_t q_ld,
+                          const void *k, int64_t k_ld, const float *gamma_q, const float *gamma_k,
+                          float eps, const int32_t *positions, const uint64_t *table,
+                          const void *grad_q_out, int64_t grad_q_out_ld, const void *grad_k_out,
+                          int64_t grad_k_out_ld, void *grad_q, int64_t grad_q_ld, void *grad_k,
+                          int64_t grad_k_ld, float *grad_gamma_q, float *grad_gamma_k,
+                          void *workspace, size_t workspace_bytes, wm_stream_t stream);
+
+/*
+ * Linear attention over B sequences of T steps with N heads, each with its own
+ * decay a and a state S of K x V values:
+ *   S_t = a S_{t-1} + k_t v_t^T,  y_t = scale S_t^T q_t.
+ * A step with resets[t, b] != 0 starts a new trajectory: it takes S_{t-1} = 0,
+ * whatever the state holds.  A step t >= lengths[b] is padding: y_t = 0, the
+ * state stays, and nothing of it enters any result.
+ *   q, k [T, B, N, K], v [T, B, N, V] in dtype: the heads of a row one after the
+ *   other, element strides q_t and q_b (...) of steps and rows.
+ *   decay [N] float32, in [0, 1] (values outside act as clamped); constants of the
+ *   model, without a gradient.
+ *   h0 [B, N, K, V] float32, nullable (0); resets [T, B] uint8, nullable (none);
+ *   lengths [B] int32, nullable (T; values outside [0, T] act as clamped).
+ *   y [T, B, N, V] in dtype; h_T [B, N, K, V] float32, nullable, may be h0: the
+ *   state after the last step (T = 1 with h0 and h_T is the form for acting).
+ *   workspace            of wm_linattn_workspace_bytes, 0 bytes where the call does
+ *                        not split the time axis.
+ * The steps of a sequence are taken 64 at a time, from its first, by matrix
+ * products: a value of a head that is not finite can make every output of that
+ * sequence and head in the same 64 steps not finite, earlier steps and other
+ * trajectories included, and through the state those after it up to a reset.
+ * K and V in 1 .. 128; scale finite; T B, B N, T B N K and T B N V at most 2^31 - 1
+ * and B N K V at most 2^31 - 1.  B = 0 is a no-op; T = 0 gives h_T = h0.
+ */
+size_t wm_linattn_workspace_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V);
+wm_status wm_linattn(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, int32_t V,
+                     const void *q, int64_t q_t, int64_t q_b, const void *k, int64_t k_t,
+                     int64_t k_b, const void *v, int64_t v_t, int64_t v_b, const float *decay,
+                     float scale, const float *h0, const uint8_t *resets, const int32_t *lengths,
+                     void *y, float *h_T, void *workspace, size_t workspace_bytes,
+                     wm_stream_t stream);
+
+/*
+ * Gradient of wm_linattn by the reverse recurrence, from its inputs.  With G the
+ * gradient of the state after step t from all later ones, G_{T-1} = grad_h_T, and
+ * F_t = G_t + scale q_t grad_y_t^T for a step inside its sequence:
+ *   grad_q_t = scale S_t grad_y_t,  grad_k_t = F_t v_t,  grad_v_t = F_t^T k_t,
+ *   G_{t-1} = a F_t, or 0 at a reset;  grad_h0 = G_{-1}.
+ * Padded steps get 0 and pass G on.
+ *   grad_y as v, grad_q, grad_k and grad_v as q, k and v (dtype, strides);
+ *   grad_h_T [B, N, K, V] float32, nullable (0); grad_h0 [B, N, K, V] float32,
+ *   nullable, may be grad_h_T.
+ */
+size_t wm_linattn_grad_workspace_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V);
+wm_status wm_linattn_grad(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, int32_t V,
+                          const void *q, int64_t q_t, int64_t q_b, const void *k, int64_t k_t,
+                          int64_t k_b, const void *v, int64_t v_t, int64_t v_b,
+                          const float *decay, float scale, const float *h0, const uint8_t *resets,
+                          const int32_t *lengths, const void *grad_y, int64_t grad_y_t,
+                          int64_t grad_y_b, const float *grad_h_T, void *grad_q, int64_t grad_q_t,
+                          int64_t grad_q_b, void *grad_k, int64_t grad_k_t, int64_t grad_k_b,
+                          void *grad_v, int64_t grad_v_t, int64_t grad_v_b, float *grad_h0,
+                          void *workspace, size_t workspace_bytes, wm_stream_t stream);
+
+/*
+ * Gated projection of a feed-forward block (its second, plain product is the
+ * caller's):
+ *   [g | u] = x W^T,  h = act(g) u.
+ *   x [rows, D], h [rows, F] in dtype; W [2F, D] in dtype, contiguous: the F rows
+ *   of the gate, then those of the other factor.
+ *   act                  WM_ACT_SILU g sigmoid(g), WM_ACT_GELU g Phi(g) with the
+ *                        normal distribution function.
+ *   pre [rows, 2F] in dtype, nullable: receives [g | u], what the gradient reads.
+ * D and F in 1 .. 65536; rows at most 2^31 - 1 and rows F at most 2^43.  rows = 0 is
+ * a no-op.
+ */
+enum { WM_ACT_SILU = 0, WM_ACT_GELU = 1 };
+wm_status wm_glu(int32_t dtype, int64_t rows, int32_t D, int32_t F, int32_t act, const void *x,
+                 int64_t x_ld, const void *W, void *h, int64_t h_ld, void *pre,
+                 wm_stream_t stream);
+
+/*
+ * Gradient of wm_glu from its inputs and `pre`:
+ *   dg = grad_h u act'(g), du = grad_h act(g);
+ *   grad_x = [dg | du] W;  grad_W = [dg | du]^T x, in dtype (the weights' own type),
+ *   summed in fp32, nullable, written whole; rows = 0 writes zeros.
+ * With bf16, g and u were rounded when they were saved, and dg and du are rounded
+ * once before the two products.
+ */
+size_t wm_glu_grad_workspace_bytes(int32_t dtype, int64_t rows, int32_t D, int32_t F);
+wm_status wm_glu_grad(int32_t dtype, int64_t rows, int32_t D, int32_t F, int32_t act,
+                      const void *x, int64_t x_ld, const void *W, const void *pre,
+                      const void *grad_h, int64_t grad_h_ld, void *grad_x, int64_t grad_x_ld,
+                      void *grad_W, void *workspace, size_t workspace_bytes, wm_stream_t stream);
+
+/*
  * Measurement aid (no counterpart in the paper).  While a prefix is set, every
  * kernel launch of the library whose name starts with it is bracketed by HIP
  * events on its stream.  Kernel names: "ctrl", "gates", "mdn" (each followed by
  * "/" and the tile that the call's sizes picked, as "gates/64x32"), "lh", "init",
  * "finish", "nll_init", "nll_reduce", "nll_means", "pack", "returns", "adam", the
- * "grad_" kernels of wm_nll_grad, and "embed", "norm", "linrec" and "clip" with
- * what follows these words in the sequence-core operators; "" selects all,
+ * "grad_" kernels of wm_nll_grad, and "embed", "norm", "linrec", "clip", "qk_norm",
+ * "linattn" and "glu" with what follows these words in the sequence-core and
+ * attending-core operators; "" selects all,
  * NULL turns timing off.  wm_profile_read waits for the recorded events and
  * returns the summed duration (ms) and count of the launches whose name
  * starts with `prefix` (NULL = all); wm_profile_reset forgets them.  Timing

@@ -32,7 +32,9 @@ EXPORTS = ("wm_packed_weights_bytes", "wm_pack_weights", "wm_workspace_bytes", "
            "wm_embed", "wm_embed_grad_workspace_bytes", "wm_embed_grad", "wm_layer_norm",
            "wm_layer_norm_grad_workspace_bytes", "wm_layer_norm_grad", "wm_linrec_states_bytes",
            "wm_linrec_workspace_bytes", "wm_linrec", "wm_linrec_grad", "wm_clip_grads_workspace_bytes",
-           "wm_clip_grads",
+           "wm_clip_grads", "wm_rotary_table", "wm_qk_norm", "wm_qk_norm_grad_workspace_bytes", "wm_qk_norm_grad",
+           "wm_linattn_workspace_bytes", "wm_linattn", "wm_linattn_grad_workspace_bytes", "wm_linattn_grad", "wm_glu",
+           "wm_glu_grad_workspace_bytes", "wm_glu_grad",
            "wm_profile_enable", "wm_profile_read", "wm_profile_reset", "wm_profile_phases",
            "wm_profile_phases_read", "wm_workspace_status",
            "wm_last_error", "wm_version")
@@ -123,6 +125,29 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.wm_clip_grads_workspace_bytes.restype = SZ
     lib.wm_clip_grads.argtypes = [I32, pg, F32, P, P, SZ, P]
     lib.wm_clip_grads.restype = I32
+    lib.wm_rotary_table.argtypes = [I32, ctypes.c_double, P]
+    lib.wm_rotary_table.restype = I32
+    lib.wm_qk_norm.argtypes = [I32, I64, I32, I32, I32, I32, I32, P, I64, P, I64, P, P, F32, P, P, P, I64, P, I64, P]
+    lib.wm_qk_norm.restype = I32
+    lib.wm_qk_norm_grad_workspace_bytes.argtypes = [I64, I32, I32, I32]
+    lib.wm_qk_norm_grad_workspace_bytes.restype = SZ
+    lib.wm_qk_norm_grad.argtypes = [I32, I64, I32, I32, I32, I32, I32, P, I64, P, I64, P, P, F32, P, P, P, I64, P, I64,
+                                    P, I64, P, I64, P, P, P, SZ, P]
+    lib.wm_qk_norm_grad.restype = I32
+    for f in (lib.wm_linattn_workspace_bytes, lib.wm_linattn_grad_workspace_bytes):
+        f.argtypes, f.restype = [I32, I32, I32, I32, I32], SZ
+    lib.wm_linattn.argtypes = [I32, I32, I32, I32, I32, I32, P, I64, I64, P, I64, I64, P, I64, I64, P, F32, P, P, P, P, P,
+                               P, SZ, P]
+    lib.wm_linattn.restype = I32
+    lib.wm_linattn_grad.argtypes = [I32, I32, I32, I32, I32, I32, P, I64, I64, P, I64, I64, P, I64, I64, P, F32, P, P, P,
+                                    P, I64, I64, P, P, I64, I64, P, I64, I64, P, I64, I64, P, P, SZ, P]
+    lib.wm_linattn_grad.restype = I32
+    lib.wm_glu.argtypes = [I32, I64, I32, I32, I32, P, I64, P, P, I64, P, P]
+    lib.wm_glu.restype = I32
+    lib.wm_glu_grad_workspace_bytes.argtypes = [I32, I64, I32, I32]
+    lib.wm_glu_grad_workspace_bytes.restype = SZ
+    lib.wm_glu_grad.argtypes = [I32, I64, I32, I32, I32, P, I64, P, P, P, I64, P, I64, P, P, SZ, P]
+    lib.wm_glu_grad.restype = I32
     lib.wm_profile_enable.argtypes = [ctypes.c_char_p]
     lib.wm_profile_enable.restype = I32
     lib.wm_profile_read.argtypes = [ctypes.c_char_p, ctypes.POINTER(ctypes.c_double),
@@ -190,8 +215,9 @@ def status(bufs) -> None:
     used ``bufs.workspace`` failed on the device (a timed-out barrier wait of
     the persistent kernels, or WM_FLAG_CHECK violations).  A recurrence that
     needs no workspace has nothing that could; the buffers of the other
-    sequence-core operators hold no status and are refused."""
-    if isinstance(bufs, (EmbedGradBuffers, LayerNormBuffers, ClipPlan)):
+    sequence-core and attending-core operators hold no status and are
+    refused."""
+    if isinstance(bufs, (EmbedGradBuffers, LayerNormBuffers, ClipPlan, QkNormBuffers, LinattnBuffers, GluBuffers)):
         raise ValueError(f"{type(bufs).__name__} holds no status")
     if isinstance(bufs, LinrecBuffers) and bufs.ws_bytes == 0:
         torch.cuda.current_stream().synchronize()
@@ -790,6 +816,266 @@ def clip_grads(plan: ClipPlan, max_norm: float):
     _check(load().wm_clip_grads(len(plan.table), plan.table, max_norm, plan.norm.data_ptr(), plan.workspace.data_ptr(),
                                 plan.ws_bytes, _stream()))
     return plan.norm
+
+
+# ---------------------------------------------------------------------------
+# attending-core operators (activations in float32 or bfloat16)
+# ---------------------------------------------------------------------------
+
+def _here(device):
+    """Launches go to the current device: refuses tensors of another one."""
+    if device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors on {device}, but the current device is {torch.cuda.current_device()}")
+
+
+class Rotary:
+    """The rotation's angles for the first R values of a head: pair i turns by
+    base^(-2 i / R) a step; pairs are (i, i + R / 2), or with ``neighbours``
+    (2 i, 2 i + 1)."""
+
+    def __init__(self, R: int, base: float = 10000.0, neighbours: bool = False, device="cuda"):
+        self.R, self.base, self.neighbours = R, base, bool(neighbours)
+        host = (ctypes.c_uint64 * max(R // 2, 1))()
+        _check(load().wm_rotary_table(R, base, host))
+        # 64-bit words, held in a signed type
+        self.table = torch.tensor([v - (v >> 63 << 64) for v in host], dtype=torch.int64).to(device)
+
+
+class QkNormBuffers:
+    """Normed and rotated queries [rows, Hq, D] and keys [rows, Hk, D], and with
+    ``grad`` the gradients and the workspace of wm_qk_norm_grad."""
+
+    def __init__(self, rows: int, Hq: int, Hk: int, D: int, dtype=torch.float32, device="cuda", grad: bool = True):
+        self.rows, self.Hq, self.Hk, self.D, self.dtype = rows, Hq, Hk, D, dtype
+        new = lambda h: torch.empty((rows, h, D), dtype=dtype, device=device)  # noqa: E731
+        self.q, self.k = new(Hq), new(Hk)
+        self.dq, self.dk = (new(Hq), new(Hk)) if grad else (None, None)
+        self.dgamma_q, self.dgamma_k = ((torch.empty(D, dtype=torch.float32, device=device) for _ in range(2)) if grad
+                                        else (None, None))
+        self.ws_bytes = load().wm_qk_norm_grad_workspace_bytes(rows, Hq, Hk, D) if grad else 0
+        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=device) if grad else None
+
+
+def _heads(name, t, H, D, dtype, device):
+    """(rows, distance between rows) of a [..., H, D] tensor whose heads lie one
+    after the other and whose leading dimensions step evenly."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != device:
+        _act(name, t, dtype)
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    shape, st = t.shape, t.stride()
+    if len(shape) < 2 or shape[-2] != H or shape[-1] != D:
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected [..., {H}, {D}]")
+    n = t.numel() // (H * D) if H else math.prod(shape[:-2])
+    if n and H and ((D > 1 and st[-1] != 1) or (H > 1 and st[-2] != D)):
+        raise ValueError(f"{name}'s heads must lie one after the other (strides {st})")
+    if n <= 1 or t.is_contiguous():
+        return n, H * D
+    lead = [(s, d) for s, d in zip(shape[:-2], st[:-2]) if s > 1]
+    for (_, a), (s, b) in zip(lead, lead[1:]):
+        if a != s * b:
+            raise ValueError(f"{name}'s rows are not evenly spaced (strides {st})")
+    if lead[-1][1] < H * D:
+        raise ValueError(f"{name}'s rows overlap (stride {lead[-1][1]}, width {H * D})")
+    return n, lead[-1][1]
+
+
+def _qk_args(q, k, positions, rotary, gamma_q, gamma_k, bufs, grad):
+    dt = _act("q", q)
+    dev, dtype = q.device, q.dtype
+    _here(dev)
+    if q.dim() < 2:
+        raise ValueError(f"q has shape {tuple(q.shape)}, expected [..., Hq, D]")
+    Hq, D = q.shape[-2:]
+    Hk = 0 if k is None else k.shape[-2] if isinstance(k, torch.Tensor) and k.dim() >= 2 else 1
+    rows, ldq = _heads("q", q, Hq, D, dtype, dev)
+    ldk = 0
+    if k is not None:
+        nk, ldk = _heads("k", k, Hk, D, dtype, dev)
+        if nk != rows:
+            raise ValueError(f"k has {nk} rows, q has {rows}")
+    pp = _arr("positions", positions, torch.int32, getattr(positions, "shape", ()), dev)
+    if positions.numel() != rows:
+        raise ValueError(f"{positions.numel()} positions for {rows} rows")
+    if rotary is not None and rotary.table.device != dev:
+        raise ValueError(f"the rotation's table is on {rotary.table.device}, expected {dev}")
+    R, nb, pt = (0, 0, None) if rotary is None else (rotary.R, int(rotary.neighbours), rotary.table.data_ptr())
+    pgq = _arr("gamma_q", gamma_q, torch.float32, (D,), dev, optional=True)
+    pgk = _arr("gamma_k", gamma_k, torch.float32, (D,), dev, optional=True)
+    if bufs is None:
+        bufs = QkNormBuffers(rows, Hq, Hk, D, dtype, dev, grad=grad)
+    if (bufs.rows, bufs.Hq, bufs.Hk, bufs.D, bufs.dtype) != (rows, Hq, Hk, D, dtype) or bufs.q.device != dev:
+        raise ValueError(f"buffers for rows={bufs.rows} Hq={bufs.Hq} Hk={bufs.Hk} D={bufs.D} {bufs.dtype} on "
+                         f"{bufs.q.device}; the call has rows={rows} Hq={Hq} Hk={Hk} D={D} {dtype} on {dev}")
+    head = (dt, rows, Hq, Hk, D, R, nb, q.data_ptr(), ldq, _ptr(k), ldk, pgq, pgk)
+    return head, (pp, pt), bufs
+
+
+def qk_norm(q, k, positions, rotary: Rotary | None, gamma_q=None, gamma_k=None, eps: float = 1e-6,
+            bufs: QkNormBuffers | None = None) -> QkNormBuffers:
+    """Launch wm_qk_norm on the current stream: every head of ``q`` [..., Hq, D]
+    and ``k`` [..., Hk, D] (None: queries alone) divided by its root mean
+    square, times gamma_q and gamma_k ([D] float32 or None), and rotated by its
+    row's int32 position.  Returns the filled buffers (q, k)."""
+    head, (pp, pt), bufs = _qk_args(q, k, positions, rotary, gamma_q, gamma_k, bufs, False)
+    _check(load().wm_qk_norm(*head, eps, pp, pt, bufs.q.data_ptr(), bufs.Hq * bufs.D, bufs.k.data_ptr(),
+                             bufs.Hk * bufs.D, _stream()))
+    return bufs
+
+
+def qk_norm_grad(q, k, dq_out, dk_out, positions, rotary: Rotary | None, gamma_q=None, gamma_k=None, eps: float = 1e-6,
+                 bufs: QkNormBuffers | None = None) -> QkNormBuffers:
+    """Launch wm_qk_norm_grad on the current stream: dq, dk, dgamma_q and
+    dgamma_k from the forward call's inputs and the gradients of its outputs."""
+    head, (pp, pt), bufs = _qk_args(q, k, positions, rotary, gamma_q, gamma_k, bufs, True)
+    if bufs.dq is None:
+        raise ValueError("qk_norm_grad needs buffers made with grad=True")
+    n, ldq = _heads("dq_out", dq_out, bufs.Hq, bufs.D, q.dtype, q.device)
+    m, ldk = (n, 0) if k is None else _heads("dk_out", dk_out, bufs.Hk, bufs.D, q.dtype, q.device)
+    if n != bufs.rows or m != bufs.rows:
+        raise ValueError(f"dq_out has {n} rows, dk_out {m}, q has {bufs.rows}")
+    _check(load().wm_qk_norm_grad(*head, eps, pp, pt, dq_out.data_ptr(), ldq, None if k is None else dk_out.data_ptr(), ldk,
+                                  bufs.dq.data_ptr(), bufs.Hq * bufs.D, bufs.dk.data_ptr(), bufs.Hk * bufs.D,
+                                  bufs.dgamma_q.data_ptr(), bufs.dgamma_k.data_ptr(), bufs.workspace.data_ptr(),
+                                  bufs.ws_bytes, _stream()))
+    return bufs
+
+
+class LinattnBuffers:
+    """Output [T, B, N, V], final state [B, N, K, V] and workspace of linear
+    attention; with ``grad`` the gradients (dq, dk and dv contiguous)."""
+
+    def __init__(self, T: int, B: int, N: int, K: int, V: int, dtype=torch.float32, device="cuda", grad: bool = True):
+        self.T, self.B, self.N, self.K, self.V, self.dtype = T, B, N, K, V, dtype
+        lib = load()
+        seq = lambda w: torch.empty((T, B, N, w), dtype=dtype, device=device)  # noqa: E731
+        state = lambda: torch.empty((B, N, K, V), dtype=torch.float32, device=device)  # noqa: E731
+        self.y, self.h_T = seq(V), state()
+        self.dq, self.dk, self.dv, self.dh0 = (seq(K), seq(K), seq(V), state()) if grad else (None,) * 4
+        size = lib.wm_linattn_grad_workspace_bytes if grad else lib.wm_linattn_workspace_bytes
+        self.ws_bytes = max(size(T, B, N, K, V), lib.wm_linattn_workspace_bytes(T, B, N, K, V))
+        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=device)
+
+
+def _steps(name, t, shape, dtype, device):
+    """Checks a [T, B, N, W] tensor whose heads lie one after the other; its
+    strides of steps and rows."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape or t.device != device:
+        _act(name, t, dtype)
+        raise ValueError(f"{name} is {tuple(t.shape)} on {t.device}, expected {tuple(shape)} on {device}")
+    st = t.stride()
+    if (shape[3] > 1 and st[3] != 1) or (shape[2] > 1 and st[2] != shape[3]):
+        raise ValueError(f"{name}'s heads must lie one after the other (strides {st})")
+    return st[0], st[1]
+
+
+def _linattn_args(q, k, v, decay, h0, resets, lengths, bufs, grad):
+    dt = _act("q", q)
+    dev, dtype = q.device, q.dtype
+    _here(dev)
+    if q.dim() != 4 or not isinstance(v, torch.Tensor) or v.dim() != 4:
+        raise ValueError("q, k and v must be [T, B, N, K] and [T, B, N, V]")
+    T, B, N, K = q.shape
+    V = v.shape[3]
+    qt, qb = _steps("q", q, (T, B, N, K), dtype, dev)
+    kt, kb = _steps("k", k, (T, B, N, K), dtype, dev)
+    vt, vb = _steps("v", v, (T, B, N, V), dtype, dev)
+    pd = _arr("decay", decay, torch.float32, (N,), dev)
+    ph = _arr("h0", h0, torch.float32, (B, N, K, V), dev, optional=True)
+    pr = _arr("resets", resets, _mask_dtype(resets), (T, B), dev, optional=True)
+    pl = _arr("lengths", lengths, torch.int32, (B,), dev, optional=True)
+    if bufs is None:
+        bufs = LinattnBuffers(T, B, N, K, V, dtype, dev, grad=grad)
+    if (bufs.T, bufs.B, bufs.N, bufs.K, bufs.V, bufs.dtype) != (T, B, N, K, V, dtype) or bufs.y.device != dev:
+        raise ValueError(f"buffers for T={bufs.T} B={bufs.B} N={bufs.N} K={bufs.K} V={bufs.V} {bufs.dtype} on "
+                         f"{bufs.y.device}; the call has T={T} B={B} N={N} K={K} V={V} {dtype} on {dev}")
+    head = (dt, T, B, N, K, V, q.data_ptr(), qt, qb, k.data_ptr(), kt, kb, v.data_ptr(), vt, vb, pd)
+    return head, (ph, pr, pl), bufs
+
+
+def linattn(q, k, v, decay, scale: float = 1.0, h0=None, resets=None, lengths=None,
+            bufs: LinattnBuffers | None = None) -> LinattnBuffers:
+    """Launch wm_linattn on the current stream: S_t = decay S_{t-1} + k_t v_t^T,
+    y_t = scale S_t^T q_t for every head over ``q``, ``k`` [T, B, N, K] and
+    ``v`` [T, B, N, V] (decay [N] float32; resets [T, B] uint8: the step starts
+    a new trajectory; lengths [B] int32).  Returns the filled buffers (y, h_T)."""
+    head, masks, bufs = _linattn_args(q, k, v, decay, h0, resets, lengths, bufs, False)
+    _check(load().wm_linattn(*head, scale, *masks, bufs.y.data_ptr(), bufs.h_T.data_ptr(), bufs.workspace.data_ptr(),
+                             bufs.ws_bytes, _stream()))
+    return bufs
+
+
+def linattn_grad(q, k, v, decay, dy, scale: float = 1.0, h0=None, dh_T=None, resets=None, lengths=None,
+                 bufs: LinattnBuffers | None = None) -> LinattnBuffers:
+    """Launch wm_linattn_grad on the current stream: dq, dk, dv and dh0 from the
+    forward call's inputs and the gradients of its outputs."""
+    head, masks, bufs = _linattn_args(q, k, v, decay, h0, resets, lengths, bufs, True)
+    if bufs.dq is None:
+        raise ValueError("linattn_grad needs buffers made with grad=True")
+    T, B, N, K, V = bufs.T, bufs.B, bufs.N, bufs.K, bufs.V
+    yt, yb = _steps("dy", dy, (T, B, N, V), q.dtype, q.device)
+    ph = _arr("dh_T", dh_T, torch.float32, (B, N, K, V), q.device, optional=True)
+    _check(load().wm_linattn_grad(*head, scale, *masks, dy.data_ptr(), yt, yb, ph, bufs.dq.data_ptr(), B * N * K, N * K,
+                                  bufs.dk.data_ptr(), B * N * K, N * K, bufs.dv.data_ptr(), B * N * V, N * V,
+                                  bufs.dh0.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
+    return bufs
+
+
+_GLU_ACTS = {"silu": 0, "gelu": 1}
+
+
+class GluBuffers:
+    """Output [rows, F] of the gated projection, and with ``grad`` its two factors
+    before the activation (``pre`` [rows, 2F]), the gradients and the workspace."""
+
+    def __init__(self, rows: int, D: int, F: int, dtype=torch.float32, device="cuda", grad: bool = True):
+        self.rows, self.D, self.F, self.dtype = rows, D, F, dtype
+        new = lambda *s: torch.empty(s, dtype=dtype, device=device)  # noqa: E731
+        self.h = new(rows, F)
+        self.pre, self.dx, self.dW = (new(rows, 2 * F), new(rows, D), new(2 * F, D)) if grad else (None,) * 3
+        self.ws_bytes = load().wm_glu_grad_workspace_bytes(_ACT[dtype], rows, D, F) if grad else 0
+        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=device) if grad else None
+
+
+def _glu_args(x, W, act, bufs):
+    dt = _act("x", x)
+    dev, dtype = x.device, x.dtype
+    _here(dev)
+    if act not in _GLU_ACTS:
+        raise ValueError(f"act is {act!r}, expected one of {sorted(_GLU_ACTS)}")
+    if not isinstance(W, torch.Tensor) or W.dim() != 2 or W.shape[0] % 2 or W.shape[0] == 0:
+        raise ValueError("W must be [2F, D]")
+    F, D = W.shape[0] // 2, W.shape[1]
+    pw = _arr("W", W, dtype, (2 * F, D), dev)
+    rows, ld = _rows("x", x, D, dtype, dev)
+    if bufs is not None and ((bufs.rows, bufs.D, bufs.F, bufs.dtype) != (rows, D, F, dtype) or bufs.h.device != dev):
+        raise ValueError(f"buffers for rows={bufs.rows} D={bufs.D} F={bufs.F} {bufs.dtype} on {bufs.h.device}; the call has "
+                         f"rows={rows} D={D} F={F} {dtype} on {dev}")
+    return (dt, rows, D, F, _GLU_ACTS[act], x.data_ptr(), ld, pw)
+
+
+def glu(x, W, act: str = "silu", bufs: GluBuffers | None = None) -> GluBuffers:
+    """Launch wm_glu on the current stream: act(x W[:F]^T) * (x W[F:]^T) for the
+    rows of ``x`` [..., D] and ``W`` [2F, D]; returns the filled buffers (h, and
+    pre, which glu_grad reads)."""
+    head = _glu_args(x, W, act, bufs)
+    if bufs is None:
+        bufs = GluBuffers(head[1], head[2], head[3], x.dtype, x.device)
+    _check(load().wm_glu(*head, bufs.h.data_ptr(), bufs.F, _ptr(bufs.pre), _stream()))
+    return bufs
+
+
+def glu_grad(x, W, dh, act: str = "silu", bufs: GluBuffers | None = None) -> GluBuffers:
+    """Launch wm_glu_grad on the current stream: dx and dW (in the weights' type)
+    from the forward call's inputs and the factors in its ``bufs``."""
+    head = _glu_args(x, W, act, bufs)
+    if bufs is None or bufs.pre is None:
+        raise ValueError("glu_grad needs the forward call's buffers, made with grad=True")
+    n, ld = _rows("dh", dh, bufs.F, x.dtype, x.device)
+    if n != bufs.rows:
+        raise ValueError(f"dh has {n} rows, x has {bufs.rows}")
+    _check(load().wm_glu_grad(*head, bufs.pre.data_ptr(), dh.data_ptr(), ld, bufs.dx.data_ptr(), bufs.D, bufs.dW.data_ptr(),
+                              bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
+    return bufs
 
 
 def profile_enable(prefix: str | None):

@@ -15,8 +15,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libwm.so")
 SOURCES = ["wm_mdn.hip", "wm_ctrl.hip", "wm_kernels.hip", "wm_persist.hip", "wm_grad.hip", "wm_recur.hip", "wm_returns.hip",
-           "wm_optim.hip", "wm_noalloc.hip", "wm_embed.hip", "wm_norm.hip", "wm_linrec.hip", "wm_clip.hip", "wm_api.cpp", "wm_profile.cpp"]
-HEADERS = ["wm_chain.h", "wm_device.h", "wm_gemm.h", "wm_kernels.h", "wm_layout.h", "wm_profile.h", "wm_seq.h", "wm_split.h",
+           "wm_optim.hip", "wm_noalloc.hip", "wm_embed.hip", "wm_norm.hip", "wm_linrec.hip", "wm_clip.hip", "wm_qknorm.hip", "wm_linattn.hip", "wm_glu.hip", "wm_api.cpp", "wm_profile.cpp"]
+HEADERS = ["wm_attend.h", "wm_chain.h", "wm_device.h", "wm_gemm.h", "wm_kernels.h", "wm_layout.h", "wm_profile.h", "wm_seq.h", "wm_split.h",
            "wm_steps.h"]
 ARCH = "gfx950"
 

@@ -6,12 +6,14 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <string>
 
 #include "../../include/wm.h"
 #include "wm_kernels.h"
+#include "wm_attend.h"
 #include "wm_seq.h"
 
 namespace {
@@ -218,6 +220,59 @@ wm_status check_linrec(int32_t T, int32_t B, int32_t H) {
     return fail(WM_ERR_INVALID_ARG, "T=%d and B=%d must not be negative, H=%d must be positive", T, B, H);
   if ((int64_t)T * B > INT32_MAX || (int64_t)B * H > INT32_MAX)
     return fail(WM_ERR_UNSUPPORTED, "T*B and B*H must stay below 2^31 (T=%d B=%d H=%d)", T, B, H);
+  return WM_OK;
+}
+
+wm_status check_qk(int64_t rows, int32_t Hq, int32_t Hk, int32_t D) {
+  if (rows < 0 || Hq <= 0 || Hk < 0 || D <= 0)
+    return fail(WM_ERR_INVALID_ARG, "rows=%lld and Hk=%d must not be negative, Hq=%d and D=%d must be positive",
+                (long long)rows, Hk, Hq, D);
+  if (Hq > 1024 || Hk > 1024 || D > wm::kQkMaxD)
+    return fail(WM_ERR_UNSUPPORTED, "Hq=%d, Hk=%d, D=%d: at most 1024 heads of %d", Hq, Hk, D, wm::kQkMaxD);
+  if (rows > INT32_MAX / (Hq + Hk)) return fail(WM_ERR_UNSUPPORTED, "rows=%lld: rows (Hq + Hk) above 2^31 - 1", (long long)rows);
+  return WM_OK;
+}
+
+wm_status check_rotation(int32_t D, int32_t R, int32_t neighbours, float eps) {
+  if (R < 0 || R > D || R % 2 != 0) return fail(WM_ERR_INVALID_ARG, "R=%d must be even, 0 .. D=%d", R, D);
+  if (neighbours != 0 && neighbours != 1) return fail(WM_ERR_INVALID_ARG, "neighbours=%d must be 0 or 1", neighbours);
+  if (!(eps >= 0.0f) || !isfinite(eps)) return fail(WM_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  return WM_OK;
+}
+
+wm_status check_linattn(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V) {
+  if (T < 0 || B < 0 || N <= 0 || K <= 0 || V <= 0)
+    return fail(WM_ERR_INVALID_ARG, "T=%d and B=%d must not be negative, N=%d, K=%d and V=%d must be positive", T, B, N, K, V);
+  if (K > wm::kAttnMax || V > wm::kAttnMax) return fail(WM_ERR_UNSUPPORTED, "K=%d, V=%d: at most %d", K, V, wm::kAttnMax);
+  const int64_t lim = INT32_MAX, heads = (int64_t)B * N, wide = std::max(K, V);
+  if ((int64_t)T * B > lim || heads > lim / (K * V) || (T > 0 && heads > lim / wide / T))
+    return fail(WM_ERR_UNSUPPORTED, "T=%d, B=%d, N=%d, K=%d, V=%d: too many values", T, B, N, K, V);
+  return WM_OK;
+}
+
+// A [T, B, N, W] array whose rows hold N W values.
+wm_status check_heads(const char* name, int32_t dtype, const void* p, int64_t t, int64_t b, int32_t T, int32_t B, int64_t row,
+                      bool output) {
+  if (T == 0 || B == 0) return WM_OK;
+  if (!p) return fail(WM_ERR_INVALID_ARG, "%s is required", name);
+  if (!aligned_el(p, dtype)) return fail(WM_ERR_INVALID_ARG, "%s is not aligned to its element", name);
+  const int64_t lim = (int64_t)1 << 48;
+  if (t < 0 || b < 0) return fail(WM_ERR_INVALID_ARG, "%s: strides must not be negative", name);
+  if ((T > 1 && t > lim / T) || (B > 1 && b > lim / B)) return fail(WM_ERR_UNSUPPORTED, "%s: rows too far apart", name);
+  if (output) {
+    const bool steps = T > 1, rows = B > 1;
+    const bool fit = (!rows || b >= row) && (!steps || t >= row) && (!steps || !rows || t >= b * (B - 1) + row || b >= t * (T - 1) + row);
+    if (!fit) return fail(WM_ERR_INVALID_ARG, "%s: rows overlap", name);
+  }
+  return WM_OK;
+}
+
+wm_status check_glu(int64_t rows, int32_t D, int32_t F, int32_t act) {
+  if (rows < 0 || D <= 0 || F <= 0)
+    return fail(WM_ERR_INVALID_ARG, "rows=%lld must not be negative, D=%d and F=%d must be positive", (long long)rows, D, F);
+  if (act != WM_ACT_SILU && act != WM_ACT_GELU) return fail(WM_ERR_INVALID_ARG, "unknown act %d", act);
+  if (D > 65536 || F > 65536 || rows > INT32_MAX || rows > ((int64_t)1 << 43) / F)
+    return fail(WM_ERR_UNSUPPORTED, "rows=%lld, D=%d, F=%d: too large", (long long)rows, D, F);
   return WM_OK;
 }
 
@@ -657,6 +712,199 @@ wm_status wm_clip_grads(int32_t n, const wm_grad_tensor* tensors, float max_norm
     return st;
   const hipError_t e = wm::launch_clip(n, tensors, max_norm, norm, workspace, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "wm_clip_grads");
+  return ok();
+}
+
+wm_status wm_rotary_table(int32_t R, double base, uint64_t* table) {
+  if (R < 0 || R > wm::kQkMaxD || R % 2 != 0) return fail(WM_ERR_INVALID_ARG, "R=%d must be even, 0 .. %d", R, wm::kQkMaxD);
+  if (!(base >= 1.0) || !std::isfinite(base)) return fail(WM_ERR_INVALID_ARG, "base must be finite and >= 1");
+  if (R > 0 && !table) return fail(WM_ERR_INVALID_ARG, "table is required");
+  // 80-bit arithmetic: the fraction is off by less than 2^-63 of a turn a step
+  const long double turn = 6.28318530717958647692528676655900577L;
+  for (int32_t i = 0; i < R / 2; ++i)
+    table[i] = (uint64_t)rintl(ldexpl(powl((long double)base, -2.0L * i / R) / turn, 64));
+  return ok();
+}
+
+wm_status wm_qk_norm(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, int32_t D, int32_t R, int32_t neighbours,
+                     const void* q, int64_t q_ld, const void* k, int64_t k_ld, const float* gamma_q, const float* gamma_k,
+                     float eps, const int32_t* positions, const uint64_t* table, void* q_out, int64_t q_out_ld, void* k_out,
+                     int64_t k_out_ld, wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_qk(rows, Hq, Hk, D)) != WM_OK || (st = check_rotation(D, R, neighbours, eps)) != WM_OK)
+    return st;
+  if (rows == 0) return ok();
+  if ((st = check_ld("q", rows, (int64_t)Hq * D, q_ld)) != WM_OK ||
+      (st = check_ld("q_out", rows, (int64_t)Hq * D, q_out_ld)) != WM_OK ||
+      (Hk > 0 && ((st = check_ld("k", rows, (int64_t)Hk * D, k_ld)) != WM_OK ||
+                  (st = check_ld("k_out", rows, (int64_t)Hk * D, k_out_ld)) != WM_OK)))
+    return st;
+  if (!q || !q_out || (Hk > 0 && (!k || !k_out)) || !positions || (R > 0 && !table))
+    return fail(WM_ERR_INVALID_ARG, "q, k, positions, table, q_out and k_out are required");
+  if (!aligned_el(q, dtype) || !aligned_el(q_out, dtype) || (Hk > 0 && (!aligned_el(k, dtype) || !aligned_el(k_out, dtype))) ||
+      !aligned4(gamma_q) || !aligned4(gamma_k) || !aligned4(positions) || (reinterpret_cast<uintptr_t>(table) & 7u))
+    return fail(WM_ERR_INVALID_ARG, "arrays must be aligned to their elements");
+  const wm::QkArgs a{(long)rows, D, R, neighbours, eps, positions, table,
+                     {{Hq, q, (long)q_ld, gamma_q, nullptr, 0, q_out, (long)q_out_ld, nullptr},
+                      {Hk, k, (long)k_ld, gamma_k, nullptr, 0, k_out, (long)k_out_ld, nullptr}},
+                     nullptr, 0};
+  const hipError_t e = wm::launch_qk_norm(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_qk_norm");
+  return ok();
+}
+
+size_t wm_qk_norm_grad_workspace_bytes(int64_t rows, int32_t Hq, int32_t Hk, int32_t D) {
+  return check_qk(rows, Hq, Hk, D) == WM_OK ? wm::qk_norm_grad_workspace((long)rows, Hq, Hk, D) : 0;
+}
+
+wm_status wm_qk_norm_grad(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, int32_t D, int32_t R, int32_t neighbours,
+                          const void* q, int64_t q_ld, const void* k, int64_t k_ld, const float* gamma_q,
+                          const float* gamma_k, float eps, const int32_t* positions, const uint64_t* table,
+                          const void* grad_q_out, int64_t grad_q_out_ld, const void* grad_k_out, int64_t grad_k_out_ld,
+                          void* grad_q, int64_t grad_q_ld, void* grad_k, int64_t grad_k_ld, float* grad_gamma_q,
+                          float* grad_gamma_k, void* workspace, size_t workspace_bytes, wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_qk(rows, Hq, Hk, D)) != WM_OK || (st = check_rotation(D, R, neighbours, eps)) != WM_OK)
+    return st;
+  if (rows > 0) {
+    if ((st = check_ld("q", rows, (int64_t)Hq * D, q_ld)) != WM_OK ||
+        (st = check_ld("grad_q_out", rows, (int64_t)Hq * D, grad_q_out_ld)) != WM_OK ||
+        (st = check_ld("grad_q", rows, (int64_t)Hq * D, grad_q_ld)) != WM_OK ||
+        (Hk > 0 && ((st = check_ld("k", rows, (int64_t)Hk * D, k_ld)) != WM_OK ||
+                    (st = check_ld("grad_k_out", rows, (int64_t)Hk * D, grad_k_out_ld)) != WM_OK ||
+                    (st = check_ld("grad_k", rows, (int64_t)Hk * D, grad_k_ld)) != WM_OK)))
+      return st;
+    if (!q || !grad_q_out || !grad_q || (Hk > 0 && (!k || !grad_k_out || !grad_k)) || !positions || (R > 0 && !table))
+      return fail(WM_ERR_INVALID_ARG, "q, k, positions, table and the gradients are required");
+  }
+  if (!aligned_el(q, dtype) || !aligned_el(grad_q_out, dtype) || !aligned_el(grad_q, dtype) ||
+      (Hk > 0 && (!aligned_el(k, dtype) || !aligned_el(grad_k_out, dtype) || !aligned_el(grad_k, dtype))) ||
+      !aligned4(gamma_q) || !aligned4(gamma_k) || !aligned4(positions) || !aligned4(grad_gamma_q) || !aligned4(grad_gamma_k) ||
+      (reinterpret_cast<uintptr_t>(table) & 7u))
+    return fail(WM_ERR_INVALID_ARG, "arrays must be aligned to their elements");
+  if ((st = check_workspace("the workspace of wm_qk_norm_grad", workspace, workspace_bytes,
+                            wm::qk_norm_grad_workspace((long)rows, Hq, Hk, D))) != WM_OK)
+    return st;
+  const wm::QkArgs a{(long)rows, D, R, neighbours, eps, positions, table,
+                     {{Hq, q, (long)q_ld, gamma_q, grad_q_out, (long)grad_q_out_ld, grad_q, (long)grad_q_ld, grad_gamma_q},
+                      {Hk, k, (long)k_ld, gamma_k, grad_k_out, (long)grad_k_out_ld, grad_k, (long)grad_k_ld, grad_gamma_k}},
+                     reinterpret_cast<float*>(workspace), 0};
+  const hipError_t e = wm::launch_qk_norm_grad(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_qk_norm_grad");
+  return ok();
+}
+
+size_t wm_linattn_workspace_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V) {
+  return check_linattn(T, B, N, K, V) == WM_OK ? wm::linattn_workspace(T, B, N, K, V) : 0;
+}
+
+size_t wm_linattn_grad_workspace_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V) {
+  return check_linattn(T, B, N, K, V) == WM_OK ? wm::linattn_grad_workspace(T, B, N, K, V) : 0;
+}
+
+wm_status wm_linattn(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, int32_t V, const void* q, int64_t q_t,
+                     int64_t q_b, const void* k, int64_t k_t, int64_t k_b, const void* v, int64_t v_t, int64_t v_b,
+                     const float* decay, float scale, const float* h0, const uint8_t* resets, const int32_t* lengths, void* y,
+                     float* h_T, void* workspace, size_t workspace_bytes, wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_linattn(T, B, N, K, V)) != WM_OK) return st;
+  const int64_t rk = (int64_t)N * K, rv = (int64_t)N * V;
+  if ((st = check_heads("q", dtype, q, q_t, q_b, T, B, rk, false)) != WM_OK ||
+      (st = check_heads("k", dtype, k, k_t, k_b, T, B, rk, false)) != WM_OK ||
+      (st = check_heads("v", dtype, v, v_t, v_b, T, B, rv, false)) != WM_OK ||
+      (st = check_heads("y", dtype, y, B * rv, rv, T, B, rv, true)) != WM_OK)
+    return st;
+  if (!isfinite(scale)) return fail(WM_ERR_INVALID_ARG, "scale must be finite");
+  if (!aligned4(decay) || !aligned4(h0) || !aligned4(lengths) || !aligned4(h_T))
+    return fail(WM_ERR_INVALID_ARG, "decay, h0, lengths and h_T must be 4-byte aligned");
+  if (B == 0) return ok();
+  if (!decay) return fail(WM_ERR_INVALID_ARG, "decay is required");
+  if ((st = check_workspace("the workspace of wm_linattn", workspace, workspace_bytes,
+                            wm::linattn_workspace(T, B, N, K, V))) != WM_OK)
+    return st;
+  const wm::LinattnArgs a{T, B, N, K, V, {q, (long)q_t, (long)q_b}, {k, (long)k_t, (long)k_b}, {v, (long)v_t, (long)v_b},
+                          decay, scale, h0, resets, lengths, y, h_T, workspace};
+  const hipError_t e = wm::launch_linattn(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_linattn");
+  return ok();
+}
+
+wm_status wm_linattn_grad(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, int32_t V, const void* q, int64_t q_t,
+                          int64_t q_b, const void* k, int64_t k_t, int64_t k_b, const void* v, int64_t v_t, int64_t v_b,
+                          const float* decay, float scale, const float* h0, const uint8_t* resets, const int32_t* lengths,
+                          const void* grad_y, int64_t grad_y_t, int64_t grad_y_b, const float* grad_h_T, void* grad_q,
+                          int64_t grad_q_t, int64_t grad_q_b, void* grad_k, int64_t grad_k_t, int64_t grad_k_b, void* grad_v,
+                          int64_t grad_v_t, int64_t grad_v_b, float* grad_h0, void* workspace, size_t workspace_bytes,
+                          wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_linattn(T, B, N, K, V)) != WM_OK) return st;
+  const int64_t rk = (int64_t)N * K, rv = (int64_t)N * V;
+  if ((st = check_heads("q", dtype, q, q_t, q_b, T, B, rk, false)) != WM_OK ||
+      (st = check_heads("k", dtype, k, k_t, k_b, T, B, rk, false)) != WM_OK ||
+      (st = check_heads("v", dtype, v, v_t, v_b, T, B, rv, false)) != WM_OK ||
+      (st = check_heads("grad_y", dtype, grad_y, grad_y_t, grad_y_b, T, B, rv, false)) != WM_OK ||
+      (st = check_heads("grad_q", dtype, grad_q, grad_q_t, grad_q_b, T, B, rk, true)) != WM_OK ||
+      (st = check_heads("grad_k", dtype, grad_k, grad_k_t, grad_k_b, T, B, rk, true)) != WM_OK ||
+      (st = check_heads("grad_v", dtype, grad_v, grad_v_t, grad_v_b, T, B, rv, true)) != WM_OK)
+    return st;
+  if (!isfinite(scale)) return fail(WM_ERR_INVALID_ARG, "scale must be finite");
+  if (!aligned4(decay) || !aligned4(h0) || !aligned4(lengths) || !aligned4(grad_h_T) || !aligned4(grad_h0))
+    return fail(WM_ERR_INVALID_ARG, "decay, h0, lengths, grad_h_T and grad_h0 must be 4-byte aligned");
+  if (B == 0) return ok();
+  if (!decay) return fail(WM_ERR_INVALID_ARG, "decay is required");
+  if ((st = check_workspace("the workspace of wm_linattn_grad", workspace, workspace_bytes,
+                            wm::linattn_grad_workspace(T, B, N, K, V))) != WM_OK)
+    return st;
+  const wm::LinattnGradArgs a{T, B, N, K, V, {q, (long)q_t, (long)q_b}, {k, (long)k_t, (long)k_b}, {v, (long)v_t, (long)v_b},
+                              {grad_y, (long)grad_y_t, (long)grad_y_b}, {grad_q, (long)grad_q_t, (long)grad_q_b},
+                              {grad_k, (long)grad_k_t, (long)grad_k_b}, {grad_v, (long)grad_v_t, (long)grad_v_b},
+                              decay, scale, h0, resets, lengths, grad_h_T, grad_h0, workspace};
+  const hipError_t e = wm::launch_linattn_grad(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_linattn_grad");
+  return ok();
+}
+
+wm_status wm_glu(int32_t dtype, int64_t rows, int32_t D, int32_t F, int32_t act, const void* x, int64_t x_ld, const void* W,
+                 void* h, int64_t h_ld, void* pre, wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_glu(rows, D, F, act)) != WM_OK || (st = check_ld("x", rows, D, x_ld)) != WM_OK ||
+      (st = check_ld("h", rows, F, h_ld)) != WM_OK)
+    return st;
+  if (rows == 0) return ok();
+  if (!x || !W || !h) return fail(WM_ERR_INVALID_ARG, "x, W and h are required");
+  if (!aligned_el(x, dtype) || !aligned_el(W, dtype) || !aligned_el(h, dtype) || !aligned_el(pre, dtype))
+    return fail(WM_ERR_INVALID_ARG, "arrays must be aligned to their elements");
+  const wm::GluArgs a{(long)rows, D, F, act, x, (long)x_ld, W, h, (long)h_ld, pre};
+  const hipError_t e = wm::launch_glu(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_glu");
+  return ok();
+}
+
+size_t wm_glu_grad_workspace_bytes(int32_t dtype, int64_t rows, int32_t D, int32_t F) {
+  return check_dtype(dtype) == WM_OK && check_glu(rows, D, F, WM_ACT_SILU) == WM_OK
+             ? wm::glu_grad_workspace(dtype, (long)rows, D, F)
+             : 0;
+}
+
+wm_status wm_glu_grad(int32_t dtype, int64_t rows, int32_t D, int32_t F, int32_t act, const void* x, int64_t x_ld,
+                      const void* W, const void* pre, const void* grad_h, int64_t grad_h_ld, void* grad_x, int64_t grad_x_ld,
+                      void* grad_W, void* workspace, size_t workspace_bytes, wm_stream_t stream) {
+  wm_status st = check_dtype(dtype);
+  if (st != WM_OK || (st = check_glu(rows, D, F, act)) != WM_OK || (st = check_ld("x", rows, D, x_ld)) != WM_OK ||
+      (st = check_ld("grad_h", rows, F, grad_h_ld)) != WM_OK || (st = check_ld("grad_x", rows, D, grad_x_ld)) != WM_OK)
+    return st;
+  if (rows > 0 && (!x || !W || !pre || !grad_h || !grad_x))
+    return fail(WM_ERR_INVALID_ARG, "x, W, pre, grad_h and grad_x are required");
+  if (!aligned_el(x, dtype) || !aligned_el(W, dtype) || !aligned_el(pre, dtype) || !aligned_el(grad_h, dtype) ||
+      !aligned_el(grad_x, dtype) || !aligned_el(grad_W, dtype))
+    return fail(WM_ERR_INVALID_ARG, "arrays must be aligned to their elements");
+  if ((st = check_workspace("the workspace of wm_glu_grad", workspace, workspace_bytes,
+                            wm::glu_grad_workspace(dtype, (long)rows, D, F))) != WM_OK)
+    return st;
+  const wm::GluGradArgs a{(long)rows, D, F, act, x, (long)x_ld, W, pre, grad_h, (long)grad_h_ld, grad_x, (long)grad_x_ld,
+                          grad_W, workspace};
+  const hipError_t e = wm::launch_glu_grad(dtype, a, reinterpret_cast<hipStream_t>(stream));
+  if (e != hipSuccess) return hip_fail(e, "wm_glu_grad");
   return ok();
 }
 

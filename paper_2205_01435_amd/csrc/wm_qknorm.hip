@@ -1,0 +1,417 @@
+// Norm of every head's queries and keys and their rotation by position, and the
+// gradient:
+//   r = (mean x^2 + eps)^-1/2, y = Rot(x r gamma);
+//   d = Rot^-1 dy, e = d gamma, dx = r (e - x r mean(e x r)), dgamma = sum d x r.
+// Rot turns pair i of a head by the angle pos f_i.
+//
+// The angle as a part of a turn is pos times the table's 64-bit binary fraction,
+// modulo 2^64: exact for every position.  Its nearest quarter turn goes into
+// signs and order, and what is left, at most an eighth of a turn either side, into
+// the Taylor sums of sine and cosine, whose first terms left out are below 2e-9.
+//
+// A lane holds whole pairs of a head: VEC pairs (8 bf16 or 4 fp32), two pieces of
+// 16 bytes, and L lanes hold a head, so that the rotation needs no other lane and
+// the sum goes over L lanes.  It computes its pairs' sines and cosines once for a
+// step and goes through the step's heads with them; where there are few steps the
+// heads are dealt to several lane groups.  Heads whose pairs do not come in whole
+// pieces go the same way, value by value.  The gradient keeps the sums for both
+// gammas in registers; a work-group leaves one row of partial sums, which a second
+// launch adds in order.
+//
+// Bound by memory.
+#include <algorithm>
+
+#include "../../include/wm.h"
+#include "wm_attend.h"
+#include "wm_profile.h"
+
+namespace wm {
+namespace {
+
+constexpr int kThreads = 256;
+
+typedef uint32_t __attribute__((ext_vector_type(4))) v4u;
+typedef v4u __attribute__((aligned(2))) v4u_2;
+typedef v4u __attribute__((aligned(4))) v4u_4;
+
+template <typename DT> struct Io;
+template <> struct Io<float> {
+  static constexpr int VEC = 4;
+  typedef v4u_4 mem;
+  __device__ static void get(v4u r, float* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
+  }
+  __device__ static v4u put(const float* v) {
+    return v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  }
+};
+template <> struct Io<bf16_t> {
+  static constexpr int VEC = 8;
+  typedef v4u_2 mem;
+  __device__ static void get(v4u r, float* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(r[i] << 16);
+      v[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+    }
+  }
+  __device__ static v4u put(const float* v) {
+    return v4u{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+  }
+};
+
+// The pairs of a head: pair p has the values at first(p) and second(p); those
+// from R / 2 on are not rotated, and the last may lack its second value.
+struct Pairs {
+  int D, R, rest;  // rest: pairs that are not rotated
+  bool neighbours;
+  __device__ Pairs(const QkArgs& a) : D(a.D), R(a.R), rest((a.D - a.R + 1) / 2), neighbours(a.neighbours != 0) {}
+  __device__ int count() const { return R / 2 + rest; }
+  __device__ int first(int p) const { return neighbours ? 2 * p : p < R / 2 ? p : R / 2 + p; }
+  __device__ int second(int p) const { return neighbours ? 2 * p + 1 : p < R / 2 ? p + R / 2 : R / 2 + p + rest; }
+};
+
+// (cos, sin) of a part of a turn, a 64-bit binary fraction.
+__device__ __forceinline__ float2 cos_sin(uint64_t turn) {
+  const uint32_t t = (uint32_t)(turn >> 32), quarter = (t + 0x20000000u) >> 30;
+  const float x = (float)(int)(t - (quarter << 30)) * 1.4629180792671596e-9f;  // 2 pi 2^-32
+  const float z = x * x;
+  const float s = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 2.7557319224e-6f, -1.9841269841e-4f), 8.3333333333e-3f), -1.6666666667e-1f), x);
+  const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -2.7557319224e-7f, 2.4801587302e-5f), -1.3888888889e-3f), 4.1666666667e-2f), -0.5f), 1.0f);
+  const float a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;
+  return make_float2(quarter == 1 || quarter == 2 ? -a : a, quarter & 2 ? -b : b);
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_plus(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// Sum over L neighbouring lanes, in every one of them.
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+  if constexpr (L >= 2) v = dpp_plus<0xB1>(v);   // quad_perm 1 0 3 2
+  if constexpr (L >= 4) v = dpp_plus<0x4E>(v);   // quad_perm 2 3 0 1
+  if constexpr (L >= 8) v = dpp_plus<0x141>(v);  // row_half_mirror
+  if constexpr (L >= 16) v = dpp_plus<0x140>(v); // row_mirror
+  if constexpr (L >= 32) v += __shfl_xor(v, 16);
+  if constexpr (L >= 64) v += __shfl_xor(v, 32);
+  return v;
+}
+
+// A lane's pairs of a head, v[0] and v[1] their first and second values.
+template <typename DT, bool WHOLE>
+struct Lane {
+  static constexpr int V = Io<DT>::VEC;
+  int at[2];  // WHOLE: where the two pieces start
+  int p0;
+  bool any;
+  __device__ Lane(const Pairs& p, int lane) : p0(lane * V), any(lane * V < p.count()) {
+    const int i = any ? p0 : 0;
+    at[0] = p.first(i);
+    at[1] = p.neighbours ? at[0] + V : p.second(i);
+  }
+  __device__ void load(v4u (&r)[2], const Pairs& p, const DT* x) const {
+    if constexpr (WHOLE) {
+      r[0] = *reinterpret_cast<const typename Io<DT>::mem*>(x + at[0]);
+      r[1] = *reinterpret_cast<const typename Io<DT>::mem*>(x + at[1]);
+    } else {
+      float v[2][V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int q = p0 + i, f = p.first(q), s = p.second(q);
+        v[0][i] = q < p.count() ? DType<DT>::load(x, f) : 0.0f;
+        v[1][i] = q < p.count() && s < p.D ? DType<DT>::load(x, s) : 0.0f;
+      }
+      r[0] = Io<DT>::put(v[0]);
+      r[1] = Io<DT>::put(v[1]);
+    }
+  }
+  // the pieces as pairs
+  __device__ void get(const v4u (&r)[2], const Pairs& p, float (&v)[2][V]) const {
+    Io<DT>::get(r[0], v[0]);
+    Io<DT>::get(r[1], v[1]);
+    if (WHOLE && p.neighbours) swap_order<true>(v);
+    if (!any) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[0][i] = v[1][i] = 0.0f;
+    }
+  }
+  // 2 V values in memory order, as V first and V second ones, and back
+  template <bool TO>
+  __device__ static void swap_order(float (&v)[2][V]) {
+    float w[2 * V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if (TO) {
+        w[2 * i] = v[2 * i / V][2 * i % V];
+        w[2 * i + 1] = v[(2 * i + 1) / V][(2 * i + 1) % V];
+      } else {
+        w[2 * i] = v[0][i];
+        w[2 * i + 1] = v[1][i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      v[0][i] = TO ? w[2 * i] : w[i];
+      v[1][i] = TO ? w[2 * i + 1] : w[V + i];
+    }
+  }
+  __device__ void store(DT* x, const Pairs& p, float (&v)[2][V]) const {
+    if (!any) return;
+    if constexpr (WHOLE) {
+      if (p.neighbours) swap_order<false>(v);
+      *reinterpret_cast<typename Io<DT>::mem*>(x + at[0]) = Io<DT>::put(v[0]);
+      *reinterpret_cast<typename Io<DT>::mem*>(x + at[1]) = Io<DT>::put(v[1]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int q = p0 + i, s = p.second(q);
+        if (q < p.count()) DType<DT>::store(x, p.first(q), v[0][i]);
+        if (q < p.count() && s < p.D) DType<DT>::store(x, s, v[1][i]);
+      }
+    }
+  }
+  // the lane's values of a [D] array (1 without one, 0 where there is no value)
+  __device__ void columns(float (&g)[2][V], const Pairs& p, const float* a) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int q = p0 + i, f = p.first(q), s = p.second(q);
+      g[0][i] = q < p.count() ? (a ? a[f] : 1.0f) : 0.0f;
+      g[1][i] = q < p.count() && s < p.D ? (a ? a[s] : 1.0f) : 0.0f;
+    }
+  }
+  __device__ void angles(float (&c)[V], float (&s)[V], const Pairs& p, const QkArgs& a, long row) const {
+    const uint64_t pos = (uint64_t)(int64_t)a.pos[row];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int q = p0 + i;
+      const float2 t = q < p.R / 2 ? cos_sin(pos * a.table[q]) : make_float2(1.0f, 0.0f);
+      c[i] = t.x;
+      s[i] = t.y;
+    }
+  }
+};
+
+// An item is `group` heads of one step; heads count through queries, then keys.
+template <typename DT, int L, bool WHOLE>
+__global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
+  constexpr int V = Io<DT>::VEC, kSlots = kThreads / L;
+  const Pairs p(a);
+  const Lane<DT, WHOLE> lane(p, threadIdx.x % L);
+  const int heads = a.side[0].heads + a.side[1].heads, parts = (heads + a.group - 1) / a.group;
+  const long item = (long)blockIdx.x * kSlots + threadIdx.x / L;
+  const long row = item / parts;
+  if (row >= a.rows) return;
+  const int h0 = (int)(item % parts) * a.group, h1 = min(h0 + a.group, heads);
+  auto in = [&](int h) {
+    const int w = h >= a.side[0].heads;
+    return reinterpret_cast<const DT*>(a.side[w].x) + row * a.side[w].x_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D;
+  };
+  v4u next[2];
+  lane.load(next, p, in(h0));
+  float c[V], s[V], g[2][V];
+  lane.angles(c, s, p, a, row);
+  const float inv = 1.0f / (float)a.D;
+  int held = -1;
+  for (int h = h0; h < h1; ++h) {
+    const int w = h >= a.side[0].heads;
+    if (w != held) lane.columns(g, p, a.side[held = w].gamma);
+    float v[2][V];
+    lane.get(next, p, v);
+    if (h + 1 < h1) lane.load(next, p, in(h + 1));
+    float m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) m = fmaf(v[0][i], v[0][i], fmaf(v[1][i], v[1][i], m));
+    const float r = 1.0f / sqrtf(group_sum<L>(m) * inv + a.eps);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float x0 = v[0][i] * r * g[0][i], x1 = v[1][i] * r * g[1][i];
+      v[0][i] = fmaf(x0, c[i], -(x1 * s[i]));
+      v[1][i] = fmaf(x0, s[i], x1 * c[i]);
+    }
+    lane.store(reinterpret_cast<DT*>(a.side[w].out) + row * a.side[w].out_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D, p, v);
+  }
+}
+
+// part [gridDim.x][2][D]: this work-group's sums for the gammas of queries and keys.
+template <typename DT, int L, bool WHOLE>
+__global__ void __launch_bounds__(kThreads) k_qk_norm_grad(const QkArgs a) {
+  constexpr int V = Io<DT>::VEC, kSlots = kThreads / L;
+  __shared__ float add[2 * V][kThreads + 1];
+  const Pairs p(a);
+  const Lane<DT, WHOLE> lane(p, threadIdx.x % L);
+  const int heads = a.side[0].heads + a.side[1].heads, parts = (heads + a.group - 1) / a.group;
+  const float inv = 1.0f / (float)a.D;
+  float dg[2][2][V];
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int i = 0; i < V; ++i) dg[w][0][i] = dg[w][1][i] = 0.0f;
+  for (long item = (long)blockIdx.x * kSlots + threadIdx.x / L; item < a.rows * parts; item += (long)gridDim.x * kSlots) {
+    const long row = item / parts;
+    const int h0 = (int)(item % parts) * a.group, h1 = min(h0 + a.group, heads);
+    float c[V], s[V];
+    lane.angles(c, s, p, a, row);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const QkSide& side = a.side[w];
+      const int off = w ? a.side[0].heads : 0, lo = max(h0 - off, 0), hi = min(h1 - off, side.heads);
+      if (lo >= hi) continue;
+      const DT* x = reinterpret_cast<const DT*>(side.x) + row * side.x_ld;
+      const DT* dy = reinterpret_cast<const DT*>(side.dout) + row * side.dout_ld;
+      DT* out = reinterpret_cast<DT*>(side.out) + row * side.out_ld;
+      float g[2][V];
+      lane.columns(g, p, side.gamma);
+      v4u nx[2], nd[2];
+      lane.load(nx, p, x + (long)lo * a.D);
+      lane.load(nd, p, dy + (long)lo * a.D);
+      for (int h = lo; h < hi; ++h) {
+        float v[2][V], d[2][V];
+        lane.get(nx, p, v);
+        lane.get(nd, p, d);
+        if (h + 1 < hi) {
+          lane.load(nx, p, x + (long)(h + 1) * a.D);
+          lane.load(nd, p, dy + (long)(h + 1) * a.D);
+        }
+        float m = 0.0f, ex = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float d0 = fmaf(d[0][i], c[i], d[1][i] * s[i]), d1 = fmaf(d[1][i], c[i], -(d[0][i] * s[i]));
+          d[0][i] = d0;
+          d[1][i] = d1;
+          m = fmaf(v[0][i], v[0][i], fmaf(v[1][i], v[1][i], m));
+          ex = fmaf(d0 * g[0][i], v[0][i], fmaf(d1 * g[1][i], v[1][i], ex));
+        }
+        const float r = 1.0f / sqrtf(group_sum<L>(m) * inv + a.eps), k = group_sum<L>(ex) * inv * r * r;
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+            dg[w][j][i] = fmaf(d[j][i], v[j][i] * r, dg[w][j][i]);
+            v[j][i] = r * (d[j][i] * g[j][i] - v[j][i] * k);
+          }
+        lane.store(out + (long)h * a.D, p, v);
+      }
+    }
+  }
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    float* const part = gridDim.x > 1 ? a.part + ((long)blockIdx.x * 2 + w) * a.D : a.side[w].dgamma;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      add[i][threadIdx.x] = dg[w][0][i];
+      add[V + i][threadIdx.x] = dg[w][1][i];
+    }
+    __syncthreads();
+    if (!part) continue;
+    // one column a thread, its slots in order
+    for (int j = threadIdx.x; j < 2 * V * L; j += kThreads) {
+      const int l = j / (2 * V), i = j % (2 * V), q = l * V + i % V;
+      const int col = i < V ? p.first(q) : p.second(q);
+      if (q >= p.count() || col >= a.D) continue;
+      float t = 0.0f;
+#pragma unroll 8
+      for (int k = 0; k < kSlots; ++k) t += add[i][k * L + l];
+      part[col] = t;
+    }
+  }
+}
+
+// Adds the n rows of partial sums: 16 columns a work-group, 16 rows at a time,
+// each in its own order, then these.
+__global__ void __launch_bounds__(kThreads) k_qk_norm_sum(const QkArgs a, int n) {
+  __shared__ float sh[16][17];
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, j = blockIdx.x * 16 + c;
+  float s = 0.0f;
+  if (j < 2 * a.D) {
+    const float* p = a.part + j;
+#pragma unroll 8
+    for (int i = r; i < n; i += 16) s += p[(long)i * 2 * a.D];
+  }
+  sh[r][c] = s;
+  __syncthreads();
+  if (r > 0 || j >= 2 * a.D) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) s += sh[i][c];
+  float* out = j < a.D ? a.side[0].dgamma : a.side[1].dgamma;
+  if (out) out[j < a.D ? j : j - a.D] = s;
+}
+
+// Lanes of a head.
+int lanes(int D, int R, int V) {
+  const int pairs = R / 2 + (D - R + 1) / 2;
+  int l = 1;
+  while (l * V < pairs) l *= 2;
+  return l;
+}
+bool whole(const QkArgs& a, int V) {
+  return a.neighbours ? a.D % (2 * V) == 0 : a.R % (2 * V) == 0 && (a.D - a.R) % (2 * V) == 0;
+}
+// Heads of one item: all of a step's, or fewer where that gives fewer than `most`
+// lane groups.
+int heads_of_item(long rows, int heads, long most) {
+  long parts = std::min<long>(heads, std::max<long>(1, most / std::max<long>(rows, 1)));
+  return (int)((heads + parts - 1) / parts);
+}
+int grad_groups(long rows, int heads, int L, int group) {
+  const long items = rows * ((heads + group - 1) / group), slots = kThreads / L;
+  return (int)std::max<long>(1, std::min<long>((items + slots - 1) / slots, 1024));
+}
+
+template <int N> using Const = std::integral_constant<int, N>;
+template <typename DT, typename F>
+hipError_t by_lanes(const QkArgs& a, F f) {
+  const bool w = whole(a, Io<DT>::VEC);
+  auto go = [&](auto l) { return w ? f(l, std::true_type()) : f(l, std::false_type()); };
+  switch (lanes(a.D, a.R, Io<DT>::VEC)) {
+    case 1: return go(Const<1>());
+    case 2: return go(Const<2>());
+    case 4: return go(Const<4>());
+    case 8: return go(Const<8>());
+    case 16: return go(Const<16>());
+    case 32: return go(Const<32>());
+    default: return go(Const<64>());
+  }
+}
+constexpr long kItems = 16384;  // lane groups that fill the device
+
+}  // namespace
+
+hipError_t launch_qk_norm(int dtype, const QkArgs& args, hipStream_t s) {
+  QkArgs a = args;
+  const int heads = a.side[0].heads + a.side[1].heads;
+  a.group = heads_of_item(a.rows, heads, kItems);
+  auto run = [&](auto dt) {
+    typedef decltype(dt) DT;
+    return by_lanes<DT>(a, [&](auto l, auto w) {
+      const long items = a.rows * ((heads + a.group - 1) / a.group), slots = kThreads / l;
+      return launch("qk_norm", k_qk_norm<DT, l, w>, dim3((unsigned)((items + slots - 1) / slots)), dim3(kThreads), 0, s, a);
+    });
+  };
+  return dtype == WM_FP32 ? run(0.0f) : run(bf16_t());
+}
+
+size_t qk_norm_grad_workspace(long rows, int Hq, int Hk, int D) {
+  (void)rows, (void)Hq, (void)Hk;
+  return (size_t)1024 * 2 * D * sizeof(float);
+}
+
+hipError_t launch_qk_norm_grad(int dtype, const QkArgs& args, hipStream_t s) {
+  QkArgs a = args;
+  const int heads = a.side[0].heads + a.side[1].heads;
+  a.group = heads_of_item(a.rows, heads, kItems);
+  const int n = grad_groups(a.rows, heads, lanes(a.D, a.R, dtype == WM_FP32 ? 4 : 8), a.group);
+  auto run = [&](auto dt) {
+    typedef decltype(dt) DT;
+    return by_lanes<DT>(a, [&](auto l, auto w) {
+      return launch("qk_norm_grad", k_qk_norm_grad<DT, l, w>, dim3(n), dim3(kThreads), 0, s, a);
+    });
+  };
+  const hipError_t e = dtype == WM_FP32 ? run(0.0f) : run(bf16_t());
+  if (e != hipSuccess || n == 1) return e;
+  return launch("qk_norm_sum", k_qk_norm_sum, dim3((unsigned)((2 * a.D + 15) / 16)), dim3(kThreads), 0, s, a, n);
+}
+
+}  // namespace wm
