@@ -33,11 +33,11 @@ typedef v2u __attribute__((aligned(2))) v2u_2;
 
 template <typename DT> struct El;
 template <> struct El<float> {
-  static constexpr int VEC = 4, BK = 32, SL = 16;  // SL: k of one 16-byte piece of a fragment for each lane group
+  static constexpr int VEC = 4, BK = 32;
   typedef v4u_4 mem;
 };
 template <> struct El<bf16_t> {
-  static constexpr int VEC = 8, BK = 64, SL = 32;
+  static constexpr int VEC = 8, BK = 64;
   typedef v4u_2 mem;
 };
 
@@ -70,15 +70,35 @@ struct Operand {
   long ld;
 };
 
+// How a tile lies in LDS: in the operands' type, or, SPLIT, fp32 values as three
+// planes of bf16 terms (wm_split.h).
+template <typename DT, bool SPLIT> struct Kind;
+template <> struct Kind<bf16_t, false> {
+  typedef bf16_t T;
+  static constexpr int PLANES = 1, SL = 32, ALONG = 16, ACROSS = 16;  // SL: k of a fragment; what pads a row
+  typedef uint4 Frag;
+};
+template <> struct Kind<float, false> {
+  typedef float T;
+  static constexpr int SL = 16, ALONG = 4, ACROSS = 8, PLANES [[maybe_unused]] = 1;
+  typedef uint4 Frag;
+};
+template <> struct Kind<float, true> {
+  typedef bf16_t T;
+  static constexpr int PLANES = 3, SL = 32, ALONG = 8, ACROSS = 16;
+  typedef Split3 Frag;
+};
+
 // A tile's 128 outputs x BK of one operand, from memory through registers into LDS.
 template <typename DT, bool ACROSS>
 struct Stage {
   static constexpr int V = El<DT>::VEC, BK = El<DT>::BK;
-  // pitches: rows of 16 neighbouring outputs (four of k) on different banks
-  static constexpr int PITCH = ACROSS ? kTile + 32 / (int)sizeof(DT) : BK + (sizeof(DT) == 2 ? 16 : 4);
   static constexpr int ROWS = ACROSS ? BK : kTile, COLS = ACROSS ? kTile : BK;
   static constexpr int N = ROWS * (COLS / V) / kThreads;
-  static constexpr int SIZE = ROWS * PITCH;
+  template <bool SPLIT>
+  static constexpr int pitch() { return COLS + (ACROSS ? Kind<DT, SPLIT>::ACROSS : Kind<DT, SPLIT>::ALONG); }
+  template <bool SPLIT>
+  static constexpr int bytes() { return Kind<DT, SPLIT>::PLANES * ROWS * pitch<SPLIT>() * (int)sizeof(typename Kind<DT, SPLIT>::T); }
   v4u r[N];
   // outputs [o0, o0 + 128) of `outs`, k [k0, k0 + BK) up to kend; `split` rows of the
   // tile on, outputs count from o1 (the other factor's columns)
@@ -96,26 +116,56 @@ struct Stage {
       }
     }
   }
-  __device__ __forceinline__ void store(DT* lds) const {
+  template <bool SPLIT>
+  __device__ __forceinline__ void store(char* lds) const {
+    typedef typename Kind<DT, SPLIT>::T T;
+    T* const t = reinterpret_cast<T*>(lds);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int q = threadIdx.x + i * kThreads;
-      *reinterpret_cast<v4u*>(lds + q / (COLS / V) * PITCH + q % (COLS / V) * V) = r[i];
+      T* const p = t + q / (COLS / V) * pitch<SPLIT>() + q % (COLS / V) * V;
+      if constexpr (SPLIT) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(r[i][e]);
+        constexpr int plane = ROWS * pitch<SPLIT>();
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          const v2u h = {pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3])};
+          *reinterpret_cast<v2u*>(p + k * plane) = h;
+          x[0] -= __uint_as_float(h.x << 16);
+          x[1] -= __uint_as_float(h.x & 0xffff0000u);
+          x[2] -= __uint_as_float(h.y << 16);
+          x[3] -= __uint_as_float(h.y & 0xffff0000u);
+        }
+      } else {
+        *reinterpret_cast<v4u*>(p) = r[i];
+      }
     }
   }
   // the fragment of sixteen outputs from o on, k from k on
-  __device__ __forceinline__ static uint4 frag(const DT* lds, int o, int k) {
+  template <bool SPLIT>
+  __device__ __forceinline__ static typename Kind<DT, SPLIT>::Frag frag(const char* lds, int o, int k) {
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
-    if constexpr (!ACROSS) {
-      return *reinterpret_cast<const uint4*>(lds + (o + j) * PITCH + k + V * g);
-    } else if constexpr (sizeof(DT) == 4) {
-      const float* p = lds + (k + 4 * g) * PITCH + o + j;
-      return make_uint4(__float_as_uint(p[0]), __float_as_uint(p[PITCH]), __float_as_uint(p[2 * PITCH]),
-                        __float_as_uint(p[3 * PITCH]));
+    constexpr int P = pitch<SPLIT>();
+    if constexpr (sizeof(typename Kind<DT, SPLIT>::T) == 4) {
+      const float* const t = reinterpret_cast<const float*>(lds);
+      if constexpr (!ACROSS) return *reinterpret_cast<const uint4*>(t + (o + j) * P + k + 4 * g);
+      const float* const p = t + (k + 4 * g) * P + o + j;
+      return make_uint4(__float_as_uint(p[0]), __float_as_uint(p[P]), __float_as_uint(p[2 * P]), __float_as_uint(p[3 * P]));
     } else {
-      const bf16_t* p = lds + (k + 8 * g + j / 4) * PITCH + o + 4 * (j % 4);
-      const v2u a = read_tr(p), b = read_tr(p + 4 * PITCH);
-      return make_uint4(a.x, a.y, b.x, b.y);
+      const bf16_t* const t = reinterpret_cast<const bf16_t*>(lds);
+      auto one = [&](int plane) {
+        const bf16_t* const q = t + plane * ROWS * P;
+        if constexpr (!ACROSS) return *reinterpret_cast<const uint4*>(q + (o + j) * P + k + 8 * g);
+        const bf16_t* const p = q + (k + 8 * g + j / 4) * P + o + 4 * (j % 4);
+        const v2u a = read_tr(p), b = read_tr(p + 4 * P);
+        return make_uint4(a.x, a.y, b.x, b.y);
+      };
+      if constexpr (SPLIT)
+        return Split3{__builtin_bit_cast(bf16x8, one(0)), __builtin_bit_cast(bf16x8, one(1)), __builtin_bit_cast(bf16x8, one(2))};
+      else
+        return one(0);
     }
   }
 };
@@ -156,55 +206,112 @@ struct ProductArgs {
   float* part;      // splits > 1: [splits][M][N]
   int splits;
   long per;         // k of a split, a multiple of BK
-  int tiles_n;
+  long tiles_m, tiles_n;
 };
 
+// Outputs n .. n + 3 of row m (GLU: `gate` and `up` of its columns).
+template <typename DT>
+__device__ __forceinline__ void put_glu(const ProductArgs& a, long m, long n, f32x4 gate, f32x4 up) {
+  float h[4], g[4], u[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    g[e] = gate[e];
+    u[e] = up[e];
+    h[e] = activate(a.act, g[e]).x * u[e];
+  }
+  store4(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, h);
+  if (a.pre) {
+    DT* pre = reinterpret_cast<DT*>(a.pre) + m * 2 * a.N;
+    store4(pre, n, a.N, g);
+    store4(pre + a.N, n, a.N, u);
+  }
+}
+template <typename DT>
+__device__ __forceinline__ void put(const ProductArgs& a, int split, long m, long n, f32x4 acc) {
+  const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
+  if (a.splits > 1)
+    store4(a.part + ((long)split * a.M + m) * a.N, n, a.N, v);
+  else
+    store4(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, v);
+}
+
+// Any sizes, strides and alignments: tiles of 128 x 128, four waves of 64 x 64,
+// the next k's pieces on their way in registers.
 template <typename DT, bool PX, bool QX, bool GLU>
-__global__ void __launch_bounds__(kThreads) k_product(const ProductArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) k_product(const ProductArgs a) {
   typedef Stage<DT, PX> SP;
   typedef Stage<DT, QX> SQ;
-  constexpr int BK = El<DT>::BK, SL = El<DT>::SL;
-  __shared__ __align__(16) DT pl[SP::SIZE];
-  __shared__ __align__(16) DT ql[SQ::SIZE];
+  constexpr int BK = El<DT>::BK;
+  constexpr bool F32 = sizeof(DT) == 4;
+  constexpr int PB = SP::template bytes<F32>(), QB = SQ::template bytes<F32>();
+  __shared__ __align__(16) char lds[PB + QB];
+  char *const pl = lds, *const ql = lds + PB;
   const int w = threadIdx.x >> 6, wp = w & 1, wq = w >> 1, lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
   const long tile = blockIdx.x / a.splits;
   const int split = (int)(blockIdx.x % a.splits);
   const long n0 = tile % a.tiles_n * (GLU ? kTile / 2 : kTile), m0 = tile / a.tiles_n * kTile;
   const long k0 = split * a.per, k1 = min(k0 + a.per, a.K);
 
-  f32x4 acc[4][4];  // [block of P][block of Q]
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  f32x4 acc[4][4];  // [block of Q][block of P]
   // where this wave's blocks of P start in the tile: half a tile together, or 32 outputs of both factors
   auto block = [&](int i) { return GLU ? 64 * (i >> 1) + 32 * wp + 16 * (i & 1) : 64 * wp + 16 * i; };
-
+  const int half = GLU ? kTile / 2 : kTile;
   SP sp;
   SQ sq;
-  const int half = GLU ? kTile / 2 : kTile;
-  sp.load(a.P, n0, a.N + n0, half, a.N, k0, k1);
-  sq.load(a.Q, m0, 0, kTile, a.M, k0, k1);
-  for (long k = k0; k < k1; k += BK) {
-    __syncthreads();
-    sp.store(pl);
-    sq.store(ql);
-    __syncthreads();
-    if (k + BK < k1) {
-      sp.load(a.P, n0, a.N + n0, half, a.N, k + BK, k1);
-      sq.load(a.Q, m0, 0, kTile, a.M, k + BK, k1);
+  // sums of the wave's blocks of Q from l0 on
+  auto run = [&](auto split_terms, auto& acc, int l0) {
+    constexpr bool SPLIT = decltype(split_terms)::value;
+    constexpr int L = sizeof(acc) / sizeof(acc[0]);
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    sp.load(a.P, n0, a.N + n0, half, a.N, k0, k1);
+    sq.load(a.Q, m0, 0, kTile, a.M, k0, k1);
+    for (long k = k0; k < k1; k += BK) {
+      __syncthreads();
+      sp.template store<SPLIT>(pl);
+      sq.template store<SPLIT>(ql);
+      __syncthreads();
+      if (k + BK < k1) {
+        sp.load(a.P, n0, a.N + n0, half, a.N, k + BK, k1);
+        sq.load(a.Q, m0, 0, kTile, a.M, k + BK, k1);
+      }
+#pragma unroll
+      for (int s = 0; s < BK; s += Kind<DT, SPLIT>::SL) {
+        typename Kind<DT, SPLIT>::Frag p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = SP::template frag<SPLIT>(pl, block(i), s);
+#pragma unroll
+        for (int l = 0; l < L; ++l) {
+          const auto q = SQ::template frag<SPLIT>(ql, 64 * wq + 16 * (l0 + l), s);
+          if constexpr (SPLIT) {
+            mfma_split(acc[l], p, q);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) Mfma<DT>::step(acc[l][i], p[i], q);
+          }
+        }
+      }
     }
+  };
+  run(std::integral_constant<bool, F32>(), acc, 0);
+  if constexpr (F32) {
+    // An infinity, or a value that rounds to one in bf16, leaves NaN in the sums that
+    // it enters: these are taken again on the fp32 unit, a block of Q at a time.
+    bool bad = false;
 #pragma unroll
-    for (int s = 0; s < BK; s += SL) {
-      uint4 p[4], q[4];
+    for (int l = 0; l < 4; ++l)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = SP::frag(pl, block(i), s);
+      for (int i = 0; i < 4; ++i) bad |= any_nan(acc[l][i]);
+    if (__syncthreads_or(bad)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) q[i] = SQ::frag(ql, 64 * wq + 16 * i, s);
+      for (int l = 0; l < 4; ++l) {
+        f32x4 again[1][4];
+        run(std::false_type(), again, l);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int l = 0; l < 4; ++l) Mfma<DT>::step(acc[i][l], p[i], q[l]);
+        for (int i = 0; i < 4; ++i) acc[l][i] = nan_to(acc[l][i], again[0][i]);
+      }
     }
   }
 
@@ -214,34 +321,144 @@ __global__ void __launch_bounds__(kThreads) k_product(const ProductArgs a) {
     if (m >= a.M) continue;
     if constexpr (GLU) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const long n = n0 + 32 * wp + 16 * i + 4 * g;
-        float gate[4], up[4], h[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          gate[e] = acc[i][l][e];
-          up[e] = acc[i + 2][l][e];
-          h[e] = activate(a.act, gate[e]).x * up[e];
-        }
-        store4(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, h);
-        if (a.pre) {
-          DT* pre = reinterpret_cast<DT*>(a.pre) + m * 2 * a.N;
-          store4(pre, n, a.N, gate);
-          store4(pre + a.N, n, a.N, up);
-        }
-      }
+      for (int i = 0; i < 2; ++i) put_glu<DT>(a, m, n0 + 32 * wp + 16 * i + 4 * g, acc[l][i], acc[l][i + 2]);
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const long n = n0 + block(i) + 4 * g;
-        float v[4];
+      for (int i = 0; i < 4; ++i) put<DT>(a, split, m, n0 + block(i) + 4 * g, acc[l][i]);
+    }
+  }
+}
+
+// bf16 with rows on 16-byte boundaries: tiles of 256 x 256, eight waves of 128 x 64,
+// k 64 at a time straight from memory into one of two buffers in LDS while the
+// other is multiplied.  A wave's load is 1 KB in a row, so that padding cannot keep
+// rows apart; the order of a row's 16-byte pieces is changed instead, by the row's
+// number, so that the lanes of one read find different banks.
+constexpr int kBig = 256, kBigThreads = 512, kBigK = 64, kBigBytes = kBig * kBigK * 2;
+__device__ __forceinline__ int turn_along(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ int turn_across(int row) { return ((row & 3) | ((row >> 1) & 4)) << 1; }
+
+template <bool ACROSS, bool GLU>
+struct Direct {
+  // per lane: where its piece of each of this wave's four loads lies
+  uint32_t off[4];
+  int k[4];  // its first k in the step
+  const bf16_t* base;
+  uint32_t bytes;
+  long ld;
+  // outputs [o0, o0 + 256) of `outs`; GLU: 128 of each factor
+  __device__ __forceinline__ Direct(const Operand& a, long o0, long outs, long K, int wave, int lane) : ld(a.ld) {
+    const bf16_t* p = reinterpret_cast<const bf16_t*>(a.p);
+    if constexpr (ACROSS) {
+      base = p + o0;
+      bytes = (uint32_t)(min(outs - o0, (long)kBig) * 2);  // of the last row
+    } else if constexpr (GLU) {
+      base = p;
+      bytes = (uint32_t)((2 * outs - 1) * ld + K) * 2;
+    } else {
+      base = p + o0 * ld;
+      bytes = (uint32_t)(((min(outs - o0, (long)kBig) - 1) * ld + K) * 2);
+    }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = acc[i][l][e];
-        if (a.splits > 1)
-          store4(a.part + ((long)split * a.M + m) * a.N, n, a.N, v);
-        else
-          store4(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, v);
+    for (int t = 0; t < 4; ++t) {
+      const int q = 4 * wave + t;
+      if constexpr (ACROSS) {
+        const int row = 2 * q + (lane >> 5), c = (lane & 31) ^ turn_across(row);
+        off[t] = (uint32_t)((row * ld + 8 * c) * 2);
+        k[t] = row;
+      } else {
+        const int row = 8 * q + (lane >> 3), c = (lane & 7) ^ turn_along(row), in = GLU ? row & 127 : row;
+        const bool ok = o0 + in < outs;
+        const long at = GLU ? (row < 128 ? o0 + in : outs + o0 + in) : row;
+        off[t] = ok ? (uint32_t)((at * ld + 8 * c) * 2) : kOffNone;
+        k[t] = 8 * c;
       }
+    }
+  }
+  __device__ __forceinline__ void issue(uint32_t lds, long k0, long k1, int wave) const {
+    const int left = (int)min(k1 - k0, (long)kBigK);
+    const u32x4 rs = ACROSS ? rsrc_words(base + k0 * ld, (uint32_t)((left - 1) * ld * 2) + bytes) : rsrc_words(base, bytes);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const uint32_t o = k[t] < left ? off[t] + (ACROSS ? 0u : (uint32_t)k0 * 2) : kOffNone;
+      dma16(rs, o, lds + (uint32_t)(4 * wave + t) * 1024u);
+    }
+  }
+  // the fragment of sixteen outputs from o on, k from 32 s on
+  __device__ __forceinline__ static uint4 frag(const char* lds, int o, int s) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
+    if constexpr (!ACROSS) {
+      return *reinterpret_cast<const uint4*>(lds + (o + j) * (kBigK * 2) + (((4 * s + g) ^ turn_along(j)) << 4));
+    } else {
+      const int row = 32 * s + 8 * g + j / 4;
+      const char* const p = lds + row * (kBig * 2) + (((o / 8) ^ turn_across(row)) << 4) + 8 * (j % 4);
+      const v2u a = read_tr(reinterpret_cast<const bf16_t*>(p)), b = read_tr(reinterpret_cast<const bf16_t*>(p + 4 * kBig * 2));
+      return make_uint4(a.x, a.y, b.x, b.y);
+    }
+  }
+};
+
+template <bool PX, bool QX, bool GLU>
+__global__ void __launch_bounds__(kBigThreads) k_product_big(const ProductArgs a) {
+  __shared__ __align__(1024) char lds[4 * kBigBytes];
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = w & 3, wq = w >> 2;
+  const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
+  // the XCDs take work-groups in turn: each gets a run of tiles, eight rows of tiles at a time
+  const long tiles = a.tiles_m * a.tiles_n, all = tiles * a.splits;
+  const long run8 = all / 8, extra = all % 8, xcd = blockIdx.x % 8;
+  const long at = xcd * run8 + min(xcd, extra) + blockIdx.x / 8;
+  const int split = (int)(at / tiles);
+  const long t = at % tiles, band = t / (8 * a.tiles_n), high = min(8L, a.tiles_m - 8 * band);
+  const long in = t - band * 8 * a.tiles_n;
+  const long m0 = (8 * band + in % high) * kBig, n0 = in / high * (GLU ? kBig / 2 : kBig);
+  const long k0 = split * a.per, k1 = min(k0 + a.per, a.K);
+
+  const Direct<PX, GLU> dp(a.P, n0, a.N, a.K, w, lane);
+  const Direct<QX, false> dq(a.Q, m0, a.M, a.K, w, lane);
+  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds);
+  f32x4 acc[8][4];  // [block of Q][block of P]
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto block = [&](int i) { return GLU ? 128 * (i >> 1) + 32 * wp + 16 * (i & 1) : 64 * wp + 16 * i; };
+  auto issue = [&](int buf, long k) {
+    dp.issue(lds0 + buf * 2 * kBigBytes, k, k1, w);
+    dq.issue(lds0 + buf * 2 * kBigBytes + kBigBytes, k, k1, w);
+  };
+  int buf = 0;
+  if (k0 < k1) issue(0, k0);
+  for (long k = k0; k < k1; k += kBigK, buf ^= 1) {
+    // this step's pieces are in LDS, and the other buffer's reads are done, in every wave
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+    if (k + kBigK < k1) issue(buf ^ 1, k + kBigK);
+    const char* const pl = lds + buf * 2 * kBigBytes;
+    const char* const ql = pl + kBigBytes;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      uint4 p[4], q[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[i] = Direct<PX, GLU>::frag(pl, block(i), s);
+#pragma unroll
+      for (int l = 0; l < 8; ++l) q[l] = Direct<QX, false>::frag(ql, 128 * wq + 16 * l, s);
+#pragma unroll
+      for (int l = 0; l < 8; ++l)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) Mfma<bf16_t>::step(acc[l][i], p[i], q[l]);
+    }
+  }
+#pragma unroll
+  for (int l = 0; l < 8; ++l) {
+    const long m = m0 + 128 * wq + 16 * l + j;
+    if (m >= a.M) continue;
+    if constexpr (GLU) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) put_glu<bf16_t>(a, m, n0 + 32 * wp + 16 * i + 4 * g, acc[l][i], acc[l][i + 2]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) put<bf16_t>(a, split, m, n0 + block(i) + 4 * g, acc[l][i]);
     }
   }
 }
@@ -280,44 +497,69 @@ __global__ void __launch_bounds__(kThreads) k_glu_back(const GluGradArgs a, DT* 
   store4(out + a.F, c, a.F, du);
 }
 
-// Splits of a sum of length K for M x N outputs.
-int splits_of(long M, long N, long K, int bk) {
-  const long tiles = std::max(1L, (M + kTile - 1) / kTile) * ((N + kTile - 1) / kTile);
+// Splits of a sum of length K for M x N outputs in tiles of `tile`.
+int splits_of(long M, long N, long K, int tile, int bk) {
+  const long tiles = std::max(1L, (M + tile - 1) / tile) * ((N + tile - 1) / tile);
   if (tiles >= 256) return 1;
   return (int)std::max<long>(1, std::min<long>(512 / tiles, K / (8 * bk)));
+}
+// The kernel of a product goes by its sizes: bf16 products with at least 64 tiles of
+// 256 x 256 take those.
+bool big(int dtype, long M, long N, long K) {
+  return dtype == WM_BF16 && K % 8 == 0 && (M + kBig - 1) / kBig * ((N + kBig - 1) / kBig) >= 64;
+}
+// Whether an operand's rows lie on 16-byte boundaries, and near enough for 32-bit offsets.
+bool direct(const Operand& a) {
+  return (reinterpret_cast<uintptr_t>(a.p) & 15) == 0 && a.ld % 8 == 0 && a.ld <= 1 << 20;
 }
 
 template <typename DT, bool PX, bool QX, bool GLU>
 hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
   constexpr int BK = El<DT>::BK;
+  const int dtype = sizeof(DT) == 4 ? WM_FP32 : WM_BF16;
+  const bool wide = big(dtype, a.M, GLU ? 2 * a.N : a.N, a.K);
+  if constexpr (sizeof(DT) == 2) {
+    if (wide && direct(a.P) && direct(a.Q) && (!GLU || 2 * a.N * a.P.ld < (1L << 30))) {
+      const int width = GLU ? kBig / 2 : kBig;
+      a.tiles_n = (a.N + width - 1) / width;
+      a.tiles_m = (a.M + kBig - 1) / kBig;
+      a.splits = GLU ? 1 : splits_of(a.M, a.N, a.K, kBig, kBigK);
+      a.per = ((a.K + a.splits - 1) / a.splits + kBigK - 1) / kBigK * kBigK;
+      const hipError_t e = launch(name, k_product_big<PX, QX, GLU>, dim3((unsigned)(a.tiles_m * a.tiles_n * a.splits)),
+                                  dim3(kBigThreads), 0, s, a);
+      if (e != hipSuccess || a.splits == 1) return e;
+      return launch("glu_sum", k_product_sum<DT>, dim3((unsigned)((a.M * a.N + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a);
+    }
+  }
   const int width = GLU ? kTile / 2 : kTile;
-  a.tiles_n = (int)((a.N + width - 1) / width);
-  const long tiles = (a.M + kTile - 1) / kTile * a.tiles_n;
-  a.splits = GLU ? 1 : splits_of(a.M, a.N, a.K, BK);
+  a.tiles_n = (a.N + width - 1) / width;
+  a.tiles_m = (a.M + kTile - 1) / kTile;
+  a.splits = GLU ? 1 : splits_of(a.M, a.N, a.K, kTile, BK);
   a.per = ((a.K + a.splits - 1) / a.splits + BK - 1) / BK * BK;
   const hipError_t e =
-      launch(name, k_product<DT, PX, QX, GLU>, dim3((unsigned)(tiles * a.splits)), dim3(kThreads), 0, s, a);
+      launch(name, k_product<DT, PX, QX, GLU>, dim3((unsigned)(a.tiles_m * a.tiles_n * a.splits)), dim3(kThreads), 0, s, a);
   if (e != hipSuccess || a.splits == 1) return e;
   return launch("glu_sum", k_product_sum<DT>, dim3((unsigned)((a.M * a.N + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a);
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
-size_t part_bytes(long M, long N, long K, int bk) {
-  const int s = splits_of(M, N, K, bk);
+// What either kernel of the product needs.
+size_t part_bytes(int dtype, long M, long N, long K) {
+  const int s = std::max(splits_of(M, N, K, kTile, dtype == WM_FP32 ? El<float>::BK : El<bf16_t>::BK),
+                         big(dtype, M, N, K) ? splits_of(M, N, K, kBig, kBigK) : 1);
   return s > 1 ? (size_t)s * M * N * sizeof(float) : 0;
 }
 
 }  // namespace
 
 hipError_t launch_glu(int dtype, const GluArgs& a, hipStream_t s) {
-  const ProductArgs p{{a.W, a.D}, {a.x, a.x_ld}, a.rows, a.F, a.D, a.h, a.h_ld, a.pre, a.act, nullptr, 1, 0, 0};
+  const ProductArgs p{{a.W, a.D}, {a.x, a.x_ld}, a.rows, a.F, a.D, a.h, a.h_ld, a.pre, a.act, nullptr, 1, 0, 0, 0};
   return dtype == WM_FP32 ? product<float, false, false, true>("glu", p, s) : product<bf16_t, false, false, true>("glu", p, s);
 }
 
 size_t glu_grad_workspace(int dtype, long rows, int D, int F) {
-  const int bk = dtype == WM_FP32 ? El<float>::BK : El<bf16_t>::BK, size = dtype == WM_FP32 ? 4 : 2;
-  return align256((size_t)rows * 2 * F * size) +
-         align256(std::max(part_bytes(rows, D, 2L * F, bk), part_bytes(2L * F, D, rows, bk)));
+  return align256((size_t)rows * 2 * F * (dtype == WM_FP32 ? 4 : 2)) +
+         align256(std::max(part_bytes(dtype, rows, D, 2L * F), part_bytes(dtype, 2L * F, D, rows)));
 }
 
 hipError_t launch_glu_grad(int dtype, const GluGradArgs& a, hipStream_t s) {
@@ -330,11 +572,11 @@ hipError_t launch_glu_grad(int dtype, const GluGradArgs& a, hipStream_t s) {
       const long n = a.rows * ((a.F + 3) / 4);
       e = launch("glu_back", k_glu_back<DT>, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a, dpre);
       if (e != hipSuccess) return e;
-      const ProductArgs dx{{a.W, a.D}, {dpre, 2L * a.F}, a.rows, a.D, 2L * a.F, a.dx, a.dx_ld, nullptr, 0, part, 1, 0, 0};
+      const ProductArgs dx{{a.W, a.D}, {dpre, 2L * a.F}, a.rows, a.D, 2L * a.F, a.dx, a.dx_ld, nullptr, 0, part, 1, 0, 0, 0};
       if ((e = product<DT, true, false, false>("glu_dx", dx, s)) != hipSuccess) return e;
     }
     if (!a.dW) return e;
-    const ProductArgs dw{{a.x, a.x_ld}, {dpre, 2L * a.F}, 2L * a.F, a.D, a.rows, a.dW, a.D, nullptr, 0, part, 1, 0, 0};
+    const ProductArgs dw{{a.x, a.x_ld}, {dpre, 2L * a.F}, 2L * a.F, a.D, a.rows, a.dW, a.D, nullptr, 0, part, 1, 0, 0, 0};
     return product<DT, true, true, false>("glu_dw", dw, s);
   };
   return dtype == WM_FP32 ? run(0.0f) : run(bf16_t());
