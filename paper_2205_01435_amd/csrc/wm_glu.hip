@@ -174,7 +174,9 @@ __device__ __forceinline__ float normal_cdf(float x) { return 0.5f * erfcf(x * -
 // act(g) and its derivative
 __device__ __forceinline__ float2 activate(int act, float g) {
   if (act == WM_ACT_SILU) {
-    const float2 s = gate_pair_of(g, expf(-fabsf(g)));
+    // (sigmoid(g), sigmoid(-g)); beyond kGateMost the smaller is 0 to any product's precision
+    const float n = fabsf(g);
+    const float2 s = gate_pair_of(g, n > kGateMost ? 0.0f : gate_exp_small(n));
     return make_float2(g * s.x, s.x * fmaf(g, s.y, 1.0f));
   }
   const float c = normal_cdf(g);
@@ -474,29 +476,76 @@ __global__ void __launch_bounds__(kThreads) k_product_sum(const ProductArgs a) {
   DType<DT>::store(reinterpret_cast<DT*>(a.out) + i / a.N * a.out_ld, i % a.N, s);
 }
 
-// dpre [rows, 2F] from pre and dh.
 template <typename DT>
-__global__ void __launch_bounds__(kThreads) k_glu_back(const GluGradArgs a, DT* dpre) {
-  const long parts = (a.F + 3) / 4, i = (long)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= a.rows * parts) return;
-  const long row = i / parts;
-  const int c = (int)(i % parts) * 4;
-  const DT* pre = reinterpret_cast<const DT*>(a.pre) + row * 2 * a.F;
-  const DT* dh = reinterpret_cast<const DT*>(a.dh) + row * a.dh_ld;
-  float dg[4], du[4];
+__device__ __forceinline__ void unpack(v4u r, float* v) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const int k = min(c + e, a.F - 1);
-    const float d = DType<DT>::load(dh, k), u = DType<DT>::load(pre, a.F + k);
-    const float2 v = activate(a.act, DType<DT>::load(pre, k));
-    dg[e] = d * u * v.y;
-    du[e] = d * v.x;
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(DT) == 4) {
+      v[i] = __uint_as_float(r[i]);
+    } else {
+      v[2 * i] = __uint_as_float(r[i] << 16);
+      v[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+    }
   }
-  DT* out = dpre + row * 2 * a.F;
-  store4(out, c, a.F, dg);
-  store4(out + a.F, c, a.F, du);
+}
+template <typename DT>
+__device__ __forceinline__ void store_piece(DT* row, long c, long width, const float* v) {
+  constexpr int V = El<DT>::VEC;
+  if (c + V <= width) {
+    v4u r;
+    if constexpr (sizeof(DT) == 4)
+      r = v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    else
+      r = v4u{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
+    *reinterpret_cast<typename El<DT>::mem*>(row + c) = r;
+  } else {
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      if (c + e < width) DType<DT>::store(row, c + e, v[e]);
+  }
 }
 
+// One piece of a row.
+template <typename DT>
+__device__ __forceinline__ void back_piece(const GluGradArgs& a, DT* dpre, long row, int c) {
+  constexpr int V = El<DT>::VEC;
+  const DT* pre = reinterpret_cast<const DT*>(a.pre) + row * 2 * a.F;
+  float g[V], u[V], d[V];
+  const v4u rg = load_piece<DT>(pre, c, a.F), ru = load_piece<DT>(pre + a.F, c, a.F),
+            rd = load_piece<DT>(reinterpret_cast<const DT*>(a.dh) + row * a.dh_ld, c, a.F);
+  unpack<DT>(rg, g);
+  unpack<DT>(ru, u);
+  unpack<DT>(rd, d);
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    const float2 v = activate(a.act, g[e]);
+    g[e] = d[e] * u[e] * v.y;
+    u[e] = d[e] * v.x;
+  }
+  DT* out = dpre + row * 2 * a.F;
+  store_piece(out, c, a.F, g);
+  store_piece(out + a.F, c, a.F, u);
+}
+
+constexpr long kBackGroups = 4096;
+// dpre [rows, 2F] from pre and dh: 16 bytes of a row a lane.
+template <typename DT>
+__global__ void __launch_bounds__(kThreads) k_glu_back(const GluGradArgs a, DT* dpre) {
+  constexpr int V = El<DT>::VEC;
+  const uint32_t parts = (uint32_t)(a.F + V - 1) / V;
+  const long pieces = a.rows * (long)parts, step = (long)gridDim.x * kThreads;
+  long at = (long)blockIdx.x * kThreads + threadIdx.x;
+  // row and piece advance by the stride's own
+  long row = at / parts;
+  uint32_t p = (uint32_t)(at % parts);
+  const long step_row = step / parts;
+  const uint32_t step_p = (uint32_t)(step % parts);
+  for (; at < pieces; at += step, row += step_row, p += step_p) {
+    if (p >= parts) p -= parts, ++row;
+    const int c = (int)p * V;
+    back_piece<DT>(a, dpre, row, c);
+  }
+}
 // Splits of a sum of length K for M x N outputs in tiles of `tile`.
 int splits_of(long M, long N, long K, int tile, int bk) {
   const long tiles = std::max(1L, (M + tile - 1) / tile) * ((N + tile - 1) / tile);
@@ -569,8 +618,9 @@ hipError_t launch_glu_grad(int dtype, const GluGradArgs& a, hipStream_t s) {
     float* part = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + align256((size_t)a.rows * 2 * a.F * sizeof(DT)));
     hipError_t e = hipSuccess;
     if (a.rows > 0) {
-      const long n = a.rows * ((a.F + 3) / 4);
-      e = launch("glu_back", k_glu_back<DT>, dim3((unsigned)((n + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a, dpre);
+      const long pieces = a.rows * ((a.F + El<DT>::VEC - 1) / El<DT>::VEC);
+      e = launch("glu_back", k_glu_back<DT>, dim3((unsigned)std::min<long>((pieces + kThreads - 1) / kThreads, kBackGroups)),
+                 dim3(kThreads), 0, s, a, dpre);
       if (e != hipSuccess) return e;
       const ProductArgs dx{{a.W, a.D}, {dpre, 2L * a.F}, a.rows, a.D, 2L * a.F, a.dx, a.dx_ld, nullptr, 0, part, 1, 0, 0, 0};
       if ((e = product<DT, true, false, false>("glu_dx", dx, s)) != hipSuccess) return e;
