@@ -39,6 +39,7 @@ struct MixArgs {
   int T, B, N;
   int ka, kc;  // widths of A and B, and of C and the output
   SeqView a, b, c, out;
+  SeqView v;  // the pair of dk and dv: v
   const float* decay;
   float s_intra, s_inter, s_upd;  // factors of the chunk's own part, the state's, and of sources on their way into it
   const float* s0;  // [B, N, ka, kc] with the strides below, or null (0)
@@ -98,245 +99,206 @@ __device__ __forceinline__ bf16x8 join(v2u a, v2u b) { return __builtin_bit_cast
 // a^n from log2 a, 1 for n = 0 also where a = 0.
 __device__ __forceinline__ float decayed(float la, int n) { return n > 0 ? __builtin_amdgcn_exp2f(la * (float)n) : 1.0f; }
 
-template <typename DT, int KA, int KC, bool REV, bool STATE>
-__global__ void __launch_bounds__(kThreads) k_mix(const MixArgs a) {
-  constexpr int V = Tile<DT>::VEC, SL = Tile<DT>::SLICE, PL = Tile<DT>::PLANES;
-  constexpr bool F32 = sizeof(DT) == 4;
-  constexpr int PA = KA + Tile<DT>::PAD, PC = KC + Tile<DT>::PAD;  // pitches in LDS
-  constexpr int AB = kChunk * (KA / V) / kThreads, CB = kChunk * (KC / V) / kThreads;  // pieces a thread stages
-  static_assert(AB > 0 && CB > 0, "a piece or more for every thread");
-  constexpr int WK = KA >= 64 ? 4 : 2, WC = 4 / WK;      // waves over the state's rows and columns
-  constexpr int KAB = KA / 16 / WK, KCB = KC / 16 / WC;  // its 16 x 16 blocks in a wave
-  __shared__ __align__(16) DT bl[kChunk * PA];
-  __shared__ __align__(16) DT cl[kChunk * PC];
-  __shared__ __align__(16) DT st[STATE ? 16 : PL * KC * PA];  // the state, columns first
-
-  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63, g = lane >> 4, j16 = lane & 15;
-  const int nct = (a.kc + KC - 1) / KC;
-  const int ct = blockIdx.x % nct * KC;
-  const long part = blockIdx.x / nct;  // (sequence and head, segment)
-  const int seg = (int)(part % a.nseg);
-  const long bn = part / a.nseg;
-  const int n = (int)(bn % a.N), b = (int)(bn / a.N);
-  const int len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
-  const float da = fminf(fmaxf(a.decay[n], 0.0f), 1.0f), la = log2f(da);
-  const int chunks = (a.T + kChunk - 1) / kChunk, first = seg * a.per, last = min(first + a.per, chunks);
-  const int wcols = min(KC, a.kc - ct);
-  const DT* const pa = reinterpret_cast<const DT*>(a.a.p) + (long)b * a.a.b + (long)n * a.ka;
-  const DT* const pb = reinterpret_cast<const DT*>(a.b.p) + (long)b * a.b.b + (long)n * a.ka;
-  const DT* const pc = reinterpret_cast<const DT*>(a.c.p) + (long)b * a.c.b + (long)n * a.kc + ct;
-
-  v4u rb[AB], rc[CB], ra[KA / SL];
-  const int r = 16 * w + j16;  // this lane's row of a chunk
-  auto load = [&](int c) {
-    const int t0 = c * kChunk, live = len - t0;
-#pragma unroll
-    for (int i = 0; i < AB; ++i) {
-      const int p = tid + i * kThreads, s = p / (KA / V);
-      rb[i] = s < live ? load_piece<DT>(pb + (long)(t0 + s) * a.b.t, p % (KA / V) * V, a.ka) : v4u{0, 0, 0, 0};
-    }
-#pragma unroll
-    for (int i = 0; i < CB; ++i) {
-      const int p = tid + i * kThreads, s = p / (KC / V);
-      rc[i] = s < live ? load_piece<DT>(pc + (long)(t0 + s) * a.c.t, p % (KC / V) * V, wcols) : v4u{0, 0, 0, 0};
-    }
-    if constexpr (!STATE) {
-#pragma unroll
-      for (int i = 0; i < KA / SL; ++i)
-        ra[i] = r < live ? load_piece<DT>(pa + (long)(t0 + r) * a.a.t, i * SL + V * g, a.ka) : v4u{0, 0, 0, 0};
-    }
+// Rows of one sequence and head of a [T, B, N, width] array.  FAST: as wide as the
+// tile, on 16-byte boundaries and near enough for 32-bit offsets: range-checked
+// loads and stores, which give zeros and nothing past the rows that exist.
+template <typename DT, int W, bool FAST>
+struct Rows {
+  DT* p;
+  long t;     // elements between steps
+  int width;  // of this tile
+  __device__ __forceinline__ Rows(const SeqView& a, int b, int n, int heads_width, int col, int width_)
+      : p(reinterpret_cast<DT*>(const_cast<void*>(a.p)) + (long)b * a.b + (long)n * heads_width + col), t(a.t), width(width_) {}
+  // rows [t0, t0 + count)
+  struct Chunk {
+    rsrc_t r;
+    DT* p;
+    int count;
   };
-  auto stage = [&]() {
-#pragma unroll
-    for (int i = 0; i < AB; ++i) {
-      const int p = tid + i * kThreads;
-      *reinterpret_cast<v4u*>(bl + p / (KA / V) * PA + p % (KA / V) * V) = rb[i];
-    }
-#pragma unroll
-    for (int i = 0; i < CB; ++i) {
-      const int p = tid + i * kThreads;
-      *reinterpret_cast<v4u*>(cl + p / (KC / V) * PC + p % (KC / V) * V) = rc[i];
-    }
-  };
-
-  // the state's blocks of this wave: rows 16 (wk KAB + i) + 4 g + 0..3, column 16 (wc KCB + k) + j16
-  const int wk = w % WK, wc = w / WK;
-  f32x4 S[KAB][KCB];
-  const float* const s0 = a.seg && !STATE ? a.seg + part * a.ka * a.kc : a.s0 && !STATE ? a.s0 + bn * a.ka * a.kc : nullptr;
-#pragma unroll
-  for (int i = 0; i < KAB; ++i)
-#pragma unroll
-    for (int k = 0; k < KCB; ++k)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = 16 * (wk * KAB + i) + 4 * g + e, col = 16 * (wc * KCB + k) + j16;
-        S[i][k][e] = s0 && row < a.ka && col < wcols ? s0[(long)row * a.st_a + (long)(ct + col) * a.st_c] : 0.0f;
-      }
-  auto stage_state = [&]() {
-    if constexpr (!STATE) {
-#pragma unroll
-      for (int i = 0; i < KAB; ++i)
-#pragma unroll
-        for (int k = 0; k < KCB; ++k) {
-          DT* const p = st + (16 * (wc * KCB + k) + j16) * PA + 16 * (wk * KAB + i) + 4 * g;
-          const f32x4 v = S[i][k];
-          if constexpr (F32) {
-            *reinterpret_cast<v4u*>(p) = __builtin_bit_cast(v4u, v);
-          } else {
-            const v2u h = {pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
-            *reinterpret_cast<v2u*>(p) = h;
-            *reinterpret_cast<v2u*>(p + KC * PA) =
-                v2u{pack2_bf16(v[0] - __uint_as_float(h.x << 16), v[1] - __uint_as_float(h.x & 0xffff0000u)),
-                    pack2_bf16(v[2] - __uint_as_float(h.y << 16), v[3] - __uint_as_float(h.y & 0xffff0000u))};
-          }
-        }
-    }
-  };
-
-  // a^|r - s| for the sources s = 16 j + 4 g + e of the lane's row
-  float wt[4][4];
-  if constexpr (!STATE) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) wt[j][e] = a.s_intra * decayed(la, abs(r - (16 * j + 4 * g + e)));
+  __device__ __forceinline__ Chunk at(int t0, int count) const {
+    Chunk c;
+    c.p = p + (long)t0 * t;
+    c.count = count;
+    if constexpr (FAST) c.r = make_rsrc(c.p, count > 0 ? (uint32_t)(((long)(count - 1) * t + W) * (long)sizeof(DT)) : 0u);
+    return c;
   }
-
-  float hold_all = 1.0f;
-  if (first < last) load(REV ? last - 1 : first);
-  for (int step = 0; step < last - first; ++step) {
-    const int c = REV ? last - 1 - step : first + step, t0 = c * kChunk;
-    const int live = min(len - t0, kChunk);  // steps of the chunk inside the sequence, 0 or less for none
-    uint64_t starts = 0;
-    if (a.resets) {
-      const bool one = lane < live && a.resets[(long)(t0 + lane) * a.B + b] != 0;
-      starts = __ballot(one);
+  // 16 bytes of row s from column c on
+  __device__ __forceinline__ v4u load(const Chunk& k, int s, int c) const {
+    if constexpr (FAST) {
+      const uint4 v = bload16(k.r, ((uint32_t)s * (uint32_t)t + (uint32_t)c) * (uint32_t)sizeof(DT));
+      return v4u{v.x, v.y, v.z, v.w};
+    } else {
+      return s < k.count ? load_piece<DT>(k.p + (long)s * t, c, width) : v4u{0, 0, 0, 0};
     }
-    __syncthreads();  // the chunk before is done with
-    stage();
-    stage_state();
-    v4u now[KA / SL];
-    if constexpr (!STATE) {
+  }
+  // four values of row s from column c on
+  __device__ __forceinline__ void store(const Chunk& k, int s, int c, const float (&v)[4]) const {
+    if constexpr (FAST) {
+      const uint32_t o = ((uint32_t)s * (uint32_t)t + (uint32_t)c) * (uint32_t)sizeof(DT);
+      if constexpr (sizeof(DT) == 4)
+        bstore16(k.r, o, make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])));
+      else
+        bstore8(k.r, o, make_uint2(pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])));
+    } else if (s < k.count) {
+      DT* const row = k.p + (long)s * t;
+      if (c + 4 <= width) {
+        if constexpr (sizeof(DT) == 4)
+          *reinterpret_cast<v4u_4*>(row + c) =
+              v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+        else
+          *reinterpret_cast<v2u_2*>(row + c) = v2u{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
+      } else {
 #pragma unroll
-      for (int i = 0; i < KA / SL; ++i) now[i] = ra[i];
+        for (int e = 0; e < 4; ++e)
+          if (c + e < width) DType<DT>::store(row, c + e, v[e]);
+      }
     }
-    if (step + 1 < last - first) load(REV ? c - 1 : c + 1);
-    __syncthreads();
+  }
+};
 
-    if constexpr (!STATE) {
-      // the sources [lo, hi] of the row, and whether the entering state reaches it
-      const uint64_t upto = ~0ull >> (63 - r);
-      const uint64_t cut = REV ? starts & ~upto : starts & upto;
-      const int lo = REV ? r : cut ? 63 - __clzll((long long)cut) : 0;
-      const int hi = REV ? (cut ? __ffsll((long long)cut) - 2 : live - 1) : r;
-      const int dist = REV ? live - 1 - r : r + 1;
-      const float win = cut == 0 ? a.s_inter * decayed(la, dist) : 0.0f;
-      DT* const orow = reinterpret_cast<DT*>(const_cast<void*>(a.out.p)) + (long)(t0 + r) * a.out.t + (long)b * a.out.b +
-                       (long)n * a.kc + ct;
-      float P[4][4];
+// A chunk's 64 rows in LDS, by all threads.
+template <typename DT, int W>
+struct Panel {
+  static constexpr int V = Tile<DT>::VEC, PITCH = W + Tile<DT>::PAD, N = kChunk * (W / V) / kThreads, SIZE = kChunk * PITCH;
+  static_assert(N > 0, "a piece or more for every thread");
+  v4u r[N];
+  template <bool FAST>
+  __device__ __forceinline__ void load(const Rows<DT, W, FAST>& rows, const typename Rows<DT, W, FAST>::Chunk& c) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        if ((REV ? j >= w : j <= w) && live > 0) {
+    for (int i = 0; i < N; ++i) {
+      const int p = threadIdx.x + i * kThreads;
+      r[i] = rows.load(c, p / (W / V), p % (W / V) * V);
+    }
+  }
+  __device__ __forceinline__ void store(DT* lds) const {
 #pragma unroll
-          for (int k = 0; k < KA / SL; ++k) {
-            const v4u x = *reinterpret_cast<const v4u*>(bl + (16 * j + j16) * PA + k * SL + V * g);
-            Mfma<DT>::step(acc, make_uint4(x.x, x.y, x.z, x.w), make_uint4(now[k].x, now[k].y, now[k].z, now[k].w));
-          }
-        }
+    for (int i = 0; i < N; ++i) {
+      const int p = threadIdx.x + i * kThreads;
+      *reinterpret_cast<v4u*>(lds + p / (W / V) * PITCH + p % (W / V) * V) = r[i];
+    }
+  }
+};
+// The lane's row of a chunk as a matrix operand, along the row.
+template <typename DT, int W>
+struct RowFrag {
+  static constexpr int SL = Tile<DT>::SLICE, V = Tile<DT>::VEC, N = W / SL;
+  v4u r[N];
+  template <bool FAST>
+  __device__ __forceinline__ void load(const Rows<DT, W, FAST>& rows, const typename Rows<DT, W, FAST>::Chunk& c, int s, int g) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int s = 16 * j + 4 * g + e;
-          P[j][e] = s >= lo && s <= hi ? acc[e] * wt[j][e] : 0.0f;
-        }
-      }
-      bf16x8 ph[2], pm[2];
-      if constexpr (!F32) {
+    for (int i = 0; i < N; ++i) r[i] = rows.load(c, s, i * SL + V * g);
+  }
+  __device__ __forceinline__ uint4 operator[](int i) const { return make_uint4(r[i].x, r[i].y, r[i].z, r[i].w); }
+};
+
+// What a work-group is at: a sequence, a head and a segment.
+struct Place {
+  int b, n, seg, len, first, last;
+  long bn, part;
+  float la;  // log2 of the decay
+  __device__ __forceinline__ Place(const MixArgs& a, long at) : part(at) {
+    seg = (int)(at % a.nseg);
+    bn = at / a.nseg;
+    n = (int)(bn % a.N);
+    b = (int)(bn / a.N);
+    len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
+    la = log2f(fminf(fmaxf(a.decay[n], 0.0f), 1.0f));
+    const int chunks = (a.T + kChunk - 1) / kChunk;
+    first = seg * a.per;
+    last = min(first + a.per, chunks);
+  }
+};
+
+// The masks of a chunk: bit s of `starts` for a step that begins a trajectory.
+template <bool REV>
+struct Mask {
+  int lo, hi;    // a row's sources
+  bool entered;  // whether the state that enters reaches the row
+  __device__ __forceinline__ Mask(uint64_t starts, int live, int r) {
+    const uint64_t upto = ~0ull >> (63 - r), cut = REV ? starts & ~upto : starts & upto;
+    lo = REV ? r : cut ? 63 - __clzll((long long)cut) : 0;
+    hi = REV ? (cut ? __ffsll((long long)cut) - 2 : live - 1) : r;
+    entered = cut == 0;
+  }
+};
+
+// The state of a head, [KA][KC], in the registers of four waves: blocks of rows
+// 16 (wk KAB + i) + 4 g + 0..3 and column 16 (wc KCB + k) + j16.
+template <typename DT, int KA, int KC>
+struct State {
+  static constexpr bool F32 = sizeof(DT) == 4;
+  static constexpr int WK = KA >= 64 ? 4 : 2, WC = 4 / WK, KAB = KA / 16 / WK, KCB = KC / 16 / WC;
+  static constexpr int PA = KA + Tile<DT>::PAD, PC = KC + Tile<DT>::PAD, PL = Tile<DT>::PLANES;
+  static constexpr int SIZE = PL * KC * PA;  // in LDS, columns first
+  f32x4 S[KAB][KCB];
+  int wk, wc, g, j16;
+  __device__ __forceinline__ State() {
+    const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    wk = w % WK;
+    wc = w / WK;
+    g = lane >> 4;
+    j16 = lane & 15;
+  }
+  __device__ __forceinline__ int row(int i) const { return 16 * (wk * KAB + i) + 4 * g; }
+  __device__ __forceinline__ int col(int k) const { return 16 * (wc * KCB + k) + j16; }
+  // p: [ka][..] with strides st_a and st_c; null for zeros
+  __device__ __forceinline__ void load(const float* p, int ka, int kc, int st_a, int st_c) {
 #pragma unroll
-        for (int jj = 0; jj < 2; ++jj) {
-          v4u h, m;
+    for (int i = 0; i < KAB; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float x = P[2 * jj + e / 2][2 * (e & 1)], y = P[2 * jj + e / 2][2 * (e & 1) + 1];
-            h[e] = pack2_bf16(x, y);
-            m[e] = pack2_bf16(x - __uint_as_float(h[e] << 16), y - __uint_as_float(h[e] & 0xffff0000u));
-          }
-          ph[jj] = __builtin_bit_cast(bf16x8, h);
-          pm[jj] = __builtin_bit_cast(bf16x8, m);
-        }
-      }
+      for (int k = 0; k < KCB; ++k)
 #pragma unroll
-      for (int cb = 0; cb < KC / 16; ++cb) {
-        if (16 * cb >= wcols) break;
-        f32x4 in = {0.f, 0.f, 0.f, 0.f}, out = {0.f, 0.f, 0.f, 0.f};
-        if (live > 0) {
+        for (int e = 0; e < 4; ++e)
+          S[i][k][e] = p && row(i) + e < ka && col(k) < kc ? p[(long)(row(i) + e) * st_a + (long)col(k) * st_c] : 0.0f;
+  }
+  __device__ __forceinline__ void save(float* p, int ka, int kc, int st_a, int st_c) const {
 #pragma unroll
-          for (int k = 0; k < KA / SL; ++k) {
-            const uint4 y = make_uint4(now[k].x, now[k].y, now[k].z, now[k].w);
+    for (int i = 0; i < KAB; ++i)
 #pragma unroll
-            for (int p = PL - 1; p >= 0; --p) {
-              const v4u x = *reinterpret_cast<const v4u*>(st + (p * KC + 16 * cb + j16) * PA + k * SL + V * g);
-              Mfma<DT>::step(in, make_uint4(x.x, x.y, x.z, x.w), y);
-            }
-          }
-          if constexpr (F32) {
+      for (int k = 0; k < KCB; ++k)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              if (REV ? j < w : j > w) continue;
+        for (int e = 0; e < 4; ++e)
+          if (row(i) + e < ka && col(k) < kc) p[(long)(row(i) + e) * st_a + (long)col(k) * st_c] = S[i][k][e];
+  }
+  __device__ __forceinline__ void stage(DT* st) const {
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                out = __builtin_amdgcn_mfma_f32_16x16x4f32(cl[(16 * j + 4 * g + e) * PC + 16 * cb + j16], P[j][e], out, 0, 0, 0);
-            }
-          } else {
+    for (int i = 0; i < KAB; ++i)
 #pragma unroll
-            for (int jj = 0; jj < 2; ++jj) {
-              if (REV ? 2 * jj + 1 < w : 2 * jj > w) continue;
-              const bf16_t* const p = cl + (32 * jj + 4 * g + j16 / 4) * PC + 16 * cb + 4 * (j16 % 4);
-              const bf16x8 x = join(read_tr(p), read_tr(p + 16 * PC));
-              out = mfma_bf16(x, pm[jj], out);
-              out = mfma_bf16(x, ph[jj], out);
-            }
-          }
-        }
-        if (t0 + r >= a.T) continue;
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = r < live ? out[e] + (cut == 0 ? win * in[e] : 0.0f) : 0.0f;
-        const int col = 16 * cb + 4 * g;
-        if (col + 4 <= wcols) {
-          if constexpr (F32)
-            *reinterpret_cast<v4u_4*>(orow + col) =
-                v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-          else
-            *reinterpret_cast<v2u_2*>(orow + col) = v2u{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
+      for (int k = 0; k < KCB; ++k) {
+        DT* const p = st + col(k) * PA + row(i);
+        const f32x4 v = S[i][k];
+        if constexpr (F32) {
+          *reinterpret_cast<v4u*>(p) = __builtin_bit_cast(v4u, v);
         } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (col + e < wcols) DType<DT>::store(orow, col + e, v[e]);
+          const v2u h = {pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3])};
+          *reinterpret_cast<v2u*>(p) = h;
+          *reinterpret_cast<v2u*>(p + KC * PA) =
+              v2u{pack2_bf16(v[0] - __uint_as_float(h.x << 16), v[1] - __uint_as_float(h.x & 0xffff0000u)),
+                  pack2_bf16(v[2] - __uint_as_float(h.y << 16), v[3] - __uint_as_float(h.y & 0xffff0000u))};
         }
       }
-    }
-
-    if (live <= 0) continue;
-    // what the state keeps, and the sources [lo, hi] that it takes in
-    const float hold = starts ? 0.0f : decayed(la, live);
+  }
+  // S becomes hold S + sum over the sources s in [lo, hi] of upd a^distance B_s C_s^T,
+  // distance to the end of the chunk that the sweep leaves by; 0 at a reset, whatever S holds
+  template <bool REV>
+  __device__ __forceinline__ void take(const DT* bl, const DT* cl, uint64_t starts, int live, float la, float upd) {
+    const float hold = decayed(la, live);
     const int lo = REV ? 0 : starts ? 63 - __clzll((long long)starts) : 0;
     const int hi = REV ? (starts ? __ffsll((long long)starts) - 2 : live - 1) : live - 1;
-    if constexpr (STATE) hold_all = starts ? 0.0f : hold_all * hold;
 #pragma unroll
     for (int i = 0; i < KAB; ++i)
 #pragma unroll
       for (int k = 0; k < KCB; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) S[i][k][e] = starts ? 0.0f : S[i][k][e] * hold;
-    auto taken = [&](int s) {
-      return s >= lo && s <= hi ? a.s_upd * decayed(la, REV ? s + 1 : live - 1 - s) : 0.0f;
-    };
 #pragma unroll
     for (int jj = 0; jj < 2; ++jj) {
       float ws[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ws[e] = taken(32 * jj + 16 * (e / 4) + 4 * g + e % 4);
+      for (int e = 0; e < 8; ++e) {
+        const int s = 32 * jj + 16 * (e / 4) + 4 * g + e % 4;
+        ws[e] = s >= lo && s <= hi ? upd * decayed(la, REV ? s + 1 : live - 1 - s) : 0.0f;
+      }
       if constexpr (F32) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -349,7 +311,7 @@ __global__ void __launch_bounds__(kThreads) k_mix(const MixArgs a) {
           }
 #pragma unroll
           for (int k = 0; k < KCB; ++k) {
-            const float y = cl[s * PC + 16 * (wc * KCB + k) + j16];
+            const float y = cl[s * PC + col(k)];
 #pragma unroll
             for (int i = 0; i < KAB; ++i) S[i][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y, S[i][k], 0, 0, 0);
           }
@@ -383,22 +345,292 @@ __global__ void __launch_bounds__(kThreads) k_mix(const MixArgs a) {
       }
     }
   }
+};
 
-  float* const s1 = STATE ? a.seg + part * a.ka * a.kc : a.seg || !a.s1 ? nullptr : a.s1 + bn * a.ka * a.kc;
-  if (s1) {
+// a^|r - s| for the sources s = 16 j + 4 g + e of the lane's row, times `scale`
+struct Weights {
+  float w[4][4];
+  __device__ __forceinline__ Weights(float la, int r, int g, float scale) {
 #pragma unroll
-    for (int i = 0; i < KAB; ++i)
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int k = 0; k < KCB; ++k)
+      for (int e = 0; e < 4; ++e) w[j][e] = scale * decayed(la, abs(r - (16 * j + 4 * g + e)));
+  }
+};
+
+// The chunk's part of the rows of wave w: the weighted products of a row with its
+// sources as a matrix operand, and their product with the sources' values.
+template <typename DT, int KA, bool REV>
+struct Intra {
+  static constexpr bool F32 = sizeof(DT) == 4;
+  static constexpr int PA = KA + Tile<DT>::PAD, SL = Tile<DT>::SLICE, V = Tile<DT>::VEC;
+  float P[4][4];
+  bf16x8 ph[2], pm[2];
+  __device__ __forceinline__ Intra(const DT* bl, const RowFrag<DT, KA>& rows, const Weights& wt, const Mask<REV>& mask, int w, int g,
+                                   int j16) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      if (REV ? j >= w : j <= w) {
+#pragma unroll
+        for (int k = 0; k < KA / SL; ++k) {
+          const v4u x = *reinterpret_cast<const v4u*>(bl + (16 * j + j16) * PA + k * SL + V * g);
+          Mfma<DT>::step(acc, make_uint4(x.x, x.y, x.z, x.w), rows[k]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int s = 16 * j + 4 * g + e;
+        P[j][e] = s >= mask.lo && s <= mask.hi ? acc[e] * wt.w[j][e] : 0.0f;
+      }
+    }
+    if constexpr (!F32) {
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        v4u h, m;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int row = 16 * (wk * KAB + i) + 4 * g + e, col = 16 * (wc * KCB + k) + j16;
-          if (row < a.ka && col < wcols) s1[(long)row * a.st_a + (long)(ct + col) * a.st_c] = S[i][k][e];
+          const float x = P[2 * jj + e / 2][2 * (e & 1)], y = P[2 * jj + e / 2][2 * (e & 1) + 1];
+          h[e] = pack2_bf16(x, y);
+          m[e] = pack2_bf16(x - __uint_as_float(h[e] << 16), y - __uint_as_float(h[e] & 0xffff0000u));
         }
+        ph[jj] = __builtin_bit_cast(bf16x8, h);
+        pm[jj] = __builtin_bit_cast(bf16x8, m);
+      }
+    }
   }
+  // columns 16 cb .. + 15 of the values at cl (pitch PC)
+  template <int PC>
+  __device__ __forceinline__ f32x4 times(const DT* cl, int cb, int w, int g, int j16) const {
+    f32x4 out = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (F32) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (REV ? j < w : j > w) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          out = __builtin_amdgcn_mfma_f32_16x16x4f32(cl[(16 * j + 4 * g + e) * PC + 16 * cb + j16], P[j][e], out, 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        if (REV ? 2 * jj + 1 < w : 2 * jj > w) continue;
+        const bf16_t* const p = cl + (32 * jj + 4 * g + j16 / 4) * PC + 16 * cb + 4 * (j16 % 4);
+        const bf16x8 x = join(read_tr(p), read_tr(p + 16 * PC));
+        out = mfma_bf16(x, pm[jj], out);
+        out = mfma_bf16(x, ph[jj], out);
+      }
+    }
+    return out;
+  }
+};
+
+// Columns 16 cb .. + 15 of the rows' products with the state in LDS ([KC][KA]).
+template <typename DT, int KA, int KC>
+__device__ __forceinline__ f32x4 entered(const DT* st, const RowFrag<DT, KA>& rows, int cb, int g, int j16) {
+  constexpr int PA = KA + Tile<DT>::PAD, SL = Tile<DT>::SLICE, V = Tile<DT>::VEC;
+  f32x4 in = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < KA / SL; ++k)
+#pragma unroll
+    for (int p = Tile<DT>::PLANES - 1; p >= 0; --p) {
+      const v4u x = *reinterpret_cast<const v4u*>(st + (p * KC + 16 * cb + j16) * PA + k * SL + V * g);
+      Mfma<DT>::step(in, make_uint4(x.x, x.y, x.z, x.w), rows[k]);
+    }
+  return in;
+}
+// The same with the state's transpose: rows of width KC, columns 16 kb .. + 15 of KA.
+template <typename DT, int KA, int KC>
+__device__ __forceinline__ f32x4 entered_across(const DT* st, const RowFrag<DT, KC>& rows, int kb, int g, int j16) {
+  constexpr int PA = KA + Tile<DT>::PAD, SL = Tile<DT>::SLICE;
+  f32x4 in = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < KC / SL; ++k) {
+    if constexpr (sizeof(DT) == 4) {
+      const float* const p = st + (k * SL + 4 * g) * PA + 16 * kb + j16;
+      Mfma<DT>::step(in, make_uint4(__float_as_uint(p[0]), __float_as_uint(p[PA]), __float_as_uint(p[2 * PA]), __float_as_uint(p[3 * PA])),
+                     rows[k]);
+    } else {
+#pragma unroll
+      for (int pl = 1; pl >= 0; --pl) {
+        const bf16_t* const p = st + (pl * KC + k * SL + 8 * g + j16 / 4) * PA + 16 * kb + 4 * (j16 % 4);
+        const v2u x = read_tr(p), y = read_tr(p + 4 * PA);
+        Mfma<DT>::step(in, make_uint4(x.x, x.y, y.x, y.y), rows[k]);
+      }
+    }
+  }
+  return in;
+}
+
+__device__ __forceinline__ uint64_t chunk_starts(const MixArgs& a, int b, int t0, int live) {
+  if (!a.resets) return 0;
+  const int lane = threadIdx.x & 63;
+  return __ballot(lane < live && a.resets[(long)(t0 + lane) * a.B + b] != 0);
+}
+
+// One sweep over a segment's chunks: the outputs of columns [ct, ct + KC), or, STATE,
+// the segment's own sum of the state alone.
+template <typename DT, int KA, int KC, bool REV, bool STATE, bool FAST>
+__device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct, DT* bl, DT* cl, DT* st) {
+  constexpr int PC = KC + Tile<DT>::PAD;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, j16 = lane & 15, r = 16 * w + j16;
+  const int wcols = min(KC, a.kc - ct);
+  const Rows<DT, KA, FAST> ra(a.a, at.b, at.n, a.ka, 0, a.ka), rb(a.b, at.b, at.n, a.ka, 0, a.ka);
+  const Rows<DT, KC, FAST> rc(a.c, at.b, at.n, a.kc, ct, wcols), ro(a.out, at.b, at.n, a.kc, ct, wcols);
+  Panel<DT, KA> pb;
+  Panel<DT, KC> pc;
+  RowFrag<DT, KA> next, now;
+  auto load = [&](int c) {
+    const int t0 = c * kChunk, live = min(at.len - t0, kChunk);
+    pb.template load<FAST>(rb, rb.at(t0, live));
+    pc.template load<FAST>(rc, rc.at(t0, live));
+    if constexpr (!STATE) next.template load<FAST>(ra, ra.at(t0, live), r, g);
+  };
+  const int steps = at.last - at.first;
+  if (steps > 0) load(REV ? at.last - 1 : at.first);
+  State<DT, KA, KC> S;
+  const float* s0 = STATE ? nullptr : a.seg ? a.seg + at.part * a.ka * a.kc : a.s0 ? a.s0 + at.bn * a.ka * a.kc : nullptr;
+  S.load(s0 ? s0 + (long)ct * a.st_c : nullptr, a.ka, wcols, a.st_a, a.st_c);
+  const Weights wt(at.la, r, g, a.s_intra);
+  float hold = 1.0f;
+  for (int step = 0; step < steps; ++step) {
+    const int c = REV ? at.last - 1 - step : at.first + step, t0 = c * kChunk;
+    const int live = min(at.len - t0, kChunk);  // steps of the chunk inside the sequence, 0 or less for none
+    const uint64_t starts = chunk_starts(a, at.b, t0, live);
+    __syncthreads();  // the chunk before is done with
+    pb.store(bl);
+    pc.store(cl);
+    if constexpr (!STATE) {
+      S.stage(st);
+      now = next;
+    }
+    if (step + 1 < steps) load(REV ? c - 1 : c + 1);
+    __syncthreads();
+    if constexpr (!STATE) {
+      const auto oc = ro.at(t0, min(a.T - t0, kChunk));
+      if (live <= 0) {
+        const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int cb = 0; cb < KC / 16; ++cb)
+          if (16 * cb < wcols) ro.store(oc, r, 16 * cb + 4 * g, zero);
+        continue;
+      }
+      const Mask<REV> mask(starts, live, r);
+      const float win = a.s_inter * decayed(at.la, REV ? live - 1 - r : r + 1);
+      const Intra<DT, KA, REV> P(bl, now, wt, mask, w, g, j16);
+#pragma unroll
+      for (int cb = 0; cb < KC / 16; ++cb) {
+        if (16 * cb >= wcols) break;
+        const f32x4 in = entered<DT, KA, KC>(st, now, cb, g, j16), own = P.template times<PC>(cl, cb, w, g, j16);
+        float v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = r < live ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+        ro.store(oc, r, 16 * cb + 4 * g, v);
+      }
+    }
+    if (live <= 0) continue;
+    if constexpr (STATE) hold = starts ? 0.0f : hold * decayed(at.la, live);
+    S.template take<REV>(bl, cl, starts, live, at.la, a.s_upd);
+  }
+  float* const s1 = STATE ? a.seg + at.part * a.ka * a.kc : a.seg || !a.s1 ? nullptr : a.s1 + at.bn * a.ka * a.kc;
+  if (s1) S.save(s1 + (long)ct * a.st_c, a.ka, wcols, a.st_a, a.st_c);
   if constexpr (STATE) {
-    if (tid == 0 && ct == 0) a.hold[part] = hold_all;
+    if (threadIdx.x == 0 && ct == 0) a.hold[at.part] = hold;
   }
+}
+
+template <typename DT, int KA, int KC, bool REV, bool STATE, bool FAST>
+__global__ void __launch_bounds__(kThreads, sizeof(DT) == 4 ? 2 : 3) k_mix(const MixArgs a) {
+  __shared__ __align__(16) DT bl[Panel<DT, KA>::SIZE];
+  __shared__ __align__(16) DT cl[Panel<DT, KC>::SIZE];
+  __shared__ __align__(16) DT st[STATE ? 16 : State<DT, KA, KC>::SIZE];
+  const int nct = (a.kc + KC - 1) / KC;
+  sweep<DT, KA, KC, REV, STATE, FAST>(a, Place(a, blockIdx.x / nct), blockIdx.x % nct * KC, bl, cl, st);
+}
+
+// The reverse sweep for both dk and dv: they share the sources q and dy and the
+// state G [K][V], which dk's rows v meet across.
+template <typename DT, int KP, int VP, bool FAST>
+__device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, const Place& at, DT* ql, DT* dl, DT* st) {
+  constexpr int PK = KP + Tile<DT>::PAD, PV = VP + Tile<DT>::PAD;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, j16 = lane & 15, r = 16 * w + j16;
+  // of dv: A = k, B = q, C = dy; a row's v are reached through c's place: dk = (A = v, B = dy, C = q)
+  const Rows<DT, KP, FAST> rk(a.a, at.b, at.n, a.ka, 0, a.ka), rq(a.b, at.b, at.n, a.ka, 0, a.ka), ok(dk, at.b, at.n, a.ka, 0, a.ka);
+  const Rows<DT, VP, FAST> rd(a.c, at.b, at.n, a.kc, 0, a.kc), rv(a.v, at.b, at.n, a.kc, 0, a.kc), ov(a.out, at.b, at.n, a.kc, 0, a.kc);
+  Panel<DT, KP> pq;
+  Panel<DT, VP> pd;
+  RowFrag<DT, KP> nk, k;
+  RowFrag<DT, VP> nv, v;
+  auto load = [&](int c) {
+    const int t0 = c * kChunk, live = min(at.len - t0, kChunk);
+    pq.template load<FAST>(rq, rq.at(t0, live));
+    pd.template load<FAST>(rd, rd.at(t0, live));
+    nk.template load<FAST>(rk, rk.at(t0, live), r, g);
+    nv.template load<FAST>(rv, rv.at(t0, live), r, g);
+  };
+  if (at.last > at.first) load(at.last - 1);
+  State<DT, KP, VP> S;
+  S.load(a.seg ? a.seg + at.part * a.ka * a.kc : a.s0 ? a.s0 + at.bn * a.ka * a.kc : nullptr, a.ka, a.kc, a.st_a, a.st_c);
+  const Weights wt(at.la, r, g, a.s_intra);
+  for (int c = at.last - 1; c >= at.first; --c) {
+    const int t0 = c * kChunk, live = min(at.len - t0, kChunk);
+    const uint64_t starts = chunk_starts(a, at.b, t0, live);
+    __syncthreads();
+    pq.store(ql);
+    pd.store(dl);
+    S.stage(st);
+    k = nk;
+    v = nv;
+    if (c > at.first) load(c - 1);
+    __syncthreads();
+    const auto ck = ok.at(t0, min(a.T - t0, kChunk));
+    const auto cv = ov.at(t0, min(a.T - t0, kChunk));
+    const Mask<true> mask(starts, live, r);
+    const float win = a.s_inter * decayed(at.la, live - 1 - r);
+    const bool on = r < live;
+    {
+      const Intra<DT, KP, true> P(ql, k, wt, mask, w, g, j16);
+#pragma unroll
+      for (int cb = 0; cb < VP / 16; ++cb) {
+        if (16 * cb >= a.kc) break;
+        const f32x4 in = entered<DT, KP, VP>(st, k, cb, g, j16), own = P.template times<PV>(dl, cb, w, g, j16);
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+        ov.store(cv, r, 16 * cb + 4 * g, x);
+      }
+    }
+    {
+      const Intra<DT, VP, true> P(dl, v, wt, mask, w, g, j16);
+#pragma unroll
+      for (int kb = 0; kb < KP / 16; ++kb) {
+        if (16 * kb >= a.ka) break;
+        const f32x4 in = entered_across<DT, KP, VP>(st, v, kb, g, j16), own = P.template times<PK>(ql, kb, w, g, j16);
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+        ok.store(ck, r, 16 * kb + 4 * g, x);
+      }
+    }
+    if (live > 0) S.template take<true>(ql, dl, starts, live, at.la, a.s_upd);
+  }
+  if (!a.seg && a.s1) S.save(a.s1 + at.bn * a.ka * a.kc, a.ka, a.kc, a.st_a, a.st_c);
+}
+
+// All three gradients of heads up to 64 wide: the forward sweep for dq, then the
+// reverse one for dk and dv, which finds k, v and dy in the caches where the
+// segment is short.
+template <typename DT, int KP, int VP, bool FAST>
+__global__ void __launch_bounds__(kThreads, sizeof(DT) == 4 ? 2 : 3) k_mix_grad(const MixArgs q, const MixArgs v, const SeqView dk) {
+  constexpr int SK = Panel<DT, KP>::SIZE, SV = Panel<DT, VP>::SIZE;
+  constexpr int ST = State<DT, KP, VP>::SIZE > State<DT, VP, KP>::SIZE ? State<DT, KP, VP>::SIZE : State<DT, VP, KP>::SIZE;
+  __shared__ __align__(16) DT kl[SK];
+  __shared__ __align__(16) DT vl[SV];
+  __shared__ __align__(16) DT st[ST];
+  const Place at(q, blockIdx.x);
+  sweep<DT, VP, KP, false, false, FAST>(q, at, 0, vl, kl, st);
+  __syncthreads();
+  sweep_back<DT, KP, VP, FAST>(v, dk, at, kl, vl, st);
 }
 
 // Runs through the segments' own sums: seg[i] becomes the state that enters it.
@@ -478,17 +710,44 @@ __global__ void __launch_bounds__(kThreads) k_linattn_step(const LinattnArgs a, 
 
 template <int N> using Const = std::integral_constant<int, N>;
 
+// Whether rows of N heads of width w can be read and written 16 bytes at a time with
+// 32-bit offsets, a chunk of them as one resource.
+bool fast_view(int dtype, const SeqView& v, int w) {
+  const long es = dtype == WM_FP32 ? 4 : 2, per = 16 / es;
+  return (w == 32 || w == 64 || w == 128) && (reinterpret_cast<uintptr_t>(v.p) & 15) == 0 && v.t % per == 0 && v.b % per == 0 &&
+         v.t >= w && v.t * es < (1L << 31) / (kChunk + 1);
+}
+
 template <bool REV, bool STATE>
 hipError_t launch_mix(const char* name, int dtype, const MixArgs& m, hipStream_t s) {
+  const bool fast = (STATE || (fast_view(dtype, m.a, m.ka) && fast_view(dtype, m.out, m.kc))) && fast_view(dtype, m.b, m.ka) &&
+                    fast_view(dtype, m.c, m.kc);
   auto go = [&](auto dt, auto ka, auto kc) {
     typedef decltype(dt) DT;
     const unsigned tiles = (unsigned)((m.kc + kc - 1) / kc);
-    return launch(name, k_mix<DT, ka, kc, REV, STATE>, dim3((unsigned)((long)m.B * m.N * m.nseg) * tiles), dim3(kThreads), 0,
+    const dim3 grid((unsigned)((long)m.B * m.N * m.nseg) * tiles);
+    return launch(name, fast ? k_mix<DT, ka, kc, REV, STATE, true> : k_mix<DT, ka, kc, REV, STATE, false>, grid, dim3(kThreads), 0,
                   s, m);
   };
   auto by = [&](auto dt) {
     auto cols = [&](auto ka) { return m.kc <= 32 ? go(dt, ka, Const<32>()) : go(dt, ka, Const<64>()); };
     return m.ka <= 32 ? cols(Const<32>()) : m.ka <= 64 ? cols(Const<64>()) : cols(Const<128>());
+  };
+  return dtype == WM_FP32 ? by(0.0f) : by(bf16_t());
+}
+
+hipError_t launch_mix_grad(int dtype, const MixArgs& q, const MixArgs& v, const SeqView& dk, hipStream_t s) {
+  const int K = v.ka, V = v.kc;
+  const bool fast = fast_view(dtype, v.a, K) && fast_view(dtype, v.b, K) && fast_view(dtype, v.c, V) && fast_view(dtype, v.v, V) &&
+                    fast_view(dtype, v.out, V) && fast_view(dtype, dk, K) && fast_view(dtype, q.out, K);
+  auto go = [&](auto dt, auto kp, auto vp) {
+    typedef decltype(dt) DT;
+    return launch("linattn_grad", fast ? k_mix_grad<DT, kp, vp, true> : k_mix_grad<DT, kp, vp, false>,
+                  dim3((unsigned)((long)v.B * v.N * v.nseg)), dim3(kThreads), 0, s, q, v, dk);
+  };
+  auto by = [&](auto dt) {
+    auto cols = [&](auto kp) { return V <= 32 ? go(dt, kp, Const<32>()) : go(dt, kp, Const<64>()); };
+    return K <= 32 ? cols(Const<32>()) : cols(Const<64>());
   };
   return dtype == WM_FP32 ? by(0.0f) : by(bf16_t());
 }
@@ -547,7 +806,7 @@ hipError_t launch_linattn(int dtype, const LinattnArgs& a, hipStream_t s) {
   }
   const Split sp = split_of(a.T, a.B, a.N);
   const long heads = (long)a.B * a.N;
-  MixArgs m{a.T, a.B, a.N, a.K, a.V, a.q, a.k, a.v, SeqView{a.y, (long)a.B * a.N * a.V, (long)a.N * a.V}, a.decay,
+  MixArgs m{a.T, a.B, a.N, a.K, a.V, a.q, a.k, a.v, SeqView{a.y, (long)a.B * a.N * a.V, (long)a.N * a.V}, {}, a.decay,
             a.scale, a.scale, 1.0f, a.h0, a.h_T, a.V, 1, a.resets, a.lengths, sp.nseg, sp.per, nullptr, nullptr};
   if (sp.nseg > 1) {
     place(m, a.ws, heads, a.K, a.V);
@@ -561,11 +820,11 @@ hipError_t launch_linattn_grad(int dtype, const LinattnGradArgs& a, hipStream_t 
   const Split sp = split_of(a.T, a.B, a.N);
   const long heads = (long)a.B * a.N;
   // the state and its transpose: [K][V] with strides (V, 1) of rows and columns, or (1, V)
-  MixArgs dq{a.T, a.B, a.N, a.V, a.K, a.dy, a.v, a.k, a.dq, a.decay, a.scale, a.scale, 1.0f, a.h0, nullptr, 1, a.V,
+  MixArgs dq{a.T, a.B, a.N, a.V, a.K, a.dy, a.v, a.k, a.dq, {}, a.decay, a.scale, a.scale, 1.0f, a.h0, nullptr, 1, a.V,
              a.resets, a.lengths, sp.nseg, sp.per, nullptr, nullptr};
-  MixArgs dv{a.T, a.B, a.N, a.K, a.V, a.k, a.q, a.dy, a.dv, a.decay, a.scale, 1.0f, a.scale, a.dh_T, a.dh0, a.V, 1,
+  MixArgs dv{a.T, a.B, a.N, a.K, a.V, a.k, a.q, a.dy, a.dv, a.v, a.decay, a.scale, 1.0f, a.scale, a.dh_T, a.dh0, a.V, 1,
              a.resets, a.lengths, sp.nseg, sp.per, nullptr, nullptr};
-  MixArgs dk{a.T, a.B, a.N, a.V, a.K, a.v, a.dy, a.q, a.dk, a.decay, a.scale, 1.0f, a.scale, a.dh_T, nullptr, 1, a.V,
+  MixArgs dk{a.T, a.B, a.N, a.V, a.K, a.v, a.dy, a.q, a.dk, {}, a.decay, a.scale, 1.0f, a.scale, a.dh_T, nullptr, 1, a.V,
              a.resets, a.lengths, sp.nseg, sp.per, nullptr, nullptr};
   hipError_t e;
   if (sp.nseg > 1) {
@@ -576,6 +835,7 @@ hipError_t launch_linattn_grad(int dtype, const LinattnGradArgs& a, hipStream_t 
     if ((e = segments<false>(dtype, dq, nullptr, s)) != hipSuccess) return e;
     if ((e = segments<true>(dtype, dv, a.dh0, s)) != hipSuccess) return e;
   }
+  if (a.K <= 64 && a.V <= 64) return launch_mix_grad(dtype, dq, dv, a.dk, s);
   if ((e = launch_mix<false, false>("linattn_dq", dtype, dq, s)) != hipSuccess) return e;
   if ((e = launch_mix<true, false>("linattn_dk", dtype, dk, s)) != hipSuccess) return e;
   return launch_mix<true, false>("linattn_dv", dtype, dv, s);
