@@ -96,8 +96,21 @@ __device__ __forceinline__ v2u read_tr(const bf16_t* p) {
 }
 __device__ __forceinline__ bf16x8 join(v2u a, v2u b) { return __builtin_bit_cast(bf16x8, v4u{a.x, a.y, b.x, b.y}); }
 
-// a^n from log2 a, 1 for n = 0 also where a = 0.
-__device__ __forceinline__ float decayed(float la, int n) { return n > 0 ? __builtin_amdgcn_exp2f(la * (float)n) : 1.0f; }
+// The same value, which the compiler takes for another one in every round of a loop:
+// what follows from it (weights, places in LDS, the sources' numbers) is computed
+// again for each chunk in place of a hundred registers held over all of them.
+__device__ __forceinline__ int anew(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+__device__ __forceinline__ float anew(float v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
+
+// a^n from log2 a (finite: log2 of 0 is held at kLogZero, so that a^0 = 1 there too).
+constexpr float kLogZero = -1e30f;
+__device__ __forceinline__ float decayed(float la, int n) { return __builtin_amdgcn_exp2f(la * (float)n); }
 
 // Rows of one sequence and head of a [T, B, N, width] array.  FAST: as wide as the
 // tile, on 16-byte boundaries and near enough for 32-bit offsets: range-checked
@@ -202,7 +215,7 @@ struct Place {
     n = (int)(bn % a.N);
     b = (int)(bn / a.N);
     len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
-    la = log2f(fminf(fmaxf(a.decay[n], 0.0f), 1.0f));
+    la = fmaxf(log2f(fminf(fmaxf(a.decay[n], 0.0f), 1.0f)), kLogZero);
     const int chunks = (a.T + kChunk - 1) / kChunk;
     first = seg * a.per;
     last = min(first + a.per, chunks);
@@ -281,7 +294,8 @@ struct State {
   // S becomes hold S + sum over the sources s in [lo, hi] of upd a^distance B_s C_s^T,
   // distance to the end of the chunk that the sweep leaves by; 0 at a reset, whatever S holds
   template <bool REV>
-  __device__ __forceinline__ void take(const DT* bl, const DT* cl, uint64_t starts, int live, float la, float upd) {
+  __device__ __forceinline__ void take(const DT* bl, const DT* cl, uint64_t starts, int live, int lane, float la, float upd) {
+    const int g = lane >> 4, j16 = lane & 15;
     const float hold = decayed(la, live);
     const int lo = REV ? 0 : starts ? 63 - __clzll((long long)starts) : 0;
     const int hi = REV ? (starts ? __ffsll((long long)starts) - 2 : live - 1) : live - 1;
@@ -311,7 +325,7 @@ struct State {
           }
 #pragma unroll
           for (int k = 0; k < KCB; ++k) {
-            const float y = cl[s * PC + col(k)];
+            const float y = cl[s * PC + 16 * (wc * KCB + k) + j16];
 #pragma unroll
             for (int i = 0; i < KAB; ++i) S[i][k] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y, S[i][k], 0, 0, 0);
           }
@@ -347,17 +361,6 @@ struct State {
   }
 };
 
-// a^|r - s| for the sources s = 16 j + 4 g + e of the lane's row, times `scale`
-struct Weights {
-  float w[4][4];
-  __device__ __forceinline__ Weights(float la, int r, int g, float scale) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[j][e] = scale * decayed(la, abs(r - (16 * j + 4 * g + e)));
-  }
-};
-
 // The chunk's part of the rows of wave w: the weighted products of a row with its
 // sources as a matrix operand, and their product with the sources' values.
 template <typename DT, int KA, bool REV>
@@ -366,8 +369,9 @@ struct Intra {
   static constexpr int PA = KA + Tile<DT>::PAD, SL = Tile<DT>::SLICE, V = Tile<DT>::VEC;
   float P[4][4];
   bf16x8 ph[2], pm[2];
-  __device__ __forceinline__ Intra(const DT* bl, const RowFrag<DT, KA>& rows, const Weights& wt, const Mask<REV>& mask, int w, int g,
-                                   int j16) {
+  // r: the lane's row; la, scale: a source s weighs scale a^|r - s|
+  __device__ __forceinline__ Intra(const DT* bl, const RowFrag<DT, KA>& rows, float la, float scale, const Mask<REV>& mask, int r,
+                                   int w, int g, int j16) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -381,7 +385,7 @@ struct Intra {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int s = 16 * j + 4 * g + e;
-        P[j][e] = s >= mask.lo && s <= mask.hi ? acc[e] * wt.w[j][e] : 0.0f;
+        P[j][e] = s >= mask.lo && s <= mask.hi ? acc[e] * (scale * decayed(la, REV ? s - r : r - s)) : 0.0f;
       }
     }
     if constexpr (!F32) {
@@ -473,38 +477,36 @@ __device__ __forceinline__ uint64_t chunk_starts(const MixArgs& a, int b, int t0
 template <typename DT, int KA, int KC, bool REV, bool STATE, bool FAST>
 __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct, DT* bl, DT* cl, DT* st) {
   constexpr int PC = KC + Tile<DT>::PAD;
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, j16 = lane & 15, r = 16 * w + j16;
+  const int w = threadIdx.x >> 6, lane0 = threadIdx.x & 63;
   const int wcols = min(KC, a.kc - ct);
   const Rows<DT, KA, FAST> ra(a.a, at.b, at.n, a.ka, 0, a.ka), rb(a.b, at.b, at.n, a.ka, 0, a.ka);
   const Rows<DT, KC, FAST> rc(a.c, at.b, at.n, a.kc, ct, wcols), ro(a.out, at.b, at.n, a.kc, ct, wcols);
   Panel<DT, KA> pb;
   Panel<DT, KC> pc;
-  RowFrag<DT, KA> next, now;
+  RowFrag<DT, KA> rows;
   auto load = [&](int c) {
+    const int lane = anew(lane0), g = lane >> 4, r = 16 * w + (lane & 15);
     const int t0 = c * kChunk, live = min(at.len - t0, kChunk);
     pb.template load<FAST>(rb, rb.at(t0, live));
     pc.template load<FAST>(rc, rc.at(t0, live));
-    if constexpr (!STATE) next.template load<FAST>(ra, ra.at(t0, live), r, g);
+    if constexpr (!STATE) rows.template load<FAST>(ra, ra.at(t0, live), r, g);
   };
   const int steps = at.last - at.first;
   if (steps > 0) load(REV ? at.last - 1 : at.first);
   State<DT, KA, KC> S;
   const float* s0 = STATE ? nullptr : a.seg ? a.seg + at.part * a.ka * a.kc : a.s0 ? a.s0 + at.bn * a.ka * a.kc : nullptr;
   S.load(s0 ? s0 + (long)ct * a.st_c : nullptr, a.ka, wcols, a.st_a, a.st_c);
-  const Weights wt(at.la, r, g, a.s_intra);
   float hold = 1.0f;
   for (int step = 0; step < steps; ++step) {
     const int c = REV ? at.last - 1 - step : at.first + step, t0 = c * kChunk;
     const int live = min(at.len - t0, kChunk);  // steps of the chunk inside the sequence, 0 or less for none
     const uint64_t starts = chunk_starts(a, at.b, t0, live);
+    const int lane = anew(lane0), g = lane >> 4, j16 = lane & 15, r = 16 * w + j16;
+    const float la = anew(at.la);
     __syncthreads();  // the chunk before is done with
     pb.store(bl);
     pc.store(cl);
-    if constexpr (!STATE) {
-      S.stage(st);
-      now = next;
-    }
-    if (step + 1 < steps) load(REV ? c - 1 : c + 1);
+    if constexpr (!STATE) S.stage(st);
     __syncthreads();
     if constexpr (!STATE) {
       const auto oc = ro.at(t0, min(a.T - t0, kChunk));
@@ -513,24 +515,28 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
 #pragma unroll
         for (int cb = 0; cb < KC / 16; ++cb)
           if (16 * cb < wcols) ro.store(oc, r, 16 * cb + 4 * g, zero);
+        if (step + 1 < steps) load(REV ? c - 1 : c + 1);
         continue;
       }
       const Mask<REV> mask(starts, live, r);
-      const float win = a.s_inter * decayed(at.la, REV ? live - 1 - r : r + 1);
-      const Intra<DT, KA, REV> P(bl, now, wt, mask, w, g, j16);
+      const float win = a.s_inter * decayed(la, REV ? live - 1 - r : r + 1);
+      const Intra<DT, KA, REV> P(bl, rows, la, a.s_intra, mask, r, w, g, j16);
 #pragma unroll
       for (int cb = 0; cb < KC / 16; ++cb) {
         if (16 * cb >= wcols) break;
-        const f32x4 in = entered<DT, KA, KC>(st, now, cb, g, j16), own = P.template times<PC>(cl, cb, w, g, j16);
+        const f32x4 in = entered<DT, KA, KC>(st, rows, cb, g, j16), own = P.template times<PC>(cl, cb, w, g, j16);
         float v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = r < live ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
         ro.store(oc, r, 16 * cb + 4 * g, v);
       }
     }
+    // (requested here, the rows in registers being done with, the pieces take no more registers
+    // than the products above)
+    if (step + 1 < steps) load(REV ? c - 1 : c + 1);
     if (live <= 0) continue;
-    if constexpr (STATE) hold = starts ? 0.0f : hold * decayed(at.la, live);
-    S.template take<REV>(bl, cl, starts, live, at.la, a.s_upd);
+    if constexpr (STATE) hold = starts ? 0.0f : hold * decayed(la, live);
+    S.template take<REV>(bl, cl, starts, live, lane, la, a.s_upd);
   }
   float* const s1 = STATE ? a.seg + at.part * a.ka * a.kc : a.seg || !a.s1 ? nullptr : a.s1 + at.bn * a.ka * a.kc;
   if (s1) S.save(s1 + (long)ct * a.st_c, a.ka, wcols, a.st_a, a.st_c);
@@ -539,8 +545,14 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
   }
 }
 
+// Waves a SIMD that the registers are to admit: as many as LDS does.
+constexpr int waves(int size, int ka, int kc, bool fast) {
+  if (ka > 64) return size == 4 ? (kc > 32 ? 1 : 2) : (kc > 32 ? 2 : 3);
+  return (size == 4 ? 3 : 4) - !fast;
+}
+
 template <typename DT, int KA, int KC, bool REV, bool STATE, bool FAST>
-__global__ void __launch_bounds__(kThreads, sizeof(DT) == 4 ? 2 : 3) k_mix(const MixArgs a) {
+__global__ void __launch_bounds__(kThreads, waves(sizeof(DT), KA, KC, FAST)) k_mix(const MixArgs a) {
   __shared__ __align__(16) DT bl[Panel<DT, KA>::SIZE];
   __shared__ __align__(16) DT cl[Panel<DT, KC>::SIZE];
   __shared__ __align__(16) DT st[STATE ? 16 : State<DT, KA, KC>::SIZE];
@@ -553,43 +565,42 @@ __global__ void __launch_bounds__(kThreads, sizeof(DT) == 4 ? 2 : 3) k_mix(const
 template <typename DT, int KP, int VP, bool FAST>
 __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, const Place& at, DT* ql, DT* dl, DT* st) {
   constexpr int PK = KP + Tile<DT>::PAD, PV = VP + Tile<DT>::PAD;
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, j16 = lane & 15, r = 16 * w + j16;
+  const int w = threadIdx.x >> 6, lane0 = threadIdx.x & 63;
   // of dv: A = k, B = q, C = dy; a row's v are reached through c's place: dk = (A = v, B = dy, C = q)
   const Rows<DT, KP, FAST> rk(a.a, at.b, at.n, a.ka, 0, a.ka), rq(a.b, at.b, at.n, a.ka, 0, a.ka), ok(dk, at.b, at.n, a.ka, 0, a.ka);
   const Rows<DT, VP, FAST> rd(a.c, at.b, at.n, a.kc, 0, a.kc), rv(a.v, at.b, at.n, a.kc, 0, a.kc), ov(a.out, at.b, at.n, a.kc, 0, a.kc);
   Panel<DT, KP> pq;
   Panel<DT, VP> pd;
-  RowFrag<DT, KP> nk, k;
-  RowFrag<DT, VP> nv, v;
+  RowFrag<DT, KP> k;
+  RowFrag<DT, VP> v;
   auto load = [&](int c) {
+    const int lane = anew(lane0), g = lane >> 4, r = 16 * w + (lane & 15);
     const int t0 = c * kChunk, live = min(at.len - t0, kChunk);
     pq.template load<FAST>(rq, rq.at(t0, live));
     pd.template load<FAST>(rd, rd.at(t0, live));
-    nk.template load<FAST>(rk, rk.at(t0, live), r, g);
-    nv.template load<FAST>(rv, rv.at(t0, live), r, g);
+    k.template load<FAST>(rk, rk.at(t0, live), r, g);
+    v.template load<FAST>(rv, rv.at(t0, live), r, g);
   };
   if (at.last > at.first) load(at.last - 1);
   State<DT, KP, VP> S;
   S.load(a.seg ? a.seg + at.part * a.ka * a.kc : a.s0 ? a.s0 + at.bn * a.ka * a.kc : nullptr, a.ka, a.kc, a.st_a, a.st_c);
-  const Weights wt(at.la, r, g, a.s_intra);
   for (int c = at.last - 1; c >= at.first; --c) {
     const int t0 = c * kChunk, live = min(at.len - t0, kChunk);
     const uint64_t starts = chunk_starts(a, at.b, t0, live);
+    const int lane = anew(lane0), g = lane >> 4, j16 = lane & 15, r = 16 * w + j16;
+    const float la = anew(at.la);
     __syncthreads();
     pq.store(ql);
     pd.store(dl);
     S.stage(st);
-    k = nk;
-    v = nv;
-    if (c > at.first) load(c - 1);
     __syncthreads();
     const auto ck = ok.at(t0, min(a.T - t0, kChunk));
     const auto cv = ov.at(t0, min(a.T - t0, kChunk));
     const Mask<true> mask(starts, live, r);
-    const float win = a.s_inter * decayed(at.la, live - 1 - r);
+    const float win = a.s_inter * decayed(la, live - 1 - r);
     const bool on = r < live;
     {
-      const Intra<DT, KP, true> P(ql, k, wt, mask, w, g, j16);
+      const Intra<DT, KP, true> P(ql, k, la, a.s_intra, mask, r, w, g, j16);
 #pragma unroll
       for (int cb = 0; cb < VP / 16; ++cb) {
         if (16 * cb >= a.kc) break;
@@ -601,7 +612,7 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
       }
     }
     {
-      const Intra<DT, VP, true> P(dl, v, wt, mask, w, g, j16);
+      const Intra<DT, VP, true> P(dl, v, la, a.s_intra, mask, r, w, g, j16);
 #pragma unroll
       for (int kb = 0; kb < KP / 16; ++kb) {
         if (16 * kb >= a.ka) break;
@@ -612,7 +623,8 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
         ok.store(ck, r, 16 * kb + 4 * g, x);
       }
     }
-    if (live > 0) S.template take<true>(ql, dl, starts, live, at.la, a.s_upd);
+    if (c > at.first) load(c - 1);
+    if (live > 0) S.template take<true>(ql, dl, starts, live, lane, la, a.s_upd);
   }
   if (!a.seg && a.s1) S.save(a.s1 + at.bn * a.ka * a.kc, a.ka, a.kc, a.st_a, a.st_c);
 }
@@ -621,7 +633,7 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
 // reverse one for dk and dv, which finds k, v and dy in the caches where the
 // segment is short.
 template <typename DT, int KP, int VP, bool FAST>
-__global__ void __launch_bounds__(kThreads, sizeof(DT) == 4 ? 2 : 3) k_mix_grad(const MixArgs q, const MixArgs v, const SeqView dk) {
+__global__ void __launch_bounds__(kThreads, waves(sizeof(DT), KP, VP, FAST)) k_mix_grad(const MixArgs q, const MixArgs v, const SeqView dk) {
   constexpr int SK = Panel<DT, KP>::SIZE, SV = Panel<DT, VP>::SIZE;
   constexpr int ST = State<DT, KP, VP>::SIZE > State<DT, VP, KP>::SIZE ? State<DT, KP, VP>::SIZE : State<DT, VP, KP>::SIZE;
   __shared__ __align__(16) DT kl[SK];
@@ -634,7 +646,10 @@ __global__ void __launch_bounds__(kThreads, sizeof(DT) == 4 ? 2 : 3) k_mix_grad(
 }
 
 // Runs through the segments' own sums: seg[i] becomes the state that enters it.
-// One value of a head's state a thread.
+// One value of a head's state a thread; the sums of kAhead segments are requested
+// together (one after the other, each store before the next load, 64 segments of 16
+// heads of 64 x 64 take 15 us).
+constexpr int kAhead = 16;
 template <bool REV>
 __global__ void __launch_bounds__(kThreads) k_segments(float* seg, const float* hold, const float* s0, float* s1, int nseg,
                                                        int width) {
@@ -642,14 +657,22 @@ __global__ void __launch_bounds__(kThreads) k_segments(float* seg, const float* 
   const long bn = blockIdx.y;
   if (i >= width) return;
   float s = s0 ? s0[bn * width + i] : 0.0f;
-  float* p = seg + bn * nseg * (long)width + i;
-  const float* h = hold + bn * nseg;
-#pragma unroll 8
-  for (int k = 0; k < nseg; ++k) {
-    const int m = REV ? nseg - 1 - k : k;
-    const float own = p[(long)m * width], f = h[m];
-    p[(long)m * width] = s;
-    s = f != 0.0f ? fmaf(f, s, own) : own;
+  float* const p = seg + bn * nseg * (long)width + i;
+  const float* const h = hold + bn * nseg;
+  for (int k = 0; k < nseg; k += kAhead) {
+    float own[kAhead], f[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int m = min(k + j, nseg - 1), at = REV ? nseg - 1 - m : m;
+      own[j] = p[(long)at * width];
+      f[j] = h[at];
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (k + j >= nseg) break;
+      p[(long)(REV ? nseg - 1 - k - j : k + j) * width] = s;
+      s = f[j] != 0.0f ? fmaf(f[j], s, own[j]) : own[j];
+    }
   }
   if (s1) s1[bn * width + i] = s;
 }
