@@ -566,8 +566,11 @@ wm_status wm_qk_norm_grad(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, i
  *   lengths [B] int32, nullable (T; values outside [0, T] act as clamped).
  *   y [T, B, N, V] in dtype; h_T [B, N, K, V] float32, nullable, may be h0: the
  *   state after the last step (T = 1 with h0 and h_T is the form for acting).
- *   workspace            of wm_linattn_workspace_bytes, 0 bytes where the call does
- *                        not split the time axis.
+ *   states               nullable: a 256-byte aligned buffer of
+ *                        wm_linattn_states_bytes that receives what
+ *                        wm_linattn_grad needs.
+ *   workspace            of wm_linattn_workspace_bytes, also for the gradient; both
+ *                        0 bytes where the call does not split the time axis.
  * The steps of a sequence are taken 64 at a time, from its first, by matrix
  * products: a value of a head that is not finite can make every output of that
  * sequence and head in the same 64 steps not finite, earlier steps and other
@@ -575,17 +578,18 @@ wm_status wm_qk_norm_grad(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, i
  * K and V in 1 .. 128; scale finite; T B, B N, T B N K and T B N V at most 2^31 - 1
  * and B N K V at most 2^31 - 1.  B = 0 is a no-op; T = 0 gives h_T = h0.
  */
+size_t wm_linattn_states_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V);
 size_t wm_linattn_workspace_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V);
 wm_status wm_linattn(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, int32_t V,
                      const void *q, int64_t q_t, int64_t q_b, const void *k, int64_t k_t,
                      int64_t k_b, const void *v, int64_t v_t, int64_t v_b, const float *decay,
                      float scale, const float *h0, const uint8_t *resets, const int32_t *lengths,
-                     void *y, float *h_T, void *workspace, size_t workspace_bytes,
-                     wm_stream_t stream);
+                     void *y, float *h_T, void *states, size_t states_bytes, void *workspace,
+                     size_t workspace_bytes, wm_stream_t stream);
 
 /*
- * Gradient of wm_linattn by the reverse recurrence, from its inputs.  With G the
- * gradient of the state after step t from all later ones, G_{T-1} = grad_h_T, and
+ * Gradient of wm_linattn by the reverse recurrence, from its inputs and the states
+ * that it saved.  With G the gradient of the state after step t from all later ones, G_{T-1} = grad_h_T, and
  * F_t = G_t + scale q_t grad_y_t^T for a step inside its sequence:
  *   grad_q_t = scale S_t grad_y_t,  grad_k_t = F_t v_t,  grad_v_t = F_t^T k_t,
  *   G_{t-1} = a F_t, or 0 at a reset;  grad_h0 = G_{-1}.
@@ -594,16 +598,16 @@ wm_status wm_linattn(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, 
  *   grad_h_T [B, N, K, V] float32, nullable (0); grad_h0 [B, N, K, V] float32,
  *   nullable, may be grad_h_T.
  */
-size_t wm_linattn_grad_workspace_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V);
 wm_status wm_linattn_grad(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, int32_t V,
                           const void *q, int64_t q_t, int64_t q_b, const void *k, int64_t k_t,
                           int64_t k_b, const void *v, int64_t v_t, int64_t v_b,
                           const float *decay, float scale, const float *h0, const uint8_t *resets,
                           const int32_t *lengths, const void *grad_y, int64_t grad_y_t,
-                          int64_t grad_y_b, const float *grad_h_T, void *grad_q, int64_t grad_q_t,
-                          int64_t grad_q_b, void *grad_k, int64_t grad_k_t, int64_t grad_k_b,
-                          void *grad_v, int64_t grad_v_t, int64_t grad_v_b, float *grad_h0,
-                          void *workspace, size_t workspace_bytes, wm_stream_t stream);
+                          int64_t grad_y_b, const float *grad_h_T, const void *states,
+                          size_t states_bytes, void *grad_q, int64_t grad_q_t, int64_t grad_q_b,
+                          void *grad_k, int64_t grad_k_t, int64_t grad_k_b, void *grad_v,
+                          int64_t grad_v_t, int64_t grad_v_b, float *grad_h0, void *workspace,
+                          size_t workspace_bytes, wm_stream_t stream);
 
 /*
  * Gated projection of a feed-forward block (its second, plain product is the

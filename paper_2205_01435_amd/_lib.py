@@ -33,7 +33,7 @@ EXPORTS = ("wm_packed_weights_bytes", "wm_pack_weights", "wm_workspace_bytes", "
            "wm_layer_norm_grad_workspace_bytes", "wm_layer_norm_grad", "wm_linrec_states_bytes",
            "wm_linrec_workspace_bytes", "wm_linrec", "wm_linrec_grad", "wm_clip_grads_workspace_bytes",
            "wm_clip_grads", "wm_rotary_table", "wm_qk_norm", "wm_qk_norm_grad_workspace_bytes", "wm_qk_norm_grad",
-           "wm_linattn_workspace_bytes", "wm_linattn", "wm_linattn_grad_workspace_bytes", "wm_linattn_grad", "wm_glu",
+           "wm_linattn_states_bytes", "wm_linattn_workspace_bytes", "wm_linattn", "wm_linattn_grad", "wm_glu",
            "wm_glu_grad_workspace_bytes", "wm_glu_grad",
            "wm_profile_enable", "wm_profile_read", "wm_profile_reset", "wm_profile_phases",
            "wm_profile_phases_read", "wm_workspace_status",
@@ -134,13 +134,13 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.wm_qk_norm_grad.argtypes = [I32, I64, I32, I32, I32, I32, I32, P, I64, P, I64, P, P, F32, P, P, P, I64, P, I64,
                                     P, I64, P, I64, P, P, P, SZ, P]
     lib.wm_qk_norm_grad.restype = I32
-    for f in (lib.wm_linattn_workspace_bytes, lib.wm_linattn_grad_workspace_bytes):
+    for f in (lib.wm_linattn_states_bytes, lib.wm_linattn_workspace_bytes):
         f.argtypes, f.restype = [I32, I32, I32, I32, I32], SZ
     lib.wm_linattn.argtypes = [I32, I32, I32, I32, I32, I32, P, I64, I64, P, I64, I64, P, I64, I64, P, F32, P, P, P, P, P,
-                               P, SZ, P]
+                               P, SZ, P, SZ, P]
     lib.wm_linattn.restype = I32
     lib.wm_linattn_grad.argtypes = [I32, I32, I32, I32, I32, I32, P, I64, I64, P, I64, I64, P, I64, I64, P, F32, P, P, P,
-                                    P, I64, I64, P, P, I64, I64, P, I64, I64, P, I64, I64, P, P, SZ, P]
+                                    P, I64, I64, P, P, SZ, P, I64, I64, P, I64, I64, P, I64, I64, P, P, SZ, P]
     lib.wm_linattn_grad.restype = I32
     lib.wm_glu.argtypes = [I32, I64, I32, I32, I32, P, I64, P, P, I64, P, P]
     lib.wm_glu.restype = I32
@@ -942,7 +942,8 @@ def qk_norm_grad(q, k, dq_out, dk_out, positions, rotary: Rotary | None, gamma_q
 
 class LinattnBuffers:
     """Output [T, B, N, V], final state [B, N, K, V] and workspace of linear
-    attention; with ``grad`` the gradients (dq, dk and dv contiguous)."""
+    attention; with ``grad`` the saved states and the gradients (dq, dk and dv
+    contiguous)."""
 
     def __init__(self, T: int, B: int, N: int, K: int, V: int, dtype=torch.float32, device="cuda", grad: bool = True):
         self.T, self.B, self.N, self.K, self.V, self.dtype = T, B, N, K, V, dtype
@@ -951,9 +952,10 @@ class LinattnBuffers:
         state = lambda: torch.empty((B, N, K, V), dtype=torch.float32, device=device)  # noqa: E731
         self.y, self.h_T = seq(V), state()
         self.dq, self.dk, self.dv, self.dh0 = (seq(K), seq(K), seq(V), state()) if grad else (None,) * 4
-        size = lib.wm_linattn_grad_workspace_bytes if grad else lib.wm_linattn_workspace_bytes
-        self.ws_bytes = max(size(T, B, N, K, V), lib.wm_linattn_workspace_bytes(T, B, N, K, V))
+        self.ws_bytes = lib.wm_linattn_workspace_bytes(T, B, N, K, V)
         self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=device)
+        self.states_bytes = lib.wm_linattn_states_bytes(T, B, N, K, V) if grad else 0
+        self.states = torch.empty(max(self.states_bytes, 1), dtype=torch.uint8, device=device) if grad else None
 
 
 def _steps(name, t, shape, dtype, device):
@@ -968,7 +970,7 @@ def _steps(name, t, shape, dtype, device):
     return st[0], st[1]
 
 
-def _linattn_args(q, k, v, decay, h0, resets, lengths, bufs, grad):
+def _linattn_args(q, k, v, decay, h0, resets, lengths, bufs):
     dt = _act("q", q)
     dev, dtype = q.device, q.dtype
     _here(dev)
@@ -984,7 +986,7 @@ def _linattn_args(q, k, v, decay, h0, resets, lengths, bufs, grad):
     pr = _arr("resets", resets, _mask_dtype(resets), (T, B), dev, optional=True)
     pl = _arr("lengths", lengths, torch.int32, (B,), dev, optional=True)
     if bufs is None:
-        bufs = LinattnBuffers(T, B, N, K, V, dtype, dev, grad=grad)
+        bufs = LinattnBuffers(T, B, N, K, V, dtype, dev)
     if (bufs.T, bufs.B, bufs.N, bufs.K, bufs.V, bufs.dtype) != (T, B, N, K, V, dtype) or bufs.y.device != dev:
         raise ValueError(f"buffers for T={bufs.T} B={bufs.B} N={bufs.N} K={bufs.K} V={bufs.V} {bufs.dtype} on "
                          f"{bufs.y.device}; the call has T={T} B={B} N={N} K={K} V={V} {dtype} on {dev}")
@@ -997,25 +999,27 @@ def linattn(q, k, v, decay, scale: float = 1.0, h0=None, resets=None, lengths=No
     """Launch wm_linattn on the current stream: S_t = decay S_{t-1} + k_t v_t^T,
     y_t = scale S_t^T q_t for every head over ``q``, ``k`` [T, B, N, K] and
     ``v`` [T, B, N, V] (decay [N] float32; resets [T, B] uint8: the step starts
-    a new trajectory; lengths [B] int32).  Returns the filled buffers (y, h_T)."""
-    head, masks, bufs = _linattn_args(q, k, v, decay, h0, resets, lengths, bufs, False)
-    _check(load().wm_linattn(*head, scale, *masks, bufs.y.data_ptr(), bufs.h_T.data_ptr(), bufs.workspace.data_ptr(),
-                             bufs.ws_bytes, _stream()))
+    a new trajectory; lengths [B] int32).  Returns the filled buffers (y, h_T, and
+    the states that linattn_grad reads)."""
+    head, masks, bufs = _linattn_args(q, k, v, decay, h0, resets, lengths, bufs)
+    _check(load().wm_linattn(*head, scale, *masks, bufs.y.data_ptr(), bufs.h_T.data_ptr(), _ptr(bufs.states),
+                             bufs.states_bytes, bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
     return bufs
 
 
 def linattn_grad(q, k, v, decay, dy, scale: float = 1.0, h0=None, dh_T=None, resets=None, lengths=None,
                  bufs: LinattnBuffers | None = None) -> LinattnBuffers:
     """Launch wm_linattn_grad on the current stream: dq, dk, dv and dh0 from the
-    forward call's inputs and the gradients of its outputs."""
-    head, masks, bufs = _linattn_args(q, k, v, decay, h0, resets, lengths, bufs, True)
-    if bufs.dq is None:
-        raise ValueError("linattn_grad needs buffers made with grad=True")
+    forward call's inputs, the gradients of its outputs and the states in its
+    ``bufs``."""
+    if bufs is None or bufs.states is None:
+        raise ValueError("linattn_grad needs the forward call's buffers, made with grad=True")
+    head, masks, bufs = _linattn_args(q, k, v, decay, h0, resets, lengths, bufs)
     T, B, N, K, V = bufs.T, bufs.B, bufs.N, bufs.K, bufs.V
     yt, yb = _steps("dy", dy, (T, B, N, V), q.dtype, q.device)
     ph = _arr("dh_T", dh_T, torch.float32, (B, N, K, V), q.device, optional=True)
-    _check(load().wm_linattn_grad(*head, scale, *masks, dy.data_ptr(), yt, yb, ph, bufs.dq.data_ptr(), B * N * K, N * K,
-                                  bufs.dk.data_ptr(), B * N * K, N * K, bufs.dv.data_ptr(), B * N * V, N * V,
+    _check(load().wm_linattn_grad(*head, scale, *masks, dy.data_ptr(), yt, yb, ph, bufs.states.data_ptr(),
+                                  bufs.states_bytes, bufs.dq.data_ptr(), B * N * K, N * K, bufs.dk.data_ptr(), B * N * K, N * K, bufs.dv.data_ptr(), B * N * V, N * V,
                                   bufs.dh0.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
     return bufs
 

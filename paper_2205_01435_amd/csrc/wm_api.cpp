@@ -798,14 +798,14 @@ size_t wm_linattn_workspace_bytes(int32_t T, int32_t B, int32_t N, int32_t K, in
   return check_linattn(T, B, N, K, V) == WM_OK ? wm::linattn_workspace(T, B, N, K, V) : 0;
 }
 
-size_t wm_linattn_grad_workspace_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V) {
-  return check_linattn(T, B, N, K, V) == WM_OK ? wm::linattn_grad_workspace(T, B, N, K, V) : 0;
+size_t wm_linattn_states_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V) {
+  return check_linattn(T, B, N, K, V) == WM_OK ? wm::linattn_states(T, B, N, K, V) : 0;
 }
 
 wm_status wm_linattn(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, int32_t V, const void* q, int64_t q_t,
                      int64_t q_b, const void* k, int64_t k_t, int64_t k_b, const void* v, int64_t v_t, int64_t v_b,
                      const float* decay, float scale, const float* h0, const uint8_t* resets, const int32_t* lengths, void* y,
-                     float* h_T, void* workspace, size_t workspace_bytes, wm_stream_t stream) {
+                     float* h_T, void* states, size_t states_bytes, void* workspace, size_t workspace_bytes, wm_stream_t stream) {
   wm_status st = check_dtype(dtype);
   if (st != WM_OK || (st = check_linattn(T, B, N, K, V)) != WM_OK) return st;
   const int64_t rk = (int64_t)N * K, rv = (int64_t)N * V;
@@ -819,11 +819,12 @@ wm_status wm_linattn(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, 
     return fail(WM_ERR_INVALID_ARG, "decay, h0, lengths and h_T must be 4-byte aligned");
   if (B == 0) return ok();
   if (!decay) return fail(WM_ERR_INVALID_ARG, "decay is required");
+  if (states && (st = check_workspace("states", states, states_bytes, wm::linattn_states(T, B, N, K, V))) != WM_OK) return st;
   if ((st = check_workspace("the workspace of wm_linattn", workspace, workspace_bytes,
                             wm::linattn_workspace(T, B, N, K, V))) != WM_OK)
     return st;
   const wm::LinattnArgs a{T, B, N, K, V, {q, (long)q_t, (long)q_b}, {k, (long)k_t, (long)k_b}, {v, (long)v_t, (long)v_b},
-                          decay, scale, h0, resets, lengths, y, h_T, workspace};
+                          decay, scale, h0, resets, lengths, y, h_T, reinterpret_cast<float*>(states), workspace};
   const hipError_t e = wm::launch_linattn(dtype, a, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "wm_linattn");
   return ok();
@@ -832,10 +833,10 @@ wm_status wm_linattn(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, 
 wm_status wm_linattn_grad(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, int32_t V, const void* q, int64_t q_t,
                           int64_t q_b, const void* k, int64_t k_t, int64_t k_b, const void* v, int64_t v_t, int64_t v_b,
                           const float* decay, float scale, const float* h0, const uint8_t* resets, const int32_t* lengths,
-                          const void* grad_y, int64_t grad_y_t, int64_t grad_y_b, const float* grad_h_T, void* grad_q,
-                          int64_t grad_q_t, int64_t grad_q_b, void* grad_k, int64_t grad_k_t, int64_t grad_k_b, void* grad_v,
-                          int64_t grad_v_t, int64_t grad_v_b, float* grad_h0, void* workspace, size_t workspace_bytes,
-                          wm_stream_t stream) {
+                          const void* grad_y, int64_t grad_y_t, int64_t grad_y_b, const float* grad_h_T, const void* states,
+                          size_t states_bytes, void* grad_q, int64_t grad_q_t, int64_t grad_q_b, void* grad_k, int64_t grad_k_t,
+                          int64_t grad_k_b, void* grad_v, int64_t grad_v_t, int64_t grad_v_b, float* grad_h0, void* workspace,
+                          size_t workspace_bytes, wm_stream_t stream) {
   wm_status st = check_dtype(dtype);
   if (st != WM_OK || (st = check_linattn(T, B, N, K, V)) != WM_OK) return st;
   const int64_t rk = (int64_t)N * K, rv = (int64_t)N * V;
@@ -852,13 +853,15 @@ wm_status wm_linattn_grad(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_
     return fail(WM_ERR_INVALID_ARG, "decay, h0, lengths, grad_h_T and grad_h0 must be 4-byte aligned");
   if (B == 0) return ok();
   if (!decay) return fail(WM_ERR_INVALID_ARG, "decay is required");
-  if ((st = check_workspace("the workspace of wm_linattn_grad", workspace, workspace_bytes,
-                            wm::linattn_grad_workspace(T, B, N, K, V))) != WM_OK)
+  if ((st = check_workspace("states", states, states_bytes, wm::linattn_states(T, B, N, K, V))) != WM_OK ||
+      (st = check_workspace("the workspace of wm_linattn_grad", workspace, workspace_bytes,
+                            wm::linattn_workspace(T, B, N, K, V))) != WM_OK)
     return st;
   const wm::LinattnGradArgs a{T, B, N, K, V, {q, (long)q_t, (long)q_b}, {k, (long)k_t, (long)k_b}, {v, (long)v_t, (long)v_b},
                               {grad_y, (long)grad_y_t, (long)grad_y_b}, {grad_q, (long)grad_q_t, (long)grad_q_b},
                               {grad_k, (long)grad_k_t, (long)grad_k_b}, {grad_v, (long)grad_v_t, (long)grad_v_b},
-                              decay, scale, h0, resets, lengths, grad_h_T, grad_h0, workspace};
+                              decay, scale, h0, resets, lengths, grad_h_T,
+                              reinterpret_cast<const float*>(states), grad_h0, workspace};
   const hipError_t e = wm::launch_linattn_grad(dtype, a, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "wm_linattn_grad");
   return ok();

@@ -48,6 +48,7 @@ struct LinattnArgs {
   const int32_t* lengths;  // [B] or null (T)
   void* y;                 // [T, B, N, V]
   float* h_T;              // [B, N, K, V] or null
+  float* states;           // linattn_states bytes or null
   void* ws;
 };
 struct LinattnGradArgs {
@@ -59,11 +60,12 @@ struct LinattnGradArgs {
   const uint8_t* resets;
   const int32_t* lengths;
   const float* dh_T;  // [B, N, K, V] or null (0)
-  float* dh0;         // or null
+  const float* states;
+  float* dh0;  // or null
   void* ws;
 };
-size_t linattn_workspace(int T, int B, int N, int K, int V);
-size_t linattn_grad_workspace(int T, int B, int N, int K, int V);
+size_t linattn_states(int T, int B, int N, int K, int V);     // bytes
+size_t linattn_workspace(int T, int B, int N, int K, int V);  // bytes
 hipError_t launch_linattn(int dtype, const LinattnArgs& a, hipStream_t s);
 hipError_t launch_linattn_grad(int dtype, const LinattnGradArgs& a, hipStream_t s);
 

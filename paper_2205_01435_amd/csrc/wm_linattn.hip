@@ -235,6 +235,44 @@ struct Mask {
   }
 };
 
+// What a chunk's sources weigh: for the lane's row, the source s = 16 j + 4 g + e;
+// and on their way into the state, s = 32 jj + 16 (e / 4) + 4 g + e % 4.  bf16 sweeps,
+// whose time goes to such arithmetic, keep both in registers and compute them again
+// only where a chunk has resets or padding, or follows one that has (T 32768, 16
+// heads of 64: outputs 81 -> 76 us, gradient 193 -> 186, states 42 -> 35); fp32 ones, whose time goes
+// to the matrix unit, have no registers for them.
+template <typename DT, bool REV>
+struct Weights {
+  static constexpr bool KEPT = sizeof(DT) == 2;
+  float w[KEPT ? 4 : 1][4], u[KEPT ? 2 : 1][8];
+  bool whole = false;  // those of a whole chunk of one trajectory
+  // the sources that the state takes
+  __device__ __forceinline__ static float taken(uint64_t starts, int live, int s, float la, float upd) {
+    const int lo = REV ? 0 : starts ? 63 - __clzll((long long)starts) : 0;
+    const int hi = REV ? (starts ? __ffsll((long long)starts) - 2 : live - 1) : live - 1;
+    return s >= lo && s <= hi ? upd * decayed(la, REV ? s + 1 : live - 1 - s) : 0.0f;
+  }
+  __device__ __forceinline__ void update(const Mask<REV>& mask, uint64_t starts, int live, int r, int g, float la, float intra,
+                                         float upd) {
+    if constexpr (KEPT) {
+      const bool plain = starts == 0 && live == kChunk;
+      if (plain && whole) return;
+      whole = plain;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[j][e] = of(mask, 16 * j + 4 * g + e, r, la, intra);
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[jj][e] = taken(starts, live, 32 * jj + 16 * (e / 4) + 4 * g + e % 4, la, upd);
+    }
+  }
+  __device__ __forceinline__ static float of(const Mask<REV>& mask, int s, int r, float la, float intra) {
+    return s >= mask.lo && s <= mask.hi ? intra * decayed(la, REV ? s - r : r - s) : 0.0f;
+  }
+};
+
 // The state of a head, [KA][KC], in the registers of four waves: blocks of rows
 // 16 (wk KAB + i) + 4 g + 0..3 and column 16 (wc KCB + k) + j16.
 template <typename DT, int KA, int KC>
@@ -291,37 +329,41 @@ struct State {
         }
       }
   }
-  // S becomes hold S + sum over the sources s in [lo, hi] of upd a^distance B_s C_s^T,
-  // distance to the end of the chunk that the sweep leaves by; 0 at a reset, whatever S holds
+  // S becomes hold S + sum over the sources of their weight times B_s C_s^T, the weights'
+  // distances counting to the end of the chunk that the sweep leaves by; at a reset
+  // hold S is 0, whatever S is
   template <bool REV>
-  __device__ __forceinline__ void take(const DT* bl, const DT* cl, uint64_t starts, int live, int lane, float la, float upd) {
+  __device__ __forceinline__ void take(const DT* bl, const DT* cl, const Weights<DT, REV>& wt, uint64_t starts, int live, int lane,
+                                       float la, float upd) {
     const int g = lane >> 4, j16 = lane & 15;
-    const float hold = decayed(la, live);
-    const int lo = REV ? 0 : starts ? 63 - __clzll((long long)starts) : 0;
-    const int hi = REV ? (starts ? __ffsll((long long)starts) - 2 : live - 1) : live - 1;
+    if (starts) {
 #pragma unroll
-    for (int i = 0; i < KAB; ++i)
+      for (int i = 0; i < KAB; ++i)
 #pragma unroll
-      for (int k = 0; k < KCB; ++k)
+        for (int k = 0; k < KCB; ++k) S[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    } else {
+      const float hold = decayed(la, live);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) S[i][k][e] = starts ? 0.0f : S[i][k][e] * hold;
+      for (int i = 0; i < KAB; ++i)
+#pragma unroll
+        for (int k = 0; k < KCB; ++k)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) S[i][k][e] *= hold;
+    }
 #pragma unroll
     for (int jj = 0; jj < 2; ++jj) {
-      float ws[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int s = 32 * jj + 16 * (e / 4) + 4 * g + e % 4;
-        ws[e] = s >= lo && s <= hi ? upd * decayed(la, REV ? s + 1 : live - 1 - s) : 0.0f;
-      }
+      if (32 * jj >= live) break;  // nothing but padding from here on
       if constexpr (F32) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
+          if (32 * jj + 16 * (e / 4) >= live) break;
           const int s = 32 * jj + 16 * (e / 4) + 4 * g + e % 4;
+          const float ws = Weights<DT, REV>::taken(starts, live, s, la, upd);
           float x[KAB];
 #pragma unroll
           for (int i = 0; i < KAB; ++i) {
             const float v = bl[s * PA + 16 * (wk * KAB + i) + j16];
-            x[i] = ws[e] != 0.0f ? v * ws[e] : 0.0f;
+            x[i] = v * ws;
           }
 #pragma unroll
           for (int k = 0; k < KCB; ++k) {
@@ -340,8 +382,8 @@ struct State {
           float f[8];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            f[2 * e] = ws[2 * e] != 0.0f ? __uint_as_float(u[e] << 16) * ws[2 * e] : 0.0f;
-            f[2 * e + 1] = ws[2 * e + 1] != 0.0f ? __uint_as_float(u[e] & 0xffff0000u) * ws[2 * e + 1] : 0.0f;
+            f[2 * e] = __uint_as_float(u[e] << 16) * wt.u[jj][2 * e];
+            f[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u) * wt.u[jj][2 * e + 1];
           }
           x[i] = split3(f);
         }
@@ -369,13 +411,12 @@ struct Intra {
   static constexpr int PA = KA + Tile<DT>::PAD, SL = Tile<DT>::SLICE, V = Tile<DT>::VEC;
   float P[4][4];
   bf16x8 ph[2], pm[2];
-  // r: the lane's row; la, scale: a source s weighs scale a^|r - s|
-  __device__ __forceinline__ Intra(const DT* bl, const RowFrag<DT, KA>& rows, float la, float scale, const Mask<REV>& mask, int r,
-                                   int w, int g, int j16) {
+  __device__ __forceinline__ Intra(const DT* bl, const RowFrag<DT, KA>& rows, const Weights<DT, REV>& wt, const Mask<REV>& mask,
+                                   int r, int w, int g, int j16, int live, float la, float scale) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-      if (REV ? j >= w : j <= w) {
+      if (REV ? j >= w && 16 * j < live : j <= w) {
 #pragma unroll
         for (int k = 0; k < KA / SL; ++k) {
           const v4u x = *reinterpret_cast<const v4u*>(bl + (16 * j + j16) * PA + k * SL + V * g);
@@ -385,7 +426,10 @@ struct Intra {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int s = 16 * j + 4 * g + e;
-        P[j][e] = s >= mask.lo && s <= mask.hi ? acc[e] * (scale * decayed(la, REV ? s - r : r - s)) : 0.0f;
+        if constexpr (F32)
+          P[j][e] = acc[e] * Weights<DT, REV>::of(mask, s, r, la, scale);
+        else
+          P[j][e] = acc[e] * wt.w[j][e];
       }
     }
     if constexpr (!F32) {
@@ -405,12 +449,12 @@ struct Intra {
   }
   // columns 16 cb .. + 15 of the values at cl (pitch PC)
   template <int PC>
-  __device__ __forceinline__ f32x4 times(const DT* cl, int cb, int w, int g, int j16) const {
+  __device__ __forceinline__ f32x4 times(const DT* cl, int cb, int w, int g, int j16, int live) const {
     f32x4 out = {0.f, 0.f, 0.f, 0.f};
     if constexpr (F32) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (REV ? j < w : j > w) continue;
+        if (REV ? j < w || 16 * j >= live : j > w) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           out = __builtin_amdgcn_mfma_f32_16x16x4f32(cl[(16 * j + 4 * g + e) * PC + 16 * cb + j16], P[j][e], out, 0, 0, 0);
@@ -418,7 +462,7 @@ struct Intra {
     } else {
 #pragma unroll
       for (int jj = 0; jj < 2; ++jj) {
-        if (REV ? 2 * jj + 1 < w : 2 * jj > w) continue;
+        if (REV ? 2 * jj + 1 < w || 32 * jj >= live : 2 * jj > w) continue;
         const bf16_t* const p = cl + (32 * jj + 4 * g + j16 / 4) * PC + 16 * cb + 4 * (j16 % 4);
         const bf16x8 x = join(read_tr(p), read_tr(p + 16 * PC));
         out = mfma_bf16(x, pm[jj], out);
@@ -496,6 +540,7 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
   State<DT, KA, KC> S;
   const float* s0 = STATE ? nullptr : a.seg ? a.seg + at.part * a.ka * a.kc : a.s0 ? a.s0 + at.bn * a.ka * a.kc : nullptr;
   S.load(s0 ? s0 + (long)ct * a.st_c : nullptr, a.ka, wcols, a.st_a, a.st_c);
+  Weights<DT, REV> wt;
   float hold = 1.0f;
   for (int step = 0; step < steps; ++step) {
     const int c = REV ? at.last - 1 - step : at.first + step, t0 = c * kChunk;
@@ -508,27 +553,27 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
     pc.store(cl);
     if constexpr (!STATE) S.stage(st);
     __syncthreads();
+    const Mask<REV> mask(starts, live, r);
+    if (live > 0) wt.update(mask, starts, live, r, g, la, a.s_intra, a.s_upd);
     if constexpr (!STATE) {
       const auto oc = ro.at(t0, min(a.T - t0, kChunk));
-      if (live <= 0) {
+      if (16 * w >= live) {  // the wave's rows are padding
         const float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int cb = 0; cb < KC / 16; ++cb)
           if (16 * cb < wcols) ro.store(oc, r, 16 * cb + 4 * g, zero);
-        if (step + 1 < steps) load(REV ? c - 1 : c + 1);
-        continue;
-      }
-      const Mask<REV> mask(starts, live, r);
-      const float win = a.s_inter * decayed(la, REV ? live - 1 - r : r + 1);
-      const Intra<DT, KA, REV> P(bl, rows, la, a.s_intra, mask, r, w, g, j16);
+      } else {
+        const float win = a.s_inter * decayed(la, REV ? live - 1 - r : r + 1);
+        const Intra<DT, KA, REV> P(bl, rows, wt, mask, r, w, g, j16, live, la, a.s_intra);
 #pragma unroll
-      for (int cb = 0; cb < KC / 16; ++cb) {
-        if (16 * cb >= wcols) break;
-        const f32x4 in = entered<DT, KA, KC>(st, rows, cb, g, j16), own = P.template times<PC>(cl, cb, w, g, j16);
-        float v[4];
+        for (int cb = 0; cb < KC / 16; ++cb) {
+          if (16 * cb >= wcols) break;
+          const f32x4 in = entered<DT, KA, KC>(st, rows, cb, g, j16), own = P.template times<PC>(cl, cb, w, g, j16, live);
+          float v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = r < live ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
-        ro.store(oc, r, 16 * cb + 4 * g, v);
+          for (int e = 0; e < 4; ++e) v[e] = r < live ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+          ro.store(oc, r, 16 * cb + 4 * g, v);
+        }
       }
     }
     // (requested here, the rows in registers being done with, the pieces take no more registers
@@ -536,7 +581,7 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
     if (step + 1 < steps) load(REV ? c - 1 : c + 1);
     if (live <= 0) continue;
     if constexpr (STATE) hold = starts ? 0.0f : hold * decayed(la, live);
-    S.template take<REV>(bl, cl, starts, live, lane, la, a.s_upd);
+    S.template take<REV>(bl, cl, wt, starts, live, lane, la, a.s_upd);
   }
   float* const s1 = STATE ? a.seg + at.part * a.ka * a.kc : a.seg || !a.s1 ? nullptr : a.s1 + at.bn * a.ka * a.kc;
   if (s1) S.save(s1 + (long)ct * a.st_c, a.ka, wcols, a.st_a, a.st_c);
@@ -548,7 +593,7 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
 // Waves a SIMD that the registers are to admit: as many as LDS does.
 constexpr int waves(int size, int ka, int kc, bool fast) {
   if (ka > 64) return size == 4 ? (kc > 32 ? 1 : 2) : (kc > 32 ? 2 : 3);
-  return (size == 4 ? 3 : 4) - !fast;
+  return size == 4 ? 3 - !fast : 3;
 }
 
 template <typename DT, int KA, int KC, bool REV, bool STATE, bool FAST>
@@ -584,6 +629,7 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
   if (at.last > at.first) load(at.last - 1);
   State<DT, KP, VP> S;
   S.load(a.seg ? a.seg + at.part * a.ka * a.kc : a.s0 ? a.s0 + at.bn * a.ka * a.kc : nullptr, a.ka, a.kc, a.st_a, a.st_c);
+  Weights<DT, true> wt;
   for (int c = at.last - 1; c >= at.first; --c) {
     const int t0 = c * kChunk, live = min(at.len - t0, kChunk);
     const uint64_t starts = chunk_starts(a, at.b, t0, live);
@@ -597,34 +643,45 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
     const auto ck = ok.at(t0, min(a.T - t0, kChunk));
     const auto cv = ov.at(t0, min(a.T - t0, kChunk));
     const Mask<true> mask(starts, live, r);
-    const float win = a.s_inter * decayed(la, live - 1 - r);
-    const bool on = r < live;
-    {
-      const Intra<DT, KP, true> P(ql, k, la, a.s_intra, mask, r, w, g, j16);
+    if (live > 0) wt.update(mask, starts, live, r, g, la, a.s_intra, a.s_upd);
+    if (16 * w >= live) {  // the wave's rows are padding
+      const float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int cb = 0; cb < VP / 16; ++cb) {
-        if (16 * cb >= a.kc) break;
-        const f32x4 in = entered<DT, KP, VP>(st, k, cb, g, j16), own = P.template times<PV>(dl, cb, w, g, j16);
-        float x[4];
+      for (int cb = 0; cb < VP / 16; ++cb)
+        if (16 * cb < a.kc) ov.store(cv, r, 16 * cb + 4 * g, zero);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
-        ov.store(cv, r, 16 * cb + 4 * g, x);
+      for (int kb = 0; kb < KP / 16; ++kb)
+        if (16 * kb < a.ka) ok.store(ck, r, 16 * kb + 4 * g, zero);
+    } else {
+      const float win = a.s_inter * decayed(la, live - 1 - r);
+      const bool on = r < live;
+      {
+        const Intra<DT, KP, true> P(ql, k, wt, mask, r, w, g, j16, live, la, a.s_intra);
+#pragma unroll
+        for (int cb = 0; cb < VP / 16; ++cb) {
+          if (16 * cb >= a.kc) break;
+          const f32x4 in = entered<DT, KP, VP>(st, k, cb, g, j16), own = P.template times<PV>(dl, cb, w, g, j16, live);
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+          ov.store(cv, r, 16 * cb + 4 * g, x);
+        }
       }
-    }
-    {
-      const Intra<DT, VP, true> P(dl, v, la, a.s_intra, mask, r, w, g, j16);
+      {
+        const Intra<DT, VP, true> P(dl, v, wt, mask, r, w, g, j16, live, la, a.s_intra);
 #pragma unroll
-      for (int kb = 0; kb < KP / 16; ++kb) {
-        if (16 * kb >= a.ka) break;
-        const f32x4 in = entered_across<DT, KP, VP>(st, v, kb, g, j16), own = P.template times<PK>(ql, kb, w, g, j16);
-        float x[4];
+        for (int kb = 0; kb < KP / 16; ++kb) {
+          if (16 * kb >= a.ka) break;
+          const f32x4 in = entered_across<DT, KP, VP>(st, v, kb, g, j16), own = P.template times<PK>(ql, kb, w, g, j16, live);
+          float x[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
-        ok.store(ck, r, 16 * kb + 4 * g, x);
+          for (int e = 0; e < 4; ++e) x[e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+          ok.store(ck, r, 16 * kb + 4 * g, x);
+        }
       }
     }
     if (c > at.first) load(c - 1);
-    if (live > 0) S.template take<true>(ql, dl, starts, live, lane, la, a.s_upd);
+    if (live > 0) S.template take<true>(ql, dl, wt, starts, live, lane, la, a.s_upd);
   }
   if (!a.seg && a.s1) S.save(a.s1 + at.bn * a.ka * a.kc, a.ka, a.kc, a.st_a, a.st_c);
 }
@@ -787,13 +844,8 @@ Split split_of(int T, int B, int N) {
   const int per = (chunks + want - 1) / want;
   return {(chunks + per - 1) / per, per};
 }
-size_t seg_bytes(long heads, int nseg, int K, int V) {
-  return ((size_t)heads * nseg * K * V * sizeof(float) + 255) / 256 * 256 + ((size_t)heads * nseg * sizeof(float) + 255) / 256 * 256;
-}
-void place(MixArgs& m, void* ws, long heads, int K, int V) {
-  m.seg = reinterpret_cast<float*>(ws);
-  m.hold = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + ((size_t)heads * m.nseg * K * V * sizeof(float) + 255) / 256 * 256);
-}
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+size_t seg_bytes(long heads, int nseg, int K, int V) { return align256((size_t)heads * nseg * K * V * sizeof(float)); }
 
 template <bool REV>
 hipError_t segments(int dtype, MixArgs m, float* s1, hipStream_t s) {
@@ -809,11 +861,15 @@ hipError_t segments(int dtype, MixArgs m, float* s1, hipStream_t s) {
 
 }  // namespace
 
-size_t linattn_workspace(int T, int B, int N, int K, int V) {
+size_t linattn_states(int T, int B, int N, int K, int V) {
   const Split sp = split_of(T, B, N);
   return sp.nseg > 1 ? seg_bytes((long)B * N, sp.nseg, K, V) : 0;
 }
-size_t linattn_grad_workspace(int T, int B, int N, int K, int V) { return 2 * linattn_workspace(T, B, N, K, V); }
+size_t linattn_workspace(int T, int B, int N, int K, int V) {
+  const Split sp = split_of(T, B, N);
+  const long heads = (long)B * N;
+  return sp.nseg > 1 ? seg_bytes(heads, sp.nseg, K, V) + align256((size_t)heads * sp.nseg * sizeof(float)) : 0;
+}
 
 hipError_t launch_linattn(int dtype, const LinattnArgs& a, hipStream_t s) {
   if (a.T == 1) {
@@ -832,7 +888,9 @@ hipError_t launch_linattn(int dtype, const LinattnArgs& a, hipStream_t s) {
   MixArgs m{a.T, a.B, a.N, a.K, a.V, a.q, a.k, a.v, SeqView{a.y, (long)a.B * a.N * a.V, (long)a.N * a.V}, {}, a.decay,
             a.scale, a.scale, 1.0f, a.h0, a.h_T, a.V, 1, a.resets, a.lengths, sp.nseg, sp.per, nullptr, nullptr};
   if (sp.nseg > 1) {
-    place(m, a.ws, heads, a.K, a.V);
+    const size_t own = seg_bytes(heads, sp.nseg, a.K, a.V);
+    m.seg = a.states ? a.states : reinterpret_cast<float*>(a.ws);
+    m.hold = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + own);
     const hipError_t e = segments<false>(dtype, m, a.h_T, s);
     if (e != hipSuccess) return e;
   }
@@ -851,11 +909,9 @@ hipError_t launch_linattn_grad(int dtype, const LinattnGradArgs& a, hipStream_t 
              a.resets, a.lengths, sp.nseg, sp.per, nullptr, nullptr};
   hipError_t e;
   if (sp.nseg > 1) {
-    char* ws = reinterpret_cast<char*>(a.ws);
-    place(dq, ws, heads, a.K, a.V);
-    place(dv, ws + seg_bytes(heads, sp.nseg, a.K, a.V), heads, a.K, a.V);
-    place(dk, ws + seg_bytes(heads, sp.nseg, a.K, a.V), heads, a.K, a.V);
-    if ((e = segments<false>(dtype, dq, nullptr, s)) != hipSuccess) return e;
+    dq.seg = const_cast<float*>(a.states);
+    dv.seg = dk.seg = reinterpret_cast<float*>(a.ws);
+    dv.hold = reinterpret_cast<float*>(reinterpret_cast<char*>(a.ws) + seg_bytes(heads, sp.nseg, a.K, a.V));
     if ((e = segments<true>(dtype, dv, a.dh0, s)) != hipSuccess) return e;
   }
   if (a.K <= 64 && a.V <= 64) return launch_mix_grad(dtype, dq, dv, a.dk, s);

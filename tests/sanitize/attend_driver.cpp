@@ -52,7 +52,7 @@ static void sizes() {
       for (int32_t N : hs)
         for (int32_t K : ds)
           for (int32_t V : ds) {
-            const size_t f = wm_linattn_workspace_bytes(T, B, N, K, V), g = wm_linattn_grad_workspace_bytes(T, B, N, K, V);
+            const size_t f = wm_linattn_workspace_bytes(T, B, N, K, V), g = wm_linattn_states_bytes(T, B, N, K, V);
             const bool in = T >= 0 && B >= 0 && N > 0 && K > 0 && K <= 128 && V > 0 && V <= 128;
             const __int128 most = INT32_MAX, w = K > V ? K : V;
             const bool ok = in && (__int128)T * B <= most && (__int128)B * N * K * V <= most && (__int128)T * B * N * w <= most;
@@ -164,16 +164,17 @@ static void attn() {
     const int32_t* len = I;
     void* y = P;
     float* hT = F;
-    void* ws = P;
-    size_t less = 0;
+    void *ws = P, *st = P;
+    size_t less = 0, sless = 0;
     wm_status fwd() const {
       const size_t b = wm_linattn_workspace_bytes(T, B, N, K, V);
-      return wm_linattn(dt, T, B, N, K, V, q, qt, qb, k, 32, 16, v, vt, vb, decay, scale, h0, U, len, y, hT, ws, b - less, nullptr);
+      return wm_linattn(dt, T, B, N, K, V, q, qt, qb, k, 32, 16, v, vt, vb, decay, scale, h0, U, len, y, hT, st, wm_linattn_states_bytes(T, B, N, K, V) - sless, ws,
+                        b - less, nullptr);
     }
     wm_status grad() const {
-      const size_t b = wm_linattn_grad_workspace_bytes(T, B, N, K, V);
-      return wm_linattn_grad(dt, T, B, N, K, V, q, qt, qb, k, 32, 16, v, vt, vb, decay, scale, h0, U, len, P, 16, 8, hT, y, ot, ob,
-                             P, 32, 16, P, 16, 8, F, ws, b - less, nullptr);
+      const size_t b = wm_linattn_workspace_bytes(T, B, N, K, V);
+      return wm_linattn_grad(dt, T, B, N, K, V, q, qt, qb, k, 32, 16, v, vt, vb, decay, scale, h0, U, len, P, 16, 8, hT, st,
+                             wm_linattn_states_bytes(T, B, N, K, V) - sless, y, ot, ob, P, 32, 16, P, 16, 8, F, ws, b - less, nullptr);
     }
   };
   EXPECT(wm_linattn_workspace_bytes(600, 2, 2, 8, 4) > 0);
@@ -204,6 +205,11 @@ static void attn() {
   bad([](A& a) { a.ws = nullptr; }, WM_ERR_WORKSPACE);
   bad([](A& a) { a.less = 1; }, WM_ERR_WORKSPACE);
   bad([](A& a) { a.ws = fake<void>(4100); }, WM_ERR_INVALID_ARG);
+  bad([](A& a) { a.sless = 1; }, WM_ERR_WORKSPACE);
+  bad([](A& a) { a.st = fake<void>(4100); }, WM_ERR_INVALID_ARG);
+  A none;
+  none.st = nullptr;
+  EXPECT(none.grad() == WM_ERR_WORKSPACE);
   bad([](A& a) { a.B = 0; }, WM_OK);
   A overlap;
   overlap.ot = 31;

@@ -103,6 +103,10 @@ def test_attention_and_gradient(T, B, N, K, V, dtype, masks):
         got = [getattr(bufs, n).clone() for n in ("y", "h_T", "dq", "dk", "dv", "dh0")]
         assert first is None or all(torch.equal(a, b) for a, b in zip(first, got))
         first = got
+    # without the states that the gradient reads
+    alone = wm.LinattnBuffers(T, B, N, K, V, TORCH[dtype], grad=False)
+    _run(d, alone, scale, grad=False)
+    assert torch.equal(alone.y, bufs.y) and torch.equal(alone.h_T, bufs.h_T)
 
 
 @pytest.mark.parametrize("T,B,N,K,V,dtype", [(1, 2, 2, 8, 8, "fp32"), (70, 2, 2, 20, 20, "bf16"), (400, 1, 2, 32, 48, "fp32")])
@@ -329,7 +333,9 @@ def test_refusals():
     with pytest.raises(ValueError):
         wm.linattn_grad(**ok, dy=v, bufs=wm.LinattnBuffers(4, 2, 3, 8, 5, grad=False))
     with pytest.raises(ValueError):
-        wm.linattn_grad(**ok, dy=q)
+        wm.linattn_grad(**ok, dy=v)
+    with pytest.raises(ValueError):
+        wm.linattn_grad(**ok, dy=q, bufs=wm.LinattnBuffers(4, 2, 3, 8, 5))
     with pytest.raises(wm.WmError) as e:
         wm.linattn(z(2, 1, 1, 129), z(2, 1, 1, 129), z(2, 1, 1, 4), z(1))
     assert e.value.status == wm.WM_ERR_UNSUPPORTED
@@ -341,3 +347,9 @@ def test_refusals():
     with pytest.raises(wm.WmError) as e:
         wm.linattn_grad(long, long, long, z(1), long, bufs=bufs)
     assert e.value.status == wm.WM_ERR_WORKSPACE
+    bufs = wm.LinattnBuffers(600, 1, 1, 8, 8)
+    bufs.states_bytes -= 1
+    for f in (lambda: wm.linattn(long, long, long, z(1), bufs=bufs), lambda: wm.linattn_grad(long, long, long, z(1), long, bufs=bufs)):
+        with pytest.raises(wm.WmError) as e:
+            f()
+        assert e.value.status == wm.WM_ERR_WORKSPACE
