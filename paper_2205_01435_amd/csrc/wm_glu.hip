@@ -25,43 +25,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTile = 128;  // outputs of a tile in each direction
 
-typedef uint32_t __attribute__((ext_vector_type(4))) v4u;
-typedef uint32_t __attribute__((ext_vector_type(2))) v2u;
-typedef v4u __attribute__((aligned(2))) v4u_2;
-typedef v4u __attribute__((aligned(4))) v4u_4;
-typedef v2u __attribute__((aligned(2))) v2u_2;
-
 template <typename DT> struct El;
 template <> struct El<float> {
   static constexpr int VEC = 4, BK = 32;
-  typedef v4u_4 mem;
 };
 template <> struct El<bf16_t> {
   static constexpr int VEC = 8, BK = 64;
-  typedef v4u_2 mem;
 };
-
-template <typename DT>
-__device__ __forceinline__ v4u load_piece(const DT* row, long c, long width) {
-  constexpr int V = El<DT>::VEC;
-  if (c + V <= width) return *reinterpret_cast<const typename El<DT>::mem*>(row + c);
-  v4u r = {0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (c + i < width) {
-      if constexpr (sizeof(DT) == 4)
-        r[i] = __float_as_uint(row[c + i]);
-      else
-        r[i / 2] |= (uint32_t)row[c + i] << (16 * (i & 1));
-    }
-  return r;
-}
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ v2u read_tr(const bf16_t* p) {
-  typedef __attribute__((address_space(3))) s16x4* lds_t;
-  return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)p));
-}
 
 // One operand: rows of `ld` elements.  Along k: row i of the tile is output i,
 // columns are k.  Across: row k, columns are outputs.
@@ -497,11 +467,69 @@ __device__ __forceinline__ void store_piece(DT* row, long c, long width, const f
       r = v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
     else
       r = v4u{pack2_bf16(v[0], v[1]), pack2_bf16(v[2], v[3]), pack2_bf16(v[4], v[5]), pack2_bf16(v[6], v[7])};
-    *reinterpret_cast<typename El<DT>::mem*>(row + c) = r;
+    *reinterpret_cast<typename Mem16<DT>::type*>(row + c) = r;
   } else {
 #pragma unroll
     for (int e = 0; e < V; ++e)
       if (c + e < width) DType<DT>::store(row, c + e, v[e]);
+  }
+}
+
+// Up to 64 rows, where the time is that of reading W: a work-group takes sixteen
+// columns of both factors, its eight waves a share of k each, straight from memory
+// into matrix operands, kFewAhead slices on their way at a time; the waves' sums are
+// added in LDS in order.
+constexpr int kFewRows = 64, kFewWaves = 8, kFewAhead = 4;
+template <typename DT, int MB>
+__global__ void __launch_bounds__(64 * kFewWaves) k_glu_few(const ProductArgs a) {
+  constexpr int V = El<DT>::VEC, SL = 4 * V;
+  __shared__ f32x4 sum[kFewWaves][2 * MB][64];
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
+  const long n0 = (long)blockIdx.x * 16;
+  const DT* const W = reinterpret_cast<const DT*>(a.P.p);
+  const DT* const pg = W + min(n0 + j, a.N - 1) * a.P.ld;
+  const DT* const pu = pg + a.N * a.P.ld;
+  const DT* px[MB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) px[m] = reinterpret_cast<const DT*>(a.Q.p) + min(16L * m + j, a.M - 1) * a.Q.ld;
+  f32x4 acc[2][MB];
+#pragma unroll
+  for (int m = 0; m < MB; ++m) acc[0][m] = acc[1][m] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // slices of k in runs of kFewAhead, dealt to the waves in turn
+  const long slices = (a.K + SL - 1) / SL;
+  for (long s0 = (long)w * kFewAhead; s0 < slices; s0 += kFewWaves * kFewAhead) {
+    v4u rg[kFewAhead], ru[kFewAhead], rx[kFewAhead][MB];
+#pragma unroll
+    for (int t = 0; t < kFewAhead; ++t) {
+      const long k = (s0 + t) * SL + V * g;
+      rg[t] = load_piece<DT>(pg, k, a.K);
+      ru[t] = load_piece<DT>(pu, k, a.K);
+#pragma unroll
+      for (int m = 0; m < MB; ++m) rx[t][m] = load_piece<DT>(px[m], k, a.K);
+    }
+#pragma unroll
+    for (int t = 0; t < kFewAhead; ++t)
+#pragma unroll
+      for (int m = 0; m < MB; ++m) {
+        const uint4 x = make_uint4(rx[t][m].x, rx[t][m].y, rx[t][m].z, rx[t][m].w);
+        Mfma<DT>::step(acc[0][m], make_uint4(rg[t].x, rg[t].y, rg[t].z, rg[t].w), x);
+        Mfma<DT>::step(acc[1][m], make_uint4(ru[t].x, ru[t].y, ru[t].z, ru[t].w), x);
+      }
+  }
+#pragma unroll
+  for (int m = 0; m < MB; ++m) {
+    sum[w][2 * m][lane] = acc[0][m];
+    sum[w][2 * m + 1][lane] = acc[1][m];
+  }
+  __syncthreads();
+  for (int m = w; m < MB; m += kFewWaves) {
+    f32x4 gate = sum[0][2 * m][lane], up = sum[0][2 * m + 1][lane];
+#pragma unroll
+    for (int k = 1; k < kFewWaves; ++k) {
+      gate += sum[k][2 * m][lane];
+      up += sum[k][2 * m + 1][lane];
+    }
+    if (16L * m + j < a.M) put_glu<DT>(a, 16L * m + j, n0 + 4 * g, gate, up);
   }
 }
 
@@ -567,6 +595,13 @@ hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
   constexpr int BK = El<DT>::BK;
   const int dtype = sizeof(DT) == 4 ? WM_FP32 : WM_BF16;
   const bool wide = big(dtype, a.M, GLU ? 2 * a.N : a.N, a.K);
+  if constexpr (GLU) {
+    if (a.M <= kFewRows) {
+      const dim3 grid((unsigned)((a.N + 15) / 16)), block(64 * kFewWaves);
+      if (a.M <= 16) return launch(name, k_glu_few<DT, 1>, grid, block, 0, s, a);
+      return launch(name, a.M <= 32 ? k_glu_few<DT, 2> : k_glu_few<DT, 4>, grid, block, 0, s, a);
+    }
+  }
   if constexpr (sizeof(DT) == 2) {
     if (wide && direct(a.P) && direct(a.Q) && (!GLU || 2 * a.N * a.P.ld < (1L << 30))) {
       const int width = GLU ? kBig / 2 : kBig;

@@ -60,40 +60,6 @@ template <> struct Tile<float> {
   static constexpr int VEC = 4, PAD = 4, SLICE = 16, PLANES = 1;
 };
 
-typedef uint32_t __attribute__((ext_vector_type(4))) v4u;
-typedef uint32_t __attribute__((ext_vector_type(2))) v2u;
-typedef v4u __attribute__((aligned(2))) v4u_2;
-typedef v4u __attribute__((aligned(4))) v4u_4;
-typedef v2u __attribute__((aligned(2))) v2u_2;
-template <typename DT> struct Mem16;
-template <> struct Mem16<float> { typedef v4u_4 type; };
-template <> struct Mem16<bf16_t> { typedef v4u_2 type; };
-
-// 16 bytes of a row from column c on, zeros past its `width`.
-template <typename DT>
-__device__ __forceinline__ v4u load_piece(const DT* row, int c, int width) {
-  constexpr int V = Tile<DT>::VEC;
-  if (c + V <= width) return *reinterpret_cast<const typename Mem16<DT>::type*>(row + c);
-  v4u r = {0, 0, 0, 0};
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (c + i < width) {
-      if constexpr (sizeof(DT) == 4)
-        r[i] = __float_as_uint(row[c + i]);
-      else
-        r[i / 2] |= (uint32_t)row[c + i] << (16 * (i & 1));
-    }
-  return r;
-}
-
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-// Four rows of one column from a row-major bf16 matrix in LDS: sixteen lanes read
-// four rows of sixteen columns, four values each (p: row j / 4, columns 4 (j % 4)
-// on, j the lane of the sixteen), and get column j.
-__device__ __forceinline__ v2u read_tr(const bf16_t* p) {
-  typedef __attribute__((address_space(3))) s16x4* lds_t;
-  return __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)p));
-}
 __device__ __forceinline__ bf16x8 join(v2u a, v2u b) { return __builtin_bit_cast(bf16x8, v4u{a.x, a.y, b.x, b.y}); }
 
 // The same value, which the compiler takes for another one in every round of a loop:
@@ -688,17 +654,22 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
 
 // All three gradients of heads up to 64 wide: the forward sweep for dq, then the
 // reverse one for dk and dv, which finds k, v and dy in the caches where the
-// segment is short.
+// segment is short; or, `apart`, each in a work-group of its own.
 template <typename DT, int KP, int VP, bool FAST>
-__global__ void __launch_bounds__(kThreads, waves(sizeof(DT), KP, VP, FAST)) k_mix_grad(const MixArgs q, const MixArgs v, const SeqView dk) {
+__global__ void __launch_bounds__(kThreads, waves(sizeof(DT), KP, VP, FAST)) k_mix_grad(const MixArgs q, const MixArgs v, const SeqView dk,
+                                                                                        int apart) {
   constexpr int SK = Panel<DT, KP>::SIZE, SV = Panel<DT, VP>::SIZE;
   constexpr int ST = State<DT, KP, VP>::SIZE > State<DT, VP, KP>::SIZE ? State<DT, KP, VP>::SIZE : State<DT, VP, KP>::SIZE;
   __shared__ __align__(16) DT kl[SK];
   __shared__ __align__(16) DT vl[SV];
   __shared__ __align__(16) DT st[ST];
-  const Place at(q, blockIdx.x);
-  sweep<DT, VP, KP, false, false, FAST>(q, at, 0, vl, kl, st);
-  __syncthreads();
+  const Place at(q, blockIdx.x >> apart);
+  const bool only = apart && (blockIdx.x & 1);
+  if (!only) {
+    sweep<DT, VP, KP, false, false, FAST>(q, at, 0, vl, kl, st);
+    if (apart) return;
+    __syncthreads();
+  }
   sweep_back<DT, KP, VP, FAST>(v, dk, at, kl, vl, st);
 }
 
@@ -816,14 +787,19 @@ hipError_t launch_mix(const char* name, int dtype, const MixArgs& m, hipStream_t
   return dtype == WM_FP32 ? by(0.0f) : by(bf16_t());
 }
 
+// Sequences, heads and segments up to which the gradient's two sweeps run beside each
+// other.
+constexpr long kApart = 512;
 hipError_t launch_mix_grad(int dtype, const MixArgs& q, const MixArgs& v, const SeqView& dk, hipStream_t s) {
   const int K = v.ka, V = v.kc;
   const bool fast = fast_view(dtype, v.a, K) && fast_view(dtype, v.b, K) && fast_view(dtype, v.c, V) && fast_view(dtype, v.v, V) &&
                     fast_view(dtype, v.out, V) && fast_view(dtype, dk, K) && fast_view(dtype, q.out, K);
+  const long places = (long)v.B * v.N * v.nseg;
+  const int apart = places <= kApart;
   auto go = [&](auto dt, auto kp, auto vp) {
     typedef decltype(dt) DT;
     return launch("linattn_grad", fast ? k_mix_grad<DT, kp, vp, true> : k_mix_grad<DT, kp, vp, false>,
-                  dim3((unsigned)((long)v.B * v.N * v.nseg)), dim3(kThreads), 0, s, q, v, dk);
+                  dim3((unsigned)(places << apart)), dim3(kThreads), 0, s, q, v, dk, apart);
   };
   auto by = [&](auto dt) {
     auto cols = [&](auto kp) { return V <= 32 ? go(dt, kp, Const<32>()) : go(dt, kp, Const<64>()); };

@@ -30,14 +30,9 @@ namespace {
 
 constexpr int kThreads = 256;
 
-typedef uint32_t __attribute__((ext_vector_type(4))) v4u;
-typedef v4u __attribute__((aligned(2))) v4u_2;
-typedef v4u __attribute__((aligned(4))) v4u_4;
-
 template <typename DT> struct Io;
 template <> struct Io<float> {
   static constexpr int VEC = 4;
-  typedef v4u_4 mem;
   __device__ static void get(v4u r, float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(r[i]);
@@ -48,7 +43,6 @@ template <> struct Io<float> {
 };
 template <> struct Io<bf16_t> {
   static constexpr int VEC = 8;
-  typedef v4u_2 mem;
   __device__ static void get(v4u r, float* v) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -113,8 +107,8 @@ struct Lane {
   }
   __device__ void load(v4u (&r)[2], const Pairs& p, const DT* x) const {
     if constexpr (WHOLE) {
-      r[0] = *reinterpret_cast<const typename Io<DT>::mem*>(x + at[0]);
-      r[1] = *reinterpret_cast<const typename Io<DT>::mem*>(x + at[1]);
+      r[0] = *reinterpret_cast<const typename Mem16<DT>::type*>(x + at[0]);
+      r[1] = *reinterpret_cast<const typename Mem16<DT>::type*>(x + at[1]);
     } else {
       float v[2][V];
 #pragma unroll
@@ -161,8 +155,8 @@ struct Lane {
     if (!any) return;
     if constexpr (WHOLE) {
       if (p.neighbours) swap_order<false>(v);
-      *reinterpret_cast<typename Io<DT>::mem*>(x + at[0]) = Io<DT>::put(v[0]);
-      *reinterpret_cast<typename Io<DT>::mem*>(x + at[1]) = Io<DT>::put(v[1]);
+      *reinterpret_cast<typename Mem16<DT>::type*>(x + at[0]) = Io<DT>::put(v[0]);
+      *reinterpret_cast<typename Mem16<DT>::type*>(x + at[1]) = Io<DT>::put(v[1]);
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
