@@ -503,7 +503,7 @@ wm_status wm_clip_grads(int32_t n, const wm_grad_tensor *tensors, float max_norm
 
 /*
  * Host function: the rotation's angles for `R` rotated values a head (even, 0 ..
- * 512): table[i], i < R / 2, receives base^(-2 i / R) / (2 pi), the part of a
+ * 256): table[i], i < R / 2, receives base^(-2 i / R) / (2 pi), the part of a
  * turn that a step adds to pair i, as a 64-bit binary fraction (the integer
  * nearest to it times 2^64).  base >= 1 and finite.  A caller with other
  * frequencies fills its own table.
@@ -524,7 +524,7 @@ wm_status wm_rotary_table(int32_t R, double base, uint64_t *table);
  *   positions [rows] int32 (of any sign; the angle is exact modulo a turn);
  *   table [R / 2] DEVICE array (ignored with R = 0).
  *   q_out, k_out as q and k, and each may be its input with the same ld.
- * D in 1 .. 512, R even, 0 .. D; Hq in 1 .. 1024, Hk in 0 .. 1024; eps >= 0 and
+ * D in 1 .. 256, R even, 0 .. D; Hq in 1 .. 1024, Hk in 0 .. 1024; eps >= 0 and
  * finite; rows (Hq + Hk) at most 2^31 - 1.  rows = 0 is a no-op.
  */
 wm_status wm_qk_norm(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, int32_t D, int32_t R,

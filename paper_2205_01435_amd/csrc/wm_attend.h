@@ -9,7 +9,7 @@
 
 namespace wm {
 
-constexpr int kQkMaxD = 512;
+constexpr int kQkMaxD = 256;
 // One of queries and keys: rows of `heads` x D values, `ld` elements apart.
 struct QkSide {
   int heads;

@@ -13,8 +13,7 @@
 // 16 bytes, and L lanes hold a head, so that the rotation needs no other lane and
 // the sum goes over L lanes.  It computes its pairs' sines and cosines once for a
 // step and goes through the step's heads with them; where there are few steps the
-// heads are dealt to several lane groups.  Heads whose pairs do not come in whole
-// pieces go the same way, value by value.  The gradient keeps the sums for both
+// heads are dealt to several lane groups.  The gradient keeps the sums for both
 // gammas in registers; a work-group leaves one row of partial sums, which a second
 // launch adds in order.
 //
@@ -55,17 +54,6 @@ template <> struct Io<bf16_t> {
   }
 };
 
-// The pairs of a head: pair p has the values at first(p) and second(p); those
-// from R / 2 on are not rotated, and the last may lack its second value.
-struct Pairs {
-  int D, R, rest;  // rest: pairs that are not rotated
-  bool neighbours;
-  __device__ Pairs(const QkArgs& a) : D(a.D), R(a.R), rest((a.D - a.R + 1) / 2), neighbours(a.neighbours != 0) {}
-  __device__ int count() const { return R / 2 + rest; }
-  __device__ int first(int p) const { return neighbours ? 2 * p : p < R / 2 ? p : R / 2 + p; }
-  __device__ int second(int p) const { return neighbours ? 2 * p + 1 : p < R / 2 ? p + R / 2 : R / 2 + p + rest; }
-};
-
 // (cos, sin) of a part of a turn, a 64-bit binary fraction.
 __device__ __forceinline__ float2 cos_sin(uint64_t turn) {
   const uint32_t t = (uint32_t)(turn >> 32), quarter = (t + 0x20000000u) >> 30;
@@ -93,47 +81,65 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// A lane's pairs of a head, v[0] and v[1] their first and second values.
+// A lane's pairs of a head, v[0] and v[1] their first and second values, as two pieces
+// of VEC neighbouring values.  Neighbours: the pieces follow each other, and pairs are
+// put together from them.  Halves: the lanes of the rotated pairs come first, a piece
+// from each half of the R values; then those of the rest, whose halves are taken as
+// pairs that do not turn (the second one may lack the last).  WHOLE: every piece of
+// every lane is full.
 template <typename DT, bool WHOLE>
 struct Lane {
   static constexpr int V = Io<DT>::VEC;
-  int at[2];  // WHOLE: where the two pieces start
-  int p0;
-  bool any;
-  __device__ Lane(const Pairs& p, int lane) : p0(lane * V), any(lane * V < p.count()) {
-    const int i = any ? p0 : 0;
-    at[0] = p.first(i);
-    at[1] = p.neighbours ? at[0] + V : p.second(i);
-  }
-  __device__ void load(v4u (&r)[2], const Pairs& p, const DT* x) const {
-    if constexpr (WHOLE) {
-      r[0] = *reinterpret_cast<const typename Mem16<DT>::type*>(x + at[0]);
-      r[1] = *reinterpret_cast<const typename Mem16<DT>::type*>(x + at[1]);
+  int at[2], n[2];   // where the pieces start, and their values
+  int end[2];        // what a piece may be read up to
+  int turn0, turns;  // the first pair's place in the table, and how many pairs turn
+  bool neighbours;
+  __device__ Lane(const QkArgs& a, int lane) : neighbours(a.neighbours != 0) {
+    const int R2 = a.R / 2, first = (R2 + V - 1) / V, rest = (a.D - a.R + 1) / 2;
+    if (neighbours) {
+      at[0] = 2 * V * lane;
+      at[1] = at[0] + V;
+      end[0] = end[1] = a.D;
+      turn0 = V * lane;
+      turns = min(max(R2 - turn0, 0), V);
+    } else if (lane < first) {
+      at[0] = turn0 = V * lane;
+      at[1] = R2 + at[0];
+      end[0] = R2;
+      end[1] = a.R;
+      turns = min(R2 - turn0, V);
     } else {
-      float v[2][V];
+      at[0] = a.R + V * (lane - first);
+      at[1] = at[0] + rest;
+      end[0] = a.R + rest;
+      end[1] = a.D;
+      turn0 = turns = 0;
+    }
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int q = p0 + i, f = p.first(q), s = p.second(q);
-        v[0][i] = q < p.count() ? DType<DT>::load(x, f) : 0.0f;
-        v[1][i] = q < p.count() && s < p.D ? DType<DT>::load(x, s) : 0.0f;
-      }
-      r[0] = Io<DT>::put(v[0]);
-      r[1] = Io<DT>::put(v[1]);
+    for (int i = 0; i < 2; ++i) n[i] = min(max(end[i] - at[i], 0), V);
+  }
+  __device__ void load(v4u (&r)[2], const DT* x) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (WHOLE)
+        r[i] = *reinterpret_cast<const typename Mem16<DT>::type*>(x + (n[0] ? at[i] : 0));
+      else
+        r[i] = load_piece<DT>(x, at[i], end[i]);
     }
   }
   // the pieces as pairs
-  __device__ void get(const v4u (&r)[2], const Pairs& p, float (&v)[2][V]) const {
+  __device__ void get(const v4u (&r)[2], float (&v)[2][V]) const {
     Io<DT>::get(r[0], v[0]);
     Io<DT>::get(r[1], v[1]);
-    if (WHOLE && p.neighbours) swap_order<true>(v);
-    if (!any) {
+    if (neighbours) order<true>(v);
+    if (WHOLE && n[0] == 0) {
 #pragma unroll
       for (int i = 0; i < V; ++i) v[0][i] = v[1][i] = 0.0f;
     }
   }
   // 2 V values in memory order, as V first and V second ones, and back
   template <bool TO>
-  __device__ static void swap_order(float (&v)[2][V]) {
+  __device__ static void order(float (&v)[2][V]) {
     float w[2 * V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -151,36 +157,39 @@ struct Lane {
       v[1][i] = TO ? w[2 * i + 1] : w[V + i];
     }
   }
-  __device__ void store(DT* x, const Pairs& p, float (&v)[2][V]) const {
-    if (!any) return;
-    if constexpr (WHOLE) {
-      if (p.neighbours) swap_order<false>(v);
-      *reinterpret_cast<typename Mem16<DT>::type*>(x + at[0]) = Io<DT>::put(v[0]);
-      *reinterpret_cast<typename Mem16<DT>::type*>(x + at[1]) = Io<DT>::put(v[1]);
-    } else {
+  __device__ void store(DT* x, float (&v)[2][V]) const {
+    if (neighbours) order<false>(v);
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int q = p0 + i, s = p.second(q);
-        if (q < p.count()) DType<DT>::store(x, p.first(q), v[0][i]);
-        if (q < p.count() && s < p.D) DType<DT>::store(x, s, v[1][i]);
+    for (int i = 0; i < 2; ++i) {
+      if (n[i] == V) {
+        *reinterpret_cast<typename Mem16<DT>::type*>(x + at[i]) = Io<DT>::put(v[i]);
+      } else if constexpr (!WHOLE) {
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+          if (k < n[i]) DType<DT>::store(x, at[i] + k, v[i][k]);
       }
     }
   }
-  // the lane's values of a [D] array (1 without one, 0 where there is no value)
-  __device__ void columns(float (&g)[2][V], const Pairs& p, const float* a) const {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int q = p0 + i, f = p.first(q), s = p.second(q);
-      g[0][i] = q < p.count() ? (a ? a[f] : 1.0f) : 0.0f;
-      g[1][i] = q < p.count() && s < p.D ? (a ? a[s] : 1.0f) : 0.0f;
-    }
+  // the column of value j (0 first, 1 second) of pair i, -1 where there is none
+  __device__ int column(int j, int i) const {
+    const int k = neighbours ? 2 * i + j : j * V + i, piece = k / V, in = k % V;
+    return in < (piece ? n[1] : n[0]) ? (piece ? at[1] : at[0]) + in : -1;
   }
-  __device__ void angles(float (&c)[V], float (&s)[V], const Pairs& p, const QkArgs& a, long row) const {
+  // the lane's values of a [D] array (1 without one, 0 where there is no value)
+  __device__ void columns(float (&g)[2][V], const float* a) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int c = column(j, i);
+        g[j][i] = c < 0 ? 0.0f : a ? a[c] : 1.0f;
+      }
+  }
+  __device__ void angles(float (&c)[V], float (&s)[V], const QkArgs& a, long row) const {
     const uint64_t pos = (uint64_t)(int64_t)a.pos[row];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const int q = p0 + i;
-      const float2 t = q < p.R / 2 ? cos_sin(pos * a.table[q]) : make_float2(1.0f, 0.0f);
+      const float2 t = i < turns ? cos_sin(pos * a.table[turn0 + i]) : make_float2(1.0f, 0.0f);
       c[i] = t.x;
       s[i] = t.y;
     }
@@ -191,8 +200,7 @@ struct Lane {
 template <typename DT, int L, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
   constexpr int V = Io<DT>::VEC, kSlots = kThreads / L;
-  const Pairs p(a);
-  const Lane<DT, WHOLE> lane(p, threadIdx.x % L);
+  const Lane<DT, WHOLE> lane(a, threadIdx.x % L);
   const int heads = a.side[0].heads + a.side[1].heads, parts = (heads + a.group - 1) / a.group;
   const long item = (long)blockIdx.x * kSlots + threadIdx.x / L;
   const long row = item / parts;
@@ -203,17 +211,17 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
     return reinterpret_cast<const DT*>(a.side[w].x) + row * a.side[w].x_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D;
   };
   v4u next[2];
-  lane.load(next, p, in(h0));
+  lane.load(next, in(h0));
   float c[V], s[V], g[2][V];
-  lane.angles(c, s, p, a, row);
+  lane.angles(c, s, a, row);
   const float inv = 1.0f / (float)a.D;
   int held = -1;
   for (int h = h0; h < h1; ++h) {
     const int w = h >= a.side[0].heads;
-    if (w != held) lane.columns(g, p, a.side[held = w].gamma);
+    if (w != held) lane.columns(g, a.side[held = w].gamma);
     float v[2][V];
-    lane.get(next, p, v);
-    if (h + 1 < h1) lane.load(next, p, in(h + 1));
+    lane.get(next, v);
+    if (h + 1 < h1) lane.load(next, in(h + 1));
     float m = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) m = fmaf(v[0][i], v[0][i], fmaf(v[1][i], v[1][i], m));
@@ -224,7 +232,7 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
       v[0][i] = fmaf(x0, c[i], -(x1 * s[i]));
       v[1][i] = fmaf(x0, s[i], x1 * c[i]);
     }
-    lane.store(reinterpret_cast<DT*>(a.side[w].out) + row * a.side[w].out_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D, p, v);
+    lane.store(reinterpret_cast<DT*>(a.side[w].out) + row * a.side[w].out_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D, v);
   }
 }
 
@@ -233,8 +241,7 @@ template <typename DT, int L, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) k_qk_norm_grad(const QkArgs a) {
   constexpr int V = Io<DT>::VEC, kSlots = kThreads / L;
   __shared__ float add[2 * V][kThreads + 1];
-  const Pairs p(a);
-  const Lane<DT, WHOLE> lane(p, threadIdx.x % L);
+  const Lane<DT, WHOLE> lane(a, threadIdx.x % L);
   const int heads = a.side[0].heads + a.side[1].heads, parts = (heads + a.group - 1) / a.group;
   const float inv = 1.0f / (float)a.D;
   float dg[2][2][V];
@@ -246,7 +253,7 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_grad(const QkArgs a) {
     const long row = item / parts;
     const int h0 = (int)(item % parts) * a.group, h1 = min(h0 + a.group, heads);
     float c[V], s[V];
-    lane.angles(c, s, p, a, row);
+    lane.angles(c, s, a, row);
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
       const QkSide& side = a.side[w];
@@ -256,17 +263,17 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_grad(const QkArgs a) {
       const DT* dy = reinterpret_cast<const DT*>(side.dout) + row * side.dout_ld;
       DT* out = reinterpret_cast<DT*>(side.out) + row * side.out_ld;
       float g[2][V];
-      lane.columns(g, p, side.gamma);
+      lane.columns(g, side.gamma);
       v4u nx[2], nd[2];
-      lane.load(nx, p, x + (long)lo * a.D);
-      lane.load(nd, p, dy + (long)lo * a.D);
+      lane.load(nx, x + (long)lo * a.D);
+      lane.load(nd, dy + (long)lo * a.D);
       for (int h = lo; h < hi; ++h) {
         float v[2][V], d[2][V];
-        lane.get(nx, p, v);
-        lane.get(nd, p, d);
+        lane.get(nx, v);
+        lane.get(nd, d);
         if (h + 1 < hi) {
-          lane.load(nx, p, x + (long)(h + 1) * a.D);
-          lane.load(nd, p, dy + (long)(h + 1) * a.D);
+          lane.load(nx, x + (long)(h + 1) * a.D);
+          lane.load(nd, dy + (long)(h + 1) * a.D);
         }
         float m = 0.0f, ex = 0.0f;
 #pragma unroll
@@ -285,7 +292,7 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_grad(const QkArgs a) {
             dg[w][j][i] = fmaf(d[j][i], v[j][i] * r, dg[w][j][i]);
             v[j][i] = r * (d[j][i] * g[j][i] - v[j][i] * k);
           }
-        lane.store(out + (long)h * a.D, p, v);
+        lane.store(out + (long)h * a.D, v);
       }
     }
   }
@@ -302,9 +309,9 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_grad(const QkArgs a) {
     if (!part) continue;
     // one column a thread, its slots in order
     for (int j = threadIdx.x; j < 2 * V * L; j += kThreads) {
-      const int l = j / (2 * V), i = j % (2 * V), q = l * V + i % V;
-      const int col = i < V ? p.first(q) : p.second(q);
-      if (q >= p.count() || col >= a.D) continue;
+      const int l = j / (2 * V), i = j % (2 * V);
+      const int col = Lane<DT, WHOLE>(a, l).column(i / V, i % V);
+      if (col < 0) continue;
       float t = 0.0f;
 #pragma unroll 8
       for (int k = 0; k < kSlots; ++k) t += add[i][k * L + l];
@@ -334,10 +341,10 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm_sum(const QkArgs a, int n)
 }
 
 // Lanes of a head.
-int lanes(int D, int R, int V) {
-  const int pairs = R / 2 + (D - R + 1) / 2;
+int lanes(const QkArgs& a, int V) {
+  const int need = a.neighbours ? (a.D + 2 * V - 1) / (2 * V) : (a.R / 2 + V - 1) / V + ((a.D - a.R + 1) / 2 + V - 1) / V;
   int l = 1;
-  while (l * V < pairs) l *= 2;
+  while (l < need) l *= 2;
   return l;
 }
 bool whole(const QkArgs& a, int V) {
@@ -359,7 +366,7 @@ template <typename DT, typename F>
 hipError_t by_lanes(const QkArgs& a, F f) {
   const bool w = whole(a, Io<DT>::VEC);
   auto go = [&](auto l) { return w ? f(l, std::true_type()) : f(l, std::false_type()); };
-  switch (lanes(a.D, a.R, Io<DT>::VEC)) {
+  switch (lanes(a, Io<DT>::VEC)) {
     case 1: return go(Const<1>());
     case 2: return go(Const<2>());
     case 4: return go(Const<4>());
@@ -396,7 +403,7 @@ hipError_t launch_qk_norm_grad(int dtype, const QkArgs& args, hipStream_t s) {
   QkArgs a = args;
   const int heads = a.side[0].heads + a.side[1].heads;
   a.group = heads_of_item(a.rows, heads, kItems);
-  const int n = grad_groups(a.rows, heads, lanes(a.D, a.R, dtype == WM_FP32 ? 4 : 8), a.group);
+  const int n = grad_groups(a.rows, heads, lanes(a, dtype == WM_FP32 ? 4 : 8), a.group);
   auto run = [&](auto dt) {
     typedef decltype(dt) DT;
     return by_lanes<DT>(a, [&](auto l, auto w) {

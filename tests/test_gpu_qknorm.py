@@ -29,8 +29,8 @@ CASES = [  # rows, Hq, Hk, D, R, neighbours, dtype, affine
     (1, 16, 16, 64, 64, False, "bf16", True), (16, 16, 4, 64, 64, False, "fp32", True), (5, 3, 3, 64, 32, False, "bf16", True),
     (7, 4, 2, 64, 64, True, "bf16", True), (33, 6, 3, 61, 34, True, "fp32", True), (33, 6, 3, 61, 34, False, "bf16", True),
     (9, 2, 2, 128, 64, True, "fp32", False), (10, 5, 1, 96, 96, False, "bf16", True), (6, 3, 2, 100, 100, False, "fp32", True),
-    (4, 2, 2, 256, 256, False, "bf16", True), (4, 2, 1, 255, 254, False, "fp32", True), (3, 1, 1, 512, 512, False, "fp32", True),
-    (3, 2, 2, 511, 256, True, "bf16", True), (700, 2, 1, 48, 16, False, "bf16", True), (2500, 8, 8, 64, 64, False, "fp32", True),
+    (4, 2, 2, 256, 256, False, "bf16", True), (4, 2, 1, 255, 254, False, "fp32", True), (3, 1, 1, 256, 254, False, "fp32", True), (5, 2, 1, 253, 126, True, "fp32", True),
+    (3, 2, 2, 251, 128, True, "bf16", True), (6, 2, 1, 201, 30, False, "bf16", True), (6, 1, 1, 3, 2, False, "bf16", True), (6, 2, 1, 7, 6, True, "fp32", True), (700, 2, 1, 48, 16, False, "bf16", True), (2500, 8, 8, 64, 64, False, "fp32", True),
     (2049, 1, 1, 8, 8, False, "fp32", True), (3000, 3, 2, 32, 32, True, "bf16", True), (20000, 2, 1, 16, 8, False, "bf16", True),
     (5, 24, 24, 128, 128, False, "bf16", True), (64, 7, 7, 40, 24, False, "fp32", True), (2, 1024, 3, 4, 2, True, "fp32", True),
 ]
@@ -218,9 +218,9 @@ def test_refusals():
     for r in (wm.Rotary(10), None):
         with pytest.raises(wm.WmError):
             wm.qk_norm(q, k, pos, r, eps=float("nan") if r is None else 1e-6)
-    for R, base in ((7, 10.0), (-2, 10.0), (514, 10.0), (8, 0.5), (8, float("inf")), (8, float("nan"))):
+    for R, base in ((7, 10.0), (-2, 10.0), (258, 10.0), (8, 0.5), (8, float("inf")), (8, float("nan"))):
         with pytest.raises(wm.WmError):
             wm.Rotary(R, base)
     with pytest.raises(wm.WmError) as e:
-        wm.qk_norm(torch.zeros(1, 1, 513, device="cuda"), None, pos[:1], rot)
+        wm.qk_norm(torch.zeros(1, 1, 257, device="cuda"), None, pos[:1], rot)
     assert e.value.status == wm.WM_ERR_UNSUPPORTED
