@@ -747,7 +747,7 @@ wm_status wm_qk_norm(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, int32_
   const wm::QkArgs a{(long)rows, D, R, neighbours, eps, positions, table,
                      {{Hq, q, (long)q_ld, gamma_q, nullptr, 0, q_out, (long)q_out_ld, nullptr},
                       {Hk, k, (long)k_ld, gamma_k, nullptr, 0, k_out, (long)k_out_ld, nullptr}},
-                     nullptr, 0};
+                     nullptr, 0, {0, 0}};
   const hipError_t e = wm::launch_qk_norm(dtype, a, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "wm_qk_norm");
   return ok();
@@ -788,7 +788,7 @@ wm_status wm_qk_norm_grad(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, i
   const wm::QkArgs a{(long)rows, D, R, neighbours, eps, positions, table,
                      {{Hq, q, (long)q_ld, gamma_q, grad_q_out, (long)grad_q_out_ld, grad_q, (long)grad_q_ld, grad_gamma_q},
                       {Hk, k, (long)k_ld, gamma_k, grad_k_out, (long)grad_k_out_ld, grad_k, (long)grad_k_ld, grad_gamma_k}},
-                     reinterpret_cast<float*>(workspace), 0};
+                     reinterpret_cast<float*>(workspace), 0, {0, 0}};
   const hipError_t e = wm::launch_qk_norm_grad(dtype, a, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "wm_qk_norm_grad");
   return ok();

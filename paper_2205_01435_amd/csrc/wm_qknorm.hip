@@ -202,10 +202,10 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
   constexpr int V = Io<DT>::VEC, kSlots = kThreads / L;
   const Lane<DT, WHOLE> lane(a, threadIdx.x % L);
   const int heads = a.side[0].heads + a.side[1].heads, parts = (heads + a.group - 1) / a.group;
-  const long item = (long)blockIdx.x * kSlots + threadIdx.x / L;
-  const long row = item / parts;
+  const uint32_t item = blockIdx.x * kSlots + threadIdx.x / L;  // (rows x heads fit 31 bits)
+  const long row = item / (uint32_t)parts;
   if (row >= a.rows) return;
-  const int h0 = (int)(item % parts) * a.group, h1 = min(h0 + a.group, heads);
+  const int h0 = (int)(item % (uint32_t)parts) * a.group, h1 = min(h0 + a.group, heads);
   auto in = [&](int h) {
     const int w = h >= a.side[0].heads;
     return reinterpret_cast<const DT*>(a.side[w].x) + row * a.side[w].x_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D;
@@ -236,108 +236,105 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
   }
 }
 
-// part [gridDim.x][2][D]: this work-group's sums for the gammas of queries and keys.
+// The first groups[0] work-groups take the queries, the others the keys: sums for one
+// gamma are half the registers of those for both (204800 rows, 20 heads of 64 bf16
+// 379 -> 325 us).  part [groups][D]: each work-group's sums; where a side has only one,
+// they are the result.
 template <typename DT, int L, bool WHOLE>
-__global__ void __launch_bounds__(kThreads) k_qk_norm_grad(const QkArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) k_qk_norm_grad(const QkArgs a) {
   constexpr int V = Io<DT>::VEC, kSlots = kThreads / L;
   __shared__ float add[2 * V][kThreads + 1];
+  const int which = (int)blockIdx.x >= a.groups[0], group = (int)blockIdx.x - (which ? a.groups[0] : 0);
+  const QkSide& side = a.side[which];
   const Lane<DT, WHOLE> lane(a, threadIdx.x % L);
-  const int heads = a.side[0].heads + a.side[1].heads, parts = (heads + a.group - 1) / a.group;
+  const uint32_t parts = (uint32_t)((side.heads + a.group - 1) / a.group), items = (uint32_t)a.rows * parts;
   const float inv = 1.0f / (float)a.D;
-  float dg[2][2][V];
+  float g[2][V], dg[2][V];
+  lane.columns(g, side.gamma);
 #pragma unroll
-  for (int w = 0; w < 2; ++w)
-#pragma unroll
-    for (int i = 0; i < V; ++i) dg[w][0][i] = dg[w][1][i] = 0.0f;
-  for (long item = (long)blockIdx.x * kSlots + threadIdx.x / L; item < a.rows * parts; item += (long)gridDim.x * kSlots) {
-    const long row = item / parts;
-    const int h0 = (int)(item % parts) * a.group, h1 = min(h0 + a.group, heads);
+  for (int i = 0; i < V; ++i) dg[0][i] = dg[1][i] = 0.0f;
+  for (uint32_t item = (uint32_t)group * kSlots + threadIdx.x / L; item < items; item += (uint32_t)a.groups[which] * kSlots) {
+    const uint32_t row = item / parts;
+    const int h0 = (int)(item - row * parts) * a.group, h1 = min(h0 + a.group, side.heads);
+    const DT* x = reinterpret_cast<const DT*>(side.x) + (long)row * side.x_ld + (long)h0 * a.D;
+    const DT* dy = reinterpret_cast<const DT*>(side.dout) + (long)row * side.dout_ld + (long)h0 * a.D;
+    DT* out = reinterpret_cast<DT*>(side.out) + (long)row * side.out_ld + (long)h0 * a.D;
+    v4u nx[2], nd[2];
+    lane.load(nx, x);
+    lane.load(nd, dy);
     float c[V], s[V];
     lane.angles(c, s, a, row);
+    for (int h = h0; h < h1; ++h, out += a.D) {
+      float v[2][V], d[2][V];
+      lane.get(nx, v);
+      lane.get(nd, d);
+      if (h + 1 < h1) {
+        x += a.D;
+        dy += a.D;
+        lane.load(nx, x);
+        lane.load(nd, dy);
+      }
+      float m = 0.0f, ex = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      const QkSide& side = a.side[w];
-      const int off = w ? a.side[0].heads : 0, lo = max(h0 - off, 0), hi = min(h1 - off, side.heads);
-      if (lo >= hi) continue;
-      const DT* x = reinterpret_cast<const DT*>(side.x) + row * side.x_ld;
-      const DT* dy = reinterpret_cast<const DT*>(side.dout) + row * side.dout_ld;
-      DT* out = reinterpret_cast<DT*>(side.out) + row * side.out_ld;
-      float g[2][V];
-      lane.columns(g, side.gamma);
-      v4u nx[2], nd[2];
-      lane.load(nx, x + (long)lo * a.D);
-      lane.load(nd, dy + (long)lo * a.D);
-      for (int h = lo; h < hi; ++h) {
-        float v[2][V], d[2][V];
-        lane.get(nx, v);
-        lane.get(nd, d);
-        if (h + 1 < hi) {
-          lane.load(nx, x + (long)(h + 1) * a.D);
-          lane.load(nd, dy + (long)(h + 1) * a.D);
-        }
-        float m = 0.0f, ex = 0.0f;
+      for (int i = 0; i < V; ++i) {
+        const float d0 = fmaf(d[0][i], c[i], d[1][i] * s[i]), d1 = fmaf(d[1][i], c[i], -(d[0][i] * s[i]));
+        d[0][i] = d0;
+        d[1][i] = d1;
+        m = fmaf(v[0][i], v[0][i], fmaf(v[1][i], v[1][i], m));
+        ex = fmaf(d0 * g[0][i], v[0][i], fmaf(d1 * g[1][i], v[1][i], ex));
+      }
+      const float r = 1.0f / sqrtf(group_sum<L>(m) * inv + a.eps), k = group_sum<L>(ex) * inv * r * r;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const float d0 = fmaf(d[0][i], c[i], d[1][i] * s[i]), d1 = fmaf(d[1][i], c[i], -(d[0][i] * s[i]));
-          d[0][i] = d0;
-          d[1][i] = d1;
-          m = fmaf(v[0][i], v[0][i], fmaf(v[1][i], v[1][i], m));
-          ex = fmaf(d0 * g[0][i], v[0][i], fmaf(d1 * g[1][i], v[1][i], ex));
+          dg[j][i] = fmaf(d[j][i], v[j][i] * r, dg[j][i]);
+          v[j][i] = r * (d[j][i] * g[j][i] - v[j][i] * k);
         }
-        const float r = 1.0f / sqrtf(group_sum<L>(m) * inv + a.eps), k = group_sum<L>(ex) * inv * r * r;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            dg[w][j][i] = fmaf(d[j][i], v[j][i] * r, dg[w][j][i]);
-            v[j][i] = r * (d[j][i] * g[j][i] - v[j][i] * k);
-          }
-        lane.store(out + (long)h * a.D, v);
-      }
+      lane.store(out, v);
     }
   }
+  float* const part = a.groups[which] > 1 ? a.part + (long)blockIdx.x * a.D : side.dgamma;
+  if (!part) return;
 #pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    float* const part = gridDim.x > 1 ? a.part + ((long)blockIdx.x * 2 + w) * a.D : a.side[w].dgamma;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      add[i][threadIdx.x] = dg[w][0][i];
-      add[V + i][threadIdx.x] = dg[w][1][i];
-    }
-    __syncthreads();
-    if (!part) continue;
-    // one column a thread, its slots in order
-    for (int j = threadIdx.x; j < 2 * V * L; j += kThreads) {
-      const int l = j / (2 * V), i = j % (2 * V);
-      const int col = Lane<DT, WHOLE>(a, l).column(i / V, i % V);
-      if (col < 0) continue;
-      float t = 0.0f;
+  for (int i = 0; i < V; ++i) {
+    add[i][threadIdx.x] = dg[0][i];
+    add[V + i][threadIdx.x] = dg[1][i];
+  }
+  __syncthreads();
+  // one column a thread, its slots in order
+  for (int j = threadIdx.x; j < 2 * V * L; j += kThreads) {
+    const int l = j / (2 * V), i = j % (2 * V);
+    const int col = Lane<DT, WHOLE>(a, l).column(i / V, i % V);
+    if (col < 0) continue;
+    float t = 0.0f;
 #pragma unroll 8
-      for (int k = 0; k < kSlots; ++k) t += add[i][k * L + l];
-      part[col] = t;
-    }
+    for (int k = 0; k < kSlots; ++k) t += add[i][k * L + l];
+    part[col] = t;
   }
 }
 
-// Adds the n rows of partial sums: 16 columns a work-group, 16 rows at a time,
-// each in its own order, then these.
-__global__ void __launch_bounds__(kThreads) k_qk_norm_sum(const QkArgs a, int n) {
-  __shared__ float sh[16][17];
+// Adds a side's rows of partial sums: 16 columns a work-group, 64 rows at a time, each
+// in its own order, then these.
+constexpr int kSumRows = 64;
+__global__ void __launch_bounds__(16 * kSumRows) k_qk_norm_sum(const QkArgs a) {
+  __shared__ float sh[kSumRows][17];
+  const int which = blockIdx.y, n = a.groups[which];
+  float* const out = a.side[which].dgamma;
+  if (n < 2 || !out) return;
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4, j = blockIdx.x * 16 + c;
   float s = 0.0f;
-  if (j < 2 * a.D) {
-    const float* p = a.part + j;
+  if (j < a.D) {
+    const float* p = a.part + (long)(which ? a.groups[0] : 0) * a.D + j;
 #pragma unroll 8
-    for (int i = r; i < n; i += 16) s += p[(long)i * 2 * a.D];
+    for (int i = r; i < n; i += kSumRows) s += p[(long)i * a.D];
   }
   sh[r][c] = s;
   __syncthreads();
-  if (r > 0 || j >= 2 * a.D) return;
-#pragma unroll
-  for (int i = 1; i < 16; ++i) s += sh[i][c];
-  float* out = j < a.D ? a.side[0].dgamma : a.side[1].dgamma;
-  if (out) out[j < a.D ? j : j - a.D] = s;
+  if (r > 0 || j >= a.D) return;
+#pragma unroll 16
+  for (int i = 1; i < kSumRows; ++i) s += sh[i][c];
+  out[j] = s;
 }
 
 // Lanes of a head.
@@ -356,9 +353,12 @@ int heads_of_item(long rows, int heads, long most) {
   long parts = std::min<long>(heads, std::max<long>(1, most / std::max<long>(rows, 1)));
   return (int)((heads + parts - 1) / parts);
 }
-int grad_groups(long rows, int heads, int L, int group) {
+// Work-groups of the gradient for one side: its share of kMost by heads, or as many as
+// it has items for (one for a side without heads: it writes zeros).
+constexpr long kMost = 1024;
+int grad_groups(long rows, int heads, int all, int L, int group) {
   const long items = rows * ((heads + group - 1) / group), slots = kThreads / L;
-  return (int)std::max<long>(1, std::min<long>((items + slots - 1) / slots, 1024));
+  return (int)std::max<long>(1, std::min<long>((items + slots - 1) / slots, kMost * heads / all));
 }
 
 template <int N> using Const = std::integral_constant<int, N>;
@@ -396,23 +396,24 @@ hipError_t launch_qk_norm(int dtype, const QkArgs& args, hipStream_t s) {
 
 size_t qk_norm_grad_workspace(long rows, int Hq, int Hk, int D) {
   (void)rows, (void)Hq, (void)Hk;
-  return (size_t)1024 * 2 * D * sizeof(float);
+  return (size_t)(kMost + 2) * D * sizeof(float);
 }
 
 hipError_t launch_qk_norm_grad(int dtype, const QkArgs& args, hipStream_t s) {
   QkArgs a = args;
   const int heads = a.side[0].heads + a.side[1].heads;
   a.group = heads_of_item(a.rows, heads, kItems);
-  const int n = grad_groups(a.rows, heads, lanes(a, dtype == WM_FP32 ? 4 : 8), a.group);
+  const int l = lanes(a, dtype == WM_FP32 ? 4 : 8);
+  for (int w = 0; w < 2; ++w) a.groups[w] = grad_groups(a.rows, a.side[w].heads, heads, l, a.group);
   auto run = [&](auto dt) {
     typedef decltype(dt) DT;
     return by_lanes<DT>(a, [&](auto l, auto w) {
-      return launch("qk_norm_grad", k_qk_norm_grad<DT, l, w>, dim3(n), dim3(kThreads), 0, s, a);
+      return launch("qk_norm_grad", k_qk_norm_grad<DT, l, w>, dim3(a.groups[0] + a.groups[1]), dim3(kThreads), 0, s, a);
     });
   };
   const hipError_t e = dtype == WM_FP32 ? run(0.0f) : run(bf16_t());
-  if (e != hipSuccess || n == 1) return e;
-  return launch("qk_norm_sum", k_qk_norm_sum, dim3((unsigned)((2 * a.D + 15) / 16)), dim3(kThreads), 0, s, a, n);
+  if (e != hipSuccess || (a.groups[0] < 2 && a.groups[1] < 2)) return e;
+  return launch("qk_norm_sum", k_qk_norm_sum, dim3((unsigned)((a.D + 15) / 16), 2), dim3(16 * kSumRows), 0, s, a);
 }
 
 }  // namespace wm
