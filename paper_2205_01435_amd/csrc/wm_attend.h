@@ -31,8 +31,8 @@ struct QkArgs {
   const uint64_t* table;  // [R / 2]
   QkSide side[2];
   float* part;  // gradient: workspace
-  // set by the launcher: heads of one work item, and the gradient's work-groups of each side
-  int group, groups[2];
+  // set by the launcher: items of a step, and the gradient's work-groups of each side
+  int parts, groups[2];
 };
 size_t qk_norm_grad_workspace(long rows, int Hq, int Hk, int D);
 hipError_t launch_qk_norm(int dtype, const QkArgs& a, hipStream_t s);

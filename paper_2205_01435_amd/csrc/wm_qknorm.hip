@@ -185,8 +185,8 @@ struct Lane {
         g[j][i] = c < 0 ? 0.0f : a ? a[c] : 1.0f;
       }
   }
-  __device__ void angles(float (&c)[V], float (&s)[V], const QkArgs& a, long row) const {
-    const uint64_t pos = (uint64_t)(int64_t)a.pos[row];
+  __device__ void angles(float (&c)[V], float (&s)[V], const QkArgs& a, int32_t position) const {
+    const uint64_t pos = (uint64_t)(int64_t)position;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float2 t = i < turns ? cos_sin(pos * a.table[turn0 + i]) : make_float2(1.0f, 0.0f);
@@ -196,16 +196,18 @@ struct Lane {
   }
 };
 
-// An item is `group` heads of one step; heads count through queries, then keys.
+// An item is every `parts`-th head of one step from head item % parts on, so that
+// neighbouring lane groups are at neighbouring heads; heads count through queries,
+// then keys.
 template <typename DT, int L, bool WHOLE>
 __global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
   constexpr int V = Io<DT>::VEC, kSlots = kThreads / L;
   const Lane<DT, WHOLE> lane(a, threadIdx.x % L);
-  const int heads = a.side[0].heads + a.side[1].heads, parts = (heads + a.group - 1) / a.group;
+  const int heads = a.side[0].heads + a.side[1].heads, parts = a.parts;
   const uint32_t item = blockIdx.x * kSlots + threadIdx.x / L;  // (rows x heads fit 31 bits)
   const long row = item / (uint32_t)parts;
   if (row >= a.rows) return;
-  const int h0 = (int)(item % (uint32_t)parts) * a.group, h1 = min(h0 + a.group, heads);
+  const int h0 = (int)(item % (uint32_t)parts);
   auto in = [&](int h) {
     const int w = h >= a.side[0].heads;
     return reinterpret_cast<const DT*>(a.side[w].x) + row * a.side[w].x_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D;
@@ -213,15 +215,15 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
   v4u next[2];
   lane.load(next, in(h0));
   float c[V], s[V], g[2][V];
-  lane.angles(c, s, a, row);
+  lane.angles(c, s, a, a.pos[row]);
   const float inv = 1.0f / (float)a.D;
   int held = -1;
-  for (int h = h0; h < h1; ++h) {
+  for (int h = h0; h < heads; h += parts) {
     const int w = h >= a.side[0].heads;
     if (w != held) lane.columns(g, a.side[held = w].gamma);
     float v[2][V];
     lane.get(next, v);
-    if (h + 1 < h1) lane.load(next, in(h + 1));
+    if (h + parts < heads) lane.load(next, in(h + parts));
     float m = 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) m = fmaf(v[0][i], v[0][i], fmaf(v[1][i], v[1][i], m));
@@ -237,42 +239,54 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
 }
 
 // The first groups[0] work-groups take the queries, the others the keys: sums for one
-// gamma are half the registers of those for both (204800 rows, 20 heads of 64 bf16
-// 379 -> 325 us).  part [groups][D]: each work-group's sums; where a side has only one,
+// gamma are half the registers of those for both (4500 rows, 9 heads of 61 fp32
+// 19.4 -> 13.5 us).  part [groups][D]: each work-group's sums; where a side has only one,
 // they are the result.
 template <typename DT, int L, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, 3) k_qk_norm_grad(const QkArgs a) {
+__global__ void __launch_bounds__(kThreads, WHOLE ? 3 : 2) k_qk_norm_grad(const QkArgs a) {
   constexpr int V = Io<DT>::VEC, kSlots = kThreads / L;
   __shared__ float add[2 * V][kThreads + 1];
   const int which = (int)blockIdx.x >= a.groups[0], group = (int)blockIdx.x - (which ? a.groups[0] : 0);
   const QkSide& side = a.side[which];
   const Lane<DT, WHOLE> lane(a, threadIdx.x % L);
-  const uint32_t parts = (uint32_t)((side.heads + a.group - 1) / a.group), items = (uint32_t)a.rows * parts;
+  const uint32_t parts = (uint32_t)min(a.parts, max(side.heads, 1)), items = (uint32_t)a.rows * parts;
   const float inv = 1.0f / (float)a.D;
   float g[2][V], dg[2][V];
   lane.columns(g, side.gamma);
 #pragma unroll
   for (int i = 0; i < V; ++i) dg[0][i] = dg[1][i] = 0.0f;
-  for (uint32_t item = (uint32_t)group * kSlots + threadIdx.x / L; item < items; item += (uint32_t)a.groups[which] * kSlots) {
+  const uint32_t stride = (uint32_t)a.groups[which] * kSlots;
+  uint32_t item = (uint32_t)group * kSlots + threadIdx.x / L;
+  if (side.heads == 0) item = items;
+  v4u nx[2], nd[2];
+  // an item's first pieces are requested while the item before is worked on
+  auto first = [&](uint32_t it) {
+    const uint32_t row = it / parts;
+    const long h = (long)(it - row * parts) * a.D;
+    lane.load(nx, reinterpret_cast<const DT*>(side.x) + (long)row * side.x_ld + h);
+    lane.load(nd, reinterpret_cast<const DT*>(side.dout) + (long)row * side.dout_ld + h);
+    return a.pos[row];
+  };
+  int32_t pos = item < items ? first(item) : 0;
+  for (; item < items; item += stride) {
     const uint32_t row = item / parts;
-    const int h0 = (int)(item - row * parts) * a.group, h1 = min(h0 + a.group, side.heads);
+    const int h0 = (int)(item - row * parts), step = (int)parts * a.D;
     const DT* x = reinterpret_cast<const DT*>(side.x) + (long)row * side.x_ld + (long)h0 * a.D;
     const DT* dy = reinterpret_cast<const DT*>(side.dout) + (long)row * side.dout_ld + (long)h0 * a.D;
     DT* out = reinterpret_cast<DT*>(side.out) + (long)row * side.out_ld + (long)h0 * a.D;
-    v4u nx[2], nd[2];
-    lane.load(nx, x);
-    lane.load(nd, dy);
     float c[V], s[V];
-    lane.angles(c, s, a, row);
-    for (int h = h0; h < h1; ++h, out += a.D) {
+    lane.angles(c, s, a, pos);
+    for (int h = h0; h < side.heads; h += (int)parts, out += step) {
       float v[2][V], d[2][V];
       lane.get(nx, v);
       lane.get(nd, d);
-      if (h + 1 < h1) {
-        x += a.D;
-        dy += a.D;
+      if (h + (int)parts < side.heads) {
+        x += step;
+        dy += step;
         lane.load(nx, x);
         lane.load(nd, dy);
+      } else if (item + stride < items) {
+        pos = first(item + stride);
       }
       float m = 0.0f, ex = 0.0f;
 #pragma unroll
@@ -347,17 +361,20 @@ int lanes(const QkArgs& a, int V) {
 bool whole(const QkArgs& a, int V) {
   return a.neighbours ? a.D % (2 * V) == 0 : a.R % (2 * V) == 0 && (a.D - a.R) % (2 * V) == 0;
 }
-// Heads of one item: all of a step's, or fewer where that gives fewer than `most`
-// lane groups.
-int heads_of_item(long rows, int heads, long most) {
-  long parts = std::min<long>(heads, std::max<long>(1, most / std::max<long>(rows, 1)));
-  return (int)((heads + parts - 1) / parts);
+// Items of a step: lane groups beside each other read longer runs of a row, but each
+// computes the angles again, of twice as many pairs a lane in bf16; more where that
+// gives fewer than kItems.  Measured, 1 and 4: 65536 rows, 16 heads of 64 fp32, 115 and
+// 100 us, gradient 160 and 154; 204800 rows, 20 heads of 64 bf16, 206 and 239, gradient
+// 379 and 463.
+constexpr long kItems = 16384;
+int parts_of(int dtype, long rows, int heads) {
+  return (int)std::min<long>(heads, std::max<long>(dtype == WM_FP32 ? 4 : 1, kItems / std::max<long>(rows, 1)));
 }
 // Work-groups of the gradient for one side: its share of kMost by heads, or as many as
 // it has items for (one for a side without heads: it writes zeros).
 constexpr long kMost = 1024;
-int grad_groups(long rows, int heads, int all, int L, int group) {
-  const long items = rows * ((heads + group - 1) / group), slots = kThreads / L;
+int grad_groups(long rows, int heads, int all, int L, int parts) {
+  const long items = rows * std::min(parts, std::max(heads, 1)), slots = kThreads / L;
   return (int)std::max<long>(1, std::min<long>((items + slots - 1) / slots, kMost * heads / all));
 }
 
@@ -376,18 +393,17 @@ hipError_t by_lanes(const QkArgs& a, F f) {
     default: return go(Const<64>());
   }
 }
-constexpr long kItems = 16384;  // lane groups that fill the device
 
 }  // namespace
 
 hipError_t launch_qk_norm(int dtype, const QkArgs& args, hipStream_t s) {
   QkArgs a = args;
   const int heads = a.side[0].heads + a.side[1].heads;
-  a.group = heads_of_item(a.rows, heads, kItems);
+  a.parts = parts_of(dtype, a.rows, heads);
   auto run = [&](auto dt) {
     typedef decltype(dt) DT;
     return by_lanes<DT>(a, [&](auto l, auto w) {
-      const long items = a.rows * ((heads + a.group - 1) / a.group), slots = kThreads / l;
+      const long items = a.rows * a.parts, slots = kThreads / l;
       return launch("qk_norm", k_qk_norm<DT, l, w>, dim3((unsigned)((items + slots - 1) / slots)), dim3(kThreads), 0, s, a);
     });
   };
@@ -402,9 +418,9 @@ size_t qk_norm_grad_workspace(long rows, int Hq, int Hk, int D) {
 hipError_t launch_qk_norm_grad(int dtype, const QkArgs& args, hipStream_t s) {
   QkArgs a = args;
   const int heads = a.side[0].heads + a.side[1].heads;
-  a.group = heads_of_item(a.rows, heads, kItems);
+  a.parts = parts_of(dtype, a.rows, heads);
   const int l = lanes(a, dtype == WM_FP32 ? 4 : 8);
-  for (int w = 0; w < 2; ++w) a.groups[w] = grad_groups(a.rows, a.side[w].heads, heads, l, a.group);
+  for (int w = 0; w < 2; ++w) a.groups[w] = grad_groups(a.rows, a.side[w].heads, heads, l, a.parts);
   auto run = [&](auto dt) {
     typedef decltype(dt) DT;
     return by_lanes<DT>(a, [&](auto l, auto w) {
