@@ -181,9 +181,56 @@ struct ProductArgs {
   long tiles_m, tiles_n;
 };
 
-// Outputs n .. n + 3 of row m (GLU: `gate` and `up` of its columns).
+// Four outputs of each of two neighbouring blocks of sixteen columns, of row m: a lane
+// holds columns 4 g .. + 3 of both, and stores them where n, the first block's first
+// column, says.  bf16 lanes first trade halves with the lanes of the next sixteen, so
+// that each has eight columns in a row of one block, 16 bytes to store in place of
+// two times 8.
 template <typename DT>
-__device__ __forceinline__ void put_glu(const ProductArgs& a, long m, long n, f32x4 gate, f32x4 up) {
+__device__ __forceinline__ void store_blocks(DT* row, long n, long width, int g, f32x4 x, f32x4 y) {
+  if constexpr (sizeof(DT) == 4) {
+    const float u[4] = {x[0], x[1], x[2], x[3]}, v[4] = {y[0], y[1], y[2], y[3]};
+    store4(row, n + 4 * g, width, u);
+    store4(row, n + 16 + 4 * g, width, v);
+  } else {
+    const auto p = __builtin_amdgcn_permlane16_swap(pack2_bf16(x[0], x[1]), pack2_bf16(y[0], y[1]), false, false);
+    const auto q = __builtin_amdgcn_permlane16_swap(pack2_bf16(x[2], x[3]), pack2_bf16(y[2], y[3]), false, false);
+    const v4u r = {p[0], q[0], p[1], q[1]};
+    const long c = n + 16 * (g & 1) + 8 * (g >> 1);
+    if (c + 8 <= width) {
+      *reinterpret_cast<v4u_2*>(row + c) = r;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < width) row[c + e] = (bf16_t)(r[e / 2] >> (16 * (e & 1)));
+    }
+  }
+}
+template <typename DT>
+__device__ __forceinline__ void put_glu(const ProductArgs& a, long m, long n, int g, const f32x4 (&gate)[2], const f32x4 (&up)[2]) {
+  f32x4 h[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) h[i][e] = activate(a.act, gate[i][e]).x * up[i][e];
+  store_blocks(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, g, h[0], h[1]);
+  if (a.pre) {
+    DT* pre = reinterpret_cast<DT*>(a.pre) + m * 2 * a.N;
+    store_blocks(pre, n, a.N, g, gate[0], gate[1]);
+    store_blocks(pre + a.N, n, a.N, g, up[0], up[1]);
+  }
+}
+template <typename DT>
+__device__ __forceinline__ void put(const ProductArgs& a, int split, long m, long n, int g, f32x4 x, f32x4 y) {
+  if (a.splits > 1)
+    store_blocks(a.part + ((long)split * a.M + m) * a.N, n, a.N, g, x, y);
+  else
+    store_blocks(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, g, x, y);
+}
+
+// Columns n .. + 3 alone.
+template <typename DT>
+__device__ __forceinline__ void put_one(const ProductArgs& a, long m, long n, f32x4 gate, f32x4 up) {
   float h[4], g[4], u[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
@@ -197,14 +244,6 @@ __device__ __forceinline__ void put_glu(const ProductArgs& a, long m, long n, f3
     store4(pre, n, a.N, g);
     store4(pre + a.N, n, a.N, u);
   }
-}
-template <typename DT>
-__device__ __forceinline__ void put(const ProductArgs& a, int split, long m, long n, f32x4 acc) {
-  const float v[4] = {acc[0], acc[1], acc[2], acc[3]};
-  if (a.splits > 1)
-    store4(a.part + ((long)split * a.M + m) * a.N, n, a.N, v);
-  else
-    store4(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, v);
 }
 
 // Any sizes, strides and alignments: tiles of 128 x 128, four waves of 64 x 64,
@@ -290,13 +329,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_product(const ProductArgs a) {
 #pragma unroll
   for (int l = 0; l < 4; ++l) {
     const long m = m0 + 64 * wq + 16 * l + j;
-    if (m >= a.M) continue;
-    if constexpr (GLU) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) put_glu<DT>(a, m, n0 + 32 * wp + 16 * i + 4 * g, acc[l][i], acc[l][i + 2]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) put<DT>(a, split, m, n0 + block(i) + 4 * g, acc[l][i]);
+    if (m < a.M) {
+      if constexpr (GLU) {
+        const f32x4 gate[2] = {acc[l][0], acc[l][1]}, up[2] = {acc[l][2], acc[l][3]};
+        put_glu<DT>(a, m, n0 + 32 * wp, g, gate, up);
+      } else {
+        put<DT>(a, split, m, n0 + block(0), g, acc[l][0], acc[l][1]);
+        put<DT>(a, split, m, n0 + block(2), g, acc[l][2], acc[l][3]);
+      }
     }
   }
 }
@@ -306,6 +346,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_product(const ProductArgs a) {
 // other is multiplied.  A wave's load is 1 KB in a row, so that padding cannot keep
 // rows apart; the order of a row's 16-byte pieces is changed instead, by the row's
 // number, so that the lanes of one read find different banks.
+constexpr int kBigGroups = 256;  // one a CU
 constexpr int kBig = 256, kBigThreads = 512, kBigK = 64, kBigBytes = kBig * kBigK * 2;
 __device__ __forceinline__ int turn_along(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int turn_across(int row) { return ((row & 3) | ((row >> 1) & 4)) << 1; }
@@ -349,7 +390,14 @@ struct Direct {
   }
   __device__ __forceinline__ void issue(uint32_t lds, long k0, long k1, int wave) const {
     const int left = (int)min(k1 - k0, (long)kBigK);
-    const u32x4 rs = ACROSS ? rsrc_words(base + k0 * ld, (uint32_t)((left - 1) * ld * 2) + bytes) : rsrc_words(base, bytes);
+    // (the same in every lane, which the compiler does not see through the tile's divisions)
+    const u32x4 rv = ACROSS ? rsrc_words(base + k0 * ld, (uint32_t)((left - 1) * ld * 2) + bytes) : rsrc_words(base, bytes);
+    u32x4 rs;
+    rs.x = (uint32_t)__builtin_amdgcn_readfirstlane((int)rv.x);
+    rs.y = (uint32_t)__builtin_amdgcn_readfirstlane((int)rv.y);
+    rs.z = (uint32_t)__builtin_amdgcn_readfirstlane((int)rv.z);
+    rs.w = 0x00020000u;
+    lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const uint32_t o = k[t] < left ? off[t] + (ACROSS ? 0u : (uint32_t)k0 * 2) : kOffNone;
@@ -370,68 +418,96 @@ struct Direct {
   }
 };
 
+// A work-group takes tile after tile, and requests the next one's first pieces before
+// it stores the present one: the stores then run beside the next tile's products.
 template <bool PX, bool QX, bool GLU>
 __global__ void __launch_bounds__(kBigThreads) k_product_big(const ProductArgs a) {
   __shared__ __align__(1024) char lds[4 * kBigBytes];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = w & 3, wq = w >> 2;
   const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
   // the XCDs take work-groups in turn: each gets a run of tiles, eight rows of tiles at a time
-  const long tiles = a.tiles_m * a.tiles_n, all = tiles * a.splits;
-  const long run8 = all / 8, extra = all % 8, xcd = blockIdx.x % 8;
-  const long at = xcd * run8 + min(xcd, extra) + blockIdx.x / 8;
-  const int split = (int)(at / tiles);
-  const long t = at % tiles, band = t / (8 * a.tiles_n), high = min(8L, a.tiles_m - 8 * band);
-  const long in = t - band * 8 * a.tiles_n;
-  const long m0 = (8 * band + in % high) * kBig, n0 = in / high * (GLU ? kBig / 2 : kBig);
-  const long k0 = split * a.per, k1 = min(k0 + a.per, a.K);
-
-  const Direct<PX, GLU> dp(a.P, n0, a.N, a.K, w, lane);
-  const Direct<QX, false> dq(a.Q, m0, a.M, a.K, w, lane);
+  const long tiles = a.tiles_m * a.tiles_n, all = tiles * a.splits, xcd = blockIdx.x % 8;
+  const long run8 = all / 8, extra = all % 8;
+  const long end = (xcd + 1) * run8 + min(xcd + 1, extra), step = gridDim.x / 8;
+  long at = xcd * run8 + min(xcd, extra) + blockIdx.x / 8;
+  if (at >= end) return;
+  struct Tile {
+    long m0, n0, k0, k1;
+    int split;
+  };
+  auto tile_at = [&](long i) {
+    Tile t;
+    t.split = (int)(i / tiles);
+    const long n = i - t.split * tiles, band = n / (8 * a.tiles_n), high = min(8L, a.tiles_m - 8 * band);
+    const long in = n - band * 8 * a.tiles_n;
+    t.m0 = (8 * band + in % high) * kBig;
+    t.n0 = in / high * (GLU ? kBig / 2 : kBig);
+    t.k0 = t.split * a.per;
+    t.k1 = min(t.k0 + a.per, a.K);
+    return t;
+  };
+  Tile t = tile_at(at);
+  Direct<PX, GLU> dp(a.P, t.n0, a.N, a.K, w, lane);
+  Direct<QX, false> dq(a.Q, t.m0, a.M, a.K, w, lane);
   const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds);
-  f32x4 acc[8][4];  // [block of Q][block of P]
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int k = 0; k < 4; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
   auto block = [&](int i) { return GLU ? 128 * (i >> 1) + 32 * wp + 16 * (i & 1) : 64 * wp + 16 * i; };
-  auto issue = [&](int buf, long k) {
+  auto issue = [&](int buf, long k, long k1) {
     dp.issue(lds0 + buf * 2 * kBigBytes, k, k1, w);
     dq.issue(lds0 + buf * 2 * kBigBytes + kBigBytes, k, k1, w);
   };
   int buf = 0;
-  if (k0 < k1) issue(0, k0);
-  for (long k = k0; k < k1; k += kBigK, buf ^= 1) {
-    // this step's pieces are in LDS, and the other buffer's reads are done, in every wave
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" : : : "memory");
-    if (k + kBigK < k1) issue(buf ^ 1, k + kBigK);
-    const char* const pl = lds + buf * 2 * kBigBytes;
-    const char* const ql = pl + kBigBytes;
+  issue(0, t.k0, t.k1);
+  for (;;) {
+    const Tile now = t;
+    const bool more = at + step < end;
+    f32x4 acc[8][4];  // [block of Q][block of P]
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      uint4 p[4], q[8];
+    for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = Direct<PX, GLU>::frag(pl, block(i), s);
+      for (int k = 0; k < 4; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (long k = now.k0; k < now.k1; k += kBigK, buf ^= 1) {
+      // this step's pieces are in LDS, and the other buffer's reads are done, in every wave
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" : : : "memory");
+      if (k + kBigK < now.k1) {
+        issue(buf ^ 1, k + kBigK, now.k1);
+      } else if (more) {
+        t = tile_at(at + step);
+        dp = Direct<PX, GLU>(a.P, t.n0, a.N, a.K, w, lane);
+        dq = Direct<QX, false>(a.Q, t.m0, a.M, a.K, w, lane);
+        issue(buf ^ 1, t.k0, t.k1);
+      }
+      const char* const pl = lds + buf * 2 * kBigBytes;
+      const char* const ql = pl + kBigBytes;
 #pragma unroll
-      for (int l = 0; l < 8; ++l) q[l] = Direct<QX, false>::frag(ql, 128 * wq + 16 * l, s);
+      for (int s = 0; s < 2; ++s) {
+        uint4 p[4], q[8];
 #pragma unroll
-      for (int l = 0; l < 8; ++l)
+        for (int i = 0; i < 4; ++i) p[i] = Direct<PX, GLU>::frag(pl, block(i), s);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) Mfma<bf16_t>::step(acc[l][i], p[i], q[l]);
+        for (int l = 0; l < 8; ++l) q[l] = Direct<QX, false>::frag(ql, 128 * wq + 16 * l, s);
+#pragma unroll
+        for (int l = 0; l < 8; ++l)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) Mfma<bf16_t>::step(acc[l][i], p[i], q[l]);
+      }
     }
-  }
 #pragma unroll
-  for (int l = 0; l < 8; ++l) {
-    const long m = m0 + 128 * wq + 16 * l + j;
-    if (m >= a.M) continue;
-    if constexpr (GLU) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) put_glu<bf16_t>(a, m, n0 + 32 * wp + 16 * i + 4 * g, acc[l][i], acc[l][i + 2]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) put<bf16_t>(a, split, m, n0 + block(i) + 4 * g, acc[l][i]);
+    for (int l = 0; l < 8; ++l) {
+      const long m = now.m0 + 128 * wq + 16 * l + j;
+      if (m < a.M) {
+        if constexpr (GLU) {
+          const f32x4 gate[2] = {acc[l][0], acc[l][1]}, up[2] = {acc[l][2], acc[l][3]};
+          put_glu<bf16_t>(a, m, now.n0 + 32 * wp, g, gate, up);
+        } else {
+          put<bf16_t>(a, now.split, m, now.n0 + block(0), g, acc[l][0], acc[l][1]);
+          put<bf16_t>(a, now.split, m, now.n0 + block(2), g, acc[l][2], acc[l][3]);
+        }
+      }
     }
+    if (!more) return;
+    at += step;
   }
 }
 
@@ -529,7 +605,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_glu_few(const ProductArgs a)
       gate += sum[k][2 * m][lane];
       up += sum[k][2 * m + 1][lane];
     }
-    if (16L * m + j < a.M) put_glu<DT>(a, 16L * m + j, n0 + 4 * g, gate, up);
+    if (16L * m + j < a.M) put_one<DT>(a, 16L * m + j, n0 + 4 * g, gate, up);
   }
 }
 
@@ -583,7 +659,7 @@ int splits_of(long M, long N, long K, int tile, int bk) {
 // The kernel of a product goes by its sizes: bf16 products with at least 64 tiles of
 // 256 x 256 take those.
 bool big(int dtype, long M, long N, long K) {
-  return dtype == WM_BF16 && K % 8 == 0 && (M + kBig - 1) / kBig * ((N + kBig - 1) / kBig) >= 64;
+  return dtype == WM_BF16 && K > 0 && K % 8 == 0 && (M + kBig - 1) / kBig * ((N + kBig - 1) / kBig) >= 64;
 }
 // Whether an operand's rows lie on 16-byte boundaries, and near enough for 32-bit offsets.
 bool direct(const Operand& a) {
@@ -609,8 +685,8 @@ hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
       a.tiles_m = (a.M + kBig - 1) / kBig;
       a.splits = GLU ? 1 : splits_of(a.M, a.N, a.K, kBig, kBigK);
       a.per = ((a.K + a.splits - 1) / a.splits + kBigK - 1) / kBigK * kBigK;
-      const hipError_t e = launch(name, k_product_big<PX, QX, GLU>, dim3((unsigned)(a.tiles_m * a.tiles_n * a.splits)),
-                                  dim3(kBigThreads), 0, s, a);
+      a.splits = (int)((a.K + a.per - 1) / a.per);  // none empty
+      const hipError_t e = launch(name, k_product_big<PX, QX, GLU>, dim3(kBigGroups), dim3(kBigThreads), 0, s, a);
       if (e != hipSuccess || a.splits == 1) return e;
       return launch("glu_sum", k_product_sum<DT>, dim3((unsigned)((a.M * a.N + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a);
     }
