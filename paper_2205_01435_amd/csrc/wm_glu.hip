@@ -140,17 +140,38 @@ struct Stage {
   }
 };
 
-__device__ __forceinline__ float normal_cdf(float x) { return 0.5f * erfcf(x * -0.70710678118654752f); }
-// act(g) and its derivative
+// act(g) and its derivative.  fp32: to full precision.  bf16, whose results are rounded
+// to 2^-9 of their value: sigmoid(g) from the hardware's exponential and reciprocal, off
+// by some 10^-7 of itself times |g|, and the normal distribution function by the formula
+// 7.1.26 of Abramowitz and Stegun's handbook, off by at most 10^-7 absolutely; of the
+// time of a tile of 256 x 256 with D 1024, the precise ones took a fifth.
+template <typename DT>
 __device__ __forceinline__ float2 activate(int act, float g) {
+  constexpr bool F32 = sizeof(DT) == 4;
   if (act == WM_ACT_SILU) {
-    // (sigmoid(g), sigmoid(-g)); beyond kGateMost the smaller is 0 to any product's precision
-    const float n = fabsf(g);
-    const float2 s = gate_pair_of(g, n > kGateMost ? 0.0f : gate_exp_small(n));
-    return make_float2(g * s.x, s.x * fmaf(g, s.y, 1.0f));
+    if constexpr (F32) {
+      // (sigmoid(g), sigmoid(-g)); beyond kGateMost the smaller is 0 to any product's precision
+      const float n = fabsf(g);
+      const float2 s = gate_pair_of(g, n > kGateMost ? 0.0f : gate_exp_small(n));
+      return make_float2(g * s.x, s.x * fmaf(g, s.y, 1.0f));
+    } else {
+      const float s = fsigmoid(g);
+      return make_float2(g * s, s * fmaf(g, 1.0f - s, 1.0f));
+    }
   }
-  const float c = normal_cdf(g);
-  return make_float2(g * c, fmaf(g * 0.39894228040143268f, expf(-0.5f * g * g), c));
+  const float density = fexp(-0.5f * g * g);
+  float c;
+  if constexpr (F32) {
+    c = 0.5f * erfcf(g * -0.70710678118654752f);
+    return make_float2(g * c, fmaf(g * 0.39894228040143268f, expf(-0.5f * g * g), c));
+  } else {
+    // with x = |g| / sqrt 2, t = 1 / (1 + 0.3275911 x): erfc(x) = (a1 t + .. + a5 t^5) e^(-x^2)
+    const float t = frcp(fmaf(fabsf(g), 0.3275911f * 0.70710678118654752f, 1.0f));
+    const float tail = 0.5f * density * t *
+                       fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    c = g < 0.0f ? tail : 1.0f - tail;
+    return make_float2(g * c, fmaf(g * 0.39894228040143268f, density, c));
+  }
 }
 
 template <typename DT>
@@ -212,7 +233,7 @@ __device__ __forceinline__ void put_glu(const ProductArgs& a, long m, long n, in
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) h[i][e] = activate(a.act, gate[i][e]).x * up[i][e];
+    for (int e = 0; e < 4; ++e) h[i][e] = activate<DT>(a.act, gate[i][e]).x * up[i][e];
   store_blocks(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, g, h[0], h[1]);
   if (a.pre) {
     DT* pre = reinterpret_cast<DT*>(a.pre) + m * 2 * a.N;
@@ -236,7 +257,7 @@ __device__ __forceinline__ void put_one(const ProductArgs& a, long m, long n, f3
   for (int e = 0; e < 4; ++e) {
     g[e] = gate[e];
     u[e] = up[e];
-    h[e] = activate(a.act, g[e]).x * u[e];
+    h[e] = activate<DT>(a.act, g[e]).x * u[e];
   }
   store4(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, h);
   if (a.pre) {
@@ -342,69 +363,82 @@ __global__ void __launch_bounds__(kThreads, 2) k_product(const ProductArgs a) {
 }
 
 // bf16 with rows on 16-byte boundaries: tiles of 256 x 256, eight waves of 128 x 64,
-// k 64 at a time straight from memory into one of two buffers in LDS while the
-// other is multiplied.  A wave's load is 1 KB in a row, so that padding cannot keep
-// rows apart; the order of a row's 16-byte pieces is changed instead, by the row's
-// number, so that the lanes of one read find different banks.
+// k 64 at a time straight from memory into one of two buffers in LDS.  A wave's load
+// is 1 KB in a row, so that padding cannot keep rows apart; the order of a row's
+// 16-byte pieces is changed instead, by the row's number, so that the lanes of one
+// read find different banks.  The products of one half of a step's k run while the
+// next half's operands are read from LDS; the one barrier of a step stands between
+// its halves, where all of its operands are read and its buffer takes the pieces of
+// the step after the next.  A work-group takes tile after tile, and its loads run on
+// into the next one, so that a tile's stores are beside the next one's products.
 constexpr int kBigGroups = 256;  // one a CU
 constexpr int kBig = 256, kBigThreads = 512, kBigK = 64, kBigBytes = kBig * kBigK * 2;
+constexpr int kBigLoads = 8;  // of a wave in a step, four for each operand
 __device__ __forceinline__ int turn_along(int row) { return (row >> 1) & 7; }
 __device__ __forceinline__ int turn_across(int row) { return ((row & 3) | ((row >> 1) & 4)) << 1; }
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 
 template <bool ACROSS, bool GLU>
 struct Direct {
-  // per lane: where its piece of each of this wave's four loads lies
-  uint32_t off[4];
-  int k[4];  // its first k in the step
-  const bf16_t* base;
-  uint32_t bytes;
-  long ld;
-  // outputs [o0, o0 + 256) of `outs`; GLU: 128 of each factor
-  __device__ __forceinline__ Direct(const Operand& a, long o0, long outs, long K, int wave, int lane) : ld(a.ld) {
+  uint32_t off[4];  // per lane: where its piece of each of this wave's four loads lies
+  uint32_t lo, hi, bytes, row;  // the resource, and the bytes that a step of k moves it by (ACROSS)
+  // outputs [o0, o0 + 256) of `outs`, GLU: 128 of each factor; k from k0 on
+  __device__ __forceinline__ void set(const Operand& a, long o0, long outs, long K, long k0, int wave, int lane) {
     const bf16_t* p = reinterpret_cast<const bf16_t*>(a.p);
+    long size;
     if constexpr (ACROSS) {
-      base = p + o0;
-      bytes = (uint32_t)(min(outs - o0, (long)kBig) * 2);  // of the last row
+      p += k0 * a.ld + o0;
+      size = min(outs - o0, (long)kBig) * 2;  // of the last row
     } else if constexpr (GLU) {
-      base = p;
-      bytes = (uint32_t)((2 * outs - 1) * ld + K) * 2;
+      size = ((2 * outs - 1) * a.ld + K) * 2;
     } else {
-      base = p + o0 * ld;
-      bytes = (uint32_t)(((min(outs - o0, (long)kBig) - 1) * ld + K) * 2);
+      p += o0 * a.ld;
+      size = ((min(outs - o0, (long)kBig) - 1) * a.ld + K) * 2;
     }
+    // (the same in every lane, which the compiler does not see through the tile's divisions)
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    lo = uniform((uint32_t)at);
+    hi = uniform((uint32_t)(at >> 32));
+    bytes = uniform((uint32_t)size);
+    row = (uint32_t)(a.ld * 2);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       const int q = 4 * wave + t;
       if constexpr (ACROSS) {
-        const int row = 2 * q + (lane >> 5), c = (lane & 31) ^ turn_across(row);
-        off[t] = (uint32_t)((row * ld + 8 * c) * 2);
-        k[t] = row;
+        const int r = 2 * q + (lane >> 5), c = (lane & 31) ^ turn_across(r);
+        off[t] = (uint32_t)((r * a.ld + 8 * c) * 2);
       } else {
-        const int row = 8 * q + (lane >> 3), c = (lane & 7) ^ turn_along(row), in = GLU ? row & 127 : row;
-        const bool ok = o0 + in < outs;
-        const long at = GLU ? (row < 128 ? o0 + in : outs + o0 + in) : row;
-        off[t] = ok ? (uint32_t)((at * ld + 8 * c) * 2) : kOffNone;
-        k[t] = 8 * c;
+        const int r = 8 * q + (lane >> 3), c = (lane & 7) ^ turn_along(r), in = GLU ? r & 127 : r;
+        const long at = GLU ? (r < 128 ? o0 + in : outs + o0 + in) : r;
+        off[t] = o0 + in < outs ? (uint32_t)((at * a.ld + 8 * c + k0) * 2) : kOffNone;
       }
     }
   }
-  __device__ __forceinline__ void issue(uint32_t lds, long k0, long k1, int wave) const {
-    const int left = (int)min(k1 - k0, (long)kBigK);
-    // (the same in every lane, which the compiler does not see through the tile's divisions)
-    const u32x4 rv = ACROSS ? rsrc_words(base + k0 * ld, (uint32_t)((left - 1) * ld * 2) + bytes) : rsrc_words(base, bytes);
+  // the pieces of the next step, which has `left` of k, into LDS
+  __device__ __forceinline__ void issue(uint32_t lds, int left, int wave, int lane) {
     u32x4 rs;
-    rs.x = (uint32_t)__builtin_amdgcn_readfirstlane((int)rv.x);
-    rs.y = (uint32_t)__builtin_amdgcn_readfirstlane((int)rv.y);
-    rs.z = (uint32_t)__builtin_amdgcn_readfirstlane((int)rv.z);
+    rs.x = uniform(lo);
+    rs.y = uniform(hi & 0xffffu);
+    rs.z = uniform(ACROSS ? (uint32_t)(min(left, kBigK) - 1) * row + bytes : bytes);
     rs.w = 0x00020000u;
-    lds = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds);
+    lds = uniform(lds);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      const uint32_t o = k[t] < left ? off[t] + (ACROSS ? 0u : (uint32_t)k0 * 2) : kOffNone;
+      uint32_t o = off[t];
+      if (left < kBigK) {  // the end of k: zeros from there on
+        const int r = ACROSS ? 2 * (4 * wave + t) + (lane >> 5) : 8 * (4 * wave + t) + (lane >> 3);
+        if ((ACROSS ? r : 8 * ((lane & 7) ^ turn_along(r))) >= left) o = kOffNone;
+      }
       dma16(rs, o, lds + (uint32_t)(4 * wave + t) * 1024u);
+      if (!ACROSS) off[t] = off[t] == kOffNone ? kOffNone : off[t] + kBigK * 2;
+    }
+    if (ACROSS) {
+      const uint64_t at = ((uint64_t)hi << 32 | lo) + (uint64_t)kBigK * row;
+      lo = (uint32_t)at;
+      hi = (uint32_t)(at >> 32);
     }
   }
-  // the fragment of sixteen outputs from o on, k from 32 s on
+  // the fragment of sixteen outputs from o on, half s of the step's k
   __device__ __forceinline__ static uint4 frag(const char* lds, int o, int s) {
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
     if constexpr (!ACROSS) {
@@ -418,81 +452,119 @@ struct Direct {
   }
 };
 
-// A work-group takes tile after tile, and requests the next one's first pieces before
-// it stores the present one: the stores then run beside the next tile's products.
 template <bool PX, bool QX, bool GLU>
 __global__ void __launch_bounds__(kBigThreads) k_product_big(const ProductArgs a) {
   __shared__ __align__(1024) char lds[4 * kBigBytes];
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wp = w & 3, wq = w >> 2;
   const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
   // the XCDs take work-groups in turn: each gets a run of tiles, eight rows of tiles at a time
-  const long tiles = a.tiles_m * a.tiles_n, all = tiles * a.splits, xcd = blockIdx.x % 8;
-  const long run8 = all / 8, extra = all % 8;
-  const long end = (xcd + 1) * run8 + min(xcd + 1, extra), step = gridDim.x / 8;
-  long at = xcd * run8 + min(xcd, extra) + blockIdx.x / 8;
-  if (at >= end) return;
+  const uint32_t tiles_m = (uint32_t)a.tiles_m, tiles_n = (uint32_t)a.tiles_n, tiles = tiles_m * tiles_n;
+  const uint32_t all = tiles * (uint32_t)a.splits, xcd = blockIdx.x % 8, run8 = all / 8, extra = all % 8;
+  const uint32_t end = (xcd + 1) * run8 + min(xcd + 1, extra), stride = gridDim.x / 8;
   struct Tile {
-    long m0, n0, k0, k1;
-    int split;
+    uint32_t at;
+    long m0, n0;
+    int split, left;  // what is left of its k
+    long k0;
   };
-  auto tile_at = [&](long i) {
+  auto tile_at = [&](uint32_t i) {
     Tile t;
+    t.at = i;
     t.split = (int)(i / tiles);
-    const long n = i - t.split * tiles, band = n / (8 * a.tiles_n), high = min(8L, a.tiles_m - 8 * band);
-    const long in = n - band * 8 * a.tiles_n;
-    t.m0 = (8 * band + in % high) * kBig;
-    t.n0 = in / high * (GLU ? kBig / 2 : kBig);
+    const uint32_t n = i - t.split * tiles, band = n / (8 * tiles_n), high = min(8u, tiles_m - 8 * band);
+    const uint32_t in = n - band * 8 * tiles_n;
+    t.m0 = (long)(8 * band + in % high) * kBig;
+    t.n0 = (long)(in / high) * (GLU ? kBig / 2 : kBig);
     t.k0 = t.split * a.per;
-    t.k1 = min(t.k0 + a.per, a.K);
+    t.left = (int)uniform((uint32_t)(min(t.k0 + a.per, a.K) - t.k0));
     return t;
   };
-  Tile t = tile_at(at);
-  Direct<PX, GLU> dp(a.P, t.n0, a.N, a.K, w, lane);
-  Direct<QX, false> dq(a.Q, t.m0, a.M, a.K, w, lane);
+  const uint32_t begin = xcd * run8 + min(xcd, extra) + blockIdx.x / 8;
+  if (begin >= end) return;
   const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)lds);
   auto block = [&](int i) { return GLU ? 128 * (i >> 1) + 32 * wp + 16 * (i & 1) : 64 * wp + 16 * i; };
-  auto issue = [&](int buf, long k, long k1) {
-    dp.issue(lds0 + buf * 2 * kBigBytes, k, k1, w);
-    dq.issue(lds0 + buf * 2 * kBigBytes + kBigBytes, k, k1, w);
+
+  // the loads' own place among the tiles, two steps ahead of the products'
+  Tile ahead = tile_at(begin);
+  Tile now = ahead;
+  bool more = true;
+  Direct<PX, GLU> dp;
+  Direct<QX, false> dq;
+  auto aim = [&]() {
+    dp.set(a.P, ahead.n0, a.N, a.K, ahead.k0, w, lane);
+    dq.set(a.Q, ahead.m0, a.M, a.K, ahead.k0, w, lane);
   };
-  int buf = 0;
-  issue(0, t.k0, t.k1);
-  for (;;) {
-    const Tile now = t;
-    const bool more = at + step < end;
-    f32x4 acc[8][4];  // [block of Q][block of P]
+  auto issue = [&](int buf) {
+    const uint32_t to = lds0 + (uint32_t)buf * 2 * kBigBytes;
+    dp.issue(to, ahead.left, w, lane);
+    dq.issue(to + kBigBytes, ahead.left, w, lane);
+    ahead.left -= kBigK;
+    if (ahead.left <= 0) {
+      more = ahead.at + stride < end;
+      if (more) {
+        ahead = tile_at(ahead.at + stride);
+        aim();
+      }
+    }
+  };
+  // operands: Q's are read for the next half as soon as their last product is under way,
+  // P's are held for both halves
+  uint4 p[4], q[8];
+  f32x4 acc[8][4];  // [block of Q][block of P]
+  auto clear = [&]() {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
       for (int k = 0; k < 4; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (long k = now.k0; k < now.k1; k += kBigK, buf ^= 1) {
-      // this step's pieces are in LDS, and the other buffer's reads are done, in every wave
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" : : : "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" : : : "memory");
-      if (k + kBigK < now.k1) {
-        issue(buf ^ 1, k + kBigK, now.k1);
-      } else if (more) {
-        t = tile_at(at + step);
-        dp = Direct<PX, GLU>(a.P, t.n0, a.N, a.K, w, lane);
-        dq = Direct<QX, false>(a.Q, t.m0, a.M, a.K, w, lane);
-        issue(buf ^ 1, t.k0, t.k1);
-      }
-      const char* const pl = lds + buf * 2 * kBigBytes;
-      const char* const ql = pl + kBigBytes;
+  };
+  auto half = [&](const char* from, int s) {
+    uint4 next[4];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        uint4 p[4], q[8];
+    for (int i = 0; i < 4; ++i) next[i] = Direct<PX, GLU>::frag(from, block(i), s);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = Direct<PX, GLU>::frag(pl, block(i), s);
+    for (int l = 0; l < 8; ++l) {
 #pragma unroll
-        for (int l = 0; l < 8; ++l) q[l] = Direct<QX, false>::frag(ql, 128 * wq + 16 * l, s);
-#pragma unroll
-        for (int l = 0; l < 8; ++l)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) Mfma<bf16_t>::step(acc[l][i], p[i], q[l]);
-      }
+      for (int i = 0; i < 4; ++i) Mfma<bf16_t>::step(acc[l][i], p[i], q[l]);
+      q[l] = Direct<QX, false>::frag(from + kBigBytes, 128 * wq + 16 * l, s);
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = next[i];
+  };
+  aim();
+  issue(0);
+  const bool second = more;
+  if (second) issue(1);
+  if (second)
+    vm_wait<kBigLoads>();
+  else
+    vm_wait<0>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" : : : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = Direct<PX, GLU>::frag(lds, block(i), 0);
+#pragma unroll
+  for (int l = 0; l < 8; ++l) q[l] = Direct<QX, false>::frag(lds + kBigBytes, 128 * wq + 16 * l, 0);
+  clear();
+  int stores = 0;  // a whole tile's, which are younger than the loads in flight
+  for (int buf = 0;; buf ^= 1) {
+    const char* const here = lds + buf * 2 * kBigBytes;
+    half(here, 1);
+    // the next step's pieces are in LDS and this one's operands in registers, in every wave
+    asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
+    if (stores == 0) vm_wait<0>();
+    else if (stores == 24) vm_wait<24>();
+    else if (stores == 16) vm_wait<16>();
+    else if (stores == 8) vm_wait<8>();
+    else vm_wait<32>();
+    stores = 0;
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" : : : "memory");
+    if (more) issue(buf);
+    // (after the last step the other buffer holds old pieces, which nothing uses)
+    half(lds + (buf ^ 1) * 2 * kBigBytes, 0);
+    now.left -= kBigK;
+    if (now.left > 0) continue;
+    // the tile is complete
 #pragma unroll
     for (int l = 0; l < 8; ++l) {
       const long m = now.m0 + 128 * wq + 16 * l + j;
@@ -506,8 +578,13 @@ __global__ void __launch_bounds__(kBigThreads) k_product_big(const ProductArgs a
         }
       }
     }
-    if (!more) return;
-    at += step;
+    // A whole tile's stores, one an instruction, are the youngest of what is in flight at the
+    // next wait; of others there may be fewer, and that wait is for all.
+    const bool whole = now.m0 + kBig <= a.M && now.n0 + (GLU ? kBig / 2 : kBig) <= a.N;
+    stores = !whole ? 0 : GLU ? (a.pre ? 24 : 8) : a.splits > 1 ? 32 : 16;
+    if (now.at + stride >= end) return;
+    now = tile_at(now.at + stride);
+    clear();
   }
 }
 
@@ -622,7 +699,7 @@ __device__ __forceinline__ void back_piece(const GluGradArgs& a, DT* dpre, long 
   unpack<DT>(rd, d);
 #pragma unroll
   for (int e = 0; e < V; ++e) {
-    const float2 v = activate(a.act, g[e]);
+    const float2 v = activate<DT>(a.act, g[e]);
     g[e] = d[e] * u[e] * v.y;
     u[e] = d[e] * v.x;
   }
