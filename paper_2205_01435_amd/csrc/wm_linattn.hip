@@ -135,6 +135,23 @@ struct Rows {
   }
 };
 
+// Columns 16 cb + 4 g .. + 3 and 16 (cb + 1) + 4 g .. + 3 of row s.  bf16 lanes first
+// trade halves with the lanes of the next sixteen, so that each has eight columns in a
+// row of one block, 16 bytes to store in place of two times 8.
+template <typename DT, int W, bool FAST>
+__device__ __forceinline__ void store_pair(const Rows<DT, W, FAST>& rows, const typename Rows<DT, W, FAST>::Chunk& k, int s, int cb,
+                                           int g, const float (&x)[4], const float (&y)[4]) {
+  if constexpr (FAST && sizeof(DT) == 2) {
+    const auto p = __builtin_amdgcn_permlane16_swap(pack2_bf16(x[0], x[1]), pack2_bf16(y[0], y[1]), false, false);
+    const auto q = __builtin_amdgcn_permlane16_swap(pack2_bf16(x[2], x[3]), pack2_bf16(y[2], y[3]), false, false);
+    const uint32_t c = (uint32_t)(16 * cb + 16 * (g & 1) + 8 * (g >> 1));
+    bstore16(k.r, ((uint32_t)s * (uint32_t)rows.t + c) * 2u, make_uint4(p[0], q[0], p[1], q[1]));
+  } else {
+    if (16 * cb < rows.width) rows.store(k, s, 16 * cb + 4 * g, x);
+    if (16 * (cb + 1) < rows.width) rows.store(k, s, 16 * (cb + 1) + 4 * g, y);
+  }
+}
+
 // A chunk's 64 rows in LDS, by all threads.
 template <typename DT, int W>
 struct Panel {
@@ -543,19 +560,21 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
       if (16 * w >= live) {  // the wave's rows are padding
         const float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int cb = 0; cb < KC / 16; ++cb)
-          if (16 * cb < wcols) ro.store(oc, r, 16 * cb + 4 * g, zero);
+        for (int cb = 0; cb < KC / 16; cb += 2) store_pair(ro, oc, r, cb, g, zero, zero);
       } else {
         const float win = a.s_inter * decayed(la, REV ? live - 1 - r : r + 1);
         const Intra<DT, KA, REV> P(bl, rows, wt, mask, r, w, g, j16, live, la, a.s_intra);
 #pragma unroll
-        for (int cb = 0; cb < KC / 16; ++cb) {
+        for (int cb = 0; cb < KC / 16; cb += 2) {
           if (16 * cb >= wcols) break;
-          const f32x4 in = entered<DT, KA, KC>(st, rows, cb, g, j16), own = P.template times<PC>(cl, cb, w, g, j16, live);
-          float v[4];
+          float v[2][4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = r < live ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
-          ro.store(oc, r, 16 * cb + 4 * g, v);
+          for (int i = 0; i < 2; ++i) {
+            const f32x4 in = entered<DT, KA, KC>(st, rows, cb + i, g, j16), own = P.template times<PC>(cl, cb + i, w, g, j16, live);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i][e] = r < live ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+          }
+          store_pair(ro, oc, r, cb, g, v[0], v[1]);
         }
       }
     }
@@ -639,36 +658,41 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
     if (16 * w >= live) {  // the wave's rows are padding
       const float zero[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int cb = 0; cb < VP / 16; ++cb)
-        if (16 * cb < a.kc) ov.store(cv, r, 16 * cb + 4 * g, zero);
+      for (int cb = 0; cb < VP / 16; cb += 2) store_pair(ov, cv, r, cb, g, zero, zero);
 #pragma unroll
-      for (int kb = 0; kb < KP / 16; ++kb)
-        if (16 * kb < a.ka) ok.store(ck, r, 16 * kb + 4 * g, zero);
+      for (int kb = 0; kb < KP / 16; kb += 2) store_pair(ok, ck, r, kb, g, zero, zero);
     } else {
       const float win = a.s_inter * decayed(la, live - 1 - r);
       const bool on = r < live;
       {
         const Intra<DT, KP, true> P(ql, k, wt, mask, r, w, g, j16, live, la, a.s_intra);
 #pragma unroll
-        for (int cb = 0; cb < VP / 16; ++cb) {
+        for (int cb = 0; cb < VP / 16; cb += 2) {
           if (16 * cb >= a.kc) break;
-          const f32x4 in = entered<DT, KP, VP>(st, k, cb, g, j16), own = P.template times<PV>(dl, cb, w, g, j16, live);
-          float x[4];
+          float x[2][4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
-          ov.store(cv, r, 16 * cb + 4 * g, x);
+          for (int i = 0; i < 2; ++i) {
+            const f32x4 in = entered<DT, KP, VP>(st, k, cb + i, g, j16), own = P.template times<PV>(dl, cb + i, w, g, j16, live);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i][e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+          }
+          store_pair(ov, cv, r, cb, g, x[0], x[1]);
         }
       }
       {
         const Intra<DT, VP, true> P(dl, v, wt, mask, r, w, g, j16, live, la, a.s_intra);
 #pragma unroll
-        for (int kb = 0; kb < KP / 16; ++kb) {
+        for (int kb = 0; kb < KP / 16; kb += 2) {
           if (16 * kb >= a.ka) break;
-          const f32x4 in = entered_across<DT, KP, VP>(st, v, kb, g, j16), own = P.template times<PK>(ql, kb, w, g, j16, live);
-          float x[4];
+          float x[2][4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
-          ok.store(ck, r, 16 * kb + 4 * g, x);
+          for (int i = 0; i < 2; ++i) {
+            const f32x4 in = entered_across<DT, KP, VP>(st, v, kb + i, g, j16),
+                        own = P.template times<PK>(ql, kb + i, w, g, j16, live);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[i][e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+          }
+          store_pair(ok, ck, r, kb, g, x[0], x[1]);
         }
       }
     }
