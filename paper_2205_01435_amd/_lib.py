@@ -862,13 +862,16 @@ def _heads(name, t, H, D, dtype, device):
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.device != device:
         _act(name, t, dtype)
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    shape, st = t.shape, t.stride()
+    shape = t.shape
     if len(shape) < 2 or shape[-2] != H or shape[-1] != D:
         raise ValueError(f"{name} has shape {tuple(shape)}, expected [..., {H}, {D}]")
-    n = t.numel() // (H * D) if H else math.prod(shape[:-2])
+    n = shape[0] if len(shape) == 3 else math.prod(shape[:-2])
+    if t.is_contiguous():
+        return n, H * D
+    st = t.stride()
     if n and H and ((D > 1 and st[-1] != 1) or (H > 1 and st[-2] != D)):
         raise ValueError(f"{name}'s heads must lie one after the other (strides {st})")
-    if n <= 1 or t.is_contiguous():
+    if n <= 1:
         return n, H * D
     lead = [(s, d) for s, d in zip(shape[:-2], st[:-2]) if s > 1]
     for (_, a), (s, b) in zip(lead, lead[1:]):
@@ -881,33 +884,38 @@ def _heads(name, t, H, D, dtype, device):
 
 def _qk_args(q, k, positions, rotary, gamma_q, gamma_k, bufs, grad):
     dt = _act("q", q)
-    dev, dtype = q.device, q.dtype
+    dev, dtype, shape = q.device, q.dtype, q.shape
     _here(dev)
-    if q.dim() < 2:
-        raise ValueError(f"q has shape {tuple(q.shape)}, expected [..., Hq, D]")
-    Hq, D = q.shape[-2:]
-    Hk = 0 if k is None else k.shape[-2] if isinstance(k, torch.Tensor) and k.dim() >= 2 else 1
+    if len(shape) < 2:
+        raise ValueError(f"q has shape {tuple(shape)}, expected [..., Hq, D]")
+    Hq, D = shape[-2], shape[-1]
     rows, ldq = _heads("q", q, Hq, D, dtype, dev)
-    ldk = 0
+    Hk, ldk, pk = 0, 0, None
     if k is not None:
+        Hk = k.shape[-2] if isinstance(k, torch.Tensor) and k.dim() >= 2 else 1
         nk, ldk = _heads("k", k, Hk, D, dtype, dev)
         if nk != rows:
             raise ValueError(f"k has {nk} rows, q has {rows}")
+        pk = k.data_ptr()
     pp = _arr("positions", positions, torch.int32, getattr(positions, "shape", ()), dev)
     if positions.numel() != rows:
         raise ValueError(f"{positions.numel()} positions for {rows} rows")
-    if rotary is not None and rotary.table.device != dev:
-        raise ValueError(f"the rotation's table is on {rotary.table.device}, expected {dev}")
-    R, nb, pt = (0, 0, None) if rotary is None else (rotary.R, int(rotary.neighbours), rotary.table.data_ptr())
+    R, nb, pt = 0, 0, None
+    if rotary is not None:
+        table = rotary.table
+        if table.device != dev:
+            raise ValueError(f"the rotation's table is on {table.device}, expected {dev}")
+        if table.dtype is not torch.int64 or table.numel() < rotary.R // 2 or not table.is_contiguous():
+            raise ValueError(f"the rotation's table must hold {rotary.R // 2} int64 words")
+        R, nb, pt = rotary.R, rotary.neighbours, table.data_ptr()
     pgq = _arr("gamma_q", gamma_q, torch.float32, (D,), dev, optional=True)
     pgk = _arr("gamma_k", gamma_k, torch.float32, (D,), dev, optional=True)
     if bufs is None:
         bufs = QkNormBuffers(rows, Hq, Hk, D, dtype, dev, grad=grad)
-    if (bufs.rows, bufs.Hq, bufs.Hk, bufs.D, bufs.dtype) != (rows, Hq, Hk, D, dtype) or bufs.q.device != dev:
+    if (bufs.rows, bufs.Hq, bufs.Hk, bufs.D) != (rows, Hq, Hk, D) or bufs.dtype is not dtype or bufs.q.device != dev:
         raise ValueError(f"buffers for rows={bufs.rows} Hq={bufs.Hq} Hk={bufs.Hk} D={bufs.D} {bufs.dtype} on "
                          f"{bufs.q.device}; the call has rows={rows} Hq={Hq} Hk={Hk} D={D} {dtype} on {dev}")
-    head = (dt, rows, Hq, Hk, D, R, nb, q.data_ptr(), ldq, _ptr(k), ldk, pgq, pgk)
-    return head, (pp, pt), bufs
+    return (dt, rows, Hq, Hk, D, R, nb, q.data_ptr(), ldq, pk, ldk, pgq, pgk), (pp, pt), bufs
 
 
 def qk_norm(q, k, positions, rotary: Rotary | None, gamma_q=None, gamma_k=None, eps: float = 1e-6,

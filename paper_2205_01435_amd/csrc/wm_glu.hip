@@ -70,6 +70,48 @@ struct Stage {
   template <bool SPLIT>
   static constexpr int bytes() { return Kind<DT, SPLIT>::PLANES * ROWS * pitch<SPLIT>() * (int)sizeof(typename Kind<DT, SPLIT>::T); }
   v4u r[N];
+  // fp32 rows lie on the 4 bytes that range-checked loads need: where they are near enough
+  // for 32-bit offsets, a piece takes one instruction, with none for its address
+  uint32_t off[N];
+  const DT* at;
+  uint32_t size;
+  __device__ __forceinline__ void aim(const Operand& a, long o0, long o1, int split, long outs, long K, long k0) {
+    const DT* p = reinterpret_cast<const DT*>(a.p);
+    const bool both = split < kTile;
+    at = ACROSS ? p + k0 * a.ld + o0 : both ? p : p + o0 * a.ld;
+    size = (uint32_t)(ACROSS ? min(outs - o0, (long)kTile) * 4 : (((both ? 2 * outs : min(outs - o0, (long)kTile)) - 1) * a.ld + K) * 4);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int q = threadIdx.x + i * kThreads, row = q / (COLS / V), col = q % (COLS / V) * V;
+      if constexpr (ACROSS) {
+        off[i] = (uint32_t)((row * a.ld + col) * 4);
+      } else {
+        const int in = row < split ? row : row - split;
+        const long o = both ? (row < split ? o0 + row : o1 + in) : row;
+        off[i] = o0 + in < outs ? (uint32_t)((o * a.ld + k0 + col) * 4) : kOffNone;
+      }
+    }
+  }
+  // the next BK, of which `left` are there
+  __device__ __forceinline__ void fetch(const Operand& a, long left) {
+    const rsrc_t rs = uniform_rsrc(at, ACROSS ? (uint32_t)((min(left, (long)BK) - 1) * a.ld * 4) + size : size);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint4 v = bload16(rs, off[i]);
+      r[i] = v4u{v.x, v.y, v.z, v.w};
+      if constexpr (!ACROSS) off[i] = off[i] == kOffNone ? kOffNone : off[i] + BK * 4;
+    }
+    if constexpr (ACROSS) {
+      at += BK * a.ld;
+    } else if (left < BK) {  // the end of k, where a row goes on with something else
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int col = (threadIdx.x + i * kThreads) % (COLS / V) * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) r[i][e] = col + e < left ? r[i][e] : 0u;
+      }
+    }
+  }
   // outputs [o0, o0 + 128) of `outs`, k [k0, k0 + BK) up to kend; `split` rows of the
   // tile on, outputs count from o1 (the other factor's columns)
   __device__ __forceinline__ void load(const Operand& a, long o0, long o1, int split, long outs, long k0, long kend) {
@@ -269,7 +311,7 @@ __device__ __forceinline__ void put_one(const ProductArgs& a, long m, long n, f3
 
 // Any sizes, strides and alignments: tiles of 128 x 128, four waves of 64 x 64,
 // the next k's pieces on their way in registers.
-template <typename DT, bool PX, bool QX, bool GLU>
+template <typename DT, bool PX, bool QX, bool GLU, bool NEAR>
 __global__ void __launch_bounds__(kThreads, 2) k_product(const ProductArgs a) {
   typedef Stage<DT, PX> SP;
   typedef Stage<DT, QX> SQ;
@@ -298,17 +340,26 @@ __global__ void __launch_bounds__(kThreads, 2) k_product(const ProductArgs a) {
     for (int i = 0; i < L; ++i)
 #pragma unroll
       for (int k = 0; k < 4; ++k) acc[i][k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    sp.load(a.P, n0, a.N + n0, half, a.N, k0, k1);
-    sq.load(a.Q, m0, 0, kTile, a.M, k0, k1);
+    auto load = [&](long k) {
+      if constexpr (NEAR) {
+        sp.fetch(a.P, k1 - k);
+        sq.fetch(a.Q, k1 - k);
+      } else {
+        sp.load(a.P, n0, a.N + n0, half, a.N, k, k1);
+        sq.load(a.Q, m0, 0, kTile, a.M, k, k1);
+      }
+    };
+    if constexpr (NEAR) {
+      sp.aim(a.P, n0, a.N + n0, half, a.N, a.K, k0);
+      sq.aim(a.Q, m0, 0, kTile, a.M, a.K, k0);
+    }
+    if (k0 < k1) load(k0);
     for (long k = k0; k < k1; k += BK) {
       __syncthreads();
       sp.template store<SPLIT>(pl);
       sq.template store<SPLIT>(ql);
       __syncthreads();
-      if (k + BK < k1) {
-        sp.load(a.P, n0, a.N + n0, half, a.N, k + BK, k1);
-        sq.load(a.Q, m0, 0, kTile, a.M, k + BK, k1);
-      }
+      if (k + BK < k1) load(k + BK);
 #pragma unroll
       for (int s = 0; s < BK; s += Kind<DT, SPLIT>::SL) {
         typename Kind<DT, SPLIT>::Frag p[4];
@@ -773,8 +824,14 @@ hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
   a.tiles_m = (a.M + kTile - 1) / kTile;
   a.splits = GLU ? 1 : splits_of(a.M, a.N, a.K, kTile, BK);
   a.per = ((a.K + a.splits - 1) / a.splits + BK - 1) / BK * BK;
-  const hipError_t e =
-      launch(name, k_product<DT, PX, QX, GLU>, dim3((unsigned)(a.tiles_m * a.tiles_n * a.splits)), dim3(kThreads), 0, s, a);
+  const dim3 grid((unsigned)(a.tiles_m * a.tiles_n * a.splits));
+  hipError_t e;
+  if constexpr (sizeof(DT) == 4) {
+    const bool near = a.P.ld <= 1 << 20 && a.Q.ld <= 1 << 20 && (!GLU || 2 * a.N * a.P.ld < (1L << 29));
+    e = launch(name, near ? k_product<DT, PX, QX, GLU, true> : k_product<DT, PX, QX, GLU, false>, grid, dim3(kThreads), 0, s, a);
+  } else {
+    e = launch(name, k_product<DT, PX, QX, GLU, false>, grid, dim3(kThreads), 0, s, a);
+  }
   if (e != hipSuccess || a.splits == 1) return e;
   return launch("glu_sum", k_product_sum<DT>, dim3((unsigned)((a.M * a.N + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a);
 }
