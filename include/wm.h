@@ -617,28 +617,31 @@ wm_status wm_linattn_grad(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_
  *   of the gate, then those of the other factor.
  *   act                  WM_ACT_SILU g sigmoid(g), WM_ACT_GELU g Phi(g) with the
  *                        normal distribution function.
- *   pre [rows, 2F] in dtype, nullable: receives [g | u], what the gradient reads.
+ *   saved                nullable: a 256-byte aligned buffer of wm_glu_saved_bytes
+ *                        that receives what wm_glu_grad needs.
  * D and F in 1 .. 65536; rows at most 2^31 - 1 and rows F at most 2^43.  rows = 0 is
  * a no-op.
  */
 enum { WM_ACT_SILU = 0, WM_ACT_GELU = 1 };
+size_t wm_glu_saved_bytes(int32_t dtype, int64_t rows, int32_t D, int32_t F);
 wm_status wm_glu(int32_t dtype, int64_t rows, int32_t D, int32_t F, int32_t act, const void *x,
-                 int64_t x_ld, const void *W, void *h, int64_t h_ld, void *pre,
-                 wm_stream_t stream);
+                 int64_t x_ld, const void *W, void *h, int64_t h_ld, void *saved,
+                 size_t saved_bytes, wm_stream_t stream);
 
 /*
- * Gradient of wm_glu from its inputs and `pre`:
+ * Gradient of wm_glu from its inputs and what it saved:
  *   dg = grad_h u act'(g), du = grad_h act(g);
  *   grad_x = [dg | du] W;  grad_W = [dg | du]^T x, in dtype (the weights' own type),
  *   summed in fp32, nullable, written whole; rows = 0 writes zeros.
- * With bf16, g and u were rounded when they were saved, and dg and du are rounded
- * once before the two products.
+ * With bf16, g and u are saved with 16 significant bits, and dg and du are rounded
+ * to bf16 before the two products.
  */
 size_t wm_glu_grad_workspace_bytes(int32_t dtype, int64_t rows, int32_t D, int32_t F);
 wm_status wm_glu_grad(int32_t dtype, int64_t rows, int32_t D, int32_t F, int32_t act,
-                      const void *x, int64_t x_ld, const void *W, const void *pre,
-                      const void *grad_h, int64_t grad_h_ld, void *grad_x, int64_t grad_x_ld,
-                      void *grad_W, void *workspace, size_t workspace_bytes, wm_stream_t stream);
+                      const void *x, int64_t x_ld, const void *W, const void *saved,
+                      size_t saved_bytes, const void *grad_h, int64_t grad_h_ld, void *grad_x,
+                      int64_t grad_x_ld, void *grad_W, void *workspace, size_t workspace_bytes,
+                      wm_stream_t stream);
 
 /*
  * Measurement aid (no counterpart in the paper).  While a prefix is set, every

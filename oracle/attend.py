@@ -170,14 +170,15 @@ def glu(x, W, act):
 
 
 def glu_grad(x, W, dh, act, dtype="fp32"):
-    """dict(dx, dW, *_err): g and u as the forward call saved them (bf16: rounded),
-    curvatures of the activation at most 1, dg and du rounded once in bf16, and the
+    """dict(dx, dW, *_err): g and u as the forward call saved them (bf16: cut to 16
+    significant bits), curvatures of the activation at most 1, dg and du rounded once in bf16, and the
     products' sums over 2F and the rows."""
     f = glu(x, W, act)
     x, W, dh = x.astype(np.float64), W.astype(np.float64), dh.astype(np.float64)
     F = W.shape[0] // 2
     r = U16 if dtype == "bf16" else 0.0
-    eg, eu = f["pre_err"][:, :F] + r * np.abs(f["g"]), f["pre_err"][:, F:] + r * np.abs(f["u"])
+    cut = 2.0 ** -15 if dtype == "bf16" else 0.0
+    eg, eu = f["pre_err"][:, :F] + cut * np.abs(f["g"]), f["pre_err"][:, F:] + cut * np.abs(f["u"])
     dg, du = dh * f["u"] * f["da"], dh * f["a"]
     edg = np.abs(dh) * (np.abs(f["u"]) * (eg + 16 * U32) + np.abs(f["da"]) * eu) + (r + 2 * U32) * np.abs(dg)
     edu = np.abs(dh) * (1.13 * eg + 16 * U32 * np.abs(f["g"])) + (r + 2 * U32) * np.abs(du)

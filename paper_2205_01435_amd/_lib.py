@@ -33,7 +33,8 @@ EXPORTS = ("wm_packed_weights_bytes", "wm_pack_weights", "wm_workspace_bytes", "
            "wm_layer_norm_grad_workspace_bytes", "wm_layer_norm_grad", "wm_linrec_states_bytes",
            "wm_linrec_workspace_bytes", "wm_linrec", "wm_linrec_grad", "wm_clip_grads_workspace_bytes",
            "wm_clip_grads", "wm_rotary_table", "wm_qk_norm", "wm_qk_norm_grad_workspace_bytes", "wm_qk_norm_grad",
-           "wm_linattn_states_bytes", "wm_linattn_workspace_bytes", "wm_linattn", "wm_linattn_grad", "wm_glu",
+           "wm_linattn_states_bytes", "wm_linattn_workspace_bytes", "wm_linattn", "wm_linattn_grad", "wm_glu_saved_bytes",
+           "wm_glu",
            "wm_glu_grad_workspace_bytes", "wm_glu_grad",
            "wm_profile_enable", "wm_profile_read", "wm_profile_reset", "wm_profile_phases",
            "wm_profile_phases_read", "wm_workspace_status",
@@ -142,11 +143,13 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.wm_linattn_grad.argtypes = [I32, I32, I32, I32, I32, I32, P, I64, I64, P, I64, I64, P, I64, I64, P, F32, P, P, P,
                                     P, I64, I64, P, P, SZ, P, I64, I64, P, I64, I64, P, I64, I64, P, P, SZ, P]
     lib.wm_linattn_grad.restype = I32
-    lib.wm_glu.argtypes = [I32, I64, I32, I32, I32, P, I64, P, P, I64, P, P]
+    lib.wm_glu_saved_bytes.argtypes = [I32, I64, I32, I32]
+    lib.wm_glu_saved_bytes.restype = SZ
+    lib.wm_glu.argtypes = [I32, I64, I32, I32, I32, P, I64, P, P, I64, P, SZ, P]
     lib.wm_glu.restype = I32
     lib.wm_glu_grad_workspace_bytes.argtypes = [I32, I64, I32, I32]
     lib.wm_glu_grad_workspace_bytes.restype = SZ
-    lib.wm_glu_grad.argtypes = [I32, I64, I32, I32, I32, P, I64, P, P, P, I64, P, I64, P, P, SZ, P]
+    lib.wm_glu_grad.argtypes = [I32, I64, I32, I32, I32, P, I64, P, P, SZ, P, I64, P, I64, P, P, SZ, P]
     lib.wm_glu_grad.restype = I32
     lib.wm_profile_enable.argtypes = [ctypes.c_char_p]
     lib.wm_profile_enable.restype = I32
@@ -1036,16 +1039,19 @@ _GLU_ACTS = {"silu": 0, "gelu": 1}
 
 
 class GluBuffers:
-    """Output [rows, F] of the gated projection, and with ``grad`` its two factors
-    before the activation (``pre`` [rows, 2F]), the gradients and the workspace."""
+    """Output [rows, F] of the gated projection, and with ``grad`` what it saves for
+    the gradient, the gradients and the workspace."""
 
     def __init__(self, rows: int, D: int, F: int, dtype=torch.float32, device="cuda", grad: bool = True):
         self.rows, self.D, self.F, self.dtype = rows, D, F, dtype
+        lib = load()
         new = lambda *s: torch.empty(s, dtype=dtype, device=device)  # noqa: E731
+        raw = lambda n: torch.empty(max(n, 1), dtype=torch.uint8, device=device) if grad else None  # noqa: E731
         self.h = new(rows, F)
-        self.pre, self.dx, self.dW = (new(rows, 2 * F), new(rows, D), new(2 * F, D)) if grad else (None,) * 3
-        self.ws_bytes = load().wm_glu_grad_workspace_bytes(_ACT[dtype], rows, D, F) if grad else 0
-        self.workspace = torch.empty(max(self.ws_bytes, 1), dtype=torch.uint8, device=device) if grad else None
+        self.dx, self.dW = (new(rows, D), new(2 * F, D)) if grad else (None, None)
+        self.saved_bytes = lib.wm_glu_saved_bytes(_ACT[dtype], rows, D, F) if grad else 0
+        self.ws_bytes = lib.wm_glu_grad_workspace_bytes(_ACT[dtype], rows, D, F) if grad else 0
+        self.saved, self.workspace = raw(self.saved_bytes), raw(self.ws_bytes)
 
 
 def _glu_args(x, W, act, bufs):
@@ -1068,25 +1074,25 @@ def _glu_args(x, W, act, bufs):
 def glu(x, W, act: str = "silu", bufs: GluBuffers | None = None) -> GluBuffers:
     """Launch wm_glu on the current stream: act(x W[:F]^T) * (x W[F:]^T) for the
     rows of ``x`` [..., D] and ``W`` [2F, D]; returns the filled buffers (h, and
-    pre, which glu_grad reads)."""
+    what glu_grad reads)."""
     head = _glu_args(x, W, act, bufs)
     if bufs is None:
         bufs = GluBuffers(head[1], head[2], head[3], x.dtype, x.device)
-    _check(load().wm_glu(*head, bufs.h.data_ptr(), bufs.F, _ptr(bufs.pre), _stream()))
+    _check(load().wm_glu(*head, bufs.h.data_ptr(), bufs.F, _ptr(bufs.saved), bufs.saved_bytes, _stream()))
     return bufs
 
 
 def glu_grad(x, W, dh, act: str = "silu", bufs: GluBuffers | None = None) -> GluBuffers:
     """Launch wm_glu_grad on the current stream: dx and dW (in the weights' type)
-    from the forward call's inputs and the factors in its ``bufs``."""
+    from the forward call's inputs and what it saved in its ``bufs``."""
     head = _glu_args(x, W, act, bufs)
-    if bufs is None or bufs.pre is None:
+    if bufs is None or bufs.saved is None:
         raise ValueError("glu_grad needs the forward call's buffers, made with grad=True")
     n, ld = _rows("dh", dh, bufs.F, x.dtype, x.device)
     if n != bufs.rows:
         raise ValueError(f"dh has {n} rows, x has {bufs.rows}")
-    _check(load().wm_glu_grad(*head, bufs.pre.data_ptr(), dh.data_ptr(), ld, bufs.dx.data_ptr(), bufs.D, bufs.dW.data_ptr(),
-                              bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
+    _check(load().wm_glu_grad(*head, bufs.saved.data_ptr(), bufs.saved_bytes, dh.data_ptr(), ld, bufs.dx.data_ptr(),
+                              bufs.D, bufs.dW.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
     return bufs
 
 

@@ -868,19 +868,24 @@ wm_status wm_linattn_grad(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_
 }
 
 wm_status wm_glu(int32_t dtype, int64_t rows, int32_t D, int32_t F, int32_t act, const void* x, int64_t x_ld, const void* W,
-                 void* h, int64_t h_ld, void* pre, wm_stream_t stream) {
+                 void* h, int64_t h_ld, void* saved, size_t saved_bytes, wm_stream_t stream) {
   wm_status st = check_dtype(dtype);
   if (st != WM_OK || (st = check_glu(rows, D, F, act)) != WM_OK || (st = check_ld("x", rows, D, x_ld)) != WM_OK ||
       (st = check_ld("h", rows, F, h_ld)) != WM_OK)
     return st;
   if (rows == 0) return ok();
   if (!x || !W || !h) return fail(WM_ERR_INVALID_ARG, "x, W and h are required");
-  if (!aligned_el(x, dtype) || !aligned_el(W, dtype) || !aligned_el(h, dtype) || !aligned_el(pre, dtype))
+  if (!aligned_el(x, dtype) || !aligned_el(W, dtype) || !aligned_el(h, dtype))
     return fail(WM_ERR_INVALID_ARG, "arrays must be aligned to their elements");
-  const wm::GluArgs a{(long)rows, D, F, act, x, (long)x_ld, W, h, (long)h_ld, pre};
+  if (saved && (st = check_workspace("saved", saved, saved_bytes, wm::glu_saved(dtype, (long)rows, F))) != WM_OK) return st;
+  const wm::GluArgs a{(long)rows, D, F, act, x, (long)x_ld, W, h, (long)h_ld, saved};
   const hipError_t e = wm::launch_glu(dtype, a, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "wm_glu");
   return ok();
+}
+
+size_t wm_glu_saved_bytes(int32_t dtype, int64_t rows, int32_t D, int32_t F) {
+  return check_dtype(dtype) == WM_OK && check_glu(rows, D, F, WM_ACT_SILU) == WM_OK ? wm::glu_saved(dtype, (long)rows, F) : 0;
 }
 
 size_t wm_glu_grad_workspace_bytes(int32_t dtype, int64_t rows, int32_t D, int32_t F) {
@@ -890,21 +895,22 @@ size_t wm_glu_grad_workspace_bytes(int32_t dtype, int64_t rows, int32_t D, int32
 }
 
 wm_status wm_glu_grad(int32_t dtype, int64_t rows, int32_t D, int32_t F, int32_t act, const void* x, int64_t x_ld,
-                      const void* W, const void* pre, const void* grad_h, int64_t grad_h_ld, void* grad_x, int64_t grad_x_ld,
-                      void* grad_W, void* workspace, size_t workspace_bytes, wm_stream_t stream) {
+                      const void* W, const void* saved, size_t saved_bytes, const void* grad_h, int64_t grad_h_ld, void* grad_x,
+                      int64_t grad_x_ld, void* grad_W, void* workspace, size_t workspace_bytes, wm_stream_t stream) {
   wm_status st = check_dtype(dtype);
   if (st != WM_OK || (st = check_glu(rows, D, F, act)) != WM_OK || (st = check_ld("x", rows, D, x_ld)) != WM_OK ||
       (st = check_ld("grad_h", rows, F, grad_h_ld)) != WM_OK || (st = check_ld("grad_x", rows, D, grad_x_ld)) != WM_OK)
     return st;
-  if (rows > 0 && (!x || !W || !pre || !grad_h || !grad_x))
-    return fail(WM_ERR_INVALID_ARG, "x, W, pre, grad_h and grad_x are required");
-  if (!aligned_el(x, dtype) || !aligned_el(W, dtype) || !aligned_el(pre, dtype) || !aligned_el(grad_h, dtype) ||
+  if (rows > 0 && (!x || !W || !grad_h || !grad_x))
+    return fail(WM_ERR_INVALID_ARG, "x, W, grad_h and grad_x are required");
+  if (!aligned_el(x, dtype) || !aligned_el(W, dtype) || !aligned_el(grad_h, dtype) ||
       !aligned_el(grad_x, dtype) || !aligned_el(grad_W, dtype))
     return fail(WM_ERR_INVALID_ARG, "arrays must be aligned to their elements");
-  if ((st = check_workspace("the workspace of wm_glu_grad", workspace, workspace_bytes,
+  if ((st = check_workspace("saved", saved, saved_bytes, wm::glu_saved(dtype, (long)rows, F))) != WM_OK ||
+      (st = check_workspace("the workspace of wm_glu_grad", workspace, workspace_bytes,
                             wm::glu_grad_workspace(dtype, (long)rows, D, F))) != WM_OK)
     return st;
-  const wm::GluGradArgs a{(long)rows, D, F, act, x, (long)x_ld, W, pre, grad_h, (long)grad_h_ld, grad_x, (long)grad_x_ld,
+  const wm::GluGradArgs a{(long)rows, D, F, act, x, (long)x_ld, W, saved, grad_h, (long)grad_h_ld, grad_x, (long)grad_x_ld,
                           grad_W, workspace};
   const hipError_t e = wm::launch_glu_grad(dtype, a, reinterpret_cast<hipStream_t>(stream));
   if (e != hipSuccess) return hip_fail(e, "wm_glu_grad");

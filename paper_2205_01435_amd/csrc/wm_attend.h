@@ -78,7 +78,7 @@ struct GluArgs {
   const void* W;  // [2F, D]: the gate's rows, then the other factor's
   void* h;
   long h_ld;
-  void* pre;  // [rows, 2F] or null
+  void* saved;  // glu_saved bytes, or null
 };
 struct GluGradArgs {
   long rows;
@@ -86,7 +86,7 @@ struct GluGradArgs {
   const void* x;
   long x_ld;
   const void* W;
-  const void* pre;
+  const void* saved;
   const void* dh;
   long dh_ld;
   void* dx;
@@ -94,6 +94,7 @@ struct GluGradArgs {
   void* dW;  // [2F, D], or null
   void* ws;
 };
+size_t glu_saved(int dtype, long rows, int F);
 size_t glu_grad_workspace(int dtype, long rows, int D, int F);
 hipError_t launch_glu(int dtype, const GluArgs& a, hipStream_t s);
 hipError_t launch_glu_grad(int dtype, const GluGradArgs& a, hipStream_t s);

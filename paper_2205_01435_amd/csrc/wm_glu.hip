@@ -236,7 +236,7 @@ struct ProductArgs {
   long M, N, K;     // outputs of Q and P, the sum's length
   void* out;        // [M, N] (GLU: h [M, N] with N = F)
   long out_ld;
-  void* pre;        // GLU: [M, 2 N] or null
+  void* saved;      // GLU: the factors for the gradient, or null
   int act;
   float* part;      // splits > 1: [splits][M][N]
   int splits;
@@ -269,6 +269,52 @@ __device__ __forceinline__ void store_blocks(DT* row, long n, long width, int g,
     }
   }
 }
+// What the gradient needs of the two factors, [rows, 2F]: fp32 values as they are; of
+// bf16 calls the upper 24 bits of the fp32 sums, as 16 in one plane and 8 in another:
+// rounded to bf16 they would put as much error into dx and dW as the rounding of these
+// themselves (2-norm of the error against the result 0.0030, with 24 bits 0.0024; 0.0017
+// is the outputs' own rounding).
+size_t low_plane(long rows, long F) { return ((size_t)rows * 2 * F * 2 + 255) / 256 * 256; }
+__device__ __forceinline__ char* low_of(void* saved, long rows, long F) {
+  return reinterpret_cast<char*>(saved) + (rows * 2 * F * 2 + 255) / 256 * 256;
+}
+typedef uint32_t __attribute__((aligned(1))) u32_1;
+typedef v2u __attribute__((aligned(1))) v2u_1;
+// the upper halves of two, and the third bytes of four
+__device__ __forceinline__ uint32_t upper2(float a, float b) {
+  return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+}
+__device__ __forceinline__ uint32_t third4(f32x4 v) {
+  const uint32_t a = __builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x0c0c0501u);
+  const uint32_t b = __builtin_amdgcn_perm(__float_as_uint(v[3]), __float_as_uint(v[2]), 0x05010c0cu);
+  return a | b;
+}
+template <typename DT>
+__device__ __forceinline__ void save_blocks(void* saved, long rows, long F, long m, long n, long width, int g, f32x4 x, f32x4 y) {
+  if constexpr (sizeof(DT) == 4) {
+    store_blocks(reinterpret_cast<float*>(saved) + m * 2 * F, n, width, g, x, y);
+  } else {
+    const auto p = __builtin_amdgcn_permlane16_swap(upper2(x[0], x[1]), upper2(y[0], y[1]), false, false);
+    const auto q = __builtin_amdgcn_permlane16_swap(upper2(x[2], x[3]), upper2(y[2], y[3]), false, false);
+    const auto t = __builtin_amdgcn_permlane16_swap(third4(x), third4(y), false, false);
+    const long c = n + 16 * (g & 1) + 8 * (g >> 1);
+    bf16_t* const hi = reinterpret_cast<bf16_t*>(saved) + m * 2 * F;
+    char* const lo = low_of(saved, rows, F) + m * 2 * F;
+    const v4u r = {p[0], q[0], p[1], q[1]};
+    const v2u l = {t[0], t[1]};
+    if (c + 8 <= width) {
+      *reinterpret_cast<v4u_2*>(hi + c) = r;
+      *reinterpret_cast<v2u_1*>(lo + c) = l;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < width) {
+          hi[c + e] = (bf16_t)(r[e / 2] >> (16 * (e & 1)));
+          lo[c + e] = (char)(l[e / 4] >> (8 * (e & 3)));
+        }
+    }
+  }
+}
 template <typename DT>
 __device__ __forceinline__ void put_glu(const ProductArgs& a, long m, long n, int g, const f32x4 (&gate)[2], const f32x4 (&up)[2]) {
   f32x4 h[2];
@@ -277,10 +323,9 @@ __device__ __forceinline__ void put_glu(const ProductArgs& a, long m, long n, in
 #pragma unroll
     for (int e = 0; e < 4; ++e) h[i][e] = activate<DT>(a.act, gate[i][e]).x * up[i][e];
   store_blocks(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, g, h[0], h[1]);
-  if (a.pre) {
-    DT* pre = reinterpret_cast<DT*>(a.pre) + m * 2 * a.N;
-    store_blocks(pre, n, a.N, g, gate[0], gate[1]);
-    store_blocks(pre + a.N, n, a.N, g, up[0], up[1]);
+  if (a.saved) {
+    save_blocks<DT>(a.saved, a.M, a.N, m, n, a.N, g, gate[0], gate[1]);
+    save_blocks<DT>(a.saved, a.M, a.N, m, a.N + n, 2 * a.N, g, up[0], up[1]);
   }
 }
 template <typename DT>
@@ -294,18 +339,27 @@ __device__ __forceinline__ void put(const ProductArgs& a, int split, long m, lon
 // Columns n .. + 3 alone.
 template <typename DT>
 __device__ __forceinline__ void put_one(const ProductArgs& a, long m, long n, f32x4 gate, f32x4 up) {
-  float h[4], g[4], u[4];
+  float h[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    g[e] = gate[e];
-    u[e] = up[e];
-    h[e] = activate<DT>(a.act, g[e]).x * u[e];
-  }
+  for (int e = 0; e < 4; ++e) h[e] = activate<DT>(a.act, gate[e]).x * up[e];
   store4(reinterpret_cast<DT*>(a.out) + m * a.out_ld, n, a.N, h);
-  if (a.pre) {
-    DT* pre = reinterpret_cast<DT*>(a.pre) + m * 2 * a.N;
-    store4(pre, n, a.N, g);
-    store4(pre + a.N, n, a.N, u);
+  if (!a.saved) return;
+#pragma unroll
+  for (int f = 0; f < 2; ++f) {
+    const f32x4 v = f ? up : gate;
+    if constexpr (sizeof(DT) == 4) {
+      const float x[4] = {v[0], v[1], v[2], v[3]};
+      store4(reinterpret_cast<float*>(a.saved) + m * 2 * a.N + f * a.N, n, a.N, x);
+    } else {
+      bf16_t* const hi = reinterpret_cast<bf16_t*>(a.saved) + m * 2 * a.N + f * a.N;
+      char* const lo = low_of(a.saved, a.M, a.N) + m * 2 * a.N + f * a.N;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (n + e < a.N) {
+          hi[n + e] = (bf16_t)(__float_as_uint(v[e]) >> 16);
+          lo[n + e] = (char)(__float_as_uint(v[e]) >> 8);
+        }
+    }
   }
 }
 
@@ -603,7 +657,7 @@ __global__ void __launch_bounds__(kBigThreads) k_product_big(const ProductArgs a
     // the next step's pieces are in LDS and this one's operands in registers, in every wave
     asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");
     if (stores == 0) vm_wait<0>();
-    else if (stores == 24) vm_wait<24>();
+    else if (stores == 40) vm_wait<40>();
     else if (stores == 16) vm_wait<16>();
     else if (stores == 8) vm_wait<8>();
     else vm_wait<32>();
@@ -632,7 +686,7 @@ __global__ void __launch_bounds__(kBigThreads) k_product_big(const ProductArgs a
     // A whole tile's stores, one an instruction, are the youngest of what is in flight at the
     // next wait; of others there may be fewer, and that wait is for all.
     const bool whole = now.m0 + kBig <= a.M && now.n0 + (GLU ? kBig / 2 : kBig) <= a.N;
-    stores = !whole ? 0 : GLU ? (a.pre ? 24 : 8) : a.splits > 1 ? 32 : 16;
+    stores = !whole ? 0 : GLU ? (a.saved ? 40 : 8) : a.splits > 1 ? 32 : 16;
     if (now.at + stride >= end) return;
     now = tile_at(now.at + stride);
     clear();
@@ -737,16 +791,38 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_glu_few(const ProductArgs a)
   }
 }
 
+// A piece of one factor of a row.
+template <typename DT>
+__device__ __forceinline__ void saved_piece(const void* saved, long rows, long F, long row, int f, int c, float* v) {
+  if constexpr (sizeof(DT) == 4) {
+    unpack<float>(load_piece<float>(reinterpret_cast<const float*>(saved) + row * 2 * F + f * F, c, F), v);
+  } else {
+    const v4u hi = load_piece<bf16_t>(reinterpret_cast<const bf16_t*>(saved) + row * 2 * F + f * F, c, F);
+    const char* const lo = low_of(const_cast<void*>(saved), rows, F) + row * 2 * F + f * F;
+    v2u l;
+    if (c + 8 <= F) {
+      l = *reinterpret_cast<const v2u_1*>(lo + c);
+    } else {
+      uint8_t b[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) b[e] = (uint8_t)lo[min(c + e, (int)F - 1)];
+      l = v2u{b[0] | b[1] << 8 | b[2] << 16 | (uint32_t)b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | (uint32_t)b[7] << 24};
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t h = e & 1 ? hi[e / 2] & 0xffff0000u : hi[e / 2] << 16;
+      v[e] = __uint_as_float(h | ((l[e / 4] >> (8 * (e & 3))) & 255u) << 8);
+    }
+  }
+}
 // One piece of a row.
 template <typename DT>
 __device__ __forceinline__ void back_piece(const GluGradArgs& a, DT* dpre, long row, int c) {
   constexpr int V = El<DT>::VEC;
-  const DT* pre = reinterpret_cast<const DT*>(a.pre) + row * 2 * a.F;
   float g[V], u[V], d[V];
-  const v4u rg = load_piece<DT>(pre, c, a.F), ru = load_piece<DT>(pre + a.F, c, a.F),
-            rd = load_piece<DT>(reinterpret_cast<const DT*>(a.dh) + row * a.dh_ld, c, a.F);
-  unpack<DT>(rg, g);
-  unpack<DT>(ru, u);
+  const v4u rd = load_piece<DT>(reinterpret_cast<const DT*>(a.dh) + row * a.dh_ld, c, a.F);
+  saved_piece<DT>(a.saved, a.rows, a.F, row, 0, c, g);
+  saved_piece<DT>(a.saved, a.rows, a.F, row, 1, c, u);
   unpack<DT>(rd, d);
 #pragma unroll
   for (int e = 0; e < V; ++e) {
@@ -760,7 +836,7 @@ __device__ __forceinline__ void back_piece(const GluGradArgs& a, DT* dpre, long 
 }
 
 constexpr long kBackGroups = 4096;
-// dpre [rows, 2F] from pre and dh: 16 bytes of a row a lane.
+// dpre [rows, 2F] from the factors and dh: 16 bytes of a row a lane.
 template <typename DT>
 __global__ void __launch_bounds__(kThreads) k_glu_back(const GluGradArgs a, DT* dpre) {
   constexpr int V = El<DT>::VEC;
@@ -847,8 +923,12 @@ size_t part_bytes(int dtype, long M, long N, long K) {
 }  // namespace
 
 hipError_t launch_glu(int dtype, const GluArgs& a, hipStream_t s) {
-  const ProductArgs p{{a.W, a.D}, {a.x, a.x_ld}, a.rows, a.F, a.D, a.h, a.h_ld, a.pre, a.act, nullptr, 1, 0, 0, 0};
+  const ProductArgs p{{a.W, a.D}, {a.x, a.x_ld}, a.rows, a.F, a.D, a.h, a.h_ld, a.saved, a.act, nullptr, 1, 0, 0, 0};
   return dtype == WM_FP32 ? product<float, false, false, true>("glu", p, s) : product<bf16_t, false, false, true>("glu", p, s);
+}
+
+size_t glu_saved(int dtype, long rows, int F) {
+  return dtype == WM_FP32 ? (size_t)rows * 2 * F * 4 : low_plane(rows, F) + (size_t)rows * 2 * F;
 }
 
 size_t glu_grad_workspace(int dtype, long rows, int D, int F) {

@@ -67,7 +67,9 @@ static void sizes() {
           const size_t b = wm_glu_grad_workspace_bytes(dt, n, D, G);
           const bool ok = (dt == 0 || dt == 1) && n >= 0 && n <= INT32_MAX && D > 0 && D <= 65536 && G > 0 && G <= 65536 &&
                           n <= ((int64_t)1 << 43) / G;
+          const size_t v = wm_glu_saved_bytes(dt, n, D, G);
           EXPECT(ok ? b >= (size_t)n * 2 * G * (dt == 0 ? 4 : 2) : b == 0);
+          EXPECT(ok ? v >= (size_t)n * 2 * G * (dt == 0 ? 4 : 3) : v == 0);
         }
 }
 
@@ -223,15 +225,18 @@ static void glu() {
     int dt = WM_FP32;
     int64_t rows = 4;
     int D = 8, G = 6, act = WM_ACT_SILU;
-    const void *x = P, *W = P, *pre = P;
+    const void *x = P, *W = P;
     int64_t xl = 8, hl = 6;
     void* h = P;
-    void* ws = P;
-    size_t less = 0;
-    wm_status fwd() const { return wm_glu(dt, rows, D, G, act, x, xl, W, h, hl, nullptr, nullptr); }
+    void *ws = P, *saved = P;
+    size_t less = 0, sless = 0;
+    wm_status fwd() const {
+      return wm_glu(dt, rows, D, G, act, x, xl, W, h, hl, saved, wm_glu_saved_bytes(dt, rows, D, G) - sless, nullptr);
+    }
     wm_status grad() const {
       const size_t b = wm_glu_grad_workspace_bytes(dt, rows, D, G);
-      return wm_glu_grad(dt, rows, D, G, act, x, xl, W, pre, h, hl, P, 8, P, ws, b - less, nullptr);
+      return wm_glu_grad(dt, rows, D, G, act, x, xl, W, saved, wm_glu_saved_bytes(dt, rows, D, G) - sless, h, hl, P, 8, P, ws,
+                         b - less, nullptr);
     }
   };
   auto bad = [](auto set, wm_status want) {
@@ -256,9 +261,13 @@ static void glu() {
   bad([](A& a) { a.x = fake<void>(4098); }, WM_ERR_INVALID_ARG);
   bad([](A& a) { a.dt = WM_BF16, a.W = fake<void>(4097); }, WM_ERR_INVALID_ARG);
   A a;
-  a.pre = nullptr;
-  EXPECT(a.grad() == WM_ERR_INVALID_ARG);
-  a.pre = P, a.less = 1;
+  a.saved = nullptr;
+  EXPECT(a.grad() == WM_ERR_WORKSPACE);
+  a.saved = P, a.sless = 1;
+  EXPECT(a.fwd() == WM_ERR_WORKSPACE && a.grad() == WM_ERR_WORKSPACE);
+  a.sless = 0, a.saved = fake<void>(4100);
+  EXPECT(a.fwd() == WM_ERR_INVALID_ARG && a.grad() == WM_ERR_INVALID_ARG);
+  a.saved = P, a.less = 1;
   EXPECT(a.grad() == WM_ERR_WORKSPACE);
   a.less = 0, a.ws = fake<void>(4100);
   EXPECT(a.grad() == WM_ERR_INVALID_ARG);

@@ -50,10 +50,13 @@ def test_projection_and_gradient(rows, D, F, dtype, act):
     x, W, dh = _make(rows, D, F, dtype)
     X, Wd, dH = dev(x, dtype), dev(W, dtype), dev(dh, dtype)
     bufs, checks = wm.GluBuffers(rows, D, F, TORCH[dtype]), []
-    for n in ("h", "pre", "dx", "dW"):
+    for n in ("h", "dx", "dW"):
         t, c = guarded(tuple(getattr(bufs, n).shape), TORCH[dtype])
         setattr(bufs, n, t)
         checks.append((n, c))
+    # what is saved, between bytes that stay
+    whole = torch.full((bufs.saved_bytes + 512,), 77, dtype=torch.uint8, device="cuda")
+    bufs.saved = whole[256:256 + bufs.saved_bytes]
     first = None
     for _ in range(2):
         bufs.workspace.fill_(255)
@@ -61,6 +64,7 @@ def test_projection_and_gradient(rows, D, F, dtype, act):
         wm.glu_grad(X, Wd, dH, act, bufs=bufs)
         for n, c in checks:
             c(n)
+        assert bool((whole[:256] == 77).all()) and bool((whole[256 + bufs.saved_bytes:] == 77).all())
         _check(bufs, x, W, dh, act, dtype)
         got = [getattr(bufs, n).clone() for n in ("h", "dx", "dW")]
         assert first is None or all(torch.equal(a, b) for a, b in zip(first, got))
@@ -213,3 +217,9 @@ def test_refusals():
     with pytest.raises(wm.WmError) as e:
         wm.glu_grad(x, W, dh, bufs=bufs)
     assert e.value.status == wm.WM_ERR_WORKSPACE
+    bufs = wm.GluBuffers(4, 8, 6)
+    bufs.saved_bytes -= 1
+    for f in (lambda: wm.glu(x, W, bufs=bufs), lambda: wm.glu_grad(x, W, dh, bufs=bufs)):
+        with pytest.raises(wm.WmError) as e:
+            f()
+        assert e.value.status == wm.WM_ERR_WORKSPACE

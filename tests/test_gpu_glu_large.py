@@ -55,7 +55,7 @@ def test_projection_and_gradient(rows, D, F, dtype, act, wide):
     r = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
     x, W, dh = r(rows, D + wide).to(dt)[:, :D], (r(2 * F, D) / math.sqrt(D)).to(dt), r(rows, F).to(dt)
     bufs, checks = wm.GluBuffers(rows, D, F, dt), []
-    for n in ("h", "pre", "dx", "dW"):
+    for n in ("h", "dx", "dW"):
         t, c = guarded(tuple(getattr(bufs, n).shape), dt)
         setattr(bufs, n, t)
         checks.append((n, c))
@@ -66,7 +66,7 @@ def test_projection_and_gradient(rows, D, F, dtype, act, wide):
         wm.glu_grad(x, W, dh, act, bufs=bufs)
         for n, c in checks:
             c(n)
-        got = [getattr(bufs, n).clone() for n in ("h", "pre", "dx", "dW")]
+        got = [getattr(bufs, n).clone() for n in ("h", "dx", "dW")]
         assert first is None or all(torch.equal(a, b) for a, b in zip(first, got))
         first = got
     X, Wd, dH = x.double(), W.double(), dh.double()
@@ -75,8 +75,8 @@ def test_projection_and_gradient(rows, D, F, dtype, act, wide):
     a, da = _act(act, g)
     err = (1.13 * mag[:, :F] + 16 * U32 * g.abs()) * u.abs() + a.abs() * mag[:, F:] + U32 * (a * u).abs()
     _close(bufs.h, a * u, err, half, "h")
-    _close(bufs.pre, pre, mag, half, "pre")
-    eg, eu = mag[:, :F] + half * g.abs(), mag[:, F:] + half * u.abs()
+    cut = 2.0 ** -15 if dtype == "bf16" else 0.0  # of what is saved
+    eg, eu = mag[:, :F] + cut * g.abs(), mag[:, F:] + cut * u.abs()
     dg, du = dH * u * da, dH * a
     edg = dH.abs() * (u.abs() * (eg + 16 * U32) + da.abs() * eu) + (half + 2 * U32) * dg.abs()
     edu = dH.abs() * (1.13 * eg + 16 * U32 * g.abs()) + (half + 2 * U32) * du.abs()
