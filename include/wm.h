@@ -560,8 +560,8 @@ wm_status wm_qk_norm_grad(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, i
  * state stays, and nothing of it enters any result.
  *   q, k [T, B, N, K], v [T, B, N, V] in dtype: the heads of a row one after the
  *   other, element strides q_t and q_b (...) of steps and rows.
- *   decay [N] float32, in [0, 1] (values outside act as clamped); constants of the
- *   model, without a gradient.
+ *   decay [N] float32, in [0, 1] (values outside act as clamped, NaN as 0);
+ *   constants of the model, without a gradient.
  *   h0 [B, N, K, V] float32, nullable (0); resets [T, B] uint8, nullable (none);
  *   lengths [B] int32, nullable (T; values outside [0, T] act as clamped).
  *   y [T, B, N, V] in dtype; h_T [B, N, K, V] float32, nullable, may be h0: the
@@ -575,8 +575,8 @@ wm_status wm_qk_norm_grad(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, i
  * products: a value of a head that is not finite can make every output of that
  * sequence and head in the same 64 steps not finite, earlier steps and other
  * trajectories included, and through the state those after it up to a reset.
- * K and V in 1 .. 128; scale finite; T B, B N, T B N K and T B N V at most 2^31 - 1
- * and B N K V at most 2^31 - 1.  B = 0 is a no-op; T = 0 gives h_T = h0.
+ * K and V in 1 .. 128; scale finite; T B, T B N K, T B N V and B N K V at most
+ * 2^31 - 1, B N at most 2^22.  B = 0 is a no-op; T = 0 gives h_T = h0.
  */
 size_t wm_linattn_states_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V);
 size_t wm_linattn_workspace_bytes(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V);
@@ -619,8 +619,8 @@ wm_status wm_linattn_grad(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_
  *                        normal distribution function.
  *   saved                nullable: a 256-byte aligned buffer of wm_glu_saved_bytes
  *                        that receives what wm_glu_grad needs.
- * D and F in 1 .. 65536; rows at most 2^31 - 1 and rows F at most 2^43.  rows = 0 is
- * a no-op.
+ * D and F in 1 .. 65536; rows at most 2^30, rows D and rows F at most 2^35.  rows = 0
+ * is a no-op.
  */
 enum { WM_ACT_SILU = 0, WM_ACT_GELU = 1 };
 size_t wm_glu_saved_bytes(int32_t dtype, int64_t rows, int32_t D, int32_t F);

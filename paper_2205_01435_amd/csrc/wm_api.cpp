@@ -245,6 +245,7 @@ wm_status check_linattn(int32_t T, int32_t B, int32_t N, int32_t K, int32_t V) {
     return fail(WM_ERR_INVALID_ARG, "T=%d and B=%d must not be negative, N=%d, K=%d and V=%d must be positive", T, B, N, K, V);
   if (K > wm::kAttnMax || V > wm::kAttnMax) return fail(WM_ERR_UNSUPPORTED, "K=%d, V=%d: at most %d", K, V, wm::kAttnMax);
   const int64_t lim = INT32_MAX, heads = (int64_t)B * N, wide = std::max(K, V);
+  if (heads > 1 << 22) return fail(WM_ERR_UNSUPPORTED, "B=%d, N=%d: at most 2^22 sequences and heads", B, N);
   if ((int64_t)T * B > lim || heads > lim / (K * V) || (T > 0 && heads > lim / wide / T))
     return fail(WM_ERR_UNSUPPORTED, "T=%d, B=%d, N=%d, K=%d, V=%d: too many values", T, B, N, K, V);
   return WM_OK;
@@ -271,7 +272,7 @@ wm_status check_glu(int64_t rows, int32_t D, int32_t F, int32_t act) {
   if (rows < 0 || D <= 0 || F <= 0)
     return fail(WM_ERR_INVALID_ARG, "rows=%lld must not be negative, D=%d and F=%d must be positive", (long long)rows, D, F);
   if (act != WM_ACT_SILU && act != WM_ACT_GELU) return fail(WM_ERR_INVALID_ARG, "unknown act %d", act);
-  if (D > 65536 || F > 65536 || rows > INT32_MAX || rows > ((int64_t)1 << 43) / F)
+  if (D > 65536 || F > 65536 || rows > 1 << 30 || rows > ((int64_t)1 << 35) / std::max(D, F))
     return fail(WM_ERR_UNSUPPORTED, "rows=%lld, D=%d, F=%d: too large", (long long)rows, D, F);
   return WM_OK;
 }

@@ -33,6 +33,7 @@ namespace wm {
 namespace {
 
 constexpr int kChunk = 64;
+__host__ __device__ constexpr int chunks_of(int T) { return T / kChunk + (T % kChunk != 0); }
 constexpr int kThreads = 256;  // four waves, 16 of a chunk's rows each
 
 struct MixArgs {
@@ -199,7 +200,7 @@ struct Place {
     b = (int)(bn / a.N);
     len = a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T;
     la = fmaxf(log2f(fminf(fmaxf(a.decay[n], 0.0f), 1.0f)), kLogZero);
-    const int chunks = (a.T + kChunk - 1) / kChunk;
+    const int chunks = chunks_of(a.T);
     first = seg * a.per;
     last = min(first + a.per, chunks);
   }
@@ -869,7 +870,7 @@ struct Split {
   int nseg, per;
 };
 Split split_of(int T, int B, int N) {
-  const int chunks = (T + kChunk - 1) / kChunk;
+  const int chunks = chunks_of(T);
   const long heads = (long)B * N;
   if (heads == 0 || chunks < 4) return {1, std::max(chunks, 1)};
   const int want = (int)std::max(1L, std::min<long>(chunks / 2, kResident / heads));

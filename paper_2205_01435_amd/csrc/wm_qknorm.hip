@@ -28,6 +28,7 @@ namespace wm {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr long kGroups = 1 << 20;  // work-groups at most, far more than run at a time
 
 template <typename DT> struct Io;
 template <> struct Io<float> {
@@ -204,37 +205,38 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
   constexpr int V = Io<DT>::VEC, kSlots = kThreads / L;
   const Lane<DT, WHOLE> lane(a, threadIdx.x % L);
   const int heads = a.side[0].heads + a.side[1].heads, parts = a.parts;
-  const uint32_t item = blockIdx.x * kSlots + threadIdx.x / L;  // (rows x heads fit 31 bits)
-  const long row = item / (uint32_t)parts;
-  if (row >= a.rows) return;
-  const int h0 = (int)(item % (uint32_t)parts);
-  auto in = [&](int h) {
-    const int w = h >= a.side[0].heads;
-    return reinterpret_cast<const DT*>(a.side[w].x) + row * a.side[w].x_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D;
-  };
-  v4u next[2];
-  lane.load(next, in(h0));
-  float c[V], s[V], g[2][V];
-  lane.angles(c, s, a, a.pos[row]);
+  const uint32_t items = (uint32_t)a.rows * (uint32_t)parts;  // (31 bits)
   const float inv = 1.0f / (float)a.D;
-  int held = -1;
-  for (int h = h0; h < heads; h += parts) {
-    const int w = h >= a.side[0].heads;
-    if (w != held) lane.columns(g, a.side[held = w].gamma);
-    float v[2][V];
-    lane.get(next, v);
-    if (h + parts < heads) lane.load(next, in(h + parts));
-    float m = 0.0f;
+  for (uint32_t item = blockIdx.x * kSlots + threadIdx.x / L; item < items; item += gridDim.x * kSlots) {
+    const long row = item / (uint32_t)parts;
+    const int h0 = (int)(item % (uint32_t)parts);
+    auto in = [&](int h) {
+      const int w = h >= a.side[0].heads;
+      return reinterpret_cast<const DT*>(a.side[w].x) + row * a.side[w].x_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D;
+    };
+    v4u next[2];
+    lane.load(next, in(h0));
+    float c[V], s[V], g[2][V];
+    lane.angles(c, s, a, a.pos[row]);
+    int held = -1;
+    for (int h = h0; h < heads; h += parts) {
+      const int w = h >= a.side[0].heads;
+      if (w != held) lane.columns(g, a.side[held = w].gamma);
+      float v[2][V];
+      lane.get(next, v);
+      if (h + parts < heads) lane.load(next, in(h + parts));
+      float m = 0.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) m = fmaf(v[0][i], v[0][i], fmaf(v[1][i], v[1][i], m));
-    const float r = 1.0f / sqrtf(group_sum<L>(m) * inv + a.eps);
+      for (int i = 0; i < V; ++i) m = fmaf(v[0][i], v[0][i], fmaf(v[1][i], v[1][i], m));
+      const float r = 1.0f / sqrtf(group_sum<L>(m) * inv + a.eps);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float x0 = v[0][i] * r * g[0][i], x1 = v[1][i] * r * g[1][i];
-      v[0][i] = fmaf(x0, c[i], -(x1 * s[i]));
-      v[1][i] = fmaf(x0, s[i], x1 * c[i]);
+      for (int i = 0; i < V; ++i) {
+        const float x0 = v[0][i] * r * g[0][i], x1 = v[1][i] * r * g[1][i];
+        v[0][i] = fmaf(x0, c[i], -(x1 * s[i]));
+        v[1][i] = fmaf(x0, s[i], x1 * c[i]);
+      }
+      lane.store(reinterpret_cast<DT*>(a.side[w].out) + row * a.side[w].out_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D, v);
     }
-    lane.store(reinterpret_cast<DT*>(a.side[w].out) + row * a.side[w].out_ld + (long)(h - (w ? a.side[0].heads : 0)) * a.D, v);
   }
 }
 
@@ -404,7 +406,7 @@ hipError_t launch_qk_norm(int dtype, const QkArgs& args, hipStream_t s) {
     typedef decltype(dt) DT;
     return by_lanes<DT>(a, [&](auto l, auto w) {
       const long items = a.rows * a.parts, slots = kThreads / l;
-      return launch("qk_norm", k_qk_norm<DT, l, w>, dim3((unsigned)((items + slots - 1) / slots)), dim3(kThreads), 0, s, a);
+      return launch("qk_norm", k_qk_norm<DT, l, w>, dim3((unsigned)std::min<long>((items + slots - 1) / slots, kGroups)), dim3(kThreads), 0, s, a);
     });
   };
   return dtype == WM_FP32 ? run(0.0f) : run(bf16_t());
