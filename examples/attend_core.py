@@ -71,6 +71,9 @@ class AttendCore:
         self.mix = wm.LinattnBuffers(T, B, N, D, D, device=device)
         self.ff = wm.GluBuffers(R, H, F, device=device)
         g = self.grads
+        # the gradients of q, k and v as the parts of their projection's
+        self.dqkv = torch.empty(T, B, 3, N, D, device=device)
+        self.qk.dq, self.qk.dk, self.mix.dv = (self.dqkv[:, :, i] for i in range(3))
         self.e_bufs.grad, self.qk.dgamma_q, self.qk.dgamma_k, self.ff.dW = g["E"], g["g_q"], g["g_k"], g["W_gu"]
         for b, n in ((self.n1, "n1"), (self.n2, "n2"), (self.n3, "n3"), (self.nh, "nh")):
             b.dgamma, b.dbeta = g[n + "_g"], g[n + "_b"]
@@ -118,7 +121,7 @@ class AttendCore:
         wm.linattn_grad(q, k, qkv[:, :, 2], self.decay, self.nh.dx.view(T, B, N, D), self.attn_scale, resets=resets,
                         lengths=lengths, bufs=self.mix)
         wm.qk_norm_grad(qkv[:, :, 0], qkv[:, :, 1], self.mix.dq, self.mix.dk, pos, self.rotary, w["g_q"], w["g_k"], bufs=self.qk)
-        dqkv = torch.cat([x.view(T * B, H) for x in (self.qk.dq, self.qk.dk, self.mix.dv)], 1)
+        dqkv = self.dqkv.view(T * B, 3 * H)
         torch.mm(dqkv.t(), self.n1.y, out=gr["W_qkv"])
         wm.layer_norm_grad(e, dqkv @ w["W_qkv"], w["n1_g"], bufs=self.n1)
         de = df + self.n1.dx

@@ -921,15 +921,26 @@ def _qk_args(q, k, positions, rotary, gamma_q, gamma_k, bufs, grad):
     return (dt, rows, Hq, Hk, D, R, nb, q.data_ptr(), ldq, pk, ldk, pgq, pgk), (pp, pt), bufs
 
 
+def _head_out(name, t, rows, H, D, like):
+    """Checks an output of ``rows`` x H heads, which may lie inside wider rows; the
+    distance between its rows."""
+    n, ld = _heads(name, t, H, D, like.dtype, like.device)
+    if n != rows:
+        raise ValueError(f"{name} has {n} rows, the call {rows}")
+    return ld
+
+
 def qk_norm(q, k, positions, rotary: Rotary | None, gamma_q=None, gamma_k=None, eps: float = 1e-6,
             bufs: QkNormBuffers | None = None) -> QkNormBuffers:
     """Launch wm_qk_norm on the current stream: every head of ``q`` [..., Hq, D]
     and ``k`` [..., Hk, D] (None: queries alone) divided by its root mean
     square, times gamma_q and gamma_k ([D] float32 or None), and rotated by its
-    row's int32 position.  Returns the filled buffers (q, k)."""
+    row's int32 position.  Returns the filled buffers (q, k; the buffers' own may be
+    set to q and k themselves: in place)."""
     head, (pp, pt), bufs = _qk_args(q, k, positions, rotary, gamma_q, gamma_k, bufs, False)
-    _check(load().wm_qk_norm(*head, eps, pp, pt, bufs.q.data_ptr(), bufs.Hq * bufs.D, bufs.k.data_ptr(),
-                             bufs.Hk * bufs.D, _stream()))
+    lq = _head_out("bufs.q", bufs.q, bufs.rows, bufs.Hq, bufs.D, q)
+    lk = _head_out("bufs.k", bufs.k, bufs.rows, bufs.Hk, bufs.D, q) if bufs.Hk else 0
+    _check(load().wm_qk_norm(*head, eps, pp, pt, bufs.q.data_ptr(), lq, bufs.k.data_ptr(), lk, _stream()))
     return bufs
 
 
@@ -944,8 +955,10 @@ def qk_norm_grad(q, k, dq_out, dk_out, positions, rotary: Rotary | None, gamma_q
     m, ldk = (n, 0) if k is None else _heads("dk_out", dk_out, bufs.Hk, bufs.D, q.dtype, q.device)
     if n != bufs.rows or m != bufs.rows:
         raise ValueError(f"dq_out has {n} rows, dk_out {m}, q has {bufs.rows}")
+    lq = _head_out("bufs.dq", bufs.dq, bufs.rows, bufs.Hq, bufs.D, q)
+    lk = _head_out("bufs.dk", bufs.dk, bufs.rows, bufs.Hk, bufs.D, q) if bufs.Hk else 0
     _check(load().wm_qk_norm_grad(*head, eps, pp, pt, dq_out.data_ptr(), ldq, None if k is None else dk_out.data_ptr(), ldk,
-                                  bufs.dq.data_ptr(), bufs.Hq * bufs.D, bufs.dk.data_ptr(), bufs.Hk * bufs.D,
+                                  bufs.dq.data_ptr(), lq, bufs.dk.data_ptr(), lk,
                                   bufs.dgamma_q.data_ptr(), bufs.dgamma_k.data_ptr(), bufs.workspace.data_ptr(),
                                   bufs.ws_bytes, _stream()))
     return bufs
@@ -1013,6 +1026,8 @@ def linattn(q, k, v, decay, scale: float = 1.0, h0=None, resets=None, lengths=No
     a new trajectory; lengths [B] int32).  Returns the filled buffers (y, h_T, and
     the states that linattn_grad reads)."""
     head, masks, bufs = _linattn_args(q, k, v, decay, h0, resets, lengths, bufs)
+    if not bufs.y.is_contiguous():
+        raise ValueError("bufs.y must be contiguous")
     _check(load().wm_linattn(*head, scale, *masks, bufs.y.data_ptr(), bufs.h_T.data_ptr(), _ptr(bufs.states),
                              bufs.states_bytes, bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
     return bufs
@@ -1029,9 +1044,12 @@ def linattn_grad(q, k, v, decay, dy, scale: float = 1.0, h0=None, dh_T=None, res
     T, B, N, K, V = bufs.T, bufs.B, bufs.N, bufs.K, bufs.V
     yt, yb = _steps("dy", dy, (T, B, N, V), q.dtype, q.device)
     ph = _arr("dh_T", dh_T, torch.float32, (B, N, K, V), q.device, optional=True)
+    out = []  # (they may lie inside wider rows: parts of a projection's gradient)
+    for name, t, w in (("bufs.dq", bufs.dq, K), ("bufs.dk", bufs.dk, K), ("bufs.dv", bufs.dv, V)):
+        out += (t.data_ptr(), *_steps(name, t, (T, B, N, w), q.dtype, q.device))
     _check(load().wm_linattn_grad(*head, scale, *masks, dy.data_ptr(), yt, yb, ph, bufs.states.data_ptr(),
-                                  bufs.states_bytes, bufs.dq.data_ptr(), B * N * K, N * K, bufs.dk.data_ptr(), B * N * K, N * K, bufs.dv.data_ptr(), B * N * V, N * V,
-                                  bufs.dh0.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
+                                  bufs.states_bytes, *out, bufs.dh0.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes,
+                                  _stream()))
     return bufs
 
 
@@ -1078,7 +1096,7 @@ def glu(x, W, act: str = "silu", bufs: GluBuffers | None = None) -> GluBuffers:
     head = _glu_args(x, W, act, bufs)
     if bufs is None:
         bufs = GluBuffers(head[1], head[2], head[3], x.dtype, x.device)
-    _check(load().wm_glu(*head, bufs.h.data_ptr(), bufs.F, _ptr(bufs.saved), bufs.saved_bytes, _stream()))
+    _check(load().wm_glu(*head, bufs.h.data_ptr(), _rows("bufs.h", bufs.h, bufs.F, x.dtype, x.device)[1], _ptr(bufs.saved), bufs.saved_bytes, _stream()))
     return bufs
 
 
@@ -1091,8 +1109,9 @@ def glu_grad(x, W, dh, act: str = "silu", bufs: GluBuffers | None = None) -> Glu
     n, ld = _rows("dh", dh, bufs.F, x.dtype, x.device)
     if n != bufs.rows:
         raise ValueError(f"dh has {n} rows, x has {bufs.rows}")
+    lx = _rows("bufs.dx", bufs.dx, bufs.D, x.dtype, x.device)[1]
     _check(load().wm_glu_grad(*head, bufs.saved.data_ptr(), bufs.saved_bytes, dh.data_ptr(), ld, bufs.dx.data_ptr(),
-                              bufs.D, bufs.dW.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
+                              lx, bufs.dW.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
     return bufs
 
 

@@ -50,7 +50,7 @@ struct MixArgs {
   const int32_t* lengths;
   int nseg, per;   // segments, and chunks in each
   float* seg;      // [B N][nseg][ka][kc]: what enters each segment (state launch: its own sum, with strides st_a, st_c)
-  float* hold;     // [B N][nseg] state launch: what a segment leaves of the state that enters it
+  float* hold;     // [B N][nseg] state launch: what a segment leaves of the state that enters it, -1 with a reset
 };
 
 template <typename DT> struct Tile;
@@ -582,7 +582,7 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
     if (!EARLY && more) load(next);
     if (more) load_rows(next);
     if (live <= 0) continue;
-    if constexpr (STATE) hold = starts ? 0.0f : hold * decayed(la, live);
+    if constexpr (STATE) hold = starts || hold < 0.0f ? -1.0f : hold * decayed(la, live);
     S.template take<REV>(bl, cl, wt, starts, live, lane, la, a.s_upd);
   }
   float* const s1 = STATE ? a.seg + at.part * a.ka * a.kc : a.seg || !a.s1 ? nullptr : a.s1 + at.bn * a.ka * a.kc;
@@ -753,7 +753,7 @@ __global__ void __launch_bounds__(kThreads) k_segments(float* seg, const float* 
     for (int j = 0; j < kAhead; ++j) {
       if (k + j >= nseg) break;
       p[(long)(REV ? nseg - 1 - k - j : k + j) * width] = s;
-      s = f[j] != 0.0f ? fmaf(f[j], s, own[j]) : own[j];
+      s = f[j] >= 0.0f ? fmaf(f[j], s, own[j]) : own[j];
     }
   }
   if (s1) s1[bn * width + i] = s;

@@ -88,6 +88,30 @@ def test_projection_and_gradient(rows, D, F, dtype, act, wide):
     assert torch.equal(alone.h, bufs.h)
 
 
+def test_more_than_2_31_values():
+    """The last rows of factors whose offsets pass 32 bits, against 64 bits."""
+    rows, D, F = 530000, 16, 2056
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(rows, D, generator=gen, device="cuda").bfloat16()
+    W = (torch.randn(2 * F, D, generator=gen, device="cuda") / 4).bfloat16()
+    dh = torch.zeros(rows, F, dtype=torch.bfloat16, device="cuda")
+    dh[-200:].normal_(generator=gen)
+    bufs = wm.glu(x, W)
+    wm.glu_grad(x, W, dh, bufs=bufs)
+    X, Wd, dH = x[-200:].double(), W.double(), dh[-200:].double()
+    pre, mag, half = X @ Wd.t(), (D + 1) * U32 * (X.abs() @ Wd.abs().t()), 2.0 ** -8
+    g, u = pre[:, :F], pre[:, F:]
+    a, da = _act("silu", g)
+    err = (1.13 * mag[:, :F] + 16 * U32 * g.abs()) * u.abs() + a.abs() * mag[:, F:] + U32 * (a * u).abs()
+    _close(bufs.h[-200:], a * u, err, half, "h")
+    d = torch.cat([dH * u * da, dH * a], 1)
+    e = (half + 2.0 ** -13) * (dH.abs().repeat(1, 2) * torch.cat([u.abs(), g.abs()], 1) * 1.13 + d.abs())
+    _close(bufs.dx[-200:], d @ Wd, e @ Wd.abs(), half, "dx")
+    # (every other row's gradient is 0)
+    assert not bool(bufs.dx[:-200].any())
+    _close(bufs.dW, d.t() @ X, e.t() @ X.abs() + 2.0 ** -14 * (d.abs().t() @ X.abs()), half, "dW")
+
+
 def test_every_kernel_runs():
     """The large tiles' launches and their kernels' names (a case above takes each)."""
     wm.profile_reset()

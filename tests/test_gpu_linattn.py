@@ -140,6 +140,25 @@ def test_parts_of_one_projection(T, dtype):
         assert torch.equal(getattr(got, n), getattr(want, n)) and torch.equal(getattr(third, n), getattr(want, n)), n
 
 
+@pytest.mark.parametrize("T", [1, 90, 400])
+def test_gradients_inside_wider_rows(T):
+    B, N, K = 2, 2, 32
+    x = _make(T, B, N, K, K, "fp32", True)
+    d = _device(x, "fp32")
+    want, got = (wm.LinattnBuffers(T, B, N, K, K) for _ in range(2))
+    _run(d, want, 0.2)
+    whole = torch.full((T, B, 4, N, K), 5.0, device="cuda")
+    got.dq, got.dk, got.dv = whole[:, :, 0], whole[:, :, 1], whole[:, :, 3]
+    _run(d, got, 0.2)
+    for n in ("dq", "dk", "dv"):
+        assert torch.equal(getattr(got, n), getattr(want, n)), n
+    assert bool((whole[:, :, 2] == 5.0).all())
+    got.y = torch.empty(T, B, 2 * N, K, device="cuda")[:, :, :N]
+    if T > 1:
+        with pytest.raises(ValueError):
+            _run(d, got, 0.2)
+
+
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf"), torch.finfo(torch.bfloat16).min])
 @pytest.mark.parametrize("T", [1, 100, 300])
 def test_padding_enters_nothing(T, bad):

@@ -162,6 +162,48 @@ def test_in_place_and_queries_alone():
     assert torch.equal(wm.qk_norm(q, k, pos, None).q, wm.qk_norm(q, k, torch.zeros_like(pos), rot).q)
 
 
+def test_outputs_inside_a_projection():
+    """In place on the parts of one projection, and gradients as such parts."""
+    rng = np.random.default_rng(8)
+    qkv = dev(rounded(rng, (6, 5, 7, 32), "fp32"), "fp32")
+    dy = dev(rounded(rng, (6, 5, 7, 32), "fp32"), "fp32")
+    pos, rot = dev(np.arange(30, dtype=np.int32).reshape(6, 5)), wm.Rotary(32)
+    want = wm.qk_norm_grad(qkv[:, :, :4], qkv[:, :, 4:6], dy[:, :, :4], dy[:, :, 4:6], pos, rot)
+    wm.qk_norm(qkv[:, :, :4], qkv[:, :, 4:6], pos, rot, bufs=want)
+    b, mine, grad = wm.QkNormBuffers(30, 4, 2, 32), qkv.clone(), torch.full_like(qkv, 3.0)
+    b.dq, b.dk = grad[:, :, :4], grad[:, :, 4:6]
+    wm.qk_norm_grad(qkv[:, :, :4], qkv[:, :, 4:6], dy[:, :, :4], dy[:, :, 4:6], pos, rot, bufs=b)
+    b.q, b.k = mine[:, :, :4], mine[:, :, 4:6]
+    wm.qk_norm(b.q, b.k, pos, rot, bufs=b)
+    assert torch.equal(b.q.reshape(30, 4, 32), want.q) and torch.equal(b.k.reshape(30, 2, 32), want.k)
+    assert torch.equal(mine[:, :, 6], qkv[:, :, 6]) and bool((grad[:, :, 6] == 3.0).all())
+    assert torch.equal(b.dq.reshape(30, 4, 32), want.dq) and torch.equal(b.dk.reshape(30, 2, 32), want.dk)
+    b.q = torch.empty(29, 4, 32, device="cuda")
+    with pytest.raises(ValueError):
+        wm.qk_norm(qkv[:, :, :4], qkv[:, :, 4:6], pos, rot, bufs=b)
+
+
+def test_more_than_2_31_values():
+    """The last rows of arrays whose offsets pass 32 bits are those of a small call."""
+    rows, H, D = 1700000, 21, 64
+    x = torch.empty(rows, H, D, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x[:5].normal_(generator=gen)
+    x[5:-300] = 1.0
+    x[-300:].normal_(generator=gen)
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda")
+    rot = wm.Rotary(D)
+    b = wm.QkNormBuffers(rows, 20, 1, D, torch.bfloat16, grad=True)
+    wm.qk_norm(x[:, :20], x[:, 20:], pos, rot, bufs=b)
+    wm.qk_norm_grad(x[:, :20], x[:, 20:], x[:, :20], x[:, 20:], pos, rot, bufs=b)
+    for part in (slice(0, 300), slice(rows - 300, rows)):
+        y = x[part].contiguous()
+        s = wm.qk_norm_grad(y[:, :20], y[:, 20:], y[:, :20], y[:, 20:], pos[part].contiguous(), rot)
+        wm.qk_norm(y[:, :20], y[:, 20:], pos[part].contiguous(), rot, bufs=s)
+        for n in ("q", "k", "dq", "dk"):
+            assert torch.equal(getattr(b, n)[part], getattr(s, n)), n
+
+
 def test_rows_that_can_go_wrong():
     D = 64
     x = np.zeros((5, 2, D), np.float32)
