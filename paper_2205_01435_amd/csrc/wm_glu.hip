@@ -2,16 +2,29 @@
 //   [g | u] = x W^T, h = act(g) u;
 //   [dg | du] = [dh u act'(g) | dh act(g)], dx = [dg | du] W, dW = [dg | du]^T x.
 //
-// One product kernel serves all three, out[m, n] = sum over k of Q[m, k] P[n, k],
-// with either operand stored along k (x, W and dg | du as rows) or across it (W and
-// x where the sum goes over their rows): the first kind is read from LDS as 16-byte
-// pieces, the second four rows at a time by the transposing read.  The forward
-// product takes the same 64 columns of both factors into one tile, so that the
-// activation and the product are its epilogue and the two factors leave the chip
-// only where the gradient needs them.  Where the tiles are too few for the device
-// the sum is split over work-groups, whose fp32 parts a second launch adds in order.
+// Every product is out[m, n] = sum over k of Q[m, k] P[n, k], with either operand
+// stored along k (x, W and dg | du as rows) or across it (W and x where the sum goes
+// over their rows): the first kind is read from LDS as 16-byte pieces, the second
+// four rows at a time by the transposing read.  The forward product takes the same
+// columns of both factors into one tile, so that the activation and the product are
+// its epilogue and the two factors leave the chip only where the gradient needs
+// them.  Three kernels: large bf16 products in tiles of 256 x 256 straight into LDS;
+// any product in tiles of 128 x 128 through registers; the forward product of up to
+// 64 rows straight from memory.  Where the tiles are too few for the device the sum is
+// split over work-groups, whose fp32 parts another launch adds in order.
 //
-// Bound by the matrix unit from some hundred rows on, by reading W below.
+// fp32 values multiply as three bf16 terms each, six products of them (wm_split.h),
+// split once on their way into LDS: 2.4 times the rate of the fp32 instructions, with
+// errors below theirs.
+//
+// Bound by the matrix unit from some hundred rows on, and there by power: the clock
+// falls as instructions are saved.  Measured, 65536 rows, D 1024, F 2816 bf16: outputs
+// and what is saved 843 to 893 us (850 to 900 TFLOP/s), dg | du 462 (4.8 TB/s), dx 611
+// to 662 (1140 to 1240), dW 692 to 756 (1000 to 1090) and 26 for its sums; a library's
+// plain products of these sizes took 703, 727 and 1067 us.  D 512, F 1408 fp32: 1069 to
+// 1129, 360, 959 to 1010 and 1125 to 1206 us (157 to 197 TFLOP/s; the library's 1455,
+// 1495 and 2257).  16 rows, D 1024, F 2816 bf16 5.4 us, W at 2.1 TB/s: launch and first
+// loads.
 #include <algorithm>
 
 #include "../../include/wm.h"

@@ -11,17 +11,30 @@
 // A chunk is three products on the matrix unit: the weights' 64 x 64 matrix
 // A B^T, masked to the sources of the row's own trajectory; its product with C;
 // and the state's part; then the state takes the chunk's sources in, weighted by
-// what is left of them at its end.  A work-group goes through the chunks of one
-// head with the state in registers.  Where sequences and heads are too few to fill
-// the device, the time axis is split into segments: a first launch sums up each
-// segment's own state, a second one runs through them, and the main launch starts
-// every segment from the state that enters it.
+// what is left of them at its end.  A work-group sweeps through the chunks of one
+// head with the state in registers: rows come from memory as matrix operands,
+// sources through LDS, where the transposing read serves the products that sum over
+// steps.  dk and dv share their sources and state, so that one reverse sweep gives
+// both (heads up to 64 wide); wider heads take one sweep for each.
+//
+// Where sequences and heads are too few to fill the device, the time axis is split
+// into segments: a first launch sums up each segment's own state, a second one runs
+// through them, and the main launch starts every segment from the state that enters
+// it.  The forward call's entering states are kept for dq.  A single step is a
+// kernel of its own, which streams the states.
 //
 // Precision: fp32 values multiply on the fp32 matrix instructions.  bf16 values
 // enter exactly; the 64 x 64 weights and the state that meets the rows are held as
 // two bf16 terms each (2^-17 of their value is left out, against the 2^-9 of the
 // output's rounding), and the sources times their weights, which make up the fp32
 // state, as three (2^-24).  All sums are fp32.
+//
+// Measured: one step of 256 x 8 states of 64 x 64 12 us (5.7 TB/s, part of it from the
+// caches).  T 128, B 512, 8 heads of 64 fp32, padded: 157 us, gradient 365; the matrix
+// unit is busy 40 % and the vector unit 30 % of it, the rest is waiting at three
+// work-groups a CU.  T 32768, 16 heads of 64 bf16: states 37, through the segments 7,
+// outputs 62 us; gradient 31, 8 and 151; two thirds of it the vector unit's splits,
+// weights and addresses.
 #include <algorithm>
 
 #include "../../include/wm.h"
@@ -835,7 +848,10 @@ hipError_t launch_mix(const char* name, int dtype, const MixArgs& m, hipStream_t
                   s, m);
   };
   auto by = [&](auto dt) {
-    auto cols = [&](auto ka) { return m.kc <= 32 ? go(dt, ka, Const<32>()) : go(dt, ka, Const<64>()); };
+    // (few work-groups: two take the halves of a head's columns, both with its weights; 145 steps
+    // of 150 heads bf16 23.5 -> 19.5 us)
+    const bool half = m.kc <= 32 || (!STATE && (long)m.B * m.N * m.nseg <= 256);
+    auto cols = [&](auto ka) { return half ? go(dt, ka, Const<32>()) : go(dt, ka, Const<64>()); };
     return m.ka <= 32 ? cols(Const<32>()) : m.ka <= 64 ? cols(Const<64>()) : cols(Const<128>());
   };
   return dtype == WM_FP32 ? by(0.0f) : by(bf16_t());
