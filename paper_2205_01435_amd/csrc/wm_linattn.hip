@@ -94,9 +94,14 @@ __device__ __forceinline__ float decayed(float la, int n) { return __builtin_amd
 
 // Rows of one sequence and head of a [T, B, N, width] array.  FAST: as wide as the
 // tile, on 16-byte boundaries and near enough for 32-bit offsets: range-checked
-// loads and stores, which give zeros and nothing past the rows that exist.
+// loads and stores, which give zeros and nothing past the rows that exist.  Others
+// load without a branch, the last piece of a row and the last row in the place of
+// what lies behind them, and put that right where the piece is used (settle): a branch
+// at each load would make each wait for the one before (T 128, B 512, 8 heads of 50
+// and 37 bf16: outputs 106 -> 81 us, gradient 284 -> 225; fp32 303 -> 214 and 700 -> 552).
 template <typename DT, int W, bool FAST>
 struct Rows {
+  static constexpr int V = Tile<DT>::VEC;
   DT* p;
   long t;     // elements between steps
   int width;  // of this tile
@@ -121,8 +126,19 @@ struct Rows {
       const uint4 v = bload16(k.r, ((uint32_t)s * (uint32_t)t + (uint32_t)c) * (uint32_t)sizeof(DT));
       return v4u{v.x, v.y, v.z, v.w};
     } else {
-      return s < k.count ? load_piece<DT>(k.p + (long)s * t, c, width) : v4u{0, 0, 0, 0};
+      if (width < V) return s < k.count ? load_piece<DT>(k.p + (long)s * t, c, width) : v4u{0, 0, 0, 0};
+      const DT* const row = k.p + (long)max(min(s, k.count - 1), 0) * t;
+      return *reinterpret_cast<const typename Mem16<DT>::type*>(row + min(c, width - V));
     }
+  }
+  // the piece that load(k, s, c) was to give, from what it gave
+  __device__ __forceinline__ v4u settle(v4u v, int count, int s, int c) const {
+    if constexpr (!FAST) {
+      if (width < V) return v;
+      if (s >= count || c >= width) return v4u{0, 0, 0, 0};
+      if (c + V > width) return elements_from<DT>(v, c + V - width);
+    }
+    return v;
   }
   // four values of row s from column c on
   __device__ __forceinline__ void store(const Chunk& k, int s, int c, const float (&v)[4]) const {
@@ -180,11 +196,12 @@ struct Panel {
       r[i] = rows.load(c, p / (W / V), p % (W / V) * V);
     }
   }
-  __device__ __forceinline__ void store(DT* lds) const {
+  template <bool FAST>
+  __device__ __forceinline__ void store(DT* lds, const Rows<DT, W, FAST>& rows, int count) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int p = threadIdx.x + i * kThreads;
-      *reinterpret_cast<v4u*>(lds + p / (W / V) * PITCH + p % (W / V) * V) = r[i];
+      *reinterpret_cast<v4u*>(lds + p / (W / V) * PITCH + p % (W / V) * V) = rows.settle(r[i], count, p / (W / V), p % (W / V) * V);
     }
   }
 };
@@ -197,6 +214,11 @@ struct RowFrag {
   __device__ __forceinline__ void load(const Rows<DT, W, FAST>& rows, const typename Rows<DT, W, FAST>::Chunk& c, int s, int g) {
 #pragma unroll
     for (int i = 0; i < N; ++i) r[i] = rows.load(c, s, i * SL + V * g);
+  }
+  template <bool FAST>
+  __device__ __forceinline__ void settle(const Rows<DT, W, FAST>& rows, int count, int s, int g) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = rows.settle(r[i], count, s, i * SL + V * g);
   }
   __device__ __forceinline__ uint4 operator[](int i) const { return make_uint4(r[i].x, r[i].y, r[i].z, r[i].w); }
 };
@@ -557,9 +579,12 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
     const int lane = anew(lane0), g = lane >> 4, j16 = lane & 15, r = 16 * w + j16;
     const float la = anew(at.la);
     __syncthreads();  // the chunk before is done with
-    pb.store(bl);
-    pc.store(cl);
-    if constexpr (!STATE) S.stage(st);
+    pb.store(bl, rb, live);
+    pc.store(cl, rc, live);
+    if constexpr (!STATE) {
+      rows.settle(ra, live, r, g);
+      S.stage(st);
+    }
     // the next chunk's pieces: requested here they are on their way during the whole
     // chunk, where there are registers for them
     constexpr bool EARLY = STATE || sizeof(DT) == 2;
@@ -605,9 +630,11 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
   }
 }
 
-// Waves a SIMD that the registers are to admit: as many as LDS does.
+// Waves a SIMD that the registers are to admit: as many as LDS does, fp32 rows that
+// are not FAST one less, and their few spills with it (bf16 gains by the third wave:
+// T 128, B 512, 8 heads of 50 and 37 with two 95 and 252 us, with three 81 and 225).
 constexpr int waves(int size, int ka, int kc, bool fast) {
-  if (ka > 64) return size == 4 ? (kc > 32 ? 1 : 2) : (kc > 32 ? 2 : 3);
+  if (ka > 64) return size == 4 ? (kc > 32 ? 1 : 2) : (kc > 32 ? 2 : 3 - !fast);
   return size == 4 ? 3 - !fast : 3;
 }
 
@@ -659,8 +686,10 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
     const int lane = anew(lane0), g = lane >> 4, j16 = lane & 15, r = 16 * w + j16;
     const float la = anew(at.la);
     __syncthreads();
-    pq.store(ql);
-    pd.store(dl);
+    pq.store(ql, rq, live);
+    pd.store(dl, rd, live);
+    k.settle(rk, live, r, g);
+    v.settle(rv, live, r, g);
     S.stage(st);
     constexpr bool EARLY = sizeof(DT) == 2;
     if (EARLY && c > at.first) load(c - 1);
@@ -848,9 +877,10 @@ hipError_t launch_mix(const char* name, int dtype, const MixArgs& m, hipStream_t
                   s, m);
   };
   auto by = [&](auto dt) {
-    // (few work-groups: two take the halves of a head's columns, both with its weights; 145 steps
-    // of 150 heads bf16 23.5 -> 19.5 us)
-    const bool half = m.kc <= 32 || (!STATE && (long)m.B * m.N * m.nseg <= 256);
+    // few work-groups: two take the halves of a head's columns, both with its weights (T 128 bf16
+    // in halves and whole, 64 heads 7.8 and 9.9 us, 256 heads 11.5 and 11.0, 384 heads 15.3 and
+    // 13.9; fp32 13.3 and 18.2, 20.7 and 20.2, 26.6 and 28.8)
+    const bool half = m.kc <= 32 || (!STATE && (long)m.B * m.N * m.nseg < 256);
     auto cols = [&](auto ka) { return half ? go(dt, ka, Const<32>()) : go(dt, ka, Const<64>()); };
     return m.ka <= 32 ? cols(Const<32>()) : m.ka <= 64 ? cols(Const<64>()) : cols(Const<128>());
   };
@@ -858,8 +888,10 @@ hipError_t launch_mix(const char* name, int dtype, const MixArgs& m, hipStream_t
 }
 
 // Sequences, heads and segments up to which the gradient's two sweeps run beside each
-// other.
-constexpr long kApart = 512;
+// other.  Measured beside and after each other, T 128, heads of 64 bf16: 64 of them 13.9
+// and 20.0 us, 384 24.2 and 26.6, 512 31.5 and 27.2; fp32 27.8 and 41.3, 54.3 and 62.0,
+// 73.5 and 64.5.
+constexpr long kApart = 384;
 hipError_t launch_mix_grad(int dtype, const MixArgs& q, const MixArgs& v, const SeqView& dk, hipStream_t s) {
   const int K = v.ka, V = v.kc;
   const bool fast = fast_view(dtype, v.a, K) && fast_view(dtype, v.b, K) && fast_view(dtype, v.c, V) && fast_view(dtype, v.v, V) &&

@@ -79,7 +79,9 @@ CASES = [  # T, B, N, K, V, dtype, masks
     (65, 5, 2, 64, 64, "bf16", True), (64, 2, 1, 1, 128, "fp32", True), (70, 3, 2, 128, 1, "bf16", True),
     (127, 4, 6, 40, 24, "fp32", True), (128, 6, 2, 64, 32, "bf16", False), (130, 3, 2, 31, 33, "fp32", True),
     (100, 2, 2, 128, 128, "fp32", True), (150, 2, 2, 128, 128, "bf16", True), (145, 4, 3, 50, 37, "bf16", True),
-    (96, 3, 2, 65, 66, "fp32", True), (96, 3, 2, 127, 95, "bf16", True),
+    (96, 3, 2, 65, 66, "fp32", True), (96, 3, 2, 127, 95, "bf16", True), (66, 2, 3, 5, 3, "bf16", True), (66, 2, 3, 2, 34, "fp32", True),
+    # heads around the numbers by which work-groups are formed
+    (130, 70, 4, 50, 37, "bf16", True), (129, 85, 3, 33, 64, "fp32", True), (66, 100, 4, 61, 40, "bf16", True), (70, 128, 3, 64, 64, "fp32", True),
     # split time axis
     (255, 2, 2, 32, 32, "fp32", True), (256, 2, 2, 32, 32, "bf16", True), (300, 3, 6, 24, 40, "fp32", True),
     (577, 2, 3, 64, 64, "bf16", True), (640, 1, 2, 64, 64, "fp32", False), (1000, 3, 1, 17, 70, "bf16", True),
@@ -107,6 +109,25 @@ def test_attention_and_gradient(T, B, N, K, V, dtype, masks):
     alone = wm.LinattnBuffers(T, B, N, K, V, TORCH[dtype], grad=False)
     _run(d, alone, scale, grad=False)
     assert torch.equal(alone.y, bufs.y) and torch.equal(alone.h_T, bufs.h_T)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_steps_far_apart(dtype):
+    """Inputs whose steps lie more than 2^31 / 65 bytes apart."""
+    T, B, N, K, V = 66, 2, 2, 64, 32
+    say("linattn far", dtype)
+    x = _make(T, B, N, K, V, dtype, True)
+    d, step = _device(x, dtype), 2 ** 24 + 2 ** 20
+    wide = torch.empty(T, step, dtype=TORCH[dtype], device="cuda")
+    at = 0
+    for n in ("q", "k", "v", "dy"):
+        w = B * N * d[n].shape[3]
+        part = wide[:, at:at + w].view(T, B, N, -1)
+        part.copy_(d[n])
+        d[n], at = part, at + w
+    bufs = wm.LinattnBuffers(T, B, N, K, V, TORCH[dtype])
+    _run(d, bufs, 0.25)
+    _check(bufs, x, 0.25, dtype)
 
 
 @pytest.mark.parametrize("T,B,N,K,V,dtype", [(1, 2, 2, 8, 8, "fp32"), (70, 2, 2, 20, 20, "bf16"), (400, 1, 2, 32, 48, "fp32")])
