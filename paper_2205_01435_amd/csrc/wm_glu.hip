@@ -746,23 +746,26 @@ __device__ __forceinline__ void store_piece(DT* row, long c, long width, const f
   }
 }
 
-// Up to 64 rows, where the time is that of reading W: a work-group takes sixteen
-// columns of both factors, its eight waves a share of k each, straight from memory
+// Up to 256 rows, where the tiles are few and the time is that of reading W: a work-group
+// takes sixteen columns of both factors for up to 64 rows, its eight waves a share of k each, straight from memory
 // into matrix operands, kFewAhead slices on their way at a time; the waves' sums are
-// added in LDS in order.
-constexpr int kFewRows = 64, kFewWaves = 8, kFewAhead = 4;
+// added in LDS in order.  Measured so and in tiles, D 1024, F 2816: bf16 16 rows 5.1 and
+// 19.2 us, 64 rows 8.2 and 21.1, 128 rows 15.5 and 21.8, 256 rows 22.8 and 22.4, 512 rows
+// 44 and 23; fp32 10 and 57, 20 and 59, 39 and 60, 57 and 61, 109 and 63; D 256, F 640 bf16,
+// 256 rows 4.3 and 8.7.
+constexpr int kFewRows = 256, kFewWaves = 8, kFewAhead = 4;
 template <typename DT, int MB>
 __global__ void __launch_bounds__(64 * kFewWaves) k_glu_few(const ProductArgs a) {
   constexpr int V = El<DT>::VEC, SL = 4 * V;
   __shared__ f32x4 sum[kFewWaves][2 * MB][64];
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
-  const long n0 = (long)blockIdx.x * 16;
+  const long n0 = (long)blockIdx.x * 16, m0 = (long)blockIdx.y * 64;
   const DT* const W = reinterpret_cast<const DT*>(a.P.p);
   const DT* const pg = W + min(n0 + j, a.N - 1) * a.P.ld;
   const DT* const pu = pg + a.N * a.P.ld;
   const DT* px[MB];
 #pragma unroll
-  for (int m = 0; m < MB; ++m) px[m] = reinterpret_cast<const DT*>(a.Q.p) + min(16L * m + j, a.M - 1) * a.Q.ld;
+  for (int m = 0; m < MB; ++m) px[m] = reinterpret_cast<const DT*>(a.Q.p) + min(m0 + 16 * m + j, a.M - 1) * a.Q.ld;
   f32x4 acc[2][MB];
 #pragma unroll
   for (int m = 0; m < MB; ++m) acc[0][m] = acc[1][m] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -800,7 +803,7 @@ __global__ void __launch_bounds__(64 * kFewWaves) k_glu_few(const ProductArgs a)
       gate += sum[k][2 * m][lane];
       up += sum[k][2 * m + 1][lane];
     }
-    if (16L * m + j < a.M) put_one<DT>(a, 16L * m + j, n0 + 4 * g, gate, up);
+    if (m0 + 16 * m + j < a.M) put_one<DT>(a, m0 + 16 * m + j, n0 + 4 * g, gate, up);
   }
 }
 
@@ -867,16 +870,38 @@ __global__ void __launch_bounds__(kThreads) k_glu_back(const GluGradArgs a, DT* 
     back_piece<DT>(a, dpre, row, c);
   }
 }
-// Splits of a sum of length K for M x N outputs in tiles of `tile`.
-int splits_of(long M, long N, long K, int tile, int bk) {
-  const long tiles = std::max(1L, (M + tile - 1) / tile) * ((N + tile - 1) / tile);
+// Splits of a sum of length K for M x N outputs in tiles of 128 x 128: up to 512 work-groups,
+// two a CU.  Gradient with up to 256, 512 and 1024 of them, fp32: 2048 rows, D 512, F 1408
+// 127, 104 and 115 us (276 without splits), 8192 rows 424, 338 and 329; 16384 rows, D 256,
+// F 640 195, 181 and 202.
+int splits_of(long M, long N, long K, int bk) {
+  const long tiles = std::max(1L, (M + kTile - 1) / kTile) * ((N + kTile - 1) / kTile);
   if (tiles >= 256) return 1;
   return (int)std::max<long>(1, std::min<long>(512 / tiles, K / (8 * bk)));
 }
-// The kernel of a product goes by its sizes: bf16 products with at least 64 tiles of
-// 256 x 256 take those.
-bool big(int dtype, long M, long N, long K) {
-  return dtype == WM_BF16 && K > 0 && K % 8 == 0 && (M + kBig - 1) / kBig * ((N + kBig - 1) / kBig) >= 64;
+// The same for tiles of 256 x 256, of which 256 are under way at a time: as many as take the
+// least time, in steps of the sum.  A tile's results are written in that of 6 steps,
+// and the parts of 20 tiles are read and added in that of one.  Gradient, D 1024, F 2816,
+// with 512 work-groups in all and so: 2048 rows 128 and 113 us, 4096 rows 196 and 172, 8192
+// rows 297 and 287.
+int splits_of_big(long M, long N, long K) {
+  const long tiles = std::max(1L, (M + kBig - 1) / kBig) * ((N + kBig - 1) / kBig), steps = (K + kBigK - 1) / kBigK;
+  if (tiles >= kBigGroups) return 1;
+  int best = 1;
+  long least = steps + 6;
+  for (int s = 2; s <= 16 && 8 * s <= steps; ++s) {
+    const long t = (tiles * s + kBigGroups - 1) / kBigGroups * ((steps + s - 1) / s + 6) + tiles * s / 20;
+    if (t < least) least = t, best = s;
+  }
+  return best;
+}
+// The kernel of a product goes by its sizes: bf16 products in at least 64 tiles of
+// 256 x 256 take those, the outputs' (no splits) in at least 160.  Measured in large tiles
+// and in small ones, D 1024, F 2816: outputs in 88 tiles 39 and 33 us, 132 tiles 38 and 32,
+// 176 tiles 39 and 49, 352 tiles 72 and 86; dW (88 tiles) over 1024 rows 33 and 32 us, 2048
+// rows 52 and 52, 4096 rows 77 and 97; dx and what goes before it in 64 tiles 94 and 134.
+bool big(int dtype, long M, long N, long K, bool glu) {
+  return dtype == WM_BF16 && K > 0 && K % 8 == 0 && (M + kBig - 1) / kBig * ((N + kBig - 1) / kBig) >= (glu ? 160 : 64);
 }
 // Whether an operand's rows lie on 16-byte boundaries, and near enough for 32-bit offsets.
 bool direct(const Operand& a) {
@@ -887,10 +912,10 @@ template <typename DT, bool PX, bool QX, bool GLU>
 hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
   constexpr int BK = El<DT>::BK;
   const int dtype = sizeof(DT) == 4 ? WM_FP32 : WM_BF16;
-  const bool wide = big(dtype, a.M, GLU ? 2 * a.N : a.N, a.K);
+  const bool wide = big(dtype, a.M, GLU ? 2 * a.N : a.N, a.K, GLU);
   if constexpr (GLU) {
     if (a.M <= kFewRows) {
-      const dim3 grid((unsigned)((a.N + 15) / 16)), block(64 * kFewWaves);
+      const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 63) / 64)), block(64 * kFewWaves);
       if (a.M <= 16) return launch(name, k_glu_few<DT, 1>, grid, block, 0, s, a);
       return launch(name, a.M <= 32 ? k_glu_few<DT, 2> : k_glu_few<DT, 4>, grid, block, 0, s, a);
     }
@@ -900,7 +925,7 @@ hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
       const int width = GLU ? kBig / 2 : kBig;
       a.tiles_n = (a.N + width - 1) / width;
       a.tiles_m = (a.M + kBig - 1) / kBig;
-      a.splits = GLU ? 1 : splits_of(a.M, a.N, a.K, kBig, kBigK);
+      a.splits = GLU ? 1 : splits_of_big(a.M, a.N, a.K);
       a.per = ((a.K + a.splits - 1) / a.splits + kBigK - 1) / kBigK * kBigK;
       a.splits = (int)((a.K + a.per - 1) / a.per);  // none empty
       const hipError_t e = launch(name, k_product_big<PX, QX, GLU>, dim3(kBigGroups), dim3(kBigThreads), 0, s, a);
@@ -911,7 +936,7 @@ hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
   const int width = GLU ? kTile / 2 : kTile;
   a.tiles_n = (a.N + width - 1) / width;
   a.tiles_m = (a.M + kTile - 1) / kTile;
-  a.splits = GLU ? 1 : splits_of(a.M, a.N, a.K, kTile, BK);
+  a.splits = GLU ? 1 : splits_of(a.M, a.N, a.K, BK);
   a.per = ((a.K + a.splits - 1) / a.splits + BK - 1) / BK * BK;
   const dim3 grid((unsigned)(a.tiles_m * a.tiles_n * a.splits));
   hipError_t e;
@@ -928,8 +953,8 @@ hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 // What either kernel of the product needs.
 size_t part_bytes(int dtype, long M, long N, long K) {
-  const int s = std::max(splits_of(M, N, K, kTile, dtype == WM_FP32 ? El<float>::BK : El<bf16_t>::BK),
-                         big(dtype, M, N, K) ? splits_of(M, N, K, kBig, kBigK) : 1);
+  const int s = std::max(splits_of(M, N, K, dtype == WM_FP32 ? El<float>::BK : El<bf16_t>::BK),
+                         big(dtype, M, N, K, false) ? splits_of_big(M, N, K) : 1);
   return s > 1 ? (size_t)s * M * N * sizeof(float) : 0;
 }
 

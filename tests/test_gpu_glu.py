@@ -27,6 +27,7 @@ CASES = [  # rows, D, F, dtype, act
     (65, 129, 66, "bf16", "silu"), (127, 63, 191, "fp32", "gelu"), (128, 64, 128, "bf16", "silu"), (129, 65, 129, "bf16", "silu"),
     (200, 512, 300, "fp32", "silu"), (300, 367, 979, "bf16", "gelu"), (1000, 40, 24, "fp32", "silu"), (1030, 72, 56, "bf16", "silu"),
     (257, 256, 512, "bf16", "gelu"), (500, 96, 1000, "fp32", "silu"), (2100, 17, 33, "bf16", "gelu"),
+    (193, 1000, 40, "bf16", "silu"), (255, 130, 100, "bf16", "gelu"), (256, 61, 130, "fp32", "silu"), (300, 1, 5, "fp32", "gelu"),
 ]
 
 

@@ -44,6 +44,7 @@ CASES = [  # rows, D, F, dtype, act, columns around the rows of x
     (16641, 264, 1000, "bf16", "gelu", 0), (257, 512, 8200, "bf16", "silu", 0), (9000, 8, 2048, "bf16", "silu", 0),
     (2000, 1024, 300, "bf16", "silu", 0), (4200, 1001, 2100, "bf16", "silu", 0), (4500, 520, 1100, "fp32", "gelu", 0),
     (3000, 260, 700, "fp32", "silu", 4), (8192, 256, 256, "bf16", "silu", 0),
+    (40000, 1024, 2816, "bf16", "silu", 0), (1100, 64, 4100, "bf16", "silu", 2 ** 20 + 8), (300, 36, 100, "fp32", "gelu", 2 ** 20 + 4),
 ]
 
 
