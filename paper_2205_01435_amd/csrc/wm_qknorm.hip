@@ -90,12 +90,15 @@ __device__ __forceinline__ float group_sum(float v) {
 // put together from them.  Halves: the lanes of the rotated pairs come first, a piece
 // from each half of the R values; then those of the rest, whose halves are taken as
 // pairs that do not turn (the second one may lack the last).  WHOLE: every piece of
-// every lane is full.
+// every lane is full.  Others are loaded from where 16 bytes of the head are left and
+// moved and cut when they are used: a branch at each load would make each wait for the
+// one before (4500 rows, 9 heads of 61 fp32 11.6 -> 10.4 us, gradient 13.7 -> 11.9).
 template <typename DT, bool WHOLE>
 struct Lane {
   static constexpr int V = Io<DT>::VEC;
   int at[2], n[2];   // where the pieces start, and their values
   int end[2];        // what a piece may be read up to
+  int from[2];       // and where its load starts, -1 where the head is shorter than one
   int turn0, turns;  // the first pair's place in the table, and how many pairs turn
   bool neighbours;
   __device__ Lane(const QkArgs& a, int lane) : neighbours(a.neighbours != 0) {
@@ -120,21 +123,34 @@ struct Lane {
       turn0 = turns = 0;
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) n[i] = min(max(end[i] - at[i], 0), V);
+    for (int i = 0; i < 2; ++i) {
+      n[i] = min(max(end[i] - at[i], 0), V);
+      from[i] = a.D < V ? -1 : min(at[i], a.D - V);
+    }
   }
   __device__ void load(v4u (&r)[2], const DT* x) const {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       if constexpr (WHOLE)
         r[i] = *reinterpret_cast<const typename Mem16<DT>::type*>(x + (n[0] ? at[i] : 0));
-      else
+      else if (from[i] < 0)
         r[i] = load_piece<DT>(x, at[i], end[i]);
+      else
+        r[i] = *reinterpret_cast<const typename Mem16<DT>::type*>(x + from[i]);
     }
   }
   // the pieces as pairs
   __device__ void get(const v4u (&r)[2], float (&v)[2][V]) const {
-    Io<DT>::get(r[0], v[0]);
-    Io<DT>::get(r[1], v[1]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (WHOLE || from[i] < 0 || n[i] == V) {
+        Io<DT>::get(r[i], v[i]);
+      } else {
+        Io<DT>::get(elements_from<DT>(r[i], at[i] - from[i]), v[i]);
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[i][k] = k < n[i] ? v[i][k] : 0.0f;
+      }
+    }
     if (neighbours) order<true>(v);
     if (WHOLE && n[0] == 0) {
 #pragma unroll
@@ -186,16 +202,22 @@ struct Lane {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         const int c = column(j, i);
-        g[j][i] = c < 0 ? 0.0f : a ? a[c] : 1.0f;
+        const float v = a ? a[max(c, 0)] : 1.0f;
+        g[j][i] = c < 0 ? 0.0f : v;
       }
   }
   __device__ void angles(float (&c)[V], float (&s)[V], const QkArgs& a, int32_t position) const {
     const uint64_t pos = (uint64_t)(int64_t)position;
+    if (a.R == 0) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) c[i] = 1.0f, s[i] = 0.0f;
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float2 t = i < turns ? cos_sin(pos * a.table[turn0 + i]) : make_float2(1.0f, 0.0f);
-      c[i] = t.x;
-      s[i] = t.y;
+      const float2 t = cos_sin(pos * a.table[min(turn0 + i, a.R / 2 - 1)]);
+      c[i] = i < turns ? t.x : 1.0f;
+      s[i] = i < turns ? t.y : 0.0f;
     }
   }
 };
@@ -368,19 +390,23 @@ bool whole(const QkArgs& a, int V) {
 }
 // Items of a step: lane groups beside each other read longer runs of a row, but each
 // computes the angles again, of twice as many pairs a lane in bf16; more where that
-// gives fewer than kItems.  Measured, 1 and 4: 65536 rows, 16 heads of 64 fp32, 115 and
+// gives fewer than kItems (8192, 16384 and 32768 of them: 1000 rows, 16 heads of 64 fp32
+// 5.2, 4.5 and 4.5 us, 4500 rows 10.2, 10.2 and 11.5, bf16 17.2, 10.5 and 10.1, gradient
+// 14.3, 13.8 and 19.3).  Measured, 1 and 4: 65536 rows, 16 heads of 64 fp32, 115 and
 // 100 us, gradient 160 and 154; 204800 rows, 20 heads of 64 bf16, 206 and 239, gradient
 // 379 and 463.
 constexpr long kItems = 16384;
 int parts_of(int dtype, long rows, int heads) {
   return (int)std::min<long>(heads, std::max<long>(dtype == WM_FP32 ? 4 : 1, kItems / std::max<long>(rows, 1)));
 }
-// Work-groups of the gradient for one side: its share of kMost by heads, or as many as
-// it has items for (one for a side without heads: it writes zeros).
-constexpr long kMost = 1024;
+// Work-groups of the gradient for one side: as many as it has items for (one for a side
+// without heads: it writes zeros), up to its share of 1024 by heads, or of kMost where a
+// lane group has four items or more.  Measured, 1024 and 2048: 204800 rows, 20 heads of
+// 64 bf16 337 and 313 us, fp32 615 and 605, 4500 rows, 9 heads of 61 fp32 19.0 and 20.9.
+constexpr long kMost = 2048;
 int grad_groups(long rows, int heads, int all, int L, int parts) {
-  const long items = rows * std::min(parts, std::max(heads, 1)), slots = kThreads / L;
-  return (int)std::max<long>(1, std::min<long>((items + slots - 1) / slots, kMost * heads / all));
+  const long items = rows * std::min(parts, std::max(heads, 1)), slots = kThreads / L, full = (items + slots - 1) / slots;
+  return (int)std::max<long>({1, std::min(full, kMost / 2 * heads / all), std::min(full / 4, kMost * heads / all)});
 }
 
 template <int N> using Const = std::integral_constant<int, N>;
