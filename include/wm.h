@@ -589,8 +589,9 @@ wm_status wm_linattn(int32_t dtype, int32_t T, int32_t B, int32_t N, int32_t K, 
 
 /*
  * Gradient of wm_linattn by the reverse recurrence, from its inputs and the states
- * that it saved.  With G the gradient of the state after step t from all later ones, G_{T-1} = grad_h_T, and
- * F_t = G_t + scale q_t grad_y_t^T for a step inside its sequence:
+ * that it saved.  With G the gradient of the state after step t from all later ones,
+ * G_{T-1} = grad_h_T, and F_t = G_t + scale q_t grad_y_t^T for a step inside its
+ * sequence:
  *   grad_q_t = scale S_t grad_y_t,  grad_k_t = F_t v_t,  grad_v_t = F_t^T k_t,
  *   G_{t-1} = a F_t, or 0 at a reset;  grad_h0 = G_{-1}.
  * Padded steps get 0 and pass G on.

@@ -955,11 +955,13 @@ def qk_norm_grad(q, k, dq_out, dk_out, positions, rotary: Rotary | None, gamma_q
     m, ldk = (n, 0) if k is None else _heads("dk_out", dk_out, bufs.Hk, bufs.D, q.dtype, q.device)
     if n != bufs.rows or m != bufs.rows:
         raise ValueError(f"dq_out has {n} rows, dk_out {m}, q has {bufs.rows}")
+    pgq = _arr("bufs.dgamma_q", bufs.dgamma_q, torch.float32, (bufs.D,), q.device)
+    pgk = _arr("bufs.dgamma_k", bufs.dgamma_k, torch.float32, (bufs.D,), q.device)
     lq = _head_out("bufs.dq", bufs.dq, bufs.rows, bufs.Hq, bufs.D, q)
     lk = _head_out("bufs.dk", bufs.dk, bufs.rows, bufs.Hk, bufs.D, q) if bufs.Hk else 0
     _check(load().wm_qk_norm_grad(*head, eps, pp, pt, dq_out.data_ptr(), ldq, None if k is None else dk_out.data_ptr(), ldk,
                                   bufs.dq.data_ptr(), lq, bufs.dk.data_ptr(), lk,
-                                  bufs.dgamma_q.data_ptr(), bufs.dgamma_k.data_ptr(), bufs.workspace.data_ptr(),
+                                  pgq, pgk, bufs.workspace.data_ptr(),
                                   bufs.ws_bytes, _stream()))
     return bufs
 
@@ -1026,9 +1028,9 @@ def linattn(q, k, v, decay, scale: float = 1.0, h0=None, resets=None, lengths=No
     a new trajectory; lengths [B] int32).  Returns the filled buffers (y, h_T, and
     the states that linattn_grad reads)."""
     head, masks, bufs = _linattn_args(q, k, v, decay, h0, resets, lengths, bufs)
-    if not bufs.y.is_contiguous():
-        raise ValueError("bufs.y must be contiguous")
-    _check(load().wm_linattn(*head, scale, *masks, bufs.y.data_ptr(), bufs.h_T.data_ptr(), _ptr(bufs.states),
+    py = _arr("bufs.y", bufs.y, q.dtype, v.shape, q.device)
+    ph = _arr("bufs.h_T", bufs.h_T, torch.float32, (bufs.B, bufs.N, bufs.K, bufs.V), q.device)
+    _check(load().wm_linattn(*head, scale, *masks, py, ph, _ptr(bufs.states),
                              bufs.states_bytes, bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
     return bufs
 
@@ -1044,11 +1046,12 @@ def linattn_grad(q, k, v, decay, dy, scale: float = 1.0, h0=None, dh_T=None, res
     T, B, N, K, V = bufs.T, bufs.B, bufs.N, bufs.K, bufs.V
     yt, yb = _steps("dy", dy, (T, B, N, V), q.dtype, q.device)
     ph = _arr("dh_T", dh_T, torch.float32, (B, N, K, V), q.device, optional=True)
+    p0 = _arr("bufs.dh0", bufs.dh0, torch.float32, (B, N, K, V), q.device)
     out = []  # (they may lie inside wider rows: parts of a projection's gradient)
     for name, t, w in (("bufs.dq", bufs.dq, K), ("bufs.dk", bufs.dk, K), ("bufs.dv", bufs.dv, V)):
         out += (t.data_ptr(), *_steps(name, t, (T, B, N, w), q.dtype, q.device))
     _check(load().wm_linattn_grad(*head, scale, *masks, dy.data_ptr(), yt, yb, ph, bufs.states.data_ptr(),
-                                  bufs.states_bytes, *out, bufs.dh0.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes,
+                                  bufs.states_bytes, *out, p0, bufs.workspace.data_ptr(), bufs.ws_bytes,
                                   _stream()))
     return bufs
 
@@ -1096,7 +1099,10 @@ def glu(x, W, act: str = "silu", bufs: GluBuffers | None = None) -> GluBuffers:
     head = _glu_args(x, W, act, bufs)
     if bufs is None:
         bufs = GluBuffers(head[1], head[2], head[3], x.dtype, x.device)
-    _check(load().wm_glu(*head, bufs.h.data_ptr(), _rows("bufs.h", bufs.h, bufs.F, x.dtype, x.device)[1], _ptr(bufs.saved), bufs.saved_bytes, _stream()))
+    n, lh = _rows("bufs.h", bufs.h, bufs.F, x.dtype, x.device)
+    if n != bufs.rows:
+        raise ValueError(f"bufs.h has {n} rows, x has {bufs.rows}")
+    _check(load().wm_glu(*head, bufs.h.data_ptr(), lh, _ptr(bufs.saved), bufs.saved_bytes, _stream()))
     return bufs
 
 
@@ -1109,9 +1115,12 @@ def glu_grad(x, W, dh, act: str = "silu", bufs: GluBuffers | None = None) -> Glu
     n, ld = _rows("dh", dh, bufs.F, x.dtype, x.device)
     if n != bufs.rows:
         raise ValueError(f"dh has {n} rows, x has {bufs.rows}")
-    lx = _rows("bufs.dx", bufs.dx, bufs.D, x.dtype, x.device)[1]
+    n, lx = _rows("bufs.dx", bufs.dx, bufs.D, x.dtype, x.device)
+    if n != bufs.rows:
+        raise ValueError(f"bufs.dx has {n} rows, x has {bufs.rows}")
+    pw = _arr("bufs.dW", bufs.dW, x.dtype, (2 * bufs.F, bufs.D), x.device)
     _check(load().wm_glu_grad(*head, bufs.saved.data_ptr(), bufs.saved_bytes, dh.data_ptr(), ld, bufs.dx.data_ptr(),
-                              lx, bufs.dW.data_ptr(), bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
+                              lx, pw, bufs.workspace.data_ptr(), bufs.ws_bytes, _stream()))
     return bufs
 
 

@@ -200,6 +200,17 @@ def test_no_rows():
     assert not bool(bufs.dW.any())
 
 
+def test_buffers_of_another_shape():
+    """Arrays that a caller puts in the place of the buffers' own."""
+    x, W, dh = torch.zeros(4, 8, device="cuda"), torch.zeros(12, 8, device="cuda"), torch.zeros(4, 6, device="cuda")
+    for name, shape in (("h", (3, 6)), ("h", (4, 5)), ("dx", (3, 8)), ("dx", (4, 7)), ("dW", (11, 8)), ("dW", (6, 16))):
+        bufs = wm.GluBuffers(4, 8, 6)
+        setattr(bufs, name, torch.zeros(shape, device="cuda"))
+        with pytest.raises(ValueError):
+            wm.glu(x, W, bufs=bufs)
+            wm.glu_grad(x, W, dh, bufs=bufs)
+
+
 def test_refusals():
     x, W, dh = torch.zeros(4, 8, device="cuda"), torch.zeros(12, 8, device="cuda"), torch.zeros(4, 6, device="cuda")
     for bad in (dict(x=x.double()), dict(W=W.bfloat16()), dict(W=W[:11]), dict(W=W[:, :7]), dict(W=W.t().contiguous().t()),

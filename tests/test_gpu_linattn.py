@@ -359,6 +359,20 @@ def test_nothing_to_do():
     wm.linattn_grad(e(5, 0, 2, 8), e(5, 0, 2, 8), e(5, 0, 2, 4), decay, e(5, 0, 2, 4), bufs=bufs)
 
 
+def test_buffers_of_another_shape():
+    """Arrays that a caller puts in the place of the buffers' own."""
+    z = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+    q, v, decay = z(4, 2, 3, 8), z(4, 2, 3, 5), z(3)
+    for name, t in (("y", z(3, 2, 3, 5)), ("y", z(4, 2, 3, 5).bfloat16()), ("y", z(4, 2, 3, 10)[..., :5]), ("h_T", z(2, 3, 5, 8)),
+                    ("h_T", z(1, 3, 8, 5)), ("h_T", z(2, 3, 8, 5).double()), ("dh0", z(2, 3, 5, 8)), ("dh0", z(2, 3, 8, 10)[..., :5]),
+                    ("dq", z(3, 2, 3, 8)), ("dk", z(4, 2, 3, 5)), ("dv", z(4, 2, 3, 8))):
+        bufs = wm.LinattnBuffers(4, 2, 3, 8, 5)
+        setattr(bufs, name, t)
+        with pytest.raises(ValueError):
+            wm.linattn(q, q, v, decay, bufs=bufs)
+            wm.linattn_grad(q, q, v, decay, v, bufs=bufs)
+
+
 def test_refusals():
     z = lambda *s: torch.zeros(s, device="cuda")  # noqa: E731
     q, v, decay = z(4, 2, 3, 8), z(4, 2, 3, 5), z(3)

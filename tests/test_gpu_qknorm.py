@@ -244,6 +244,19 @@ def test_no_rows():
     assert not bool(bufs.dgamma_q.any()) and not bool(bufs.dgamma_k.any())
 
 
+def test_buffers_of_another_shape():
+    """Arrays that a caller puts in the place of the buffers' own."""
+    z = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+    q, k, pos, rot = z(4, 2, 8), z(4, 1, 8), torch.zeros(4, dtype=torch.int32, device="cuda"), wm.Rotary(8)
+    for name, t in (("q", z(3, 2, 8)), ("k", z(4, 2, 8)), ("dq", z(3, 2, 8)), ("dk", z(4, 1, 7)), ("dgamma_q", z(7)),
+                    ("dgamma_k", z(16)[::2]), ("dgamma_k", z(8).double())):
+        bufs = wm.QkNormBuffers(4, 2, 1, 8, grad=True)
+        setattr(bufs, name, t)
+        with pytest.raises(ValueError):
+            wm.qk_norm(q, k, pos, rot, bufs=bufs)
+            wm.qk_norm_grad(q, k, q, k, pos, rot, bufs=bufs)
+
+
 def test_refusals():
     q, k = torch.zeros(4, 2, 8, device="cuda"), torch.zeros(4, 1, 8, device="cuda")
     pos, rot = torch.zeros(4, dtype=torch.int32, device="cuda"), wm.Rotary(8)
