@@ -19,7 +19,7 @@
 //
 // Bound by memory.  Measured: 65536 rows, 16 heads of 64 fp32 91 to 100 us (5.4 to 5.9
 // TB/s), gradient 152 (5.3); 204800 rows, 20 heads of 64 bf16 205 us (5.1 TB/s),
-// gradient 372 (4.2); 4500 rows, 9 heads of 61 fp32 11 and 13 us and 3 for the sums,
+// gradient 330 (4.8); 4500 rows, 9 heads of 61 fp32 10 and 12 us and 4 for the sums,
 // their launches and first loads.
 #include <algorithm>
 
