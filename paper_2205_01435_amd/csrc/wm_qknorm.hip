@@ -19,7 +19,7 @@
 //
 // Bound by memory.  Measured: 65536 rows, 16 heads of 64 fp32 91 to 100 us (5.4 to 5.9
 // TB/s), gradient 152 (5.3); 204800 rows, 20 heads of 64 bf16 205 us (5.1 TB/s),
-// gradient 330 (4.8); 4500 rows, 9 heads of 61 fp32 10 and 12 us and 4 for the sums,
+// gradient 315 to 322 (4.9); 4500 rows, 9 heads of 61 fp32 10 and 12 us and 4 for the sums,
 // their launches and first loads.
 #include <algorithm>
 
@@ -269,8 +269,10 @@ __global__ void __launch_bounds__(kThreads) k_qk_norm(const QkArgs a) {
 // gamma are half the registers of those for both (4500 rows, 9 heads of 61 fp32
 // 19.4 -> 13.5 us).  part [groups][D]: each work-group's sums; where a side has only one,
 // they are the result.
+// Two waves a SIMD for bf16, whose 172 registers three do not admit without spills (204800
+// rows, 20 heads of 64 320 and 307 us).
 template <typename DT, int L, bool WHOLE>
-__global__ void __launch_bounds__(kThreads, WHOLE ? 3 : 2) k_qk_norm_grad(const QkArgs a) {
+__global__ void __launch_bounds__(kThreads, WHOLE && sizeof(DT) == 4 ? 3 : 2) k_qk_norm_grad(const QkArgs a) {
   constexpr int V = Io<DT>::VEC, kSlots = kThreads / L;
   __shared__ float add[2 * V][kThreads + 1];
   const int which = (int)blockIdx.x >= a.groups[0], group = (int)blockIdx.x - (which ? a.groups[0] : 0);
