@@ -565,7 +565,8 @@ wm_status wm_qk_norm_grad(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, i
  *   h0 [B, N, K, V] float32, nullable (0); resets [T, B] uint8, nullable (none);
  *   lengths [B] int32, nullable (T; values outside [0, T] act as clamped).
  *   y [T, B, N, V] in dtype; h_T [B, N, K, V] float32, nullable, may be h0: the
- *   state after the last step (T = 1 with h0 and h_T is the form for acting).
+ *   state after the last step (T = 1 with h0 and h_T is the form for acting; the
+ *   gradient reads h0, so that h_T = h0 is for calls without one).
  *   states               nullable: a 256-byte aligned buffer of
  *                        wm_linattn_states_bytes that receives what
  *                        wm_linattn_grad needs.

@@ -369,8 +369,13 @@ __global__ void __launch_bounds__(16 * kSumRows) k_qk_norm_sum(const QkArgs a) {
   float s = 0.0f;
   if (j < a.D) {
     const float* p = a.part + (long)(which ? a.groups[0] : 0) * a.D + j;
-#pragma unroll 8
-    for (int i = r; i < n; i += kSumRows) s += p[(long)i * a.D];
+    for (int i0 = r; i0 < n; i0 += 16 * kSumRows) {
+      float v[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] = p[(long)min(i0 + k * kSumRows, n - 1) * a.D];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) s += i0 + k * kSumRows < n ? v[k] : 0.0f;
+    }
   }
   sh[r][c] = s;
   __syncthreads();
