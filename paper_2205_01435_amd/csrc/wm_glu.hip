@@ -10,7 +10,7 @@
 // its epilogue and the two factors leave the chip only where the gradient needs
 // them.  Three kernels: large bf16 products in tiles of 256 x 256 straight into LDS;
 // any product in tiles of 128 x 128 through registers; the forward product of up to
-// 64 rows straight from memory.  Where the tiles are too few for the device the sum is
+// 256 rows straight from memory.  Where the tiles are too few for the device the sum is
 // split over work-groups, whose fp32 parts another launch adds in order.
 //
 // fp32 values multiply as three bf16 terms each, six products of them (wm_split.h),
