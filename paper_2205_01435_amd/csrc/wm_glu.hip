@@ -526,7 +526,10 @@ struct Direct {
     long size;
     if constexpr (ACROSS) {
       p += k0 * a.ld + o0;
-      size = min(outs - o0, (long)kBig) * 2;  // of the last row
+      // of the last row, in whole dwords: one that reaches over the end would be read as 0, and
+      // with it an odd row's last value.  The half behind it lies in the row's own 16 bytes and
+      // belongs to an output that does not exist.
+      size = (min(outs - o0, (long)kBig) + 1) / 2 * 4;
     } else if constexpr (GLU) {
       size = ((2 * outs - 1) * a.ld + K) * 2;
     } else {
