@@ -653,7 +653,8 @@ wm_status wm_glu_grad(int32_t dtype, int64_t rows, int32_t D, int32_t F, int32_t
  * "finish", "nll_init", "nll_reduce", "nll_means", "pack", "returns", "adam", the
  * "grad_" kernels of wm_nll_grad, and "embed", "norm", "linrec", "clip", "qk_norm",
  * "linattn" and "glu" with what follows these words in the sequence-core and
- * attending-core operators; "" selects all,
+ * attending-core operators (the products of "glu" with "/" and their kernel:
+ * "glu/few", "glu/128", "glu/256"); "" selects all,
  * NULL turns timing off.  wm_profile_read waits for the recorded events and
  * returns the summed duration (ms) and count of the launches whose name
  * starts with `prefix` (NULL = all); wm_profile_reset forgets them.  Timing

@@ -931,16 +931,21 @@ bool direct(const Operand& a) {
   return (reinterpret_cast<uintptr_t>(a.p) & 15) == 0 && a.ld % 8 == 0 && a.ld <= 1 << 20;
 }
 
+// A product's launch names, by the kernel that it takes.
+struct Names {
+  const char *few, *tiles, *big;
+};
+
 template <typename DT, bool PX, bool QX, bool GLU>
-hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
+hipError_t product(const Names& name, ProductArgs a, hipStream_t s) {
   constexpr int BK = El<DT>::BK;
   const int dtype = sizeof(DT) == 4 ? WM_FP32 : WM_BF16;
   const bool wide = big(dtype, a.M, GLU ? 2 * a.N : a.N, a.K, GLU);
   if constexpr (GLU) {
     if (a.M <= kFewRows) {
       const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 63) / 64)), block(64 * kFewWaves);
-      if (a.M <= 16) return launch(name, k_glu_few<DT, 1>, grid, block, 0, s, a);
-      return launch(name, a.M <= 32 ? k_glu_few<DT, 2> : k_glu_few<DT, 4>, grid, block, 0, s, a);
+      if (a.M <= 16) return launch(name.few, k_glu_few<DT, 1>, grid, block, 0, s, a);
+      return launch(name.few, a.M <= 32 ? k_glu_few<DT, 2> : k_glu_few<DT, 4>, grid, block, 0, s, a);
     }
   }
   if constexpr (sizeof(DT) == 2) {
@@ -951,7 +956,7 @@ hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
       a.splits = GLU ? 1 : splits_of_big(a.M, a.N, a.K);
       a.per = ((a.K + a.splits - 1) / a.splits + kBigK - 1) / kBigK * kBigK;
       a.splits = (int)((a.K + a.per - 1) / a.per);  // none empty
-      const hipError_t e = launch(name, k_product_big<PX, QX, GLU>, dim3(kBigGroups), dim3(kBigThreads), 0, s, a);
+      const hipError_t e = launch(name.big, k_product_big<PX, QX, GLU>, dim3(kBigGroups), dim3(kBigThreads), 0, s, a);
       if (e != hipSuccess || a.splits == 1) return e;
       return launch("glu_sum", k_product_sum<DT>, dim3((unsigned)((a.M * a.N + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a);
     }
@@ -965,9 +970,9 @@ hipError_t product(const char* name, ProductArgs a, hipStream_t s) {
   hipError_t e;
   if constexpr (sizeof(DT) == 4) {
     const bool near = a.P.ld <= 1 << 20 && a.Q.ld <= 1 << 20 && (!GLU || 2 * a.N * a.P.ld < (1L << 29));
-    e = launch(name, near ? k_product<DT, PX, QX, GLU, true> : k_product<DT, PX, QX, GLU, false>, grid, dim3(kThreads), 0, s, a);
+    e = launch(name.tiles, near ? k_product<DT, PX, QX, GLU, true> : k_product<DT, PX, QX, GLU, false>, grid, dim3(kThreads), 0, s, a);
   } else {
-    e = launch(name, k_product<DT, PX, QX, GLU, false>, grid, dim3(kThreads), 0, s, a);
+    e = launch(name.tiles, k_product<DT, PX, QX, GLU, false>, grid, dim3(kThreads), 0, s, a);
   }
   if (e != hipSuccess || a.splits == 1) return e;
   return launch("glu_sum", k_product_sum<DT>, dim3((unsigned)((a.M * a.N + kThreads - 1) / kThreads)), dim3(kThreads), 0, s, a);
@@ -985,7 +990,8 @@ size_t part_bytes(int dtype, long M, long N, long K) {
 
 hipError_t launch_glu(int dtype, const GluArgs& a, hipStream_t s) {
   const ProductArgs p{{a.W, a.D}, {a.x, a.x_ld}, a.rows, a.F, a.D, a.h, a.h_ld, a.saved, a.act, nullptr, 1, 0, 0, 0};
-  return dtype == WM_FP32 ? product<float, false, false, true>("glu", p, s) : product<bf16_t, false, false, true>("glu", p, s);
+  const Names name{"glu/few", "glu/128", "glu/256"};
+  return dtype == WM_FP32 ? product<float, false, false, true>(name, p, s) : product<bf16_t, false, false, true>(name, p, s);
 }
 
 size_t glu_saved(int dtype, long rows, int F) {
@@ -1009,11 +1015,11 @@ hipError_t launch_glu_grad(int dtype, const GluGradArgs& a, hipStream_t s) {
                  dim3(kThreads), 0, s, a, dpre);
       if (e != hipSuccess) return e;
       const ProductArgs dx{{a.W, a.D}, {dpre, 2L * a.F}, a.rows, a.D, 2L * a.F, a.dx, a.dx_ld, nullptr, 0, part, 1, 0, 0, 0};
-      if ((e = product<DT, true, false, false>("glu_dx", dx, s)) != hipSuccess) return e;
+      if ((e = product<DT, true, false, false>({nullptr, "glu_dx/128", "glu_dx/256"}, dx, s)) != hipSuccess) return e;
     }
     if (!a.dW) return e;
     const ProductArgs dw{{a.x, a.x_ld}, {dpre, 2L * a.F}, 2L * a.F, a.D, a.rows, a.dW, a.D, nullptr, 0, part, 1, 0, 0, 0};
-    return product<DT, true, true, false>("glu_dw", dw, s);
+    return product<DT, true, true, false>({nullptr, "glu_dw/128", "glu_dw/256"}, dw, s);
   };
   return dtype == WM_FP32 ? run(0.0f) : run(bf16_t());
 }
