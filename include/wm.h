@@ -572,10 +572,11 @@ wm_status wm_qk_norm_grad(int32_t dtype, int64_t rows, int32_t Hq, int32_t Hk, i
  *                        wm_linattn_grad needs.
  *   workspace            of wm_linattn_workspace_bytes, also for the gradient; both
  *                        0 bytes where the call does not split the time axis.
- * The steps of a sequence are taken 64 at a time, from its first, by matrix
- * products: a value of a head that is not finite can make every output of that
- * sequence and head in the same 64 steps not finite, earlier steps and other
- * trajectories included, and through the state those after it up to a reset.
+ * A value that is not finite reaches what the recurrence takes it into and nothing
+ * else: no earlier step (in the gradient: no later one), no other trajectory,
+ * sequence or head.  Results that it does reach may be NaN in the place of an
+ * infinity, and segments of the time axis that hold NaN are taken a second time, step
+ * by step: such a call takes longer.
  * K and V in 1 .. 128; scale finite; T B, T B N K, T B N V and B N K V at most
  * 2^31 - 1, B N at most 2^22.  B = 0 is a no-op; T = 0 gives h_T = h0.
  */

@@ -23,6 +23,9 @@
 // it.  The forward call's entering states are kept for dq.  A single step is a
 // kernel of its own, which streams the states.
 //
+// The products take a source that a row does not see as 0 times its value, which is NaN
+// where that is not finite.  What comes out as NaN is taken again step by step (by_steps).
+//
 // Precision: fp32 values multiply on the fp32 matrix instructions.  bf16 values
 // enter exactly; the 64 x 64 weights and the state that meets the rows are held as
 // two bf16 terms each (2^-17 of their value is left out, against the 2^-9 of the
@@ -321,14 +324,24 @@ struct State {
         for (int e = 0; e < 4; ++e)
           S[i][k][e] = p && row(i) + e < ka && col(k) < kc ? p[(long)(row(i) + e) * st_a + (long)col(k) * st_c] : 0.0f;
   }
-  __device__ __forceinline__ void save(float* p, int ka, int kc, int st_a, int st_c) const {
+  // `finite`: leaves what p holds in the place of NaN
+  __device__ __forceinline__ void save(float* p, int ka, int kc, int st_a, int st_c, bool finite) const {
 #pragma unroll
     for (int i = 0; i < KAB; ++i)
 #pragma unroll
       for (int k = 0; k < KCB; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (row(i) + e < ka && col(k) < kc) p[(long)(row(i) + e) * st_a + (long)col(k) * st_c] = S[i][k][e];
+          if (row(i) + e < ka && col(k) < kc && !(finite && S[i][k][e] != S[i][k][e]))
+            p[(long)(row(i) + e) * st_a + (long)col(k) * st_c] = S[i][k][e];
+  }
+  __device__ __forceinline__ bool nan() const {
+    bool n = false;
+#pragma unroll
+    for (int i = 0; i < KAB; ++i)
+#pragma unroll
+      for (int k = 0; k < KCB; ++k) n |= any_nan(S[i][k]);
+    return n;
   }
   __device__ __forceinline__ void stage(DT* st) const {
 #pragma unroll
@@ -536,10 +549,93 @@ __device__ __forceinline__ uint32_t reset_of(const MixArgs& a, int b, int t0, in
   return a.resets && lane < live ? a.resets[(long)(t0 + lane) * a.B + b] : 0;
 }
 
+// Whether `v` holds in any of the work-group's threads (`words`: four, which nothing else uses).
+__device__ __forceinline__ bool in_any(bool v, int* words) {
+  const bool any = __any(v);
+  if ((threadIdx.x & 63) == 0) words[threadIdx.x >> 6] = any;
+  __syncthreads();
+  return (words[0] | words[1] | words[2] | words[3]) != 0;
+}
+
+// The launch's arguments, loaded again, for code that hardly ever runs: the sweeps keep
+// no registers for it.  `at`: which bytes of them.
+template <typename T>
+__device__ __forceinline__ const T& argument(int at) {
+  auto p = (const __attribute__((address_space(4))) char*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const T*)(p + at);
+}
+
+// A masked source counts as 0 times its value in the products, which is NaN where the
+// value, or its product with the row, is not finite.  A segment that comes out with NaN
+// is therefore taken a second time, step by step as the recurrence says, and what this
+// gives replaces NaN, so that nothing reaches a step on the other side of its own or
+// another trajectory.  Finite results stay as they are.
+//   F = (state that enters) + upd B_t C_t^T, out_t = inter A_t . F;
+// columns [ct, ct + cols) of C and the output; s0, s1: the state that enters and the one
+// that leaves, [ka][kc] with strides st_a and st_c.  Sixteen columns at a time, sixteen
+// threads each, up to 16 R rows of the state: little code, which the sweeps have beside
+// their own (three times as much of it, and the gradient of T 128, B 512, 8 heads of 64
+// fp32 took 388 us in place of 361).  A step takes some 2 us: with NaN in every v that
+// call takes 10.6 ms in place of 0.5.
+template <typename DT, int R, bool REV, bool OUT>
+__device__ __forceinline__ void by_steps(const MixArgs& a, long part, const SeqView& va, const SeqView& vb, const SeqView& vc,
+                                         const SeqView& vo, int ka, int kc, int ct, int cols, const float* s0, float* s1, int st_a,
+                                         int st_c, float* sum) {
+  asm volatile("" : "+s"(part));
+  const Place at(a, part);
+  auto line = [&](const SeqView& v, int width) { return reinterpret_cast<DT*>(const_cast<void*>(v.p)) + (long)at.b * v.b + (long)at.n * width; };
+  const DT *const A = line(va, ka), *const B = line(vb, ka), *const C = line(vc, kc);
+  DT* const out = line(vo, kc);
+  const float decay = fminf(fmaxf(a.decay[at.n], 0.0f), 1.0f);
+  const int begin = at.first * kChunk, steps = min((int)min((long)at.last * kChunk, (long)a.T), at.len) - begin;
+  const int row0 = threadIdx.x / 16 * R;
+#pragma unroll 1
+  for (int c0 = 0; c0 < cols; c0 += 16) {
+    const int in = c0 + threadIdx.x % 16, col = ct + min(in, cols - 1);  // (those past the end do the last one's work)
+    float S[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) S[r] = s0 && row0 + r < ka ? s0[(long)(row0 + r) * st_a + (long)col * st_c] : 0.0f;
+#pragma unroll 1
+    for (int i = 0; i < steps; ++i) {
+      const long t = REV ? begin + steps - 1 - i : begin + i;
+      const bool start = a.resets && a.resets[t * a.B + at.b] != 0;
+      const DT *const x = A + t * va.t, *const z = B + t * vb.t;
+      const float c = a.s_upd * DType<DT>::load(C + t * vc.t, col);
+      float y = 0.0f;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (row0 + r >= ka) break;
+        const float b = DType<DT>::load(z, row0 + r) * c;
+        S[r] = REV ? S[r] + b : start ? b : fmaf(decay, S[r], b);
+        if (OUT) y = fmaf(DType<DT>::load(x, row0 + r), S[r], y);
+        if (REV) S[r] = start ? 0.0f : decay * S[r];
+      }
+      if constexpr (OUT) {
+        __syncthreads();
+        sum[threadIdx.x] = y;
+        __syncthreads();
+        if (threadIdx.x == in - c0 && in < cols) {
+          for (int g = 16; g < kThreads; g += 16) y += sum[g + threadIdx.x];
+          DT* const p = out + t * vo.t;
+          const float old = DType<DT>::load(p, col);
+          if (old != old) DType<DT>::store(p, col, a.s_inter * y);
+        }
+      }
+    }
+    if (s1 && in < cols) {
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (row0 + r < ka) s1[(long)(row0 + r) * st_a + (long)col * st_c] = S[r];
+    }
+  }
+  __syncthreads();
+}
+
 // One sweep over a segment's chunks: the outputs of columns [ct, ct + KC), or, STATE,
 // the segment's own sum of the state alone.
 template <typename DT, int KA, int KC, bool REV, bool STATE, bool FAST>
-__device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct, DT* bl, DT* cl, DT* st) {
+__device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct, DT* bl, DT* cl, DT* st) {  // a: the launch's first
   constexpr int PC = KC + Tile<DT>::PAD;
   const int w = threadIdx.x >> 6, lane0 = threadIdx.x & 63;
   const int wcols = min(KC, a.kc - ct);
@@ -562,6 +658,7 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
       rows.template load<FAST>(ra, ra.at(t0, live), r, g);
     }
   };
+  __shared__ int words[4];
   const int steps = at.last - at.first;
   if (steps > 0) {
     load(REV ? at.last - 1 : at.first);
@@ -572,6 +669,7 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
   S.load(s0 ? s0 + (long)ct * a.st_c : nullptr, a.ka, wcols, a.st_a, a.st_c);
   Weights<DT, REV> wt;
   float hold = 1.0f;
+  bool nan = false;
   for (int step = 0; step < steps; ++step) {
     const int c = REV ? at.last - 1 - step : at.first + step, t0 = c * kChunk;
     const int live = min(at.len - t0, kChunk);  // steps of the chunk inside the sequence, 0 or less for none
@@ -612,6 +710,7 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
             const f32x4 in = entered<DT, KA, KC>(st, rows, cb + i, g, j16), own = P.template times<PC>(cl, cb + i, w, g, j16, live);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[i][e] = r < live ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+            nan |= __builtin_isunordered(v[i][0], v[i][1]) || __builtin_isunordered(v[i][2], v[i][3]);
           }
           store_pair(ro, oc, r, cb, g, v[0], v[1]);
         }
@@ -624,7 +723,14 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
     S.template take<REV>(bl, cl, wt, starts, live, lane, la, a.s_upd);
   }
   float* const s1 = STATE ? a.seg + at.part * a.ka * a.kc : a.seg || !a.s1 ? nullptr : a.s1 + at.bn * a.ka * a.kc;
-  if (s1) S.save(s1 + (long)ct * a.st_c, a.ka, wcols, a.st_a, a.st_c);
+  if (s1) nan |= S.nan();
+  const bool again = in_any(nan, words);
+  if (__builtin_expect(again, 0)) {
+    const MixArgs& b = argument<MixArgs>(0);
+    by_steps<DT, KA / 16, REV, !STATE>(b, at.part, b.a, b.b, b.c, b.out, b.ka, b.kc, ct, wcols, s0, s1, b.st_a, b.st_c,
+                                       reinterpret_cast<float*>(bl));
+  }
+  if (s1) S.save(s1 + (long)ct * a.st_c, a.ka, wcols, a.st_a, a.st_c, again);
   if constexpr (STATE) {
     if (threadIdx.x == 0 && ct == 0) a.hold[at.part] = hold;
   }
@@ -632,9 +738,11 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
 
 // Waves a SIMD that the registers are to admit: as many as LDS does, fp32 rows that
 // are not FAST one less, and their few spills with it (bf16 gains by the third wave:
-// T 128, B 512, 8 heads of 50 and 37 with two 95 and 252 us, with three 81 and 225).
+// T 128, B 512, 8 heads of 50 and 37 with two 95 and 252 us, with three 81 and 225);
+// four for heads of 32 (T 512, B 256, 8 heads fp32, gradient 388 and 366 us).
 constexpr int waves(int size, int ka, int kc, bool fast) {
   if (ka > 64) return size == 4 ? (kc > 32 ? 1 : 2) : (kc > 32 ? 2 : 3 - !fast);
+  if (ka <= 32 && kc <= 32 && fast) return 4;
   return size == 4 ? 3 - !fast : 3;
 }
 
@@ -673,13 +781,16 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
     k.template load<FAST>(rk, rk.at(t0, live), r, g);
     v.template load<FAST>(rv, rv.at(t0, live), r, g);
   };
+  __shared__ int words[4];
   if (at.last > at.first) {
     load(at.last - 1);
     load_rows(at.last - 1);
   }
   State<DT, KP, VP> S;
-  S.load(a.seg ? a.seg + at.part * a.ka * a.kc : a.s0 ? a.s0 + at.bn * a.ka * a.kc : nullptr, a.ka, a.kc, a.st_a, a.st_c);
+  const float* const s0 = a.seg ? a.seg + at.part * a.ka * a.kc : a.s0 ? a.s0 + at.bn * a.ka * a.kc : nullptr;
+  S.load(s0, a.ka, a.kc, a.st_a, a.st_c);
   Weights<DT, true> wt;
+  bool nan = false;
   for (int c = at.last - 1; c >= at.first; --c) {
     const int t0 = c * kChunk, live = min(at.len - t0, kChunk);
     const uint64_t starts = __ballot(reset != 0);
@@ -718,6 +829,7 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
             const f32x4 in = entered<DT, KP, VP>(st, k, cb + i, g, j16), own = P.template times<PV>(dl, cb + i, w, g, j16, live);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[i][e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+            nan |= __builtin_isunordered(x[i][0], x[i][1]) || __builtin_isunordered(x[i][2], x[i][3]);
           }
           store_pair(ov, cv, r, cb, g, x[0], x[1]);
         }
@@ -734,6 +846,7 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
                         own = P.template times<PK>(ql, kb + i, w, g, j16, live);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[i][e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
+            nan |= __builtin_isunordered(x[i][0], x[i][1]) || __builtin_isunordered(x[i][2], x[i][3]);
           }
           store_pair(ok, ck, r, kb, g, x[0], x[1]);
         }
@@ -745,12 +858,27 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
     }
     if (live > 0) S.template take<true>(ql, dl, wt, starts, live, lane, la, a.s_upd);
   }
-  if (!a.seg && a.s1) S.save(a.s1 + at.bn * a.ka * a.kc, a.ka, a.kc, a.st_a, a.st_c);
+  float* const s1 = a.seg || !a.s1 ? nullptr : a.s1 + at.bn * a.ka * a.kc;
+  if (s1) nan |= S.nan();
+  const bool again = in_any(nan, words);
+  if (__builtin_expect(again, 0)) {
+    const MixArgs& b = argument<MixArgs>(sizeof(MixArgs));
+#pragma unroll 1
+    for (int of_k = 1; of_k >= 0; --of_k) {
+      const SeqView &va = of_k ? b.v : b.a, &vb = of_k ? b.c : b.b, &vc = of_k ? b.b : b.c,
+                    &vo = of_k ? argument<SeqView>(2 * sizeof(MixArgs)) : b.out;
+      const int ka = of_k ? b.kc : b.ka, kc = of_k ? b.ka : b.kc;
+      by_steps<DT, (KP > VP ? KP : VP) / 16, true, true>(b, at.part, va, vb, vc, vo, ka, kc, 0, kc, s0, of_k ? nullptr : s1,
+                                                         of_k ? b.st_c : b.st_a, of_k ? b.st_a : b.st_c, reinterpret_cast<float*>(ql));
+    }
+  }
+  if (s1) S.save(s1, a.ka, a.kc, a.st_a, a.st_c, again);
 }
 
 // All three gradients of heads up to 64 wide: the forward sweep for dq, then the
 // reverse one for dk and dv, which finds k, v and dy in the caches where the
-// segment is short; or, `apart`, each in a work-group of its own.
+// segment is short; or, `apart`, each in a work-group of its own.  (The arguments stay in
+// this order: by_steps finds them by their places.)
 template <typename DT, int KP, int VP, bool FAST>
 __global__ void __launch_bounds__(kThreads, waves(sizeof(DT), KP, VP, FAST)) k_mix_grad(const MixArgs q, const MixArgs v, const SeqView dk,
                                                                                         int apart) {
