@@ -1026,7 +1026,8 @@ def linattn(q, k, v, decay, scale: float = 1.0, h0=None, resets=None, lengths=No
     y_t = scale S_t^T q_t for every head over ``q``, ``k`` [T, B, N, K] and
     ``v`` [T, B, N, V] (decay [N] float32; resets [T, B] uint8: the step starts
     a new trajectory; lengths [B] int32).  Returns the filled buffers (y, h_T, and
-    the states that linattn_grad reads)."""
+    the states that linattn_grad reads; buffers made with grad=False hold the outputs
+    alone)."""
     head, masks, bufs = _linattn_args(q, k, v, decay, h0, resets, lengths, bufs)
     py = _arr("bufs.y", bufs.y, q.dtype, v.shape, q.device)
     ph = _arr("bufs.h_T", bufs.h_T, torch.float32, (bufs.B, bufs.N, bufs.K, bufs.V), q.device)
@@ -1095,7 +1096,7 @@ def _glu_args(x, W, act, bufs):
 def glu(x, W, act: str = "silu", bufs: GluBuffers | None = None) -> GluBuffers:
     """Launch wm_glu on the current stream: act(x W[:F]^T) * (x W[F:]^T) for the
     rows of ``x`` [..., D] and ``W`` [2F, D]; returns the filled buffers (h, and
-    what glu_grad reads)."""
+    what glu_grad reads, 2F values a row; buffers made with grad=False hold h alone)."""
     head = _glu_args(x, W, act, bufs)
     if bufs is None:
         bufs = GluBuffers(head[1], head[2], head[3], x.dtype, x.device)

@@ -669,7 +669,7 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
   S.load(s0 ? s0 + (long)ct * a.st_c : nullptr, a.ka, wcols, a.st_a, a.st_c);
   Weights<DT, REV> wt;
   float hold = 1.0f;
-  bool nan = false;
+  float all = 0.0f;  // the outputs' sum, which is not finite where one of them is not
   for (int step = 0; step < steps; ++step) {
     const int c = REV ? at.last - 1 - step : at.first + step, t0 = c * kChunk;
     const int live = min(at.len - t0, kChunk);  // steps of the chunk inside the sequence, 0 or less for none
@@ -710,7 +710,7 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
             const f32x4 in = entered<DT, KA, KC>(st, rows, cb + i, g, j16), own = P.template times<PC>(cl, cb + i, w, g, j16, live);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[i][e] = r < live ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
-            nan |= __builtin_isunordered(v[i][0], v[i][1]) || __builtin_isunordered(v[i][2], v[i][3]);
+            all += (v[i][0] + v[i][1]) + (v[i][2] + v[i][3]);
           }
           store_pair(ro, oc, r, cb, g, v[0], v[1]);
         }
@@ -723,8 +723,7 @@ __device__ __forceinline__ void sweep(const MixArgs& a, const Place& at, int ct,
     S.template take<REV>(bl, cl, wt, starts, live, lane, la, a.s_upd);
   }
   float* const s1 = STATE ? a.seg + at.part * a.ka * a.kc : a.seg || !a.s1 ? nullptr : a.s1 + at.bn * a.ka * a.kc;
-  if (s1) nan |= S.nan();
-  const bool again = in_any(nan, words);
+  const bool again = in_any(all - all != 0.0f || (s1 && S.nan()), words);
   if (__builtin_expect(again, 0)) {
     const MixArgs& b = argument<MixArgs>(0);
     by_steps<DT, KA / 16, REV, !STATE>(b, at.part, b.a, b.b, b.c, b.out, b.ka, b.kc, ct, wcols, s0, s1, b.st_a, b.st_c,
@@ -790,7 +789,7 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
   const float* const s0 = a.seg ? a.seg + at.part * a.ka * a.kc : a.s0 ? a.s0 + at.bn * a.ka * a.kc : nullptr;
   S.load(s0, a.ka, a.kc, a.st_a, a.st_c);
   Weights<DT, true> wt;
-  bool nan = false;
+  float all = 0.0f;  // the outputs' sum, which is not finite where one of them is not
   for (int c = at.last - 1; c >= at.first; --c) {
     const int t0 = c * kChunk, live = min(at.len - t0, kChunk);
     const uint64_t starts = __ballot(reset != 0);
@@ -829,7 +828,7 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
             const f32x4 in = entered<DT, KP, VP>(st, k, cb + i, g, j16), own = P.template times<PV>(dl, cb + i, w, g, j16, live);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[i][e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
-            nan |= __builtin_isunordered(x[i][0], x[i][1]) || __builtin_isunordered(x[i][2], x[i][3]);
+            all += (x[i][0] + x[i][1]) + (x[i][2] + x[i][3]);
           }
           store_pair(ov, cv, r, cb, g, x[0], x[1]);
         }
@@ -846,7 +845,7 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
                         own = P.template times<PK>(ql, kb + i, w, g, j16, live);
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[i][e] = on ? own[e] + (mask.entered ? win * in[e] : 0.0f) : 0.0f;
-            nan |= __builtin_isunordered(x[i][0], x[i][1]) || __builtin_isunordered(x[i][2], x[i][3]);
+            all += (x[i][0] + x[i][1]) + (x[i][2] + x[i][3]);
           }
           store_pair(ok, ck, r, kb, g, x[0], x[1]);
         }
@@ -859,8 +858,7 @@ __device__ __forceinline__ void sweep_back(const MixArgs& a, const SeqView& dk, 
     if (live > 0) S.template take<true>(ql, dl, wt, starts, live, lane, la, a.s_upd);
   }
   float* const s1 = a.seg || !a.s1 ? nullptr : a.s1 + at.bn * a.ka * a.kc;
-  if (s1) nan |= S.nan();
-  const bool again = in_any(nan, words);
+  const bool again = in_any(all - all != 0.0f || (s1 && S.nan()), words);
   if (__builtin_expect(again, 0)) {
     const MixArgs& b = argument<MixArgs>(sizeof(MixArgs));
 #pragma unroll 1
