@@ -18,13 +18,16 @@
 // errors below theirs.
 //
 // Bound by the matrix unit from some hundred rows on, and there by power: the clock
-// falls as instructions are saved.  Measured, 65536 rows, D 1024, F 2816 bf16: outputs
-// and what is saved 843 to 893 us (850 to 900 TFLOP/s), dg | du 462 (4.8 TB/s), dx 611
-// to 662 (1140 to 1240), dW 692 to 756 (1000 to 1090) and 26 for its sums; a library's
-// plain products of these sizes took 703, 727 and 1067 us.  D 512, F 1408 fp32: 1069 to
-// 1129, 360, 959 to 1010 and 1125 to 1206 us (157 to 197 TFLOP/s; the library's 1455,
-// 1495 and 2257).  16 rows, D 1024, F 2816 bf16 5.4 us, W at 2.1 TB/s: launch and first
-// loads.
+// falls as instructions are saved.  Measured, the least and the mean of twelve calls one
+// after the other, 65536 rows, D 1024, F 2816 bf16: outputs and what is saved 860 and 907
+// us (880 and 830 TFLOP/s), dg | du 455 and 461 (4.8 TB/s), dx 615 and 683 (1230 and
+// 1110), dW 703 and 766 (1080 and 990) and 32 for its sums; a library's plain products of
+// these sizes took 703, 727 and 1067 us.  D 512, F 1408 fp32: 1067 and 1152, 358 and 367,
+// 963 and 1033, 1144 and 1241 us (152 to 196 TFLOP/s; the library's 1455, 1495 and 2257).
+// 16 rows, D 1024, F 2816 bf16 5.4 us, W at 2.1 TB/s: launch and first loads.
+//
+// Registers: the large tiles of dx spill 12, and fp32 products of rows more than 2^20
+// elements apart up to 62; the others none.
 #include <algorithm>
 
 #include "../../include/wm.h"

@@ -33,11 +33,15 @@
 // state, as three (2^-24).  All sums are fp32.
 //
 // Measured: one step of 256 x 8 states of 64 x 64 12 us (5.7 TB/s, part of it from the
-// caches).  T 128, B 512, 8 heads of 64 fp32, padded: 157 us, gradient 365; the matrix
+// caches).  The least and the mean of twelve calls one after the other: T 128, B 512, 8
+// heads of 64 fp32, padded, 151 and 160 us, gradient 367 and 397; the matrix
 // unit is busy 40 % and the vector unit 30 % of it, the rest is waiting at three
-// work-groups a CU.  T 32768, 16 heads of 64 bf16: states 37, through the segments 7,
-// outputs 62 us; gradient 31, 8 and 151; two thirds of it the vector unit's splits,
-// weights and addresses.
+// work-groups a CU.  T 32768, 16 heads of 64 bf16: states 28 and 30, through the segments
+// 7, outputs 61 and 66 us; gradient 30 and 32, 8, 152 and 166; two thirds of it the vector
+// unit's splits, weights and addresses.  Heads of 128, whose gradient takes three sweeps, T
+// 128, B 512, 8 heads: bf16 273 us, with gradient 1085 (64: 100 and 304); fp32, one wave a
+// SIMD by its 85 KB of LDS, 906 and 3642 (181 and 638).  T 32768, 16 heads of 128: 290 and
+// 976, fp32 930 and 3305 (64: 89 and 274, 247 and 756).
 #include <algorithm>
 
 #include "../../include/wm.h"

@@ -17,10 +17,11 @@
 // gammas in registers; a work-group leaves one row of partial sums, which a second
 // launch adds in order.
 //
-// Bound by memory.  Measured: 65536 rows, 16 heads of 64 fp32 91 to 100 us (5.4 to 5.9
-// TB/s), gradient 152 (5.3); 204800 rows, 20 heads of 64 bf16 205 us (5.1 TB/s),
-// gradient 315 to 322 (4.9); 4500 rows, 9 heads of 61 fp32 10 and 12 us and 4 for the sums,
-// their launches and first loads.
+// Bound by memory.  Measured, the least and the mean of twelve calls one after the other:
+// 65536 rows, 16 heads of 64 fp32 93 and 99 us (5.8 and 5.4 TB/s), gradient 151 and 155
+// (5.3 and 5.2); 204800 rows, 20 heads of 64 bf16 204 and 215 us (5.1 and 4.9 TB/s),
+// gradient 312 and 326 (5.0 and 4.8); 4500 rows, 9 heads of 61 fp32 10 and 12 us and 4 for
+// the sums, their launches and first loads.
 #include <algorithm>
 
 #include "../../include/wm.h"
